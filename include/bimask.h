@@ -76,7 +76,8 @@ uint64_t bimask_launch_count(void);
  * reduction length K (K = J for the forward operand, K = I for the backward one). */
 size_t bimask_hw_meta_bytes(int rows, int K);
 
-/* Bytes of scratch (`ws`) large enough for every call below on a layer of this size. */
+/* Bytes of scratch (`ws`) large enough for every call below on a layer of this size, except those that name a size
+ * query of their own. */
 size_t bimask_workspace_bytes(int T, int I, int J, int P);
 
 /* Eq. 4 + packing.  Forward mask: in every row, every aligned block of M along J keeps its N
@@ -176,6 +177,53 @@ int bimask_spmm_dgrad(const uint16_t* dY, const int32_t* perm, const uint16_t* v
  * unmasked, fp32 I x J. */
 int bimask_wgrad(const uint16_t* dY, const uint16_t* X, int T, int I, int J, float* dW,
                  void* ws, size_t ws_bytes, int32_t* status_word, void* stream);
+
+/* ---- A linear layer around the sparse product: epilogue, its gradient, 8-bit activation checkpoints ----
+ *
+ * What a network has between two sparse layers, and what it must keep of them until the backward pass.  (No counterpart
+ * in the paper: its layers are bare products.)  A layer is  Z = X (B.W)^T + b,  Y = act(Z) + R;  its backward pass is
+ * bimask_act_bwd (dZ, db; the residual's gradient is dY itself), then bimask_spmm_dgrad and bimask_wgrad or
+ * bimask_wgrad_ckpt with dZ in the place of dY.
+ *
+ * Activations:
+ *   NONE z;  RELU max(z, 0);  GELU z Phi(z);  GELU_TANH z (1 + tanh(c (z + 0.044715 z^3))) / 2, c = sqrt(2 / pi);
+ *   SILU z / (1 + e^-z).  Evaluated in fp32 to about 1e-6; the slope of RELU at 0 is 0.
+ *
+ * Checkpoint of a T x C matrix (C % 32 == 0): q, T x C signed bytes, and s, T x C/32 bytes.  For 32 consecutive channels
+ * of a token, p = 2^(s - 127) is the smallest power of two not below 2^-126 with max |x| <= 127 p, and q = x / p rounded
+ * to the nearest integer (ties to even), so |q| <= 127; the value it stands for, q p, is exact in bf16.  A block with a
+ * value whose rounding up to bf16 is not finite gets s = 255 and stands for NaN throughout (its q is unspecified); s = 0
+ * is never written.  33 bytes for 64 of bf16; the error of a value is at most p / 2 <= max |x| / 127. */
+enum { BIMASK_ACT_NONE = 0, BIMASK_ACT_RELU = 1, BIMASK_ACT_GELU = 2, BIMASK_ACT_GELU_TANH = 3, BIMASK_ACT_SILU = 4 };
+
+/* Bytes of scratch for bimask_act_bwd on T x I activations and for bimask_wgrad_ckpt on a T, I, J layer. */
+size_t bimask_linear_workspace_bytes(int T, int I, int J);
+
+/* Y[t, i] = act(sum_j X[t, j] (B * W)[i, j] + bias[i]) + R[t, i], all of it in fp32 before the one rounding to bf16.
+ * The operand is that of bimask_spmm_fwd (hw_meta_f == NULL: the dense masked operand).
+ *   bias  I fp32, or NULL;   R  T x I bf16, or NULL; may be Y itself
+ *   Zq, Zs  out, both or neither: the checkpoint of the pre-activation sum + bias (taken from its fp32 value) */
+int bimask_linear_fwd(const uint16_t* X, const uint16_t* vals_f, const void* hw_meta_f, const float* bias_or_null, int act,
+                      const uint16_t* R_or_null, int T, int I, int J, uint16_t* Y, int8_t* Zq_or_null, uint8_t* Zs_or_null,
+                      int32_t* status_word, void* stream);
+
+/* Gradient through activation and bias: dZ = dY * act'(Z) (T x C bf16, rounded once) and dbias[c] = sum_t of the same
+ * values before rounding (fp32, added in an order that depends on the sizes alone).  Z is a checkpoint.
+ *   Zq, Zs  may be NULL with BIMASK_ACT_NONE
+ *   dZ      out, or NULL (bias gradient only); may be dY itself
+ *   dbias   out, C fp32, or NULL;  ws: scratch of bimask_linear_workspace_bytes(T, C, 32) bytes or more, needed with dbias */
+int bimask_act_bwd(const uint16_t* dY, const int8_t* Zq, const uint8_t* Zs, int act, int T, int C, uint16_t* dZ_or_null,
+                   float* dbias_or_null, void* ws, size_t ws_bytes, void* stream);
+
+/* Checkpoint of X (T x C bf16), and back: X = act of the values (BIMASK_ACT_NONE: the values themselves, exactly). */
+int bimask_ckpt_pack(const uint16_t* X, int T, int C, int8_t* q, uint8_t* s, void* stream);
+int bimask_ckpt_unpack(const int8_t* q, const uint8_t* s, int act, int T, int C, uint16_t* X, void* stream);
+
+/* bimask_wgrad with the input as a checkpoint: dW[i, j] = sum_t dY[t, i] x[t, j], x the values of (Xq, Xs), dense, fp32.
+ * No more than 8192 tokens are added up inside the tensor core, whose fp32 sums do not round to nearest; longer sums are
+ * put together in fp32.   ws: scratch of bimask_linear_workspace_bytes(T, I, J) bytes */
+int bimask_wgrad_ckpt(const uint16_t* dY, const int8_t* Xq, const uint8_t* Xs, int T, int I, int J, float* dW, void* ws,
+                      size_t ws_bytes, int32_t* status_word, void* stream);
 
 /* One iteration of Alg. 1 for one layer (without the optimizer update): fwd mask + pack, sparse
  * forward, [search if do_search], bwd mask + pack, sparse input gradient, dense weight

@@ -22,7 +22,9 @@ EXPORTS = ("bimask_last_error", "bimask_launch_count", "bimask_hw_meta_bytes", "
            "bimask_check_perms", "bimask_debug_wait_probe", "bimask_perm_search_static",
            "bimask_perm_search_static_max_entries", "bimask_sgd_fwd_mask", "bimask_train_step",
            "bimask_bwd_mask_criterion", "bimask_conv_workspace_bytes", "bimask_conv_layer_step",
-           "bimask_refine_workspace_bytes", "bimask_perm_refine", "bimask_debug_gen_candidates", "bimask_debug_status")
+           "bimask_refine_workspace_bytes", "bimask_perm_refine", "bimask_debug_gen_candidates", "bimask_debug_status",
+           "bimask_linear_workspace_bytes", "bimask_linear_fwd", "bimask_act_bwd", "bimask_ckpt_pack", "bimask_ckpt_unpack",
+           "bimask_wgrad_ckpt")
 
 
 class BimaskError(RuntimeError):
@@ -99,6 +101,16 @@ def lib() -> ctypes.CDLL:
         L.bimask_sgd_fwd_mask.argtypes = [c_void_p, c_void_p, c_void_p, c_int, c_int, c_int, c_int, c_float, c_float,
                                           c_float, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p]
         L.bimask_train_step.argtypes = [POINTER(TrainArgs)]
+        L.bimask_linear_workspace_bytes.restype = c_size_t
+        L.bimask_linear_workspace_bytes.argtypes = [c_int, c_int, c_int]
+        L.bimask_linear_fwd.argtypes = [c_void_p, c_void_p, c_void_p, c_void_p, c_int, c_void_p, c_int, c_int, c_int, c_void_p,
+                                        c_void_p, c_void_p, c_void_p, c_void_p]
+        L.bimask_act_bwd.argtypes = [c_void_p, c_void_p, c_void_p, c_int, c_int, c_int, c_void_p, c_void_p, c_void_p, c_size_t,
+                                     c_void_p]
+        L.bimask_ckpt_pack.argtypes = [c_void_p, c_int, c_int, c_void_p, c_void_p, c_void_p]
+        L.bimask_ckpt_unpack.argtypes = [c_void_p, c_void_p, c_int, c_int, c_int, c_void_p, c_void_p]
+        L.bimask_wgrad_ckpt.argtypes = [c_void_p, c_void_p, c_void_p, c_int, c_int, c_int, c_void_p, c_void_p, c_size_t, c_void_p,
+                                        c_void_p]
         L.bimask_check_perms.argtypes = [c_void_p, c_int, c_int, c_void_p, c_void_p, c_size_t, c_void_p]
         L.bimask_debug_wait_probe.argtypes = [c_void_p, c_void_p]
         L.bimask_debug_status.argtypes = [c_void_p]
@@ -109,7 +121,7 @@ def lib() -> ctypes.CDLL:
         for name in EXPORTS:
             if name not in ("bimask_last_error", "bimask_launch_count", "bimask_hw_meta_bytes", "bimask_workspace_bytes",
                             "bimask_perm_search_static_max_entries", "bimask_conv_workspace_bytes",
-                            "bimask_refine_workspace_bytes"):
+                            "bimask_refine_workspace_bytes", "bimask_linear_workspace_bytes"):
                 getattr(L, name).restype = c_int
         _lib = L
     return _lib
@@ -206,6 +218,38 @@ def bimask_spmm_dgrad(dY, perm, vals_b, hw_meta_b, T, I, J, dX, ws, ws_bytes, st
 def bimask_wgrad(dY, X, T, I, J, dW, ws, ws_bytes, status_word, stream=None):
     return _check(lib().bimask_wgrad(_ptr(dY), _ptr(X), T, I, J, _ptr(dW), _ptr(ws), ws_bytes, _ptr(status_word),
                                      _stream(stream)))
+
+
+ACT_NONE, ACT_RELU, ACT_GELU, ACT_GELU_TANH, ACT_SILU = 0, 1, 2, 3, 4
+
+
+def bimask_linear_workspace_bytes(T: int, I: int, J: int) -> int:
+    return lib().bimask_linear_workspace_bytes(T, I, J)
+
+
+def bimask_linear_fwd(X, vals_f, hw_meta_f, bias_or_null, act, R_or_null, T, I, J, Y, Zq_or_null, Zs_or_null, status_word,
+                      stream=None):
+    return _check(lib().bimask_linear_fwd(_ptr(X), _ptr(vals_f), _ptr(hw_meta_f), _ptr(bias_or_null), act, _ptr(R_or_null),
+                                          T, I, J, _ptr(Y), _ptr(Zq_or_null), _ptr(Zs_or_null), _ptr(status_word),
+                                          _stream(stream)))
+
+
+def bimask_act_bwd(dY, Zq, Zs, act, T, C, dZ_or_null, dbias_or_null, ws, ws_bytes, stream=None):
+    return _check(lib().bimask_act_bwd(_ptr(dY), _ptr(Zq), _ptr(Zs), act, T, C, _ptr(dZ_or_null), _ptr(dbias_or_null),
+                                       _ptr(ws), ws_bytes, _stream(stream)))
+
+
+def bimask_ckpt_pack(X, T, C, q, s, stream=None):
+    return _check(lib().bimask_ckpt_pack(_ptr(X), T, C, _ptr(q), _ptr(s), _stream(stream)))
+
+
+def bimask_ckpt_unpack(q, s, act, T, C, X, stream=None):
+    return _check(lib().bimask_ckpt_unpack(_ptr(q), _ptr(s), act, T, C, _ptr(X), _stream(stream)))
+
+
+def bimask_wgrad_ckpt(dY, Xq, Xs, T, I, J, dW, ws, ws_bytes, status_word, stream=None):
+    return _check(lib().bimask_wgrad_ckpt(_ptr(dY), _ptr(Xq), _ptr(Xs), T, I, J, _ptr(dW), _ptr(ws), ws_bytes,
+                                          _ptr(status_word), _stream(stream)))
 
 
 def make_layer_args(T, I, J, N, M, P, seed, do_search, bufs: dict, stream=None) -> LayerArgs:

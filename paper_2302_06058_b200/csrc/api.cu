@@ -318,6 +318,83 @@ int bimask_wgrad(const uint16_t* dY, const uint16_t* X, int T, int I, int J, flo
   return launch_wgrad_impl(dY, X, T, I, J, dW, partials, status_word, (cudaStream_t)stream);
 }
 
+// ---- linear layers: epilogue, its gradient, 8-bit activation checkpoints ----
+
+static int check_act(const char* who, int act) {
+  BIMASK_REQUIRE(act >= BIMASK_ACT_NONE && act <= BIMASK_ACT_SILU, BIMASK_EINVAL, "%s: activation %d out of range 0..4", who, act);
+  return BIMASK_OK;
+}
+
+static int check_rows(const char* who, int T, int C) {
+  BIMASK_REQUIRE(T > 0 && C > 0 && C % 32 == 0, BIMASK_EINVAL, "%s: T = %d, C = %d: T positive, C a positive multiple of 32", who, T, C);
+  return BIMASK_OK;
+}
+
+size_t bimask_linear_workspace_bytes(int T, int I, int J) {
+  if (T <= 0 || I <= 0 || J <= 0 || I % 32 != 0 || J % 32 != 0) return 0;
+  const size_t a = act_bwd_partial_bytes(T, I), w = wgrad_ckpt_bytes(T, I, J);
+  return align_up(a > w ? a : w, 256);
+}
+
+int bimask_linear_fwd(const uint16_t* X, const uint16_t* vals_f, const void* hw_meta_f, const float* bias, int act, const uint16_t* R,
+                      int T, int I, int J, uint16_t* Y, int8_t* Zq, uint8_t* Zs, int32_t* status_word, void* stream) {
+  int rc = check_gemm(T, I, J);
+  if (rc != BIMASK_OK) return rc;
+  if ((rc = check_act("bimask_linear_fwd", act)) != BIMASK_OK) return rc;
+  BIMASK_REQUIRE(X && vals_f && Y && status_word, BIMASK_EINVAL, "bimask_linear_fwd: null pointer");
+  BIMASK_REQUIRE((Zq != nullptr) == (Zs != nullptr), BIMASK_EINVAL, "bimask_linear_fwd: a checkpoint needs both Zq and Zs");
+  BIMASK_REQUIRE(aligned16(X) && aligned16(vals_f) && aligned16(hw_meta_f) && aligned16(bias) && aligned16(R) && aligned16(Y) &&
+                     aligned16(Zq) && aligned16(Zs),
+                 BIMASK_EINVAL, "bimask_linear_fwd: pointers must be 16-byte aligned");
+  const LinearEpilogue le{bias, act, R, Zq, Zs};
+  return launch_linear_fwd(vals_f, hw_meta_f, X, I, T, J, le, Y, status_word, (cudaStream_t)stream);
+}
+
+int bimask_act_bwd(const uint16_t* dY, const int8_t* Zq, const uint8_t* Zs, int act, int T, int C, uint16_t* dZ, float* dbias,
+                   void* ws, size_t ws_bytes, void* stream) {
+  int rc = check_rows("bimask_act_bwd", T, C);
+  if (rc != BIMASK_OK) return rc;
+  if ((rc = check_act("bimask_act_bwd", act)) != BIMASK_OK) return rc;
+  BIMASK_REQUIRE(dY && (dZ || dbias), BIMASK_EINVAL, "bimask_act_bwd: null pointer (dY, or both results)");
+  BIMASK_REQUIRE(act == BIMASK_ACT_NONE || (Zq && Zs), BIMASK_EINVAL, "bimask_act_bwd: the slope of an activation needs Zq and Zs");
+  BIMASK_REQUIRE(aligned16(dY) && aligned16(Zq) && aligned16(Zs) && aligned16(dZ) && aligned16(dbias) && aligned16(ws), BIMASK_EINVAL,
+                 "bimask_act_bwd: pointers must be 16-byte aligned");
+  if (dbias) {
+    const size_t need = act_bwd_partial_bytes(T, C);
+    BIMASK_REQUIRE(ws && ws_bytes >= need, BIMASK_EINVAL, "bimask_act_bwd: workspace too small (%zu bytes, need %zu)", ws ? ws_bytes : 0, need);
+  }
+  return launch_act_bwd(dY, Zq, Zs, act, T, C, dZ, dbias, reinterpret_cast<float*>(ws), (cudaStream_t)stream);
+}
+
+int bimask_ckpt_pack(const uint16_t* X, int T, int C, int8_t* q, uint8_t* s, void* stream) {
+  int rc = check_rows("bimask_ckpt_pack", T, C);
+  if (rc != BIMASK_OK) return rc;
+  BIMASK_REQUIRE(X && q && s, BIMASK_EINVAL, "bimask_ckpt_pack: null pointer");
+  BIMASK_REQUIRE(aligned16(X) && aligned16(q) && aligned16(s), BIMASK_EINVAL, "bimask_ckpt_pack: pointers must be 16-byte aligned");
+  return launch_ckpt_pack(X, T, C, q, s, (cudaStream_t)stream);
+}
+
+int bimask_ckpt_unpack(const int8_t* q, const uint8_t* s, int act, int T, int C, uint16_t* X, void* stream) {
+  int rc = check_rows("bimask_ckpt_unpack", T, C);
+  if (rc != BIMASK_OK) return rc;
+  if ((rc = check_act("bimask_ckpt_unpack", act)) != BIMASK_OK) return rc;
+  BIMASK_REQUIRE(X && q && s, BIMASK_EINVAL, "bimask_ckpt_unpack: null pointer");
+  BIMASK_REQUIRE(aligned16(X) && aligned16(q) && aligned16(s), BIMASK_EINVAL, "bimask_ckpt_unpack: pointers must be 16-byte aligned");
+  return launch_ckpt_unpack(q, s, act, T, C, X, (cudaStream_t)stream);
+}
+
+int bimask_wgrad_ckpt(const uint16_t* dY, const int8_t* Xq, const uint8_t* Xs, int T, int I, int J, float* dW, void* ws,
+                      size_t ws_bytes, int32_t* status_word, void* stream) {
+  int rc = check_gemm(T, I, J);
+  if (rc != BIMASK_OK) return rc;
+  BIMASK_REQUIRE(dY && Xq && Xs && dW && ws && status_word, BIMASK_EINVAL, "bimask_wgrad_ckpt: null pointer");
+  BIMASK_REQUIRE(aligned16(dY) && aligned16(Xq) && aligned16(Xs) && aligned16(dW) && aligned16(ws), BIMASK_EINVAL,
+                 "bimask_wgrad_ckpt: pointers must be 16-byte aligned");
+  const size_t need = wgrad_ckpt_bytes(T, I, J);
+  BIMASK_REQUIRE(ws_bytes >= need, BIMASK_EINVAL, "bimask_wgrad_ckpt: workspace too small (%zu bytes, need %zu)", ws_bytes, need);
+  return launch_wgrad_ckpt(dY, Xq, Xs, T, I, J, dW, ws, status_word, (cudaStream_t)stream);
+}
+
 }  // extern "C"
 
 // A 3x3 convolution layer seen by the layer step: geometry, which products fetch shifted pixel

@@ -201,6 +201,28 @@ int launch_wgrad_conv(const uint16_t* dy, const uint16_t* x, int NB, int H, int 
 // A bf16 [Mdim][Kdim], B bf16 [Ndim][Kdim], out bf16 [Ndim][Mdim] (same roles as launch_spmm).
 int launch_dense_nt(const uint16_t* A, const uint16_t* Bop, int Mdim, int Ndim, int Kdim, uint16_t* out,
                     int32_t* status_word, cudaStream_t s);
+// Linear layer: out[n][m] = act(sum_k A[m][k] X[n][k] + bias[m]) + res[n][m], optionally with the checkpoint of the
+// pre-activation.  hw_meta null: dense operand.  Any field but act may be null.
+struct LinearEpilogue {
+  const float* bias;
+  int act;
+  const uint16_t* res;
+  int8_t* zq;
+  uint8_t* zs;
+};
+int launch_linear_fwd(const uint16_t* vals, const void* hw_meta, const uint16_t* X, int Mdim, int Ndim, int Kdim,
+                      const LinearEpilogue& le, uint16_t* out, int32_t* status_word, cudaStream_t s);
+// 8-bit checkpoints and the gradient of the epilogue (linear_kernels.cu).  partial: act_bwd_partial_bytes(T, C), used
+// when dbias is wanted.
+int launch_ckpt_pack(const uint16_t* x, int T, int C, int8_t* q, uint8_t* s, cudaStream_t st);
+int launch_ckpt_unpack(const int8_t* q, const uint8_t* s, int act, int T, int C, uint16_t* x, cudaStream_t st);
+size_t act_bwd_partial_bytes(int T, int C);
+int launch_act_bwd(const uint16_t* dY, const int8_t* zq, const uint8_t* zs, int act, int T, int C, uint16_t* dZ, float* dbias,
+                   float* partial, cudaStream_t st);
+// Weight gradient whose token operand is a checkpoint; ws: wgrad_ckpt_bytes(T, I, J).
+size_t wgrad_ckpt_bytes(int T, int I, int J);
+int launch_wgrad_ckpt(const uint16_t* dY, const int8_t* q, const uint8_t* s, int T, int I, int J, float* dW, void* ws,
+                      int32_t* status_word, cudaStream_t st);
 void wgrad_plan(int T, int I, int J, int* n_tile, int* splits, int* k_tiles_per_split);
 int launch_wgrad_impl(const uint16_t* dY, const uint16_t* X, int T, int I, int J, float* dW, float* partials,
                       int32_t* status_word, cudaStream_t s, cudaStream_t reduce_stream = nullptr,

@@ -4,6 +4,7 @@
 #pragma once
 #include "common.cuh"
 #include "sm100_ptx.cuh"
+#include "act_math.cuh"
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <atomic>
@@ -327,6 +328,189 @@ __device__ __forceinline__ bool store_chunks(const CUtensorMap* tmapD, int c0, i
 }
 // Shared memory must outlive the stores that read it.
 __device__ __forceinline__ void store_finish() { ptx::bulk_wait_read<0>(); }
+
+// ---- epilogue of a linear layer -----------------------------------------------------------------
+// Y = act(D + b) + R, and the checkpoint of D + b, on the way out of the accumulator (EPI instantiations of the product
+// kernels).
+struct EpiParams {
+  const float* bias;        // Mdim, or null
+  int act;                  // BIMASK_ACT_*
+  int has_res;              // residual R, [Ndim][Mdim] bf16, through its tensor map
+  int8_t* zq;               // checkpoint of D + b, [Ndim][Mdim], or null
+  uint8_t* zs;              // its scales, [Ndim][Mdim / 32]
+};
+
+// Checkpoint of one warp's chunk: 32 rows = one block of 32 channels, 32 tokens.  `z` in the accumulator-fragment
+// layout (lane = 4 a + b: index 16 h + 4 g + 2 j + e is row 16 h + 8 j + a, token 8 g + 2 b + e).
+//   scales: the maximum of a token's 32 values is four registers and the eight lanes that share b; the halving exchange
+//           (two tokens per register, half of the registers sent away at each step) takes 4 shuffles, handing the
+//           eight scale bytes back to every lane 2.
+//   bytes:  two bytes of a token (rows a and a + 8 of a half) make a 16-bit element, which stmatrix transposes like
+//           any other; a lane reads back the 16 bytes of half a block, undoes the pairing and stores them: a token's 32
+//           bytes are one whole sector.
+// `area`: 32 token rows of 128 bytes of which this warp may use units u0, u0 + 1 (16 bytes each, XOR token mod 8) as
+// scratch.  q_out / s_out: where token 0's block and scale go; ntok: tokens of the chunk that exist.
+__device__ __forceinline__ void emit_checkpoint(const float (&z)[32], uint32_t area, uint32_t u0, int lane, int8_t* q_out, size_t q_pitch,
+                                                uint8_t* s_out, size_t s_pitch, int ntok) {
+  uint32_t p[4];
+#pragma unroll
+  for (int g = 0; g < 4; ++g) {
+    float m[2];
+#pragma unroll
+    for (int e = 0; e < 2; ++e)
+      m[e] = act::max_nan(act::max_nan(fabsf(z[4 * g + e]), fabsf(z[4 * g + 2 + e])),
+                          act::max_nan(fabsf(z[16 + 4 * g + e]), fabsf(z[16 + 4 * g + 2 + e])));
+    p[g] = ckpt::up16(m[0]) | (ckpt::up16(m[1]) << 16);
+  }
+  const bool hi = (lane & 16) != 0, mid = (lane & 8) != 0;
+  uint32_t k0 = hi ? p[2] : p[0], k1 = hi ? p[3] : p[1];
+  k0 = __vmaxu2(k0, __shfl_xor_sync(0xFFFFFFFFu, hi ? p[0] : p[2], 16));
+  k1 = __vmaxu2(k1, __shfl_xor_sync(0xFFFFFFFFu, hi ? p[1] : p[3], 16));
+  uint32_t k = mid ? k1 : k0;
+  k = __vmaxu2(k, __shfl_xor_sync(0xFFFFFFFFu, mid ? k0 : k1, 8));
+  k = __vmaxu2(k, __shfl_xor_sync(0xFFFFFFFFu, k, 4));     // tokens 8 g + 2 b + {0, 1}, g = lane / 8
+  const uint32_t s0 = ckpt::scale_of(k & 0xFFFFu), s1 = ckpt::scale_of(k >> 16);
+  const int st = 8 * (lane >> 3) + 2 * (lane & 3) + ((lane >> 2) & 1);
+  if (st < ntok) s_out[(size_t)st * s_pitch] = (uint8_t)((lane & 4) ? s1 : s0);
+  const uint32_t both = s0 | (s1 << 8);
+  const uint32_t o8 = __shfl_xor_sync(0xFFFFFFFFu, both, 8);
+  const uint32_t quad = mid ? (o8 | (both << 16)) : (both | (o8 << 16));
+  const uint32_t o16 = __shfl_xor_sync(0xFFFFFFFFu, quad, 16);
+  const uint32_t sc[2] = {hi ? o16 : quad, hi ? quad : o16};      // bytes 2 (g & 1) + e of sc[g >> 1]
+  uint32_t w[8];                                          // w[2 g + h]: low half token e = 0, high half e = 1
+#pragma unroll
+  for (int g = 0; g < 4; ++g) {
+    const float i0 = ckpt::inverse_scale((sc[g >> 1] >> (16 * (g & 1))) & 0xFFu);
+    const float i1 = ckpt::inverse_scale((sc[g >> 1] >> (16 * (g & 1) + 8)) & 0xFFu);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const float* v = &z[16 * h + 4 * g];
+      const uint32_t e0 = __byte_perm(ckpt::round_bits(v[0], i0), ckpt::round_bits(v[2], i0), 0x0040);
+      const uint32_t e1 = __byte_perm(ckpt::round_bits(v[1], i1), ckpt::round_bits(v[3], i1), 0x0040);
+      w[2 * g + h] = __byte_perm(e0, e1, 0x5410);
+    }
+  }
+  const uint32_t lt = (uint32_t)lane & 7u, li = (uint32_t)lane >> 3;   // stmatrix: lane 8 i + k addresses token k of matrix i
+#pragma unroll
+  for (int g = 0; g < 4; g += 2)                          // matrices (g, half 0), (g, half 1), (g + 1, half 0), (g + 1, half 1)
+    ptx::stmatrix_x4_trans(area + (8u * (g + (li >> 1)) + lt) * 128u + (((u0 + (li & 1u)) ^ lt) << 4), w[2 * g], w[2 * g + 1],
+                           w[2 * g + 2], w[2 * g + 3]);
+  __syncwarp();
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int t = 16 * i + (lane & 15), h = lane >> 4;
+    const uint4 v = ptx::ld_shared_v4(area + (uint32_t)t * 128u + (((u0 + (uint32_t)h) ^ ((uint32_t)t & 7u)) << 4));
+    if (t < ntok)
+      *reinterpret_cast<uint4*>(q_out + (size_t)t * q_pitch + 16 * h) =
+          make_uint4(__byte_perm(v.x, v.y, 0x6420), __byte_perm(v.z, v.w, 0x6420), __byte_perm(v.x, v.y, 0x7531), __byte_perm(v.z, v.w, 0x7531));
+  }
+  __syncwarp();                                           // the scratch area is the warp's again
+}
+
+// drain_chunks_tma with the epilogue applied.  With a residual, `freed[t]` is completed by the arrival of the residual
+// tile of the chunk in staging tile t (store_chunks_epi loads it there as soon as the tile's last store has read it), so
+// it is waited for on every use; ldmatrix reads the tile in the fragment layout that stmatrix then writes back.
+// x0: first row of the CTA's 128; y0: first token of chunk 0.
+template <int NT>
+__device__ __forceinline__ bool drain_chunks_epi(uint32_t acc, int c0, int cstep, int nchunks, uint32_t release_bar, uint32_t stg,
+                                                 uint32_t bars, uint32_t& u, int q, int lane, const EpiParams& e, int x0, int y0,
+                                                 int Mdim, int Ndim, volatile int* abort_flag) {
+  if (c0 >= nchunks) { release_accumulator(release_bar, lane); return true; }
+  const uint32_t half = stg + (uint32_t)(q >> 1) * 4096u;
+  const uint32_t dst = half + (uint32_t)(lane & 7) * 128u +
+                       ((((uint32_t)(4 * (q & 1)) + ((uint32_t)lane >> 3)) ^ ((uint32_t)lane & 7u)) << 4);
+  const int row0 = x0 + 32 * q;                           // this warp's 32 rows all exist or none does
+  const bool rows_ok = row0 < Mdim;
+  float b[4];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) b[k] = (e.bias != nullptr && rows_ok) ? __ldg(e.bias + row0 + 8 * k + (lane >> 2)) : 0.f;
+  bool ok = true;
+  drain_loop<32>(acc, c0, cstep, nchunks, false, release_bar, lane, [&](const uint32_t (&r)[32], int c) {
+    const uint32_t slot = u % NT, use = u / NT;
+    ++u;
+    float z[32];
+#pragma unroll
+    for (int i = 0; i < 32; ++i) z[i] = __uint_as_float(r[i]) + b[2 * (i >> 4) + ((i >> 1) & 1)];
+    if (ok) {
+      if (e.has_res) ok = ptx::mbar_wait_bounded(bars + 8u * (NT + slot), use & 1u, abort_flag, WAIT_BUDGET);
+      else if (use > 0) ok = ptx::mbar_wait_bounded(bars + 8u * (NT + slot), (use - 1u) & 1u, abort_flag, WAIT_BUDGET);
+    }
+    __syncwarp();
+    uint32_t res[16];
+    if (e.has_res) {
+#pragma unroll
+      for (int g = 0; g < 4; ++g) ptx::ldmatrix_x4_trans(dst + slot * 8192u + 1024u * g, res[4 * g], res[4 * g + 1], res[4 * g + 2], res[4 * g + 3]);
+      __syncwarp();
+    }
+    if (e.zq != nullptr && rows_ok) {
+      const int t0 = y0 + 32 * c;
+      emit_checkpoint(z, half + slot * 8192u, 4u * (q & 1), lane, e.zq + (size_t)t0 * Mdim + row0, (size_t)Mdim,
+                      e.zs + (size_t)t0 * (Mdim >> 5) + (row0 >> 5), (size_t)(Mdim >> 5), Ndim - t0);
+    }
+    act::apply(e.act, z);
+    if (e.has_res) {
+#pragma unroll
+      for (int g = 0; g < 4; ++g)
+#pragma unroll
+        for (int m = 0; m < 4; ++m) {                     // matrix m: rows 8 m + a
+          z[16 * (m >> 1) + 4 * g + 2 * (m & 1)] += bf16_lo(res[4 * g + m]);
+          z[16 * (m >> 1) + 4 * g + 2 * (m & 1) + 1] += bf16_hi(res[4 * g + m]);
+        }
+    }
+    uint32_t out[32];
+#pragma unroll
+    for (int i = 0; i < 32; ++i) out[i] = __float_as_uint(z[i]);
+    epi_stage<32, 1024u>(out, dst + slot * 8192u);
+    ptx::fence_proxy_async();
+    __syncwarp();
+    if (lane == 0) ptx::mbar_arrive(bars + 8u * slot);
+  });
+  return ok;
+}
+
+// The store thread's side: chunk n of the group (over all its tiles) goes to rows x0.., tokens y.. as coord(n, x0, y)
+// says, false past the last one.  With a residual it also loads the residual tile of chunk n + NT into the staging tile
+// of chunk n once that chunk's store has read it.
+template <int NT, typename Coord>
+__device__ __forceinline__ bool store_chunks_epi(const CUtensorMap* tmapD, const CUtensorMap* tmapR, bool has_res, uint32_t stg,
+                                                 uint32_t bars, int Mdim, int Ndim, volatile int* abort_flag, Coord&& coord) {
+  uint32_t loaded = 0;                                    // residual tiles requested so far
+  auto load = [&](uint32_t n) {
+    int x0, y;
+    if (!coord(n, x0, y)) return;
+    const uint32_t slot = n % NT, bar = bars + 8u * (NT + slot);
+    ptx::mbar_expect_tx(bar, 8192);
+    ptx::tma_load_2d(stg + slot * 8192u, tmapR, x0, y, bar);
+    ptx::tma_load_2d(stg + slot * 8192u + 4096u, tmapR, x0 + 64, y, bar);
+    ++loaded;
+  };
+  if (has_res)
+    for (uint32_t n = 0; n < NT; ++n) load(n);
+  bool ok = true;
+  int x0, y;
+  for (uint32_t n = 0; coord(n, x0, y); ++n) {
+    const uint32_t slot = n % NT, use = n / NT;
+    ok = ptx::mbar_wait_bounded(bars + 8u * slot, use & 1u, abort_flag, WAIT_BUDGET);
+    if (!ok) break;
+    if (y < Ndim && x0 < Mdim) {
+      ptx::tma_store_2d(tmapD, x0, y, stg + slot * 8192u);
+      if (x0 + 64 < Mdim) ptx::tma_store_2d(tmapD, x0 + 64, y, stg + slot * 8192u + 4096u);
+    }
+    ptx::bulk_commit();
+    if (n > 0) {
+      ptx::bulk_wait_read<1>();
+      if (has_res) load(n - 1 + NT);
+      else ptx::mbar_arrive(bars + 8u * (NT + (n - 1u) % NT));
+    }
+  }
+  if (!ok && has_res) {                                   // giving up: no load may be in flight when the kernel ends
+    volatile int none = 0;
+    for (uint32_t n = loaded > NT ? loaded - NT : 0; n < loaded; ++n)
+      ptx::mbar_wait_bounded(bars + 8u * (NT + n % NT), (n / NT) & 1u, &none, WAIT_BUDGET);
+  }
+  store_finish();
+  return ok;
+}
 
 // ---- host helpers (gemm_host.cu) -----------------------------------------------------------
 int sm_count();

@@ -26,10 +26,13 @@ namespace {
 // SPARSE = false: the same pipeline on a dense bf16 A operand (masked weights of a pattern the
 // 2:4 format cannot hold): 128 x 128 A tile per stage as two 64-wide boxes, eight K = 16 MMAs.
 // CONV: the token operand is fetched as shifted pixel boxes (see ConvGeom); N_TILE tokens = one box.
-template <int N_TILE, int STAGES, bool SPARSE, bool CONV>
+// EPI (in all three kernels of this file): the epilogue of a linear layer (EpiParams; tmapR: its residual).
+template <int N_TILE, int STAGES, bool SPARSE, bool CONV, bool EPI = false>
 __global__ void __launch_bounds__(PAIR_THREADS, 1)
 spmm_single_kernel(const __grid_constant__ CUtensorMap tmapA, const __grid_constant__ CUtensorMap tmapB,
-                   const __grid_constant__ CUtensorMap tmapD, const GemmParams p) {
+                   const __grid_constant__ CUtensorMap tmapD, const GemmParams p, const __grid_constant__ CUtensorMap tmapR,
+                   const EpiParams e) {
+  static_assert(!(CONV && EPI), "the implicit convolution has no epilogue");
   pdl_launch_dependents();
   using C = Cfg<N_TILE, STAGES, SPARSE>;
   extern __shared__ uint8_t smem_raw[];
@@ -190,6 +193,12 @@ spmm_single_kernel(const __grid_constant__ CUtensorMap tmapA, const __grid_const
           if (w >= p.conv.W || h >= p.conv.H || n >= p.conv.NB) return nullptr;
           return outp + conv_out_pixel(p.conv, n, h, w) * p.Mdim + m0;
         });
+      } else if constexpr (EPI) {
+        uint32_t u = 0;
+        if (!drain_chunks_epi<C::EPI_NT>(tmem_base + ((uint32_t)(32 * q) << 16), eg, EPI_GROUPS, N_TILE / 32, 0u,
+                                         staging + eg * (C::EPI_NT * 8192), epi_bars_of<C::EPI_NT>(bar_base, eg), u, q, lane, e, m0, n0,
+                                         p.Mdim, p.Ndim, abort_flag))
+          *abort_flag = 1;
       } else {
         uint32_t u = 0;
         if (!drain_chunks_tma<32, C::EPI_NT>(tmem_base + ((uint32_t)(32 * q) << 16), eg, EPI_GROUPS, N_TILE / 32, num_kt <= 0, 0u,
@@ -202,11 +211,21 @@ spmm_single_kernel(const __grid_constant__ CUtensorMap tmapA, const __grid_const
     // ------------------------------ store threads: one per epilogue group ------------------------------
     if (ptx::elect_one()) {
       const int g = warp - 2 - EPI_WARPS;
+      if constexpr (EPI) {
+        if (!store_chunks_epi<C::EPI_NT>(&tmapD, &tmapR, e.has_res != 0, staging + g * (C::EPI_NT * 8192), epi_bars_of<C::EPI_NT>(bar_base, g),
+                                         p.Mdim, p.Ndim, abort_flag, [&](uint32_t n, int& x0, int& y) {
+              const int c = g + EPI_GROUPS * (int)n;
+              x0 = m0; y = n0 + 32 * c;
+              return c < N_TILE / 32;
+            }))
+          *abort_flag = 1;
+      } else {
       uint32_t u = 0;
       if (!store_chunks<32, C::EPI_NT>(&tmapD, g, EPI_GROUPS, N_TILE / 32, staging + g * (C::EPI_NT * 8192),
                                        epi_bars_of<C::EPI_NT>(bar_base, g), u, m0, n0, p.Mdim, p.Ndim, abort_flag))
         *abort_flag = 1;
       store_finish();
+      }
     }
   }
 
@@ -247,12 +266,13 @@ struct PairPCfg {
 // SPARSE = false: the same kernel on a dense bf16 A operand (masked weights of a pattern the 2:4 format cannot
 // hold): a 256 x 128 A tile per stage as two 64-wide boxes per CTA, eight K = 16 MMAs, no metadata, and two
 // accumulators at every N (tmapE is not used).
-template <int STAGES, bool CONV, bool SPARSE = true>
+template <int STAGES, bool CONV, bool SPARSE = true, bool EPI = false>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PAIR_THREADS, 1)
 spmm_pair_persistent_kernel(const __grid_constant__ CUtensorMap tmapA, const __grid_constant__ CUtensorMap tmapB,
                             const __grid_constant__ CUtensorMap tmapE, const __grid_constant__ CUtensorMap tmapD,
-                            const GemmParams p) {
+                            const GemmParams p, const __grid_constant__ CUtensorMap tmapR, const EpiParams e) {
   static_assert(SPARSE || !CONV, "the implicit convolution runs on 2:4 operands only");
+  static_assert(!(CONV && EPI), "the implicit convolution has no epilogue");
   pdl_launch_dependents();
   using C = PairPCfg<STAGES, SPARSE>;
   extern __shared__ uint8_t smem_raw[];
@@ -434,6 +454,12 @@ spmm_pair_persistent_kernel(const __grid_constant__ CUtensorMap tmapA, const __g
           if (w >= p.conv.W || h >= p.conv.H || n >= p.conv.NB) return nullptr;
           return outp + conv_out_pixel(p.conv, n, h, w) * p.Mdim + m0;
         });
+      } else if constexpr (EPI) {
+        if (!drain_chunks_epi<C::EPI_NT>(acc, eg, EPI_GROUPS, nchunks, release_bar, stg, ebars, u, q, lane, e, m0, n0, p.Mdim, p.Ndim,
+                                         abort_flag)) {
+          *abort_flag = 1;
+          break;
+        }
       } else if (!drain_chunks_tma<32, C::EPI_NT>(acc, eg, EPI_GROUPS, nchunks, false, release_bar, stg, ebars, u, q, lane,
                                                   abort_flag)) {
         *abort_flag = 1;
@@ -446,6 +472,21 @@ spmm_pair_persistent_kernel(const __grid_constant__ CUtensorMap tmapA, const __g
       const int g = warp - 2 - EPI_WARPS;
       const uint32_t stg = staging + g * (C::EPI_NT * 8192);
       const uint32_t ebars = epi_bars_of<C::EPI_NT>(bar_base, g);
+      if constexpr (EPI) {
+        const int per_tile = (SP_N / 32 - g + 1) / 2;      // the group's chunks of a tile
+        if (!store_chunks_epi<C::EPI_NT>(&tmapD, &tmapR, e.has_res != 0, stg, ebars, p.Mdim, p.Ndim, abort_flag,
+                                         [&](uint32_t n, int& x0, int& y) {
+              if (per_tile <= 0) return false;
+              const int nt = (int)n / per_tile, tile = cluster_id + nt * num_clusters;
+              if (tile >= num_tiles) return false;
+              int tile_m, tile_n;
+              raster(tile, p.tiles_m, p.tiles_n, p.raster_group, tile_m, tile_n);
+              x0 = (2 * tile_m + (int)rank) * 128;
+              y = tile_n * SP_N + 32 * (g + 2 * ((int)n - nt * per_tile));
+              return true;
+            }))
+          *abort_flag = 1;
+      } else {
       uint32_t u = 0;
       for (int tile = cluster_id; tile < num_tiles; tile += num_clusters) {
         int tile_m, tile_n;
@@ -457,6 +498,7 @@ spmm_pair_persistent_kernel(const __grid_constant__ CUtensorMap tmapA, const __g
         }
       }
       store_finish();
+      }
     }
   }
 
@@ -498,11 +540,11 @@ struct Pair2MCfg {
   static constexpr int SMEM_BYTES = STAGES * STAGE_BYTES + STAGING_BYTES + 1024 + 256;
 };
 
-template <int STAGES>
+template <int STAGES, bool EPI = false>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(GEMM2M_THREADS, 1)
 spmm_pair2m_kernel(const __grid_constant__ CUtensorMap tmapA, const __grid_constant__ CUtensorMap tmapB,
                    const __grid_constant__ CUtensorMap tmapE, const __grid_constant__ CUtensorMap tmapD,
-                   const GemmParams p) {
+                   const GemmParams p, const __grid_constant__ CUtensorMap tmapR, const EpiParams e) {
   pdl_launch_dependents();
   using C = Pair2MCfg<STAGES>;
   extern __shared__ uint8_t smem_raw[];
@@ -658,7 +700,13 @@ spmm_pair2m_kernel(const __grid_constant__ CUtensorMap tmapA, const __grid_const
 #pragma unroll 1
       for (int mt = 0; mt < 2; ++mt) {
         const uint32_t acc = tmem_base + 256u * mt + ((uint32_t)(32 * q) << 16);
-        if (!drain_chunks_tma<32, C::EPI_NT>(acc, (g ^ mt) & 1, 2, SP_N / 32, false, mt ? release1 : release0, stg, ebars, u, q,
+        if constexpr (EPI) {
+          int tile_m, tile_n;
+          raster(tile, p.tiles_m, p.tiles_n, p.raster_group, tile_m, tile_n);
+          if (!drain_chunks_epi<C::EPI_NT>(acc, (g ^ mt) & 1, 2, SP_N / 32, mt ? release1 : release0, stg, ebars, u, q, lane, e,
+                                           mt128_of(tile_m, mt) * 128, tile_n * SP_N, p.Mdim, p.Ndim, abort_flag))
+            *abort_flag = 1;
+        } else if (!drain_chunks_tma<32, C::EPI_NT>(acc, (g ^ mt) & 1, 2, SP_N / 32, false, mt ? release1 : release0, stg, ebars, u, q,
                                              lane, abort_flag))
           *abort_flag = 1;
       }
@@ -670,6 +718,21 @@ spmm_pair2m_kernel(const __grid_constant__ CUtensorMap tmapA, const __grid_const
       const int g = warp - 2 - EPI_WARPS;
       const uint32_t stg = staging + g * (C::EPI_NT * 8192);
       const uint32_t ebars = epi_bars_of<C::EPI_NT>(bar_base, g);
+      if constexpr (EPI) {
+        const int nchunks = SP_N / 32, first = (nchunks - g + 1) / 2;   // the group's chunks of row tile 0; the rest of nchunks are row tile 1's
+        if (!store_chunks_epi<C::EPI_NT>(&tmapD, &tmapR, e.has_res != 0, stg, ebars, p.Mdim, p.Ndim, abort_flag,
+                                         [&](uint32_t n, int& x0, int& y) {
+              const int nt = (int)n / nchunks, tile = cluster_id + nt * num_clusters;
+              if (tile >= num_tiles) return false;
+              int tile_m, tile_n;
+              raster(tile, p.tiles_m, p.tiles_n, p.raster_group, tile_m, tile_n);
+              const int r = (int)n - nt * nchunks, mt = r >= first ? 1 : 0;
+              x0 = mt128_of(tile_m, mt) * 128;
+              y = tile_n * SP_N + 32 * (((g ^ mt) & 1) + 2 * (mt ? r - first : r));
+              return true;
+            }))
+          *abort_flag = 1;
+      } else {
       uint32_t u = 0;
       bool ok = true;
       for (int tile = cluster_id; tile < num_tiles && ok; tile += num_clusters) {
@@ -681,6 +744,7 @@ spmm_pair2m_kernel(const __grid_constant__ CUtensorMap tmapA, const __grid_const
       }
       if (!ok) *abort_flag = 1;
       store_finish();
+      }
     }
   }
 
@@ -694,16 +758,29 @@ spmm_pair2m_kernel(const __grid_constant__ CUtensorMap tmapA, const __grid_const
   }
 }
 
-template <int N_TILE, int STAGES, bool SPARSE = true>
+// What a product kernel with an epilogue gets besides the operands: the residual's tensor map (any valid map without one).
+int epi_args(const LinearEpilogue* le, int Mdim, int Ndim, const CUtensorMap& unused, CUtensorMap* tr, EpiParams* e) {
+  *tr = unused;
+  *e = EpiParams{};
+  if (le == nullptr) return BIMASK_OK;
+  e->bias = le->bias; e->act = le->act; e->has_res = le->res != nullptr; e->zq = le->zq; e->zs = le->zs;
+  return le->res != nullptr ? make_tmap(tr, le->res, (uint64_t)Mdim, (uint64_t)Ndim, 32) : BIMASK_OK;
+}
+
+// EPI in the host functions below: `le` describes the epilogue (null otherwise).
+template <int N_TILE, int STAGES, bool SPARSE = true, bool EPI = false>
 int run_single(const uint16_t* vals, const void* hw_meta, const uint16_t* Bop, int Mdim, int Ndim, int Kdim,
-               uint16_t* out, int32_t* status_word, cudaStream_t s) {
+               uint16_t* out, int32_t* status_word, cudaStream_t s, const LinearEpilogue* le = nullptr) {
   using C = Cfg<N_TILE, STAGES, SPARSE>;
   CUtensorMap ta, tb, td;
   int rc;
   if ((rc = make_tmap(&ta, vals, SPARSE ? (uint64_t)Kdim / 2 : (uint64_t)Kdim, (uint64_t)Mdim, 128)) != BIMASK_OK) return rc;
   if ((rc = make_tmap(&tb, Bop, (uint64_t)Kdim, (uint64_t)Ndim, N_TILE)) != BIMASK_OK) return rc;
   if ((rc = make_tmap(&td, out, (uint64_t)Mdim, (uint64_t)Ndim, 32)) != BIMASK_OK) return rc;   // result: 32 tokens x 64 rows per store
-  auto kern = spmm_single_kernel<N_TILE, STAGES, SPARSE, false>;
+  CUtensorMap tr;
+  EpiParams e;
+  if ((rc = epi_args(le, Mdim, Ndim, td, &tr, &e)) != BIMASK_OK) return rc;
+  auto kern = spmm_single_kernel<N_TILE, STAGES, SPARSE, false, EPI>;
   if ((rc = set_smem_attr(kern, C::SMEM_BYTES)) != BIMASK_OK) return rc;
   GemmParams p;
   p.conv.mode = 0;
@@ -717,7 +794,7 @@ int run_single(const uint16_t* vals, const void* hw_meta, const uint16_t* Bop, i
   p.tiles_n = (Ndim + N_TILE - 1) / N_TILE;
   p.raster_group = 16;
   dim3 grid(p.tiles_m * p.tiles_n, 1, 1);
-  BIMASK_CUDA_OK(launch_pdl(kern, grid, PAIR_THREADS, C::SMEM_BYTES, s, ta, tb, td, p));
+  BIMASK_CUDA_OK(launch_pdl(kern, grid, PAIR_THREADS, C::SMEM_BYTES, s, ta, tb, td, p, tr, e));
   count_launch();
   BIMASK_CUDA_OK(cudaGetLastError());
   return BIMASK_OK;
@@ -745,8 +822,9 @@ int choose_sparse_n(int pair_tiles_m, int Ndim, int k_tiles, int clusters) {
   return best_n;
 }
 
+template <bool EPI = false>
 int run_sparse_pair_persistent(const uint16_t* vals, const void* hw_meta, const uint16_t* Bop, int Mdim, int Ndim,
-                               int Kdim, uint16_t* out, int32_t* status_word, cudaStream_t s) {
+                               int Kdim, uint16_t* out, int32_t* status_word, cudaStream_t s, const LinearEpilogue* le = nullptr) {
   constexpr int STAGES = 3;
   using C = PairPCfg<STAGES>;
   CUtensorMap ta, tb, te, td;
@@ -758,7 +836,10 @@ int run_sparse_pair_persistent(const uint16_t* vals, const void* hw_meta, const 
   if ((rc = make_tmap(&tb, Bop, (uint64_t)Kdim, (uint64_t)Ndim, n_tile / 2)) != BIMASK_OK) return rc;
   if ((rc = make_tmap_meta(&te, hw_meta, (uint64_t)tiles_m * tiles_k)) != BIMASK_OK) return rc;
   if ((rc = make_tmap(&td, out, (uint64_t)Mdim, (uint64_t)Ndim, 32)) != BIMASK_OK) return rc;   // one chunk of the drain: 32 tokens x 64 rows per store
-  auto kern = spmm_pair_persistent_kernel<STAGES, false>;
+  CUtensorMap tr;
+  EpiParams e;
+  if ((rc = epi_args(le, Mdim, Ndim, td, &tr, &e)) != BIMASK_OK) return rc;
+  auto kern = spmm_pair_persistent_kernel<STAGES, false, true, EPI>;
   if ((rc = set_smem_attr(kern, C::SMEM_BYTES)) != BIMASK_OK) return rc;
   GemmParams p;
   p.conv.mode = 0;
@@ -774,7 +855,7 @@ int run_sparse_pair_persistent(const uint16_t* vals, const void* hw_meta, const 
   p.raster_group = 8;
   const int total = p.tiles_m * p.tiles_n;
   const int clusters = total < sms / 2 ? total : sms / 2;
-  BIMASK_CUDA_OK(launch_pdl(kern, 2 * clusters, PAIR_THREADS, C::SMEM_BYTES, s, ta, tb, te, td, p));
+  BIMASK_CUDA_OK(launch_pdl(kern, 2 * clusters, PAIR_THREADS, C::SMEM_BYTES, s, ta, tb, te, td, p, tr, e));
   count_launch();
   BIMASK_CUDA_OK(cudaGetLastError());
   return BIMASK_OK;
@@ -794,8 +875,9 @@ int choose_sparse_n_2m(int tiles_m512, int Ndim, int k_tiles, int clusters) {
   return best_n;
 }
 
+template <bool EPI = false>
 int run_sparse_pair2m(const uint16_t* vals, const void* hw_meta, const uint16_t* Bop, int Mdim, int Ndim, int Kdim,
-                      uint16_t* out, int32_t* status_word, cudaStream_t s) {
+                      uint16_t* out, int32_t* status_word, cudaStream_t s, const LinearEpilogue* le = nullptr) {
   constexpr int STAGES = 3;
   using C = Pair2MCfg<STAGES>;
   CUtensorMap ta, tb, te, td;
@@ -808,7 +890,10 @@ int run_sparse_pair2m(const uint16_t* vals, const void* hw_meta, const uint16_t*
   if ((rc = make_tmap(&tb, Bop, (uint64_t)Kdim, (uint64_t)Ndim, n_tile / 2)) != BIMASK_OK) return rc;
   if ((rc = make_tmap_meta(&te, hw_meta, (uint64_t)tiles_m * tiles_k)) != BIMASK_OK) return rc;
   if ((rc = make_tmap(&td, out, (uint64_t)Mdim, (uint64_t)Ndim, 32)) != BIMASK_OK) return rc;
-  auto kern = spmm_pair2m_kernel<STAGES>;
+  CUtensorMap tr;
+  EpiParams e;
+  if ((rc = epi_args(le, Mdim, Ndim, td, &tr, &e)) != BIMASK_OK) return rc;
+  auto kern = spmm_pair2m_kernel<STAGES, EPI>;
   if ((rc = set_smem_attr(kern, C::SMEM_BYTES)) != BIMASK_OK) return rc;
   GemmParams p;
   p.conv.mode = 0;
@@ -826,7 +911,7 @@ int run_sparse_pair2m(const uint16_t* vals, const void* hw_meta, const uint16_t*
   p.raster_group = 8;
   const int total = p.tiles_m * p.tiles_n;
   const int clusters = total < sms / 2 ? total : sms / 2;
-  BIMASK_CUDA_OK(launch_pdl(kern, 2 * clusters, GEMM2M_THREADS, C::SMEM_BYTES, s, ta, tb, te, td, p));
+  BIMASK_CUDA_OK(launch_pdl(kern, 2 * clusters, GEMM2M_THREADS, C::SMEM_BYTES, s, ta, tb, te, td, p, tr, e));
   count_launch();
   BIMASK_CUDA_OK(cudaGetLastError());
   return BIMASK_OK;
@@ -872,7 +957,7 @@ int run_conv_single(const uint16_t* vals, int a_rows, int a_kdim, const void* hw
   p.raster_group = 16;
   p.n_tile = N_TILE;
   dim3 grid(p.tiles_m * p.tiles_n, 1, 1);
-  BIMASK_CUDA_OK(launch_pdl(kern, grid, PAIR_THREADS, C::SMEM_BYTES, s, ta, tb, ta /* result map: not used by the convolution */, p));
+  BIMASK_CUDA_OK(launch_pdl(kern, grid, PAIR_THREADS, C::SMEM_BYTES, s, ta, tb, ta /* result map: not used by the convolution */, p, ta, EpiParams{}));
   count_launch();
   BIMASK_CUDA_OK(cudaGetLastError());
   return BIMASK_OK;
@@ -908,7 +993,7 @@ int run_conv_pair(const uint16_t* vals, int a_rows, int a_kdim, const void* hw_m
   p.raster_group = 8;
   const int total = p.tiles_m * p.tiles_n;
   const int clusters = total < sms / 2 ? total : sms / 2;
-  BIMASK_CUDA_OK(launch_pdl(kern, 2 * clusters, PAIR_THREADS, C::SMEM_BYTES, s, ta, tb, te, ta /* result map: not used by the convolution */, p));
+  BIMASK_CUDA_OK(launch_pdl(kern, 2 * clusters, PAIR_THREADS, C::SMEM_BYTES, s, ta, tb, te, ta /* result map: not used by the convolution */, p, ta, EpiParams{}));
   count_launch();
   BIMASK_CUDA_OK(cudaGetLastError());
   return BIMASK_OK;
@@ -977,8 +1062,9 @@ namespace {
 
 // Dense operand, CTA pairs: 256 x N tiles, N the multiple of 32 (at most 256) that wastes the fewest token columns
 // among those with the fewest rounds over the pairs.
+template <bool EPI = false>
 int run_dense_pair_persistent(const uint16_t* A, const uint16_t* Bop, int Mdim, int Ndim, int Kdim, uint16_t* out,
-                              int32_t* status_word, cudaStream_t s) {
+                              int32_t* status_word, cudaStream_t s, const LinearEpilogue* le = nullptr) {
   constexpr int STAGES = 3;
   using C = PairPCfg<STAGES, false>;
   CUtensorMap ta, tb, td;
@@ -996,7 +1082,10 @@ int run_dense_pair_persistent(const uint16_t* A, const uint16_t* Bop, int Mdim, 
   if ((rc = make_tmap(&ta, A, (uint64_t)Kdim, (uint64_t)Mdim, 128)) != BIMASK_OK) return rc;
   if ((rc = make_tmap(&tb, Bop, (uint64_t)Kdim, (uint64_t)Ndim, n_tile / 2)) != BIMASK_OK) return rc;
   if ((rc = make_tmap(&td, out, (uint64_t)Mdim, (uint64_t)Ndim, 32)) != BIMASK_OK) return rc;
-  auto kern = spmm_pair_persistent_kernel<STAGES, false, false>;
+  CUtensorMap tr;
+  EpiParams e;
+  if ((rc = epi_args(le, Mdim, Ndim, td, &tr, &e)) != BIMASK_OK) return rc;
+  auto kern = spmm_pair_persistent_kernel<STAGES, false, false, EPI>;
   if ((rc = set_smem_attr(kern, C::SMEM_BYTES)) != BIMASK_OK) return rc;
   GemmParams p;
   p.conv.mode = 0;
@@ -1012,7 +1101,7 @@ int run_dense_pair_persistent(const uint16_t* A, const uint16_t* Bop, int Mdim, 
   p.raster_group = 8;
   const int total = p.tiles_m * p.tiles_n;
   const int clusters = total < sms / 2 ? total : sms / 2;
-  BIMASK_CUDA_OK(launch_pdl(kern, 2 * clusters, PAIR_THREADS, C::SMEM_BYTES, s, ta, tb, ta /* no metadata */, td, p));
+  BIMASK_CUDA_OK(launch_pdl(kern, 2 * clusters, PAIR_THREADS, C::SMEM_BYTES, s, ta, tb, ta /* no metadata */, td, p, tr, e));
   count_launch();
   BIMASK_CUDA_OK(cudaGetLastError());
   return BIMASK_OK;
@@ -1025,6 +1114,23 @@ int launch_dense_nt(const uint16_t* A, const uint16_t* Bop, int Mdim, int Ndim, 
   if (Ndim > 128 && Mdim > 128) return run_dense_pair_persistent(A, Bop, Mdim, Ndim, Kdim, out, status_word, s);
   if (Ndim > 128) return run_single<256, 2, false>(A, nullptr, Bop, Mdim, Ndim, Kdim, out, status_word, s);
   return run_single<128, 3, false>(A, nullptr, Bop, Mdim, Ndim, Kdim, out, status_word, s);
+}
+
+// Linear layer: the product of launch_spmm (hw_meta given) or launch_dense_nt (null) with the epilogue of `le`, on the
+// same kernels by the same rules.
+int launch_linear_fwd(const uint16_t* vals, const void* hw_meta, const uint16_t* X, int Mdim, int Ndim, int Kdim,
+                      const LinearEpilogue& le, uint16_t* out, int32_t* status_word, cudaStream_t s) {
+  const bool many = Ndim > 128 && Mdim > 128;
+  if (hw_meta != nullptr) {
+    if (Ndim >= 1024 && Mdim >= 2048 && Kdim >= 4096)
+      return run_sparse_pair2m<true>(vals, hw_meta, X, Mdim, Ndim, Kdim, out, status_word, s, &le);
+    if (many) return run_sparse_pair_persistent<true>(vals, hw_meta, X, Mdim, Ndim, Kdim, out, status_word, s, &le);
+    if (Ndim > 128) return run_single<256, 2, true, true>(vals, hw_meta, X, Mdim, Ndim, Kdim, out, status_word, s, &le);
+    return run_single<128, 3, true, true>(vals, hw_meta, X, Mdim, Ndim, Kdim, out, status_word, s, &le);
+  }
+  if (many) return run_dense_pair_persistent<true>(vals, X, Mdim, Ndim, Kdim, out, status_word, s, &le);
+  if (Ndim > 128) return run_single<256, 2, false, true>(vals, nullptr, X, Mdim, Ndim, Kdim, out, status_word, s, &le);
+  return run_single<128, 3, false, true>(vals, nullptr, X, Mdim, Ndim, Kdim, out, status_word, s, &le);
 }
 
 }  // namespace bimask
