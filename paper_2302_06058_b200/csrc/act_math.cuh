@@ -32,75 +32,134 @@ __device__ __forceinline__ float min_nan(float a, float b) {
   return y;
 }
 
+// The largest of three magnitudes, NaN if any is one.
+__device__ __forceinline__ float max_abs3(float a, float b, float c) {
+  float y;
+  asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(y) : "f"(a), "f"(b), "f"(c));
+  return y;
+}
+
+// Two fp32 numbers in one register pair: one instruction for both, each rounded as by the scalar one.
+struct Pair { unsigned long long v; };
+__device__ __forceinline__ Pair pair(float lo, float hi) {
+  Pair p;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(p.v) : "f"(lo), "f"(hi));
+  return p;
+}
+__device__ __forceinline__ Pair both(float x) { return pair(x, x); }
+__device__ __forceinline__ void split(Pair p, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(p.v)); }
+__device__ __forceinline__ Pair fma2(Pair a, Pair b, Pair c) {
+  Pair d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+  return d;
+}
+__device__ __forceinline__ Pair mul2(Pair a, Pair b) {
+  Pair d;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d.v) : "l"(a.v), "l"(b.v));
+  return d;
+}
+__device__ __forceinline__ Pair add2(Pair a, Pair b) {
+  Pair d;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d.v) : "l"(a.v), "l"(b.v));
+  return d;
+}
+template <typename F>
+__device__ __forceinline__ Pair map2(Pair a, F f) {
+  float x, y;
+  split(a, x, y);
+  return pair(f(x), f(y));
+}
+
 constexpr float LOG2E = 1.4426950408889634f;
 constexpr float GELU_C = 0.7978845608028654f;            // sqrt(2 / pi)
 constexpr float GELU_A = 0.044715f;
 constexpr float INV_SQRT_2PI = 0.3989422804014327f;
 
+// Both GELUs are z times a distribution function F with F(-a) = 1 - F(a), so
+//   z F(z) = max(z, 0) - a t(a),   a = |z|,  t(a) = F(-a),
+// and log2 t is smooth: t = 2^P(a) with a polynomial P, one special-function operation where e^x and a reciprocal (or
+// an error function) would take two and more.  P is the minimax fit of a t(a) (of 0.3 t(a) below a = 0.3, which keeps
+// small results exact in their leading digits), by linear programming on a dense grid, held near log2 t further out and
+// below -127 at CUT, where a is cut off: there 2^P is flushed to 0, and infinity times 0 cannot arise.  The error of
+// a t(a) in fp32 is 1.5e-7 (normal, degree 6) and 2.5e-7 (tanh form, degree 8).
+struct NormalTail {                                       // t(a) = erfc(a / sqrt 2) / 2
+  static constexpr float CUT = 13.5f;
+  static constexpr int N = 7;
+  static __device__ __forceinline__ constexpr float c(int i) {
+    constexpr float k[N] = {-1.00000101f, -1.15111779f, -0.459027313f, -0.0530767738f, 0.00787010158f, -0.00070691381f, 2.61608362e-05f};
+    return k[i];
+  }
+};
+struct TanhTail {                                         // t(a) = (1 - tanh(c (a + 0.044715 a^3))) / 2
+  static constexpr float CUT = 9.4f;
+  static constexpr int N = 9;
+  static __device__ __forceinline__ constexpr float c(int i) {
+    constexpr float k[N] = {-0.999997816f, -1.15116158f, -0.459060495f, -0.0511946513f, 0.00609492494f, 0.00223345144f,
+                            -0.00187715303f, 0.000335500797f, -1.86449501e-05f};
+    return k[i];
+  }
+};
+template <typename T>
+__device__ __forceinline__ float tail(float a) {          // a in [0, CUT]
+  float p = T::c(T::N - 1);
+#pragma unroll
+  for (int i = T::N - 2; i >= 0; --i) p = fmaf(p, a, T::c(i));
+  return ex2(p);
+}
+template <typename T>
+__device__ __forceinline__ float cut(float z) { return min_nan(fabsf(z), T::CUT); }
+
 // sigma(x) = 1 / (1 + e^-x); e^-x = inf for very negative x gives 0
 __device__ __forceinline__ float sigmoid(float x) { return rcp(1.0f + ex2(-LOG2E * x)); }
 
-// Phi(z) = erfc(-z / sqrt 2) / 2 by formula 7.1.26 of Abramowitz and Stegun: with x = |z| / sqrt 2 and
-// t = 1 / (1 + 0.3275911 x), erfc(x) = t (a1 + t (a2 + t (a3 + t (a4 + t a5)))) e^(-x^2) to 1.5e-7.  The factor
-// e^(-z^2 / 2) is handed back too: it is the density's.
-__device__ __forceinline__ float normal_cdf(float z, float& gauss) {
-  const float a = fabsf(z);
-  const float t = rcp(fmaf(0.3275911f * 0.7071067811865476f, a, 1.0f));
-  gauss = ex2(-0.5f * LOG2E * z * z);
-  float p = fmaf(1.061405429f * 0.5f, t, -1.453152027f * 0.5f);
-  p = fmaf(p, t, 1.421413741f * 0.5f);
-  p = fmaf(p, t, -0.284496736f * 0.5f);
-  p = fmaf(p, t, 0.254829592f * 0.5f);
-  const float tail = p * t * gauss;                       // Phi(-|z|)
-  return z < 0.0f ? tail : 1.0f - tail;
+__device__ __forceinline__ float relu(float z) { return max_nan(z, 0.0f); }
+__device__ __forceinline__ float gelu(float z) {
+  const float a = cut<NormalTail>(z);
+  return fmaf(-a, tail<NormalTail>(a), relu(z));
 }
-
-__device__ __forceinline__ float relu(float z) { return z > 0.0f ? z : (z != z ? z : 0.0f); }
-__device__ __forceinline__ float gelu(float z) { float g; return z * normal_cdf(z, g); }
-__device__ __forceinline__ float gelu_tanh(float z) {     // z (1 + tanh u) / 2 = z sigma(2 u), u = c (z + a z^3)
-  return z * sigmoid(2.0f * GELU_C * z * fmaf(GELU_A * z, z, 1.0f));
+__device__ __forceinline__ float gelu_tanh(float z) {
+  const float a = cut<TanhTail>(z);
+  return fmaf(-a, tail<TanhTail>(a), relu(z));
 }
 __device__ __forceinline__ float silu(float z) { return z * sigmoid(z); }
 
+// Slopes.  With m(a) = t(a) - a f(a), f the density, the slope is m for negative and 1 - m for positive arguments.
+__device__ __forceinline__ float from_tail(float z, float m) { return z < 0.0f ? m : 1.0f - m; }
 __device__ __forceinline__ float relu_slope(float z) { return z > 0.0f ? 1.0f : (z != z ? z : 0.0f); }
 __device__ __forceinline__ float gelu_slope(float z) {
-  float g;
-  const float c = normal_cdf(z, g);
-  return fmaf(INV_SQRT_2PI * g, z, c);
+  const float a = cut<NormalTail>(z);
+  return from_tail(z, fmaf(-a * INV_SQRT_2PI, ex2(-0.5f * LOG2E * a * a), tail<NormalTail>(a)));
 }
-__device__ __forceinline__ float gelu_tanh_slope(float z) {
-  z = min_nan(max_nan(z, -16.0f), 16.0f);                 // 0 and 1 to fp32 beyond: keeps z^2 times 0 finite
-  const float s = sigmoid(2.0f * GELU_C * z * fmaf(GELU_A * z, z, 1.0f));
-  return fmaf(z * s * (1.0f - s), 2.0f * GELU_C * fmaf(3.0f * GELU_A * z, z, 1.0f), s);
+__device__ __forceinline__ float gelu_tanh_slope(float z) {        // f = t (1 - t) 2 c (1 + 3 * 0.044715 a^2)
+  const float a = cut<TanhTail>(z);
+  const float t = tail<TanhTail>(a);
+  return from_tail(z, fmaf(-a * t * (1.0f - t), 2.0f * GELU_C * fmaf(3.0f * GELU_A * a, a, 1.0f), t));
 }
-__device__ __forceinline__ float silu_slope(float z) {
-  z = min_nan(max_nan(z, -128.0f), 128.0f);
-  const float s = sigmoid(z);
-  return s * fmaf(z, 1.0f - s, 1.0f);
+__device__ __forceinline__ float silu_slope(float z) {             // f = t (1 - t)
+  const float a = min_nan(fabsf(z), 128.0f);
+  const float t = sigmoid(-a);
+  return from_tail(z, fmaf(-a * t, 1.0f - t, t));
 }
 
-// f over an array, the activation chosen once for all of it
-template <int N>
-__device__ __forceinline__ void apply(int kind, float (&z)[N]) {
-  switch (kind) {
-    case BIMASK_ACT_RELU:
+// ---- the same on pairs ----
+__device__ __forceinline__ Pair sigmoid2(Pair minus_log2e_x) {     // of -log2(e) x
+  return map2(add2(map2(minus_log2e_x, [](float v) { return ex2(v); }), both(1.0f)), [](float v) { return rcp(v); });
+}
+__device__ __forceinline__ Pair relu2(Pair z) { return map2(z, [](float v) { return max_nan(v, 0.0f); }); }
+template <typename T>
+__device__ __forceinline__ Pair gelu2(Pair z) {
+  const Pair a = map2(z, [](float v) { return cut<T>(v); });
+  Pair p = both(T::c(T::N - 1));
 #pragma unroll
-      for (int i = 0; i < N; ++i) z[i] = relu(z[i]);
-      break;
-    case BIMASK_ACT_GELU:
-#pragma unroll
-      for (int i = 0; i < N; ++i) z[i] = gelu(z[i]);
-      break;
-    case BIMASK_ACT_GELU_TANH:
-#pragma unroll
-      for (int i = 0; i < N; ++i) z[i] = gelu_tanh(z[i]);
-      break;
-    case BIMASK_ACT_SILU:
-#pragma unroll
-      for (int i = 0; i < N; ++i) z[i] = silu(z[i]);
-      break;
-    default: break;
-  }
+  for (int i = T::N - 2; i >= 0; --i) p = fma2(p, a, both(T::c(i)));
+  return fma2(map2(a, [](float v) { return -v; }), map2(p, [](float v) { return ex2(v); }), relu2(z));
+}
+__device__ __forceinline__ Pair silu2(Pair z) { return mul2(z, sigmoid2(mul2(z, both(-LOG2E)))); }
+
+template <int KIND>
+__device__ __forceinline__ Pair value2(Pair z) {
+  return KIND == BIMASK_ACT_RELU ? relu2(z) : KIND == BIMASK_ACT_GELU ? gelu2<NormalTail>(z) : KIND == BIMASK_ACT_GELU_TANH ? gelu2<TanhTail>(z)
+         : KIND == BIMASK_ACT_SILU ? silu2(z) : z;
 }
 
 template <int KIND>
@@ -136,7 +195,8 @@ __device__ __forceinline__ float inverse_scale(uint32_t s) { return __uint_as_fl
 __device__ __forceinline__ float scale_value(uint32_t s) { return __uint_as_float(s == 255u ? 0x7FC00000u : s << 23); }
 
 // Round x / 2^(s-127) to the nearest integer (ties to even): it is the low byte of the result's bits.
-__device__ __forceinline__ uint32_t round_bits(float x, float inv) { return __float_as_uint(fmaf(x, inv, 12582912.0f)); }
+constexpr float ROUNDER = 12582912.0f;                    // 1.5 * 2^23
+__device__ __forceinline__ uint32_t round_bits(float x, float inv) { return __float_as_uint(fmaf(x, inv, ROUNDER)); }
 
 // bytes 0..3 of w as fp32 integers times the scale.  The byte plus 128 goes into the low bits of 2^23: exact.
 __device__ __forceinline__ void decode4(uint32_t w, float scale, float* out) {

@@ -8,6 +8,7 @@
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <atomic>
+#include <type_traits>
 
 namespace bimask {
 
@@ -334,33 +335,40 @@ __device__ __forceinline__ void store_finish() { ptx::bulk_wait_read<0>(); }
 // kernels).
 struct EpiParams {
   const float* bias;        // Mdim, or null
-  int act;                  // BIMASK_ACT_*
+  int mode;                 // 3 BIMASK_ACT_* + 0 (no residual), 1 (residual), 2 (residual and checkpoint)
   int has_res;              // residual R, [Ndim][Mdim] bf16, through its tensor map
   int8_t* zq;               // checkpoint of D + b, [Ndim][Mdim], or null
   uint8_t* zs;              // its scales, [Ndim][Mdim / 32]
 };
 
+// The epilogue's arithmetic takes several times the instructions of a plain drain (20 to 30 per result with GELU and a
+// checkpoint), and two warps per scheduler do not cover its latencies: the EPI kernels have sixteen draining warps in four
+// groups.  Two groups share a RING of staging tiles and its store thread (ring r holds the chunks r, r + 2, ... of every
+// tile); the ring's running chunk number n decides which of its two groups takes the chunk (n % 2).
+constexpr int LIN_EPI_WARPS = 16;
+constexpr int LIN_THREADS = 64 + 32 * LIN_EPI_WARPS + 32 * EPI_GROUPS;
+
 // Checkpoint of one warp's chunk: 32 rows = one block of 32 channels, 32 tokens.  `z` in the accumulator-fragment
-// layout (lane = 4 a + b: index 16 h + 4 g + 2 j + e is row 16 h + 8 j + a, token 8 g + 2 b + e).
+// layout (lane = 4 a + b: pair 8 h + 2 g + j holds row 16 h + 8 j + a, tokens 8 g + 2 b + {0, 1}).
 //   scales: the maximum of a token's 32 values is four registers and the eight lanes that share b; the halving exchange
 //           (two tokens per register, half of the registers sent away at each step) takes 4 shuffles, handing the
-//           eight scale bytes back to every lane 2.
+//           inverse scales of its eight tokens (powers of two, exact in bf16) back to every lane 3.
 //   bytes:  two bytes of a token (rows a and a + 8 of a half) make a 16-bit element, which stmatrix transposes like
 //           any other; a lane reads back the 16 bytes of half a block, undoes the pairing and stores them: a token's 32
 //           bytes are one whole sector.
 // `area`: 32 token rows of 128 bytes of which this warp may use units u0, u0 + 1 (16 bytes each, XOR token mod 8) as
 // scratch.  q_out / s_out: where token 0's block and scale go; ntok: tokens of the chunk that exist.
-__device__ __forceinline__ void emit_checkpoint(const float (&z)[32], uint32_t area, uint32_t u0, int lane, int8_t* q_out, size_t q_pitch,
-                                                uint8_t* s_out, size_t s_pitch, int ntok) {
+__device__ __forceinline__ void emit_checkpoint(const act::Pair (&z)[16], uint32_t area, uint32_t u0, int lane, int8_t* q_out,
+                                                size_t q_pitch, uint8_t* s_out, size_t s_pitch, int ntok) {
   uint32_t p[4];
 #pragma unroll
   for (int g = 0; g < 4; ++g) {
-    float m[2];
+    float v[4][2];
 #pragma unroll
-    for (int e = 0; e < 2; ++e)
-      m[e] = act::max_nan(act::max_nan(fabsf(z[4 * g + e]), fabsf(z[4 * g + 2 + e])),
-                          act::max_nan(fabsf(z[16 + 4 * g + e]), fabsf(z[16 + 4 * g + 2 + e])));
-    p[g] = ckpt::up16(m[0]) | (ckpt::up16(m[1]) << 16);
+    for (int m = 0; m < 4; ++m) act::split(z[8 * (m >> 1) + 2 * g + (m & 1)], v[m][0], v[m][1]);
+    const float m0 = act::max_abs3(act::max_abs3(v[0][0], v[1][0], v[2][0]), v[3][0], 0.0f);
+    const float m1 = act::max_abs3(act::max_abs3(v[0][1], v[1][1], v[2][1]), v[3][1], 0.0f);
+    p[g] = __byte_perm(__float_as_uint(m0) + 0xFFFFu, __float_as_uint(m1) + 0xFFFFu, 0x7632);   // both rounded up to 16 bits
   }
   const bool hi = (lane & 16) != 0, mid = (lane & 8) != 0;
   uint32_t k0 = hi ? p[2] : p[0], k1 = hi ? p[3] : p[1];
@@ -369,25 +377,28 @@ __device__ __forceinline__ void emit_checkpoint(const float (&z)[32], uint32_t a
   uint32_t k = mid ? k1 : k0;
   k = __vmaxu2(k, __shfl_xor_sync(0xFFFFFFFFu, mid ? k0 : k1, 8));
   k = __vmaxu2(k, __shfl_xor_sync(0xFFFFFFFFu, k, 4));     // tokens 8 g + 2 b + {0, 1}, g = lane / 8
-  const uint32_t s0 = ckpt::scale_of(k & 0xFFFFu), s1 = ckpt::scale_of(k >> 16);
+  // ckpt::scale_of on both halves: `raw` is the scale of a finite block, the or'ed part is 255 where a block is not
+  const uint32_t raw = __vmaxu2(((k + 0x00010001u) >> 7) & 0x01FF01FFu, 0x00070007u) - 0x00060006u;
+  const uint32_t over = (k + 0x00800080u) & 0x80008000u;
+  const uint32_t s2 = raw | ((over >> 7) - (over >> 15));
   const int st = 8 * (lane >> 3) + 2 * (lane & 3) + ((lane >> 2) & 1);
-  if (st < ntok) s_out[(size_t)st * s_pitch] = (uint8_t)((lane & 4) ? s1 : s0);
-  const uint32_t both = s0 | (s1 << 8);
-  const uint32_t o8 = __shfl_xor_sync(0xFFFFFFFFu, both, 8);
-  const uint32_t quad = mid ? (o8 | (both << 16)) : (both | (o8 << 16));
-  const uint32_t o16 = __shfl_xor_sync(0xFFFFFFFFu, quad, 16);
-  const uint32_t sc[2] = {hi ? o16 : quad, hi ? quad : o16};      // bytes 2 (g & 1) + e of sc[g >> 1]
+  if (st < ntok) s_out[(size_t)st * s_pitch] = (uint8_t)((lane & 4) ? s2 >> 16 : s2);
+  const uint32_t inv2 = (0x00FE00FEu - raw) << 7;         // 2^(127 - s) of both tokens, as bf16
+  const uint32_t o8 = __shfl_xor_sync(0xFFFFFFFFu, inv2, 8);
+  const uint32_t g0 = mid ? o8 : inv2, g1 = mid ? inv2 : o8;
+  const uint32_t h0 = __shfl_xor_sync(0xFFFFFFFFu, g0, 16), h1 = __shfl_xor_sync(0xFFFFFFFFu, g1, 16);
+  const uint32_t invs[4] = {hi ? h0 : g0, hi ? h1 : g1, hi ? g0 : h0, hi ? g1 : h1};
   uint32_t w[8];                                          // w[2 g + h]: low half token e = 0, high half e = 1
 #pragma unroll
   for (int g = 0; g < 4; ++g) {
-    const float i0 = ckpt::inverse_scale((sc[g >> 1] >> (16 * (g & 1))) & 0xFFu);
-    const float i1 = ckpt::inverse_scale((sc[g >> 1] >> (16 * (g & 1) + 8)) & 0xFFu);
+    const act::Pair inv = act::pair(bf16_lo(invs[g]), bf16_hi(invs[g]));
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      const float* v = &z[16 * h + 4 * g];
-      const uint32_t e0 = __byte_perm(ckpt::round_bits(v[0], i0), ckpt::round_bits(v[2], i0), 0x0040);
-      const uint32_t e1 = __byte_perm(ckpt::round_bits(v[1], i1), ckpt::round_bits(v[3], i1), 0x0040);
-      w[2 * g + h] = __byte_perm(e0, e1, 0x5410);
+      float a0, a1, b0, b1;
+      act::split(act::fma2(z[8 * h + 2 * g], inv, act::both(ckpt::ROUNDER)), a0, a1);
+      act::split(act::fma2(z[8 * h + 2 * g + 1], inv, act::both(ckpt::ROUNDER)), b0, b1);
+      w[2 * g + h] = __byte_perm(__byte_perm(__float_as_uint(a0), __float_as_uint(b0), 0x0040),
+                                 __byte_perm(__float_as_uint(a1), __float_as_uint(b1), 0x0040), 0x5410);
     }
   }
   const uint32_t lt = (uint32_t)lane & 7u, li = (uint32_t)lane >> 3;   // stmatrix: lane 8 i + k addresses token k of matrix i
@@ -399,7 +410,7 @@ __device__ __forceinline__ void emit_checkpoint(const float (&z)[32], uint32_t a
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
     const int t = 16 * i + (lane & 15), h = lane >> 4;
-    const uint4 v = ptx::ld_shared_v4(area + (uint32_t)t * 128u + (((u0 + (uint32_t)h) ^ ((uint32_t)t & 7u)) << 4));
+    const uint4 v = ptx::ld_shared_v4(area + (uint32_t)t * 128u + (((u0 + (uint32_t)h) ^ lt) << 4));
     if (t < ntok)
       *reinterpret_cast<uint4*>(q_out + (size_t)t * q_pitch + 16 * h) =
           make_uint4(__byte_perm(v.x, v.y, 0x6420), __byte_perm(v.z, v.w, 0x6420), __byte_perm(v.x, v.y, 0x7531), __byte_perm(v.z, v.w, 0x7531));
@@ -407,88 +418,126 @@ __device__ __forceinline__ void emit_checkpoint(const float (&z)[32], uint32_t a
   __syncwarp();                                           // the scratch area is the warp's again
 }
 
-// drain_chunks_tma with the epilogue applied.  With a residual, `freed[t]` is completed by the arrival of the residual
-// tile of the chunk in staging tile t (store_chunks_epi loads it there as soon as the tile's last store has read it), so
-// it is waited for on every use; ldmatrix reads the tile in the fragment layout that stmatrix then writes back.
-// x0: first row of the CTA's 128; y0: first token of chunk 0.
+// act(z) + residual, packed to bf16 and staged: straight-line code for each combination.  RES 1: the residual is in the
+// staging tile on entry and is read in the fragment layout that stmatrix writes back; 2: it has been read into `res`
+// already.  `dst`: this lane's stmatrix row for token group 0.
+template <int ACT, int RES>
+__device__ __forceinline__ void emit_result(const act::Pair (&z)[16], uint32_t dst, const uint32_t (&res)[16]) {
+#pragma unroll
+  for (int g = 0; g < 4; ++g) {
+    uint32_t y[4];                                        // matrix m: rows 8 m + a, tokens 8 g + 2 b + {0, 1}
+    if (RES == 1) ptx::ldmatrix_x4_trans(dst + 1024u * g, y[0], y[1], y[2], y[3]);
+#pragma unroll
+    for (int m = 0; m < 4; ++m) {
+      act::Pair v = act::value2<ACT>(z[8 * (m >> 1) + 2 * g + (m & 1)]);
+      if (RES != 0) {
+        const uint32_t r = RES == 1 ? y[m] : res[4 * g + m];
+        v = act::add2(v, act::pair(bf16_lo(r), bf16_hi(r)));
+      }
+      float lo, hi;
+      act::split(v, lo, hi);
+      y[m] = pack_bf16_f(lo, hi);
+    }
+    if (RES == 1) __syncwarp();                           // all lanes have read these eight tokens
+    ptx::stmatrix_x4_trans(dst + 1024u * g, y[0], y[1], y[2], y[3]);
+  }
+}
+
+// The bias of a draining warp's rows in the fragment layout: rows 8 k + lane / 4 of the 32 from row0 on.  Loaded before
+// the accumulator is waited for.
+__device__ __forceinline__ void epi_bias(const float* bias, int row0, int Mdim, int lane, float (&b)[4]) {
+#pragma unroll
+  for (int k = 0; k < 4; ++k) b[k] = (bias != nullptr && row0 < Mdim) ? __ldg(bias + row0 + 8 * k + (lane >> 2)) : 0.f;
+}
+
+// One tile's share of a draining warp: the ring's chunks of this tile are c = ring, ring + 2, ... (`first`: the ring's
+// index for this tile, 0 or 1; they carry the running numbers n0, n0 + 1, ...), and the group takes those whose number
+// is `sub` modulo 2.  n0 is advanced by the ring's count.
+// With a residual, `freed[t]` is completed by the arrival of the residual tile of the chunk in staging tile t
+// (store_chunks_epi loads it there as soon as the tile's last store has read it), so it is waited for on every use;
+// ldmatrix reads the tile in the fragment layout that stmatrix then writes back.
+// b: epi_bias of the warp's rows; x0: first row of the CTA's 128; y0: first token of chunk 0.
 template <int NT>
-__device__ __forceinline__ bool drain_chunks_epi(uint32_t acc, int c0, int cstep, int nchunks, uint32_t release_bar, uint32_t stg,
-                                                 uint32_t bars, uint32_t& u, int q, int lane, const EpiParams& e, int x0, int y0,
-                                                 int Mdim, int Ndim, volatile int* abort_flag) {
-  if (c0 >= nchunks) { release_accumulator(release_bar, lane); return true; }
+__device__ __forceinline__ bool drain_chunks_epi(uint32_t acc, int first, int sub, int nchunks, uint32_t release_bar, uint32_t stg,
+                                                 uint32_t bars, uint32_t& n0, int q, int lane, const EpiParams& e,
+                                                 const float (&b)[4], int x0, int y0, int Mdim, int Ndim, volatile int* abort_flag) {
+  const int count = (nchunks - first + 1) / 2;
+  uint32_t n = n0 + (((uint32_t)sub - n0) & 1u);           // the group's first chunk of this tile
+  const uint32_t end = n0 + (uint32_t)count;
+  if (n >= end) { release_accumulator(release_bar, lane); n0 = end; return true; }
   const uint32_t half = stg + (uint32_t)(q >> 1) * 4096u;
   const uint32_t dst = half + (uint32_t)(lane & 7) * 128u +
                        ((((uint32_t)(4 * (q & 1)) + ((uint32_t)lane >> 3)) ^ ((uint32_t)lane & 7u)) << 4);
   const int row0 = x0 + 32 * q;                           // this warp's 32 rows all exist or none does
   const bool rows_ok = row0 < Mdim;
-  float b[4];
-#pragma unroll
-  for (int k = 0; k < 4; ++k) b[k] = (e.bias != nullptr && rows_ok) ? __ldg(e.bias + row0 + 8 * k + (lane >> 2)) : 0.f;
   bool ok = true;
-  drain_loop<32>(acc, c0, cstep, nchunks, false, release_bar, lane, [&](const uint32_t (&r)[32], int c) {
-    const uint32_t slot = u % NT, use = u / NT;
-    ++u;
-    float z[32];
+#pragma unroll 1
+  for (; n < end; n += 2) {
+    const int c = first + 2 * (int)(n - n0);
+    const uint32_t slot = n % NT, use = n / NT;
+    act::Pair z[16];
+    {
+      uint32_t r[32];
+      epi_load<32>(acc + 32 * c, r, false);
+      ptx::tmem_ld_wait();
+      if (n + 2 >= end) release_accumulator(release_bar, lane);
 #pragma unroll
-    for (int i = 0; i < 32; ++i) z[i] = __uint_as_float(r[i]) + b[2 * (i >> 4) + ((i >> 1) & 1)];
+      for (int i = 0; i < 16; ++i)
+        z[i] = act::add2(act::pair(__uint_as_float(r[2 * i]), __uint_as_float(r[2 * i + 1])), act::both(b[2 * (i >> 3) + (i & 1)]));
+    }
     if (ok) {
       if (e.has_res) ok = ptx::mbar_wait_bounded(bars + 8u * (NT + slot), use & 1u, abort_flag, WAIT_BUDGET);
       else if (use > 0) ok = ptx::mbar_wait_bounded(bars + 8u * (NT + slot), (use - 1u) & 1u, abort_flag, WAIT_BUDGET);
     }
     __syncwarp();
+    const uint32_t tile = slot * 8192u;
     uint32_t res[16];
-    if (e.has_res) {
+    if (e.zq != nullptr) {
+      if (e.has_res) {                                    // the checkpoint's scratch is where the residual lies
 #pragma unroll
-      for (int g = 0; g < 4; ++g) ptx::ldmatrix_x4_trans(dst + slot * 8192u + 1024u * g, res[4 * g], res[4 * g + 1], res[4 * g + 2], res[4 * g + 3]);
-      __syncwarp();
-    }
-    if (e.zq != nullptr && rows_ok) {
+        for (int g = 0; g < 4; ++g) ptx::ldmatrix_x4_trans(dst + tile + 1024u * g, res[4 * g], res[4 * g + 1], res[4 * g + 2], res[4 * g + 3]);
+        __syncwarp();
+      }
       const int t0 = y0 + 32 * c;
-      emit_checkpoint(z, half + slot * 8192u, 4u * (q & 1), lane, e.zq + (size_t)t0 * Mdim + row0, (size_t)Mdim,
-                      e.zs + (size_t)t0 * (Mdim >> 5) + (row0 >> 5), (size_t)(Mdim >> 5), Ndim - t0);
+      emit_checkpoint(z, half + tile, 4u * (q & 1), lane, e.zq + (size_t)t0 * Mdim + row0, (size_t)Mdim,
+                      e.zs + (size_t)t0 * (Mdim >> 5) + (row0 >> 5), (size_t)(Mdim >> 5), rows_ok ? Ndim - t0 : 0);
     }
-    act::apply(e.act, z);
-    if (e.has_res) {
-#pragma unroll
-      for (int g = 0; g < 4; ++g)
-#pragma unroll
-        for (int m = 0; m < 4; ++m) {                     // matrix m: rows 8 m + a
-          z[16 * (m >> 1) + 4 * g + 2 * (m & 1)] += bf16_lo(res[4 * g + m]);
-          z[16 * (m >> 1) + 4 * g + 2 * (m & 1) + 1] += bf16_hi(res[4 * g + m]);
-        }
+    switch (e.mode) {
+#define BIMASK_EMIT(m) case m: emit_result<m / 3, m % 3>(z, dst + tile, res); break;
+      BIMASK_EMIT(0) BIMASK_EMIT(1) BIMASK_EMIT(2) BIMASK_EMIT(3) BIMASK_EMIT(4) BIMASK_EMIT(5) BIMASK_EMIT(6) BIMASK_EMIT(7)
+      BIMASK_EMIT(8) BIMASK_EMIT(9) BIMASK_EMIT(10) BIMASK_EMIT(11) BIMASK_EMIT(12) BIMASK_EMIT(13) BIMASK_EMIT(14)
+#undef BIMASK_EMIT
     }
-    uint32_t out[32];
-#pragma unroll
-    for (int i = 0; i < 32; ++i) out[i] = __float_as_uint(z[i]);
-    epi_stage<32, 1024u>(out, dst + slot * 8192u);
     ptx::fence_proxy_async();
     __syncwarp();
     if (lane == 0) ptx::mbar_arrive(bars + 8u * slot);
-  });
+  }
+  n0 = end;
   return ok;
 }
 
-// The store thread's side: chunk n of the group (over all its tiles) goes to rows x0.., tokens y.. as coord(n, x0, y)
-// says, false past the last one.  With a residual it also loads the residual tile of chunk n + NT into the staging tile
-// of chunk n once that chunk's store has read it.
-template <int NT, typename Coord>
+// The store thread's side.  `walk` yields the ring's chunks one after the other, over all its tiles: next(x0, y) gives
+// the first row and token, false past the last.  With a residual a second copy of it runs NT chunks ahead: the residual
+// tile of chunk n + NT is loaded into the staging tile of chunk n once that chunk's store has read it.
+template <int NT, typename Walk>
 __device__ __forceinline__ bool store_chunks_epi(const CUtensorMap* tmapD, const CUtensorMap* tmapR, bool has_res, uint32_t stg,
-                                                 uint32_t bars, int Mdim, int Ndim, volatile int* abort_flag, Coord&& coord) {
+                                                 uint32_t bars, int Mdim, int Ndim, volatile int* abort_flag, Walk walk) {
+  Walk ahead = walk;
   uint32_t loaded = 0;                                    // residual tiles requested so far
-  auto load = [&](uint32_t n) {
+  auto load = [&]() {
     int x0, y;
-    if (!coord(n, x0, y)) return;
-    const uint32_t slot = n % NT, bar = bars + 8u * (NT + slot);
+    if (!ahead.next(x0, y)) return;
+    const uint32_t slot = loaded % NT, bar = bars + 8u * (NT + slot);
     ptx::mbar_expect_tx(bar, 8192);
     ptx::tma_load_2d(stg + slot * 8192u, tmapR, x0, y, bar);
     ptx::tma_load_2d(stg + slot * 8192u + 4096u, tmapR, x0 + 64, y, bar);
     ++loaded;
   };
   if (has_res)
-    for (uint32_t n = 0; n < NT; ++n) load(n);
+    for (uint32_t n = 0; n < NT; ++n) load();
   bool ok = true;
   int x0, y;
-  for (uint32_t n = 0; coord(n, x0, y); ++n) {
+  for (uint32_t n = 0; walk.next(x0, y); ++n) {
     const uint32_t slot = n % NT, use = n / NT;
     ok = ptx::mbar_wait_bounded(bars + 8u * slot, use & 1u, abort_flag, WAIT_BUDGET);
     if (!ok) break;
@@ -499,7 +548,7 @@ __device__ __forceinline__ bool store_chunks_epi(const CUtensorMap* tmapD, const
     ptx::bulk_commit();
     if (n > 0) {
       ptx::bulk_wait_read<1>();
-      if (has_res) load(n - 1 + NT);
+      if (has_res) load();
       else ptx::mbar_arrive(bars + 8u * (NT + (n - 1u) % NT));
     }
   }
@@ -510,6 +559,49 @@ __device__ __forceinline__ bool store_chunks_epi(const CUtensorMap* tmapD, const
   }
   store_finish();
   return ok;
+}
+
+// The chunks of ring `ring` in the order of the draining warps.  A tile is ROWS accumulators of 128 rows of this CTA,
+// `row_step` rows apart, drained one after the other; accumulator m takes the chunks (ring ^ m) & 1, + 2, ...
+template <int ROWS>
+struct ChunkWalk {
+  int tile, step, num_tiles, tiles_m, tiles_n, group;     // the CTA's tiles
+  int rows_per_tile, row_off, row_step, n_tile, ring;
+  int m, c, x0, y0;                                       // position: accumulator and chunk of the current tile
+  __device__ __forceinline__ void enter() {
+    if (tile < num_tiles) {
+      int tile_m, tile_n;
+      raster(tile, tiles_m, tiles_n, group, tile_m, tile_n);
+      x0 = tile_m * rows_per_tile + row_off;
+      y0 = tile_n * n_tile;
+    }
+    m = 0;
+    c = ring;
+  }
+  __device__ __forceinline__ bool next(int& x, int& y) {
+    while (32 * c >= n_tile) {                            // past the accumulator's last chunk
+      if (tile >= num_tiles) return false;
+      if (ROWS > 1 && m + 1 < ROWS) {
+        ++m;
+        c = (ring ^ m) & 1;
+      } else {
+        tile += step;
+        enter();
+      }
+    }
+    if (tile >= num_tiles) return false;
+    x = x0 + m * row_step;
+    y = y0 + 32 * c;
+    c += 2;
+    return true;
+  }
+};
+template <int ROWS>
+__device__ __forceinline__ ChunkWalk<ROWS> chunk_walk(const GemmParams& p, int tile, int step, int num_tiles, int rows_per_tile, int row_off,
+                                                      int row_step, int n_tile, int ring) {
+  ChunkWalk<ROWS> w{tile, step, num_tiles, p.tiles_m, p.tiles_n, p.raster_group, rows_per_tile, row_off, row_step, n_tile, ring, 0, 0, 0, 0};
+  w.enter();
+  return w;
 }
 
 // ---- host helpers (gemm_host.cu) -----------------------------------------------------------

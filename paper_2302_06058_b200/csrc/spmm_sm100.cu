@@ -28,11 +28,12 @@ namespace {
 // CONV: the token operand is fetched as shifted pixel boxes (see ConvGeom); N_TILE tokens = one box.
 // EPI (in all three kernels of this file): the epilogue of a linear layer (EpiParams; tmapR: its residual).
 template <int N_TILE, int STAGES, bool SPARSE, bool CONV, bool EPI = false>
-__global__ void __launch_bounds__(PAIR_THREADS, 1)
+__global__ void __launch_bounds__(EPI ? LIN_THREADS : PAIR_THREADS, 1)
 spmm_single_kernel(const __grid_constant__ CUtensorMap tmapA, const __grid_constant__ CUtensorMap tmapB,
                    const __grid_constant__ CUtensorMap tmapD, const GemmParams p, const __grid_constant__ CUtensorMap tmapR,
                    const EpiParams e) {
   static_assert(!(CONV && EPI), "the implicit convolution has no epilogue");
+  constexpr int DRAIN_WARPS = EPI ? LIN_EPI_WARPS : EPI_WARPS;
   pdl_launch_dependents();
   using C = Cfg<N_TILE, STAGES, SPARSE>;
   extern __shared__ uint8_t smem_raw[];
@@ -171,9 +172,11 @@ spmm_single_kernel(const __grid_constant__ CUtensorMap tmapA, const __grid_const
       }
       if (ok) ptx::tc_commit(tmem_full_bar);
     }
-  } else if (warp < 2 + EPI_WARPS) {
+  } else if (warp < 2 + DRAIN_WARPS) {
     // ------------------------------ epilogue ------------------------------
     const int q = warp & 3;                               // TMEM lane quadrant this warp may read
+    float bias[4];
+    if (EPI) epi_bias(e.bias, m0 + 32 * q, p.Mdim, lane, bias);
     bool ok = true;
     if (num_kt > 0) ok = ptx::mbar_wait_bounded(tmem_full_bar, 0, abort_flag, WAIT_BUDGET);
     if (!ok) *abort_flag = 1;
@@ -194,9 +197,10 @@ spmm_single_kernel(const __grid_constant__ CUtensorMap tmapA, const __grid_const
           return outp + conv_out_pixel(p.conv, n, h, w) * p.Mdim + m0;
         });
       } else if constexpr (EPI) {
-        uint32_t u = 0;
-        if (!drain_chunks_epi<C::EPI_NT>(tmem_base + ((uint32_t)(32 * q) << 16), eg, EPI_GROUPS, N_TILE / 32, 0u,
-                                         staging + eg * (C::EPI_NT * 8192), epi_bars_of<C::EPI_NT>(bar_base, eg), u, q, lane, e, m0, n0,
+        uint32_t n = 0;
+        const int ring = eg & 1;
+        if (!drain_chunks_epi<C::EPI_NT>(tmem_base + ((uint32_t)(32 * q) << 16), ring, eg >> 1, N_TILE / 32, 0u,
+                                         staging + ring * (C::EPI_NT * 8192), epi_bars_of<C::EPI_NT>(bar_base, ring), n, q, lane, e, bias, m0, n0,
                                          p.Mdim, p.Ndim, abort_flag))
           *abort_flag = 1;
       } else {
@@ -210,14 +214,11 @@ spmm_single_kernel(const __grid_constant__ CUtensorMap tmapA, const __grid_const
   } else if (!CONV) {
     // ------------------------------ store threads: one per epilogue group ------------------------------
     if (ptx::elect_one()) {
-      const int g = warp - 2 - EPI_WARPS;
+      const int g = warp - 2 - DRAIN_WARPS;
       if constexpr (EPI) {
         if (!store_chunks_epi<C::EPI_NT>(&tmapD, &tmapR, e.has_res != 0, staging + g * (C::EPI_NT * 8192), epi_bars_of<C::EPI_NT>(bar_base, g),
-                                         p.Mdim, p.Ndim, abort_flag, [&](uint32_t n, int& x0, int& y) {
-              const int c = g + EPI_GROUPS * (int)n;
-              x0 = m0; y = n0 + 32 * c;
-              return c < N_TILE / 32;
-            }))
+                                         p.Mdim, p.Ndim, abort_flag,
+                                         chunk_walk<1>(p, (int)blockIdx.x, (int)gridDim.x, (int)gridDim.x, C::M_TILE, 0, 0, N_TILE, g)))
           *abort_flag = 1;
       } else {
       uint32_t u = 0;
@@ -267,12 +268,13 @@ struct PairPCfg {
 // hold): a 256 x 128 A tile per stage as two 64-wide boxes per CTA, eight K = 16 MMAs, no metadata, and two
 // accumulators at every N (tmapE is not used).
 template <int STAGES, bool CONV, bool SPARSE = true, bool EPI = false>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PAIR_THREADS, 1)
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(EPI ? LIN_THREADS : PAIR_THREADS, 1)
 spmm_pair_persistent_kernel(const __grid_constant__ CUtensorMap tmapA, const __grid_constant__ CUtensorMap tmapB,
                             const __grid_constant__ CUtensorMap tmapE, const __grid_constant__ CUtensorMap tmapD,
                             const GemmParams p, const __grid_constant__ CUtensorMap tmapR, const EpiParams e) {
   static_assert(SPARSE || !CONV, "the implicit convolution runs on 2:4 operands only");
   static_assert(!(CONV && EPI), "the implicit convolution has no epilogue");
+  constexpr int DRAIN_WARPS = EPI ? LIN_EPI_WARPS : EPI_WARPS;
   pdl_launch_dependents();
   using C = PairPCfg<STAGES, SPARSE>;
   extern __shared__ uint8_t smem_raw[];
@@ -307,7 +309,7 @@ spmm_pair_persistent_kernel(const __grid_constant__ CUtensorMap tmapA, const __g
     }
     for (int b = 0; b < 2; ++b) {
       ptx::mbar_init(tmem_full_bar(b), 1);
-      ptx::mbar_init(tmem_empty_bar(b), 2 * EPI_WARPS);   // the epilogue warps of both CTAs of the pair
+      ptx::mbar_init(tmem_empty_bar(b), 2 * DRAIN_WARPS);   // the epilogue warps of both CTAs of the pair
     }
     epi_bars_init<C::EPI_NT>(bar_base);
     ptx::fence_barrier_init();
@@ -419,13 +421,14 @@ spmm_pair_persistent_kernel(const __grid_constant__ CUtensorMap tmapA, const __g
         if (ok) ptx::tc_commit_pair(tmem_full_bar(buf), 3);
       }
     }
-  } else if (warp < 2 + EPI_WARPS) {
+  } else if (warp < 2 + DRAIN_WARPS) {
     // Each epilogue warp reads 32 accumulator rows (its TMEM lane quadrant); the four warps of a group share
     // the group's staging tiles.
     const int q = warp & 3;
     const int eg = (warp - 2) >> 2;                        // EPI_GROUPS groups of four warps take chunks in turn
-    const uint32_t stg = staging + eg * (C::EPI_NT * 8192);
-    const uint32_t ebars = epi_bars_of<C::EPI_NT>(bar_base, eg);
+    const int ring = EPI ? eg & 1 : eg;                    // staging tiles: one set per group, or (EPI) per two groups
+    const uint32_t stg = staging + ring * (C::EPI_NT * 8192);
+    const uint32_t ebars = epi_bars_of<C::EPI_NT>(bar_base, ring);
     uint16_t* outp = reinterpret_cast<uint16_t*>(p.out);
     uint32_t tcount = 0, u = 0;
     for (int tile = cluster_id; tile < num_tiles; tile += num_clusters, ++tcount) {
@@ -433,6 +436,8 @@ spmm_pair_persistent_kernel(const __grid_constant__ CUtensorMap tmapA, const __g
       raster(tile, p.tiles_m, p.tiles_n, p.raster_group, tile_m, tile_n);
       const int m0 = (2 * tile_m + (int)rank) * 128, n0 = tile_n * SP_N;
       const uint32_t buf = tcount % nbuf;
+      float bias[4];
+      if (EPI) epi_bias(e.bias, m0 + 32 * q, p.Mdim, lane, bias);
       bool ok = ptx::mbar_wait_bounded(tmem_full_bar(buf), (tcount / nbuf) & 1u, abort_flag, WAIT_BUDGET);
       ok = ptx::named_bar_and(1 + eg, 128, ok);            // the four warps of a group go on or give up together
       if (!ok) { *abort_flag = 1; break; }
@@ -455,7 +460,7 @@ spmm_pair_persistent_kernel(const __grid_constant__ CUtensorMap tmapA, const __g
           return outp + conv_out_pixel(p.conv, n, h, w) * p.Mdim + m0;
         });
       } else if constexpr (EPI) {
-        if (!drain_chunks_epi<C::EPI_NT>(acc, eg, EPI_GROUPS, nchunks, release_bar, stg, ebars, u, q, lane, e, m0, n0, p.Mdim, p.Ndim,
+        if (!drain_chunks_epi<C::EPI_NT>(acc, ring, eg >> 1, nchunks, release_bar, stg, ebars, u, q, lane, e, bias, m0, n0, p.Mdim, p.Ndim,
                                          abort_flag)) {
           *abort_flag = 1;
           break;
@@ -469,22 +474,12 @@ spmm_pair_persistent_kernel(const __grid_constant__ CUtensorMap tmapA, const __g
   } else if (!CONV) {
     // store threads, one per epilogue group: the same walk over tiles and chunks as the group's draining warps
     if (ptx::elect_one()) {
-      const int g = warp - 2 - EPI_WARPS;
+      const int g = warp - 2 - DRAIN_WARPS;
       const uint32_t stg = staging + g * (C::EPI_NT * 8192);
       const uint32_t ebars = epi_bars_of<C::EPI_NT>(bar_base, g);
       if constexpr (EPI) {
-        const int per_tile = (SP_N / 32 - g + 1) / 2;      // the group's chunks of a tile
         if (!store_chunks_epi<C::EPI_NT>(&tmapD, &tmapR, e.has_res != 0, stg, ebars, p.Mdim, p.Ndim, abort_flag,
-                                         [&](uint32_t n, int& x0, int& y) {
-              if (per_tile <= 0) return false;
-              const int nt = (int)n / per_tile, tile = cluster_id + nt * num_clusters;
-              if (tile >= num_tiles) return false;
-              int tile_m, tile_n;
-              raster(tile, p.tiles_m, p.tiles_n, p.raster_group, tile_m, tile_n);
-              x0 = (2 * tile_m + (int)rank) * 128;
-              y = tile_n * SP_N + 32 * (g + 2 * ((int)n - nt * per_tile));
-              return true;
-            }))
+                                         chunk_walk<1>(p, cluster_id, num_clusters, num_tiles, 256, 128 * (int)rank, 0, SP_N, g)))
           *abort_flag = 1;
       } else {
       uint32_t u = 0;
@@ -541,10 +536,11 @@ struct Pair2MCfg {
 };
 
 template <int STAGES, bool EPI = false>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(GEMM2M_THREADS, 1)
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(EPI ? LIN_THREADS : GEMM2M_THREADS, 1)
 spmm_pair2m_kernel(const __grid_constant__ CUtensorMap tmapA, const __grid_constant__ CUtensorMap tmapB,
                    const __grid_constant__ CUtensorMap tmapE, const __grid_constant__ CUtensorMap tmapD,
                    const GemmParams p, const __grid_constant__ CUtensorMap tmapR, const EpiParams e) {
+  constexpr int DRAIN_WARPS = EPI ? LIN_EPI_WARPS : EPI_WARPS;
   pdl_launch_dependents();
   using C = Pair2MCfg<STAGES>;
   extern __shared__ uint8_t smem_raw[];
@@ -578,8 +574,8 @@ spmm_pair2m_kernel(const __grid_constant__ CUtensorMap tmapA, const __grid_const
       ptx::mbar_init(empty_bar(s), 1);
     }
     ptx::mbar_init(tmem_full_bar, 1);
-    ptx::mbar_init(tmem_empty_bar0, 2 * EPI_WARPS);       // the epilogue warps of both CTAs of the pair
-    ptx::mbar_init(tmem_empty_bar1, 2 * EPI_WARPS);
+    ptx::mbar_init(tmem_empty_bar0, 2 * DRAIN_WARPS);       // the epilogue warps of both CTAs of the pair
+    ptx::mbar_init(tmem_empty_bar1, 2 * DRAIN_WARPS);
     epi_bars_init<C::EPI_NT>(bar_base);
     ptx::fence_barrier_init();
     ptx::prefetch_tmap(&tmapA);
@@ -681,29 +677,35 @@ spmm_pair2m_kernel(const __grid_constant__ CUtensorMap tmapA, const __grid_const
         if (ok) ptx::tc_commit_pair(tmem_full_bar, 3);
       }
     }
-  } else if (warp < 2 + EPI_WARPS) {
+  } else if (warp < 2 + DRAIN_WARPS) {
     // two groups of four epilogue warps (one warp per tensor-memory lane quadrant); both groups drain accumulator 0
     // first, taking alternate 32-token chunks, then accumulator 1: accumulator 0 is free again at half time, which
     // is what lets the next tile's first MMAs start under the second half of the drain
     const int q = warp & 3;
-    const int g = (warp - 2) >> 2;
+    const int eg = (warp - 2) >> 2, g = EPI ? eg & 1 : eg;   // EPI: four groups, two per set of staging tiles
     const uint32_t stg = staging + g * (C::EPI_NT * 8192);
     const uint32_t ebars = epi_bars_of<C::EPI_NT>(bar_base, g);
     uint32_t u = 0;
     const uint32_t release0 = ptx::mapa(tmem_empty_bar0, 0), release1 = ptx::mapa(tmem_empty_bar1, 0);
     uint32_t tcount = 0;
     for (int tile = cluster_id; tile < num_tiles; tile += num_clusters, ++tcount) {
+      int tile_m = 0, tile_n = 0;
+      float bias[2][4];
+      if (EPI) {
+        raster(tile, p.tiles_m, p.tiles_n, p.raster_group, tile_m, tile_n);
+        for (int mt = 0; mt < 2; ++mt) epi_bias(e.bias, mt128_of(tile_m, mt) * 128 + 32 * q, p.Mdim, lane, bias[mt]);
+      }
       bool ok = ptx::mbar_wait_bounded(tmem_full_bar, tcount & 1u, abort_flag, WAIT_BUDGET);
-      ok = ptx::named_bar_and(1 + g, 128, ok);             // the four warps of a group go on or give up together
+      ok = ptx::named_bar_and(1 + eg, 128, ok);            // the four warps of a group go on or give up together
       if (!ok) { *abort_flag = 1; break; }
       ptx::tc_fence_after();
 #pragma unroll 1
       for (int mt = 0; mt < 2; ++mt) {
         const uint32_t acc = tmem_base + 256u * mt + ((uint32_t)(32 * q) << 16);
         if constexpr (EPI) {
-          int tile_m, tile_n;
-          raster(tile, p.tiles_m, p.tiles_n, p.raster_group, tile_m, tile_n);
-          if (!drain_chunks_epi<C::EPI_NT>(acc, (g ^ mt) & 1, 2, SP_N / 32, mt ? release1 : release0, stg, ebars, u, q, lane, e,
+          float b[4];
+          for (int k = 0; k < 4; ++k) b[k] = mt ? bias[1][k] : bias[0][k];
+          if (!drain_chunks_epi<C::EPI_NT>(acc, (g ^ mt) & 1, eg >> 1, SP_N / 32, mt ? release1 : release0, stg, ebars, u, q, lane, e, b,
                                            mt128_of(tile_m, mt) * 128, tile_n * SP_N, p.Mdim, p.Ndim, abort_flag))
             *abort_flag = 1;
         } else if (!drain_chunks_tma<32, C::EPI_NT>(acc, (g ^ mt) & 1, 2, SP_N / 32, false, mt ? release1 : release0, stg, ebars, u, q,
@@ -715,22 +717,12 @@ spmm_pair2m_kernel(const __grid_constant__ CUtensorMap tmapA, const __grid_const
   } else {
     // store threads, one per epilogue group: the same walk over tiles, row tiles and chunks as the group's draining warps
     if (ptx::elect_one()) {
-      const int g = warp - 2 - EPI_WARPS;
+      const int g = warp - 2 - DRAIN_WARPS;
       const uint32_t stg = staging + g * (C::EPI_NT * 8192);
       const uint32_t ebars = epi_bars_of<C::EPI_NT>(bar_base, g);
       if constexpr (EPI) {
-        const int nchunks = SP_N / 32, first = (nchunks - g + 1) / 2;   // the group's chunks of row tile 0; the rest of nchunks are row tile 1's
         if (!store_chunks_epi<C::EPI_NT>(&tmapD, &tmapR, e.has_res != 0, stg, ebars, p.Mdim, p.Ndim, abort_flag,
-                                         [&](uint32_t n, int& x0, int& y) {
-              const int nt = (int)n / nchunks, tile = cluster_id + nt * num_clusters;
-              if (tile >= num_tiles) return false;
-              int tile_m, tile_n;
-              raster(tile, p.tiles_m, p.tiles_n, p.raster_group, tile_m, tile_n);
-              const int r = (int)n - nt * nchunks, mt = r >= first ? 1 : 0;
-              x0 = mt128_of(tile_m, mt) * 128;
-              y = tile_n * SP_N + 32 * (((g ^ mt) & 1) + 2 * (mt ? r - first : r));
-              return true;
-            }))
+                                         chunk_walk<2>(p, cluster_id, num_clusters, num_tiles, 512, 128 * (int)rank, 256, SP_N, g)))
           *abort_flag = 1;
       } else {
       uint32_t u = 0;
@@ -763,7 +755,8 @@ int epi_args(const LinearEpilogue* le, int Mdim, int Ndim, const CUtensorMap& un
   *tr = unused;
   *e = EpiParams{};
   if (le == nullptr) return BIMASK_OK;
-  e->bias = le->bias; e->act = le->act; e->has_res = le->res != nullptr; e->zq = le->zq; e->zs = le->zs;
+  e->bias = le->bias; e->has_res = le->res != nullptr; e->zq = le->zq; e->zs = le->zs;
+  e->mode = 3 * le->act + (le->res == nullptr ? 0 : le->zq == nullptr ? 1 : 2);
   return le->res != nullptr ? make_tmap(tr, le->res, (uint64_t)Mdim, (uint64_t)Ndim, 32) : BIMASK_OK;
 }
 
@@ -794,7 +787,7 @@ int run_single(const uint16_t* vals, const void* hw_meta, const uint16_t* Bop, i
   p.tiles_n = (Ndim + N_TILE - 1) / N_TILE;
   p.raster_group = 16;
   dim3 grid(p.tiles_m * p.tiles_n, 1, 1);
-  BIMASK_CUDA_OK(launch_pdl(kern, grid, PAIR_THREADS, C::SMEM_BYTES, s, ta, tb, td, p, tr, e));
+  BIMASK_CUDA_OK(launch_pdl(kern, grid, EPI ? LIN_THREADS : PAIR_THREADS, C::SMEM_BYTES, s, ta, tb, td, p, tr, e));
   count_launch();
   BIMASK_CUDA_OK(cudaGetLastError());
   return BIMASK_OK;
@@ -855,7 +848,7 @@ int run_sparse_pair_persistent(const uint16_t* vals, const void* hw_meta, const 
   p.raster_group = 8;
   const int total = p.tiles_m * p.tiles_n;
   const int clusters = total < sms / 2 ? total : sms / 2;
-  BIMASK_CUDA_OK(launch_pdl(kern, 2 * clusters, PAIR_THREADS, C::SMEM_BYTES, s, ta, tb, te, td, p, tr, e));
+  BIMASK_CUDA_OK(launch_pdl(kern, 2 * clusters, EPI ? LIN_THREADS : PAIR_THREADS, C::SMEM_BYTES, s, ta, tb, te, td, p, tr, e));
   count_launch();
   BIMASK_CUDA_OK(cudaGetLastError());
   return BIMASK_OK;
@@ -911,7 +904,7 @@ int run_sparse_pair2m(const uint16_t* vals, const void* hw_meta, const uint16_t*
   p.raster_group = 8;
   const int total = p.tiles_m * p.tiles_n;
   const int clusters = total < sms / 2 ? total : sms / 2;
-  BIMASK_CUDA_OK(launch_pdl(kern, 2 * clusters, GEMM2M_THREADS, C::SMEM_BYTES, s, ta, tb, te, td, p, tr, e));
+  BIMASK_CUDA_OK(launch_pdl(kern, 2 * clusters, EPI ? LIN_THREADS : GEMM2M_THREADS, C::SMEM_BYTES, s, ta, tb, te, td, p, tr, e));
   count_launch();
   BIMASK_CUDA_OK(cudaGetLastError());
   return BIMASK_OK;
@@ -1101,7 +1094,7 @@ int run_dense_pair_persistent(const uint16_t* A, const uint16_t* Bop, int Mdim, 
   p.raster_group = 8;
   const int total = p.tiles_m * p.tiles_n;
   const int clusters = total < sms / 2 ? total : sms / 2;
-  BIMASK_CUDA_OK(launch_pdl(kern, 2 * clusters, PAIR_THREADS, C::SMEM_BYTES, s, ta, tb, ta /* no metadata */, td, p, tr, e));
+  BIMASK_CUDA_OK(launch_pdl(kern, 2 * clusters, EPI ? LIN_THREADS : PAIR_THREADS, C::SMEM_BYTES, s, ta, tb, ta /* no metadata */, td, p, tr, e));
   count_launch();
   BIMASK_CUDA_OK(cudaGetLastError());
   return BIMASK_OK;
