@@ -141,6 +141,17 @@ __device__ __forceinline__ float silu_slope(float z) {             // f = t (1 -
   return from_tail(z, fmaf(-a * t, 1.0f - t, t));
 }
 
+// one activation, chosen at run time
+__device__ __forceinline__ float value_of(int kind, float z) {
+  switch (kind) {
+    case BIMASK_ACT_RELU: return relu(z);
+    case BIMASK_ACT_GELU: return gelu(z);
+    case BIMASK_ACT_GELU_TANH: return gelu_tanh(z);
+    case BIMASK_ACT_SILU: return silu(z);
+    default: return z;
+  }
+}
+
 // ---- the same on pairs ----
 __device__ __forceinline__ Pair sigmoid2(Pair minus_log2e_x) {     // of -log2(e) x
   return map2(add2(map2(minus_log2e_x, [](float v) { return ex2(v); }), both(1.0f)), [](float v) { return rcp(v); });

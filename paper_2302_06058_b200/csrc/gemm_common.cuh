@@ -546,10 +546,12 @@ __device__ __forceinline__ bool store_chunks_epi(const CUtensorMap* tmapD, const
       if (x0 + 64 < Mdim) ptx::tma_store_2d(tmapD, x0 + 64, y, stg + slot * 8192u + 4096u);
     }
     ptx::bulk_commit();
-    if (n > 0) {
-      ptx::bulk_wait_read<1>();
+    // With two tiles, one per group, a tile is handed back as soon as its store has read it: its group cannot go on
+    // before (1 % on the 16384-row layers).  With three, the wait goes under the next store (5 % on the ViT layers).
+    if (NT <= 2 || n > 0) {
+      ptx::bulk_wait_read<(NT <= 2 ? 0 : 1)>();
       if (has_res) load();
-      else ptx::mbar_arrive(bars + 8u * (NT + (n - 1u) % NT));
+      else ptx::mbar_arrive(bars + 8u * (NT + (NT <= 2 ? slot : (n - 1u) % NT)));
     }
   }
   if (!ok && has_res) {                                   // giving up: no load may be in flight when the kernel ends

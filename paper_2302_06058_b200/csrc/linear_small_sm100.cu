@@ -1,0 +1,256 @@
+// A linear layer for few tokens (at most 128): the form of generation and of small batches.  Its time is the reading of
+// the weights, so the work is cut along the reduction as well: a cluster of `splits` CTAs owns 128 rows x N_TILE tokens,
+// each streams its share of the k tiles through a deep ring of stages (the same TMA -> tcgen05.mma pipeline as the large
+// products), leaves its fp32 partial sums in its own shared memory, and after a cluster barrier the CTAs add one another's
+// parts over distributed shared memory, token by token in rank order -- no workspace, no second kernel, and a result that
+// does not depend on timing -- and finish the layer on them: bias, checkpoint, activation, residual, one rounding.
+#include "gemm_common.cuh"
+
+namespace bimask {
+
+namespace {
+
+constexpr int SMALL_THREADS = 256;                       // warp 0 TMA, warp 1 MMA, warps 2-5 drain; all eight finish
+
+template <int N_TILE, int STAGES, bool SPARSE>
+struct SmallCfg {
+  static constexpr int A_BYTES = SPARSE ? 16384 : 32768;
+  static constexpr int B_BYTES = N_TILE * 256;
+  static constexpr int E_BYTES = SPARSE ? 2048 : 0;
+  static constexpr int STAGE_BYTES = A_BYTES + B_BYTES + E_BYTES;
+  static constexpr int PART_BYTES = N_TILE * 512;        // [token][128 rows] fp32, over the stages once they are done with
+  static constexpr int TMEM_COLS = N_TILE + 4 <= 64 ? 64 : N_TILE + 4 <= 128 ? 128 : 256;
+  static constexpr int SMEM_BYTES = STAGES * STAGE_BYTES + 1024 + 256;
+  static_assert(PART_BYTES <= STAGES * STAGE_BYTES, "the partial sums lie over the stages");
+};
+
+struct SmallParams {
+  const uint8_t* hw_meta;
+  int tiles_k, k_per_split, tiles_m;
+  int Mdim, Ndim;
+  const float* bias;
+  int act;
+  const uint16_t* res;
+  uint16_t* out;
+  int8_t* zq;
+  uint8_t* zs;
+  int32_t* status_word;
+};
+
+template <int N_TILE, int STAGES, bool SPARSE>
+__global__ void __launch_bounds__(SMALL_THREADS, 1)
+linear_small_kernel(const __grid_constant__ CUtensorMap tmapA, const __grid_constant__ CUtensorMap tmapB, const SmallParams p, int splits) {
+  pdl_launch_dependents();
+  using C = SmallCfg<N_TILE, STAGES, SPARSE>;
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t raw = ptx::smem_u32(smem_raw);
+  const uint32_t base = (raw + 1023u) & ~1023u;
+  uint8_t* base_ptr = smem_raw + (base - raw);
+  const uint32_t bar_base = base + STAGES * C::STAGE_BYTES;
+  auto full_bar = [&](int s) { return bar_base + 8u * s; };
+  auto empty_bar = [&](int s) { return bar_base + 8u * (STAGES + s); };
+  const uint32_t tmem_full_bar = bar_base + 8u * (2 * STAGES);
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(base_ptr + STAGES * C::STAGE_BYTES + 8 * (2 * STAGES + 1));
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int rank = (int)ptx::cluster_ctarank();           // = blockIdx.x % splits
+  const int tile = (int)blockIdx.x / splits;
+  const int tile_m = tile % p.tiles_m, tile_n = tile / p.tiles_m;
+  const int m0 = tile_m * 128, n0 = tile_n * N_TILE;
+  const int kt_begin = rank * p.k_per_split;
+  const int num_kt = min(p.tiles_k, kt_begin + p.k_per_split) - kt_begin;   // >= 1: the host leaves no CTA without work
+
+  if (threadIdx.x == 0) {
+    *abort_flag = 0;
+    for (int s = 0; s < STAGES; ++s) {
+      ptx::mbar_init(full_bar(s), 1);
+      ptx::mbar_init(empty_bar(s), 1);
+    }
+    ptx::mbar_init(tmem_full_bar, 1);
+    ptx::fence_barrier_init();
+    ptx::prefetch_tmap(&tmapA);
+    ptx::prefetch_tmap(&tmapB);
+  }
+  if (warp == 1) {
+    ptx::tmem_alloc(ptx::smem_u32(tmem_slot), C::TMEM_COLS);
+    ptx::tmem_relinquish();
+  }
+  ptx::tc_fence_before();
+  __syncthreads();
+  ptx::tc_fence_after();
+  const uint32_t tmem_base = *tmem_slot;
+  const uint32_t tmem_meta = tmem_base + N_TILE;
+  pdl_wait();
+
+  if (warp == 0) {
+    if (ptx::elect_one()) {
+      int it = 0;
+      for (; it < num_kt; ++it) {
+        const int s = it % STAGES;
+        if (!ptx::mbar_wait_bounded(empty_bar(s), ((uint32_t)(it / STAGES) & 1u) ^ 1u, abort_flag, WAIT_BUDGET)) { *abort_flag = 1; break; }
+        const int kt = kt_begin + it;
+        const uint32_t a_s = base + s * C::STAGE_BYTES, b_s = a_s + C::A_BYTES;
+        ptx::mbar_expect_tx(full_bar(s), C::STAGE_BYTES);
+        if (SPARSE) {
+          ptx::tma_load_2d(a_s, &tmapA, kt * 64, m0, full_bar(s));
+          ptx::bulk_load(b_s + C::B_BYTES, p.hw_meta + ((size_t)tile_m * p.tiles_k + kt) * 2048, 2048, full_bar(s));
+        } else {
+          ptx::tma_load_2d(a_s, &tmapA, kt * 128, m0, full_bar(s));
+          ptx::tma_load_2d(a_s + 16384, &tmapA, kt * 128 + 64, m0, full_bar(s));
+        }
+        ptx::tma_load_2d(b_s, &tmapB, kt * 128, n0, full_bar(s));
+        ptx::tma_load_2d(b_s + N_TILE * 128, &tmapB, kt * 128 + 64, n0, full_bar(s));
+      }
+      if (it < num_kt) {                                  // giving up: no load may be in flight when the CTA ends
+        volatile int none = 0;
+        for (int k = max(0, it - STAGES); k < it; ++k) ptx::mbar_wait_bounded(full_bar(k % STAGES), (uint32_t)(k / STAGES) & 1u, &none, WAIT_BUDGET);
+      }
+    }
+  } else if (warp == 1) {
+    if (ptx::elect_one()) {
+      constexpr uint32_t idesc = ptx::idesc_bf16(128, N_TILE, false, false, SPARSE);
+      bool ok = true;
+      for (int it = 0; it < num_kt; ++it) {
+        const int s = it % STAGES;
+        if (!ptx::mbar_wait_bounded(full_bar(s), (uint32_t)(it / STAGES) & 1u, abort_flag, WAIT_BUDGET)) { *abort_flag = 1; ok = false; break; }
+        ptx::tc_fence_after();
+        const uint32_t a_s = base + s * C::STAGE_BYTES, b_s = a_s + C::A_BYTES;
+        if constexpr (SPARSE) {
+          ptx::tmem_cp_128x128b(tmem_meta, ptx::smem_desc(b_s + C::B_BYTES, 0, 128, 0));
+#pragma unroll
+          for (int kb = 0; kb < 4; ++kb)
+            ptx::mma_sparse(tmem_base, ptx::smem_desc(a_s + kb * 32, 16, 1024, 2),
+                            ptx::smem_desc(b_s + (kb >> 1) * (N_TILE * 128) + (kb & 1) * 64, 16, 1024, 2), tmem_meta + (kb & ~1),
+                            idesc | (uint32_t)(kb & 1), (it | kb) != 0);
+        } else {
+#pragma unroll
+          for (int kb = 0; kb < 8; ++kb)
+            ptx::mma_dense(tmem_base, ptx::smem_desc(a_s + (kb >> 2) * 16384 + (kb & 3) * 32, 16, 1024, 2),
+                           ptx::smem_desc(b_s + (kb >> 2) * (N_TILE * 128) + (kb & 3) * 32, 16, 1024, 2), idesc, (it | kb) != 0);
+        }
+        ptx::tc_commit(empty_bar(s));
+      }
+      if (ok) ptx::tc_commit(tmem_full_bar);
+    }
+  } else if (warp < 6) {
+    // accumulator -> shared memory, [token][row]: lane = row, so a store covers 128 contiguous bytes
+    const int q = warp & 3;
+    const bool ok = ptx::mbar_wait_bounded(tmem_full_bar, 0, abort_flag, WAIT_BUDGET);
+    if (!ok) *abort_flag = 1;
+    ptx::tc_fence_after();
+    __syncwarp();
+    if (__all_sync(0xFFFFFFFFu, ok)) {
+      float* part = reinterpret_cast<float*>(base_ptr) + 32 * q + lane;
+#pragma unroll 1
+      for (int c = 0; c < N_TILE; c += 32) {
+        if (n0 + c >= p.Ndim) break;                      // no such tokens: nobody reads their sums
+        uint32_t r[32];
+        ptx::tmem_ld_32x32(tmem_base + ((uint32_t)(32 * q) << 16) + c, r);
+        ptx::tmem_ld_wait();
+#pragma unroll
+        for (int t = 0; t < 32; ++t) part[(c + t) * 128] = __uint_as_float(r[t]);
+      }
+    }
+  }
+
+  // every CTA's partial sums are in place (or its abort flag is up: then the results are void, and the status says so)
+  ptx::tc_fence_before();
+  __syncthreads();
+  ptx::cluster_sync();
+  if (warp == 1) {
+    ptx::tc_fence_after();
+    ptx::tmem_dealloc(tmem_base, C::TMEM_COLS);
+  }
+  if (threadIdx.x == 0 && *abort_flag) atomicExch(p.status_word, (int32_t)BIMASK_ETIMEOUT);
+
+  // tokens rank, rank + splits, ... are this CTA's to finish, one warp per token: lane = four rows
+  const int ntok = min(N_TILE, p.Ndim - n0);
+  const int row = m0 + 4 * lane;
+  const bool rows_ok = row < p.Mdim;                      // Mdim % 32 == 0: true for whole blocks of eight lanes
+  float4 b = make_float4(0.f, 0.f, 0.f, 0.f);
+  if (p.bias != nullptr && rows_ok) b = __ldg(reinterpret_cast<const float4*>(p.bias + row));
+  for (int t = rank + splits * warp; t < ntok; t += splits * (SMALL_THREADS / 32)) {
+    const size_t at = (size_t)(n0 + t) * p.Mdim + row;
+    uint2 res = make_uint2(0u, 0u);
+    if (p.res != nullptr && rows_ok) res = *reinterpret_cast<const uint2*>(p.res + at);   // may be `out`: a plain load
+    const uint32_t src = base + (uint32_t)(t * 512 + 16 * lane);
+    float4 z = b;
+    for (int s0 = 0; s0 < splits; s0 += 4) {
+      float4 v[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) v[u] = s0 + u < splits ? ptx::ld_cluster_v4(ptx::mapa(src, s0 + u)) : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int u = 0; u < 4; ++u) { z.x += v[u].x; z.y += v[u].y; z.z += v[u].z; z.w += v[u].w; }
+    }
+    if (p.zq != nullptr) {                                // eight lanes = one block of 32 channels
+      uint32_t h = ckpt::up16(act::max_nan(act::max_nan(fabsf(z.x), fabsf(z.y)), act::max_nan(fabsf(z.z), fabsf(z.w))));
+#pragma unroll
+      for (int d = 1; d < 8; d <<= 1) h = max(h, __shfl_xor_sync(0xFFFFFFFFu, h, d));
+      const uint32_t sc = ckpt::scale_of(h);
+      const float inv = ckpt::inverse_scale(sc);
+      const uint32_t lo = __byte_perm(ckpt::round_bits(z.x, inv), ckpt::round_bits(z.y, inv), 0x0040);
+      const uint32_t hi = __byte_perm(ckpt::round_bits(z.z, inv), ckpt::round_bits(z.w, inv), 0x0040);
+      if (rows_ok) {
+        *reinterpret_cast<uint32_t*>(p.zq + at) = __byte_perm(lo, hi, 0x5410);
+        if ((lane & 7) == 0) p.zs[at >> 5] = (uint8_t)sc;
+      }
+    }
+    if (rows_ok)
+      *reinterpret_cast<uint2*>(p.out + at) =
+          make_uint2(pack_bf16_f(act::value_of(p.act, z.x) + bf16_lo(res.x), act::value_of(p.act, z.y) + bf16_hi(res.x)),
+                     pack_bf16_f(act::value_of(p.act, z.z) + bf16_lo(res.y), act::value_of(p.act, z.w) + bf16_hi(res.y)));
+  }
+  __syncthreads();
+  ptx::cluster_sync();                                    // shared memory must outlive the peers' reads of it
+}
+
+template <int N_TILE, int STAGES, bool SPARSE>
+int run_small(const uint16_t* vals, const void* hw_meta, const uint16_t* X, int Mdim, int Ndim, int Kdim, const LinearEpilogue& le,
+              uint16_t* out, int32_t* status_word, cudaStream_t s) {
+  using C = SmallCfg<N_TILE, STAGES, SPARSE>;
+  CUtensorMap ta, tb;
+  int rc;
+  if ((rc = make_tmap(&ta, vals, SPARSE ? (uint64_t)Kdim / 2 : (uint64_t)Kdim, (uint64_t)Mdim, 128)) != BIMASK_OK) return rc;
+  if ((rc = make_tmap(&tb, X, (uint64_t)Kdim, (uint64_t)Ndim, N_TILE)) != BIMASK_OK) return rc;
+  auto kern = linear_small_kernel<N_TILE, STAGES, SPARSE>;
+  if ((rc = set_smem_attr(kern, C::SMEM_BYTES)) != BIMASK_OK) return rc;
+  SmallParams p;
+  p.hw_meta = reinterpret_cast<const uint8_t*>(hw_meta);
+  p.tiles_k = (Kdim + 127) / 128;
+  p.tiles_m = (Mdim + 127) / 128;
+  p.Mdim = Mdim; p.Ndim = Ndim;
+  p.bias = le.bias; p.act = le.act; p.res = le.res; p.out = out; p.zq = le.zq; p.zs = le.zs;
+  p.status_word = status_word;
+  const int tiles = p.tiles_m * ((Ndim + N_TILE - 1) / N_TILE);
+  // As many CTAs as there are SMs, at most eight per cluster (the portable size) and at least four k tiles each.
+  int splits = sm_count() / tiles;
+  if (splits > p.tiles_k / 4) splits = p.tiles_k / 4;
+  if (splits > 8) splits = 8;
+  if (splits < 1) splits = 1;
+  p.k_per_split = (p.tiles_k + splits - 1) / splits;
+  splits = (p.tiles_k + p.k_per_split - 1) / p.k_per_split;
+  BIMASK_CUDA_OK(launch_pdl_cluster(kern, splits * tiles, SMALL_THREADS, splits, C::SMEM_BYTES, s, ta, tb, p, splits));
+  count_launch();
+  BIMASK_CUDA_OK(cudaGetLastError());
+  return BIMASK_OK;
+}
+
+template <bool SPARSE>
+int run_small_any(const uint16_t* vals, const void* hw_meta, const uint16_t* X, int Mdim, int Ndim, int Kdim, const LinearEpilogue& le,
+                  uint16_t* out, int32_t* status_word, cudaStream_t s) {
+  // stages: what fits 220 KB (26 / 34 / 50 KB each, dense 40 / 48 / 64 KB)
+  if (Ndim <= 32) return run_small<32, SPARSE ? 8 : 5, SPARSE>(vals, hw_meta, X, Mdim, Ndim, Kdim, le, out, status_word, s);
+  if (Ndim <= 64) return run_small<64, SPARSE ? 6 : 4, SPARSE>(vals, hw_meta, X, Mdim, Ndim, Kdim, le, out, status_word, s);
+  return run_small<128, SPARSE ? 4 : 3, SPARSE>(vals, hw_meta, X, Mdim, Ndim, Kdim, le, out, status_word, s);
+}
+
+}  // namespace
+
+int launch_linear_small(const uint16_t* vals, const void* hw_meta, const uint16_t* X, int Mdim, int Ndim, int Kdim,
+                        const LinearEpilogue& le, uint16_t* out, int32_t* status_word, cudaStream_t s) {
+  return hw_meta != nullptr ? run_small_any<true>(vals, hw_meta, X, Mdim, Ndim, Kdim, le, out, status_word, s)
+                            : run_small_any<false>(vals, hw_meta, X, Mdim, Ndim, Kdim, le, out, status_word, s);
+}
+
+}  // namespace bimask

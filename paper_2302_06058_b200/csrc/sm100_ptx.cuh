@@ -299,6 +299,13 @@ __device__ __forceinline__ void tc_commit_pair(uint32_t bar, uint16_t cta_mask) 
 }
 
 
+// 16 bytes of another CTA's shared memory (a shared::cluster address).
+__device__ __forceinline__ float4 ld_cluster_v4(uint32_t addr) {
+  float4 v;
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
+  return v;
+}
+
 // ---- epilogue helpers -----------------------------------------------------------------
 // Arrive on an mbarrier given by a shared::cluster address (may be the pair's other CTA).  Relaxed: what the
 // barrier guards is tensor memory, ordered by tcgen05.fence::before_thread_sync; a release at cluster scope made

@@ -1110,20 +1110,18 @@ int launch_dense_nt(const uint16_t* A, const uint16_t* Bop, int Mdim, int Ndim, 
 }
 
 // Linear layer: the product of launch_spmm (hw_meta given) or launch_dense_nt (null) with the epilogue of `le`, on the
-// same kernels by the same rules.
+// same kernels by the same rules; at most 128 tokens go to the kernel for few tokens.
 int launch_linear_fwd(const uint16_t* vals, const void* hw_meta, const uint16_t* X, int Mdim, int Ndim, int Kdim,
                       const LinearEpilogue& le, uint16_t* out, int32_t* status_word, cudaStream_t s) {
-  const bool many = Ndim > 128 && Mdim > 128;
+  if (Ndim <= 128) return launch_linear_small(vals, hw_meta, X, Mdim, Ndim, Kdim, le, out, status_word, s);
   if (hw_meta != nullptr) {
     if (Ndim >= 1024 && Mdim >= 2048 && Kdim >= 4096)
       return run_sparse_pair2m<true>(vals, hw_meta, X, Mdim, Ndim, Kdim, out, status_word, s, &le);
-    if (many) return run_sparse_pair_persistent<true>(vals, hw_meta, X, Mdim, Ndim, Kdim, out, status_word, s, &le);
-    if (Ndim > 128) return run_single<256, 2, true, true>(vals, hw_meta, X, Mdim, Ndim, Kdim, out, status_word, s, &le);
-    return run_single<128, 3, true, true>(vals, hw_meta, X, Mdim, Ndim, Kdim, out, status_word, s, &le);
+    if (Mdim > 128) return run_sparse_pair_persistent<true>(vals, hw_meta, X, Mdim, Ndim, Kdim, out, status_word, s, &le);
+    return run_single<256, 2, true, true>(vals, hw_meta, X, Mdim, Ndim, Kdim, out, status_word, s, &le);
   }
-  if (many) return run_dense_pair_persistent<true>(vals, X, Mdim, Ndim, Kdim, out, status_word, s, &le);
-  if (Ndim > 128) return run_single<256, 2, false, true>(vals, nullptr, X, Mdim, Ndim, Kdim, out, status_word, s, &le);
-  return run_single<128, 3, false, true>(vals, nullptr, X, Mdim, Ndim, Kdim, out, status_word, s, &le);
+  if (Mdim > 128) return run_dense_pair_persistent<true>(vals, X, Mdim, Ndim, Kdim, out, status_word, s, &le);
+  return run_single<256, 2, false, true>(vals, nullptr, X, Mdim, Ndim, Kdim, out, status_word, s, &le);
 }
 
 }  // namespace bimask
