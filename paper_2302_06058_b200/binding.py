@@ -140,9 +140,13 @@ def _ptr(x):
     raise TypeError(type(x))
 
 
+# the handle alone: 0.3 us a call, where building the Stream object takes 3 us, as long as a launch
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda device: torch.cuda.current_stream(device).cuda_stream)
+
+
 def _stream(stream):
     if stream is None:
-        return torch.cuda.current_stream().cuda_stream
+        return _raw_stream(torch.cuda.current_device())
     if isinstance(stream, torch.cuda.Stream):
         return stream.cuda_stream
     return int(stream)

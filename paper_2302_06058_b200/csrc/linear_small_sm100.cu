@@ -157,7 +157,7 @@ linear_small_kernel(const __grid_constant__ CUtensorMap tmapA, const __grid_cons
   // every CTA's partial sums are in place (or its abort flag is up: then the results are void, and the status says so)
   ptx::tc_fence_before();
   __syncthreads();
-  ptx::cluster_sync();
+  if (splits > 1) ptx::cluster_sync();
   if (warp == 1) {
     ptx::tc_fence_after();
     ptx::tmem_dealloc(tmem_base, C::TMEM_COLS);
@@ -202,7 +202,7 @@ linear_small_kernel(const __grid_constant__ CUtensorMap tmapA, const __grid_cons
                      pack_bf16_f(act::value_of(p.act, z.z) + bf16_lo(res.y), act::value_of(p.act, z.w) + bf16_hi(res.y)));
   }
   __syncthreads();
-  ptx::cluster_sync();                                    // shared memory must outlive the peers' reads of it
+  if (splits > 1) ptx::cluster_sync();                    // shared memory must outlive the peers' reads of it
 }
 
 template <int N_TILE, int STAGES, bool SPARSE>
