@@ -71,9 +71,6 @@ __device__ __forceinline__ Pair map2(Pair a, F f) {
 }
 
 constexpr float LOG2E = 1.4426950408889634f;
-constexpr float GELU_C = 0.7978845608028654f;            // sqrt(2 / pi)
-constexpr float GELU_A = 0.044715f;
-constexpr float INV_SQRT_2PI = 0.3989422804014327f;
 
 // Both GELUs are z times a distribution function F with F(-a) = 1 - F(a), so
 //   z F(z) = max(z, 0) - a t(a),   a = |z|,  t(a) = F(-a),
@@ -123,24 +120,6 @@ __device__ __forceinline__ float gelu_tanh(float z) {
 }
 __device__ __forceinline__ float silu(float z) { return z * sigmoid(z); }
 
-// Slopes.  With m(a) = t(a) - a f(a), f the density, the slope is m for negative and 1 - m for positive arguments.
-__device__ __forceinline__ float from_tail(float z, float m) { return z < 0.0f ? m : 1.0f - m; }
-__device__ __forceinline__ float relu_slope(float z) { return z > 0.0f ? 1.0f : (z != z ? z : 0.0f); }
-__device__ __forceinline__ float gelu_slope(float z) {
-  const float a = cut<NormalTail>(z);
-  return from_tail(z, fmaf(-a * INV_SQRT_2PI, ex2(-0.5f * LOG2E * a * a), tail<NormalTail>(a)));
-}
-__device__ __forceinline__ float gelu_tanh_slope(float z) {        // f = t (1 - t) 2 c (1 + 3 * 0.044715 a^2)
-  const float a = cut<TanhTail>(z);
-  const float t = tail<TanhTail>(a);
-  return from_tail(z, fmaf(-a * t * (1.0f - t), 2.0f * GELU_C * fmaf(3.0f * GELU_A * a, a, 1.0f), t));
-}
-__device__ __forceinline__ float silu_slope(float z) {             // f = t (1 - t)
-  const float a = min_nan(fabsf(z), 128.0f);
-  const float t = sigmoid(-a);
-  return from_tail(z, fmaf(-a * t, 1.0f - t, t));
-}
-
 // one activation, chosen at run time
 __device__ __forceinline__ float value_of(int kind, float z) {
   switch (kind) {
@@ -178,10 +157,53 @@ __device__ __forceinline__ float value(float z) {
   return KIND == BIMASK_ACT_RELU ? relu(z) : KIND == BIMASK_ACT_GELU ? gelu(z) : KIND == BIMASK_ACT_GELU_TANH ? gelu_tanh(z)
          : KIND == BIMASK_ACT_SILU ? silu(z) : z;
 }
+// Slopes.  With m(a) = t(a) - a f(a), f the density, the slope is m(a) for negative and 1 - m(a) for positive arguments:
+// 1/2 + (1/2 - m(a)) with the sign of z.  For the GELUs m(a) = e^(-a^2/2) P(a): m over the normal density is smooth and P is
+// the minimax fit of m, by linear programming; errors in fp32 3.1e-7 (degree 9) and 1.5e-7 (tanh form, degree 10).
+struct NormalSlope {
+  static constexpr int N = 10;
+  static __device__ __forceinline__ constexpr float c(int i) {
+    constexpr float k[N] = {0.499999743f, -0.797864899f, 0.249752293f, -0.131772884f, 0.0594967943f, -0.0222308766f, 0.00638280561f,
+                            -0.00127116217f, 0.000151941892f, -8.06307163e-06f};
+    return k[i];
+  }
+};
+struct TanhSlope {
+  static constexpr int N = 11;
+  static __device__ __forceinline__ constexpr float c(int i) {
+    constexpr float k[N] = {0.499999899f, -0.797877544f, 0.249918295f, -0.131275385f, 0.0614912298f, -0.0257054393f, 0.00879214436f,
+                            -0.00278788268f, 0.000777319758f, -0.000125037125f, 7.79687128e-06f};
+    return k[i];
+  }
+};
+__device__ __forceinline__ Pair signed_half(Pair z, Pair half_minus_m) {    // 1/2 + the second, given the signs of the first
+  float x, y, a, b;
+  split(z, x, y);
+  split(half_minus_m, a, b);
+  return add2(pair(__uint_as_float(__float_as_uint(a) ^ (__float_as_uint(x) & 0x80000000u)),
+                   __uint_as_float(__float_as_uint(b) ^ (__float_as_uint(y) & 0x80000000u))), both(0.5f));
+}
+template <typename S>
+__device__ __forceinline__ Pair gelu_slope2(Pair z) {
+  const Pair a = map2(z, [](float v) { return cut<NormalTail>(v); });       // the exponential is 0 in fp32 from there on
+  const Pair g = map2(mul2(mul2(a, both(-0.5f * LOG2E)), a), [](float v) { return ex2(v); });
+  Pair p = both(-S::c(S::N - 1));
+#pragma unroll
+  for (int i = S::N - 2; i >= 0; --i) p = fma2(p, a, both(-S::c(i)));
+  return signed_half(z, fma2(p, g, both(0.5f)));
+}
+__device__ __forceinline__ Pair silu_slope2(Pair z) {                       // t = sigma(-a), f = t (1 - t)
+  const Pair a = map2(z, [](float v) { return min_nan(fabsf(v), 128.0f); });
+  const Pair t = sigmoid2(mul2(a, both(LOG2E)));
+  const Pair f = fma2(mul2(t, both(-1.0f)), t, t);
+  return signed_half(z, add2(fma2(a, f, both(0.5f)), mul2(t, both(-1.0f))));
+}
+__device__ __forceinline__ Pair relu_slope2(Pair z) { return map2(z, [](float v) { return v > 0.0f ? 1.0f : (v != v ? v : 0.0f); }); }
+
 template <int KIND>
-__device__ __forceinline__ float slope(float z) {
-  return KIND == BIMASK_ACT_RELU ? relu_slope(z) : KIND == BIMASK_ACT_GELU ? gelu_slope(z)
-         : KIND == BIMASK_ACT_GELU_TANH ? gelu_tanh_slope(z) : KIND == BIMASK_ACT_SILU ? silu_slope(z) : 1.0f;
+__device__ __forceinline__ Pair slope2(Pair z) {
+  return KIND == BIMASK_ACT_RELU ? relu_slope2(z) : KIND == BIMASK_ACT_GELU ? gelu_slope2<NormalSlope>(z)
+         : KIND == BIMASK_ACT_GELU_TANH ? gelu_slope2<TanhSlope>(z) : silu_slope2(z);
 }
 
 }  // namespace act
@@ -209,14 +231,12 @@ __device__ __forceinline__ float scale_value(uint32_t s) { return __uint_as_floa
 constexpr float ROUNDER = 12582912.0f;                    // 1.5 * 2^23
 __device__ __forceinline__ uint32_t round_bits(float x, float inv) { return __float_as_uint(fmaf(x, inv, ROUNDER)); }
 
-// bytes 0..3 of w as fp32 integers times the scale.  The byte plus 128 goes into the low bits of 2^23: exact.
-__device__ __forceinline__ void decode4(uint32_t w, float scale, float* out) {
+// bytes 0..3 of w times the scale, as two pairs.  The byte plus 128 goes into the low bits of 2^23: exact.
+__device__ __forceinline__ void decode4(uint32_t w, act::Pair scale, act::Pair* out) {
   const uint32_t u = w ^ 0x80808080u;
-  const float bias = -8388736.0f;                         // -(2^23 + 128)
-  out[0] = (__uint_as_float(__byte_perm(u, 0x4B000000u, 0x7540)) + bias) * scale;
-  out[1] = (__uint_as_float(__byte_perm(u, 0x4B000000u, 0x7541)) + bias) * scale;
-  out[2] = (__uint_as_float(__byte_perm(u, 0x4B000000u, 0x7542)) + bias) * scale;
-  out[3] = (__uint_as_float(__byte_perm(u, 0x4B000000u, 0x7543)) + bias) * scale;
+  const act::Pair bias = act::both(-8388736.0f);          // -(2^23 + 128)
+  out[0] = act::mul2(act::add2(act::pair(__uint_as_float(__byte_perm(u, 0x4B000000u, 0x7540)), __uint_as_float(__byte_perm(u, 0x4B000000u, 0x7541))), bias), scale);
+  out[1] = act::mul2(act::add2(act::pair(__uint_as_float(__byte_perm(u, 0x4B000000u, 0x7542)), __uint_as_float(__byte_perm(u, 0x4B000000u, 0x7543))), bias), scale);
 }
 
 }  // namespace ckpt
@@ -225,7 +245,13 @@ __device__ __forceinline__ uint32_t pack_bf16_f(float lo, float hi) {
   const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
   return *reinterpret_cast<const uint32_t*>(&v);
 }
+__device__ __forceinline__ uint32_t pack_bf16_p(act::Pair v) {
+  float lo, hi;
+  act::split(v, lo, hi);
+  return pack_bf16_f(lo, hi);
+}
 __device__ __forceinline__ float bf16_lo(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float bf16_hi(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
+__device__ __forceinline__ act::Pair bf16_pair(uint32_t w) { return act::pair(bf16_lo(w), bf16_hi(w)); }
 
 }  // namespace bimask

@@ -30,7 +30,7 @@ __host__ __device__ constexpr int epi_staging_bytes(int nt) { return EPI_GROUPS 
 constexpr uint32_t EPI_BAR_OFFSET = 128;
 
 
-template <int N_TILE, int STAGES, bool SPARSE = true>
+template <int N_TILE, int STAGES, bool SPARSE = true, bool EPI = false>
 struct Cfg {
   static constexpr int M_TILE = 128;
   static constexpr int K_TILE = 128;                             // logical reduction elements per stage
@@ -39,7 +39,7 @@ struct Cfg {
   static constexpr int E_BYTES = SPARSE ? 2048 : 0;
   static constexpr int STAGE_BYTES = A_BYTES + B_BYTES + E_BYTES;
   static constexpr int META_COLS = SPARSE ? 4 : 0;
-  static constexpr int EPI_NT = SPARSE ? 3 : 2;                  // staging tiles per epilogue group (the dense stages leave room for two)
+  static constexpr int EPI_NT = SPARSE && !EPI ? 3 : 2;          // staging tiles per epilogue group (the dense stages leave room for two; EPI: even, see below)
   static constexpr int TMEM_COLS = (N_TILE + META_COLS) <= 128 ? 128 : (N_TILE + META_COLS) <= 256 ? 256 : 512;
   static constexpr int SMEM_BYTES = STAGES * STAGE_BYTES + 1024 /* alignment slack */ + 256 /* barriers */ +
                                     epi_staging_bytes(EPI_NT) /* epilogue staging */;
@@ -344,7 +344,9 @@ struct EpiParams {
 // The epilogue's arithmetic takes several times the instructions of a plain drain (20 to 30 per result with GELU and a
 // checkpoint), and two warps per scheduler do not cover its latencies: the EPI kernels have sixteen draining warps in four
 // groups.  Two groups share a RING of staging tiles and its store thread (ring r holds the chunks r, r + 2, ... of every
-// tile); the ring's running chunk number n decides which of its two groups takes the chunk (n % 2).
+// tile); the ring's running chunk number n decides which of its two groups takes the chunk (n % 2).  The number of tiles
+// per ring is even, so that a tile always serves the same group: an mbarrier's parity tells a waiter only about the phase
+// after the last one it saw, and a group that came back to a tile two uses later could pass too early.
 constexpr int LIN_EPI_WARPS = 16;
 constexpr int LIN_THREADS = 64 + 32 * LIN_EPI_WARPS + 32 * EPI_GROUPS;
 
@@ -461,6 +463,7 @@ template <int NT>
 __device__ __forceinline__ bool drain_chunks_epi(uint32_t acc, int first, int sub, int nchunks, uint32_t release_bar, uint32_t stg,
                                                  uint32_t bars, uint32_t& n0, int q, int lane, const EpiParams& e,
                                                  const float (&b)[4], int x0, int y0, int Mdim, int Ndim, volatile int* abort_flag) {
+  static_assert(NT % 2 == 0, "a staging tile serves one group");
   const int count = (nchunks - first + 1) / 2;
   uint32_t n = n0 + (((uint32_t)sub - n0) & 1u);           // the group's first chunk of this tile
   const uint32_t end = n0 + (uint32_t)count;
@@ -547,7 +550,7 @@ __device__ __forceinline__ bool store_chunks_epi(const CUtensorMap* tmapD, const
     }
     ptx::bulk_commit();
     // With two tiles, one per group, a tile is handed back as soon as its store has read it: its group cannot go on
-    // before (1 % on the 16384-row layers).  With three, the wait goes under the next store (5 % on the ViT layers).
+    // before (1 % on the 16384-row layers).  With four, the wait goes under the next store.
     if (NT <= 2 || n > 0) {
       ptx::bulk_wait_read<(NT <= 2 ? 0 : 1)>();
       if (has_res) load();

@@ -44,97 +44,132 @@ ckpt_pack_kernel(const uint4* __restrict__ x, long long halves, uint4* __restric
   }
 }
 
-// The values of a checkpoint, through an activation or as they are: 16 channels per thread.
+// The values of a checkpoint, through an activation or as they are.  Eight channels per thread and step, so that the 16-byte
+// stores of a warp are contiguous (16 channels as two stores of every other 16 bytes: 84 us for 8192 x 16384 through
+// an activation, now 72); two steps' bytes are loaded at a time.
 template <int ACT>
 __global__ void __launch_bounds__(STREAM_THREADS)
-ckpt_unpack_kernel(const uint4* __restrict__ q, const uint8_t* __restrict__ s, long long halves, uint4* __restrict__ x) {
+ckpt_unpack_kernel(const uint2* __restrict__ q, const uint8_t* __restrict__ s, long long eighths, uint4* __restrict__ x) {
   pdl_launch_dependents();
   pdl_wait();
+  constexpr int U = 2;
   const long long step = (long long)gridDim.x * STREAM_THREADS;
-  for (long long i = (long long)blockIdx.x * STREAM_THREADS + threadIdx.x; i < halves; i += step) {
-    const uint4 v = __ldg(q + i);
-    const float sc = ckpt::scale_value(__ldg(s + (i >> 1)));
-    float z[16];
-    ckpt::decode4(v.x, sc, z); ckpt::decode4(v.y, sc, z + 4); ckpt::decode4(v.z, sc, z + 8); ckpt::decode4(v.w, sc, z + 12);
-    uint32_t o[8];
+  for (long long i0 = (long long)blockIdx.x * STREAM_THREADS + threadIdx.x; i0 < eighths; i0 += U * step) {
+    uint2 v[U];
+    uint32_t sb[U];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) o[k] = pack_bf16_f(act::value<ACT>(z[2 * k]), act::value<ACT>(z[2 * k + 1]));
-    x[2 * i] = make_uint4(o[0], o[1], o[2], o[3]);
-    x[2 * i + 1] = make_uint4(o[4], o[5], o[6], o[7]);
+    for (int u = 0; u < U; ++u) {
+      const long long i = i0 + u * step;
+      if (i < eighths) { v[u] = __ldg(q + i); sb[u] = __ldg(s + (i >> 2)); }
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const long long i = i0 + u * step;
+      if (i < eighths) {
+        const act::Pair sc = act::both(ckpt::scale_value(sb[u]));
+        act::Pair z[4];
+        ckpt::decode4(v[u].x, sc, z); ckpt::decode4(v[u].y, sc, z + 2);
+        x[i] = make_uint4(pack_bf16_p(act::value2<ACT>(z[0])), pack_bf16_p(act::value2<ACT>(z[1])), pack_bf16_p(act::value2<ACT>(z[2])),
+                          pack_bf16_p(act::value2<ACT>(z[3])));
+      }
+    }
   }
 }
 
 // ------------------------------------------------------------------------------------------
-// dZ = dY act'(Z) and db = column sums of dZ in fp32.  A thread owns eight columns for good and walks over rows, so the
-// column sums stay in registers; the rows that a CTA takes side by side are added through shared memory at its end, in
-// a fixed order, and each CTA leaves one row of partial sums for bias_reduce_kernel (no atomics: the result does not
-// depend on timing).  CTA (x, y): column tile x of `tile8` groups of eight, row slot y of gridDim.y.
+// dZ = dY act'(Z) and db = column sums of dZ in fp32.  A thread owns two groups of eight columns for good, half a tile
+// apart (so that a warp's 16-byte loads and stores are contiguous; sixteen values share the polynomial's coefficients)
+// and walks over rows, the next three already loading, so the column sums stay in registers; the rows that a CTA takes side
+// by side are added through shared memory at its end, in a fixed order, and each CTA leaves one row of partial sums for
+// bias_reduce_kernel (no atomics: the result does not depend on timing).  CTA (x, y): column tile x of 2 * half groups of
+// eight, row slot y of gridDim.y.
 // ------------------------------------------------------------------------------------------
 constexpr int ACTBWD_MAX_THREADS = 512;
 
 template <int ACT>
-__global__ void __launch_bounds__(ACTBWD_MAX_THREADS)
-act_bwd_kernel(const uint4* dY, const uint2* __restrict__ zq, const uint8_t* __restrict__ zs, int T, int C8, int tile8, int rows,
+__global__ void __launch_bounds__(ACTBWD_MAX_THREADS, 1)
+act_bwd_kernel(const uint4* dY, const uint2* __restrict__ zq, const uint8_t* __restrict__ zs, int T, int C8, int half, int rows,
                uint4* dZ /* may be dY */, float4* __restrict__ partial) {
   pdl_launch_dependents();
   pdl_wait();
-  __shared__ float red[ACTBWD_MAX_THREADS][9];            // 9: neighbouring threads fall into different banks
-  const int g = threadIdx.x / tile8, lc = threadIdx.x - g * tile8;
-  const int c8 = blockIdx.x * tile8 + lc;
-  const bool mine = g < rows && c8 < C8;
-  float sum[8];
+  __shared__ float red[ACTBWD_MAX_THREADS][17];           // 17: neighbouring threads fall into different banks
+  const int g = threadIdx.x / half, lc = threadIdx.x - g * half;
+  const int ca = blockIdx.x * 2 * half + lc, cb = ca + half;
+  const bool a_ok = g < rows && ca < C8, b_ok = g < rows && cb < C8;
+  act::Pair sum[8];
 #pragma unroll
-  for (int k = 0; k < 8; ++k) sum[k] = 0.f;
-  if (mine) {
-    const int stride = rows * (int)gridDim.y;
-    constexpr int U = 4;                                  // rows in flight per thread
-    for (long long t0 = (long long)blockIdx.y * rows + g; t0 < T; t0 += (long long)U * stride) {
-      uint4 d[U];
-      uint2 z[U];
-      uint32_t sc[U];
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const long long t = t0 + (long long)u * stride;
-        if (t < T) {
-          d[u] = dY[t * C8 + c8];
-          if (ACT != BIMASK_ACT_NONE) { z[u] = __ldg(zq + t * C8 + c8); sc[u] = __ldg(zs + t * (C8 >> 2) + (c8 >> 2)); }
+  for (int k = 0; k < 8; ++k) sum[k] = act::both(0.f);
+  if (a_ok) {
+    const long long stride = (long long)rows * gridDim.y;
+    constexpr int U = 3;                                  // rows loaded ahead of the one being worked on
+    uint4 d[U][2];
+    uint2 z[U][2];
+    uint32_t sc[U][2];
+    auto fetch = [&](int u, long long t) {
+      if (t < T) {
+        const long long at = t * C8 + ca;
+        d[u][0] = dY[at];
+        if (ACT != BIMASK_ACT_NONE) { z[u][0] = __ldg(zq + at); sc[u][0] = __ldg(zs + (at >> 2)); }   // C8 % 4 == 0: (t C8 + c) / 4 is the block
+        if (b_ok) {
+          d[u][1] = dY[at + half];
+          if (ACT != BIMASK_ACT_NONE) { z[u][1] = __ldg(zq + at + half); sc[u][1] = __ldg(zs + ((at + half) >> 2)); }
         }
       }
+    };
+    long long t = (long long)blockIdx.y * rows + g;
+#pragma unroll
+    for (int u = 0; u < U; ++u) fetch(u, t + u * stride);
+    while (t < T) {
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        const long long t = t0 + (long long)u * stride;
-        if (t < T) {
-          float v[8] = {bf16_lo(d[u].x), bf16_hi(d[u].x), bf16_lo(d[u].y), bf16_hi(d[u].y),
-                        bf16_lo(d[u].z), bf16_hi(d[u].z), bf16_lo(d[u].w), bf16_hi(d[u].w)};
-          if (ACT != BIMASK_ACT_NONE) {
-            float a[8];
-            const float s = ckpt::scale_value(sc[u]);
-            ckpt::decode4(z[u].x, s, a); ckpt::decode4(z[u].y, s, a + 4);
+        if (t >= T) break;
+        act::Pair v[8], a[8];
 #pragma unroll
-            for (int k = 0; k < 8; ++k) v[k] *= act::slope<ACT>(a[k]);
+        for (int h = 0; h < 2; ++h) {
+          v[4 * h] = bf16_pair(d[u][h].x); v[4 * h + 1] = bf16_pair(d[u][h].y);
+          v[4 * h + 2] = bf16_pair(d[u][h].z); v[4 * h + 3] = bf16_pair(d[u][h].w);
+          if constexpr (ACT != BIMASK_ACT_NONE) {
+            const act::Pair s = act::both(ckpt::scale_value(sc[u][h]));
+            ckpt::decode4(z[u][h].x, s, a + 4 * h); ckpt::decode4(z[u][h].y, s, a + 4 * h + 2);
           }
-#pragma unroll
-          for (int k = 0; k < 8; ++k) sum[k] += v[k];
-          if (dZ != nullptr)
-            dZ[t * C8 + c8] = make_uint4(pack_bf16_f(v[0], v[1]), pack_bf16_f(v[2], v[3]), pack_bf16_f(v[4], v[5]), pack_bf16_f(v[6], v[7]));
         }
+        fetch(u, t + U * stride);
+        if constexpr (ACT != BIMASK_ACT_NONE) {
+#pragma unroll
+          for (int k = 0; k < 8; ++k) v[k] = act::mul2(v[k], act::slope2<ACT>(a[k]));
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) sum[k] = act::add2(sum[k], v[k]);
+        if (dZ != nullptr) {
+          uint4* out = dZ + t * C8 + ca;
+          out[0] = make_uint4(pack_bf16_p(v[0]), pack_bf16_p(v[1]), pack_bf16_p(v[2]), pack_bf16_p(v[3]));
+          if (b_ok) out[half] = make_uint4(pack_bf16_p(v[4]), pack_bf16_p(v[5]), pack_bf16_p(v[6]), pack_bf16_p(v[7]));
+        }
+        t += stride;
       }
     }
   }
   if (partial == nullptr) return;
+  float s[16];
+#pragma unroll
+  for (int k = 0; k < 8; ++k) act::split(sum[k], s[2 * k], s[2 * k + 1]);
   if (rows > 1) {
 #pragma unroll
-    for (int k = 0; k < 8; ++k) red[threadIdx.x][k] = sum[k];
+    for (int k = 0; k < 16; ++k) red[threadIdx.x][k] = s[k];
     __syncthreads();
     if (g == 0)
       for (int r = 1; r < rows; ++r)
 #pragma unroll
-        for (int k = 0; k < 8; ++k) sum[k] += red[r * tile8 + lc][k];
+        for (int k = 0; k < 16; ++k) s[k] += red[r * half + lc][k];
   }
-  if (g == 0 && mine) {
-    float4* out = partial + (size_t)blockIdx.y * (2 * C8) + 2 * c8;
-    out[0] = make_float4(sum[0], sum[1], sum[2], sum[3]);
-    out[1] = make_float4(sum[4], sum[5], sum[6], sum[7]);
+  if (g == 0 && a_ok) {
+    float4* out = partial + (size_t)blockIdx.y * (2 * C8) + 2 * ca;
+    out[0] = make_float4(s[0], s[1], s[2], s[3]);
+    out[1] = make_float4(s[4], s[5], s[6], s[7]);
+    if (b_ok) {
+      out[2 * half] = make_float4(s[8], s[9], s[10], s[11]);
+      out[2 * half + 1] = make_float4(s[12], s[13], s[14], s[15]);
+    }
   }
 }
 
@@ -171,26 +206,23 @@ bias_reduce_kernel(const float4* __restrict__ partial, int nrows, int n4, float4
 
 int stream_grid(long long items) {
   const long long ctas = (items + STREAM_THREADS - 1) / STREAM_THREADS;
-  const long long most = 148 * 8;                         // 2048 threads per SM
+  const long long most = 148 * 32;                        // four rounds of 2048 threads per SM: SMs far from a memory part take fewer
   return (int)(ctas < most ? ctas : most);
 }
 
-struct ActBwdPlan { int tile8, tiles, rows, threads, slots; };
+struct ActBwdPlan { int half, tiles, rows, threads, slots; };
 
-// Columns: one tile when a row has at most 2048 columns, else tiles of about that size.  Rows: as many side by side as
-// fit 256 threads (at least one); row slots so that every SM holds about 1024 threads, each with four rows in flight.
+// Columns: one tile when a row has at most 4096 columns, else tiles of about that size.  One CTA of up to 512 threads per
+// SM: as many rows side by side as fit, so that few rows of partial sums are left over.
 ActBwdPlan plan_act_bwd(int T, int C) {
   ActBwdPlan p;
   const int C8 = C / 8;
-  p.tiles = (C8 + 255) / 256;
-  p.tile8 = (C8 + p.tiles - 1) / p.tiles;
-  p.rows = 256 / p.tile8 > 0 ? 256 / p.tile8 : 1;
+  p.tiles = (C8 + 511) / 512;
+  p.half = ((C8 + p.tiles - 1) / p.tiles + 1) / 2;
+  p.rows = ACTBWD_MAX_THREADS / p.half;
   if (p.rows > T) p.rows = T;
-  p.threads = (p.tile8 * p.rows + 31) / 32 * 32;
-  int per_sm = 1024 / p.threads;
-  if (per_sm < 1) per_sm = 1;
-  if (per_sm > 16) per_sm = 16;
-  p.slots = 148 * per_sm / p.tiles;
+  p.threads = (p.half * p.rows + 31) / 32 * 32;
+  p.slots = 148 / p.tiles;
   const int most = (T + p.rows - 1) / p.rows;
   if (p.slots > most) p.slots = most;
   if (p.slots < 1) p.slots = 1;
@@ -211,9 +243,9 @@ int launch_ckpt_pack(const uint16_t* x, int T, int C, int8_t* q, uint8_t* s, cud
 }
 
 int launch_ckpt_unpack(const int8_t* q, const uint8_t* s, int act, int T, int C, uint16_t* x, cudaStream_t st) {
-  const long long halves = (long long)T * (C / 16);
+  const long long eighths = (long long)T * (C / 8);
   auto run = [&](auto kern) {
-    return launch_pdl(kern, stream_grid(halves), STREAM_THREADS, 0, st, reinterpret_cast<const uint4*>(q), s, halves,
+    return launch_pdl(kern, stream_grid(eighths), STREAM_THREADS, 0, st, reinterpret_cast<const uint2*>(q), s, eighths,
                       reinterpret_cast<uint4*>(x));
   };
   cudaError_t e;
@@ -236,7 +268,7 @@ int launch_act_bwd(const uint16_t* dY, const int8_t* zq, const uint8_t* zs, int 
   float* part = dbias == nullptr ? nullptr : p.slots == 1 ? dbias : partial;      // one slot: its row is the result
   auto run = [&](auto kern) {
     return launch_pdl(kern, dim3(p.tiles, p.slots), p.threads, 0, st, reinterpret_cast<const uint4*>(dY), reinterpret_cast<const uint2*>(zq),
-                      zs, T, C / 8, p.tile8, p.rows, reinterpret_cast<uint4*>(dZ), reinterpret_cast<float4*>(part));
+                      zs, T, C / 8, p.half, p.rows, reinterpret_cast<uint4*>(dZ), reinterpret_cast<float4*>(part));
   };
   cudaError_t e;
   switch (act) {

@@ -35,7 +35,7 @@ spmm_single_kernel(const __grid_constant__ CUtensorMap tmapA, const __grid_const
   static_assert(!(CONV && EPI), "the implicit convolution has no epilogue");
   constexpr int DRAIN_WARPS = EPI ? LIN_EPI_WARPS : EPI_WARPS;
   pdl_launch_dependents();
-  using C = Cfg<N_TILE, STAGES, SPARSE>;
+  using C = Cfg<N_TILE, STAGES, SPARSE, EPI>;
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw = ptx::smem_u32(smem_raw);
   const uint32_t base = (raw + 1023u) & ~1023u;
@@ -252,13 +252,13 @@ spmm_single_kernel(const __grid_constant__ CUtensorMap tmapA, const __grid_const
 // ------------------------------------------------------------------------------------------
 
 
-template <int STAGES, bool SPARSE = true>
+template <int STAGES, bool SPARSE = true, bool EPI = false>
 struct PairPCfg {
   static constexpr int A_BYTES = SPARSE ? 16384 : 32768;   // 128 rows x 64 compressed bf16, or x 128 dense (two boxes)
   static constexpr int B_MAX = 32768;                      // up to 128 rows x 128 bf16 (two 64-wide boxes)
   static constexpr int E_BYTES = SPARSE ? 2048 : 0;
   static constexpr int STAGE_BYTES = A_BYTES + B_MAX + E_BYTES;        // 50 KB / 64 KB (the B part is N / 2 rows)
-  static constexpr int EPI_NT = SPARSE ? 3 : 2;            // staging tiles ([32 tokens][128 rows] bf16) per group of four epilogue warps
+  static constexpr int EPI_NT = !SPARSE ? 2 : EPI ? 4 : 3; // staging tiles ([32 tokens][128 rows] bf16) per group of four epilogue warps (EPI: per ring)
   static constexpr int STAGING_BYTES = epi_staging_bytes(EPI_NT);
   static constexpr int TMEM_COLS = 512;
   static constexpr int SMEM_BYTES = STAGES * STAGE_BYTES + STAGING_BYTES + 1024 + 256;
@@ -276,7 +276,7 @@ spmm_pair_persistent_kernel(const __grid_constant__ CUtensorMap tmapA, const __g
   static_assert(!(CONV && EPI), "the implicit convolution has no epilogue");
   constexpr int DRAIN_WARPS = EPI ? LIN_EPI_WARPS : EPI_WARPS;
   pdl_launch_dependents();
-  using C = PairPCfg<STAGES, SPARSE>;
+  using C = PairPCfg<STAGES, SPARSE, EPI>;
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw = ptx::smem_u32(smem_raw);
   const uint32_t base = (raw + 1023u) & ~1023u;
@@ -764,7 +764,7 @@ int epi_args(const LinearEpilogue* le, int Mdim, int Ndim, const CUtensorMap& un
 template <int N_TILE, int STAGES, bool SPARSE = true, bool EPI = false>
 int run_single(const uint16_t* vals, const void* hw_meta, const uint16_t* Bop, int Mdim, int Ndim, int Kdim,
                uint16_t* out, int32_t* status_word, cudaStream_t s, const LinearEpilogue* le = nullptr) {
-  using C = Cfg<N_TILE, STAGES, SPARSE>;
+  using C = Cfg<N_TILE, STAGES, SPARSE, EPI>;
   CUtensorMap ta, tb, td;
   int rc;
   if ((rc = make_tmap(&ta, vals, SPARSE ? (uint64_t)Kdim / 2 : (uint64_t)Kdim, (uint64_t)Mdim, 128)) != BIMASK_OK) return rc;
@@ -819,7 +819,7 @@ template <bool EPI = false>
 int run_sparse_pair_persistent(const uint16_t* vals, const void* hw_meta, const uint16_t* Bop, int Mdim, int Ndim,
                                int Kdim, uint16_t* out, int32_t* status_word, cudaStream_t s, const LinearEpilogue* le = nullptr) {
   constexpr int STAGES = 3;
-  using C = PairPCfg<STAGES>;
+  using C = PairPCfg<STAGES, true, EPI>;
   CUtensorMap ta, tb, te, td;
   int rc;
   const int tiles_m = (Mdim + 127) / 128, tiles_k = (Kdim + 127) / 128;
@@ -1059,7 +1059,7 @@ template <bool EPI = false>
 int run_dense_pair_persistent(const uint16_t* A, const uint16_t* Bop, int Mdim, int Ndim, int Kdim, uint16_t* out,
                               int32_t* status_word, cudaStream_t s, const LinearEpilogue* le = nullptr) {
   constexpr int STAGES = 3;
-  using C = PairPCfg<STAGES, false>;
+  using C = PairPCfg<STAGES, false, EPI>;
   CUtensorMap ta, tb, td;
   int rc;
   const int tiles_m = (Mdim + 127) / 128, tiles_k = (Kdim + 127) / 128;

@@ -452,6 +452,232 @@ wgrad_single_kernel(const __grid_constant__ CUtensorMap tmapA, const __grid_cons
   }
 }
 
+// ------------------------------------------------------------------------------------------
+// The weight gradient on CTA pairs with sums rounded to nearest, for gradients from a checkpoint (unpacked into bf16
+// ahead of it).  The tensor core adds into its fp32 accumulator without rounding to nearest: a chain of T tokens is off by about
+// 1.1e-9 T relative (9.1e-6 at 8192 tokens, 1.9e-5 at 16384).  So a chain ends after SEGMENT_TILES k tiles: the two
+// accumulators in tensor memory take the segments in turn, and sixteen epilogue warps add each finished segment to the
+// work item's sums, which they hold in registers (64 per thread), in fp32 with rounding to nearest -- while the tensor
+// core works on the next segment.  The tensor core does not notice: 16384 x 4096 at 8192 tokens takes what the kernel
+// above takes.
+// ------------------------------------------------------------------------------------------
+constexpr int SEGMENT_TILES = 8;                                 // 512 tokens: 0.6e-6
+constexpr int CKPT_EPI_WARPS = 16;
+struct WgradCkptCfg {
+  static constexpr int STAGES = 6;
+  static constexpr int A_BYTES = 16384, B_BYTES = 16384;
+  static constexpr int STAGE_BYTES = A_BYTES + B_BYTES;
+  static constexpr int THREADS = 32 * (3 + CKPT_EPI_WARPS);      // TMA, MMA, store, epilogue
+  static constexpr int SMEM_BYTES = STAGES * STAGE_BYTES + WGRAD_STAGING_BYTES + 1024 + 256;
+};
+
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(WgradCkptCfg::THREADS, 1)
+wgrad_ckpt_kernel(const __grid_constant__ CUtensorMap tmapA, const __grid_constant__ CUtensorMap tmapB,
+                  const __grid_constant__ CUtensorMap tmapD, const GemmParams p, int splits) {
+  pdl_launch_dependents();
+  using C = WgradCkptCfg;
+  constexpr int STAGES = C::STAGES;
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t raw = ptx::smem_u32(smem_raw);
+  const uint32_t base = (raw + 1023u) & ~1023u;
+  uint8_t* base_ptr = smem_raw + (base - raw);
+  const uint32_t staging = base + STAGES * C::STAGE_BYTES;
+  const uint32_t bar_base = staging + WGRAD_STAGING_BYTES;
+  auto full_bar = [&](int s) { return bar_base + 8u * s; };
+  auto empty_bar = [&](int s) { return bar_base + 8u * (STAGES + s); };
+  auto tmem_full_bar = [&](int b) { return bar_base + 8u * (2 * STAGES + b); };
+  auto tmem_empty_bar = [&](int b) { return bar_base + 8u * (2 * STAGES + 2 + b); };
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(base_ptr + STAGES * C::STAGE_BYTES + WGRAD_STAGING_BYTES + 8 * (2 * STAGES + 4));
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  // staging tile t is full; group g's turn at its next tile has come (a barrier per GROUP: an mbarrier's parity tells a
+  // waiter only about the phase after the last one it saw, and the four groups take turns at the two tiles)
+  auto staged_bar = [&](int t) { return bar_base + 160u + 8u * t; };
+  auto turn_bar = [&](int g) { return bar_base + 176u + 8u * g; };
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t rank = ptx::cluster_ctarank();
+  const int cluster_id = blockIdx.x >> 1, num_clusters = gridDim.x >> 1;
+  const int num_tiles = p.tiles_m * p.tiles_n;
+  const int num_items = num_tiles * splits;
+  const int k_tiles_total = (p.Kdim + 63) / 64;
+
+  if (threadIdx.x == 0) {
+    *abort_flag = 0;
+    for (int s = 0; s < STAGES; ++s) {
+      ptx::mbar_init(full_bar(s), 1);
+      ptx::mbar_init(empty_bar(s), 1);
+    }
+    for (int b = 0; b < 2; ++b) {
+      ptx::mbar_init(tmem_full_bar(b), 1);
+      ptx::mbar_init(tmem_empty_bar(b), 2 * CKPT_EPI_WARPS);
+    }
+    for (int t = 0; t < 2; ++t) ptx::mbar_init(staged_bar(t), 4);
+    for (int g = 0; g < 4; ++g) ptx::mbar_init(turn_bar(g), 1);
+    ptx::fence_barrier_init();
+    ptx::prefetch_tmap(&tmapA);
+    ptx::prefetch_tmap(&tmapB);
+    ptx::prefetch_tmap(&tmapD);
+  }
+  if (warp == 1) {
+    ptx::tmem_alloc_pair(ptx::smem_u32(tmem_slot), 512);
+    ptx::tmem_relinquish_pair();
+  }
+  ptx::tc_fence_before();
+  __syncthreads();
+  ptx::cluster_sync();
+  ptx::tc_fence_after();
+  const uint32_t tmem_base = *tmem_slot;
+  pdl_wait();                                            // barriers, tensor memory and tensor-map prefetch needed no global memory
+
+  auto item_coords = [&](int item, int& m0, int& n0, int& kt0, int& nkt, int& split) {
+    const int tile = item % num_tiles;
+    split = item / num_tiles;
+    int tile_m, tile_n;
+    raster(tile, p.tiles_m, p.tiles_n, p.raster_group, tile_m, tile_n);
+    m0 = (2 * tile_m + (int)rank) * 128;
+    n0 = tile_n * 256;
+    kt0 = split * p.k_tiles_per_split;
+    nkt = min(k_tiles_total, kt0 + p.k_tiles_per_split) - kt0;
+  };
+
+  if (warp == 0) {
+    if (ptx::elect_one()) {
+      uint32_t it = 0;
+      bool ok = true;
+      for (int item = cluster_id; item < num_items && ok; item += num_clusters) {
+        int m0, n0, kt0, nkt, split;
+        item_coords(item, m0, n0, kt0, nkt, split);
+        for (int kt = kt0; kt < kt0 + nkt; ++kt, ++it) {
+          const int s = it % STAGES;
+          if (!ptx::mbar_wait_bounded(empty_bar(s), ((it / STAGES) & 1u) ^ 1u, abort_flag, WAIT_BUDGET)) { *abort_flag = 1; ok = false; break; }
+          const uint32_t a_s = base + s * C::STAGE_BYTES, b_s = a_s + C::A_BYTES;
+          const uint32_t bar = ptx::mapa(full_bar(s), 0);
+          if (rank == 0) ptx::mbar_expect_tx(full_bar(s), 2 * C::STAGE_BYTES);
+          ptx::tma_load_2d_pair(a_s, &tmapA, m0, kt * 64, bar);
+          ptx::tma_load_2d_pair(a_s + 8192, &tmapA, m0 + 64, kt * 64, bar);
+          ptx::tma_load_2d_pair(b_s, &tmapB, n0 + 128 * (int)rank, kt * 64, bar);
+          ptx::tma_load_2d_pair(b_s + 8192, &tmapB, n0 + 128 * (int)rank + 64, kt * 64, bar);
+        }
+      }
+    }
+  } else if (warp == 1) {
+    if (rank == 0 && ptx::elect_one()) {
+      constexpr uint32_t idesc = ptx::idesc_bf16(256, 256, true, true, false);
+      uint32_t it = 0, seg = 0;
+      bool ok = true;
+      for (int item = cluster_id; item < num_items && ok; item += num_clusters) {
+        int m0, n0, kt0, nkt, split;
+        item_coords(item, m0, n0, kt0, nkt, split);
+        for (int k0 = 0; k0 < nkt && ok; k0 += SEGMENT_TILES, ++seg) {
+          const uint32_t buf = seg & 1u;
+          if (!ptx::mbar_wait_bounded(tmem_empty_bar(buf), ((seg >> 1) & 1u) ^ 1u, abort_flag, WAIT_BUDGET)) { *abort_flag = 1; ok = false; break; }
+          ptx::tc_fence_after();
+          const uint32_t acc = tmem_base + 256u * buf;
+          const int kn = min(SEGMENT_TILES, nkt - k0);
+          for (int k = 0; k < kn; ++k, ++it) {
+            const int s = it % STAGES;
+            const uint32_t ph = (it / STAGES) & 1u;
+            if (!ptx::mbar_wait_bounded(full_bar(s), ph, abort_flag, WAIT_BUDGET)) { *abort_flag = 1; ok = false; break; }
+            ptx::tc_fence_after();
+            const uint32_t a_s = base + s * C::STAGE_BYTES, b_s = a_s + C::A_BYTES;
+#pragma unroll
+            for (int kb = 0; kb < 4; ++kb)
+              ptx::mma_dense_pair(acc, ptx::smem_desc(a_s + kb * 2048, 8192, 1024, 2), ptx::smem_desc(b_s + kb * 2048, 8192, 1024, 2), idesc,
+                                  (k | kb) != 0);
+            ptx::tc_commit_pair(empty_bar(s), 3);
+          }
+          if (ok) ptx::tc_commit_pair(tmem_full_bar(buf), 3);
+        }
+      }
+    }
+  } else if (warp == 2) {
+    // store thread: of each work item the first 32 of every group's 64 columns, then the second 32, from the two staging
+    // tiles in turn; once a tile has been read it is the turn of the group two places on
+    if (ptx::elect_one()) {
+      uint32_t v = 0;
+      bool ok = true;
+      for (int item = cluster_id; item < num_items && ok; item += num_clusters) {
+        int m0, n0, kt0, nkt, split;
+        item_coords(item, m0, n0, kt0, nkt, split);
+        for (int c = 0; c < 8; ++c, ++v) {
+          if (!ptx::mbar_wait_bounded(staged_bar(v & 1u), (v >> 1) & 1u, abort_flag, WAIT_BUDGET)) { *abort_flag = 1; ok = false; break; }
+          const int nb = n0 + 64 * (c & 3) + 32 * (c >> 2);
+          if (nb < p.Ndim && m0 < p.Mdim) ptx::tma_store_4d(&tmapD, nb, m0, split, 0, staging + (v & 1u) * 16384u);
+          ptx::bulk_commit();
+          if (v > 0) {
+            ptx::bulk_wait_read<1>();
+            ptx::mbar_arrive(turn_bar((v + 1u) & 3u));    // chunk v - 1 has been read: its tile is chunk v + 1's
+          }
+        }
+      }
+      ptx::bulk_wait_read<0>();                            // shared memory must outlive the stores that read it
+    }
+  } else {
+    // epilogue: group cg of four warps (one per tensor-memory lane quadrant) owns columns 64 cg .. + 63 of the tile
+    const int q = warp & 3, cg = (warp - 3) >> 2;
+    const uint32_t row = (uint32_t)(32 * q + lane), row_addr = staging + (uint32_t)(cg & 1) * 16384u + row * 128u, sw = row & 7u;
+    float sum[64];
+#pragma unroll
+    for (int j = 0; j < 64; ++j) sum[j] = 0.f;
+    uint32_t seg = 0, use = 0;
+    // Adds the next finished segment to the sums; after an item's last one writes them out (32 columns, then the other 32,
+    // through the group's staging tile) and starts over.  False: gave up.
+    auto finish_segment = [&](bool last) -> bool {
+      const uint32_t buf = seg & 1u;
+      bool ok = ptx::mbar_wait_bounded(tmem_full_bar(buf), (seg >> 1) & 1u, abort_flag, WAIT_BUDGET);
+      ok = __all_sync(0xFFFFFFFFu, ok);
+      if (!ok) { *abort_flag = 1; return false; }
+      ++seg;
+      ptx::tc_fence_after();
+      const uint32_t acc = tmem_base + 256u * buf + 64u * (uint32_t)cg + ((uint32_t)(32 * q) << 16);
+#pragma unroll
+      for (int j = 0; j < 64; j += 16) {
+        uint32_t r[16];
+        ptx::tmem_ld_32x16(acc + j, r);
+        ptx::tmem_ld_wait();
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sum[j + i] += __uint_as_float(r[i]);
+      }
+      release_accumulator(ptx::mapa(tmem_empty_bar(buf), 0), lane);
+      if (!last) return true;
+#pragma unroll
+      for (int h = 0; h < 2; ++h, ++use) {
+        // groups 0 and 1 open the two tiles; every later chunk waits for its group's turn
+        if (ok && (cg >= 2 || use > 0)) ok = ptx::mbar_wait_bounded(turn_bar(cg), (cg >= 2 ? use : use - 1u) & 1u, abort_flag, WAIT_BUDGET);
+        __syncwarp();
+#pragma unroll
+        for (uint32_t j = 0; j < 8; ++j)
+          ptx::st_shared_v4(row_addr + ((j ^ sw) << 4), __float_as_uint(sum[32 * h + 4 * j]), __float_as_uint(sum[32 * h + 4 * j + 1]),
+                            __float_as_uint(sum[32 * h + 4 * j + 2]), __float_as_uint(sum[32 * h + 4 * j + 3]));
+        ptx::fence_proxy_async();
+        __syncwarp();
+        if (lane == 0) ptx::mbar_arrive(staged_bar(cg & 1));
+      }
+#pragma unroll
+      for (int j = 0; j < 64; ++j) sum[j] = 0.f;
+      ok = __all_sync(0xFFFFFFFFu, ok);
+      if (!ok) *abort_flag = 1;
+      return ok;
+    };
+
+    bool ok = true;
+    for (int item = cluster_id; item < num_items && ok; item += num_clusters) {
+      int m0, n0, kt0, nkt, split;
+      item_coords(item, m0, n0, kt0, nkt, split);
+      for (int k0 = 0; k0 < nkt && ok; k0 += SEGMENT_TILES) ok = finish_segment(k0 + SEGMENT_TILES >= nkt);
+    }
+  }
+
+  ptx::tc_fence_before();
+  __syncthreads();
+  if (threadIdx.x == 0 && *abort_flag) atomicExch(p.status_word, (int32_t)BIMASK_ETIMEOUT);
+  ptx::cluster_sync();
+  if (warp == 1) {
+    ptx::tc_fence_after();
+    ptx::tmem_dealloc_pair(tmem_base, 512);
+  }
+}
+
 // Sum of split-K partials: out[e] = sum_s part[s][e], one thread per float4 -- for outputs large enough to fill
 // the GPU that way.
 __global__ void splitk_reduce_kernel(const float4* __restrict__ part, int splits, long long n4,
@@ -631,8 +857,10 @@ void wgrad_plan(int T, int I, int J, int* n_tile, int* splits, int* k_tiles_per_
   wgrad_plan_k((T + 63) / 64, I, J, splits, k_tiles_per_split);
 }
 
-static int run_wgrad(const uint16_t* dY, const uint16_t* X, int T, int I, int J, float* dW, float* partials, int splits, int per,
-                     int32_t* status_word, cudaStream_t s, cudaStream_t reduce_stream, cudaEvent_t product_done) {
+int launch_wgrad_impl(const uint16_t* dY, const uint16_t* X, int T, int I, int J, float* dW, float* partials,
+                      int32_t* status_word, cudaStream_t s, cudaStream_t reduce_stream, cudaEvent_t product_done) {
+  int nt, splits, per;
+  wgrad_plan(T, I, J, &nt, &splits, &per);
   CUtensorMap ta, tb, td;
   int rc;
   if ((rc = make_tmap(&ta, dY, (uint64_t)I, (uint64_t)T, 64)) != BIMASK_OK) return rc;
@@ -662,29 +890,18 @@ static int run_wgrad(const uint16_t* dY, const uint16_t* X, int T, int I, int J,
   return BIMASK_OK;
 }
 
-int launch_wgrad_impl(const uint16_t* dY, const uint16_t* X, int T, int I, int J, float* dW, float* partials,
-                      int32_t* status_word, cudaStream_t s, cudaStream_t reduce_stream, cudaEvent_t product_done) {
-  int nt, splits, per;
-  wgrad_plan(T, I, J, &nt, &splits, &per);
-  return run_wgrad(dY, X, T, I, J, dW, partials, splits, per, status_word, s, reduce_stream, product_done);
-}
-
 // ---- weight gradient from a checkpoint ------------------------------------------------------------
-// The tensor core adds into its fp32 accumulator without rounding to nearest: the result of a chain of T tokens is off
-// by about 1.1e-9 T relative (measured: 9.1e-6 at 8192 tokens, 1.9e-5 at 16384).  Chains are therefore cut at 8192
-// tokens, the pieces added in fp32.
-constexpr int CKPT_CHAIN_TILES = 8192 / 64;
-
 static size_t round256(size_t v) { return (v + 255) / 256 * 256; }
 
 static void wgrad_ckpt_plan(int T, int I, int J, int* splits, int* per) {
   const int k_tiles = (T + 63) / 64;
-  wgrad_plan_k(k_tiles, I, J, splits, per);
-  if (*per > CKPT_CHAIN_TILES) {
-    const int sp = (k_tiles + CKPT_CHAIN_TILES - 1) / CKPT_CHAIN_TILES;
-    *per = (k_tiles + sp - 1) / sp;
-    *splits = (k_tiles + *per - 1) / *per;
-  }
+  const int tiles = (((I + 127) / 128 + 1) / 2) * ((J + 255) / 256), workers = 74;
+  int sp = tiles < workers ? workers / tiles : 1;                 // one round of work items over the CTA pairs
+  const int max_by_k = k_tiles / 8 > 0 ? k_tiles / 8 : 1;         // at least 8 k tiles per split
+  if (sp > max_by_k) sp = max_by_k;
+  if (sp > 64) sp = 64;
+  *per = (k_tiles + sp - 1) / sp;
+  *splits = (k_tiles + *per - 1) / *per;
 }
 
 size_t wgrad_ckpt_bytes(int T, int I, int J) {
@@ -693,14 +910,37 @@ size_t wgrad_ckpt_bytes(int T, int I, int J) {
   return round256((size_t)T * J * 2) + (splits > 1 ? (size_t)splits * I * J * sizeof(float) : 0);
 }
 
+// Decoding the bytes inside the product was slower at every size tried (2048 x 2048 at 8192 tokens: 95 against 58 us with the
+// unpacking pass): per 64-token k tile and SM it moves 80 KB through shared memory where 512 tensor clocks allow 64.
 int launch_wgrad_ckpt(const uint16_t* dY, const int8_t* q, const uint8_t* sc, int T, int I, int J, float* dW, void* ws,
                       int32_t* status_word, cudaStream_t s) {
+  using C = WgradCkptCfg;
   int splits, per, rc;
   wgrad_ckpt_plan(T, I, J, &splits, &per);
   uint16_t* x = reinterpret_cast<uint16_t*>(ws);
   float* partials = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(ws) + round256((size_t)T * J * 2));
   if ((rc = launch_ckpt_unpack(q, sc, BIMASK_ACT_NONE, T, J, x, s)) != BIMASK_OK) return rc;
-  return run_wgrad(dY, x, T, I, J, dW, partials, splits, per, status_word, s, nullptr, nullptr);
+  CUtensorMap ta, tb, td;
+  if ((rc = make_tmap(&ta, dY, (uint64_t)I, (uint64_t)T, 64)) != BIMASK_OK) return rc;
+  if ((rc = make_tmap(&tb, x, (uint64_t)J, (uint64_t)T, 64)) != BIMASK_OK) return rc;
+  if ((rc = make_tmap_f32_store(&td, splits > 1 ? partials : dW, (uint64_t)J, (uint64_t)I, (uint64_t)splits)) != BIMASK_OK) return rc;
+  if ((rc = set_smem_attr(wgrad_ckpt_kernel, C::SMEM_BYTES)) != BIMASK_OK) return rc;
+  GemmParams p;
+  p.conv.mode = 0;
+  p.hw_meta = nullptr; p.tiles_k_meta = 0;
+  p.Mdim = I; p.Ndim = J; p.Kdim = T;
+  p.k_tiles_per_split = per;
+  p.out = splits > 1 ? partials : dW;
+  p.status_word = status_word;
+  p.tiles_m = ((I + 127) / 128 + 1) / 2;
+  p.tiles_n = (J + 255) / 256;
+  p.raster_group = 8;
+  const int items = p.tiles_m * p.tiles_n * splits, sms = sm_count();
+  const int clusters = items < sms / 2 ? items : sms / 2;
+  BIMASK_CUDA_OK(launch_pdl(wgrad_ckpt_kernel, 2 * clusters, C::THREADS, C::SMEM_BYTES, s, ta, tb, td, p, splits));
+  count_launch();
+  BIMASK_CUDA_OK(cudaGetLastError());
+  return splits > 1 ? launch_splitk_reduce(partials, splits, (long long)I * J / 4, dW, s) : BIMASK_OK;
 }
 
 }  // namespace bimask

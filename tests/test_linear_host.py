@@ -82,9 +82,8 @@ def test_workspace_query(bm):
     q = bm.bimask_linear_workspace_bytes
     assert q(0, 64, 64) == 0 and q(4, 48, 64) == 0 and q(4, 64, 48) == 0 and q(-1, 64, 64) == 0
     assert q(1, 32, 32) >= 64
-    for T, I, J in ((12608, 384, 1536), (8192, 16384, 4096), (1, 64, 96), (70000, 32, 32)):
-        assert q(T, I, J) >= 2 * T * J
-        assert q(T, I, 32) <= q(T, I, J) or J == 32
+    assert q(8192, 16384, 4096) >= 2 * 8192 * 4096          # many output tiles: the checkpoint is unpacked into it
+    assert q(12608, 384, 1536) >= 2 * 4 * 384 * 1536         # few: partial sums of several pieces of the tokens
 
 
 def test_refusals_name_the_cause(bm):
@@ -120,7 +119,7 @@ def test_refusals_name_the_cause(bm):
         return L.bimask_wgrad_ckpt(dY, q, s, T, I, J, dW, ws, n, st, None)
 
     for kw, word in (({"T": 0}, "T = 0"), ({"I": 16}, "I = 16"), ({"J": 65}, "J = 65"), ({"dY": None}, "null"), ({"q": None}, "null"),
-                     ({"s": None}, "null"), ({"dW": None}, "null"), ({"ws": None}, "null"), ({"st": None}, "null"), ({"n": 16}, "workspace"),
+                     ({"s": None}, "null"), ({"dW": None}, "null"), ({"ws": None}, "null"), ({"st": None}, "null"), ({"n": 16, "T": 4096}, "workspace"),
                      ({"dW": odd}, "aligned"), ({"s": odd}, "aligned")):
         assert wg(**kw) == inval and word in bm.bimask_last_error(), (kw, bm.bimask_last_error())
     assert bm.bimask_launch_count() == n0
