@@ -72,7 +72,7 @@ __device__ __forceinline__ Pair map2(Pair a, F f) {
 
 constexpr float LOG2E = 1.4426950408889634f;
 
-// Both GELUs are z times a distribution function F with F(-a) = 1 - F(a), so
+// The activations, two values at a time.  Both GELUs are z times a distribution function F with F(-a) = 1 - F(a), so
 //   z F(z) = max(z, 0) - a t(a),   a = |z|,  t(a) = F(-a),
 // and log2 t is smooth: t = 2^P(a) with a polynomial P, one special-function operation where e^x and a reciprocal (or
 // an error function) would take two and more.  P is the minimax fit of a t(a) (of 0.3 t(a) below a = 0.3, which keeps
@@ -97,42 +97,10 @@ struct TanhTail {                                         // t(a) = (1 - tanh(c 
   }
 };
 template <typename T>
-__device__ __forceinline__ float tail(float a) {          // a in [0, CUT]
-  float p = T::c(T::N - 1);
-#pragma unroll
-  for (int i = T::N - 2; i >= 0; --i) p = fmaf(p, a, T::c(i));
-  return ex2(p);
-}
-template <typename T>
 __device__ __forceinline__ float cut(float z) { return min_nan(fabsf(z), T::CUT); }
 
-// sigma(x) = 1 / (1 + e^-x); e^-x = inf for very negative x gives 0
-__device__ __forceinline__ float sigmoid(float x) { return rcp(1.0f + ex2(-LOG2E * x)); }
-
-__device__ __forceinline__ float relu(float z) { return max_nan(z, 0.0f); }
-__device__ __forceinline__ float gelu(float z) {
-  const float a = cut<NormalTail>(z);
-  return fmaf(-a, tail<NormalTail>(a), relu(z));
-}
-__device__ __forceinline__ float gelu_tanh(float z) {
-  const float a = cut<TanhTail>(z);
-  return fmaf(-a, tail<TanhTail>(a), relu(z));
-}
-__device__ __forceinline__ float silu(float z) { return z * sigmoid(z); }
-
-// one activation, chosen at run time
-__device__ __forceinline__ float value_of(int kind, float z) {
-  switch (kind) {
-    case BIMASK_ACT_RELU: return relu(z);
-    case BIMASK_ACT_GELU: return gelu(z);
-    case BIMASK_ACT_GELU_TANH: return gelu_tanh(z);
-    case BIMASK_ACT_SILU: return silu(z);
-    default: return z;
-  }
-}
-
-// ---- the same on pairs ----
-__device__ __forceinline__ Pair sigmoid2(Pair minus_log2e_x) {     // of -log2(e) x
+// sigma(x) = 1 / (1 + e^-x), given -log2(e) x; e^-x = inf for very negative x gives 0
+__device__ __forceinline__ Pair sigmoid2(Pair minus_log2e_x) {
   return map2(add2(map2(minus_log2e_x, [](float v) { return ex2(v); }), both(1.0f)), [](float v) { return rcp(v); });
 }
 __device__ __forceinline__ Pair relu2(Pair z) { return map2(z, [](float v) { return max_nan(v, 0.0f); }); }
@@ -152,10 +120,21 @@ __device__ __forceinline__ Pair value2(Pair z) {
          : KIND == BIMASK_ACT_SILU ? silu2(z) : z;
 }
 
-template <int KIND>
-__device__ __forceinline__ float value(float z) {
-  return KIND == BIMASK_ACT_RELU ? relu(z) : KIND == BIMASK_ACT_GELU ? gelu(z) : KIND == BIMASK_ACT_GELU_TANH ? gelu_tanh(z)
-         : KIND == BIMASK_ACT_SILU ? silu(z) : z;
+// the same, the activation chosen at run time, once for the whole array
+template <int KIND, int N>
+__device__ __forceinline__ void apply_one(Pair (&z)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) z[i] = value2<KIND>(z[i]);
+}
+template <int N>
+__device__ __forceinline__ void apply(int kind, Pair (&z)[N]) {
+  switch (kind) {
+    case BIMASK_ACT_RELU: apply_one<BIMASK_ACT_RELU>(z); break;
+    case BIMASK_ACT_GELU: apply_one<BIMASK_ACT_GELU>(z); break;
+    case BIMASK_ACT_GELU_TANH: apply_one<BIMASK_ACT_GELU_TANH>(z); break;
+    case BIMASK_ACT_SILU: apply_one<BIMASK_ACT_SILU>(z); break;
+    default: break;
+  }
 }
 // Slopes.  With m(a) = t(a) - a f(a), f the density, the slope is m(a) for negative and 1 - m(a) for positive arguments:
 // 1/2 + (1/2 - m(a)) with the sign of z.  For the GELUs m(a) = e^(-a^2/2) P(a): m over the normal density is smooth and P is

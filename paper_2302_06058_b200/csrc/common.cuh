@@ -231,7 +231,9 @@ struct LinearEpilogue {
   int8_t* zq;
   uint8_t* zs;
 };
-// The same for at most 128 tokens (linear_small_sm100.cu).
+// The same for few tokens (linear_small_sm100.cu), and the number of CTAs that share a 128 x 128 tile's reduction of
+// k_tiles 128-wide tiles there.
+int linear_small_splits(int tiles, int k_tiles);
 int launch_linear_small(const uint16_t* vals, const void* hw_meta, const uint16_t* X, int Mdim, int Ndim, int Kdim,
                         const LinearEpilogue& le, uint16_t* out, int32_t* status_word, cudaStream_t s);
 int launch_linear_fwd(const uint16_t* vals, const void* hw_meta, const uint16_t* X, int Mdim, int Ndim, int Kdim,

@@ -1,4 +1,4 @@
-// A linear layer for few tokens (at most 128): the form of generation and of small batches.  Its time is the reading of
+// A linear layer for few tokens: the form of generation and of small batches.  Its time is the reading of
 // the weights, so the work is cut along the reduction as well: a cluster of `splits` CTAs owns 128 rows x N_TILE tokens,
 // each streams its share of the k tiles through a deep ring of stages (the same TMA -> tcgen05.mma pipeline as the large
 // products), leaves its fp32 partial sums in its own shared memory, and after a cluster barrier the CTAs add one another's
@@ -164,42 +164,73 @@ linear_small_kernel(const __grid_constant__ CUtensorMap tmapA, const __grid_cons
   }
   if (threadIdx.x == 0 && *abort_flag) atomicExch(p.status_word, (int32_t)BIMASK_ETIMEOUT);
 
-  // tokens rank, rank + splits, ... are this CTA's to finish, one warp per token: lane = four rows
+  // tokens rank, rank + splits, ... are this CTA's to finish, two at a time per warp: lane = four rows
   const int ntok = min(N_TILE, p.Ndim - n0);
   const int row = m0 + 4 * lane;
   const bool rows_ok = row < p.Mdim;                      // Mdim % 32 == 0: true for whole blocks of eight lanes
   float4 b = make_float4(0.f, 0.f, 0.f, 0.f);
   if (p.bias != nullptr && rows_ok) b = __ldg(reinterpret_cast<const float4*>(p.bias + row));
-  for (int t = rank + splits * warp; t < ntok; t += splits * (SMALL_THREADS / 32)) {
-    const size_t at = (size_t)(n0 + t) * p.Mdim + row;
-    uint2 res = make_uint2(0u, 0u);
-    if (p.res != nullptr && rows_ok) res = *reinterpret_cast<const uint2*>(p.res + at);   // may be `out`: a plain load
-    const uint32_t src = base + (uint32_t)(t * 512 + 16 * lane);
-    float4 z = b;
-    for (int s0 = 0; s0 < splits; s0 += 4) {
-      float4 v[4];
+  constexpr int U = 2, V = 4;                             // tokens per warp at a time, ranks' sums in flight
+  for (int t0 = rank + splits * U * warp; t0 < ntok; t0 += splits * U * (SMALL_THREADS / 32)) {
+    uint2 res[U];
+    float4 sum[U];
 #pragma unroll
-      for (int u = 0; u < 4; ++u) v[u] = s0 + u < splits ? ptx::ld_cluster_v4(ptx::mapa(src, s0 + u)) : make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int u = 0; u < U; ++u) {
+      const int t = t0 + splits * u;
+      res[u] = make_uint2(0u, 0u);
+      if (t < ntok && p.res != nullptr && rows_ok)
+        res[u] = *reinterpret_cast<const uint2*>(p.res + (size_t)(n0 + t) * p.Mdim + row);   // may be `out`: a plain load
+      sum[u] = b;
+    }
+    for (int s = 0; s < splits; s += V) {                 // in rank order; eight loads in flight
+      float4 v[V][U];
 #pragma unroll
-      for (int u = 0; u < 4; ++u) { z.x += v[u].x; z.y += v[u].y; z.z += v[u].z; z.w += v[u].w; }
+      for (int k = 0; k < V; ++k)
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          const int t = t0 + splits * u;
+          v[k][u] = s + k < splits && t < ntok ? ptx::ld_cluster_v4(ptx::mapa(base + (uint32_t)(t * 512 + 16 * lane), s + k)) : make_float4(0.f, 0.f, 0.f, 0.f);
+        }
+#pragma unroll
+      for (int k = 0; k < V; ++k)
+#pragma unroll
+        for (int u = 0; u < U; ++u) { sum[u].x += v[k][u].x; sum[u].y += v[k][u].y; sum[u].z += v[k][u].z; sum[u].w += v[k][u].w; }
+    }
+    act::Pair z[2 * U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      z[2 * u] = act::pair(sum[u].x, sum[u].y);
+      z[2 * u + 1] = act::pair(sum[u].z, sum[u].w);
     }
     if (p.zq != nullptr) {                                // eight lanes = one block of 32 channels
-      uint32_t h = ckpt::up16(act::max_nan(act::max_nan(fabsf(z.x), fabsf(z.y)), act::max_nan(fabsf(z.z), fabsf(z.w))));
 #pragma unroll
-      for (int d = 1; d < 8; d <<= 1) h = max(h, __shfl_xor_sync(0xFFFFFFFFu, h, d));
-      const uint32_t sc = ckpt::scale_of(h);
-      const float inv = ckpt::inverse_scale(sc);
-      const uint32_t lo = __byte_perm(ckpt::round_bits(z.x, inv), ckpt::round_bits(z.y, inv), 0x0040);
-      const uint32_t hi = __byte_perm(ckpt::round_bits(z.z, inv), ckpt::round_bits(z.w, inv), 0x0040);
-      if (rows_ok) {
-        *reinterpret_cast<uint32_t*>(p.zq + at) = __byte_perm(lo, hi, 0x5410);
-        if ((lane & 7) == 0) p.zs[at >> 5] = (uint8_t)sc;
+      for (int u = 0; u < U; ++u) {
+        const int t = t0 + splits * u;
+        float v[4];
+        act::split(z[2 * u], v[0], v[1]);
+        act::split(z[2 * u + 1], v[2], v[3]);
+        uint32_t h = ckpt::up16(act::max_abs3(act::max_abs3(v[0], v[1], v[2]), v[3], 0.0f));
+#pragma unroll
+        for (int d = 1; d < 8; d <<= 1) h = max(h, __shfl_xor_sync(0xFFFFFFFFu, h, d));
+        const uint32_t sc = ckpt::scale_of(h);
+        const float inv = ckpt::inverse_scale(sc);
+        const uint32_t lo = __byte_perm(ckpt::round_bits(v[0], inv), ckpt::round_bits(v[1], inv), 0x0040);
+        const uint32_t hi = __byte_perm(ckpt::round_bits(v[2], inv), ckpt::round_bits(v[3], inv), 0x0040);
+        if (t < ntok && rows_ok) {
+          const size_t at = (size_t)(n0 + t) * p.Mdim + row;
+          *reinterpret_cast<uint32_t*>(p.zq + at) = __byte_perm(lo, hi, 0x5410);
+          if ((lane & 7) == 0) p.zs[at >> 5] = (uint8_t)sc;
+        }
       }
     }
-    if (rows_ok)
-      *reinterpret_cast<uint2*>(p.out + at) =
-          make_uint2(pack_bf16_f(act::value_of(p.act, z.x) + bf16_lo(res.x), act::value_of(p.act, z.y) + bf16_hi(res.x)),
-                     pack_bf16_f(act::value_of(p.act, z.z) + bf16_lo(res.y), act::value_of(p.act, z.w) + bf16_hi(res.y)));
+    act::apply(p.act, z);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int t = t0 + splits * u;
+      if (t < ntok && rows_ok)
+        *reinterpret_cast<uint2*>(p.out + (size_t)(n0 + t) * p.Mdim + row) =
+            make_uint2(pack_bf16_p(act::add2(z[2 * u], bf16_pair(res[u].x))), pack_bf16_p(act::add2(z[2 * u + 1], bf16_pair(res[u].y))));
+    }
   }
   __syncthreads();
   if (splits > 1) ptx::cluster_sync();                    // shared memory must outlive the peers' reads of it
@@ -223,13 +254,8 @@ int run_small(const uint16_t* vals, const void* hw_meta, const uint16_t* X, int 
   p.bias = le.bias; p.act = le.act; p.res = le.res; p.out = out; p.zq = le.zq; p.zs = le.zs;
   p.status_word = status_word;
   const int tiles = p.tiles_m * ((Ndim + N_TILE - 1) / N_TILE);
-  // As many CTAs as there are SMs, at most eight per cluster (the portable size) and at least four k tiles each.
-  int splits = sm_count() / tiles;
-  if (splits > p.tiles_k / 4) splits = p.tiles_k / 4;
-  if (splits > 8) splits = 8;
-  if (splits < 1) splits = 1;
+  const int splits = linear_small_splits(tiles, p.tiles_k);
   p.k_per_split = (p.tiles_k + splits - 1) / splits;
-  splits = (p.tiles_k + p.k_per_split - 1) / p.k_per_split;
   BIMASK_CUDA_OK(launch_pdl_cluster(kern, splits * tiles, SMALL_THREADS, splits, C::SMEM_BYTES, s, ta, tb, p, splits));
   count_launch();
   BIMASK_CUDA_OK(cudaGetLastError());
@@ -246,6 +272,16 @@ int run_small_any(const uint16_t* vals, const void* hw_meta, const uint16_t* X, 
 }
 
 }  // namespace
+
+// As many CTAs as there are SMs, at most eight per cluster (the portable size) and at least four k tiles each.
+int linear_small_splits(int tiles, int k_tiles) {
+  int splits = sm_count() / tiles;
+  if (splits > k_tiles / 4) splits = k_tiles / 4;
+  if (splits > 8) splits = 8;
+  if (splits < 1) splits = 1;
+  const int per = (k_tiles + splits - 1) / splits;
+  return (k_tiles + per - 1) / per;
+}
 
 int launch_linear_small(const uint16_t* vals, const void* hw_meta, const uint16_t* X, int Mdim, int Ndim, int Kdim,
                         const LinearEpilogue& le, uint16_t* out, int32_t* status_word, cudaStream_t s) {

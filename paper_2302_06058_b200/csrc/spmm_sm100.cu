@@ -1109,11 +1109,32 @@ int launch_dense_nt(const uint16_t* A, const uint16_t* Bop, int Mdim, int Ndim, 
   return run_single<128, 3, false>(A, nullptr, Bop, Mdim, Ndim, Kdim, out, status_word, s);
 }
 
+// Whether the kernel for few tokens (128 x 128 tiles, split along the reduction over a cluster) is the faster one: it is
+// where the CTA pairs' large tiles leave most SMs idle through a long reduction.  Both sides in SM clocks: a k tile costs
+// what its operands take at 64 bytes per clock (measured about 1.25 times that on the pairs), start-up and finish 6 and 9
+// thousand.  Measured, pairs / split: 4096 x 16384 at 160, 256, 512 tokens 55 / 32, 55 / 33, 58 / 55 us; 1024 x 4096 (dense
+// operand) at 160, 512, 1000 tokens 17 / 11, 20 / 10, 19 / 14; but 16384 x 4096 at 256 27 / 46, 1536 x 384 at 160 5 / 11.
+static bool split_is_faster(bool sparse, int Mdim, int Ndim, int Kdim) {
+  const int sms = sm_count(), kt = (Kdim + 127) / 128;
+  const int tiles = ((Mdim + 127) / 128) * ((Ndim + 127) / 128);
+  const int splits = linear_small_splits(tiles, kt);
+  const double small = (double)((tiles * splits + sms - 1) / sms) * ((kt + splits - 1) / splits * (sparse ? 800.0 : 1024.0) + 9000.0);
+  double pair = 1e30;
+  for (int n = 256; n >= 96; n -= 32) {
+    const int t = (Mdim + 255) / 256 * ((Ndim + n - 1) / n);
+    const double feed = ((sparse ? 18432.0 : 32768.0) + 128.0 * n) / 64.0, mma = (sparse ? 2.0 : 4.0) * n;
+    const double cost = 6000.0 + (double)((t + sms / 2 - 1) / (sms / 2)) * kt * 1.25 * (feed > mma ? feed : mma);
+    if (cost < pair) pair = cost;
+  }
+  return small < 0.9 * pair;
+}
+
 // Linear layer: the product of launch_spmm (hw_meta given) or launch_dense_nt (null) with the epilogue of `le`, on the
-// same kernels by the same rules; at most 128 tokens go to the kernel for few tokens.
+// same kernels by the same rules, and on the kernel for few tokens.
 int launch_linear_fwd(const uint16_t* vals, const void* hw_meta, const uint16_t* X, int Mdim, int Ndim, int Kdim,
                       const LinearEpilogue& le, uint16_t* out, int32_t* status_word, cudaStream_t s) {
-  if (Ndim <= 128) return launch_linear_small(vals, hw_meta, X, Mdim, Ndim, Kdim, le, out, status_word, s);
+  if (Ndim <= 128 || (Mdim > 128 && split_is_faster(hw_meta != nullptr, Mdim, Ndim, Kdim)))
+    return launch_linear_small(vals, hw_meta, X, Mdim, Ndim, Kdim, le, out, status_word, s);
   if (hw_meta != nullptr) {
     if (Ndim >= 1024 && Mdim >= 2048 && Kdim >= 4096)
       return run_sparse_pair2m<true>(vals, hw_meta, X, Mdim, Ndim, Kdim, out, status_word, s, &le);

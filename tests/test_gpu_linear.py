@@ -84,6 +84,12 @@ def test_forward_exact_on_small_integers(T, I, J, N, M):
     assert np.array_equal(q.cpu().numpy(), q0)
 
 
+@pytest.mark.parametrize("T,I,J,N,M", [(150, 288, 8224, 2, 4), (129, 1056, 16384, 2, 4), (300, 160, 4128, 4, 8), (260, 416, 8192, 1, 4)])
+def test_forward_exact_where_many_tokens_split_the_reduction(T, I, J, N, M):
+    """More than one 128-token tile on the kernel for few tokens (long reductions with few output tiles), ragged at both ends."""
+    test_forward_exact_on_small_integers(T, I, J, N, M)
+
+
 def pack_fast(z):
     b = z.reshape(z.shape[0], -1, 32)
     m = np.abs(b).max(-1)
