@@ -28,6 +28,9 @@ constexpr int PAIR_THREADS = 64 + 32 * EPI_WARPS + 32 * EPI_GROUPS;
 // "freed" mbarriers, kept EPI_BAR_OFFSET bytes into the kernels' barrier area.
 __host__ __device__ constexpr int epi_staging_bytes(int nt) { return EPI_GROUPS * nt * 8192; }
 constexpr uint32_t EPI_BAR_OFFSET = 128;
+// Past the 256 bytes of barriers: the checkpoint's scales on their way out, a word per token, 128 bytes per staging tile.
+constexpr uint32_t EPI_SCALES_OFFSET = 256;
+__host__ __device__ constexpr int epi_scales_bytes(int nt) { return EPI_GROUPS * nt * 128; }
 
 
 template <int N_TILE, int STAGES, bool SPARSE = true, bool EPI = false>
@@ -359,9 +362,11 @@ constexpr int LIN_THREADS = 64 + 32 * LIN_EPI_WARPS + 32 * EPI_GROUPS;
 //           any other; a lane reads back the 16 bytes of half a block, undoes the pairing and stores them: a token's 32
 //           bytes are one whole sector.
 // `area`: 32 token rows of 128 bytes of which this warp may use units u0, u0 + 1 (16 bytes each, XOR token mod 8) as
-// scratch.  q_out / s_out: where token 0's block and scale go; ntok: tokens of the chunk that exist.
+// scratch.  q_out: where token 0's block goes; ntok: tokens of the chunk that exist.  The scales go to shared memory, one
+// byte of a word per token (`scales`: this warp's byte of token 0): the store warp writes the four warps' together (bytes
+// stored one by one cost 30 of 643 us on the 16384-row layer).
 __device__ __forceinline__ void emit_checkpoint(const act::Pair (&z)[16], uint32_t area, uint32_t u0, int lane, int8_t* q_out,
-                                                size_t q_pitch, uint8_t* s_out, size_t s_pitch, int ntok) {
+                                                size_t q_pitch, uint32_t scales, int ntok) {
   uint32_t p[4];
 #pragma unroll
   for (int g = 0; g < 4; ++g) {
@@ -384,7 +389,7 @@ __device__ __forceinline__ void emit_checkpoint(const act::Pair (&z)[16], uint32
   const uint32_t over = (k + 0x00800080u) & 0x80008000u;
   const uint32_t s2 = raw | ((over >> 7) - (over >> 15));
   const int st = 8 * (lane >> 3) + 2 * (lane & 3) + ((lane >> 2) & 1);
-  if (st < ntok) s_out[(size_t)st * s_pitch] = (uint8_t)((lane & 4) ? s2 >> 16 : s2);
+  ptx::st_shared_u8(scales + 4u * (uint32_t)st, (lane & 4) ? s2 >> 16 : s2);
   const uint32_t inv2 = (0x00FE00FEu - raw) << 7;         // 2^(127 - s) of both tokens, as bf16
   const uint32_t o8 = __shfl_xor_sync(0xFFFFFFFFu, inv2, 8);
   const uint32_t g0 = mid ? o8 : inv2, g1 = mid ? inv2 : o8;
@@ -461,7 +466,7 @@ __device__ __forceinline__ void epi_bias(const float* bias, int row0, int Mdim, 
 // b: epi_bias of the warp's rows; x0: first row of the CTA's 128; y0: first token of chunk 0.
 template <int NT>
 __device__ __forceinline__ bool drain_chunks_epi(uint32_t acc, int first, int sub, int nchunks, uint32_t release_bar, uint32_t stg,
-                                                 uint32_t bars, uint32_t& n0, int q, int lane, const EpiParams& e,
+                                                 uint32_t bars, uint32_t scales, uint32_t& n0, int q, int lane, const EpiParams& e,
                                                  const float (&b)[4], int x0, int y0, int Mdim, int Ndim, volatile int* abort_flag) {
   static_assert(NT % 2 == 0, "a staging tile serves one group");
   const int count = (nchunks - first + 1) / 2;
@@ -502,8 +507,8 @@ __device__ __forceinline__ bool drain_chunks_epi(uint32_t acc, int first, int su
         __syncwarp();
       }
       const int t0 = y0 + 32 * c;
-      emit_checkpoint(z, half + tile, 4u * (q & 1), lane, e.zq + (size_t)t0 * Mdim + row0, (size_t)Mdim,
-                      e.zs + (size_t)t0 * (Mdim >> 5) + (row0 >> 5), (size_t)(Mdim >> 5), rows_ok ? Ndim - t0 : 0);
+      emit_checkpoint(z, half + tile, 4u * (q & 1), lane, e.zq + (size_t)t0 * Mdim + row0, (size_t)Mdim, scales + 128u * slot + (uint32_t)q,
+                      rows_ok ? Ndim - t0 : 0);
     }
     switch (e.mode) {
 #define BIMASK_EMIT(m) case m: emit_result<m / 3, m % 3>(z, dst + tile, res); break;
@@ -519,13 +524,16 @@ __device__ __forceinline__ bool drain_chunks_epi(uint32_t acc, int first, int su
   return ok;
 }
 
-// The store thread's side.  `walk` yields the ring's chunks one after the other, over all its tiles: next(x0, y) gives
-// the first row and token, false past the last.  With a residual a second copy of it runs NT chunks ahead: the residual
-// tile of chunk n + NT is loaded into the staging tile of chunk n once that chunk's store has read it.
+// The store warp's side.  `walk` yields the ring's chunks one after the other, over all its tiles: next(x0, y) gives
+// the first row and token, false past the last.  Lane 0 sends the tiles off; with a checkpoint every lane stores one token's
+// scales (`scales`: a word per token and staging tile).  With a residual a second copy of the walk runs NT chunks ahead: the
+// residual tile of chunk n + NT is loaded into the staging tile of chunk n once that chunk's store has read it.
 template <int NT, typename Walk>
-__device__ __forceinline__ bool store_chunks_epi(const CUtensorMap* tmapD, const CUtensorMap* tmapR, bool has_res, uint32_t stg,
-                                                 uint32_t bars, int Mdim, int Ndim, volatile int* abort_flag, Walk walk) {
+__device__ __forceinline__ bool store_chunks_epi(const CUtensorMap* tmapD, const CUtensorMap* tmapR, const EpiParams& e, uint32_t stg,
+                                                 uint32_t bars, uint32_t scales, int lane, int Mdim, int Ndim, volatile int* abort_flag,
+                                                 Walk walk) {
   Walk ahead = walk;
+  const bool has_res = e.has_res != 0;
   uint32_t loaded = 0;                                    // residual tiles requested so far
   auto load = [&]() {
     int x0, y;
@@ -536,33 +544,52 @@ __device__ __forceinline__ bool store_chunks_epi(const CUtensorMap* tmapD, const
     ptx::tma_load_2d(stg + slot * 8192u + 4096u, tmapR, x0 + 64, y, bar);
     ++loaded;
   };
-  if (has_res)
+  if (has_res && lane == 0)
     for (uint32_t n = 0; n < NT; ++n) load();
   bool ok = true;
   int x0, y;
   for (uint32_t n = 0; walk.next(x0, y); ++n) {
     const uint32_t slot = n % NT, use = n / NT;
     ok = ptx::mbar_wait_bounded(bars + 8u * slot, use & 1u, abort_flag, WAIT_BUDGET);
+    ok = __all_sync(0xFFFFFFFFu, ok);
     if (!ok) break;
-    if (y < Ndim && x0 < Mdim) {
-      ptx::tma_store_2d(tmapD, x0, y, stg + slot * 8192u);
-      if (x0 + 64 < Mdim) ptx::tma_store_2d(tmapD, x0 + 64, y, stg + slot * 8192u + 4096u);
+    if (lane == 0) {
+      if (y < Ndim && x0 < Mdim) {
+        ptx::tma_store_2d(tmapD, x0, y, stg + slot * 8192u);
+        if (x0 + 64 < Mdim) ptx::tma_store_2d(tmapD, x0 + 64, y, stg + slot * 8192u + 4096u);
+      }
+      ptx::bulk_commit();
     }
-    ptx::bulk_commit();
+    if (e.zq != nullptr && x0 < Mdim) {
+      const uint32_t w = ptx::ld_shared_u32(scales + 128u * slot + 4u * (uint32_t)lane);
+      if (y + lane < Ndim) {
+        uint8_t* out = e.zs + (size_t)(y + lane) * (Mdim >> 5) + (x0 >> 5);
+        if (Mdim % 128 == 0) {
+          *reinterpret_cast<uint32_t*>(out) = w;
+        } else {
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            if (x0 + 32 * k < Mdim) out[k] = (uint8_t)(w >> (8 * k));
+        }
+      }
+      __syncwarp();                                       // the words have been read: the tile may be handed back
+    }
     // With two tiles, one per group, a tile is handed back as soon as its store has read it: its group cannot go on
     // before (1 % on the 16384-row layers).  With four, the wait goes under the next store.
-    if (NT <= 2 || n > 0) {
+    if (lane == 0 && (NT <= 2 || n > 0)) {
       ptx::bulk_wait_read<(NT <= 2 ? 0 : 1)>();
       if (has_res) load();
       else ptx::mbar_arrive(bars + 8u * (NT + (NT <= 2 ? slot : (n - 1u) % NT)));
     }
   }
-  if (!ok && has_res) {                                   // giving up: no load may be in flight when the kernel ends
-    volatile int none = 0;
-    for (uint32_t n = loaded > NT ? loaded - NT : 0; n < loaded; ++n)
-      ptx::mbar_wait_bounded(bars + 8u * (NT + n % NT), (n / NT) & 1u, &none, WAIT_BUDGET);
+  if (lane == 0) {
+    if (!ok && has_res) {                                 // giving up: no load may be in flight when the kernel ends
+      volatile int none = 0;
+      for (uint32_t n = loaded > NT ? loaded - NT : 0; n < loaded; ++n)
+        ptx::mbar_wait_bounded(bars + 8u * (NT + n % NT), (n / NT) & 1u, &none, WAIT_BUDGET);
+    }
+    store_finish();
   }
-  store_finish();
   return ok;
 }
 

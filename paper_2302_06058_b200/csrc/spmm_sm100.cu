@@ -200,7 +200,8 @@ spmm_single_kernel(const __grid_constant__ CUtensorMap tmapA, const __grid_const
         uint32_t n = 0;
         const int ring = eg & 1;
         if (!drain_chunks_epi<C::EPI_NT>(tmem_base + ((uint32_t)(32 * q) << 16), ring, eg >> 1, N_TILE / 32, 0u,
-                                         staging + ring * (C::EPI_NT * 8192), epi_bars_of<C::EPI_NT>(bar_base, ring), n, q, lane, e, bias, m0, n0,
+                                         staging + ring * (C::EPI_NT * 8192), epi_bars_of<C::EPI_NT>(bar_base, ring),
+                                         bar_base + EPI_SCALES_OFFSET + ring * (C::EPI_NT * 128), n, q, lane, e, bias, m0, n0,
                                          p.Mdim, p.Ndim, abort_flag))
           *abort_flag = 1;
       } else {
@@ -212,12 +213,12 @@ spmm_single_kernel(const __grid_constant__ CUtensorMap tmapA, const __grid_const
       }
     }
   } else if (!CONV) {
-    // ------------------------------ store threads: one per epilogue group ------------------------------
-    if (ptx::elect_one()) {
+    // ------------------------------ store threads: one per epilogue group (EPI: the whole warp) ------------------------------
+    if (EPI || ptx::elect_one()) {
       const int g = warp - 2 - DRAIN_WARPS;
       if constexpr (EPI) {
-        if (!store_chunks_epi<C::EPI_NT>(&tmapD, &tmapR, e.has_res != 0, staging + g * (C::EPI_NT * 8192), epi_bars_of<C::EPI_NT>(bar_base, g),
-                                         p.Mdim, p.Ndim, abort_flag,
+        if (!store_chunks_epi<C::EPI_NT>(&tmapD, &tmapR, e, staging + g * (C::EPI_NT * 8192), epi_bars_of<C::EPI_NT>(bar_base, g),
+                                         bar_base + EPI_SCALES_OFFSET + g * (C::EPI_NT * 128), lane, p.Mdim, p.Ndim, abort_flag,
                                          chunk_walk<1>(p, (int)blockIdx.x, (int)gridDim.x, (int)gridDim.x, C::M_TILE, 0, 0, N_TILE, g)))
           *abort_flag = 1;
       } else {
@@ -460,7 +461,8 @@ spmm_pair_persistent_kernel(const __grid_constant__ CUtensorMap tmapA, const __g
           return outp + conv_out_pixel(p.conv, n, h, w) * p.Mdim + m0;
         });
       } else if constexpr (EPI) {
-        if (!drain_chunks_epi<C::EPI_NT>(acc, ring, eg >> 1, nchunks, release_bar, stg, ebars, u, q, lane, e, bias, m0, n0, p.Mdim, p.Ndim,
+        if (!drain_chunks_epi<C::EPI_NT>(acc, ring, eg >> 1, nchunks, release_bar, stg, ebars, bar_base + EPI_SCALES_OFFSET + ring * (C::EPI_NT * 128),
+                                         u, q, lane, e, bias, m0, n0, p.Mdim, p.Ndim,
                                          abort_flag)) {
           *abort_flag = 1;
           break;
@@ -472,13 +474,13 @@ spmm_pair_persistent_kernel(const __grid_constant__ CUtensorMap tmapA, const __g
       }
     }
   } else if (!CONV) {
-    // store threads, one per epilogue group: the same walk over tiles and chunks as the group's draining warps
-    if (ptx::elect_one()) {
+    // store threads, one per epilogue group (EPI: the whole warp): the same walk over tiles and chunks as the draining warps
+    if (EPI || ptx::elect_one()) {
       const int g = warp - 2 - DRAIN_WARPS;
       const uint32_t stg = staging + g * (C::EPI_NT * 8192);
       const uint32_t ebars = epi_bars_of<C::EPI_NT>(bar_base, g);
       if constexpr (EPI) {
-        if (!store_chunks_epi<C::EPI_NT>(&tmapD, &tmapR, e.has_res != 0, stg, ebars, p.Mdim, p.Ndim, abort_flag,
+        if (!store_chunks_epi<C::EPI_NT>(&tmapD, &tmapR, e, stg, ebars, bar_base + EPI_SCALES_OFFSET + g * (C::EPI_NT * 128), lane, p.Mdim, p.Ndim, abort_flag,
                                          chunk_walk<1>(p, cluster_id, num_clusters, num_tiles, 256, 128 * (int)rank, 0, SP_N, g)))
           *abort_flag = 1;
       } else {
@@ -705,7 +707,8 @@ spmm_pair2m_kernel(const __grid_constant__ CUtensorMap tmapA, const __grid_const
         if constexpr (EPI) {
           float b[4];
           for (int k = 0; k < 4; ++k) b[k] = mt ? bias[1][k] : bias[0][k];
-          if (!drain_chunks_epi<C::EPI_NT>(acc, (g ^ mt) & 1, eg >> 1, SP_N / 32, mt ? release1 : release0, stg, ebars, u, q, lane, e, b,
+          if (!drain_chunks_epi<C::EPI_NT>(acc, (g ^ mt) & 1, eg >> 1, SP_N / 32, mt ? release1 : release0, stg, ebars,
+                                           bar_base + EPI_SCALES_OFFSET + g * (C::EPI_NT * 128), u, q, lane, e, b,
                                            mt128_of(tile_m, mt) * 128, tile_n * SP_N, p.Mdim, p.Ndim, abort_flag))
             *abort_flag = 1;
         } else if (!drain_chunks_tma<32, C::EPI_NT>(acc, (g ^ mt) & 1, 2, SP_N / 32, false, mt ? release1 : release0, stg, ebars, u, q,
@@ -715,13 +718,13 @@ spmm_pair2m_kernel(const __grid_constant__ CUtensorMap tmapA, const __grid_const
       if (*abort_flag) break;
     }
   } else {
-    // store threads, one per epilogue group: the same walk over tiles, row tiles and chunks as the group's draining warps
-    if (ptx::elect_one()) {
+    // store threads, one per epilogue group (EPI: the whole warp): the same walk over tiles, row tiles and chunks as the draining warps
+    if (EPI || ptx::elect_one()) {
       const int g = warp - 2 - DRAIN_WARPS;
       const uint32_t stg = staging + g * (C::EPI_NT * 8192);
       const uint32_t ebars = epi_bars_of<C::EPI_NT>(bar_base, g);
       if constexpr (EPI) {
-        if (!store_chunks_epi<C::EPI_NT>(&tmapD, &tmapR, e.has_res != 0, stg, ebars, p.Mdim, p.Ndim, abort_flag,
+        if (!store_chunks_epi<C::EPI_NT>(&tmapD, &tmapR, e, stg, ebars, bar_base + EPI_SCALES_OFFSET + g * (C::EPI_NT * 128), lane, p.Mdim, p.Ndim, abort_flag,
                                          chunk_walk<2>(p, cluster_id, num_clusters, num_tiles, 512, 128 * (int)rank, 256, SP_N, g)))
           *abort_flag = 1;
       } else {
@@ -774,7 +777,8 @@ int run_single(const uint16_t* vals, const void* hw_meta, const uint16_t* Bop, i
   EpiParams e;
   if ((rc = epi_args(le, Mdim, Ndim, td, &tr, &e)) != BIMASK_OK) return rc;
   auto kern = spmm_single_kernel<N_TILE, STAGES, SPARSE, false, EPI>;
-  if ((rc = set_smem_attr(kern, C::SMEM_BYTES)) != BIMASK_OK) return rc;
+  constexpr int smem = C::SMEM_BYTES + (EPI ? epi_scales_bytes(C::EPI_NT) : 0);
+  if ((rc = set_smem_attr(kern, smem)) != BIMASK_OK) return rc;
   GemmParams p;
   p.conv.mode = 0;
   p.hw_meta = reinterpret_cast<const uint8_t*>(hw_meta);
@@ -787,7 +791,7 @@ int run_single(const uint16_t* vals, const void* hw_meta, const uint16_t* Bop, i
   p.tiles_n = (Ndim + N_TILE - 1) / N_TILE;
   p.raster_group = 16;
   dim3 grid(p.tiles_m * p.tiles_n, 1, 1);
-  BIMASK_CUDA_OK(launch_pdl(kern, grid, EPI ? LIN_THREADS : PAIR_THREADS, C::SMEM_BYTES, s, ta, tb, td, p, tr, e));
+  BIMASK_CUDA_OK(launch_pdl(kern, grid, EPI ? LIN_THREADS : PAIR_THREADS, smem, s, ta, tb, td, p, tr, e));
   count_launch();
   BIMASK_CUDA_OK(cudaGetLastError());
   return BIMASK_OK;
@@ -833,7 +837,8 @@ int run_sparse_pair_persistent(const uint16_t* vals, const void* hw_meta, const 
   EpiParams e;
   if ((rc = epi_args(le, Mdim, Ndim, td, &tr, &e)) != BIMASK_OK) return rc;
   auto kern = spmm_pair_persistent_kernel<STAGES, false, true, EPI>;
-  if ((rc = set_smem_attr(kern, C::SMEM_BYTES)) != BIMASK_OK) return rc;
+  constexpr int smem = C::SMEM_BYTES + (EPI ? epi_scales_bytes(C::EPI_NT) : 0);
+  if ((rc = set_smem_attr(kern, smem)) != BIMASK_OK) return rc;
   GemmParams p;
   p.conv.mode = 0;
   p.hw_meta = reinterpret_cast<const uint8_t*>(hw_meta);
@@ -848,7 +853,7 @@ int run_sparse_pair_persistent(const uint16_t* vals, const void* hw_meta, const 
   p.raster_group = 8;
   const int total = p.tiles_m * p.tiles_n;
   const int clusters = total < sms / 2 ? total : sms / 2;
-  BIMASK_CUDA_OK(launch_pdl(kern, 2 * clusters, EPI ? LIN_THREADS : PAIR_THREADS, C::SMEM_BYTES, s, ta, tb, te, td, p, tr, e));
+  BIMASK_CUDA_OK(launch_pdl(kern, 2 * clusters, EPI ? LIN_THREADS : PAIR_THREADS, smem, s, ta, tb, te, td, p, tr, e));
   count_launch();
   BIMASK_CUDA_OK(cudaGetLastError());
   return BIMASK_OK;
@@ -887,7 +892,8 @@ int run_sparse_pair2m(const uint16_t* vals, const void* hw_meta, const uint16_t*
   EpiParams e;
   if ((rc = epi_args(le, Mdim, Ndim, td, &tr, &e)) != BIMASK_OK) return rc;
   auto kern = spmm_pair2m_kernel<STAGES, EPI>;
-  if ((rc = set_smem_attr(kern, C::SMEM_BYTES)) != BIMASK_OK) return rc;
+  constexpr int smem = C::SMEM_BYTES + (EPI ? epi_scales_bytes(C::EPI_NT) : 0);
+  if ((rc = set_smem_attr(kern, smem)) != BIMASK_OK) return rc;
   GemmParams p;
   p.conv.mode = 0;
   p.hw_meta = reinterpret_cast<const uint8_t*>(hw_meta);
@@ -904,7 +910,7 @@ int run_sparse_pair2m(const uint16_t* vals, const void* hw_meta, const uint16_t*
   p.raster_group = 8;
   const int total = p.tiles_m * p.tiles_n;
   const int clusters = total < sms / 2 ? total : sms / 2;
-  BIMASK_CUDA_OK(launch_pdl(kern, 2 * clusters, EPI ? LIN_THREADS : GEMM2M_THREADS, C::SMEM_BYTES, s, ta, tb, te, td, p, tr, e));
+  BIMASK_CUDA_OK(launch_pdl(kern, 2 * clusters, EPI ? LIN_THREADS : GEMM2M_THREADS, smem, s, ta, tb, te, td, p, tr, e));
   count_launch();
   BIMASK_CUDA_OK(cudaGetLastError());
   return BIMASK_OK;
@@ -1079,7 +1085,8 @@ int run_dense_pair_persistent(const uint16_t* A, const uint16_t* Bop, int Mdim, 
   EpiParams e;
   if ((rc = epi_args(le, Mdim, Ndim, td, &tr, &e)) != BIMASK_OK) return rc;
   auto kern = spmm_pair_persistent_kernel<STAGES, false, false, EPI>;
-  if ((rc = set_smem_attr(kern, C::SMEM_BYTES)) != BIMASK_OK) return rc;
+  constexpr int smem = C::SMEM_BYTES + (EPI ? epi_scales_bytes(C::EPI_NT) : 0);
+  if ((rc = set_smem_attr(kern, smem)) != BIMASK_OK) return rc;
   GemmParams p;
   p.conv.mode = 0;
   p.hw_meta = nullptr;
@@ -1094,7 +1101,7 @@ int run_dense_pair_persistent(const uint16_t* A, const uint16_t* Bop, int Mdim, 
   p.raster_group = 8;
   const int total = p.tiles_m * p.tiles_n;
   const int clusters = total < sms / 2 ? total : sms / 2;
-  BIMASK_CUDA_OK(launch_pdl(kern, 2 * clusters, EPI ? LIN_THREADS : PAIR_THREADS, C::SMEM_BYTES, s, ta, tb, ta /* no metadata */, td, p, tr, e));
+  BIMASK_CUDA_OK(launch_pdl(kern, 2 * clusters, EPI ? LIN_THREADS : PAIR_THREADS, smem, s, ta, tb, ta /* no metadata */, td, p, tr, e));
   count_launch();
   BIMASK_CUDA_OK(cudaGetLastError());
   return BIMASK_OK;
