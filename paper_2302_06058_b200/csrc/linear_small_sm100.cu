@@ -19,7 +19,7 @@ struct SmallCfg {
   static constexpr int E_BYTES = SPARSE ? 2048 : 0;
   static constexpr int STAGE_BYTES = A_BYTES + B_BYTES + E_BYTES;
   static constexpr int PART_BYTES = N_TILE * 512;        // [token][128 rows] fp32, over the stages once they are done with
-  static constexpr int TMEM_COLS = N_TILE + 4 <= 64 ? 64 : N_TILE + 4 <= 128 ? 128 : 256;
+  static constexpr int TMEM_COLS = N_TILE + 4 <= 32 ? 32 : N_TILE + 4 <= 64 ? 64 : N_TILE + 4 <= 128 ? 128 : 256;
   static constexpr int SMEM_BYTES = STAGES * STAGE_BYTES + 1024 + 256;
   static_assert(PART_BYTES <= STAGES * STAGE_BYTES, "the partial sums lie over the stages");
 };
@@ -143,13 +143,13 @@ linear_small_kernel(const __grid_constant__ CUtensorMap tmapA, const __grid_cons
     if (__all_sync(0xFFFFFFFFu, ok)) {
       float* part = reinterpret_cast<float*>(base_ptr) + 32 * q + lane;
 #pragma unroll 1
-      for (int c = 0; c < N_TILE; c += 32) {
+      for (int c = 0; c < N_TILE; c += 16) {
         if (n0 + c >= p.Ndim) break;                      // no such tokens: nobody reads their sums
-        uint32_t r[32];
-        ptx::tmem_ld_32x32(tmem_base + ((uint32_t)(32 * q) << 16) + c, r);
+        uint32_t r[16];
+        ptx::tmem_ld_32x16(tmem_base + ((uint32_t)(32 * q) << 16) + c, r);
         ptx::tmem_ld_wait();
 #pragma unroll
-        for (int t = 0; t < 32; ++t) part[(c + t) * 128] = __uint_as_float(r[t]);
+        for (int t = 0; t < 16; ++t) part[(c + t) * 128] = __uint_as_float(r[t]);
       }
     }
   }
@@ -265,7 +265,10 @@ int run_small(const uint16_t* vals, const void* hw_meta, const uint16_t* X, int 
 template <bool SPARSE>
 int run_small_any(const uint16_t* vals, const void* hw_meta, const uint16_t* X, int Mdim, int Ndim, int Kdim, const LinearEpilogue& le,
                   uint16_t* out, int32_t* status_word, cudaStream_t s) {
-  // stages: what fits 220 KB (26 / 34 / 50 KB each, dense 40 / 48 / 64 KB)
+  // stages: what fits 220 KB (22 / 26 / 34 / 50 KB each, dense 36 / 40 / 48 / 64 KB)
+  // Very few tokens: narrower token tiles leave room for more stages of weights (one token, 4096 -> 16384: 16.0 -> 15.0 us;
+  // 16384 -> 4096: 16.0 -> 16.3; 16 tokens, 4096 -> 16384: 14.9 -> 15.3, so not there).
+  if (Ndim <= 8) return run_small<16, SPARSE ? 10 : 6, SPARSE>(vals, hw_meta, X, Mdim, Ndim, Kdim, le, out, status_word, s);
   if (Ndim <= 32) return run_small<32, SPARSE ? 8 : 5, SPARSE>(vals, hw_meta, X, Mdim, Ndim, Kdim, le, out, status_word, s);
   if (Ndim <= 64) return run_small<64, SPARSE ? 6 : 4, SPARSE>(vals, hw_meta, X, Mdim, Ndim, Kdim, le, out, status_word, s);
   return run_small<128, SPARSE ? 4 : 3, SPARSE>(vals, hw_meta, X, Mdim, Ndim, Kdim, le, out, status_word, s);
