@@ -463,10 +463,8 @@ spmm_pair_persistent_kernel(const __grid_constant__ CUtensorMap tmapA, const __g
       } else if constexpr (EPI) {
         if (!drain_chunks_epi<C::EPI_NT>(acc, ring, eg >> 1, nchunks, release_bar, stg, ebars, bar_base + EPI_SCALES_OFFSET + ring * (C::EPI_NT * 128),
                                          u, q, lane, e, bias, m0, n0, p.Mdim, p.Ndim,
-                                         abort_flag)) {
-          *abort_flag = 1;
-          break;
-        }
+                                         abort_flag))
+          *abort_flag = 1;                                 // the group leaves together, at the next tile's barrier
       } else if (!drain_chunks_tma<32, C::EPI_NT>(acc, eg, EPI_GROUPS, nchunks, false, release_bar, stg, ebars, u, q, lane,
                                                   abort_flag)) {
         *abort_flag = 1;
@@ -715,7 +713,7 @@ spmm_pair2m_kernel(const __grid_constant__ CUtensorMap tmapA, const __grid_const
                                              lane, abort_flag))
           *abort_flag = 1;
       }
-      if (*abort_flag) break;
+      if (!EPI && *abort_flag) break;                      // EPI: the group leaves together, at the next tile's barrier
     }
   } else {
     // store threads, one per epilogue group (EPI: the whole warp): the same walk over tiles, row tiles and chunks as the draining warps
