@@ -127,10 +127,15 @@ def lib() -> ctypes.CDLL:
     return _lib
 
 
+_Tensor = torch.Tensor
+
+
 def _ptr(x):
     """Address of a tensor's storage (device or pinned host), an int address, or None."""
     if x is None:
         return None
+    if type(x) is _Tensor and x.is_contiguous():         # the common case first: a call has up to nine of them
+        return x.data_ptr()
     if isinstance(x, int):
         return x
     if isinstance(x, torch.Tensor):

@@ -452,3 +452,20 @@ def test_offsets_past_32_bits():
     bm.bimask_ckpt_unpack(q, s, 0, T, C, x)
     bm.bimask_ckpt_unpack(q0, s0, 0, 3, C, dz)
     assert torch.equal(x[-3:], dz)
+
+
+def test_forward_offsets_past_32_bits():
+    """More than 2^31 results: the last tokens' results and checkpoint must be those of the same tokens alone."""
+    T, I, J, last = 131201, 16416, 64, 150
+    assert T * I > 1 << 31
+    vals, hw, _ = operand(np.random.default_rng(1).standard_normal((I, J)), 2, 4)
+    g = torch.Generator(device="cuda").manual_seed(2)
+    X = torch.randn(T, J, generator=g, device="cuda").to(torch.bfloat16)
+    bias = torch.randn(I, generator=g, device="cuda")
+    Y, q, s = run_linear(vals, hw, X, bias, bm.ACT_GELU, None, T, I, J, True)
+    Y0, q0, s0 = run_linear(vals, hw, X[-last:].contiguous(), bias, bm.ACT_GELU, None, last, I, J, True)
+    assert torch.equal(Y[-last:], Y0) and torch.equal(q[-last:], q0) and torch.equal(s[-last:], s0)
+    R = Y
+    Y2, _, _ = run_linear(vals, hw, X, None, bm.ACT_NONE, R, T, I, J, False, Y=R)
+    Y3, _, _ = run_linear(vals, hw, X[-last:].contiguous(), None, bm.ACT_NONE, Y0.clone(), last, I, J, False)
+    assert torch.equal(Y2[-last:], Y3)
