@@ -220,8 +220,9 @@ int bimask_ckpt_pack(const uint16_t* X, int T, int C, int8_t* q, uint8_t* s, voi
 int bimask_ckpt_unpack(const int8_t* q, const uint8_t* s, int act, int T, int C, uint16_t* X, void* stream);
 
 /* bimask_wgrad with the input as a checkpoint: dW[i, j] = sum_t dY[t, i] x[t, j], x the values of (Xq, Xs), dense, fp32.
- * No more than 8192 tokens are added up inside the tensor core, whose fp32 sums do not round to nearest; longer sums are
- * put together in fp32.   ws: scratch of bimask_linear_workspace_bytes(T, I, J) bytes */
+ * No more than 512 tokens are added up inside the tensor core, whose fp32 sums do not round to nearest (they make
+ * bimask_wgrad's error 9e-6 after 8192 tokens); longer sums are put together in fp32 registers: 2e-7.
+ *   ws: scratch of bimask_linear_workspace_bytes(T, I, J) bytes (the unpacked input, partial sums) */
 int bimask_wgrad_ckpt(const uint16_t* dY, const int8_t* Xq, const uint8_t* Xs, int T, int I, int J, float* dW, void* ws,
                       size_t ws_bytes, int32_t* status_word, void* stream);
 

