@@ -222,11 +222,11 @@ spmm_single_kernel(const __grid_constant__ CUtensorMap tmapA, const __grid_const
                                          chunk_walk<1>(p, (int)blockIdx.x, (int)gridDim.x, (int)gridDim.x, C::M_TILE, 0, 0, N_TILE, g)))
           *abort_flag = 1;
       } else {
-      uint32_t u = 0;
-      if (!store_chunks<32, C::EPI_NT>(&tmapD, g, EPI_GROUPS, N_TILE / 32, staging + g * (C::EPI_NT * 8192),
-                                       epi_bars_of<C::EPI_NT>(bar_base, g), u, m0, n0, p.Mdim, p.Ndim, abort_flag))
-        *abort_flag = 1;
-      store_finish();
+        uint32_t u = 0;
+        if (!store_chunks<32, C::EPI_NT>(&tmapD, g, EPI_GROUPS, N_TILE / 32, staging + g * (C::EPI_NT * 8192),
+                                         epi_bars_of<C::EPI_NT>(bar_base, g), u, m0, n0, p.Mdim, p.Ndim, abort_flag))
+          *abort_flag = 1;
+        store_finish();
       }
     }
   }
@@ -482,17 +482,17 @@ spmm_pair_persistent_kernel(const __grid_constant__ CUtensorMap tmapA, const __g
                                          chunk_walk<1>(p, cluster_id, num_clusters, num_tiles, 256, 128 * (int)rank, 0, SP_N, g)))
           *abort_flag = 1;
       } else {
-      uint32_t u = 0;
-      for (int tile = cluster_id; tile < num_tiles; tile += num_clusters) {
-        int tile_m, tile_n;
-        raster(tile, p.tiles_m, p.tiles_n, p.raster_group, tile_m, tile_n);
-        const int m0 = (2 * tile_m + (int)rank) * 128, n0 = tile_n * SP_N;
-        if (!store_chunks<32, C::EPI_NT>(&tmapD, g, EPI_GROUPS, SP_N / 32, stg, ebars, u, m0, n0, p.Mdim, p.Ndim, abort_flag)) {
-          *abort_flag = 1;
-          break;
+        uint32_t u = 0;
+        for (int tile = cluster_id; tile < num_tiles; tile += num_clusters) {
+          int tile_m, tile_n;
+          raster(tile, p.tiles_m, p.tiles_n, p.raster_group, tile_m, tile_n);
+          const int m0 = (2 * tile_m + (int)rank) * 128, n0 = tile_n * SP_N;
+          if (!store_chunks<32, C::EPI_NT>(&tmapD, g, EPI_GROUPS, SP_N / 32, stg, ebars, u, m0, n0, p.Mdim, p.Ndim, abort_flag)) {
+            *abort_flag = 1;
+            break;
+          }
         }
-      }
-      store_finish();
+        store_finish();
       }
     }
   }
@@ -726,17 +726,17 @@ spmm_pair2m_kernel(const __grid_constant__ CUtensorMap tmapA, const __grid_const
                                          chunk_walk<2>(p, cluster_id, num_clusters, num_tiles, 512, 128 * (int)rank, 256, SP_N, g)))
           *abort_flag = 1;
       } else {
-      uint32_t u = 0;
-      bool ok = true;
-      for (int tile = cluster_id; tile < num_tiles && ok; tile += num_clusters) {
-        int tile_m, tile_n;
-        raster(tile, p.tiles_m, p.tiles_n, p.raster_group, tile_m, tile_n);
-        for (int mt = 0; mt < 2 && ok; ++mt)
-          ok = store_chunks<32, C::EPI_NT>(&tmapD, (g ^ mt) & 1, 2, SP_N / 32, stg, ebars, u, mt128_of(tile_m, mt) * 128, tile_n * SP_N,
-                                           p.Mdim, p.Ndim, abort_flag);
-      }
-      if (!ok) *abort_flag = 1;
-      store_finish();
+        uint32_t u = 0;
+        bool ok = true;
+        for (int tile = cluster_id; tile < num_tiles && ok; tile += num_clusters) {
+          int tile_m, tile_n;
+          raster(tile, p.tiles_m, p.tiles_n, p.raster_group, tile_m, tile_n);
+          for (int mt = 0; mt < 2 && ok; ++mt)
+            ok = store_chunks<32, C::EPI_NT>(&tmapD, (g ^ mt) & 1, 2, SP_N / 32, stg, ebars, u, mt128_of(tile_m, mt) * 128, tile_n * SP_N,
+                                             p.Mdim, p.Ndim, abort_flag);
+        }
+        if (!ok) *abort_flag = 1;
+        store_finish();
       }
     }
   }
