@@ -4,8 +4,13 @@
 // products), leaves its fp32 partial sums in its own shared memory, and after a cluster barrier the CTAs add one another's
 // parts over distributed shared memory, token by token in rank order -- no workspace, no second kernel, and a result that
 // does not depend on timing -- and finish the layer on them: bias, checkpoint, activation, residual, one rounding.
-// One token, 4096 -> 16384 with the weights in HBM: 15.0 us (75.6 MB, 5.05 TB/s over the whole call; without the split and
-// the deep ring 34 us); 24 tokens, 16384 -> 4096: 16.3 us (54 us).  Left: start-up, the first loads' latency and the join,
+// The tensor core adds into its fp32 accumulator without rounding to nearest, and the error grows with the length of the
+// chain; so a chain ends after 32 MMAs (1024 products' worth of 2:4 reduction, 512 dense).  Two accumulators take the
+// segments in turn, and the draining warps, idle until the end otherwise, add each finished one to sums in registers,
+// rounded to nearest, while the next is under way.  A 2:4 row of 16384 positive products is off by at most
+// 5.0e-7 relative (dense operand 3.5e-7); as one chain 3.2e-5 (4.0e-5).  The end of a chain costs the issuing thread 0.06 us.
+// One token, 4096 -> 16384 with the weights in HBM: 15.7 us (75.6 MB, 4.8 TB/s over the whole call; without the split and
+// the deep ring 34 us); 24 tokens, 16384 -> 4096: 16.9 us (54 us).  Left: start-up, the first loads' latency and the join,
 // about 4 us.
 #include "gemm_common.cuh"
 
@@ -21,10 +26,12 @@ struct SmallCfg {
   static constexpr int B_BYTES = N_TILE * 256;
   static constexpr int E_BYTES = SPARSE ? 2048 : 0;
   static constexpr int STAGE_BYTES = A_BYTES + B_BYTES + E_BYTES;
+  static constexpr int SEGMENT = SPARSE ? 8 : 4;         // k tiles per chain: 32 MMAs
   static constexpr int PART_BYTES = N_TILE * 512;        // [token][128 rows] fp32, over the stages once they are done with
-  static constexpr int TMEM_COLS = N_TILE + 4 <= 32 ? 32 : N_TILE + 4 <= 64 ? 64 : N_TILE + 4 <= 128 ? 128 : 256;
+  static constexpr int TMEM_COLS = 4 * N_TILE;           // two accumulators, the metadata, rounded up to a power of two
   static constexpr int SMEM_BYTES = STAGES * STAGE_BYTES + 1024 + 256;
   static_assert(PART_BYTES <= STAGES * STAGE_BYTES, "the partial sums lie over the stages");
+  static_assert(8 * (2 * STAGES + 4) + 8 <= 256, "barriers, tensor-memory address and abort flag");
 };
 
 struct SmallParams {
@@ -52,8 +59,9 @@ linear_small_kernel(const __grid_constant__ CUtensorMap tmapA, const __grid_cons
   const uint32_t bar_base = base + STAGES * C::STAGE_BYTES;
   auto full_bar = [&](int s) { return bar_base + 8u * s; };
   auto empty_bar = [&](int s) { return bar_base + 8u * (STAGES + s); };
-  const uint32_t tmem_full_bar = bar_base + 8u * (2 * STAGES);
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(base_ptr + STAGES * C::STAGE_BYTES + 8 * (2 * STAGES + 1));
+  auto tmem_full_bar = [&](uint32_t b) { return bar_base + 8u * (2 * STAGES + b); };
+  auto tmem_empty_bar = [&](uint32_t b) { return bar_base + 8u * (2 * STAGES + 2 + b); };
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(base_ptr + STAGES * C::STAGE_BYTES + 8 * (2 * STAGES + 4));
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -70,7 +78,10 @@ linear_small_kernel(const __grid_constant__ CUtensorMap tmapA, const __grid_cons
       ptx::mbar_init(full_bar(s), 1);
       ptx::mbar_init(empty_bar(s), 1);
     }
-    ptx::mbar_init(tmem_full_bar, 1);
+    for (uint32_t b = 0; b < 2; ++b) {
+      ptx::mbar_init(tmem_full_bar(b), 1);
+      ptx::mbar_init(tmem_empty_bar(b), 4);               // the draining warps
+    }
     ptx::fence_barrier_init();
     ptx::prefetch_tmap(&tmapA);
     ptx::prefetch_tmap(&tmapB);
@@ -83,7 +94,7 @@ linear_small_kernel(const __grid_constant__ CUtensorMap tmapA, const __grid_cons
   __syncthreads();
   ptx::tc_fence_after();
   const uint32_t tmem_base = *tmem_slot;
-  const uint32_t tmem_meta = tmem_base + N_TILE;
+  const uint32_t tmem_meta = tmem_base + 2 * N_TILE;
   pdl_wait();
 
   if (warp == 0) {
@@ -114,45 +125,74 @@ linear_small_kernel(const __grid_constant__ CUtensorMap tmapA, const __grid_cons
     if (ptx::elect_one()) {
       constexpr uint32_t idesc = ptx::idesc_bf16(128, N_TILE, false, false, SPARSE);
       bool ok = true;
-      for (int it = 0; it < num_kt; ++it) {
-        const int s = it % STAGES;
-        if (!ptx::mbar_wait_bounded(full_bar(s), (uint32_t)(it / STAGES) & 1u, abort_flag, WAIT_BUDGET)) { *abort_flag = 1; ok = false; break; }
-        ptx::tc_fence_after();
-        const uint32_t a_s = base + s * C::STAGE_BYTES, b_s = a_s + C::A_BYTES;
-        if constexpr (SPARSE) {
-          ptx::tmem_cp_128x128b(tmem_meta, ptx::smem_desc(b_s + C::B_BYTES, 0, 128, 0));
+      int it = 0;
+      for (int seg = 0; it < num_kt && ok; ++seg) {
+        const uint32_t buf = (uint32_t)seg & 1u, acc = tmem_base + N_TILE * buf;
+        // both accumulators start out free
+        if (seg >= 2 && !ptx::mbar_wait_bounded(tmem_empty_bar(buf), ((uint32_t)(seg >> 1) & 1u) ^ 1u, abort_flag, WAIT_BUDGET)) { *abort_flag = 1; break; }
+        const int end = min(num_kt, it + C::SEGMENT);
+        for (int k = 0; it < end; ++it, ++k) {
+          const int s = it % STAGES;
+          if (!ptx::mbar_wait_bounded(full_bar(s), (uint32_t)(it / STAGES) & 1u, abort_flag, WAIT_BUDGET)) { *abort_flag = 1; ok = false; break; }
+          ptx::tc_fence_after();
+          const uint32_t a_s = base + s * C::STAGE_BYTES, b_s = a_s + C::A_BYTES;
+          if constexpr (SPARSE) {
+            ptx::tmem_cp_128x128b(tmem_meta, ptx::smem_desc(b_s + C::B_BYTES, 0, 128, 0));
 #pragma unroll
-          for (int kb = 0; kb < 4; ++kb)
-            ptx::mma_sparse(tmem_base, ptx::smem_desc(a_s + kb * 32, 16, 1024, 2),
-                            ptx::smem_desc(b_s + (kb >> 1) * (N_TILE * 128) + (kb & 1) * 64, 16, 1024, 2), tmem_meta + (kb & ~1),
-                            idesc | (uint32_t)(kb & 1), (it | kb) != 0);
-        } else {
+            for (int kb = 0; kb < 4; ++kb)
+              ptx::mma_sparse(acc, ptx::smem_desc(a_s + kb * 32, 16, 1024, 2),
+                              ptx::smem_desc(b_s + (kb >> 1) * (N_TILE * 128) + (kb & 1) * 64, 16, 1024, 2), tmem_meta + (kb & ~1),
+                              idesc | (uint32_t)(kb & 1), (k | kb) != 0);
+          } else {
 #pragma unroll
-          for (int kb = 0; kb < 8; ++kb)
-            ptx::mma_dense(tmem_base, ptx::smem_desc(a_s + (kb >> 2) * 16384 + (kb & 3) * 32, 16, 1024, 2),
-                           ptx::smem_desc(b_s + (kb >> 2) * (N_TILE * 128) + (kb & 3) * 32, 16, 1024, 2), idesc, (it | kb) != 0);
+            for (int kb = 0; kb < 8; ++kb)
+              ptx::mma_dense(acc, ptx::smem_desc(a_s + (kb >> 2) * 16384 + (kb & 3) * 32, 16, 1024, 2),
+                             ptx::smem_desc(b_s + (kb >> 2) * (N_TILE * 128) + (kb & 3) * 32, 16, 1024, 2), idesc, (k | kb) != 0);
+          }
+          ptx::tc_commit(empty_bar(s));
         }
-        ptx::tc_commit(empty_bar(s));
+        if (ok) ptx::tc_commit(tmem_full_bar(buf));
       }
-      if (ok) ptx::tc_commit(tmem_full_bar);
     }
   } else if (warp < 6) {
-    // accumulator -> shared memory, [token][row]: lane = row, so a store covers 128 contiguous bytes
+    // segments -> sums in registers (lane = row, a register per token) -> shared memory, [token][row]: a store covers 128
+    // contiguous bytes.  The last segment's commit says that every MMA is done with the stages.
     const int q = warp & 3;
-    const bool ok = ptx::mbar_wait_bounded(tmem_full_bar, 0, abort_flag, WAIT_BUDGET);
-    if (!ok) *abort_flag = 1;
-    ptx::tc_fence_after();
-    __syncwarp();
-    if (__all_sync(0xFFFFFFFFu, ok)) {
-      float* part = reinterpret_cast<float*>(base_ptr) + 32 * q + lane;
-#pragma unroll 1
-      for (int c = 0; c < N_TILE; c += 16) {
-        if (n0 + c >= p.Ndim) break;                      // no such tokens: nobody reads their sums
-        uint32_t r[16];
-        ptx::tmem_ld_32x16(tmem_base + ((uint32_t)(32 * q) << 16) + c, r);
-        ptx::tmem_ld_wait();
+    const int ntok = p.Ndim - n0;                         // columns past it hold nothing that anybody reads
+    float sum[N_TILE];
 #pragma unroll
-        for (int t = 0; t < 16; ++t) part[(c + t) * 128] = __uint_as_float(r[t]);
+    for (int t = 0; t < N_TILE; ++t) sum[t] = 0.f;
+    bool ok = true;
+#pragma unroll 1
+    for (int seg = 0; seg * C::SEGMENT < num_kt; ++seg) {
+      const uint32_t buf = (uint32_t)seg & 1u;
+      ok = ptx::mbar_wait_bounded(tmem_full_bar(buf), (uint32_t)(seg >> 1) & 1u, abort_flag, WAIT_BUDGET);
+      ok = __all_sync(0xFFFFFFFFu, ok);
+      if (!ok) { *abort_flag = 1; break; }
+      ptx::tc_fence_after();
+      const uint32_t acc = tmem_base + N_TILE * buf + ((uint32_t)(32 * q) << 16);
+#pragma unroll
+      for (int c = 0; c < N_TILE; c += 16) {
+        if (c < ntok) {
+          uint32_t r[16];
+          ptx::tmem_ld_32x16(acc + c, r);
+          ptx::tmem_ld_wait();
+#pragma unroll
+          for (int t = 0; t < 16; ++t) sum[c + t] += __uint_as_float(r[t]);
+        }
+      }
+      ptx::tc_fence_before();
+      __syncwarp();
+      if (lane == 0) ptx::mbar_arrive(tmem_empty_bar(buf));
+    }
+    if (ok) {
+      float* part = reinterpret_cast<float*>(base_ptr) + 32 * q + lane;
+#pragma unroll
+      for (int c = 0; c < N_TILE; c += 16) {
+        if (c < ntok) {
+#pragma unroll
+          for (int t = 0; t < 16; ++t) part[(c + t) * 128] = sum[c + t];
+        }
       }
     }
   }
