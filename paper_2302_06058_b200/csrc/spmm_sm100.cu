@@ -1137,6 +1137,10 @@ static bool split_is_faster(bool sparse, int Mdim, int Ndim, int Kdim) {
 
 // Linear layer: the product of launch_spmm (hw_meta given) or launch_dense_nt (null) with the epilogue of `le`, on the
 // same kernels by the same rules, and on the kernel for few tokens.
+// Sums: the kernels of this file keep one tensor-core chain over the reduction, which does not round to nearest (relative
+// error of a sum, mixed signs: 1.0e-7 at 384, 2.6e-7 at 2048, 1.3e-6 at 4096, 6.2e-6 at 16384; rounded fp32 sums about
+// 1e-7).  A choice for speed: ending the chains early takes a second accumulator, for which the 512-row tiles of the wide
+// layers leave no tensor memory, and 256-row tiles are bound by the L2 feed (16384 x 4096 at 8192 tokens 655 against 575 us).
 int launch_linear_fwd(const uint16_t* vals, const void* hw_meta, const uint16_t* X, int Mdim, int Ndim, int Kdim,
                       const LinearEpilogue& le, uint16_t* out, int32_t* status_word, cudaStream_t s) {
   if (Ndim <= 128 || (Mdim > 128 && split_is_faster(hw_meta != nullptr, Mdim, Ndim, Kdim)))
