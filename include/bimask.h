@@ -409,6 +409,13 @@ size_t bimask_perm_search_static_max_entries(void);
  * normally (no trap: the context stays usable). */
 int bimask_debug_wait_probe(int32_t* status_word, void* stream);
 
+/* Debug helper, host only: what a tensor-core kernel that gave up (BIMASK_ETIMEOUT) waits for before it ends, when its
+ * producers had issued issued0 and issued1 loads (the two CTAs of a pair; equal for a single CTA) into rings of `stages`
+ * stages.  Writes up to 2 * stages rows {stage, phase parity, settle} to the HOST array `out`, in order, and returns
+ * their number (settle: 0 both issued the load; 1 only CTA 1 did: CTA 0 arrives and expects its bytes; 2 only CTA 0
+ * did: the other's bytes are counted as sent), or BIMASK_EINVAL. */
+int bimask_debug_drain_plan(int issued0, int issued1, int stages, int32_t* out);
+
 /* Debug build (libbimask_debug.so, compiled with -DBIMASK_DEBUG): every kernel that turns a caller-supplied row
  * index (an entry of perm or of a candidate) into an address checks it against I.  Both builds clamp a bad index
  * into range, so nothing can fault; the debug build also records the first offender.  This call waits for the

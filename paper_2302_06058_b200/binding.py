@@ -22,7 +22,7 @@ EXPORTS = ("bimask_last_error", "bimask_launch_count", "bimask_hw_meta_bytes", "
            "bimask_check_perms", "bimask_debug_wait_probe", "bimask_perm_search_static",
            "bimask_perm_search_static_max_entries", "bimask_sgd_fwd_mask", "bimask_train_step",
            "bimask_bwd_mask_criterion", "bimask_conv_workspace_bytes", "bimask_conv_layer_step",
-           "bimask_refine_workspace_bytes", "bimask_perm_refine", "bimask_debug_gen_candidates", "bimask_debug_status",
+           "bimask_refine_workspace_bytes", "bimask_perm_refine", "bimask_debug_gen_candidates", "bimask_debug_status", "bimask_debug_drain_plan",
            "bimask_linear_workspace_bytes", "bimask_linear_fwd", "bimask_act_bwd", "bimask_ckpt_pack", "bimask_ckpt_unpack",
            "bimask_wgrad_ckpt")
 
@@ -114,6 +114,7 @@ def lib() -> ctypes.CDLL:
         L.bimask_check_perms.argtypes = [c_void_p, c_int, c_int, c_void_p, c_void_p, c_size_t, c_void_p]
         L.bimask_debug_wait_probe.argtypes = [c_void_p, c_void_p]
         L.bimask_debug_status.argtypes = [c_void_p]
+        L.bimask_debug_drain_plan.argtypes = [c_int, c_int, c_int, c_void_p]
         L.bimask_debug_gen_candidates.argtypes = [c_uint64, c_int, c_int, c_int, c_void_p, c_void_p]
         L.bimask_perm_search_static.argtypes = [c_void_p, c_int, c_int, c_int, c_int, c_int, c_uint64,
                                                 c_void_p, c_void_p, c_void_p, c_void_p]
@@ -328,6 +329,15 @@ def bimask_host_sync():
 
 def bimask_debug_wait_probe(status_word, stream=None):
     return _check(lib().bimask_debug_wait_probe(_ptr(status_word), _stream(stream)))
+
+
+def bimask_debug_drain_plan(issued0, issued1, stages):
+    """[(stage, parity, settle), ...] that a kernel which gave up waits for."""
+    out = (c_int32 * (6 * max(stages, 1)))()
+    n = lib().bimask_debug_drain_plan(issued0, issued1, stages, ctypes.cast(out, c_void_p))
+    if n < 0:
+        _check(n)
+    return [tuple(out[3 * i:3 * i + 3]) for i in range(n)]
 
 
 def bimask_debug_status():

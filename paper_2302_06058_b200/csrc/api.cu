@@ -864,6 +864,19 @@ int bimask_debug_wait_probe(int32_t* status_word, void* stream) {
   return launch_wait_probe(status_word, (cudaStream_t)stream);
 }
 
+int bimask_debug_drain_plan(int issued0, int issued1, int stages, int32_t* out) {
+  const int gap = issued0 < issued1 ? issued1 - issued0 : issued0 - issued1;
+  BIMASK_REQUIRE(out != nullptr && issued0 >= 0 && issued1 >= 0 && stages > 0 && gap <= stages, BIMASK_EINVAL,
+                 "bimask_debug_drain_plan: issued %d, %d with %d stages", issued0, issued1, stages);
+  int n = 0;
+  for (int k = drain_begin(issued0, issued1, stages); k < drain_end(issued0, issued1); ++k, ++n) {
+    out[3 * n] = k % stages;
+    out[3 * n + 1] = (k / stages) & 1;
+    out[3 * n + 2] = drain_settle(k, issued0, issued1);
+  }
+  return n;
+}
+
 int bimask_debug_status(int32_t* out) {
   BIMASK_REQUIRE(out != nullptr, BIMASK_EINVAL, "bimask_debug_status: null pointer");
   out[0] = out[1] = out[2] = out[3] = 0;

@@ -32,6 +32,27 @@ int cuda_fail(cudaError_t e, const char* what);
 
 static inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
+#ifdef __CUDACC__
+#define BIMASK_HD __host__ __device__
+#else
+#define BIMASK_HD
+#endif
+// Loads still in flight when a tensor-core kernel gives up.  A producer has issued loads 0 .. issued - 1 in order into a ring
+// of `stages` stages; of a CTA pair, whose loads of one stage complete on ONE barrier of rank 0, the two counts may
+// differ (by at most `stages`: the next round of a stage starts after both loads of this one).  Waiting for the loads
+// from drain_begin to drain_end on their barriers, each in its phase (k / stages) & 1, is waiting for all of them, once a load
+// that only one CTA issued has been made up for: rank 0 arrives and expects the peer's bytes, or counts the bytes that
+// the peer never sent.
+enum { SETTLE_NONE = 0, SETTLE_EXPECT = 1, SETTLE_COUNT = 2 };
+BIMASK_HD inline int drain_begin(int issued0, int issued1, int stages) {
+  const int both = issued0 < issued1 ? issued0 : issued1;
+  return both > stages ? both - stages : 0;
+}
+BIMASK_HD inline int drain_end(int issued0, int issued1) { return issued0 < issued1 ? issued1 : issued0; }
+BIMASK_HD inline int drain_settle(int k, int issued0, int issued1) {
+  return k >= issued0 ? SETTLE_EXPECT : k >= issued1 ? SETTLE_COUNT : SETTLE_NONE;
+}
+
 // Programmatic dependent launch.  Every kernel of the library is launched with the attribute below, tells the
 // runtime at its very start that the next kernel in the stream may be scheduled (pdl_launch_dependents) and
 // waits for the kernels before it (pdl_wait) only after the part of its prologue that touches no global memory:

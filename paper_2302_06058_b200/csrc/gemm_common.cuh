@@ -14,6 +14,7 @@ namespace bimask {
 
 
 constexpr long long WAIT_BUDGET = 4000000000ll;      // ~2 s of SM clocks
+constexpr long long DRAIN_BUDGET = 100000000ll;      // ~50 ms: a load that has been issued lands within microseconds
 constexpr int GEMM_THREADS = 192;                    // warp 0 TMA, warp 1 MMA, warps 2-5 epilogue
 // The sparse kernels that drain bf16 results use eight epilogue warps (two groups of four, one warp per
 // tensor-memory lane quadrant, taking alternate column chunks): products with a short reduction are bound by
@@ -46,6 +47,76 @@ struct Cfg {
   static constexpr int TMEM_COLS = (N_TILE + META_COLS) <= 128 ? 128 : (N_TILE + META_COLS) <= 256 ? 256 : 512;
   static constexpr int SMEM_BYTES = STAGES * STAGE_BYTES + 1024 /* alignment slack */ + 256 /* barriers */ +
                                     epi_staging_bytes(EPI_NT) /* epilogue staging */;
+};
+
+// ---- leaving a kernel ---------------------------------------------------------------------------
+// A role whose wait runs out of budget raises the CTA's abort flag and leaves; the others follow.  Before such a CTA may free
+// its tensor memory and end, the MMAs issued so far and the loads in flight into its shared memory must have finished,
+// whichever role gave up: the producer may have left long before with everything issued.  In shared memory behind the
+// tensor-memory address: the abort flag, the number of loads that the producer issued, a barrier for the MMAs.
+struct Unwind {
+  volatile int* abort_flag;
+  volatile int* issued;
+  uint32_t mma_bar;
+  __device__ __forceinline__ explicit Unwind(uint32_t* tmem_slot)
+      : abort_flag(reinterpret_cast<volatile int*>(tmem_slot + 1)), issued(reinterpret_cast<volatile int*>(tmem_slot + 2)),
+        mma_bar(ptx::smem_u32(tmem_slot) + 16u) {}
+  static constexpr int BYTES = 24;                                // with the tensor-memory address
+  __device__ __forceinline__ void init() const {                  // one thread, before fence_barrier_init
+    *abort_flag = 0;
+    *issued = 0;
+    ptx::mbar_init(mma_bar, 1);
+  }
+  __device__ __forceinline__ void drain_loads(uint32_t full_bar0, int stages, int issued0, int issued1, uint32_t cta_bytes) const {
+    volatile int none = 0;
+    for (int k = drain_begin(issued0, issued1, stages); k < drain_end(issued0, issued1); ++k) {
+      const uint32_t bar = full_bar0 + 8u * (uint32_t)(k % stages);
+      const int settle = drain_settle(k, issued0, issued1);
+      if (settle == SETTLE_EXPECT) ptx::mbar_expect_tx(bar, cta_bytes);
+      if (settle == SETTLE_COUNT) ptx::mbar_complete_tx(bar, cta_bytes);
+      ptx::mbar_wait_bounded(bar, (uint32_t)(k / stages) & 1u, &none, DRAIN_BUDGET);
+    }
+  }
+  // All threads, after the barrier that joins the roles.  Warp 1 issued the MMAs (elect_one picks the same lane each time, and
+  // a commit covers what its thread has issued).
+  __device__ __forceinline__ void leave(uint32_t full_bar0, int stages, int warp, int32_t* status_word) const {
+    if (!*abort_flag) return;
+    volatile int none = 0;
+    if (warp == 1 && ptx::elect_one()) {
+      ptx::tc_commit(mma_bar);
+      ptx::mbar_wait_bounded(mma_bar, 0, &none, DRAIN_BUDGET);
+    }
+    if (threadIdx.x == 0) {
+      atomicExch(status_word, (int32_t)BIMASK_ETIMEOUT);
+      drain_loads(full_bar0, stages, *issued, *issued, 0u);
+    }
+    __syncthreads();
+  }
+  // The same for a CTA pair, cluster barrier included: both leave together.  cta_bytes: one CTA's bytes per stage.
+  __device__ __forceinline__ void leave_pair(uint32_t full_bar0, int stages, uint32_t cta_bytes, uint32_t rank, int warp,
+                                             int32_t* status_word) const {
+    const uint32_t flag = ptx::smem_u32(const_cast<int*>(abort_flag));
+    if (threadIdx.x == 0 && *abort_flag) {
+      atomicExch(status_word, (int32_t)BIMASK_ETIMEOUT);
+      ptx::st_cluster_u32(ptx::mapa(flag, rank ^ 1u), 1u);
+    }
+    __syncwarp();
+    ptx::cluster_sync();
+    if (!*abort_flag) return;
+    if (rank == 0) {
+      volatile int none = 0;
+      if (warp == 1 && ptx::elect_one()) {
+        ptx::tc_commit_pair(mma_bar, 1);
+        ptx::mbar_wait_bounded(mma_bar, 0, &none, DRAIN_BUDGET);
+      }
+      if (threadIdx.x == 0) {
+        const uint32_t peer = ptx::mapa(ptx::smem_u32(const_cast<int*>(issued)), 1);
+        drain_loads(full_bar0, stages, *issued, (int)ptx::ld_cluster_u32(peer), cta_bytes);
+      }
+    }
+    __syncthreads();
+    ptx::cluster_sync();
+  }
 };
 
 // A 3x3 convolution as an implicit GEMM: the token operand is an NHWC tensor and a "tile of
@@ -583,10 +654,10 @@ __device__ __forceinline__ bool store_chunks_epi(const CUtensorMap* tmapD, const
     }
   }
   if (lane == 0) {
-    if (!ok && has_res) {                                 // giving up: no load may be in flight when the kernel ends
+    if (has_res) {                                        // no load may be in flight when the kernel ends, whoever gave up
       volatile int none = 0;
       for (uint32_t n = loaded > NT ? loaded - NT : 0; n < loaded; ++n)
-        ptx::mbar_wait_bounded(bars + 8u * (NT + n % NT), (n / NT) & 1u, &none, WAIT_BUDGET);
+        ptx::mbar_wait_bounded(bars + 8u * (NT + n % NT), (n / NT) & 1u, &none, DRAIN_BUDGET);
     }
     store_finish();
   }

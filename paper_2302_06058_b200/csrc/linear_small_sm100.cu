@@ -31,7 +31,7 @@ struct SmallCfg {
   static constexpr int TMEM_COLS = 4 * N_TILE;           // two accumulators, the metadata, rounded up to a power of two
   static constexpr int SMEM_BYTES = STAGES * STAGE_BYTES + 1024 + 256;
   static_assert(PART_BYTES <= STAGES * STAGE_BYTES, "the partial sums lie over the stages");
-  static_assert(8 * (2 * STAGES + 4) + 8 <= 256, "barriers, tensor-memory address and abort flag");
+  static_assert(8 * (2 * STAGES + 4) + Unwind::BYTES <= 256, "barriers, tensor-memory address and what leaving needs");
 };
 
 struct SmallParams {
@@ -62,7 +62,8 @@ linear_small_kernel(const __grid_constant__ CUtensorMap tmapA, const __grid_cons
   auto tmem_full_bar = [&](uint32_t b) { return bar_base + 8u * (2 * STAGES + b); };
   auto tmem_empty_bar = [&](uint32_t b) { return bar_base + 8u * (2 * STAGES + 2 + b); };
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(base_ptr + STAGES * C::STAGE_BYTES + 8 * (2 * STAGES + 4));
-  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  const Unwind unwind(tmem_slot);
+  volatile int* abort_flag = unwind.abort_flag;
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int rank = (int)ptx::cluster_ctarank();           // = blockIdx.x % splits
@@ -73,7 +74,7 @@ linear_small_kernel(const __grid_constant__ CUtensorMap tmapA, const __grid_cons
   const int num_kt = min(p.tiles_k, kt_begin + p.k_per_split) - kt_begin;   // >= 1: the host leaves no CTA without work
 
   if (threadIdx.x == 0) {
-    *abort_flag = 0;
+    unwind.init();
     for (int s = 0; s < STAGES; ++s) {
       ptx::mbar_init(full_bar(s), 1);
       ptx::mbar_init(empty_bar(s), 1);
@@ -116,10 +117,7 @@ linear_small_kernel(const __grid_constant__ CUtensorMap tmapA, const __grid_cons
         ptx::tma_load_2d(b_s, &tmapB, kt * 128, n0, full_bar(s));
         ptx::tma_load_2d(b_s + N_TILE * 128, &tmapB, kt * 128 + 64, n0, full_bar(s));
       }
-      if (it < num_kt) {                                  // giving up: no load may be in flight when the CTA ends
-        volatile int none = 0;
-        for (int k = max(0, it - STAGES); k < it; ++k) ptx::mbar_wait_bounded(full_bar(k % STAGES), (uint32_t)(k / STAGES) & 1u, &none, WAIT_BUDGET);
-      }
+      *unwind.issued = it;
     }
   } else if (warp == 1) {
     if (ptx::elect_one()) {
@@ -200,12 +198,12 @@ linear_small_kernel(const __grid_constant__ CUtensorMap tmapA, const __grid_cons
   // every CTA's partial sums are in place (or its abort flag is up: then the results are void, and the status says so)
   ptx::tc_fence_before();
   __syncthreads();
+  unwind.leave(full_bar(0), STAGES, warp, p.status_word);
   if (splits > 1) ptx::cluster_sync();
   if (warp == 1) {
     ptx::tc_fence_after();
     ptx::tmem_dealloc(tmem_base, C::TMEM_COLS);
   }
-  if (threadIdx.x == 0 && *abort_flag) atomicExch(p.status_word, (int32_t)BIMASK_ETIMEOUT);
 
   // tokens rank, rank + splits, ... are this CTA's to finish, two at a time per warp: lane = four rows
   const int ntok = min(N_TILE, p.Ndim - n0);

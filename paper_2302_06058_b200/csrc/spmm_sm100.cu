@@ -15,8 +15,8 @@
 // takes a dense A operand (masked weights of a pattern the 2:4 format cannot hold).
 //
 // Every wait on an mbarrier carries a cycle budget: when it runs out the kernel writes
-// BIMASK_ETIMEOUT to the caller's status word, all roles unwind, tensor memory is released and
-// the kernel returns.
+// BIMASK_ETIMEOUT to the caller's status word, all roles unwind, the MMAs and loads in flight finish
+// (Unwind in gemm_common.cuh), tensor memory is released and the kernel returns.
 #include "gemm_common.cuh"
 
 namespace bimask {
@@ -46,7 +46,8 @@ spmm_single_kernel(const __grid_constant__ CUtensorMap tmapA, const __grid_const
   auto empty_bar = [&](int s) { return bar_base + 8u * (STAGES + s); };
   const uint32_t tmem_full_bar = bar_base + 8u * (2 * STAGES);
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(base_ptr + STAGES * C::STAGE_BYTES + epi_staging_bytes(C::EPI_NT) + 8 * (2 * STAGES + 1));
-  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  const Unwind unwind(tmem_slot);
+  volatile int* abort_flag = unwind.abort_flag;
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   int tile_m, tile_n;
@@ -61,7 +62,7 @@ spmm_single_kernel(const __grid_constant__ CUtensorMap tmapA, const __grid_const
   const int num_kt = kt_end - kt_begin;
 
   if (threadIdx.x == 0) {
-    *abort_flag = 0;
+    unwind.init();
     for (int s = 0; s < STAGES; ++s) {
       ptx::mbar_init(full_bar(s), 1);
       ptx::mbar_init(empty_bar(s), 1);
@@ -87,7 +88,8 @@ spmm_single_kernel(const __grid_constant__ CUtensorMap tmapA, const __grid_const
   if (warp == 0) {
     // ------------------------------ TMA producer ------------------------------
     if (ptx::elect_one()) {
-      for (int it = 0; it < num_kt; ++it) {
+      int it = 0;
+      for (; it < num_kt; ++it) {
         const int s = it % STAGES;
         const uint32_t ph = (uint32_t)(it / STAGES) & 1u;
         if (!ptx::mbar_wait_bounded(empty_bar(s), ph ^ 1u, abort_flag, WAIT_BUDGET)) { *abort_flag = 1; break; }
@@ -139,6 +141,7 @@ spmm_single_kernel(const __grid_constant__ CUtensorMap tmapA, const __grid_const
           ptx::bulk_load(b_s + C::B_BYTES,
                          p.hw_meta + ((size_t)tile_m * p.tiles_k_meta + kt) * 2048, 2048, full_bar(s));
       }
+      *unwind.issued = (int)it;
     }
   } else if (warp == 1) {
     // ------------------------------ MMA issuer ------------------------------
@@ -233,7 +236,7 @@ spmm_single_kernel(const __grid_constant__ CUtensorMap tmapA, const __grid_const
 
   ptx::tc_fence_before();
   __syncthreads();
-  if (threadIdx.x == 0 && *abort_flag) atomicExch(p.status_word, (int32_t)BIMASK_ETIMEOUT);
+  unwind.leave(full_bar(0), STAGES, warp, p.status_word);
   if (warp == 1) {
     ptx::tc_fence_after();
     ptx::tmem_dealloc(tmem_base, C::TMEM_COLS);
@@ -290,7 +293,8 @@ spmm_pair_persistent_kernel(const __grid_constant__ CUtensorMap tmapA, const __g
   auto tmem_full_bar = [&](int b) { return bar_base + 8u * (2 * STAGES + b); };
   auto tmem_empty_bar = [&](int b) { return bar_base + 8u * (2 * STAGES + 2 + b); };
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(staging_ptr + C::STAGING_BYTES + 8 * (2 * STAGES + 4));
-  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  const Unwind unwind(tmem_slot);
+  volatile int* abort_flag = unwind.abort_flag;
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = ptx::cluster_ctarank();
@@ -303,7 +307,7 @@ spmm_pair_persistent_kernel(const __grid_constant__ CUtensorMap tmapA, const __g
   const uint32_t stage_tx = C::A_BYTES + 2u * b_box + C::E_BYTES;
 
   if (threadIdx.x == 0) {
-    *abort_flag = 0;
+    unwind.init();
     for (int s = 0; s < STAGES; ++s) {
       ptx::mbar_init(full_bar(s), 1);
       ptx::mbar_init(empty_bar(s), 1);
@@ -382,6 +386,7 @@ spmm_pair_persistent_kernel(const __grid_constant__ CUtensorMap tmapA, const __g
           if (SPARSE) ptx::tma_load_2d_pair(b_s + C::B_MAX, &tmapE, 0, 2 * (mt128 * p.tiles_k_meta + kt), bar);
         }
       }
+      *unwind.issued = (int)it;
     }
   } else if (warp == 1) {
     if (rank == 0 && ptx::elect_one()) {
@@ -499,8 +504,7 @@ spmm_pair_persistent_kernel(const __grid_constant__ CUtensorMap tmapA, const __g
 
   ptx::tc_fence_before();
   __syncthreads();
-  if (threadIdx.x == 0 && *abort_flag) atomicExch(p.status_word, (int32_t)BIMASK_ETIMEOUT);
-  ptx::cluster_sync();
+  unwind.leave_pair(full_bar(0), STAGES, stage_tx, rank, warp, p.status_word);
   if (warp == 1) {
     ptx::tc_fence_after();
     ptx::tmem_dealloc_pair(tmem_base, C::TMEM_COLS);
@@ -556,7 +560,8 @@ spmm_pair2m_kernel(const __grid_constant__ CUtensorMap tmapA, const __grid_const
   const uint32_t tmem_empty_bar0 = bar_base + 8u * (2 * STAGES + 1);   // accumulator 0 drained
   const uint32_t tmem_empty_bar1 = bar_base + 8u * (2 * STAGES + 2);   // accumulator 1 drained
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(staging_ptr + C::STAGING_BYTES + 8 * (2 * STAGES + 3));
-  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  const Unwind unwind(tmem_slot);
+  volatile int* abort_flag = unwind.abort_flag;
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = ptx::cluster_ctarank();
@@ -568,7 +573,7 @@ spmm_pair2m_kernel(const __grid_constant__ CUtensorMap tmapA, const __grid_const
   const uint32_t stage_tx = 2u * C::A_BYTES + 2u * b_box + 2u * C::E_BYTES;
 
   if (threadIdx.x == 0) {
-    *abort_flag = 0;
+    unwind.init();
     for (int s = 0; s < STAGES; ++s) {
       ptx::mbar_init(full_bar(s), 1);
       ptx::mbar_init(empty_bar(s), 1);
@@ -625,6 +630,7 @@ spmm_pair2m_kernel(const __grid_constant__ CUtensorMap tmapA, const __grid_const
           ptx::tma_load_2d_pair(b_s + b_box, &tmapB, kt * 128 + 64, nrow, bar);
         }
       }
+      *unwind.issued = (int)it;
     }
   } else if (warp == 1) {
     if (rank == 0 && ptx::elect_one()) {
@@ -743,8 +749,7 @@ spmm_pair2m_kernel(const __grid_constant__ CUtensorMap tmapA, const __grid_const
 
   ptx::tc_fence_before();
   __syncthreads();
-  if (threadIdx.x == 0 && *abort_flag) atomicExch(p.status_word, (int32_t)BIMASK_ETIMEOUT);
-  ptx::cluster_sync();
+  unwind.leave_pair(full_bar(0), STAGES, stage_tx, rank, warp, p.status_word);
   if (warp == 1) {
     ptx::tc_fence_after();
     ptx::tmem_dealloc_pair(tmem_base, C::TMEM_COLS);

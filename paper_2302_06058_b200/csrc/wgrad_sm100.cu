@@ -118,7 +118,8 @@ wgrad_pair_kernel(const __grid_constant__ CUtensorMap tmapA, const __grid_consta
   auto tmem_full_bar = [&](int b) { return bar_base + 8u * (2 * STAGES + b); };
   auto tmem_empty_bar = [&](int b) { return bar_base + 8u * (2 * STAGES + 2 + b); };
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(base_ptr + STAGES * C::STAGE_BYTES + WGRAD_STAGING_BYTES + 8 * (2 * STAGES + 4));
-  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  const Unwind unwind(tmem_slot);
+  volatile int* abort_flag = unwind.abort_flag;
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = ptx::cluster_ctarank();
@@ -128,7 +129,7 @@ wgrad_pair_kernel(const __grid_constant__ CUtensorMap tmapA, const __grid_consta
   const int k_tiles_total = (p.Kdim + 63) / 64;
 
   if (threadIdx.x == 0) {
-    *abort_flag = 0;
+    unwind.init();
     for (int s = 0; s < STAGES; ++s) {
       ptx::mbar_init(full_bar(s), 1);
       ptx::mbar_init(empty_bar(s), 1);
@@ -202,6 +203,7 @@ wgrad_pair_kernel(const __grid_constant__ CUtensorMap tmapA, const __grid_consta
           ptx::tma_load_2d_pair(b_s + 8192, &tmapB, n0 + 128 * (int)rank + 64, kt * 64, bar);
         }
       }
+      *unwind.issued = (int)it;
     }
   } else if (warp == 1) {
     if (rank == 0 && ptx::elect_one()) {
@@ -265,8 +267,7 @@ wgrad_pair_kernel(const __grid_constant__ CUtensorMap tmapA, const __grid_consta
 
   ptx::tc_fence_before();
   __syncthreads();
-  if (threadIdx.x == 0 && *abort_flag) atomicExch(p.status_word, (int32_t)BIMASK_ETIMEOUT);
-  ptx::cluster_sync();
+  unwind.leave_pair(full_bar(0), STAGES, C::STAGE_BYTES, rank, warp, p.status_word);
   if (warp == 1) {
     ptx::tc_fence_after();
     ptx::tmem_dealloc_pair(tmem_base, C::TMEM_COLS);
@@ -304,7 +305,8 @@ wgrad_single_kernel(const __grid_constant__ CUtensorMap tmapA, const __grid_cons
   auto tmem_full_bar = [&](int b) { return bar_base + 8u * (2 * STAGES + b); };
   auto tmem_empty_bar = [&](int b) { return bar_base + 8u * (2 * STAGES + 2 + b); };
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(base_ptr + STAGES * C::STAGE_BYTES + WGRAD_STAGING_BYTES + 8 * (2 * STAGES + 4));
-  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  const Unwind unwind(tmem_slot);
+  volatile int* abort_flag = unwind.abort_flag;
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int num_tiles = p.tiles_m * p.tiles_n;            // tiles_m counts 128-row tiles
@@ -312,7 +314,7 @@ wgrad_single_kernel(const __grid_constant__ CUtensorMap tmapA, const __grid_cons
   const int k_tiles_total = (p.Kdim + 63) / 64;
 
   if (threadIdx.x == 0) {
-    *abort_flag = 0;
+    unwind.init();
     for (int s = 0; s < STAGES; ++s) {
       ptx::mbar_init(full_bar(s), 1);
       ptx::mbar_init(empty_bar(s), 1);
@@ -383,6 +385,7 @@ wgrad_single_kernel(const __grid_constant__ CUtensorMap tmapA, const __grid_cons
           for (int q = 0; q < 4; ++q) ptx::tma_load_2d(b_s + q * 8192, &tmapB, n0 + 64 * q, kt * 64, full_bar(s));
         }
       }
+      *unwind.issued = (int)it;
     }
   } else if (warp == 1) {
     if (ptx::elect_one()) {
@@ -445,7 +448,7 @@ wgrad_single_kernel(const __grid_constant__ CUtensorMap tmapA, const __grid_cons
 
   ptx::tc_fence_before();
   __syncthreads();
-  if (threadIdx.x == 0 && *abort_flag) atomicExch(p.status_word, (int32_t)BIMASK_ETIMEOUT);
+  unwind.leave(full_bar(0), STAGES, warp, p.status_word);
   if (warp == 1) {
     ptx::tc_fence_after();
     ptx::tmem_dealloc(tmem_base, C::TMEM_COLS);
@@ -488,7 +491,8 @@ wgrad_ckpt_kernel(const __grid_constant__ CUtensorMap tmapA, const __grid_consta
   auto tmem_full_bar = [&](int b) { return bar_base + 8u * (2 * STAGES + b); };
   auto tmem_empty_bar = [&](int b) { return bar_base + 8u * (2 * STAGES + 2 + b); };
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(base_ptr + STAGES * C::STAGE_BYTES + WGRAD_STAGING_BYTES + 8 * (2 * STAGES + 4));
-  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  const Unwind unwind(tmem_slot);
+  volatile int* abort_flag = unwind.abort_flag;
   // staging tile t is full; group g's turn at its next tile has come (a barrier per GROUP: an mbarrier's parity tells a
   // waiter only about the phase after the last one it saw, and the four groups take turns at the two tiles)
   auto staged_bar = [&](int t) { return bar_base + 160u + 8u * t; };
@@ -502,7 +506,7 @@ wgrad_ckpt_kernel(const __grid_constant__ CUtensorMap tmapA, const __grid_consta
   const int k_tiles_total = (p.Kdim + 63) / 64;
 
   if (threadIdx.x == 0) {
-    *abort_flag = 0;
+    unwind.init();
     for (int s = 0; s < STAGES; ++s) {
       ptx::mbar_init(full_bar(s), 1);
       ptx::mbar_init(empty_bar(s), 1);
@@ -559,6 +563,7 @@ wgrad_ckpt_kernel(const __grid_constant__ CUtensorMap tmapA, const __grid_consta
           ptx::tma_load_2d_pair(b_s + 8192, &tmapB, n0 + 128 * (int)rank + 64, kt * 64, bar);
         }
       }
+      *unwind.issued = (int)it;
     }
   } else if (warp == 1) {
     if (rank == 0 && ptx::elect_one()) {
@@ -670,8 +675,7 @@ wgrad_ckpt_kernel(const __grid_constant__ CUtensorMap tmapA, const __grid_consta
 
   ptx::tc_fence_before();
   __syncthreads();
-  if (threadIdx.x == 0 && *abort_flag) atomicExch(p.status_word, (int32_t)BIMASK_ETIMEOUT);
-  ptx::cluster_sync();
+  unwind.leave_pair(full_bar(0), STAGES, C::STAGE_BYTES, rank, warp, p.status_word);
   if (warp == 1) {
     ptx::tc_fence_after();
     ptx::tmem_dealloc_pair(tmem_base, 512);
