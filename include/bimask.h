@@ -77,7 +77,7 @@ uint64_t bimask_launch_count(void);
 size_t bimask_hw_meta_bytes(int rows, int K);
 
 /* Bytes of scratch (`ws`) large enough for every call below on a layer of this size, except those that name a size
- * query of their own. */
+ * query of their own.  Never smaller for more tokens: one buffer for the largest T serves every smaller batch. */
 size_t bimask_workspace_bytes(int T, int I, int J, int P);
 
 /* Eq. 4 + packing.  Forward mask: in every row, every aligned block of M along J keeps its N
@@ -196,7 +196,8 @@ int bimask_wgrad(const uint16_t* dY, const uint16_t* X, int T, int I, int J, flo
  * is never written.  33 bytes for 64 of bf16; the error of a value is at most p / 2 <= max |x| / 127. */
 enum { BIMASK_ACT_NONE = 0, BIMASK_ACT_RELU = 1, BIMASK_ACT_GELU = 2, BIMASK_ACT_GELU_TANH = 3, BIMASK_ACT_SILU = 4 };
 
-/* Bytes of scratch for bimask_act_bwd on T x I activations and for bimask_wgrad_ckpt on a T, I, J layer. */
+/* Bytes of scratch for bimask_act_bwd on T x I activations and for bimask_wgrad_ckpt on a T, I, J layer.  Never smaller for
+ * more tokens: one buffer for the largest T serves every smaller batch. */
 size_t bimask_linear_workspace_bytes(int T, int I, int J);
 
 /* Y[t, i] = act(sum_j X[t, j] (B * W)[i, j] + bias[i]) + R[t, i], all of it in fp32 before the one rounding to bf16.

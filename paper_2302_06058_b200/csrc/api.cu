@@ -73,7 +73,10 @@ size_t bimask_hw_meta_bytes(int rows, int K) {
 
 size_t bimask_workspace_bytes(int T, int I, int J, int P) {
   if (I <= 0 || J <= 0) return 0;
-  return plan_ws(T, I, J, P).total;
+  const WsPlan w = plan_ws(T, I, J, P);
+  const int splits = T > 0 ? wgrad_most_splits(T, I, J) : 1;      // as many partial sums as any smaller batch takes
+  const size_t total = w.part_off + (splits > 1 ? align_up((size_t)splits * I * J * sizeof(float), 256) : 0);
+  return total > w.total ? total : w.total;
 }
 
 int bimask_fwd_mask(const float* W, int I, int J, int N, int M, uint32_t* maskbits_f, uint16_t* vals_f,
@@ -332,7 +335,7 @@ static int check_rows(const char* who, int T, int C) {
 
 size_t bimask_linear_workspace_bytes(int T, int I, int J) {
   if (T <= 0 || I <= 0 || J <= 0 || I % 32 != 0 || J % 32 != 0) return 0;
-  const size_t a = act_bwd_partial_bytes(T, I), w = wgrad_ckpt_bytes(T, I, J);
+  const size_t a = act_bwd_partial_bytes(T, I), w = wgrad_ckpt_query_bytes(T, I, J);
   return align_up(a > w ? a : w, 256);
 }
 

@@ -266,8 +266,11 @@ int launch_ckpt_unpack(const int8_t* q, const uint8_t* s, int act, int T, int C,
 size_t act_bwd_partial_bytes(int T, int C);
 int launch_act_bwd(const uint16_t* dY, const int8_t* zq, const uint8_t* zs, int act, int T, int C, uint16_t* dZ, float* dbias,
                    float* partial, cudaStream_t st);
-// Weight gradient whose token operand is a checkpoint; ws: wgrad_ckpt_bytes(T, I, J).
+// Weight gradient whose token operand is a checkpoint; ws: wgrad_ckpt_bytes(T, I, J).  wgrad_ckpt_query_bytes: enough for T and
+// every smaller number of tokens; wgrad_most_splits: the same for the partial sums of launch_wgrad_impl.
 size_t wgrad_ckpt_bytes(int T, int I, int J);
+size_t wgrad_ckpt_query_bytes(int T, int I, int J);
+int wgrad_most_splits(int T, int I, int J);
 int launch_wgrad_ckpt(const uint16_t* dY, const int8_t* q, const uint8_t* s, int T, int I, int J, float* dW, void* ws,
                       int32_t* status_word, cudaStream_t st);
 void wgrad_plan(int T, int I, int J, int* n_tile, int* splits, int* k_tiles_per_split);

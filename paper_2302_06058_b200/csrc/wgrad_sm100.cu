@@ -753,17 +753,24 @@ static int launch_splitk_reduce(const float* partials, int splits, long long n4,
 // Split-K plan of the dense product for a reduction of k_tiles 64-deep tiles.
 static bool wgrad_uses_single(int I) { return I <= 128; }       // one 128-row tile: no CTA pairs
 
-static void wgrad_plan_k(int k_tiles, int I, int J, int* splits, int* k_tiles_per_split) {
+// The splits wanted: one round of work items over the workers, at least 8 k tiles each.  Never fewer for more k tiles, so
+// a workspace query that counts with them covers every smaller batch (the plan's own count, rounded to equal shares, may
+// fall from one batch to a larger one).
+static int splits_wanted(int k_tiles, int tiles, int workers) {
+  int sp = tiles < workers ? workers / tiles : 1;
+  const int max_by_k = k_tiles / 8 > 0 ? k_tiles / 8 : 1;
+  if (sp > max_by_k) sp = max_by_k;
+  return sp < 64 ? sp : 64;
+}
+
+static int wgrad_splits_wanted(int k_tiles, int I, int J) {
   const bool single = wgrad_uses_single(I);
   const int tiles = single ? (J + 255) / 256 : (((I + 127) / 128 + 1) / 2) * ((J + 255) / 256);   // 128 / 256 x 256 tiles
-  const int workers = single ? 148 : 74;                          // CTAs or CTA pairs
-  int sp = 1;
-  if (tiles < workers) {
-    sp = workers / tiles;                                         // one round of work items over the workers
-    const int max_by_k = k_tiles / 8 > 0 ? k_tiles / 8 : 1;        // at least 8 k tiles per split
-    if (sp > max_by_k) sp = max_by_k;
-    if (sp > 64) sp = 64;
-  }
+  return splits_wanted(k_tiles, tiles, single ? 148 : 74);        // CTAs or CTA pairs
+}
+
+static void wgrad_plan_k(int k_tiles, int I, int J, int* splits, int* k_tiles_per_split) {
+  int sp = wgrad_splits_wanted(k_tiles, I, J);
   int per = (k_tiles + sp - 1) / sp;
   sp = (k_tiles + per - 1) / per;
   *splits = sp; *k_tiles_per_split = per;
@@ -861,6 +868,8 @@ void wgrad_plan(int T, int I, int J, int* n_tile, int* splits, int* k_tiles_per_
   wgrad_plan_k((T + 63) / 64, I, J, splits, k_tiles_per_split);
 }
 
+int wgrad_most_splits(int T, int I, int J) { return wgrad_splits_wanted((T + 63) / 64, I, J); }
+
 int launch_wgrad_impl(const uint16_t* dY, const uint16_t* X, int T, int I, int J, float* dW, float* partials,
                       int32_t* status_word, cudaStream_t s, cudaStream_t reduce_stream, cudaEvent_t product_done) {
   int nt, splits, per;
@@ -897,22 +906,27 @@ int launch_wgrad_impl(const uint16_t* dY, const uint16_t* X, int T, int I, int J
 // ---- weight gradient from a checkpoint ------------------------------------------------------------
 static size_t round256(size_t v) { return (v + 255) / 256 * 256; }
 
+static int wgrad_ckpt_splits_wanted(int T, int I, int J) {
+  return splits_wanted((T + 63) / 64, (((I + 127) / 128 + 1) / 2) * ((J + 255) / 256), 74);       // over the CTA pairs
+}
+
 static void wgrad_ckpt_plan(int T, int I, int J, int* splits, int* per) {
-  const int k_tiles = (T + 63) / 64;
-  const int tiles = (((I + 127) / 128 + 1) / 2) * ((J + 255) / 256), workers = 74;
-  int sp = tiles < workers ? workers / tiles : 1;                 // one round of work items over the CTA pairs
-  const int max_by_k = k_tiles / 8 > 0 ? k_tiles / 8 : 1;         // at least 8 k tiles per split
-  if (sp > max_by_k) sp = max_by_k;
-  if (sp > 64) sp = 64;
+  const int k_tiles = (T + 63) / 64, sp = wgrad_ckpt_splits_wanted(T, I, J);
   *per = (k_tiles + sp - 1) / sp;
   *splits = (k_tiles + *per - 1) / *per;
+}
+
+static size_t wgrad_ckpt_bytes_for(int T, int I, int J, int splits) {
+  return round256((size_t)T * J * 2) + (splits > 1 ? (size_t)splits * I * J * sizeof(float) : 0);
 }
 
 size_t wgrad_ckpt_bytes(int T, int I, int J) {
   int splits, per;
   wgrad_ckpt_plan(T, I, J, &splits, &per);
-  return round256((size_t)T * J * 2) + (splits > 1 ? (size_t)splits * I * J * sizeof(float) : 0);
+  return wgrad_ckpt_bytes_for(T, I, J, splits);
 }
+
+size_t wgrad_ckpt_query_bytes(int T, int I, int J) { return wgrad_ckpt_bytes_for(T, I, J, wgrad_ckpt_splits_wanted(T, I, J)); }
 
 // Decoding the bytes inside the product was slower at every size tried (2048 x 2048 at 8192 tokens: 95 against 58 us with the
 // unpacking pass): per 64-token k tile and SM it moves 80 KB through shared memory where 512 tensor clocks allow 64.
