@@ -67,6 +67,8 @@ class SparseLinear:
 
 
 class SparseMLP:
+    """The block; a batch has at most T tokens."""
+
     def __init__(self, T, width, hidden, seed=0):
         g = torch.Generator(device="cuda").manual_seed(seed)
         self.T, self.width, self.hidden = T, width, hidden
@@ -81,25 +83,29 @@ class SparseMLP:
         return sum(t.numel() for t in (self.Xq, self.Xs, self.Zq, self.Zs))
 
     def forward(self, X):
-        bm.bimask_ckpt_pack(X, X.shape[0], self.width, self.Xq, self.Xs)
-        self.fc1.forward(X, bm.ACT_GELU, None, self.H, self.Zq, self.Zs)
-        self.fc2.forward(self.H, bm.ACT_NONE, X, self.Y)
-        return self.Y
+        T = X.shape[0]                                    # this batch's tokens: the first T rows of every buffer
+        if T > self.T:
+            raise ValueError(f"{T} tokens in a block for at most {self.T}")
+        bm.bimask_ckpt_pack(X, T, self.width, self.Xq, self.Xs)
+        self.fc1.forward(X, bm.ACT_GELU, None, self.H[:T], self.Zq, self.Zs)
+        self.fc2.forward(self.H[:T], bm.ACT_NONE, X, self.Y[:T])
+        return self.Y[:T]
 
     def backward(self, dY):
         T, a, b = dY.shape[0], self.fc1, self.fc2
+        H, dH, dX = self.H[:T], self.dH[:T], self.dX[:T]
         for layer in (a, b):
             layer.backward_operand()
         # second layer: bias, input and weight gradient, its input recomputed from the pre-activation's checkpoint
         bm.bimask_act_bwd(dY, None, None, bm.ACT_NONE, T, b.I, None, b.db, b.ws, b.ws.numel())
-        b.input_gradient(dY, self.dH)
-        bm.bimask_ckpt_unpack(self.Zq, self.Zs, bm.ACT_GELU, T, self.hidden, self.H)
-        bm.bimask_wgrad(dY, self.H, T, b.I, b.J, b.b["dW"], b.b["ws"], b.b["ws"].numel(), b.b["status_word"])
+        b.input_gradient(dY, dH)
+        bm.bimask_ckpt_unpack(self.Zq, self.Zs, bm.ACT_GELU, T, self.hidden, H)
+        bm.bimask_wgrad(dY, H, T, b.I, b.J, b.b["dW"], b.b["ws"], b.b["ws"].numel(), b.b["status_word"])
         # through the activation (in place), then the first layer
-        bm.bimask_act_bwd(self.dH, self.Zq, self.Zs, bm.ACT_GELU, T, a.I, self.dH, a.db, a.ws, a.ws.numel())
-        a.input_gradient(self.dH, self.dX)
-        bm.bimask_wgrad_ckpt(self.dH, self.Xq, self.Xs, T, a.I, a.J, a.b["dW"], a.ws, a.ws.numel(), a.b["status_word"])
-        return self.dX.add_(dY)                           # the residual's gradient is dY itself
+        bm.bimask_act_bwd(dH, self.Zq, self.Zs, bm.ACT_GELU, T, a.I, dH, a.db, a.ws, a.ws.numel())
+        a.input_gradient(dH, dX)
+        bm.bimask_wgrad_ckpt(dH, self.Xq, self.Xs, T, a.I, a.J, a.b["dW"], a.ws, a.ws.numel(), a.b["status_word"])
+        return dX.add_(dY)                                # the residual's gradient is dY itself
 
     def search(self, seed):
         self.fc1.search(seed)
