@@ -63,7 +63,7 @@ def act_bwd(dY, z, kind):
     return dz, dz.sum(axis=0)
 
 
-BF16_MAX = (2.0 - 2.0 ** -7) * 2.0 ** 127
+LARGEST = 127.0 * 2.0 ** 121          # the next scale, 2^122, would round a larger magnitude to 64 steps: 2^128, infinity in bf16
 
 
 def pack(x):
@@ -76,7 +76,7 @@ def pack(x):
         for g in range(b.shape[1]):
             v = b[t, g]
             m = np.max(np.abs(v))
-            if not m <= BF16_MAX:                               # NaN and infinity included
+            if not m <= LARGEST:                                # NaN and infinity included
                 s[t, g] = 255
                 continue
             e = -126

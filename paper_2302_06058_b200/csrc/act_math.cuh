@@ -196,10 +196,12 @@ namespace ckpt {
 __device__ __forceinline__ uint32_t up16(float abs_x) { return (__float_as_uint(abs_x) + 0xFFFFu) >> 16; }
 
 // Scale byte of a block from that maximum h: 2^(s-127) is the smallest power of two, not below 2^-126, with
-// max |x| <= 127 * 2^(s-127); 255: the block holds a value that is not finite in bf16.
+// max |x| <= 127 * 2^(s-127); 255: the block holds a NaN or a magnitude above 127 * 2^121 (bf16 0x7F7E), whose byte would be
+// 64 steps of 2^122 and stand for 2^128, infinity.
+constexpr uint32_t LARGEST = 0x7F7Eu;
 __device__ __forceinline__ uint32_t scale_of(uint32_t h) {
   const int s = (int)((h + 1u) >> 7) - 6;                 // exponent of h, one more when its mantissa is above 1.984375 = 127 / 64
-  return h >= 0x7F80u ? 255u : (uint32_t)(s < 1 ? 1 : s);
+  return h > LARGEST ? 255u : (uint32_t)(s < 1 ? 1 : s);
 }
 // 2^(127 - s): x times it is exact, and rounds to the byte
 __device__ __forceinline__ float inverse_scale(uint32_t s) { return __uint_as_float((254u - s) << 23); }

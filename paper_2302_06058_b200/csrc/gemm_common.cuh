@@ -455,9 +455,9 @@ __device__ __forceinline__ void emit_checkpoint(const act::Pair (&z)[16], uint32
   uint32_t k = mid ? k1 : k0;
   k = __vmaxu2(k, __shfl_xor_sync(0xFFFFFFFFu, mid ? k0 : k1, 8));
   k = __vmaxu2(k, __shfl_xor_sync(0xFFFFFFFFu, k, 4));     // tokens 8 g + 2 b + {0, 1}, g = lane / 8
-  // ckpt::scale_of on both halves: `raw` is the scale of a finite block, the or'ed part is 255 where a block is not
+  // ckpt::scale_of on both halves: `raw` is the scale of a block in range, the or'ed part is 255 where a block is not
   const uint32_t raw = __vmaxu2(((k + 0x00010001u) >> 7) & 0x01FF01FFu, 0x00070007u) - 0x00060006u;
-  const uint32_t over = (k + 0x00800080u) & 0x80008000u;
+  const uint32_t over = (k + 0x00010001u * (0x7FFFu - ckpt::LARGEST)) & 0x80008000u;
   const uint32_t s2 = raw | ((over >> 7) - (over >> 15));
   const int st = 8 * (lane >> 3) + 2 * (lane & 3) + ((lane >> 2) & 1);
   ptx::st_shared_u8(scales + 4u * (uint32_t)st, (lane & 4) ? s2 >> 16 : s2);
