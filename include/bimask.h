@@ -187,7 +187,9 @@ int bimask_wgrad(const uint16_t* dY, const uint16_t* X, int T, int I, int J, flo
  *
  * Activations:
  *   NONE z;  RELU max(z, 0);  GELU z Phi(z);  GELU_TANH z (1 + tanh(c (z + 0.044715 z^3))) / 2, c = sqrt(2 / pi);
- *   SILU z / (1 + e^-z).  Evaluated in fp32 to about 1e-6; the slope of RELU at 0 is 0.
+ *   SILU z / (1 + e^-z).  Evaluated in fp32 to about 1e-6 (1 + |z|), slopes to 1e-6: absolute errors, so few digits are
+ *   right in the far left tails, where the values are below 1e-4.  The slope of RELU at 0 is 0.  At minus infinity all but
+ *   NONE are 0, their limit; NaN stays NaN.
  *
  * Checkpoint of a T x C matrix (C % 32 == 0): q, T x C signed bytes, and s, T x C/32 bytes.  For 32 consecutive channels
  * of a token, p = 2^(s - 127) is the smallest power of two not below 2^-126 with max |x| <= 127 p, and q = x / p rounded

@@ -112,7 +112,10 @@ __device__ __forceinline__ Pair gelu2(Pair z) {
   for (int i = T::N - 2; i >= 0; --i) p = fma2(p, a, both(T::c(i)));
   return fma2(map2(a, [](float v) { return -v; }), map2(p, [](float v) { return ex2(v); }), relu2(z));
 }
-__device__ __forceinline__ Pair silu2(Pair z) { return mul2(z, sigmoid2(mul2(z, both(-LOG2E)))); }
+// z is cut off at the least finite number: minus infinity times 0 would be NaN where the GELUs, and the limit, are 0
+__device__ __forceinline__ Pair silu2(Pair z) {
+  return mul2(map2(z, [](float v) { return max_nan(v, -3.402823466e38f); }), sigmoid2(mul2(z, both(-LOG2E))));
+}
 
 template <int KIND>
 __device__ __forceinline__ Pair value2(Pair z) {
