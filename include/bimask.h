@@ -413,6 +413,11 @@ size_t bimask_perm_search_static_max_entries(void);
  * normally (no trap: the context stays usable). */
 int bimask_debug_wait_probe(int32_t* status_word, void* stream);
 
+/* Debug helper, host only: how bimask_linear_fwd runs a layer of this size (dense: hw_meta_f == NULL).  HOST array out[4] =
+ * {kernel: 0 few tokens, 1 one row tile, 2 CTA pairs, 3 CTA pairs with two row tiles each; CTAs that share a tile's
+ * reduction; tiles of 128 rows x 128 tokens; clusters of that many CTAs that the device holds at once}. */
+int bimask_debug_linear_plan(int T, int I, int J, int dense, int32_t* out);
+
 /* Debug helper, host only: what a tensor-core kernel that gave up (BIMASK_ETIMEOUT) waits for before it ends, when its
  * producers had issued issued0 and issued1 loads (the two CTAs of a pair; equal for a single CTA) into rings of `stages`
  * stages.  Writes up to 2 * stages rows {stage, phase parity, settle} to the HOST array `out`, in order, and returns

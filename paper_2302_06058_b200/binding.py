@@ -23,6 +23,7 @@ EXPORTS = ("bimask_last_error", "bimask_launch_count", "bimask_hw_meta_bytes", "
            "bimask_perm_search_static_max_entries", "bimask_sgd_fwd_mask", "bimask_train_step",
            "bimask_bwd_mask_criterion", "bimask_conv_workspace_bytes", "bimask_conv_layer_step",
            "bimask_refine_workspace_bytes", "bimask_perm_refine", "bimask_debug_gen_candidates", "bimask_debug_status", "bimask_debug_drain_plan",
+           "bimask_debug_linear_plan",
            "bimask_linear_workspace_bytes", "bimask_linear_fwd", "bimask_act_bwd", "bimask_ckpt_pack", "bimask_ckpt_unpack",
            "bimask_wgrad_ckpt")
 
@@ -114,6 +115,7 @@ def lib() -> ctypes.CDLL:
         L.bimask_check_perms.argtypes = [c_void_p, c_int, c_int, c_void_p, c_void_p, c_size_t, c_void_p]
         L.bimask_debug_wait_probe.argtypes = [c_void_p, c_void_p]
         L.bimask_debug_status.argtypes = [c_void_p]
+        L.bimask_debug_linear_plan.argtypes = [c_int, c_int, c_int, c_int, c_void_p]
         L.bimask_debug_drain_plan.argtypes = [c_int, c_int, c_int, c_void_p]
         L.bimask_debug_gen_candidates.argtypes = [c_uint64, c_int, c_int, c_int, c_void_p, c_void_p]
         L.bimask_perm_search_static.argtypes = [c_void_p, c_int, c_int, c_int, c_int, c_int, c_uint64,
@@ -329,6 +331,13 @@ def bimask_host_sync():
 
 def bimask_debug_wait_probe(status_word, stream=None):
     return _check(lib().bimask_debug_wait_probe(_ptr(status_word), _stream(stream)))
+
+
+def bimask_debug_linear_plan(T, I, J, dense=False):
+    """(kernel, CTAs per tile, tiles, clusters that fit) of a bimask_linear_fwd call."""
+    out = (c_int32 * 4)()
+    _check(lib().bimask_debug_linear_plan(T, I, J, int(dense), ctypes.cast(out, c_void_p)))
+    return tuple(out)
 
 
 def bimask_debug_drain_plan(issued0, issued1, stages):

@@ -867,6 +867,18 @@ int bimask_debug_wait_probe(int32_t* status_word, void* stream) {
   return launch_wait_probe(status_word, (cudaStream_t)stream);
 }
 
+int bimask_debug_linear_plan(int T, int I, int J, int dense, int32_t* out) {
+  const int rc = check_gemm(T, I, J);
+  if (rc != BIMASK_OK) return rc;
+  BIMASK_REQUIRE(out != nullptr, BIMASK_EINVAL, "bimask_debug_linear_plan: null pointer");
+  const int tiles = ((I + 127) / 128) * ((T + 127) / 128);
+  out[0] = linear_kernel_choice(dense == 0, I, T, J);
+  out[1] = out[0] == LINEAR_FEW_TOKENS ? linear_small_splits(tiles, (J + 127) / 128) : 1;
+  out[2] = tiles;
+  out[3] = linear_small_fit(out[1]);
+  return BIMASK_OK;
+}
+
 int bimask_debug_drain_plan(int issued0, int issued1, int stages, int32_t* out) {
   const int gap = issued0 < issued1 ? issued1 - issued0 : issued0 - issued1;
   BIMASK_REQUIRE(out != nullptr && issued0 >= 0 && issued1 >= 0 && stages > 0 && gap <= stages, BIMASK_EINVAL,

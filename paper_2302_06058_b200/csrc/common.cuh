@@ -252,13 +252,17 @@ struct LinearEpilogue {
   int8_t* zq;
   uint8_t* zs;
 };
-// The same for few tokens (linear_small_sm100.cu), and the number of CTAs that share a 128 x 128 tile's reduction of
-// k_tiles 128-wide tiles there.
+// The same for few tokens (linear_small_sm100.cu); the number of CTAs that share a 128 x 128 tile's reduction of k_tiles
+// 128-wide tiles there, and how many clusters of that many the device holds at once.
 int linear_small_splits(int tiles, int k_tiles);
+int linear_small_fit(int size);
 int launch_linear_small(const uint16_t* vals, const void* hw_meta, const uint16_t* X, int Mdim, int Ndim, int Kdim,
                         const LinearEpilogue& le, uint16_t* out, int32_t* status_word, cudaStream_t s);
 int launch_linear_fwd(const uint16_t* vals, const void* hw_meta, const uint16_t* X, int Mdim, int Ndim, int Kdim,
                       const LinearEpilogue& le, uint16_t* out, int32_t* status_word, cudaStream_t s);
+// The kernel that launch_linear_fwd takes.
+enum { LINEAR_FEW_TOKENS = 0, LINEAR_ONE_ROW_TILE = 1, LINEAR_PAIR = 2, LINEAR_PAIR_TWO_ROW_TILES = 3 };
+int linear_kernel_choice(bool sparse, int Mdim, int Ndim, int Kdim);
 // 8-bit checkpoints and the gradient of the epilogue (linear_kernels.cu).  partial: act_bwd_partial_bytes(T, C), used
 // when dbias is wanted.
 int launch_ckpt_pack(const uint16_t* x, int T, int C, int8_t* q, uint8_t* s, cudaStream_t st);

@@ -317,12 +317,45 @@ int run_small_any(const uint16_t* vals, const void* hw_meta, const uint16_t* X, 
 
 }  // namespace
 
-// As many CTAs as there are SMs, at most eight per cluster (the portable size) and at least four k tiles each.
+// Clusters of `size` CTAs of this file's kernels that the device holds at once (one CTA per SM, and a cluster must lie within
+// a GPC: 74, 45, 33, 26, 22, 15, 15 of two to eight on a device where 148 SMs are spread unevenly).
+int linear_small_fit(int size) {
+  constexpr int DEVICES = 64;
+  static std::atomic<int> known[DEVICES][9];
+  int dev = 0;
+  if (size <= 1 || size > 8 || cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= DEVICES) return sm_count() / (size < 1 ? 1 : size);
+  int n = known[dev][size].load(std::memory_order_relaxed);
+  if (n > 0) return n;
+  using C = SmallCfg<32, 8, true>;
+  auto kern = linear_small_kernel<32, 8, true>;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)size);
+  cfg.blockDim = dim3(SMALL_THREADS);
+  cfg.dynamicSmemBytes = C::SMEM_BYTES;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = (unsigned)size;
+  attr[0].val.clusterDim.y = 1;
+  attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  if (set_smem_attr(kern, C::SMEM_BYTES) != BIMASK_OK || cudaOccupancyMaxActiveClusters(&n, kern, &cfg) != cudaSuccess || n < 1) {
+    cudaGetLastError();                                   // the query alone failed: the launch will say what is wrong
+    return sm_count() / size;
+  }
+  known[dev][size].store(n, std::memory_order_relaxed);
+  return n;
+}
+
+// The largest cluster, at most eight (the portable size) and at least four k tiles per CTA, of which all tiles' fit at once: a
+// second round costs what the split saves and more.  24 tokens, reduction 4096, in one round / one size larger, in two:
+// 20 row tiles 6 / 7 CTAs 7.1 / 12.2 us, 24: 5 / 6 7.4 / 12.6, 28: 4 / 5 7.4 / 12.9, 36: 3 / 4 8.2 / 13.0, 48: 2 / 3
+// 9.3 / 14.7; reduction 16384: 20 row tiles 12.7 / 19.2, 36: 18.5 / 26.2.  Four CTAs where six fit would save another
+// 4 % at 4096 and lose 2 % at 16384.
 int linear_small_splits(int tiles, int k_tiles) {
-  int splits = sm_count() / tiles;
-  if (splits > k_tiles / 4) splits = k_tiles / 4;
-  if (splits > 8) splits = 8;
-  if (splits < 1) splits = 1;
+  int splits = 1;
+  for (int c = 8; c > 1 && splits == 1; --c)
+    if (4 * c <= k_tiles && tiles <= linear_small_fit(c)) splits = c;
   const int per = (k_tiles + splits - 1) / splits;
   return (k_tiles + per - 1) / per;
 }

@@ -1129,7 +1129,8 @@ static bool split_is_faster(bool sparse, int Mdim, int Ndim, int Kdim) {
   const int sms = sm_count(), kt = (Kdim + 127) / 128;
   const int tiles = ((Mdim + 127) / 128) * ((Ndim + 127) / 128);
   const int splits = linear_small_splits(tiles, kt);
-  const double small = (double)((tiles * splits + sms - 1) / sms) * ((kt + splits - 1) / splits * (sparse ? 800.0 : 1024.0) + 9000.0);
+  const int fit = linear_small_fit(splits);
+  const double small = (double)((tiles + fit - 1) / fit) * ((kt + splits - 1) / splits * (sparse ? 800.0 : 1024.0) + 9000.0);
   double pair = 1e30;
   for (int n = 256; n >= 96; n -= 32) {
     const int t = (Mdim + 255) / 256 * ((Ndim + n - 1) / n);
@@ -1146,18 +1147,25 @@ static bool split_is_faster(bool sparse, int Mdim, int Ndim, int Kdim) {
 // error of a sum, mixed signs: 1.0e-7 at 384, 2.6e-7 at 2048, 1.3e-6 at 4096, 6.2e-6 at 16384; rounded fp32 sums about
 // 1e-7).  A choice for speed: ending the chains early takes a second accumulator, for which the 512-row tiles of the wide
 // layers leave no tensor memory, and 256-row tiles are bound by the L2 feed (16384 x 4096 at 8192 tokens 655 against 575 us).
+int linear_kernel_choice(bool sparse, int Mdim, int Ndim, int Kdim) {
+  if (Ndim <= 128 || (Mdim > 128 && split_is_faster(sparse, Mdim, Ndim, Kdim))) return LINEAR_FEW_TOKENS;
+  if (Mdim <= 128) return LINEAR_ONE_ROW_TILE;
+  return sparse && Ndim >= 1024 && Mdim >= 2048 && Kdim >= 4096 ? LINEAR_PAIR_TWO_ROW_TILES : LINEAR_PAIR;
+}
+
 int launch_linear_fwd(const uint16_t* vals, const void* hw_meta, const uint16_t* X, int Mdim, int Ndim, int Kdim,
                       const LinearEpilogue& le, uint16_t* out, int32_t* status_word, cudaStream_t s) {
-  if (Ndim <= 128 || (Mdim > 128 && split_is_faster(hw_meta != nullptr, Mdim, Ndim, Kdim)))
-    return launch_linear_small(vals, hw_meta, X, Mdim, Ndim, Kdim, le, out, status_word, s);
-  if (hw_meta != nullptr) {
-    if (Ndim >= 1024 && Mdim >= 2048 && Kdim >= 4096)
-      return run_sparse_pair2m<true>(vals, hw_meta, X, Mdim, Ndim, Kdim, out, status_word, s, &le);
-    if (Mdim > 128) return run_sparse_pair_persistent<true>(vals, hw_meta, X, Mdim, Ndim, Kdim, out, status_word, s, &le);
-    return run_single<256, 2, true, true>(vals, hw_meta, X, Mdim, Ndim, Kdim, out, status_word, s, &le);
+  const bool sparse = hw_meta != nullptr;
+  switch (linear_kernel_choice(sparse, Mdim, Ndim, Kdim)) {
+    case LINEAR_FEW_TOKENS: return launch_linear_small(vals, hw_meta, X, Mdim, Ndim, Kdim, le, out, status_word, s);
+    case LINEAR_ONE_ROW_TILE:
+      return sparse ? run_single<256, 2, true, true>(vals, hw_meta, X, Mdim, Ndim, Kdim, out, status_word, s, &le)
+                    : run_single<256, 2, false, true>(vals, nullptr, X, Mdim, Ndim, Kdim, out, status_word, s, &le);
+    case LINEAR_PAIR_TWO_ROW_TILES: return run_sparse_pair2m<true>(vals, hw_meta, X, Mdim, Ndim, Kdim, out, status_word, s, &le);
+    default:
+      return sparse ? run_sparse_pair_persistent<true>(vals, hw_meta, X, Mdim, Ndim, Kdim, out, status_word, s, &le)
+                    : run_dense_pair_persistent<true>(vals, X, Mdim, Ndim, Kdim, out, status_word, s, &le);
   }
-  if (Mdim > 128) return run_dense_pair_persistent<true>(vals, X, Mdim, Ndim, Kdim, out, status_word, s, &le);
-  return run_single<256, 2, false, true>(vals, nullptr, X, Mdim, Ndim, Kdim, out, status_word, s, &le);
 }
 
 }  // namespace bimask
