@@ -1121,24 +1121,31 @@ int launch_dense_nt(const uint16_t* A, const uint16_t* Bop, int Mdim, int Ndim, 
 }
 
 // Whether the kernel for few tokens (128 x 128 tiles, split along the reduction over a cluster) is the faster one: it is
-// where the CTA pairs' large tiles leave most SMs idle through a long reduction.  Both sides in SM clocks: a k tile costs
-// what its operands take at 64 bytes per clock (measured about 1.25 times that on the pairs), start-up and finish 6 and 9
-// thousand.  Measured, pairs / split: 4096 x 16384 at 160, 256, 512 tokens 55 / 32, 55 / 33, 58 / 55 us; 1024 x 4096 (dense
-// operand) at 160, 512, 1000 tokens 17 / 11, 20 / 10, 19 / 14; but 16384 x 4096 at 256 27 / 46, 1536 x 384 at 160 5 / 11.
+// where large tiles leave most SMs idle through a long reduction.  Both sides in SM clocks: a k tile costs what its
+// operands take at 64 bytes per clock (measured about 1.25 times that on the pairs; 1500, dense operand 1750, on one row
+// tile, whose ring of two stages waits for its loads), start-up and finish 6 and 9 thousand.  Measured, pairs / split:
+// 4096 x 16384 at 160, 256, 512 tokens 55 / 30, 55 / 31, 58 / 58 us; 1024 x 4096 (dense operand) at 160, 512, 1000 tokens
+// 17 / 10, 20 / 11, 19 / 15; but 16384 x 4096 at 256 27 / 46, 1536 x 384 at 160 5 / 11.  One row tile / split, at most 128
+// rows: reduction 384 at 129, 8192, 50432 tokens 5.8 / 7.0, 8.1 / 8.5, 18.8 / 27.8; 1152 9.2 / 6.9, 12.9 / 9.9, 33.2 / 39.6;
+// 4096 21.8 / 7.5, 31.8 / 17.7, 86 / 85; 16384 100 / 12.4, 108 / 50, 293 / 260 (dense operand the same within 10 %).
 static bool split_is_faster(bool sparse, int Mdim, int Ndim, int Kdim) {
   const int sms = sm_count(), kt = (Kdim + 127) / 128;
   const int tiles = ((Mdim + 127) / 128) * ((Ndim + 127) / 128);
   const int splits = linear_small_splits(tiles, kt);
   const int fit = linear_small_fit(splits);
   const double small = (double)((tiles + fit - 1) / fit) * ((kt + splits - 1) / splits * (sparse ? 800.0 : 1024.0) + 9000.0);
-  double pair = 1e30;
-  for (int n = 256; n >= 96; n -= 32) {
-    const int t = (Mdim + 255) / 256 * ((Ndim + n - 1) / n);
-    const double feed = ((sparse ? 18432.0 : 32768.0) + 128.0 * n) / 64.0, mma = (sparse ? 2.0 : 4.0) * n;
-    const double cost = 6000.0 + (double)((t + sms / 2 - 1) / (sms / 2)) * kt * 1.25 * (feed > mma ? feed : mma);
-    if (cost < pair) pair = cost;
+  double large = 1e30;
+  if (Mdim <= 128) {
+    large = 6000.0 + (double)(((Ndim + 255) / 256 + sms - 1) / sms) * kt * (sparse ? 1500.0 : 1750.0);
+  } else {
+    for (int n = 256; n >= 96; n -= 32) {
+      const int t = (Mdim + 255) / 256 * ((Ndim + n - 1) / n);
+      const double feed = ((sparse ? 18432.0 : 32768.0) + 128.0 * n) / 64.0, mma = (sparse ? 2.0 : 4.0) * n;
+      const double cost = 6000.0 + (double)((t + sms / 2 - 1) / (sms / 2)) * kt * 1.25 * (feed > mma ? feed : mma);
+      if (cost < large) large = cost;
+    }
   }
-  return small < 0.9 * pair;
+  return small < 0.9 * large;
 }
 
 // Linear layer: the product of launch_spmm (hw_meta given) or launch_dense_nt (null) with the epilogue of `le`, on the
@@ -1148,7 +1155,7 @@ static bool split_is_faster(bool sparse, int Mdim, int Ndim, int Kdim) {
 // 1e-7).  A choice for speed: ending the chains early takes a second accumulator, for which the 512-row tiles of the wide
 // layers leave no tensor memory, and 256-row tiles are bound by the L2 feed (16384 x 4096 at 8192 tokens 655 against 575 us).
 int linear_kernel_choice(bool sparse, int Mdim, int Ndim, int Kdim) {
-  if (Ndim <= 128 || (Mdim > 128 && split_is_faster(sparse, Mdim, Ndim, Kdim))) return LINEAR_FEW_TOKENS;
+  if (Ndim <= 128 || split_is_faster(sparse, Mdim, Ndim, Kdim)) return LINEAR_FEW_TOKENS;
   if (Mdim <= 128) return LINEAR_ONE_ROW_TILE;
   return sparse && Ndim >= 1024 && Mdim >= 2048 && Kdim >= 4096 ? LINEAR_PAIR_TWO_ROW_TILES : LINEAR_PAIR;
 }
