@@ -196,7 +196,9 @@ int bimask_wgrad(const uint16_t* dY, const uint16_t* X, int T, int I, int J, flo
  * to the nearest integer (ties to even), so |q| <= 127; the value it stands for, q p, is exact in bf16.  A block with a NaN
  * or a magnitude above 127 * 2^121 = 3.376e38 (at the next p its byte would stand for 2^128, not finite in bf16) gets
  * s = 255 and stands for NaN throughout (its q is unspecified); s = 0 is never written.  33 bytes for 64 of bf16; the error of
- * a value is at most p / 2, which is at most max |x| / 127 (unless p = 2^-126, the least). */
+ * a value is at most p / 2, which is at most max |x| / 127 (unless p = 2^-126, the least).  A pre-activation within p / 2 of
+ * zero becomes zero, where RELU's slope is 0: about one active channel in a hundred (normal pre-activations) gets no
+ * gradient through a checkpoint. */
 enum { BIMASK_ACT_NONE = 0, BIMASK_ACT_RELU = 1, BIMASK_ACT_GELU = 2, BIMASK_ACT_GELU_TANH = 3, BIMASK_ACT_SILU = 4 };
 
 /* Bytes of scratch for bimask_act_bwd on T x I activations and for bimask_wgrad_ckpt on a T, I, J layer.  Never smaller for
