@@ -307,8 +307,10 @@ template <bool SPARSE>
 int run_small_any(const uint16_t* vals, const void* hw_meta, const uint16_t* X, int Mdim, int Ndim, int Kdim, const LinearEpilogue& le,
                   uint16_t* out, int32_t* status_word, cudaStream_t s) {
   // stages: what fits 220 KB (22 / 26 / 34 / 50 KB each, dense 36 / 40 / 48 / 64 KB)
-  // Very few tokens: narrower token tiles leave room for more stages of weights (one token, 4096 -> 16384: 16.0 -> 15.0 us;
-  // 16384 -> 4096: 16.0 -> 16.3; 16 tokens, 4096 -> 16384: 14.9 -> 15.3, so not there).
+  // Very few tokens: narrower token tiles leave room for more stages of weights.  16- / 32-token tiles, us: 16384 x 4096 at
+  // 1, 8, 16 tokens 15.8 / 16.6, 15.8 / 16.0, 15.8 / 15.5; 9600 x 16384 33.8 / 37.1, 33.6 / 34.5, 33.1 / 34.1; 4096 x 4096
+  // 7.2 / 7.3, 7.5 / 7.7, 7.6 / 7.7; but 4096 x 16384 16.6 / 16.4, 16.8 / 16.2, 17.0 / 16.5.  Dense operand: 16384 x 4096
+  // 24.9 / 25.3, 25.6 / 25.8, 25.4 / 25.4; 4096 x 16384 26.8 / 26.5, 27.2 / 26.7, 26.8 / 26.1.  Smaller layers within 1 %.
   if (Ndim <= 8) return run_small<16, SPARSE ? 10 : 6, SPARSE>(vals, hw_meta, X, Mdim, Ndim, Kdim, le, out, status_word, s);
   if (Ndim <= 32) return run_small<32, SPARSE ? 8 : 5, SPARSE>(vals, hw_meta, X, Mdim, Ndim, Kdim, le, out, status_word, s);
   if (Ndim <= 64) return run_small<64, SPARSE ? 6 : 4, SPARSE>(vals, hw_meta, X, Mdim, Ndim, Kdim, le, out, status_word, s);
