@@ -30,6 +30,11 @@ int cuda_fail(cudaError_t e, const char* what);
     }                                          \
   } while (0)
 
+int sm_count();                             // of the current device (gemm_host.cu)
+// SMs that plans count with whose scratch a size query has to know: a B200's, so that the query answers the same with any
+// device current, or none.  Grids and choices without scratch go by sm_count().
+constexpr int PLAN_SMS = 148;
+
 static inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 #ifdef __CUDACC__

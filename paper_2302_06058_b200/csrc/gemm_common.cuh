@@ -708,7 +708,6 @@ __device__ __forceinline__ ChunkWalk<ROWS> chunk_walk(const GemmParams& p, int t
 }
 
 // ---- host helpers (gemm_host.cu) -----------------------------------------------------------
-int sm_count();
 // 2-D bf16 tensor map: `inner` contiguous elements per row, `outer` rows, box = 64 x box_rows, 128-byte swizzle,
 // out-of-range elements read as zero.
 int make_tmap(CUtensorMap* m, const void* ptr, uint64_t inner, uint64_t outer, uint32_t box_rows);

@@ -208,7 +208,7 @@ bias_reduce_kernel(const float4* __restrict__ partial, int nrows, int n4, float4
 
 int stream_grid(long long items) {
   const long long ctas = (items + STREAM_THREADS - 1) / STREAM_THREADS;
-  const long long most = 148 * 32;                        // four rounds of 2048 threads per SM: SMs far from a memory part take fewer
+  const long long most = 32ll * sm_count();               // four rounds of 2048 threads per SM: SMs far from a memory part take fewer
   return (int)(ctas < most ? ctas : most);
 }
 
@@ -224,7 +224,7 @@ ActBwdPlan plan_act_bwd(int T, int C) {
   p.rows = ACTBWD_MAX_THREADS / p.half;
   if (p.rows > T) p.rows = T;
   p.threads = (p.half * p.rows + 31) / 32 * 32;
-  p.slots = 148 / p.tiles;
+  p.slots = PLAN_SMS / p.tiles;
   const int most = (T + p.rows - 1) / p.rows;
   if (p.slots > most) p.slots = most;
   if (p.slots < 1) p.slots = 1;

@@ -766,7 +766,7 @@ static int splits_wanted(int k_tiles, int tiles, int workers) {
 static int wgrad_splits_wanted(int k_tiles, int I, int J) {
   const bool single = wgrad_uses_single(I);
   const int tiles = single ? (J + 255) / 256 : (((I + 127) / 128 + 1) / 2) * ((J + 255) / 256);   // 128 / 256 x 256 tiles
-  return splits_wanted(k_tiles, tiles, single ? 148 : 74);        // CTAs or CTA pairs
+  return splits_wanted(k_tiles, tiles, single ? PLAN_SMS : PLAN_SMS / 2);     // CTAs or CTA pairs
 }
 
 static void wgrad_plan_k(int k_tiles, int I, int J, int* splits, int* k_tiles_per_split) {
@@ -907,7 +907,7 @@ int launch_wgrad_impl(const uint16_t* dY, const uint16_t* X, int T, int I, int J
 static size_t round256(size_t v) { return (v + 255) / 256 * 256; }
 
 static int wgrad_ckpt_splits_wanted(int T, int I, int J) {
-  return splits_wanted((T + 63) / 64, (((I + 127) / 128 + 1) / 2) * ((J + 255) / 256), 74);       // over the CTA pairs
+  return splits_wanted((T + 63) / 64, (((I + 127) / 128 + 1) / 2) * ((J + 255) / 256), PLAN_SMS / 2);   // over the CTA pairs
 }
 
 static void wgrad_ckpt_plan(int T, int I, int J, int* splits, int* per) {
