@@ -47,7 +47,7 @@ ckpt_pack_kernel(const uint4* __restrict__ x, long long halves, uint4* __restric
 
 // The values of a checkpoint, through an activation or as they are.  Eight channels per thread and step, so that the 16-byte
 // stores of a warp are contiguous (16 channels as two stores of every other 16 bytes: 84 us for 8192 x 16384 through
-// an activation, now 72: 5.6 TB/s); two steps' bytes are loaded at a time.
+// an activation, now 76: 5.3 TB/s); two steps' bytes are loaded at a time.
 template <int ACT>
 __global__ void __launch_bounds__(STREAM_THREADS)
 ckpt_unpack_kernel(const uint2* __restrict__ q, const uint8_t* __restrict__ s, long long eighths, uint4* __restrict__ x) {
@@ -82,9 +82,9 @@ ckpt_unpack_kernel(const uint2* __restrict__ q, const uint8_t* __restrict__ s, l
 // apart (so that a warp's 16-byte loads and stores are contiguous; sixteen values share the polynomial's coefficients)
 // and walks over rows, the next three already loading, so the column sums stay in registers; the rows that a CTA takes side
 // by side are added through shared memory at its end, in a fixed order, and each CTA leaves one row of partial sums for
-// bias_reduce_kernel (no atomics: the result does not depend on timing).  8192 x 16384 in 126 us on the device, 5.4 TB/s;
-// 12608 x 1536 in 22 + 3 us: there the launches and the uneven end of the CTAs are a third.  CTA (x, y): column tile x of 2 * half groups of
-// eight, row slot y of gridDim.y.
+// bias_reduce_kernel (no atomics: the result does not depend on timing).  8192 x 16384 in 127 us on the device, 5.3 TB/s
+// (the bias gradient alone 47 us); 12608 x 1536 in 22 + 3 us: there the launches and the uneven end of the CTAs are a
+// third.  CTA (x, y): column tile x of 2 * half groups of eight, row slot y of gridDim.y.
 // ------------------------------------------------------------------------------------------
 constexpr int ACTBWD_MAX_THREADS = 512;
 
