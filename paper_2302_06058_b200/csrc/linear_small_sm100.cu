@@ -13,6 +13,7 @@
 // the deep ring 34 us); 24 tokens, 16384 -> 4096: 16.9 us (54 us).  Left: start-up, the first loads' latency and the join,
 // about 4 us.
 #include "gemm_common.cuh"
+#include <mutex>
 
 namespace bimask {
 
@@ -319,35 +320,47 @@ int run_small_any(const uint16_t* vals, const void* hw_meta, const uint16_t* X, 
 
 }  // namespace
 
-// Clusters of `size` CTAs of this file's kernels that the device holds at once (one CTA per SM, and a cluster must lie within
-// a GPC: 74, 45, 33, 26, 22, 15, 15 of two to eight on a device where 148 SMs are spread unevenly).
-int linear_small_fit(int size) {
+// Clusters of 1 .. 8 CTAs of this file's kernels that the current device holds at once (one CTA per SM, and a cluster must
+// lie within a GPC: 148, 74, 45, 33, 26, 22, 15, 15 on a device whose SMs are spread unevenly).  Asked once per device.
+static const int* fit_table() {
   constexpr int DEVICES = 64;
-  static std::atomic<int> known[DEVICES][9];
+  struct Table { std::atomic<bool> known{false}; int fit[9] = {0, 148, 74, 49, 37, 29, 24, 21, 18}; };
+  static Table tables[DEVICES];
+  static const Table unknown;                             // no device: nothing is launched by it
+  static std::mutex mutex;
   int dev = 0;
-  if (size <= 1 || size > 8 || cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= DEVICES) return sm_count() / (size < 1 ? 1 : size);
-  int n = known[dev][size].load(std::memory_order_relaxed);
-  if (n > 0) return n;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= DEVICES) return unknown.fit;
+  Table& t = tables[dev];
+  if (t.known.load(std::memory_order_acquire)) return t.fit;
+  std::lock_guard<std::mutex> lock(mutex);
+  if (t.known.load(std::memory_order_relaxed)) return t.fit;
   using C = SmallCfg<32, 8, true>;
   auto kern = linear_small_kernel<32, 8, true>;
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)size);
-  cfg.blockDim = dim3(SMALL_THREADS);
-  cfg.dynamicSmemBytes = C::SMEM_BYTES;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = (unsigned)size;
-  attr[0].val.clusterDim.y = 1;
-  attr[0].val.clusterDim.z = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  if (set_smem_attr(kern, C::SMEM_BYTES) != BIMASK_OK || cudaOccupancyMaxActiveClusters(&n, kern, &cfg) != cudaSuccess || n < 1) {
-    cudaGetLastError();                                   // the query alone failed: the launch will say what is wrong
-    return sm_count() / size;
+  if (set_smem_attr(kern, C::SMEM_BYTES) != BIMASK_OK) return unknown.fit;        // the launch will say what is wrong
+  int fit[9] = {0, sm_count()};
+  for (int size = 2; size <= 8; ++size) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)size);
+    cfg.blockDim = dim3(SMALL_THREADS);
+    cfg.dynamicSmemBytes = C::SMEM_BYTES;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)size;
+    attr[0].val.clusterDim.y = 1;
+    attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    if (cudaOccupancyMaxActiveClusters(&fit[size], kern, &cfg) != cudaSuccess || fit[size] < 1) {
+      cudaGetLastError();
+      return unknown.fit;
+    }
   }
-  known[dev][size].store(n, std::memory_order_relaxed);
-  return n;
+  for (int size = 1; size <= 8; ++size) t.fit[size] = fit[size];
+  t.known.store(true, std::memory_order_release);
+  return t.fit;
 }
+
+int linear_small_fit(int size) { return fit_table()[size < 1 ? 1 : size > 8 ? 8 : size]; }
 
 // The largest cluster, at most eight (the portable size) and at least four k tiles per CTA, of which all tiles' fit at once: a
 // second round costs what the split saves and more.  24 tokens, reduction 4096, in one round / one size larger, in two:
@@ -356,8 +369,11 @@ int linear_small_fit(int size) {
 // 4 % at 4096 and lose 2 % at 16384.
 int linear_small_splits(int tiles, int k_tiles) {
   int splits = 1;
-  for (int c = 8; c > 1 && splits == 1; --c)
-    if (4 * c <= k_tiles && tiles <= linear_small_fit(c)) splits = c;
+  if (k_tiles >= 8) {
+    const int* fit = fit_table();
+    for (int c = 8; c > 1 && splits == 1; --c)
+      if (4 * c <= k_tiles && tiles <= fit[c]) splits = c;
+  }
   const int per = (k_tiles + splits - 1) / splits;
   return (k_tiles + per - 1) / per;
 }
