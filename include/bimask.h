@@ -209,11 +209,12 @@ size_t bimask_linear_workspace_bytes(int T, int I, int J);
  * The operand is that of bimask_spmm_fwd (hw_meta_f == NULL: the dense masked operand).
  *   bias  I fp32, or NULL;   R  T x I bf16, or NULL; may be Y itself
  *   Zq, Zs  out, both or neither: the checkpoint of the pre-activation sum + bias (taken from its fp32 value)
- * Sums: with at most 128 tokens (and wherever the reduction is split) no more than 32 tensor-core steps are added up
- * inside the tensor core, whose fp32 sums do not round to nearest; the rest is added in fp32 registers: 5e-7 relative at
- * worst.  More tokens take the chains of bimask_spmm_fwd, one over the whole reduction: a sum is off by 1.0e-7
- * (J = 384), 1.3e-6 (4096), 6.2e-6 (16384) relative, small next to the 2e-3 of the bf16 result.  A checkpoint byte or a
- * rounding of Y may fall to the other side of its boundary for that. */
+ * Sums: the tensor core's fp32 sums do not round to nearest, so it adds up no more than 32 steps (at most 128 tokens, and
+ * wherever the reduction is split) or 96 (other layers) before fp32 registers take over: a sum is off by 5e-7 or 1.7e-6
+ * relative at worst.  Two kinds of layers keep one chain over the whole reduction, as bimask_spmm_fwd does: wide ones (2:4,
+ * T >= 1024, I >= 2048, J >= 4096: 1.3e-6 relative at J = 4096, 6.2e-6 at 16384, mixed signs) and those of at most 128 rows
+ * with more than 16384 tokens.  Small next to the 2e-3 of a bf16 result; a checkpoint byte or a rounding of Y may fall to the
+ * other side of its boundary for that. */
 int bimask_linear_fwd(const uint16_t* X, const uint16_t* vals_f, const void* hw_meta_f, const float* bias_or_null, int act,
                       const uint16_t* R_or_null, int T, int I, int J, uint16_t* Y, int8_t* Zq_or_null, uint8_t* Zs_or_null,
                       int32_t* status_word, void* stream);

@@ -424,6 +424,65 @@ struct EpiParams {
 constexpr int LIN_EPI_WARPS = 16;
 constexpr int LIN_THREADS = 64 + 32 * LIN_EPI_WARPS + 32 * EPI_GROUPS;
 
+// Long reductions.  The tensor core's fp32 sums do not round to nearest, and their error grows with the chain: a sum of
+// positive products is off by 1.3e-6 after 64 MMAs, by 3.7e-6 after 128, 3.2e-5 after 512.  So the CTA-pair kernel ends a
+// chain after at most 96 (24 k tiles of a 2:4 operand, 12 of a dense one), a tile's chains about equally long; the two
+// accumulators take them in turn, and the draining warps add them up (64 columns of one lane quadrant each) in fp32
+// registers while the next chain runs.  The total goes back into the last chain's accumulator, from which the tile is drained
+// like any other.  96, not 32 as elsewhere: a chain should last longer than the drain of the tile before it, which holds the
+// other accumulator meanwhile.  512 rows x 6816 at 2495 tokens: 8.7e-6 -> 1.3e-6, and 30.0 -> 31.4 us; 1536 x 4096 at 8192
+// 58.4 -> 60.4; dense 4096 x 4096 at 8192 174 -> 182; at worst 16384 x 4096 at 512 46 -> 51 (one round of tiles, nothing
+// to hide the joining under).
+__host__ __device__ constexpr int epi_segment(bool sparse) { return sparse ? 24 : 12; }   // k tiles
+// Called by all sixteen draining warps; `quadrant`: tensor memory with the warp's lane offset, col0: its first column.  scount:
+// running number of the tile's first chain on entry, of its last on return (chain c in accumulator c % nbuf).  The warps go on or
+// give up together: a warp whose wait ran out still comes to the barrier.
+__device__ __forceinline__ bool join_chains(uint32_t full_bar0, uint32_t empty_bar0, uint32_t quadrant, int col0, int n_tile, int nseg,
+                                            uint32_t nbuf, uint32_t& scount, int lane, volatile int* abort_flag) {
+  float sum[64];
+#pragma unroll
+  for (int j = 0; j < 64; ++j) sum[j] = 0.f;
+  bool ok = true;
+#pragma unroll 1
+  for (int seg = 0; seg + 1 < nseg; ++seg, ++scount) {
+    const uint32_t buf = scount & (nbuf - 1u), phase = (scount >> (nbuf - 1u)) & 1u;
+    if (ok) ok = __all_sync(0xFFFFFFFFu, ptx::mbar_wait_bounded(full_bar0 + 8u * buf, phase, abort_flag, WAIT_BUDGET));
+    if (!ok) continue;
+    ptx::tc_fence_after();
+#pragma unroll
+    for (int j = 0; j < 64; j += 16) {
+      if (col0 + j < n_tile) {
+        uint32_t r[16];
+        ptx::tmem_ld_32x16(quadrant + 256u * buf + (uint32_t)(col0 + j), r);
+        ptx::tmem_ld_wait();
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sum[j + i] += __uint_as_float(r[i]);
+      }
+    }
+    release_accumulator(ptx::mapa(empty_bar0 + 8u * buf, 0), lane);
+  }
+  const uint32_t buf = scount & (nbuf - 1u), phase = (scount >> (nbuf - 1u)) & 1u;
+  if (ok) ok = ptx::mbar_wait_bounded(full_bar0 + 8u * buf, phase, abort_flag, WAIT_BUDGET);
+  ok = ptx::named_bar_and(1 + LIN_EPI_WARPS / 4, 32 * LIN_EPI_WARPS, ok);
+  if (!ok) return false;
+  ptx::tc_fence_after();
+#pragma unroll
+  for (int j = 0; j < 64; j += 16) {
+    if (col0 + j < n_tile) {
+      uint32_t r[16];
+      ptx::tmem_ld_32x16(quadrant + 256u * buf + (uint32_t)(col0 + j), r);
+      ptx::tmem_ld_wait();
+#pragma unroll
+      for (int i = 0; i < 16; ++i) r[i] = __float_as_uint(sum[j + i] + __uint_as_float(r[i]));
+      ptx::tmem_st_32x16(quadrant + 256u * buf + (uint32_t)(col0 + j), r);
+    }
+  }
+  ptx::tmem_st_wait();
+  ptx::tc_fence_before();
+  ptx::named_bar_sync(1 + LIN_EPI_WARPS / 4, 32 * LIN_EPI_WARPS);     // the chunks are drained by other warps than summed them
+  return true;
+}
+
 // Checkpoint of one warp's chunk: 32 rows = one block of 32 channels, 32 tokens.  `z` in the accumulator-fragment
 // layout (lane = 4 a + b: pair 8 h + 2 g + j holds row 16 h + 8 j + a, tokens 8 g + 2 b + {0, 1}).
 //   scales: the maximum of a token's 32 values is four registers and the eight lanes that share b; the halving exchange

@@ -271,7 +271,8 @@ struct PairPCfg {
 // SPARSE = false: the same kernel on a dense bf16 A operand (masked weights of a pattern the 2:4 format cannot
 // hold): a 256 x 128 A tile per stage as two 64-wide boxes per CTA, eight K = 16 MMAs, no metadata, and two
 // accumulators at every N (tmapE is not used).
-template <int STAGES, bool CONV, bool SPARSE = true, bool EPI = false>
+// LONG (with EPI): several tensor-core chains per tile (join_chains).
+template <int STAGES, bool CONV, bool SPARSE = true, bool EPI = false, bool LONG = false>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(EPI ? LIN_THREADS : PAIR_THREADS, 1)
 spmm_pair_persistent_kernel(const __grid_constant__ CUtensorMap tmapA, const __grid_constant__ CUtensorMap tmapB,
                             const __grid_constant__ CUtensorMap tmapE, const __grid_constant__ CUtensorMap tmapD,
@@ -303,6 +304,8 @@ spmm_pair_persistent_kernel(const __grid_constant__ CUtensorMap tmapA, const __g
   const int num_kt = (p.Kdim + 127) / 128;
   const int SP_N = p.n_tile;                              // output columns (tokens) per tile
   const uint32_t nbuf = (!SPARSE || SP_N <= 240) ? 2u : 1u;   // accumulators in tensor memory
+  const int nseg = LONG ? (num_kt + epi_segment(SPARSE) - 1) / epi_segment(SPARSE) : 1;   // tensor-core chains per tile, of about
+  const int segment = LONG ? (num_kt + nseg - 1) / nseg : num_kt;                        // equal length, none empty
   const uint32_t b_box = (uint32_t)(SP_N / 2) * 128u;     // bytes of one 64-wide box of this CTA's B rows
   const uint32_t stage_tx = C::A_BYTES + 2u * b_box + C::E_BYTES;
 
@@ -391,15 +394,17 @@ spmm_pair_persistent_kernel(const __grid_constant__ CUtensorMap tmapA, const __g
   } else if (warp == 1) {
     if (rank == 0 && ptx::elect_one()) {
       const uint32_t idesc = ptx::idesc_bf16(256, SP_N, false, false, SPARSE);
-      uint32_t it = 0, tcount = 0;
+      uint32_t it = 0, scount = 0;                          // chains: one per tile, LONG several
       bool ok = true;
-      for (int tile = cluster_id; tile < num_tiles && ok; tile += num_clusters, ++tcount) {
-        const uint32_t buf = tcount % nbuf;
+      const int num_chains = nseg * ((num_tiles - cluster_id + num_clusters - 1) / num_clusters);
+      for (int seg = 0; (int)scount < num_chains && ok; ++scount, seg = seg + 1 < nseg ? seg + 1 : 0) {
+        const uint32_t buf = scount % nbuf;
         // this accumulator must have been drained by both CTAs' epilogues
-        if (!ptx::mbar_wait_bounded(tmem_empty_bar(buf), ((tcount / nbuf) & 1u) ^ 1u, abort_flag, WAIT_BUDGET)) { *abort_flag = 1; break; }
+        if (!ptx::mbar_wait_bounded(tmem_empty_bar(buf), ((scount / nbuf) & 1u) ^ 1u, abort_flag, WAIT_BUDGET)) { *abort_flag = 1; break; }
         ptx::tc_fence_after();
         const uint32_t acc = tmem_base + 256u * buf;
-        for (int kt = 0; kt < num_kt; ++kt, ++it) {
+        const int kn = LONG ? min(segment, num_kt - seg * segment) : num_kt;
+        for (int kt = 0; kt < kn; ++kt, ++it) {
           const int s = it % STAGES;
           const uint32_t ph = (it / STAGES) & 1u;
           if (!ptx::mbar_wait_bounded(full_bar(s), ph, abort_flag, WAIT_BUDGET)) { *abort_flag = 1; ok = false; break; }
@@ -436,17 +441,23 @@ spmm_pair_persistent_kernel(const __grid_constant__ CUtensorMap tmapA, const __g
     const uint32_t stg = staging + ring * (C::EPI_NT * 8192);
     const uint32_t ebars = epi_bars_of<C::EPI_NT>(bar_base, ring);
     uint16_t* outp = reinterpret_cast<uint16_t*>(p.out);
-    uint32_t tcount = 0, u = 0;
-    for (int tile = cluster_id; tile < num_tiles; tile += num_clusters, ++tcount) {
+    uint32_t scount = 0, u = 0;
+    for (int tile = cluster_id; tile < num_tiles; tile += num_clusters, ++scount) {
+      bool ok = true;
+      if constexpr (LONG)
+        ok = join_chains(tmem_full_bar(0), tmem_empty_bar(0), tmem_base + ((uint32_t)(32 * q) << 16), 64 * eg, SP_N, nseg, nbuf, scount, lane,
+                         abort_flag);
       int tile_m, tile_n;
       raster(tile, p.tiles_m, p.tiles_n, p.raster_group, tile_m, tile_n);
       const int m0 = (2 * tile_m + (int)rank) * 128, n0 = tile_n * SP_N;
-      const uint32_t buf = tcount % nbuf;
       float bias[4];
       if (EPI) epi_bias(e.bias, m0 + 32 * q, p.Mdim, lane, bias);
-      bool ok = ptx::mbar_wait_bounded(tmem_full_bar(buf), (tcount / nbuf) & 1u, abort_flag, WAIT_BUDGET);
-      ok = ptx::named_bar_and(1 + eg, 128, ok);            // the four warps of a group go on or give up together
+      if (!LONG) {
+        ok = ptx::mbar_wait_bounded(tmem_full_bar(scount % nbuf), (scount / nbuf) & 1u, abort_flag, WAIT_BUDGET);
+        ok = ptx::named_bar_and(1 + eg, 128, ok);          // the four warps of a group go on or give up together
+      }
       if (!ok) { *abort_flag = 1; break; }
+      const uint32_t buf = scount % nbuf;
       ptx::tc_fence_after();
       const uint32_t acc = tmem_base + 256u * buf + ((uint32_t)(32 * q) << 16);
       const uint32_t release_bar = ptx::mapa(tmem_empty_bar(buf), 0);
@@ -806,7 +817,7 @@ int run_single(const uint16_t* vals, const void* hw_meta, const uint16_t* Bop, i
 // groups of four draining warps, a store warp each) takes about 430 clocks per 32-column chunk and group; with
 // N <= 224 the two overlap (two accumulators), with N = 256 they add up; the kernel's time is the number of passes
 // over the clusters times the tile time.
-int choose_sparse_n(int pair_tiles_m, int Ndim, int k_tiles, int clusters) {
+int choose_sparse_n(int pair_tiles_m, int Ndim, int k_tiles, int clusters, bool chains = false) {
   int best_n = 256;
   double best = 1e30;
   for (int n = 256; n >= 96; n -= 32) {                     // multiples of 32 only: 16-column chunks drain at 570 clocks each
@@ -815,7 +826,8 @@ int choose_sparse_n(int pair_tiles_m, int Ndim, int k_tiles, int clusters) {
     const double feed = (18432.0 + 128.0 * n) / 64.0;
     const double mainloop = (double)k_tiles * (2.0 * n > feed ? 2.0 * n : feed);
     const double epilogue = ((n / 32 + 1) / 2) * 430.0;
-    const double tile = n == 256 ? mainloop + epilogue : (mainloop > epilogue ? mainloop : epilogue);
+    const double joins = chains ? 1500.0 * (k_tiles / epi_segment(true)) : 0.0;       // several chains: with one accumulator the next waits
+    const double tile = n == 256 ? mainloop + epilogue + joins : (mainloop > epilogue ? mainloop : epilogue);
     const double cost = (double)rounds * tile * (1.0 + 0.001 * (256 - n));
     if (cost < best) { best = cost; best_n = n; }
   }
@@ -831,7 +843,8 @@ int run_sparse_pair_persistent(const uint16_t* vals, const void* hw_meta, const 
   int rc;
   const int tiles_m = (Mdim + 127) / 128, tiles_k = (Kdim + 127) / 128;
   const int sms = sm_count();
-  const int n_tile = choose_sparse_n((tiles_m + 1) / 2, Ndim, tiles_k, sms / 2);
+  const bool is_long = EPI && tiles_k > epi_segment(true);
+  const int n_tile = choose_sparse_n((tiles_m + 1) / 2, Ndim, tiles_k, sms / 2, is_long);
   if ((rc = make_tmap(&ta, vals, (uint64_t)Kdim / 2, (uint64_t)Mdim, 128)) != BIMASK_OK) return rc;
   if ((rc = make_tmap(&tb, Bop, (uint64_t)Kdim, (uint64_t)Ndim, n_tile / 2)) != BIMASK_OK) return rc;
   if ((rc = make_tmap_meta(&te, hw_meta, (uint64_t)tiles_m * tiles_k)) != BIMASK_OK) return rc;
@@ -839,7 +852,7 @@ int run_sparse_pair_persistent(const uint16_t* vals, const void* hw_meta, const 
   CUtensorMap tr;
   EpiParams e;
   if ((rc = epi_args(le, Mdim, Ndim, td, &tr, &e)) != BIMASK_OK) return rc;
-  auto kern = spmm_pair_persistent_kernel<STAGES, false, true, EPI>;
+  auto kern = is_long ? spmm_pair_persistent_kernel<STAGES, false, true, EPI, EPI> : spmm_pair_persistent_kernel<STAGES, false, true, EPI>;
   constexpr int smem = C::SMEM_BYTES + (EPI ? epi_scales_bytes(C::EPI_NT) : 0);
   if ((rc = set_smem_attr(kern, smem)) != BIMASK_OK) return rc;
   GemmParams p;
@@ -1088,7 +1101,8 @@ int run_dense_pair_persistent(const uint16_t* A, const uint16_t* Bop, int Mdim, 
   CUtensorMap tr;
   EpiParams e;
   if ((rc = epi_args(le, Mdim, Ndim, td, &tr, &e)) != BIMASK_OK) return rc;
-  auto kern = spmm_pair_persistent_kernel<STAGES, false, false, EPI>;
+  auto kern = EPI && tiles_k > epi_segment(false) ? spmm_pair_persistent_kernel<STAGES, false, false, EPI, EPI>
+                                                  : spmm_pair_persistent_kernel<STAGES, false, false, EPI>;
   constexpr int smem = C::SMEM_BYTES + (EPI ? epi_scales_bytes(C::EPI_NT) : 0);
   if ((rc = set_smem_attr(kern, smem)) != BIMASK_OK) return rc;
   GemmParams p;
@@ -1150,11 +1164,12 @@ static bool split_is_faster(bool sparse, int Mdim, int Ndim, int Kdim) {
 
 // Linear layer: the product of launch_spmm (hw_meta given) or launch_dense_nt (null) with the epilogue of `le`, on the
 // same kernels by the same rules, and on the kernel for few tokens.
-// Sums: the kernels of this file keep one tensor-core chain over the reduction, which does not round to nearest (relative
-// error of a sum, mixed signs: 1.0e-7 at 384, 2.6e-7 at 2048, 1.3e-6 at 4096, 6.2e-6 at 16384; rounded fp32 sums about
-// 1e-7).  A choice for speed: ending the chains early takes a second accumulator, for which the 512-row tiles of the wide
-// layers leave no tensor memory, and 256-row tiles are bound by the L2 feed (8192 tokens: 16384 x 4096 with tanh-GELU and
-// checkpoint 563 against 490 us, 4096 x 16384 with a residual 496 against 399).
+// Sums.  The tensor core does not round its fp32 sums to nearest.  The kernel for few tokens and the CTA pairs end its chains
+// after 32 and 96 MMAs (a sum of positive products is off by 5e-7 and 1.7e-6 at worst, whatever the reduction).  Two keep
+// one chain over the reduction, a choice for speed: the 512-row tiles of the wide layers, which leave no tensor memory for a second
+// accumulator (mixed signs: 1.3e-6 at 4096, 6.2e-6 at 16384; 256-row tiles are bound by the L2 feed: 8192 tokens, 16384 x 4096
+// with tanh-GELU and checkpoint 563 against 490 us, 4096 x 16384 with a residual 496 against 399), and the one row tile of at
+// most 128 rows, taken where reductions are short or tokens more than 16384.
 int linear_kernel_choice(bool sparse, int Mdim, int Ndim, int Kdim) {
   if (Ndim <= 128 || split_is_faster(sparse, Mdim, Ndim, Kdim)) return LINEAR_FEW_TOKENS;
   if (Mdim <= 128) return LINEAR_ONE_ROW_TILE;

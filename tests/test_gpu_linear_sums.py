@@ -45,3 +45,24 @@ def test_few_tokens_sum_long_reductions_in_short_chains(T, dense):
     allowed = ((512 / 16 + 32) * 2.0 ** -23 + (J / 512 + 1) * 2.0 ** -24) * (1 + 2.0 ** -8)
     print(f"T {T} dense {dense}: worst {off.max().item():.2e}, mean {off.mean().item():.2e}, allowed {allowed:.2e}")
     assert float(off.max()) <= allowed
+
+
+@pytest.mark.parametrize("T,I,J,dense", [(700, 2048, 16384, False), (900, 4096, 16384, False), (8192, 1536, 16384, False), (1200, 4096, 16384, True)])
+def test_pairs_sum_long_reductions_in_several_chains(T, I, J, dense):
+    """CTA pairs: chains of at most 96 MMAs.  Allowed: one unit of the last place per MMA of a chain and 32 for the products inside
+    them (2^-23 of the chain's sum each), an addition per chain, the rounding of the bias.  One chain over everything is off by more."""
+    assert bm.bimask_debug_linear_plan(T, I, J, dense)[0] == 2
+    vals, hw, Wm = positive_operand(I, J, dense, 5)
+    x = (torch.rand(J, generator=torch.Generator(device="cuda").manual_seed(6), device="cuda") + 0.5).to(torch.bfloat16)
+    exact = torch.cat([Wm[i:i + 1024].double() @ x.double() for i in range(0, I, 1024)])
+    bias = -exact.float()
+    Y = torch.empty(T, I, dtype=torch.bfloat16, device="cuda")
+    st = torch.zeros(1, dtype=torch.int32, device="cuda")
+    bm.bimask_linear_fwd(x.expand(T, J).contiguous(), vals, hw, bias, bm.ACT_NONE, None, T, I, J, Y, None, None, st)
+    torch.cuda.synchronize()
+    assert int(st.item()) == 0
+    off = (Y.double() - (exact + bias.double())).abs() / exact
+    chains = -(-J // (12 * 128 if dense else 24 * 128))
+    allowed = ((96 + 32) * 2.0 ** -23 + (chains + 1) * 2.0 ** -24) * (1 + 2.0 ** -8)
+    print(f"{T} {I} {J} dense {dense}: worst {off.max().item():.2e}, allowed {allowed:.2e}")
+    assert float(off.max()) <= allowed
