@@ -238,6 +238,88 @@ int bimask_ckpt_unpack(const int8_t* q, const uint8_t* s, int act, int T, int C,
 int bimask_wgrad_ckpt(const uint16_t* dY, const int8_t* Xq, const uint8_t* Xs, int T, int I, int J, float* dW, void* ws,
                       size_t ws_bytes, int32_t* status_word, void* stream);
 
+/* ---- Between the layers of a transformer block: dropout, and the junction of a block with its residual stream ----
+ *
+ * (No counterpart in the paper.)  TYPE: element type of a matrix that may be either. */
+enum { BIMASK_TYPE_BF16 = 0, BIMASK_TYPE_F32 = 1 };
+enum { BIMASK_NORM_NONE = 0, BIMASK_NORM_RMS = 1, BIMASK_NORM_LAYER = 2 };
+
+/* Dropout whose mask is never stored: it is a function of seed, stream number and position, so that the gradient's call
+ * draws it again.  Element e = t C + c of a T x C matrix belongs to block e / 8; the 128 bits of a block are Philox4x32-10
+ * (Salmon et al., SC 2011) of the counter (block low, block high, n low, n high), 32 bits each, under the key
+ * (seed low, seed high), with n = stream_no + *counter.  Element 8 b + k takes the low (k even) or high (k odd) half of word
+ * k / 2; it is kept iff these 16 bits are at least thr = 65536 p rounded to the nearest integer (at most 65535), and is then
+ * multiplied by 65536 / (65536 - thr): p is honoured in steps of 2^-16, without bias.  A dropped element is +0, even where it
+ * was not finite.  Row t of a smaller batch has the mask of row t of a larger one.  Calls that must not share a mask differ in
+ * stream_no (one per layer, say) or in *counter (one per step); with p below 2^-17 nothing is dropped or drawn. */
+typedef struct {
+  float p;                     /* 0 <= p < 1 */
+  uint64_t seed;
+  uint64_t stream_no;
+  const uint64_t* counter;     /* DEVICE memory read when the kernel runs, or NULL (0): lets a captured graph draw new masks */
+} bimask_dropout_args;
+
+/* Y = drop(X), T x C of `type`; Y may be X.  Its own gradient: dX = drop(dY) with the same arguments. */
+int bimask_dropout(const void* X, int type, int T, int C, const bimask_dropout_args* drop, void* Y, void* stream);
+
+/* bimask_ckpt_unpack and bimask_act_bwd of a hidden layer H = drop(act(Z)):
+ *   X = drop(act(values)), rounded once;   dZ = drop(dY) * act'(Z), dbias its column sums. */
+int bimask_ckpt_unpack_dropout(const int8_t* q, const uint8_t* s, int act, const bimask_dropout_args* drop, int T, int C, uint16_t* X,
+                               void* stream);
+int bimask_act_dropout_bwd(const uint16_t* dY, const int8_t* Zq, const uint8_t* Zs, int act, const bimask_dropout_args* drop, int T, int C,
+                           uint16_t* dZ_or_null, float* dbias_or_null, void* ws, size_t ws_bytes, void* stream);
+
+/* The junction of a block's result y with the residual stream x, up to the input n of the next block:
+ *
+ *     u = norm_post(y),   x' = alpha x + scale * gate * drop(u),   n = norm_pre(x')
+ *
+ * norm(v) = (v - mean) rstd w + b per token, rstd = 1 / sqrt(mean((v - mean)^2) + eps); RMS: with 0 in the place of the mean.
+ * Every part but x may be absent: y == NULL leaves the norm of alpha x alone (the first block's input), norm NONE leaves its
+ * norm out, gate / scale / w / b == NULL stand for 1, 1, 1 and 0, drop.p == 0 for no dropout, alpha is 1 for a plain residual.
+ * All arithmetic is fp32, results are rounded once; n is taken from x' before its rounding.  Squares are fp32: a row with
+ * magnitudes above 1e18 may overflow them.
+ *
+ * Sizes: C % 32 == 0, C <= 8192 (BIMASK_EUNSUPPORTED above), any T.  T x C matrices of the stream (x, xo, dx, dxo) have
+ * stream_type; y, n, gate and their gradients are bf16; C-vectors are fp32.  stats: T x 2 fp32 (mean, rstd; mean 0 for RMS),
+ * what the backward pass needs of a norm.
+ * gate: row t / gate_span serves token t; 1: one row per token, the tokens of a sample: one row per sample.  Rows are gate_pitch
+ * elements apart (a multiple of 8, at least C: a column slice of a wider matrix will do), those of dgate as well.
+ *
+ * Forward.   in: x, y, gate, scale, w_*, b_*.  out: xo = x' (may be x; may be NULL when there is a norm before), n (with a norm
+ *            before; may be y), stats_post, stats_pre (may be NULL).
+ * Backward.  in: dxo, the gradient of x' from its other uses (NULL: zero), dn; xo, stats_pre with a norm before, stats_post with a
+ *            norm after, gate, scale, w_*, b_post, drop as in the forward pass; y with a norm after, dgate or dscale.
+ *            out, each of them NULL where it is not wanted: dx (may be dxo), dy (may be dn or y), dgate (summed over its span, rounded
+ *            once), dscale, dw_post, db_post, dw_pre, db_pre (fp32, added in an order that depends on the sizes alone).
+ *            With y absent in the forward pass only dx, dw_pre and db_pre are asked for (xo: alpha x).
+ *            ws: bimask_residual_norm_workspace_bytes(T, C, gate_span, or 1 without a gate) bytes, needed for gradients of vectors
+ *            and of a gate with gate_span > 1.  Never fewer for more tokens. */
+typedef struct {
+  int T, C;
+  int stream_type, post, pre;  /* BIMASK_TYPE_*, BIMASK_NORM_* */
+  int gate_span;               /* >= 1 with a gate */
+  int64_t gate_pitch;
+  float eps_post, eps_pre, alpha;
+  bimask_dropout_args drop;
+  const void* x;
+  const uint16_t *y, *gate;
+  const float *scale, *w_post, *b_post, *w_pre, *b_pre;
+  void* xo;
+  uint16_t* n;
+  float *stats_post, *stats_pre;
+  const void* dxo;
+  const uint16_t* dn;
+  void* dx;
+  uint16_t *dy, *dgate;
+  float *dscale, *dw_post, *db_post, *dw_pre, *db_pre;
+  void* ws;
+  size_t ws_bytes;
+} bimask_residual_args;
+
+size_t bimask_residual_norm_workspace_bytes(int T, int C, int gate_span);
+int bimask_residual_norm_fwd(const bimask_residual_args* args, void* stream);
+int bimask_residual_norm_bwd(const bimask_residual_args* args, void* stream);
+
 /* One iteration of Alg. 1 for one layer (without the optimizer update): fwd mask + pack, sparse
  * forward, [search if do_search], bwd mask + pack, sparse input gradient, dense weight
  * gradient.  The caller sees one ordered step on `stream`: everything the call enqueues starts after the work

@@ -25,7 +25,8 @@ EXPORTS = ("bimask_last_error", "bimask_launch_count", "bimask_hw_meta_bytes", "
            "bimask_refine_workspace_bytes", "bimask_perm_refine", "bimask_debug_gen_candidates", "bimask_debug_status", "bimask_debug_drain_plan",
            "bimask_debug_linear_plan",
            "bimask_linear_workspace_bytes", "bimask_linear_fwd", "bimask_act_bwd", "bimask_ckpt_pack", "bimask_ckpt_unpack",
-           "bimask_wgrad_ckpt")
+           "bimask_wgrad_ckpt", "bimask_dropout", "bimask_ckpt_unpack_dropout", "bimask_act_dropout_bwd",
+           "bimask_residual_norm_workspace_bytes", "bimask_residual_norm_fwd", "bimask_residual_norm_bwd")
 
 
 class BimaskError(RuntimeError):
@@ -56,6 +57,22 @@ class ConvArgs(Structure):
     """Mirror of bimask_conv_args."""
     _fields_ = [("layer", LayerArgs), ("NB", c_int), ("H", c_int), ("W", c_int), ("C", c_int), ("mode", c_int),
                 ("stride", c_int)]
+
+
+class Dropout(Structure):
+    """Mirror of bimask_dropout_args."""
+    _fields_ = [("p", c_float), ("seed", c_uint64), ("stream_no", c_uint64), ("counter", c_void_p)]
+
+
+_RESIDUAL_POINTERS = ("x", "y", "gate", "scale", "w_post", "b_post", "w_pre", "b_pre", "xo", "n", "stats_post", "stats_pre",
+                      "dxo", "dn", "dx", "dy", "dgate", "dscale", "dw_post", "db_post", "dw_pre", "db_pre", "ws")
+
+
+class ResidualArgs(Structure):
+    """Mirror of bimask_residual_args."""
+    _fields_ = [("T", c_int), ("C", c_int), ("stream_type", c_int), ("post", c_int), ("pre", c_int), ("gate_span", c_int),
+                ("gate_pitch", c_int64), ("eps_post", c_float), ("eps_pre", c_float), ("alpha", c_float), ("drop", Dropout),
+                *((name, c_void_p) for name in _RESIDUAL_POINTERS), ("ws_bytes", c_size_t)]
 
 
 CONV_AUTO, CONV_EXPLICIT, CONV_IMPLICIT = 0, 1, 2
@@ -112,6 +129,14 @@ def lib() -> ctypes.CDLL:
         L.bimask_ckpt_unpack.argtypes = [c_void_p, c_void_p, c_int, c_int, c_int, c_void_p, c_void_p]
         L.bimask_wgrad_ckpt.argtypes = [c_void_p, c_void_p, c_void_p, c_int, c_int, c_int, c_void_p, c_void_p, c_size_t, c_void_p,
                                         c_void_p]
+        L.bimask_dropout.argtypes = [c_void_p, c_int, c_int, c_int, POINTER(Dropout), c_void_p, c_void_p]
+        L.bimask_ckpt_unpack_dropout.argtypes = [c_void_p, c_void_p, c_int, POINTER(Dropout), c_int, c_int, c_void_p, c_void_p]
+        L.bimask_act_dropout_bwd.argtypes = [c_void_p, c_void_p, c_void_p, c_int, POINTER(Dropout), c_int, c_int, c_void_p, c_void_p,
+                                             c_void_p, c_size_t, c_void_p]
+        L.bimask_residual_norm_workspace_bytes.restype = c_size_t
+        L.bimask_residual_norm_workspace_bytes.argtypes = [c_int, c_int, c_int]
+        L.bimask_residual_norm_fwd.argtypes = [POINTER(ResidualArgs), c_void_p]
+        L.bimask_residual_norm_bwd.argtypes = [POINTER(ResidualArgs), c_void_p]
         L.bimask_check_perms.argtypes = [c_void_p, c_int, c_int, c_void_p, c_void_p, c_size_t, c_void_p]
         L.bimask_debug_wait_probe.argtypes = [c_void_p, c_void_p]
         L.bimask_debug_status.argtypes = [c_void_p]
@@ -124,7 +149,8 @@ def lib() -> ctypes.CDLL:
         for name in EXPORTS:
             if name not in ("bimask_last_error", "bimask_launch_count", "bimask_hw_meta_bytes", "bimask_workspace_bytes",
                             "bimask_perm_search_static_max_entries", "bimask_conv_workspace_bytes",
-                            "bimask_refine_workspace_bytes", "bimask_linear_workspace_bytes"):
+                            "bimask_refine_workspace_bytes", "bimask_linear_workspace_bytes",
+                            "bimask_residual_norm_workspace_bytes"):
                 getattr(L, name).restype = c_int
         _lib = L
     return _lib
@@ -262,6 +288,73 @@ def bimask_ckpt_unpack(q, s, act, T, C, X, stream=None):
 def bimask_wgrad_ckpt(dY, Xq, Xs, T, I, J, dW, ws, ws_bytes, status_word, stream=None):
     return _check(lib().bimask_wgrad_ckpt(_ptr(dY), _ptr(Xq), _ptr(Xs), T, I, J, _ptr(dW), _ptr(ws), ws_bytes,
                                           _ptr(status_word), _stream(stream)))
+
+
+TYPE_BF16, TYPE_F32 = 0, 1
+NORM_NONE, NORM_RMS, NORM_LAYER = 0, 1, 2
+
+
+def make_dropout(p, seed, stream_no=0, counter=None) -> Dropout:
+    """Probability, seed and stream number of a dropout; counter: one-element int64 CUDA tensor that is added to the stream
+    number when the kernel runs."""
+    return Dropout(p, seed, stream_no, _ptr(counter))
+
+
+def bimask_dropout(X, type, T, C, drop, Y, stream=None):
+    return _check(lib().bimask_dropout(_ptr(X), type, T, C, drop, _ptr(Y), _stream(stream)))
+
+
+def bimask_ckpt_unpack_dropout(q, s, act, drop, T, C, X, stream=None):
+    return _check(lib().bimask_ckpt_unpack_dropout(_ptr(q), _ptr(s), act, drop, T, C, _ptr(X), _stream(stream)))
+
+
+def bimask_act_dropout_bwd(dY, Zq, Zs, act, drop, T, C, dZ_or_null, dbias_or_null, ws, ws_bytes, stream=None):
+    return _check(lib().bimask_act_dropout_bwd(_ptr(dY), _ptr(Zq), _ptr(Zs), act, drop, T, C, _ptr(dZ_or_null), _ptr(dbias_or_null),
+                                               _ptr(ws), ws_bytes, _stream(stream)))
+
+
+def bimask_residual_norm_workspace_bytes(T: int, C: int, gate_span: int = 1) -> int:
+    return lib().bimask_residual_norm_workspace_bytes(T, C, gate_span)
+
+
+def _row_pitch(t, C):
+    """Elements between the rows of a gate: a tensor of rows that are contiguous in themselves."""
+    if not isinstance(t, torch.Tensor) or t.is_contiguous():
+        return C
+    if t.dim() != 2 or t.stride(1) != 1:
+        raise ValueError("a gate's rows must be contiguous")
+    return t.stride(0)
+
+
+def make_residual_args(T, C, bufs: dict, stream_type=TYPE_BF16, post=NORM_NONE, pre=NORM_NONE, eps_post=1e-5, eps_pre=1e-5, alpha=1.0,
+                       gate_span=1, drop: Dropout | None = None) -> ResidualArgs:
+    """Fill a bimask_residual_args from a dict of tensors keyed by field name (missing keys -> NULL).  The rows of gate and dgate
+    may be slices of a wider matrix, both of the same pitch (bufs["gate_pitch"] gives it where they are addresses)."""
+    a = ResidualArgs(T, C, stream_type, post, pre, gate_span, 0, eps_post, eps_pre, alpha)
+    if drop is not None:
+        a.drop = drop
+    get = bufs.get
+    for name in _RESIDUAL_POINTERS:
+        t = get(name)
+        if t is not None:
+            if name == "gate" or name == "dgate":
+                pitch = _row_pitch(t, get("gate_pitch", C))
+                if a.gate_pitch not in (0, pitch):
+                    raise ValueError("gate and dgate must have the same row pitch")
+                a.gate_pitch = pitch
+                t = t.data_ptr() if isinstance(t, torch.Tensor) else t
+            setattr(a, name, _ptr(t))
+    ws = get("ws")
+    a.ws_bytes = ws.numel() * ws.element_size() if isinstance(ws, torch.Tensor) else int(get("ws_bytes", 0))
+    return a
+
+
+def bimask_residual_norm_fwd(args: ResidualArgs, stream=None):
+    return _check(lib().bimask_residual_norm_fwd(args, _stream(stream)))
+
+
+def bimask_residual_norm_bwd(args: ResidualArgs, stream=None):
+    return _check(lib().bimask_residual_norm_bwd(args, _stream(stream)))
 
 
 def make_layer_args(T, I, J, N, M, P, seed, do_search, bufs: dict, stream=None) -> LayerArgs:

@@ -353,19 +353,26 @@ int bimask_linear_fwd(const uint16_t* X, const uint16_t* vals_f, const void* hw_
   return launch_linear_fwd(vals_f, hw_meta_f, X, I, T, J, le, Y, status_word, (cudaStream_t)stream);
 }
 
-int bimask_act_bwd(const uint16_t* dY, const int8_t* Zq, const uint8_t* Zs, int act, int T, int C, uint16_t* dZ, float* dbias,
-                   void* ws, size_t ws_bytes, void* stream) {
-  int rc = check_rows("bimask_act_bwd", T, C);
+static int check_act_bwd(const char* who, const uint16_t* dY, const int8_t* Zq, const uint8_t* Zs, int act, int T, int C, const uint16_t* dZ,
+                         const float* dbias, const void* ws, size_t ws_bytes) {
+  int rc = check_rows(who, T, C);
   if (rc != BIMASK_OK) return rc;
-  if ((rc = check_act("bimask_act_bwd", act)) != BIMASK_OK) return rc;
-  BIMASK_REQUIRE(dY && (dZ || dbias), BIMASK_EINVAL, "bimask_act_bwd: null pointer (dY, or both results)");
-  BIMASK_REQUIRE(act == BIMASK_ACT_NONE || (Zq && Zs), BIMASK_EINVAL, "bimask_act_bwd: the slope of an activation needs Zq and Zs");
+  if ((rc = check_act(who, act)) != BIMASK_OK) return rc;
+  BIMASK_REQUIRE(dY && (dZ || dbias), BIMASK_EINVAL, "%s: null pointer (dY, or both results)", who);
+  BIMASK_REQUIRE(act == BIMASK_ACT_NONE || (Zq && Zs), BIMASK_EINVAL, "%s: the slope of an activation needs Zq and Zs", who);
   BIMASK_REQUIRE(aligned16(dY) && aligned16(Zq) && aligned16(Zs) && aligned16(dZ) && aligned16(dbias) && aligned16(ws), BIMASK_EINVAL,
-                 "bimask_act_bwd: pointers must be 16-byte aligned");
+                 "%s: pointers must be 16-byte aligned", who);
   if (dbias) {
     const size_t need = act_bwd_partial_bytes(T, C);
-    BIMASK_REQUIRE(ws && ws_bytes >= need, BIMASK_EINVAL, "bimask_act_bwd: workspace too small (%zu bytes, need %zu)", ws ? ws_bytes : 0, need);
+    BIMASK_REQUIRE(ws && ws_bytes >= need, BIMASK_EINVAL, "%s: workspace too small (%zu bytes, need %zu)", who, ws ? ws_bytes : 0, need);
   }
+  return BIMASK_OK;
+}
+
+int bimask_act_bwd(const uint16_t* dY, const int8_t* Zq, const uint8_t* Zs, int act, int T, int C, uint16_t* dZ, float* dbias,
+                   void* ws, size_t ws_bytes, void* stream) {
+  const int rc = check_act_bwd("bimask_act_bwd", dY, Zq, Zs, act, T, C, dZ, dbias, ws, ws_bytes);
+  if (rc != BIMASK_OK) return rc;
   return launch_act_bwd(dY, Zq, Zs, act, T, C, dZ, dbias, reinterpret_cast<float*>(ws), (cudaStream_t)stream);
 }
 
@@ -384,6 +391,113 @@ int bimask_ckpt_unpack(const int8_t* q, const uint8_t* s, int act, int T, int C,
   BIMASK_REQUIRE(X && q && s, BIMASK_EINVAL, "bimask_ckpt_unpack: null pointer");
   BIMASK_REQUIRE(aligned16(X) && aligned16(q) && aligned16(s), BIMASK_EINVAL, "bimask_ckpt_unpack: pointers must be 16-byte aligned");
   return launch_ckpt_unpack(q, s, act, T, C, X, (cudaStream_t)stream);
+}
+
+// ---- dropout and the residual junction ----
+
+static int check_drop(const char* who, const bimask_dropout_args* d) {
+  BIMASK_REQUIRE(d != nullptr, BIMASK_EINVAL, "%s: null pointer (drop)", who);
+  BIMASK_REQUIRE(d->p >= 0.f && d->p < 1.f, BIMASK_EINVAL, "%s: p = %g out of range 0 <= p < 1", who, (double)d->p);
+  BIMASK_REQUIRE((uintptr_t)d->counter % 8 == 0, BIMASK_EINVAL, "%s: counter must be 8-byte aligned", who);
+  return BIMASK_OK;
+}
+
+static int check_type(const char* who, int type) {
+  BIMASK_REQUIRE(type == BIMASK_TYPE_BF16 || type == BIMASK_TYPE_F32, BIMASK_EINVAL, "%s: type %d out of range 0..1", who, type);
+  return BIMASK_OK;
+}
+
+int bimask_dropout(const void* X, int type, int T, int C, const bimask_dropout_args* drop, void* Y, void* stream) {
+  int rc = check_rows("bimask_dropout", T, C);
+  if (rc != BIMASK_OK) return rc;
+  if ((rc = check_type("bimask_dropout", type)) != BIMASK_OK) return rc;
+  if ((rc = check_drop("bimask_dropout", drop)) != BIMASK_OK) return rc;
+  BIMASK_REQUIRE(X && Y, BIMASK_EINVAL, "bimask_dropout: null pointer");
+  BIMASK_REQUIRE(aligned16(X) && aligned16(Y), BIMASK_EINVAL, "bimask_dropout: pointers must be 16-byte aligned");
+  return launch_dropout(X, type, T, C, *drop, Y, (cudaStream_t)stream);
+}
+
+int bimask_ckpt_unpack_dropout(const int8_t* q, const uint8_t* s, int act, const bimask_dropout_args* drop, int T, int C, uint16_t* X,
+                               void* stream) {
+  int rc = check_rows("bimask_ckpt_unpack_dropout", T, C);
+  if (rc != BIMASK_OK) return rc;
+  if ((rc = check_act("bimask_ckpt_unpack_dropout", act)) != BIMASK_OK) return rc;
+  if ((rc = check_drop("bimask_ckpt_unpack_dropout", drop)) != BIMASK_OK) return rc;
+  BIMASK_REQUIRE(X && q && s, BIMASK_EINVAL, "bimask_ckpt_unpack_dropout: null pointer");
+  BIMASK_REQUIRE(aligned16(X) && aligned16(q) && aligned16(s), BIMASK_EINVAL, "bimask_ckpt_unpack_dropout: pointers must be 16-byte aligned");
+  return launch_ckpt_unpack(q, s, act, T, C, X, (cudaStream_t)stream, drop);
+}
+
+int bimask_act_dropout_bwd(const uint16_t* dY, const int8_t* Zq, const uint8_t* Zs, int act, const bimask_dropout_args* drop, int T, int C,
+                           uint16_t* dZ, float* dbias, void* ws, size_t ws_bytes, void* stream) {
+  int rc = check_act_bwd("bimask_act_dropout_bwd", dY, Zq, Zs, act, T, C, dZ, dbias, ws, ws_bytes);
+  if (rc != BIMASK_OK) return rc;
+  if ((rc = check_drop("bimask_act_dropout_bwd", drop)) != BIMASK_OK) return rc;
+  return launch_act_bwd(dY, Zq, Zs, act, T, C, dZ, dbias, reinterpret_cast<float*>(ws), (cudaStream_t)stream, drop);
+}
+
+size_t bimask_residual_norm_workspace_bytes(int T, int C, int gate_span) {
+  if (T <= 0 || C <= 0 || C % 32 != 0 || C > RESIDUAL_MAX_C || gate_span < 1) return 0;
+  return residual_workspace_bytes(T, C, gate_span);
+}
+
+// What both directions ask of the arguments.  branch: there is a y, or the gradient of one is wanted.
+static int check_residual(const char* who, const bimask_residual_args* a, bool branch) {
+  int rc = check_rows(who, a->T, a->C);
+  if (rc != BIMASK_OK) return rc;
+  BIMASK_REQUIRE(a->C <= RESIDUAL_MAX_C, BIMASK_EUNSUPPORTED, "%s: C = %d: rows of at most %d columns are implemented", who, a->C, RESIDUAL_MAX_C);
+  if ((rc = check_type(who, a->stream_type)) != BIMASK_OK) return rc;
+  BIMASK_REQUIRE(a->post >= BIMASK_NORM_NONE && a->post <= BIMASK_NORM_LAYER && a->pre >= BIMASK_NORM_NONE && a->pre <= BIMASK_NORM_LAYER,
+                 BIMASK_EINVAL, "%s: norm %d / %d out of range 0..2", who, a->post, a->pre);
+  BIMASK_REQUIRE((a->post == BIMASK_NORM_NONE || (a->eps_post >= 0.f && isfinite(a->eps_post))) &&
+                     (a->pre == BIMASK_NORM_NONE || (a->eps_pre >= 0.f && isfinite(a->eps_pre))),
+                 BIMASK_EINVAL, "%s: eps must be finite and not negative", who);
+  BIMASK_REQUIRE(isfinite(a->alpha), BIMASK_EINVAL, "%s: alpha must be finite", who);
+  if ((rc = check_drop(who, &a->drop)) != BIMASK_OK) return rc;
+  BIMASK_REQUIRE(branch || (a->post == BIMASK_NORM_NONE && !a->gate && !a->scale && a->drop.p == 0.f), BIMASK_EINVAL,
+                 "%s: a norm after, a gate, a scale or dropout without a branch y", who);
+  BIMASK_REQUIRE((a->post != BIMASK_NORM_NONE || (!a->w_post && !a->b_post)) && (a->pre != BIMASK_NORM_NONE || (!a->w_pre && !a->b_pre)),
+                 BIMASK_EINVAL, "%s: weights or biases without their norm", who);
+  BIMASK_REQUIRE(!a->gate || a->gate_span >= 1, BIMASK_EINVAL, "%s: gate_span = %d: a gate needs at least 1", who, a->gate_span);
+  BIMASK_REQUIRE(!a->gate || (a->gate_pitch >= a->C && a->gate_pitch % 8 == 0), BIMASK_EINVAL,
+                 "%s: gate_pitch = %lld: a multiple of 8, at least C", who, (long long)a->gate_pitch);
+  const void* all[] = {a->x, a->y, a->gate, a->scale, a->w_post, a->b_post, a->w_pre, a->b_pre, a->xo, a->n, a->stats_post, a->stats_pre,
+                       a->dxo, a->dn, a->dx, a->dy, a->dgate, a->dscale, a->dw_post, a->db_post, a->dw_pre, a->db_pre, a->ws};
+  for (const void* p : all) BIMASK_REQUIRE(aligned16(p), BIMASK_EINVAL, "%s: pointers must be 16-byte aligned", who);
+  return BIMASK_OK;
+}
+
+int bimask_residual_norm_fwd(const bimask_residual_args* a, void* stream) {
+  BIMASK_REQUIRE(a != nullptr, BIMASK_EINVAL, "bimask_residual_norm_fwd: null argument struct");
+  const int rc = check_residual("bimask_residual_norm_fwd", a, a->y != nullptr);
+  if (rc != BIMASK_OK) return rc;
+  const bool pre = a->pre != BIMASK_NORM_NONE;
+  BIMASK_REQUIRE(a->x && (a->xo || pre) && (a->n || !pre), BIMASK_EINVAL, "bimask_residual_norm_fwd: null pointer (x, xo or n)");
+  return launch_residual_fwd(*a, (cudaStream_t)stream);
+}
+
+int bimask_residual_norm_bwd(const bimask_residual_args* a, void* stream) {
+  BIMASK_REQUIRE(a != nullptr, BIMASK_EINVAL, "bimask_residual_norm_bwd: null argument struct");
+  const char* who = "bimask_residual_norm_bwd";
+  const bool branch = a->dy || a->dgate || a->dscale || a->dw_post || a->db_post;
+  const int rc = check_residual(who, a, branch || a->y);
+  if (rc != BIMASK_OK) return rc;
+  const bool pre = a->pre != BIMASK_NORM_NONE, post = a->post != BIMASK_NORM_NONE;
+  BIMASK_REQUIRE(branch || a->dx || a->dw_pre || a->db_pre, BIMASK_EINVAL, "%s: null pointer (no gradient asked for)", who);
+  BIMASK_REQUIRE(pre ? a->dn && a->xo && a->stats_pre : a->dxo != nullptr, BIMASK_EINVAL,
+                 "%s: null pointer (dn, xo and stats_pre with a norm before, dxo without)", who);
+  BIMASK_REQUIRE(pre || (!a->dw_pre && !a->db_pre), BIMASK_EINVAL, "%s: gradients of the norm before, which is absent", who);
+  BIMASK_REQUIRE(post || (!a->dw_post && !a->db_post), BIMASK_EINVAL, "%s: gradients of the norm after, which is absent", who);
+  BIMASK_REQUIRE(!a->dgate || a->gate, BIMASK_EINVAL, "%s: the gradient of a gate needs the gate", who);
+  BIMASK_REQUIRE(!branch || a->y || !(post || a->dgate || a->dscale), BIMASK_EINVAL,
+                 "%s: null pointer (y is needed with a norm after, dgate or dscale)", who);
+  BIMASK_REQUIRE(!branch || !post || a->stats_post, BIMASK_EINVAL, "%s: null pointer (stats_post)", who);
+  const bool spanned = a->dgate && a->gate_span > 1;
+  if (spanned || a->dscale || a->dw_post || a->db_post || a->dw_pre || a->db_pre) {
+    const size_t need = residual_workspace_bytes(a->T, a->C, spanned ? a->gate_span : 1);
+    BIMASK_REQUIRE(a->ws && a->ws_bytes >= need, BIMASK_EINVAL, "%s: workspace too small (%zu bytes, need %zu)", who, a->ws ? a->ws_bytes : 0, need);
+  }
+  return launch_residual_bwd(*a, (cudaStream_t)stream);
 }
 
 int bimask_wgrad_ckpt(const uint16_t* dY, const int8_t* Xq, const uint8_t* Xs, int T, int I, int J, float* dW, void* ws,

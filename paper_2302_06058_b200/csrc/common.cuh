@@ -5,6 +5,7 @@
 #include <stdint.h>
 #include <stdio.h>
 #include <stdarg.h>
+#include <math.h>
 #include <atomic>
 #include "../../include/bimask.h"
 
@@ -271,10 +272,21 @@ int linear_kernel_choice(bool sparse, int Mdim, int Ndim, int Kdim);
 // 8-bit checkpoints and the gradient of the epilogue (linear_kernels.cu).  partial: act_bwd_partial_bytes(T, C), used
 // when dbias is wanted.
 int launch_ckpt_pack(const uint16_t* x, int T, int C, int8_t* q, uint8_t* s, cudaStream_t st);
-int launch_ckpt_unpack(const int8_t* q, const uint8_t* s, int act, int T, int C, uint16_t* x, cudaStream_t st);
+int launch_ckpt_unpack(const int8_t* q, const uint8_t* s, int act, int T, int C, uint16_t* x, cudaStream_t st,
+                       const bimask_dropout_args* drop = nullptr);
 size_t act_bwd_partial_bytes(int T, int C);
 int launch_act_bwd(const uint16_t* dY, const int8_t* zq, const uint8_t* zs, int act, int T, int C, uint16_t* dZ, float* dbias,
-                   float* partial, cudaStream_t st);
+                   float* partial, cudaStream_t st, const bimask_dropout_args* drop = nullptr);
+// Dropout and the residual junction (residual_kernels.cu).  Kept iff 16 random bits are at least the threshold.
+inline uint32_t drop_threshold(float p) {
+  const long t = lrint(65536.0 * (double)p);
+  return t > 65535 ? 65535u : (uint32_t)t;
+}
+int launch_dropout(const void* x, int type, int T, int C, const bimask_dropout_args& d, void* y, cudaStream_t s);
+constexpr int RESIDUAL_MAX_C = 8192;                      // 16 warps of 16 columns per thread
+size_t residual_workspace_bytes(int T, int C, int span);
+int launch_residual_fwd(const bimask_residual_args& a, cudaStream_t s);
+int launch_residual_bwd(const bimask_residual_args& a, cudaStream_t s);
 // Weight gradient whose token operand is a checkpoint; ws: wgrad_ckpt_bytes(T, I, J).  wgrad_ckpt_query_bytes: enough for T and
 // every smaller number of tokens; wgrad_most_splits: the same for the partial sums of launch_wgrad_impl.
 size_t wgrad_ckpt_bytes(int T, int I, int J);

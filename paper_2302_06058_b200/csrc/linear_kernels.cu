@@ -1,6 +1,6 @@
 // The streaming kernels around a linear layer: 8-bit activation checkpoints written and read, and the gradient through
 // the activation and the bias.  All three are bound by HBM.
-#include "act_math.cuh"
+#include "dropout.cuh"
 
 namespace bimask {
 
@@ -47,12 +47,14 @@ ckpt_pack_kernel(const uint4* __restrict__ x, long long halves, uint4* __restric
 
 // The values of a checkpoint, through an activation or as they are.  Eight channels per thread and step, so that the 16-byte
 // stores of a warp are contiguous (16 channels as two stores of every other 16 bytes: 84 us for 8192 x 16384 through
-// an activation, now 76: 5.3 TB/s); two steps' bytes are loaded at a time.
-template <int ACT>
+// an activation, now 76: 5.3 TB/s); two steps' bytes are loaded at a time.  DROP: dropout of the result; its blocks of eight
+// are the threads'.
+template <int ACT, bool DROP>
 __global__ void __launch_bounds__(STREAM_THREADS)
-ckpt_unpack_kernel(const uint2* __restrict__ q, const uint8_t* __restrict__ s, long long eighths, uint4* __restrict__ x) {
+ckpt_unpack_kernel(const uint2* __restrict__ q, const uint8_t* __restrict__ s, long long eighths, uint4* __restrict__ x, const DropParams d) {
   pdl_launch_dependents();
   pdl_wait();
+  const DropKey key = DROP ? drop_key(d) : DropKey{};
   constexpr int U = 2;
   const long long step = (long long)gridDim.x * STREAM_THREADS;
   for (long long i0 = (long long)blockIdx.x * STREAM_THREADS + threadIdx.x; i0 < eighths; i0 += U * step) {
@@ -70,8 +72,10 @@ ckpt_unpack_kernel(const uint2* __restrict__ q, const uint8_t* __restrict__ s, l
         const act::Pair sc = act::both(ckpt::scale_value(sb[u]));
         act::Pair z[4];
         ckpt::decode4(v[u].x, sc, z); ckpt::decode4(v[u].y, sc, z + 2);
-        x[i] = make_uint4(pack_bf16_p(act::value2<ACT>(z[0])), pack_bf16_p(act::value2<ACT>(z[1])), pack_bf16_p(act::value2<ACT>(z[2])),
-                          pack_bf16_p(act::value2<ACT>(z[3])));
+#pragma unroll
+        for (int k = 0; k < 4; ++k) z[k] = act::value2<ACT>(z[k]);
+        if constexpr (DROP) drop8(z, (unsigned long long)i, key, d.thr, d.scale);
+        x[i] = make_uint4(pack_bf16_p(z[0]), pack_bf16_p(z[1]), pack_bf16_p(z[2]), pack_bf16_p(z[3]));
       }
     }
   }
@@ -84,16 +88,18 @@ ckpt_unpack_kernel(const uint2* __restrict__ q, const uint8_t* __restrict__ s, l
 // by side are added through shared memory at its end, in a fixed order, and each CTA leaves one row of partial sums for
 // bias_reduce_kernel (no atomics: the result does not depend on timing).  8192 x 16384 in 127 us on the device, 5.3 TB/s
 // (the bias gradient alone 47 us); 12608 x 1536 in 22 + 3 us: there the launches and the uneven end of the CTAs are a
-// third.  CTA (x, y): column tile x of 2 * half groups of eight, row slot y of gridDim.y.
+// third.  CTA (x, y): column tile x of 2 * half groups of eight, row slot y of gridDim.y.  DROP: dY is first dropped; its
+// blocks of eight are the threads' groups.
 // ------------------------------------------------------------------------------------------
 constexpr int ACTBWD_MAX_THREADS = 512;
 
-template <int ACT>
+template <int ACT, bool DROP>
 __global__ void __launch_bounds__(ACTBWD_MAX_THREADS, 1)
 act_bwd_kernel(const uint4* dY, const uint2* __restrict__ zq, const uint8_t* __restrict__ zs, int T, int C8, int half, int rows,
-               uint4* dZ /* may be dY */, float4* __restrict__ partial) {
+               uint4* dZ /* may be dY */, float4* __restrict__ partial, const DropParams drop) {
   pdl_launch_dependents();
   pdl_wait();
+  const DropKey key = DROP ? drop_key(drop) : DropKey{};
   __shared__ float red[ACTBWD_MAX_THREADS][17];           // 17: neighbouring threads fall into different banks
   const int g = threadIdx.x / half, lc = threadIdx.x - g * half;
   const int ca = blockIdx.x * 2 * half + lc, cb = ca + half;
@@ -136,6 +142,15 @@ act_bwd_kernel(const uint4* dY, const uint2* __restrict__ zq, const uint8_t* __r
           }
         }
         fetch(u, t + U * stride);
+        if constexpr (DROP) {
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            act::Pair w[4] = {v[4 * h], v[4 * h + 1], v[4 * h + 2], v[4 * h + 3]};
+            drop8(w, (unsigned long long)(t * C8 + ca + (h != 0 ? half : 0)), key, drop.thr, drop.scale);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) v[4 * h + k] = w[k];
+          }
+        }
         if constexpr (ACT != BIMASK_ACT_NONE) {
 #pragma unroll
           for (int k = 0; k < 8; ++k) v[k] = act::mul2(v[k], act::slope2<ACT>(a[k]));
@@ -244,20 +259,23 @@ int launch_ckpt_pack(const uint16_t* x, int T, int C, int8_t* q, uint8_t* s, cud
   return BIMASK_OK;
 }
 
-int launch_ckpt_unpack(const int8_t* q, const uint8_t* s, int act, int T, int C, uint16_t* x, cudaStream_t st) {
+int launch_ckpt_unpack(const int8_t* q, const uint8_t* s, int act, int T, int C, uint16_t* x, cudaStream_t st, const bimask_dropout_args* drop) {
   const long long eighths = (long long)T * (C / 8);
+  const DropParams d = drop_params(drop);
   auto run = [&](auto kern) {
     return launch_pdl(kern, stream_grid(eighths), STREAM_THREADS, 0, st, reinterpret_cast<const uint2*>(q), s, eighths,
-                      reinterpret_cast<uint4*>(x));
+                      reinterpret_cast<uint4*>(x), d);
   };
   cudaError_t e;
+#define BIMASK_RUN(ACT) (d.thr != 0u ? run(ckpt_unpack_kernel<ACT, true>) : run(ckpt_unpack_kernel<ACT, false>))
   switch (act) {
-    case BIMASK_ACT_RELU: e = run(ckpt_unpack_kernel<BIMASK_ACT_RELU>); break;
-    case BIMASK_ACT_GELU: e = run(ckpt_unpack_kernel<BIMASK_ACT_GELU>); break;
-    case BIMASK_ACT_GELU_TANH: e = run(ckpt_unpack_kernel<BIMASK_ACT_GELU_TANH>); break;
-    case BIMASK_ACT_SILU: e = run(ckpt_unpack_kernel<BIMASK_ACT_SILU>); break;
-    default: e = run(ckpt_unpack_kernel<BIMASK_ACT_NONE>); break;
+    case BIMASK_ACT_RELU: e = BIMASK_RUN(BIMASK_ACT_RELU); break;
+    case BIMASK_ACT_GELU: e = BIMASK_RUN(BIMASK_ACT_GELU); break;
+    case BIMASK_ACT_GELU_TANH: e = BIMASK_RUN(BIMASK_ACT_GELU_TANH); break;
+    case BIMASK_ACT_SILU: e = BIMASK_RUN(BIMASK_ACT_SILU); break;
+    default: e = BIMASK_RUN(BIMASK_ACT_NONE); break;
   }
+#undef BIMASK_RUN
   BIMASK_CUDA_OK(e);
   count_launch();
   BIMASK_CUDA_OK(cudaGetLastError());
@@ -265,21 +283,24 @@ int launch_ckpt_unpack(const int8_t* q, const uint8_t* s, int act, int T, int C,
 }
 
 int launch_act_bwd(const uint16_t* dY, const int8_t* zq, const uint8_t* zs, int act, int T, int C, uint16_t* dZ, float* dbias,
-                   float* partial, cudaStream_t st) {
+                   float* partial, cudaStream_t st, const bimask_dropout_args* drop) {
   const ActBwdPlan p = plan_act_bwd(T, C);
+  const DropParams d = drop_params(drop);
   float* part = dbias == nullptr ? nullptr : p.slots == 1 ? dbias : partial;      // one slot: its row is the result
   auto run = [&](auto kern) {
     return launch_pdl(kern, dim3(p.tiles, p.slots), p.threads, 0, st, reinterpret_cast<const uint4*>(dY), reinterpret_cast<const uint2*>(zq),
-                      zs, T, C / 8, p.half, p.rows, reinterpret_cast<uint4*>(dZ), reinterpret_cast<float4*>(part));
+                      zs, T, C / 8, p.half, p.rows, reinterpret_cast<uint4*>(dZ), reinterpret_cast<float4*>(part), d);
   };
   cudaError_t e;
+#define BIMASK_RUN(ACT) (d.thr != 0u ? run(act_bwd_kernel<ACT, true>) : run(act_bwd_kernel<ACT, false>))
   switch (act) {
-    case BIMASK_ACT_RELU: e = run(act_bwd_kernel<BIMASK_ACT_RELU>); break;
-    case BIMASK_ACT_GELU: e = run(act_bwd_kernel<BIMASK_ACT_GELU>); break;
-    case BIMASK_ACT_GELU_TANH: e = run(act_bwd_kernel<BIMASK_ACT_GELU_TANH>); break;
-    case BIMASK_ACT_SILU: e = run(act_bwd_kernel<BIMASK_ACT_SILU>); break;
-    default: e = run(act_bwd_kernel<BIMASK_ACT_NONE>); break;
+    case BIMASK_ACT_RELU: e = BIMASK_RUN(BIMASK_ACT_RELU); break;
+    case BIMASK_ACT_GELU: e = BIMASK_RUN(BIMASK_ACT_GELU); break;
+    case BIMASK_ACT_GELU_TANH: e = BIMASK_RUN(BIMASK_ACT_GELU_TANH); break;
+    case BIMASK_ACT_SILU: e = BIMASK_RUN(BIMASK_ACT_SILU); break;
+    default: e = BIMASK_RUN(BIMASK_ACT_NONE); break;
   }
+#undef BIMASK_RUN
   BIMASK_CUDA_OK(e);
   count_launch();
   if (dbias != nullptr && p.slots > 1) {
