@@ -279,7 +279,7 @@ int bimask_act_dropout_bwd(const uint16_t* dY, const int8_t* Zq, const uint8_t* 
  * All arithmetic is fp32, results are rounded once; n is taken from x' before its rounding.  Squares are fp32: a row with
  * magnitudes above 1e18 may overflow them.
  *
- * Sizes: C % 32 == 0, C <= 8192 (BIMASK_EUNSUPPORTED above), any T.  T x C matrices of the stream (x, xo, dx, dxo) have
+ * Sizes: C % 32 == 0, C <= 16384 (BIMASK_EUNSUPPORTED above), any T.  T x C matrices of the stream (x, xo, dx, dxo) have
  * stream_type; y, n, gate and their gradients are bf16; C-vectors are fp32.  stats: T x 2 fp32 (mean, rstd; mean 0 for RMS),
  * what the backward pass needs of a norm.
  * gate: row t / gate_span serves token t; 1: one row per token, the tokens of a sample: one row per sample.  Rows are gate_pitch

@@ -283,7 +283,7 @@ inline uint32_t drop_threshold(float p) {
   return t > 65535 ? 65535u : (uint32_t)t;
 }
 int launch_dropout(const void* x, int type, int T, int C, const bimask_dropout_args& d, void* y, cudaStream_t s);
-constexpr int RESIDUAL_MAX_C = 8192;                      // 16 warps of 16 columns per thread
+constexpr int RESIDUAL_MAX_C = 16384;                     // 16 warps of eight columns per thread, in each of four CTAs
 size_t residual_workspace_bytes(int T, int C, int span);
 int launch_residual_fwd(const bimask_residual_args& a, cudaStream_t s);
 int launch_residual_bwd(const bimask_residual_args& a, cudaStream_t s);

@@ -54,7 +54,7 @@ __global__ void __launch_bounds__(STREAM_THREADS)
 ckpt_unpack_kernel(const uint2* __restrict__ q, const uint8_t* __restrict__ s, long long eighths, uint4* __restrict__ x, const DropParams d) {
   pdl_launch_dependents();
   pdl_wait();
-  const DropKey key = DROP ? drop_key(d) : DropKey{};
+  const unsigned long long number = DROP ? drop_number(d) : 0ull;
   constexpr int U = 2;
   const long long step = (long long)gridDim.x * STREAM_THREADS;
   for (long long i0 = (long long)blockIdx.x * STREAM_THREADS + threadIdx.x; i0 < eighths; i0 += U * step) {
@@ -74,7 +74,7 @@ ckpt_unpack_kernel(const uint2* __restrict__ q, const uint8_t* __restrict__ s, l
         ckpt::decode4(v[u].x, sc, z); ckpt::decode4(v[u].y, sc, z + 2);
 #pragma unroll
         for (int k = 0; k < 4; ++k) z[k] = act::value2<ACT>(z[k]);
-        if constexpr (DROP) drop8(z, (unsigned long long)i, key, d.thr, d.scale);
+        if constexpr (DROP) drop8(z, (unsigned long long)i, number, d);
         x[i] = make_uint4(pack_bf16_p(z[0]), pack_bf16_p(z[1]), pack_bf16_p(z[2]), pack_bf16_p(z[3]));
       }
     }
@@ -99,7 +99,7 @@ act_bwd_kernel(const uint4* dY, const uint2* __restrict__ zq, const uint8_t* __r
                uint4* dZ /* may be dY */, float4* __restrict__ partial, const DropParams drop) {
   pdl_launch_dependents();
   pdl_wait();
-  const DropKey key = DROP ? drop_key(drop) : DropKey{};
+  const unsigned long long number = DROP ? drop_number(drop) : 0ull;
   __shared__ float red[ACTBWD_MAX_THREADS][17];           // 17: neighbouring threads fall into different banks
   const int g = threadIdx.x / half, lc = threadIdx.x - g * half;
   const int ca = blockIdx.x * 2 * half + lc, cb = ca + half;
@@ -146,7 +146,7 @@ act_bwd_kernel(const uint4* dY, const uint2* __restrict__ zq, const uint8_t* __r
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
             act::Pair w[4] = {v[4 * h], v[4 * h + 1], v[4 * h + 2], v[4 * h + 3]};
-            drop8(w, (unsigned long long)(t * C8 + ca + (h != 0 ? half : 0)), key, drop.thr, drop.scale);
+            drop8(w, (unsigned long long)(t * C8 + ca + (h != 0 ? half : 0)), number, drop);
 #pragma unroll
             for (int k = 0; k < 4; ++k) v[4 * h + k] = w[k];
           }

@@ -2,6 +2,7 @@
 // next block), its gradient, and dropout alone.  All of them stream: every matrix is read once and written once, a row stays
 // in the registers of the warps that share it, and the statistics are exchanged by shuffles and one barrier per norm.
 #include "dropout.cuh"
+#include "sm100_ptx.cuh"
 #include <type_traits>
 
 namespace bimask {
@@ -67,7 +68,7 @@ __global__ void __launch_bounds__(DROP_THREADS)
 dropout_kernel(const void* x, long long blocks, void* y /* may be x */, const DropParams d) {
   pdl_launch_dependents();
   pdl_wait();
-  const DropKey key = drop_key(d);
+  const unsigned long long number = drop_number(d);
   constexpr int U = 2;
   const long long step = (long long)gridDim.x * DROP_THREADS;
   for (long long i0 = (long long)blockIdx.x * DROP_THREADS + threadIdx.x; i0 < blocks; i0 += U * step) {
@@ -81,7 +82,7 @@ dropout_kernel(const void* x, long long blocks, void* y /* may be x */, const Dr
       if (i < blocks) {
         Pair p[4];
         unpack8<F32>(v[u], p);
-        if (d.thr != 0u) drop8(p, (unsigned long long)i, key, d.thr, d.scale);
+        if (d.thr != 0u) drop8(p, (unsigned long long)i, number, d);
         store8<F32>(y, i, p);
       }
     }
@@ -89,14 +90,27 @@ dropout_kernel(const void* x, long long blocks, void* y /* may be x */, const Dr
 }
 
 // ------------------------------------------------------------------------------------------
-// Rows.  W warps share a row; thread l of the 32 W takes blocks l, l + 32 W, ... (V of them) of eight columns.  G such
-// groups in a CTA work on rows of their own and never meet (named barriers).
+// Rows.  A thread owns one block of eight columns for good; `warps` warps of a CTA, and up to four CTAs of a cluster above 4096
+// columns, share a row.  A CTA holds as many such groups as its 16 warps give; they work on rows of their own and never meet (named
+// barriers).  A group takes two rows per step: what its threads exchange for both travels together, and the two rows' chains
+// of dependent instructions run side by side.  The rows of the next step are already on their way: every thread copies its own
+// 16-byte pieces into its own places in shared memory (cp.async), so no barrier guards them, no registers wait for them, and
+// whoever writes a row in place has its old values safely fetched.
+// What bounds these kernels next to HBM is the instructions they issue, so the rows' code has no branches but those of absent
+// parts: columns and rows past the end are copied as zeros (from a clamped address, of which cp.async reads nothing) and work like
+// the others, but for their stores.
 // ------------------------------------------------------------------------------------------
+constexpr int ROWS = 2, STAGES = 2;
+constexpr int ROW_THREADS = 512;
+constexpr int MAX_ROW_WARPS = 64;                         // of a cluster of four CTAs
+static_assert(RESIDUAL_MAX_C == 256 * MAX_ROW_WARPS, "eight columns per thread");
+
 struct ResidualParams {
-  int T, C8, warps;                  // warps per row
+  uint32_t T, C8;
+  int warps, cluster;                // warps per row in a CTA, CTAs per row
   int post, pre;
   float eps_post, eps_pre, alpha, inv_c;
-  int gate_span;                     // 0: no gate
+  uint32_t gate_span;                // 0: no gate
   long long gate_pitch8;
   DropParams drop;
   const void* x;
@@ -117,214 +131,431 @@ struct ResidualParams {
   void* dx;
   uint4* dy;
   uint4* dgate;
-  float* sums;                       // [CTAs][wanted arrays][C]
+  float* sums;                       // [clusters][wanted arrays][C]
   float* gate_sums;                  // [units][C]
   int want;                          // bits: SUM_* arrays that are wanted
   int branch;                        // a gradient of the branch is wanted
-  int unit_rows, units_per_span;     // rows that a group takes at a time, such units in a gate row's span
+  // Rows are given out in units of consecutive ones.  units_per_span: 0, or the units that a gate row's span is cut into.
+  uint32_t units, unit_rows, units_per_span;
 };
 
-__device__ __forceinline__ void group_sync(int group, int warps) {
-  if (warps > 1) asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "r"(32 * warps) : "memory");
+__device__ __forceinline__ uint32_t smem_addr(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+// 16 bytes, or as many zeros
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool live) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(live ? 16 : 0) : "memory");
 }
-__device__ __forceinline__ float warp_sum(float v) {
-#pragma unroll
-  for (int d = 16; d >= 1; d >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, d);
+__device__ __forceinline__ void copy8(uint32_t dst, const void* src, bool live) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(dst), "l"(src), "r"(live ? 8 : 0) : "memory");
+}
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int PENDING>
+__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(PENDING) : "memory"); }
+__device__ __forceinline__ float2 read_pair(uint32_t at) {
+  float2 v;
+  asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(at) : "memory");
   return v;
 }
-__device__ __forceinline__ float sum16(float v) {         // over the lanes' low four bits
-#pragma unroll
-  for (int d = 8; d >= 1; d >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, d);
+__device__ __forceinline__ float read_word(uint32_t at) {
+  float v;
+  asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(at) : "memory");
   return v;
 }
+
 __device__ __forceinline__ float horizontal(Pair v) {
   float a, b;
   act::split(v, a, b);
   return a + b;
 }
-
-// eight fp32 parameters of block c, or a constant
-__device__ __forceinline__ void param8(const float* base, int c, float otherwise, Pair (&p)[4]) {
-  if (base != nullptr) {
-    const float4 a = __ldg(reinterpret_cast<const float4*>(base) + 2 * c), b = __ldg(reinterpret_cast<const float4*>(base) + 2 * c + 1);
-    p[0] = act::pair(a.x, a.y); p[1] = act::pair(a.z, a.w); p[2] = act::pair(b.x, b.y); p[3] = act::pair(b.z, b.w);
-  } else {
-#pragma unroll
-    for (int k = 0; k < 4; ++k) p[k] = act::both(otherwise);
-  }
+__device__ __forceinline__ Pair sum8(const Pair (&v)[4]) { return act::add2(act::add2(v[0], v[1]), act::add2(v[2], v[3])); }
+__device__ __forceinline__ Pair dot8(const Pair (&v)[4], const Pair (&w)[4]) {
+  return act::add2(act::fma2(v[1], w[1], act::mul2(v[0], w[0])), act::fma2(v[3], w[3], act::mul2(v[2], w[2])));
 }
 
-struct Row {                                              // a thread's place in its row
-  int lane, warp, group, warps, turn;
-  float inv_count;                                        // 1 / columns of the row that this warp holds
-  float peer_count;                                       // columns that warp lane % 16 of the group holds
-  float2* red;                                            // the group's [2][16]
+// eight fp32 parameters of block c
+__device__ __forceinline__ void param8(const float* base, uint32_t c, Pair (&p)[4]) {
+  const float4 a = __ldg(reinterpret_cast<const float4*>(base) + 2 * c), b = __ldg(reinterpret_cast<const float4*>(base) + 2 * c + 1);
+  p[0] = act::pair(a.x, a.y); p[1] = act::pair(a.z, a.w); p[2] = act::pair(b.x, b.y); p[3] = act::pair(b.z, b.w);
+}
+__device__ __forceinline__ void times8(Pair (&v)[4], const Pair (&w)[4]) {
+#pragma unroll
+  for (int k = 0; k < 4; ++k) v[k] = act::mul2(v[k], w[k]);
+}
+__device__ __forceinline__ void plus8(Pair (&v)[4], const Pair (&w)[4]) {
+#pragma unroll
+  for (int k = 0; k < 4; ++k) v[k] = act::add2(v[k], w[k]);
+}
+__device__ __forceinline__ void fill8(Pair (&v)[4], float x) {
+#pragma unroll
+  for (int k = 0; k < 4; ++k) v[k] = act::both(x);
+}
+// (v - mean) rstd, as one multiplication and addition: off by a rounding of (|v| + |mean|) rstd, like the difference first
+__device__ __forceinline__ void normalise(Pair (&v)[4], float2 st) {
+  const Pair rstd = act::both(st.y), shift = act::both(-st.x * st.y);
+#pragma unroll
+  for (int k = 0; k < 4; ++k) v[k] = act::fma2(v[k], rstd, shift);
+}
+
+// columns that a row's warp w holds
+__device__ __forceinline__ float columns_of(int w, uint32_t C8) { return 8.f * (float)min(max((int)C8 - 32 * w, 0), 32); }
+
+// Exchange buffers: a group's two, of four values from each of its row's warps, their number made even (zero where there is no
+// such warp).  Groups of two warps or more: three words for two warps at worst.
+template <bool CLUSTER>
+struct Exchange {
+  static constexpr int WORDS = CLUSTER ? MAX_ROW_WARPS : ROW_THREADS / 64 * 3;
+  static constexpr int BYTES = 2 * 4 * WORDS * 4;
+};
+template <bool CLUSTER>
+struct Group {                                            // a thread's place among those that share its rows
+  int lane, group, warps;                                 // warps: of the row in this CTA
+  int warp;                                               // the thread's warp, counted through the row
+  bool alone;                                             // the row is one warp's
+  int cluster;
+  float inv_columns;                                      // 1 / columns that this warp holds
+  float peer_columns;                                     // columns of warp lane % 16 (only without clusters)
+  uint32_t mine, buffer;                                  // address of this warp's first word, and of the buffer in use
+  uint32_t flip;
+  int width;                                              // words of a value
+
+  __device__ __forceinline__ Group(const ResidualParams& p, uint32_t exchange) {
+    const int w = threadIdx.x >> 5;
+    lane = threadIdx.x & 31;
+    warps = p.warps;
+    group = w / warps;
+    cluster = p.cluster;
+    warp = w - group * warps + (CLUSTER ? (int)ptx::cluster_ctarank() * warps : 0);
+    alone = !CLUSTER && warps == 1;
+    inv_columns = 1.f / fmaxf(columns_of(warp, p.C8), 1.f);
+    peer_columns = columns_of(lane & 15, p.C8);
+    width = CLUSTER ? MAX_ROW_WARPS : warps + (warps & 1);
+    buffer = exchange + (uint32_t)((alone ? 0 : group) * 2 * 4 * width * 4);
+    mine = 4u * (uint32_t)warp;
+    flip = buffer ^ (buffer + 4u * (uint32_t)width * 4u);
+  }
+  // Value i of this warp, to every CTA that shares the row ...
+  __device__ __forceinline__ void publish(int i, float v) const {
+    const uint32_t at = buffer + mine + (uint32_t)(i * width * 4);
+    if (!CLUSTER) asm volatile("st.shared.f32 [%0], %1;" ::"r"(at), "f"(v) : "memory");
+    else
+      for (int r = 0; r < cluster; ++r) ptx::st_cluster_u32(ptx::mapa(at, (uint32_t)r), __float_as_uint(v));
+  }
+  __device__ __forceinline__ void meet() const {
+    if (CLUSTER) ptx::cluster_sync();
+    else ptx::named_bar_sync(group + 1, 32 * warps);
+  }
+  // ... and all warps' values, after they have met.  Two buffers in turn: who writes one has met the others over the other one, and
+  // by then everybody had read this one.
+  __device__ __forceinline__ uint32_t published(int i, int w) const { return buffer + (uint32_t)((i * width + w) * 4); }
+  __device__ __forceinline__ void turn() { buffer ^= flip; }
 };
 
-__device__ __forceinline__ float columns_of_warp(int warp, int warps, int V, int C8) {
-  int n = 0;
-  for (int j = 0; j < V; ++j) n += min(max(C8 - 32 * (warp + j * warps), 0), 32);
-  return 8.f * (float)n;
+// Sums over a warp of two or four values at a time: at each step a lane keeps half of its values and hands the others to its
+// partner.  The total of value i ends in the lanes 16 i .. or 8 i ..
+__device__ __forceinline__ float fold2(float a, float b, int lane) {
+  const bool hi = (lane & 16) != 0;
+  float v = (hi ? b : a) + __shfl_xor_sync(0xFFFFFFFFu, hi ? a : b, 16);
+#pragma unroll
+  for (int d = 8; d >= 1; d >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, d);
+  return v;
+}
+__device__ __forceinline__ float fold4(const float (&c)[4], int lane) {
+  const bool hi = (lane & 16) != 0, mid = (lane & 8) != 0;
+  const float k0 = (hi ? c[2] : c[0]) + __shfl_xor_sync(0xFFFFFFFFu, hi ? c[0] : c[2], 16);
+  const float k1 = (hi ? c[3] : c[1]) + __shfl_xor_sync(0xFFFFFFFFu, hi ? c[1] : c[3], 16);
+  float v = (mid ? k1 : k0) + __shfl_xor_sync(0xFFFFFFFFu, mid ? k0 : k1, 8);
+#pragma unroll
+  for (int d = 4; d >= 1; d >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, d);
+  return v;
 }
 
-__device__ __forceinline__ Row make_row(int warps, int V, int C8, float2* red) {
-  Row r;
-  const int w = threadIdx.x >> 5;
-  r.lane = threadIdx.x & 31;
-  r.group = w / warps;
-  r.warp = w - r.group * warps;
-  r.warps = warps;
-  r.turn = 0;
-  r.inv_count = 1.f / fmaxf(columns_of_warp(r.warp, warps, V, C8), 1.f);
-  r.peer_count = (r.lane & 15) < warps ? columns_of_warp(r.lane & 15, warps, V, C8) : 0.f;
-  r.red = red + 32 * r.group;
-  return r;
+// Totals over the row of four values; `folded`: fold4 of the thread's.  Split in two, so that other work can be done in between.
+template <bool CLUSTER>
+__device__ __forceinline__ void totals_begin(const Group<CLUSTER>& g, float folded) {
+  if (!g.alone && (g.lane & 7) == 0) g.publish(g.lane >> 3, folded);
 }
-
-// Every warp of the group hands in a pair; lane i of each warp gets warp i % 16's (zero past the last).  Two buffers in
-// turn: a warp that writes one has passed the barrier of the other, before which everybody had read this one.
-__device__ __forceinline__ float2 exchange(Row& r, float2 mine) {
-  float2* buf = r.red + 16 * r.turn;
-  r.turn ^= 1;
-  if (r.lane == 0) buf[r.warp] = mine;
-  group_sync(r.group, r.warps);
-  const int i = r.lane & 15;
-  return i < r.warps ? buf[i] : make_float2(0.f, 0.f);
-}
-
-// Mean and 1 / deviation of a row.  The squares are taken about each warp's own mean, and the warps are put together by
-// M = sum M_w + sum n_w (m_w - m)^2: one exchange, and no difference of large squares.  rms: all about zero.
-template <int V>
-__device__ __forceinline__ float2 row_stats(const Pair (&v)[V][4], const bool (&ok)[V], int kind, float eps, float inv_c, Row& r) {
-  const bool layer = kind == BIMASK_NORM_LAYER;
-  float mean = 0.f;
-  if (layer) {
-    Pair a = act::both(0.f);
+template <bool CLUSTER>
+__device__ __forceinline__ void totals_end(Group<CLUSTER>& g, float folded, float (&c)[4]) {
+  if (!g.alone) {
+    g.meet();
+    folded = 0.f;
 #pragma unroll
-    for (int j = 0; j < V; ++j)
-      if (ok[j]) a = act::add2(a, act::add2(act::add2(v[j][0], v[j][1]), act::add2(v[j][2], v[j][3])));
-    mean = warp_sum(horizontal(a)) * r.inv_count;
-  }
-  Pair q = act::both(0.f);
-  const Pair shift = act::both(-mean);
-#pragma unroll
-  for (int j = 0; j < V; ++j)
-    if (ok[j])
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const Pair d = act::add2(v[j][k], shift);
-        q = act::fma2(d, d, q);
+    for (int k = 0; k < (CLUSTER ? 4 : 1); ++k) {
+      const int w = 2 * (g.lane & 7) + 16 * k;
+      if (w < g.width) {
+        const float2 v = read_pair(g.published(g.lane >> 3, w));
+        folded += v.x + v.y;
       }
-  float sq = warp_sum(horizontal(q));
-  if (r.warps > 1) {
-    const float2 e = exchange(r, make_float2(mean, sq));
-    float part = e.y;
-    if (layer) {
-      mean = sum16(r.peer_count * e.x) * inv_c;
-      const float d = e.x - mean;
-      part = fmaf(r.peer_count * d, d, part);
     }
-    sq = sum16(part);
+#pragma unroll
+    for (int d = 4; d >= 1; d >>= 1) folded += __shfl_xor_sync(0xFFFFFFFFu, folded, d);
+    g.turn();
   }
-  return make_float2(mean, 1.f / sqrtf(fmaf(sq, inv_c, eps)));
+#pragma unroll
+  for (int i = 0; i < 4; ++i) c[i] = __shfl_sync(0xFFFFFFFFu, folded, 8 * i);
 }
 
-// (v - mean) rstd w + b.  The difference first: mean * rstd could be far larger than the result.
-__device__ __forceinline__ void normalise(Pair (&v)[4], float2 st) {
-  const Pair shift = act::both(-st.x), rstd = act::both(st.y);
+// Mean and 1 / deviation of two rows.  The squares are taken about each warp's own mean, and the warps are put together by
+// M = sum M_w + sum n_w (m_w - m)^2: one exchange, and no difference of large squares.  rms: all about zero.
+template <bool CLUSTER>
+__device__ __forceinline__ void row_stats(const Pair (&v)[ROWS][4], bool ok, bool layer, float eps, float inv_c, uint32_t C8,
+                                          Group<CLUSTER>& g, float2 (&st)[ROWS]) {
+  static_assert(ROWS == 2, "two rows are folded together");
+  const int half = g.lane >> 4;                           // the row whose totals this lane holds
+  float m = 0.f, q[ROWS];
+  if (layer) {
+    m = fold2(horizontal(sum8(v[0])), horizontal(sum8(v[1])), g.lane) * g.inv_columns;
 #pragma unroll
-  for (int k = 0; k < 4; ++k) v[k] = act::mul2(act::add2(v[k], shift), rstd);
-}
-__device__ __forceinline__ void affine(Pair (&v)[4], const float* w, const float* b, int c) {
-  Pair p[4];
-  if (w != nullptr) {
-    param8(w, c, 1.f, p);
+    for (int r = 0; r < ROWS; ++r) {
+      const Pair shift = act::both(-__shfl_sync(0xFFFFFFFFu, m, 16 * r));
+      Pair d[4];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) v[k] = act::mul2(v[k], p[k]);
+      for (int k = 0; k < 4; ++k) d[k] = act::add2(v[r][k], shift);
+      q[r] = ok ? horizontal(dot8(d, d)) : 0.f;
+    }
+  } else {
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) q[r] = horizontal(dot8(v[r], v[r]));
   }
-  if (b != nullptr) {
-    param8(b, c, 0.f, p);
+  float sq = fold2(q[0], q[1], g.lane);
+  if (!g.alone) {
+    if ((g.lane & 15) == 0) {
+      if (layer) g.publish(half, m);
+      g.publish(2 + half, sq);
+    }
+    g.meet();
+    sq = 0.f;
+    if (CLUSTER) {
+      if (layer) {
+        m = 0.f;
+        for (int w = g.lane & 15; w < MAX_ROW_WARPS; w += 16) m = fmaf(columns_of(w, C8), read_word(g.published(half, w)), m);
 #pragma unroll
-    for (int k = 0; k < 4; ++k) v[k] = act::add2(v[k], p[k]);
-  }
-}
-
-constexpr int FWD_THREADS = 512;
-
-template <int V, bool F32>
-__global__ void __launch_bounds__(FWD_THREADS)
-residual_fwd_kernel(const ResidualParams p) {
-  __shared__ float2 red[16 * 32];
-  pdl_launch_dependents();
-  pdl_wait();
-  const DropKey key = drop_key(p.drop);
-  Row r = make_row(p.warps, V, p.C8, red);
-  const int groups = blockDim.x / (32 * p.warps);
-  const int l = 32 * r.warp + r.lane;
-  int col[V];
-  bool ok[V];
-#pragma unroll
-  for (int j = 0; j < V; ++j) { col[j] = l + 32 * j * p.warps; ok[j] = col[j] < p.C8; }
-  for (long long t = (long long)blockIdx.x * groups + r.group; t < p.T; t += (long long)gridDim.x * groups) {
-    const long long row = t * p.C8;
-    Vec8<F32> xv[V];
-    Vec8<false> yv[V], gv[V];
-    const long long grow = p.gate_span != 0 ? (t / p.gate_span) * p.gate_pitch8 : 0;
-#pragma unroll
-    for (int j = 0; j < V; ++j)
-      if (ok[j]) {
-        xv[j] = load8<F32>(p.x, row + col[j]);
-        if (p.y != nullptr) yv[j] = load8<false>(p.y, row + col[j]);
-        if (p.gate_span != 0) gv[j].w[0] = __ldg(p.gate + grow + col[j]);
+        for (int d = 8; d >= 1; d >>= 1) m += __shfl_xor_sync(0xFFFFFFFFu, m, d);
+        m *= inv_c;
       }
-    Pair v[V][4];
+      for (int w = g.lane & 15; w < MAX_ROW_WARPS; w += 16) {
+        sq += read_word(g.published(2 + half, w));
+        if (layer) {
+          const float d = read_word(g.published(half, w)) - m;
+          sq = fmaf(columns_of(w, C8) * d, d, sq);
+        }
+      }
+    } else {
+      const int w = min(g.lane & 15, g.width - 1);
+      sq = (g.lane & 15) < g.width ? read_word(g.published(2 + half, w)) : 0.f;
+      if (layer) {
+        const float own = read_word(g.published(half, w));
+        m = g.peer_columns * own;
+#pragma unroll
+        for (int d = 8; d >= 1; d >>= 1) m += __shfl_xor_sync(0xFFFFFFFFu, m, d);
+        m *= inv_c;
+        sq = fmaf(g.peer_columns * (own - m), own - m, sq);
+      }
+    }
+#pragma unroll
+    for (int d = 8; d >= 1; d >>= 1) sq += __shfl_xor_sync(0xFFFFFFFFu, sq, d);
+    g.turn();
+  }
+  const float rstd = rsqrtf(fmaf(sq, inv_c, eps));        // two units in the last place
+#pragma unroll
+  for (int r = 0; r < ROWS; ++r) st[r] = make_float2(layer ? __shfl_sync(0xFFFFFFFFu, m, 16 * r) : 0.f, __shfl_sync(0xFFFFFFFFu, rstd, 16 * r));
+}
+
+// A group's walk over its units, ROWS rows at a time.  SPAN: units of many rows that end with their gate row's span; else of one
+// row (all others of the step are none) or ROWS.
+template <bool SPAN>
+struct Walk {
+  uint32_t unit, t, end;
+  __device__ __forceinline__ void enter(const ResidualParams& p) {
+    if (!SPAN) {
+      t = unit * p.unit_rows;
+      end = min(t + p.unit_rows, p.T);
+    } else {
+      const uint32_t span = unit / p.units_per_span, part = unit - span * p.units_per_span;
+      t = span * p.gate_span + part * p.unit_rows;
+      end = min(min(t + p.unit_rows, (span + 1) * p.gate_span), p.T);
+    }
+  }
+  __device__ __forceinline__ bool more(const ResidualParams& p) const { return unit < p.units; }
+  __device__ __forceinline__ bool last() const { return t + ROWS >= end; }    // of the unit
+  __device__ __forceinline__ void next(const ResidualParams& p, uint32_t stride) {
+    if (!SPAN) {
+      unit += stride;
+      enter(p);
+    } else {
+      t += ROWS;
+      if (t >= end) {
+        unit += stride;
+        if (more(p)) enter(p);
+        else t = end = 0;
+      }
+    }
+  }
+};
+
+// Shared memory of a CTA: the ring of the threads' pieces, the statistics of every warp's rows, the exchange buffers.
+constexpr int PITCH = ROW_THREADS * 16;                   // from a thread's piece to its next
+constexpr int STATS_STAGE = 2 * ROWS * 8;                 // bytes of a warp's statistics: before, after
+constexpr int STATS_BYTES = STAGES * (ROW_THREADS / 32) * STATS_STAGE;
+BIMASK_HD constexpr int fwd_slots(bool f32, bool gate) { return (f32 ? 2 : 1) + 1 + (gate ? 1 : 0); }
+BIMASK_HD constexpr int bwd_slots(bool f32, bool gate) { return (f32 ? 4 : 2) + 2 + (gate ? 1 : 0); }
+BIMASK_HD constexpr int ring_bytes(int slots) { return STAGES * ROWS * slots * PITCH; }
+
+template <bool F32>
+__device__ __forceinline__ void copy_block(uint32_t dst, const void* base, unsigned long long block, bool live) {
+  const uint4* src = reinterpret_cast<const uint4*>(base) + block * (F32 ? 2 : 1);
+  copy16(dst, src, live);
+  if (F32) copy16(dst + PITCH, src + 1, live);
+}
+template <bool F32>
+__device__ __forceinline__ void read_block(uint32_t at, Pair (&v)[4]) {
+  Vec8<F32> raw;
+#pragma unroll
+  for (int h = 0; h < (F32 ? 2 : 1); ++h)
+    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(raw.w[h].x), "=r"(raw.w[h].y), "=r"(raw.w[h].z), "=r"(raw.w[h].w)
+                 : "r"(at + h * PITCH) : "memory");
+  unpack8<F32>(raw, v);
+}
+template <bool CLUSTER>
+__device__ __forceinline__ void clear_exchange(float* exchange) {
+  for (int i = threadIdx.x; i < Exchange<CLUSTER>::BYTES / 4; i += blockDim.x) exchange[i] = 0.f;
+  if (CLUSTER) ptx::cluster_sync();                       // before a peer writes here, and before this CTA writes to a peer
+  else __syncthreads();
+}
+
+template <bool F32, bool GATE, bool CLUSTER>
+__global__ void __launch_bounds__(ROW_THREADS, 2)
+residual_fwd_kernel(const __grid_constant__ ResidualParams p) {
+  extern __shared__ float4 smem[];
+  constexpr int SLOTS = fwd_slots(F32, GATE), X = 0, Y = F32 ? 2 : 1, G = Y + 1;
+  constexpr uint32_t STAGE = ROWS * SLOTS * PITCH;
+  float* exchange = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(smem) + ring_bytes(SLOTS));
+  pdl_launch_dependents();
+  clear_exchange<CLUSTER>(exchange);
+  Group<CLUSTER> g(p, smem_addr(exchange));
+  const uint32_t col = 32u * (uint32_t)g.warp + (uint32_t)g.lane, colc = min(col, p.C8 - 1u);
+  const bool ok = col < p.C8;
+  const uint32_t groups = blockDim.x / (32u * (uint32_t)p.warps);
+  const uint32_t stride = CLUSTER ? gridDim.x / (uint32_t)p.cluster : gridDim.x * groups;
+  const uint32_t ring = smem_addr(smem) + threadIdx.x * 16u;
+  Walk<false> work, ahead;
+  work.unit = CLUSTER ? blockIdx.x / (uint32_t)p.cluster : blockIdx.x * groups + (uint32_t)g.group;
+  work.enter(p);
+  ahead = work;
+  pdl_wait();
+  const unsigned long long number = drop_number(p.drop);
+  auto fetch = [&](const Walk<false>& w, uint32_t stage) {
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) {
+      const bool live = ok && w.more(p) && w.t + r < w.end;
+      const uint32_t t = min(w.t + r, p.T - 1u), at = ring + stage * STAGE + r * SLOTS * PITCH;
+      const unsigned long long block = (unsigned long long)t * p.C8 + colc;
+      copy_block<F32>(at + X * PITCH, p.x, block, live);
+      if (p.y != nullptr) copy16(at + Y * PITCH, p.y + block, live);
+      if (GATE) copy16(at + G * PITCH, p.gate + (long long)(p.gate_span == 1u ? t : t / p.gate_span) * p.gate_pitch8 + colc, live);
+    }
+    copies_commit();
+  };
+  fetch(ahead, 0);
+  uint32_t stage = 0;
+  while (work.more(p)) {
+    ahead.next(p, stride);
+    fetch(ahead, stage ^ 1u);
+    copies_wait<1>();
+    bool live[ROWS];
+    const uint32_t at = ring + stage * STAGE;
+    unsigned long long block[ROWS];
+    Pair v[ROWS][4];
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) {
+      live[r] = ok && work.t + r < work.end;
+      block[r] = (unsigned long long)(work.t + r) * p.C8 + col;
+    }
     if (p.y != nullptr) {
 #pragma unroll
-      for (int j = 0; j < V; ++j) {
-        if (ok[j]) unpack8<false>(yv[j], v[j]);
-      }
+      for (int r = 0; r < ROWS; ++r) read_block<false>(at + (r * SLOTS + Y) * PITCH, v[r]);
       if (p.post != BIMASK_NORM_NONE) {
-        const float2 st = row_stats<V>(v, ok, p.post, p.eps_post, p.inv_c, r);
-        if (p.stats_post != nullptr && l == 0) p.stats_post[t] = st;
+        float2 st[ROWS];
+        row_stats(v, ok, p.post == BIMASK_NORM_LAYER, p.eps_post, p.inv_c, p.C8, g, st);
 #pragma unroll
-        for (int j = 0; j < V; ++j)
-          if (ok[j]) { normalise(v[j], st); affine(v[j], p.w_post, p.b_post, col[j]); }
-      }
-#pragma unroll
-      for (int j = 0; j < V; ++j)
-        if (ok[j]) {
-          if (p.drop.thr != 0u) drop8(v[j], (unsigned long long)(row + col[j]), key, p.drop.thr, p.drop.scale);
-          if (p.gate_span != 0) {
-            Pair g[4];
-            unpack8<false>(gv[j], g);
-#pragma unroll
-            for (int k = 0; k < 4; ++k) v[j][k] = act::mul2(v[j][k], g[k]);
-          }
-          affine(v[j], p.scale, nullptr, col[j]);
+        for (int r = 0; r < ROWS; ++r) {
+          if (p.stats_post != nullptr && col == 0 && live[r]) p.stats_post[work.t + r] = st[r];
+          normalise(v[r], st[r]);
         }
+        Pair w[4];
+        if (p.w_post != nullptr) {
+          param8(p.w_post, colc, w);
+#pragma unroll
+          for (int r = 0; r < ROWS; ++r) times8(v[r], w);
+        }
+        if (p.b_post != nullptr) {
+          param8(p.b_post, colc, w);
+#pragma unroll
+          for (int r = 0; r < ROWS; ++r) plus8(v[r], w);
+        }
+      }
+      if (p.drop.thr != 0u) {
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r) drop8(v[r], block[r], number, p.drop);
+      }
+      if (GATE) {
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r) {
+          Pair w[4];
+          read_block<false>(at + (r * SLOTS + G) * PITCH, w);
+          times8(v[r], w);
+        }
+      }
+      if (p.scale != nullptr) {
+        Pair w[4];
+        param8(p.scale, colc, w);
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r) times8(v[r], w);
+      }
+    } else {
+#pragma unroll
+      for (int r = 0; r < ROWS; ++r) fill8(v[r], 0.f);
     }
     const Pair alpha = act::both(p.alpha);
 #pragma unroll
-    for (int j = 0; j < V; ++j)
-      if (ok[j]) {
-        Pair x[4];
-        unpack8<F32>(xv[j], x);
+    for (int r = 0; r < ROWS; ++r) {
+      Pair x[4];
+      read_block<F32>(at + (r * SLOTS + X) * PITCH, x);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) v[j][k] = p.y != nullptr ? act::fma2(x[k], alpha, v[j][k]) : act::mul2(x[k], alpha);
-        if (p.xo != nullptr) store8<F32>(p.xo, row + col[j], v[j]);
-      }
-    if (p.pre != BIMASK_NORM_NONE) {
-      const float2 st = row_stats<V>(v, ok, p.pre, p.eps_pre, p.inv_c, r);
-      if (p.stats_pre != nullptr && l == 0) p.stats_pre[t] = st;
-#pragma unroll
-      for (int j = 0; j < V; ++j)
-        if (ok[j]) {
-          normalise(v[j], st);
-          affine(v[j], p.w_pre, p.b_pre, col[j]);
-          store8<false>(p.n, row + col[j], v[j]);
-        }
+      for (int k = 0; k < 4; ++k) v[r][k] = act::fma2(x[k], alpha, v[r][k]);
+      if (p.xo != nullptr && live[r]) store8<F32>(p.xo, (long long)block[r], v[r]);
     }
+    if (p.pre != BIMASK_NORM_NONE) {
+      float2 st[ROWS];
+      if (!ok) {                                          // whatever came of the zeros there (a bias, an infinite statistic) stays out
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r) fill8(v[r], 0.f);
+      }
+      row_stats(v, ok, p.pre == BIMASK_NORM_LAYER, p.eps_pre, p.inv_c, p.C8, g, st);
+      Pair w[4];
+#pragma unroll
+      for (int r = 0; r < ROWS; ++r) {
+        if (p.stats_pre != nullptr && col == 0 && live[r]) p.stats_pre[work.t + r] = st[r];
+        normalise(v[r], st[r]);
+      }
+      if (p.w_pre != nullptr) {
+        param8(p.w_pre, colc, w);
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r) times8(v[r], w);
+      }
+      if (p.b_pre != nullptr) {
+        param8(p.b_pre, colc, w);
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r) plus8(v[r], w);
+      }
+#pragma unroll
+      for (int r = 0; r < ROWS; ++r)
+        if (live[r]) store8<false>(p.n, (long long)block[r], v[r]);
+    }
+    work.next(p, stride);
+    stage ^= 1u;
   }
+  copies_wait<0>();
+  if (CLUSTER) ptx::cluster_sync();                       // shared memory outlives the peers' writes to it
 }
 
 // ------------------------------------------------------------------------------------------
@@ -333,223 +564,256 @@ residual_fwd_kernel(const ResidualParams p) {
 //   e  = m gate D;  dy the same norm formula on scale e w_post;                   dgate = m D scale u
 // and four column sums carry every parameter's gradient: G1 = sum dn xh (w_pre), G2 = sum dn (b_pre), A = sum e yh, B = sum e:
 //   dw_post = scale A,  db_post = scale B,  dscale = w_post A + b_post B.
-// A thread owns its columns for good and keeps the sums in registers; each CTA leaves one row of partial sums.
+// A thread keeps its columns' sums in registers; each cluster (CTA) leaves one row of partial sums.
+// Columns and rows past the end: dx', dn and y are zeros, and so are D (its means are left out there) and every sum.
+// GATE: 0 no gate, 1 a gate whose gradient, if wanted, is a row per token, 2 one whose gradient is summed over spans.
 // ------------------------------------------------------------------------------------------
-constexpr int BWD_THREADS = 512;
 enum { SUM_A = 1, SUM_B = 2, SUM_G1 = 4, SUM_G2 = 8 };
 
-__device__ __forceinline__ float2 row_sums(float a, float b, bool two, Row& r) {
-  a = warp_sum(a);
-  if (two) b = warp_sum(b);
-  if (r.warps > 1) {
-    const float2 e = exchange(r, make_float2(a, b));
-    a = sum16(e.x);
-    if (two) b = sum16(e.y);
-  }
-  return make_float2(a, b);
-}
-
-// One gate row's span (or any row without one) is worked off in units of consecutive rows.
-struct Unit { long long begin, end; };
-__device__ __forceinline__ Unit unit_rows(const ResidualParams& p, long long k) {
-  if (p.units_per_span == 0) return {k, k + 1};
-  const long long span = k / p.units_per_span, part = k - span * p.units_per_span;
-  const long long begin = span * p.gate_span + part * p.unit_rows;
-  const long long end = min(min(begin + p.unit_rows, (span + 1) * p.gate_span), (long long)p.T);
-  return {begin, end};
-}
-
-template <int V, bool F32, bool SPAN>
-__global__ void __launch_bounds__(BWD_THREADS, 1)
-residual_bwd_kernel(const ResidualParams p, long long units) {
-  __shared__ float2 red[16 * 32];
-  extern __shared__ float4 fold[];                        // [threads][2 V] (one array at a time)
+template <bool F32, int GATE, bool CLUSTER>
+__global__ void __launch_bounds__(ROW_THREADS, 1)
+residual_bwd_kernel(const __grid_constant__ ResidualParams p) {
+  extern __shared__ float4 smem[];
+  constexpr int SLOTS = bwd_slots(F32, GATE != 0), XB = F32 ? 2 : 1, X = 0, DX = XB, DN = 2 * XB, Y = DN + 1, G = Y + 1;
+  constexpr uint32_t STAGE = ROWS * SLOTS * PITCH;
+  uint8_t* const after = reinterpret_cast<uint8_t*>(smem) + ring_bytes(SLOTS);
+  float* const exchange = reinterpret_cast<float*>(after + STATS_BYTES);
   pdl_launch_dependents();
+  clear_exchange<CLUSTER>(exchange);
+  Group<CLUSTER> g(p, smem_addr(exchange));
+  const uint32_t col = 32u * (uint32_t)g.warp + (uint32_t)g.lane, colc = min(col, p.C8 - 1u);
+  const bool ok = col < p.C8;
+  const float inv_c = ok ? p.inv_c : 0.f;
+  const uint32_t groups = blockDim.x / (32u * (uint32_t)p.warps);
+  const uint32_t stride = CLUSTER ? gridDim.x / (uint32_t)p.cluster : gridDim.x * groups;
+  const uint32_t ring = smem_addr(smem) + threadIdx.x * 16u;
+  const uint32_t stats = smem_addr(after) + (threadIdx.x >> 5) * (STAGES * STATS_STAGE);
+  Walk<GATE == 2> work, ahead;
+  work.unit = CLUSTER ? blockIdx.x / (uint32_t)p.cluster : blockIdx.x * groups + (uint32_t)g.group;
+  work.enter(p);
+  ahead = work;
   pdl_wait();
-  const DropKey key = drop_key(p.drop);
-  Row r = make_row(p.warps, V, p.C8, red);
-  const int groups = blockDim.x / (32 * p.warps);
-  const int l = 32 * r.warp + r.lane;
-  int col[V];
-  bool ok[V];
-  Pair sums[4][V][4], fsum[SPAN ? V : 1][4];
+  const unsigned long long number = drop_number(p.drop);
+  const bool pre = p.pre != BIMASK_NORM_NONE, post = p.post != BIMASK_NORM_NONE && p.branch != 0;
+  const bool layer_pre = p.pre == BIMASK_NORM_LAYER, layer_post = p.post == BIMASK_NORM_LAYER;
+  auto fetch = [&](const Walk<GATE == 2>& w, uint32_t stage) {
+    const bool more = w.more(p);
 #pragma unroll
-  for (int j = 0; j < V; ++j) {
-    col[j] = l + 32 * j * p.warps;
-    ok[j] = col[j] < p.C8;
+    for (int r = 0; r < ROWS; ++r) {
+      const bool live = ok && more && w.t + r < w.end;
+      const uint32_t t = min(w.t + r, p.T - 1u), at = ring + stage * STAGE + r * SLOTS * PITCH;
+      const unsigned long long block = (unsigned long long)t * p.C8 + colc;
+      if (pre) {
+        copy_block<F32>(at + X * PITCH, p.xo, block, live);
+        copy16(at + DN * PITCH, p.dn + block, live);
+      }
+      if (p.dxo != nullptr) copy_block<F32>(at + DX * PITCH, p.dxo, block, live);
+      if (p.y != nullptr) copy16(at + Y * PITCH, p.y + block, live);
+      if (GATE != 0) copy16(at + G * PITCH, p.gate + (long long)(p.gate_span == 1u ? t : t / p.gate_span) * p.gate_pitch8 + colc, live);
+    }
+    if (g.lane < 2 * ROWS) {                              // lanes 0, 1: the rows' statistics before, 2, 3: after
+      const uint32_t t = w.t + (g.lane & 1);
+      const float2* src = g.lane < 2 ? p.stats_pre : p.stats_post;
+      if (src != nullptr) copy8(stats + stage * STATS_STAGE + g.lane * 8u, src + min(t, p.T - 1u), more && t < w.end);
+    }
+    copies_commit();
+  };
+  Pair sums[4][4], fsum[4];
 #pragma unroll
-    for (int a = 0; a < 4; ++a)
+  for (int a = 0; a < 4; ++a) fill8(sums[a], 0.f);
+  fill8(fsum, 0.f);
+  fetch(ahead, 0);
+  uint32_t stage = 0;
+  while (work.more(p)) {
+    __syncwarp();                                         // every lane has read the statistics that are overwritten now
+    ahead.next(p, stride);
+    fetch(ahead, stage ^ 1u);
+    copies_wait<1>();
+    __syncwarp();                                         // the statistics are other lanes' copies
+    bool live[ROWS];
+    const uint32_t at = ring + stage * STAGE, st_at = stats + stage * STATS_STAGE;
+    unsigned long long block[ROWS];
+    Pair D[ROWS][4];
+    uint4 bits[ROWS];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) sums[a][j][k] = act::both(0.f);
-  }
-  for (long long unit = (long long)blockIdx.x * groups + r.group; unit < units; unit += (long long)gridDim.x * groups) {
-    const Unit rows = unit_rows(p, unit);
-    if (SPAN)
+    for (int r = 0; r < ROWS; ++r) {
+      live[r] = ok && work.t + r < work.end;
+      block[r] = (unsigned long long)(work.t + r) * p.C8 + col;
+      if (p.dxo != nullptr) read_block<F32>(at + (r * SLOTS + DX) * PITCH, D[r]);
+      else fill8(D[r], 0.f);
+    }
+    auto draw = [&]() {
+      if (p.drop.thr != 0u) {
 #pragma unroll
-      for (int j = 0; j < V; ++j)
+        for (int r = 0; r < ROWS; ++r) bits[r] = philox(block[r], number, p.drop);
+      }
+    };
+    if (pre) {
+      Pair xh[ROWS][4], gr[ROWS][4];
+      float c[4], rstd[ROWS];
+      Pair w[4];
+      if (p.w_pre != nullptr) param8(p.w_pre, colc, w);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) fsum[j][k] = act::both(0.f);
-    for (long long t = rows.begin; t < rows.end; ++t) {
-      const long long row = t * p.C8;
-      Vec8<F32> dxv[V], xv[V];
-      Vec8<false> dnv[V], yv[V], gv[V];
-      const long long grow = p.gate_span != 0 ? (t / p.gate_span) * p.gate_pitch8 : 0;
+      for (int r = 0; r < ROWS; ++r) {
+        const float2 st = read_pair(st_at + 8 * r);
+        rstd[r] = st.y;
+        read_block<F32>(at + (r * SLOTS + X) * PITCH, xh[r]);
+        read_block<false>(at + (r * SLOTS + DN) * PITCH, gr[r]);
+        normalise(xh[r], st);
 #pragma unroll
-      for (int j = 0; j < V; ++j)
-        if (ok[j]) {
-          if (p.dxo != nullptr) dxv[j] = load8<F32>(p.dxo, row + col[j]);
-          if (p.pre != BIMASK_NORM_NONE) {
-            dnv[j] = load8<false>(p.dn, row + col[j]);
-            xv[j] = load8<F32>(p.xo, row + col[j]);
-          }
-          if (p.y != nullptr) yv[j] = load8<false>(p.y, row + col[j]);
-          if (p.gate_span != 0) gv[j].w[0] = __ldg(p.gate + grow + col[j]);
+        for (int k = 0; k < 4; ++k) sums[2][k] = act::fma2(gr[r][k], xh[r][k], sums[2][k]);
+        if (p.want & SUM_G2) plus8(sums[3], gr[r]);
+        if (p.w_pre != nullptr) times8(gr[r], w);
+        c[2 * r] = horizontal(dot8(gr[r], xh[r]));
+        c[2 * r + 1] = layer_pre ? horizontal(sum8(gr[r])) : 0.f;
+      }
+      const float folded = fold4(c, g.lane);
+      totals_begin(g, folded);
+      draw();                                             // needs nothing of the others: done while they arrive
+      totals_end(g, folded, c);
+#pragma unroll
+      for (int r = 0; r < ROWS; ++r) {
+        const float scaled = -rstd[r] * inv_c;
+        const Pair c1 = act::both(c[2 * r] * scaled), rs = act::both(rstd[r]);
+        if (layer_pre) {
+          const Pair c2 = act::both(c[2 * r + 1] * scaled);
+#pragma unroll
+          for (int k = 0; k < 4; ++k) D[r][k] = act::add2(D[r][k], c2);
         }
-      Pair D[V][4];
 #pragma unroll
-      for (int j = 0; j < V; ++j) {
-        if (p.dxo != nullptr && ok[j]) unpack8<F32>(dxv[j], D[j]);
+        for (int k = 0; k < 4; ++k) D[r][k] = act::fma2(gr[r][k], rs, act::fma2(xh[r][k], c1, D[r][k]));
+      }
+    } else {
+      draw();
+    }
+    if (p.dx != nullptr) {
+      const Pair alpha = act::both(p.alpha);
+#pragma unroll
+      for (int r = 0; r < ROWS; ++r) {
+        Pair o[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) o[k] = act::mul2(D[r][k], alpha);
+        if (live[r]) store8<F32>(p.dx, (long long)block[r], o);
+      }
+    }
+    if (p.branch) {
+      Pair yh[ROWS][4];
+      float c[4], rstd[ROWS];
+      Pair w[4];                                          // scale w_post
+      const bool weighted = p.scale != nullptr || p.w_post != nullptr;
+      if (p.w_post != nullptr) param8(p.w_post, colc, w);
+      if (p.scale != nullptr) {
+        Pair s[4];
+        param8(p.scale, colc, s);
+        if (p.w_post != nullptr) times8(w, s);
         else
 #pragma unroll
-          for (int k = 0; k < 4; ++k) D[j][k] = act::both(0.f);
+          for (int k = 0; k < 4; ++k) w[k] = s[k];
       }
-      if (p.pre != BIMASK_NORM_NONE) {
-        const float2 st = p.stats_pre[t];
-        Pair xh[V][4], g[V][4];
-        Pair s1 = act::both(0.f), s2 = act::both(0.f);
 #pragma unroll
-        for (int j = 0; j < V; ++j)
-          if (ok[j]) {
-            unpack8<F32>(xv[j], xh[j]);
-            normalise(xh[j], st);
-            unpack8<false>(dnv[j], g[j]);
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              sums[2][j][k] = act::fma2(g[j][k], xh[j][k], sums[2][j][k]);
-              sums[3][j][k] = act::add2(sums[3][j][k], g[j][k]);
-            }
-            affine(g[j], p.w_pre, nullptr, col[j]);
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              s1 = act::fma2(g[j][k], xh[j][k], s1);
-              s2 = act::add2(s2, g[j][k]);
-            }
-          }
-        const bool layer = p.pre == BIMASK_NORM_LAYER;
-        const float2 c = row_sums(horizontal(s1), horizontal(s2), layer, r);
-        const Pair c1 = act::both(-c.x * p.inv_c), c2 = act::both(layer ? -c.y * p.inv_c : 0.f), rstd = act::both(st.y);
-#pragma unroll
-        for (int j = 0; j < V; ++j)
-          if (ok[j])
-#pragma unroll
-            for (int k = 0; k < 4; ++k) D[j][k] = act::fma2(act::fma2(xh[j][k], c1, act::add2(g[j][k], c2)), rstd, D[j][k]);
-      }
-      if (p.dx != nullptr) {
-        const Pair alpha = act::both(p.alpha);
-#pragma unroll
-        for (int j = 0; j < V; ++j)
-          if (ok[j]) {
-            Pair o[4];
-#pragma unroll
-            for (int k = 0; k < 4; ++k) o[k] = act::mul2(D[j][k], alpha);
-            store8<F32>(p.dx, row + col[j], o);
-          }
-      }
-      if (!p.branch) continue;
-      Pair yh[V][4];
-      float2 st = make_float2(0.f, 1.f);
-      if (p.post != BIMASK_NORM_NONE) st = p.stats_post[t];
-      Pair s1 = act::both(0.f), s2 = act::both(0.f);
-#pragma unroll
-      for (int j = 0; j < V; ++j)
-        if (ok[j]) {
-          if (p.y != nullptr) unpack8<false>(yv[j], yh[j]);
-          else                                            // not needed: any value
-#pragma unroll
-            for (int k = 0; k < 4; ++k) yh[j][k] = act::both(0.f);
-          if (p.post != BIMASK_NORM_NONE) normalise(yh[j], st);
-          if (p.drop.thr != 0u) drop8(D[j], (unsigned long long)(row + col[j]), key, p.drop.thr, p.drop.scale);
-          if (p.gate_span != 0) {
-            Pair g[4], u[4];
-#pragma unroll
-            for (int k = 0; k < 4; ++k) u[k] = yh[j][k];
-            affine(u, p.w_post, p.b_post, col[j]);
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              if (SPAN) fsum[j][k] = act::fma2(D[j][k], u[k], fsum[j][k]);
-              else u[k] = act::mul2(D[j][k], u[k]);
-            }
-            if (!SPAN && p.dgate != nullptr) {
-              affine(u, p.scale, nullptr, col[j]);
-              store8<false>(p.dgate, grow + col[j], u);
-            }
-            unpack8<false>(gv[j], g);
-#pragma unroll
-            for (int k = 0; k < 4; ++k) D[j][k] = act::mul2(D[j][k], g[k]);
-          }
-#pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            sums[0][j][k] = act::fma2(D[j][k], yh[j][k], sums[0][j][k]);
-            sums[1][j][k] = act::add2(sums[1][j][k], D[j][k]);
-          }
-          affine(D[j], p.scale, nullptr, col[j]);
-          if (p.post != BIMASK_NORM_NONE) {
-            affine(D[j], p.w_post, nullptr, col[j]);
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              s1 = act::fma2(D[j][k], yh[j][k], s1);
-              s2 = act::add2(s2, D[j][k]);
-            }
-          }
+      for (int r = 0; r < ROWS; ++r) {
+        rstd[r] = 1.f;
+        if (p.y != nullptr) read_block<false>(at + (r * SLOTS + Y) * PITCH, yh[r]);
+        else fill8(yh[r], 0.f);
+        if (post) {
+          const float2 st = read_pair(st_at + 8 * (ROWS + r));
+          rstd[r] = st.y;
+          normalise(yh[r], st);
         }
-      if (p.post != BIMASK_NORM_NONE) {
-        const bool layer = p.post == BIMASK_NORM_LAYER;
-        const float2 c = row_sums(horizontal(s1), horizontal(s2), layer, r);
-        const Pair c1 = act::both(-c.x * p.inv_c), c2 = act::both(layer ? -c.y * p.inv_c : 0.f), rstd = act::both(st.y);
+        if (p.drop.thr != 0u) {
+          D[r][0] = drop_pair(D[r][0], bits[r].x, p.drop.thr, p.drop.scale);
+          D[r][1] = drop_pair(D[r][1], bits[r].y, p.drop.thr, p.drop.scale);
+          D[r][2] = drop_pair(D[r][2], bits[r].z, p.drop.thr, p.drop.scale);
+          D[r][3] = drop_pair(D[r][3], bits[r].w, p.drop.thr, p.drop.scale);
+        }
+        if (GATE != 0) {
+          if (GATE == 2 || p.dgate != nullptr) {          // scale u
+            Pair u[4];
 #pragma unroll
-        for (int j = 0; j < V; ++j)
-          if (ok[j])
+            for (int k = 0; k < 4; ++k) u[k] = yh[r][k];
+            if (weighted) times8(u, w);
+            if (p.b_post != nullptr) {
+              Pair b[4];
+              param8(p.b_post, colc, b);
+              if (p.scale != nullptr) {
+                Pair s[4];
+                param8(p.scale, colc, s);
+                times8(b, s);
+              }
+              plus8(u, b);
+            }
+            if (GATE == 2) {
 #pragma unroll
-            for (int k = 0; k < 4; ++k) D[j][k] = act::mul2(act::fma2(yh[j][k], c1, act::add2(D[j][k], c2)), rstd);
+              for (int k = 0; k < 4; ++k) fsum[k] = act::fma2(D[r][k], u[k], fsum[k]);
+            } else {
+              times8(u, D[r]);
+              if (live[r]) store8<false>(p.dgate, (long long)(work.t + r) * p.gate_pitch8 + col, u);
+            }
+          }
+          Pair gt[4];
+          read_block<false>(at + (r * SLOTS + G) * PITCH, gt);
+          times8(D[r], gt);
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) sums[0][k] = act::fma2(D[r][k], yh[r][k], sums[0][k]);
+        if (p.want & SUM_B) plus8(sums[1], D[r]);
+        if (weighted) times8(D[r], w);
+      }
+      if (post) {
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r) {
+          c[2 * r] = horizontal(dot8(D[r], yh[r]));
+          c[2 * r + 1] = layer_post ? horizontal(sum8(D[r])) : 0.f;
+        }
+        const float folded = fold4(c, g.lane);
+        totals_begin(g, folded);
+        totals_end(g, folded, c);
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r) {
+          const float scaled = -rstd[r] * inv_c;
+          const Pair c1 = act::both(c[2 * r] * scaled), c2 = act::both(layer_post ? c[2 * r + 1] * scaled : 0.f), rs = act::both(rstd[r]);
+#pragma unroll
+          for (int k = 0; k < 4; ++k) D[r][k] = act::fma2(D[r][k], rs, act::fma2(yh[r][k], c1, c2));
+        }
       }
       if (p.dy != nullptr) {
 #pragma unroll
-        for (int j = 0; j < V; ++j)
-          if (ok[j]) store8<false>(p.dy, row + col[j], D[j]);
+        for (int r = 0; r < ROWS; ++r)
+          if (live[r]) store8<false>(p.dy, (long long)block[r], D[r]);
+      }
+      if (GATE == 2 && work.last()) {
+        if (ok) store8<true>(p.gate_sums, (long long)work.unit * p.C8 + col, fsum);
+        fill8(fsum, 0.f);
       }
     }
-    if (SPAN) {
-#pragma unroll
-      for (int j = 0; j < V; ++j)
-        if (ok[j]) store8<true>(p.gate_sums, unit * p.C8 + col[j], fsum[j]);
-    }
+    work.next(p, stride);
+    stage ^= 1u;
   }
-  // the groups' sums are added through shared memory, in their order
+  copies_wait<0>();
+  // the groups' sums are added through the ring, in their order
   int slot = 0;
 #pragma unroll
   for (int a = 0; a < 4; ++a) {
     if (!(p.want & (1 << a))) continue;                   // the same for every thread
-#pragma unroll
-    for (int j = 0; j < V; ++j) {
-      if (groups > 1) {
-        __syncthreads();
-        const Vec8<true> v = pack8<true>(sums[a][j]);
-        reinterpret_cast<uint4*>(fold)[2 * threadIdx.x] = v.w[0];
-        reinterpret_cast<uint4*>(fold)[2 * threadIdx.x + 1] = v.w[1];
-        __syncthreads();
+    if (groups > 1) {
+      __syncthreads();
+      const Vec8<true> v = pack8<true>(sums[a]);
+      uint4* mine = reinterpret_cast<uint4*>(smem) + threadIdx.x;
+      mine[0] = v.w[0];
+      mine[ROW_THREADS] = v.w[1];
+      __syncthreads();
+    }
+    if (g.group == 0 && ok) {
+      for (uint32_t o = 1; o < groups; ++o) {
+        Pair q[4];
+        read_block<true>(ring + o * (uint32_t)p.warps * 512u, q);
+        plus8(sums[a], q);
       }
-      if (r.group == 0 && ok[j]) {
-        for (int g = 1; g < groups; ++g) {
-          Pair q[4];
-          unpack8<true>(load8<true>(fold, l + 32 * p.warps * g), q);
-#pragma unroll
-          for (int k = 0; k < 4; ++k) sums[a][j][k] = act::add2(sums[a][j][k], q[k]);
-        }
-        store8<true>(p.sums, ((long long)blockIdx.x * __popc(p.want) + slot) * p.C8 + col[j], sums[a][j]);
-      }
+      store8<true>(p.sums, ((long long)(CLUSTER ? blockIdx.x / (uint32_t)p.cluster : blockIdx.x) * __popc(p.want) + slot) * p.C8 + col, sums[a]);
     }
     ++slot;
   }
+  if (CLUSTER) ptx::cluster_sync();                       // shared memory outlives the peers' writes to it
 }
 
 // The parameters' gradients from the CTAs' partial sums: a CTA covers 8 float4 columns, its 32 row slots take the partial
@@ -610,10 +874,9 @@ residual_reduce_kernel(const ResidualReduce p) {
   if (p.db_pre != nullptr) p.db_pre[e] = total[3];
 }
 
-// dgate of a row that serves a span of tokens: scale times the sum of its units, in order.
+// dgate of a row that serves a span of tokens: the sum of its units, in order.
 __global__ void __launch_bounds__(256)
-gate_reduce_kernel(const float4* __restrict__ sums, int units_per_span, long long gates, int C4, const float4* __restrict__ scale,
-                   uint2* dgate, long long pitch4) {
+gate_reduce_kernel(const float4* __restrict__ sums, int units_per_span, long long gates, int C4, uint2* dgate, long long pitch4) {
   pdl_launch_dependents();
   pdl_wait();
   const long long all = gates * C4;
@@ -624,60 +887,79 @@ gate_reduce_kernel(const float4* __restrict__ sums, int units_per_span, long lon
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 8
     for (int u = 0; u < units_per_span; ++u) acc = add4(acc, src[(long long)u * C4]);
-    if (scale != nullptr) acc = mul4(acc, __ldg(scale + c));
     dgate[g * pitch4 + c] = make_uint2(pack_bf16_f(acc.x, acc.y), pack_bf16_f(acc.z, acc.w));
   }
 }
 
 // ---- plans --------------------------------------------------------------------------------------
-struct BwdPlan {
-  int vec, warps, groups, threads;                        // blocks of eight per thread, warps per row, rows side by side
-  int slots;                                              // CTAs
-  int unit_rows, units_per_span;                          // with a gate row per span: rows of a unit
+struct RowPlan {
+  int cluster, warps, groups, threads;                    // CTAs that share a row, its warps in each, rows side by side
+  int slots;                                              // clusters (CTAs) of the grid
   long long units, gates;
+  int unit_rows, units_per_span;
 };
 
-BwdPlan plan_bwd(int T, int C, int span) {
-  BwdPlan b;
-  const int C8 = C / 8;
-  b.vec = C8 > 512 ? 2 : 1;
-  b.warps = (C8 + 32 * b.vec - 1) / (32 * b.vec);
-  b.groups = BWD_THREADS / (32 * b.warps);
+// ctas: how many the card holds.  span > 1: units end where a gate row's span ends, and are as many as the groups of warps.
+RowPlan plan_rows(int T, int C, int span, int ctas) {
+  RowPlan b = {};
+  const int all = (C / 8 + 31) / 32;                      // warps of a row
+  b.cluster = all > 32 ? 4 : all > 16 ? 2 : 1;
+  b.warps = (all + b.cluster - 1) / b.cluster;
+  b.groups = ROW_THREADS / 32 / b.warps;
   b.threads = 32 * b.warps * b.groups;
-  b.unit_rows = 1;
-  b.units_per_span = 0;
-  b.units = T;
-  b.gates = 0;
+  const long long room = (long long)(ctas / b.cluster) * b.groups;
   if (span > 1) {
-    const long long all = (long long)PLAN_SMS * b.groups;
     const int len = span < T ? span : T;
     b.gates = (T + (long long)span - 1) / span;
-    b.unit_rows = (int)((T + all - 1) / all);
+    b.unit_rows = (int)((T + room - 1) / room);
+    if (b.unit_rows > 1 && b.unit_rows % ROWS != 0) b.unit_rows += ROWS - b.unit_rows % ROWS;
     if (b.unit_rows > len) b.unit_rows = len;
     b.units_per_span = (len + b.unit_rows - 1) / b.unit_rows;
     b.units = b.gates * b.units_per_span;
+  } else {
+    b.unit_rows = T > room ? ROWS : 1;                    // fewer rows than groups: one each
+    b.units = ((long long)T + b.unit_rows - 1) / b.unit_rows;
   }
-  const long long ctas = (b.units + b.groups - 1) / b.groups;
-  b.slots = (int)(ctas < PLAN_SMS ? ctas : PLAN_SMS);
+  const long long slots = (b.units + b.groups - 1) / b.groups;
+  b.slots = (int)(slots < ctas / b.cluster ? slots : ctas / b.cluster);
   return b;
+}
+
+template <typename K>
+int launch_rows(K kernel, const RowPlan& b, int bytes, cudaStream_t s, const ResidualParams& p) {
+  const int rc = set_smem_attr(kernel, bytes);
+  if (rc != BIMASK_OK) return rc;
+  if (b.cluster == 1) BIMASK_CUDA_OK(launch_pdl(kernel, (unsigned)b.slots, b.threads, (size_t)bytes, s, p));
+  else BIMASK_CUDA_OK(launch_pdl_cluster(kernel, (unsigned)(b.slots * b.cluster), b.threads, b.cluster, (size_t)bytes, s, p));
+  count_launch();
+  return BIMASK_OK;
+}
+
+void take_plan(ResidualParams& p, const RowPlan& b) {
+  p.warps = b.warps;
+  p.cluster = b.cluster;
+  p.units = (uint32_t)b.units;
+  p.unit_rows = (uint32_t)b.unit_rows;
+  p.units_per_span = (uint32_t)b.units_per_span;
 }
 
 }  // namespace
 
 static size_t up256(size_t v) { return (v + 255) / 256 * 256; }
 
-// Scratch of the backward pass: the CTAs' partial sums (four arrays at most), then the units' of a spanned gate, each for T
+// Scratch of the backward pass: the clusters' partial sums (four arrays at most), then the units' of a spanned gate, each for T
 // tokens and every smaller number.  With spans there are at most 2 T units (a last span that is not full has its empty ones),
 // and at most two per group of warps and one more per gate row.
 static size_t column_sums_bytes(int T, int C, int span) {
-  const BwdPlan b = plan_bwd(1, C, 0);
-  const long long ctas = ((span > 1 ? 2ll : 1ll) * T + b.groups - 1) / b.groups;
-  return up256((size_t)(ctas < PLAN_SMS ? ctas : PLAN_SMS) * 4 * C * sizeof(float));
+  const RowPlan b = plan_rows(1, C, 1, PLAN_SMS);
+  const long long most = PLAN_SMS / b.cluster, slots = ((span > 1 ? 2ll : 1ll) * T + b.groups - 1) / b.groups;
+  return up256((size_t)(slots < most ? slots : most) * 4 * C * sizeof(float));
 }
 size_t residual_workspace_bytes(int T, int C, int span) {
   size_t bytes = column_sums_bytes(T, C, span);
   if (span > 1) {
-    const long long gates = (T + (long long)span - 1) / span, most = 2ll * PLAN_SMS * plan_bwd(1, C, 0).groups + gates;
+    const RowPlan b = plan_rows(1, C, 1, PLAN_SMS);
+    const long long gates = (T + (long long)span - 1) / span, most = 2ll * (PLAN_SMS / b.cluster) * b.groups + gates;
     bytes += (size_t)(most < 2ll * T ? most : 2ll * T) * C * sizeof(float);
   }
   return bytes;
@@ -687,10 +969,13 @@ DropParams drop_params(const bimask_dropout_args* d) {
   DropParams p = {};
   p.scale = 1.f;
   if (d == nullptr) return p;
-  p.thr = drop_threshold(d->p);
-  p.scale = (float)(65536.0 / (65536.0 - p.thr));
-  p.key0 = (uint32_t)d->seed;
-  p.key1 = (uint32_t)(d->seed >> 32);
+  const uint32_t thr = drop_threshold(d->p);
+  p.thr = thr << 16;
+  p.scale = (float)(65536.0 / (65536.0 - thr));
+  for (int r = 0; r < 10; ++r) {
+    p.key[2 * r] = (uint32_t)d->seed + 0x9E3779B9u * r;
+    p.key[2 * r + 1] = (uint32_t)(d->seed >> 32) + 0xBB67AE85u * r;
+  }
   p.number = d->stream_no;
   p.counter = reinterpret_cast<const unsigned long long*>(d->counter);
   return p;
@@ -710,15 +995,15 @@ int launch_dropout(const void* x, int type, int T, int C, const bimask_dropout_a
 
 static ResidualParams residual_params(const bimask_residual_args& a) {
   ResidualParams p = {};
-  p.T = a.T;
-  p.C8 = a.C / 8;
+  p.T = (uint32_t)a.T;
+  p.C8 = (uint32_t)a.C / 8;
   p.post = a.post;
   p.pre = a.pre;
   p.eps_post = a.eps_post;
   p.eps_pre = a.eps_pre;
   p.alpha = a.alpha;
   p.inv_c = 1.f / (float)a.C;
-  p.gate_span = a.gate != nullptr ? a.gate_span : 0;
+  p.gate_span = a.gate != nullptr ? (uint32_t)a.gate_span : 0u;
   p.gate_pitch8 = a.gate_pitch / 8;
   p.drop = drop_params(&a.drop);
   p.x = a.x;
@@ -743,15 +1028,18 @@ static ResidualParams residual_params(const bimask_residual_args& a) {
 
 int launch_residual_fwd(const bimask_residual_args& a, cudaStream_t s) {
   ResidualParams p = residual_params(a);
-  const int vec = p.C8 > 32 ? 2 : 1;
-  p.warps = (p.C8 + 32 * vec - 1) / (32 * vec);
-  const int groups = p.warps < 8 ? 8 / p.warps : 1, threads = 32 * p.warps * groups;
-  const long long ctas = ((long long)a.T + groups - 1) / groups, most = (long long)sm_count() * (threads > 256 ? 2 : 4);
-  auto run = [&](auto kern) { return launch_pdl(kern, (unsigned)(ctas < most ? ctas : most), threads, 0, s, p); };
-  const bool f32 = a.stream_type == BIMASK_TYPE_F32;
-  BIMASK_CUDA_OK(vec == 1 ? (f32 ? run(residual_fwd_kernel<1, true>) : run(residual_fwd_kernel<1, false>))
-                          : (f32 ? run(residual_fwd_kernel<2, true>) : run(residual_fwd_kernel<2, false>)));
-  count_launch();
+  const RowPlan b = plan_rows(a.T, a.C, 1, 2 * sm_count());
+  take_plan(p, b);
+  auto run = [&](auto f32, auto gate, auto cluster) -> int {
+    constexpr bool F = decltype(f32)::value, G = decltype(gate)::value, K = decltype(cluster)::value;
+    return launch_rows(residual_fwd_kernel<F, G, K>, b, ring_bytes(fwd_slots(F, G)) + Exchange<K>::BYTES, s, p);
+  };
+  using Yes = std::true_type;
+  using No = std::false_type;
+  auto pick = [&](auto f32, auto gate) -> int { return b.cluster > 1 ? run(f32, gate, Yes()) : run(f32, gate, No()); };
+  const bool gate = p.gate_span != 0;
+  const int rc = a.stream_type == BIMASK_TYPE_F32 ? (gate ? pick(Yes(), Yes()) : pick(Yes(), No())) : (gate ? pick(No(), Yes()) : pick(No(), No()));
+  if (rc != BIMASK_OK) return rc;
   BIMASK_CUDA_OK(cudaGetLastError());
   return BIMASK_OK;
 }
@@ -759,25 +1047,30 @@ int launch_residual_fwd(const bimask_residual_args& a, cudaStream_t s) {
 int launch_residual_bwd(const bimask_residual_args& a, cudaStream_t s) {
   ResidualParams p = residual_params(a);
   const bool spanned = a.dgate != nullptr && p.gate_span > 1;
-  const BwdPlan b = plan_bwd(a.T, a.C, spanned ? p.gate_span : 1);
+  const RowPlan b = plan_rows(a.T, a.C, spanned ? (int)p.gate_span : 1, PLAN_SMS);
+  take_plan(p, b);
   p.branch = a.dy || a.dgate || a.dscale || a.dw_post || a.db_post;
-  p.warps = b.warps;
-  p.unit_rows = b.unit_rows;
-  p.units_per_span = b.units_per_span;
+  if (!p.branch) { p.y = nullptr; p.stats_post = nullptr; }
+  if (p.pre == BIMASK_NORM_NONE) p.stats_pre = nullptr;
+  if (p.post == BIMASK_NORM_NONE) p.stats_post = nullptr;
   const bool scale = a.dscale != nullptr;
   p.want = (a.dw_post || scale ? SUM_A : 0) | (a.db_post || (scale && a.b_post) ? SUM_B : 0) | (a.dw_pre ? SUM_G1 : 0) | (a.db_pre ? SUM_G2 : 0);
   p.sums = reinterpret_cast<float*>(a.ws);
-  if (spanned) p.gate_sums = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(a.ws) + column_sums_bytes(a.T, a.C, p.gate_span));
-  auto run = [&](auto kern) { return launch_pdl(kern, (unsigned)b.slots, b.threads, (size_t)b.threads * 32, s, p, b.units); };
-  auto pick = [&](auto f32, auto span) {
-    constexpr bool F = decltype(f32)::value, S = decltype(span)::value;
-    return b.vec == 1 ? run(residual_bwd_kernel<1, F, S>) : run(residual_bwd_kernel<2, F, S>);
+  if (spanned) p.gate_sums = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(a.ws) + column_sums_bytes(a.T, a.C, (int)p.gate_span));
+  auto run = [&](auto f32, auto gate, auto cluster) -> int {
+    constexpr bool F = decltype(f32)::value, K = decltype(cluster)::value;
+    constexpr int G = decltype(gate)::value, bytes = ring_bytes(bwd_slots(F, G != 0)) + STATS_BYTES + Exchange<K>::BYTES;
+    static_assert(bytes <= 227 * 1024, "shared memory of a CTA");
+    return launch_rows(residual_bwd_kernel<F, G, K>, b, bytes, s, p);
   };
-  using Yes = std::true_type;
-  using No = std::false_type;
-  const bool f32 = a.stream_type == BIMASK_TYPE_F32;
-  BIMASK_CUDA_OK(f32 ? (spanned ? pick(Yes(), Yes()) : pick(Yes(), No())) : (spanned ? pick(No(), Yes()) : pick(No(), No())));
-  count_launch();
+  auto pick2 = [&](auto f32, auto gate) -> int { return b.cluster > 1 ? run(f32, gate, std::true_type()) : run(f32, gate, std::false_type()); };
+  auto pick = [&](auto f32) -> int {
+    if (spanned) return pick2(f32, std::integral_constant<int, 2>());
+    if (p.gate_span != 0) return pick2(f32, std::integral_constant<int, 1>());
+    return pick2(f32, std::integral_constant<int, 0>());
+  };
+  const int rc = a.stream_type == BIMASK_TYPE_F32 ? pick(std::true_type()) : pick(std::false_type());
+  if (rc != BIMASK_OK) return rc;
   if (p.want != 0) {
     ResidualReduce r = {};
     r.sums = reinterpret_cast<const float4*>(a.ws);
@@ -798,8 +1091,7 @@ int launch_residual_bwd(const bimask_residual_args& a, cudaStream_t s) {
   if (p.gate_sums != nullptr) {
     const long long ctas = (b.gates * (a.C / 4) + 255) / 256, most = 8ll * sm_count();
     BIMASK_CUDA_OK(launch_pdl(gate_reduce_kernel, (unsigned)(ctas < most ? ctas : most), 256, 0, s, reinterpret_cast<const float4*>(p.gate_sums),
-                              b.units_per_span, b.gates, a.C / 4, reinterpret_cast<const float4*>(a.scale), reinterpret_cast<uint2*>(a.dgate),
-                              a.gate_pitch / 4));
+                              b.units_per_span, b.gates, a.C / 4, reinterpret_cast<uint2*>(a.dgate), a.gate_pitch / 4));
     count_launch();
   }
   BIMASK_CUDA_OK(cudaGetLastError());

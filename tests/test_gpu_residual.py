@@ -205,8 +205,8 @@ class Problem:
         return out
 
 
-# one token, a few, several rows per group; one warp, parts of one, several, the widest one-vector and two-vector rows
-SIZES = [(1, 32), (3, 64), (2, 256), (37, 288), (5, 512), (70, 544), (301, 384), (33, 1152), (6, 2080), (4, 4096), (3, 4128), (5, 8192)]
+# one token, a few, several rows per group; one warp, parts of one, several, the widest rows of one, two and four CTAs
+SIZES = [(1, 32), (3, 64), (2, 256), (37, 288), (5, 512), (70, 544), (301, 384), (33, 1152), (6, 2080), (4, 4096), (3, 4128), (5, 8192), (3, 8224), (9, 16384)]
 FORMS = [(0, 1), (0, 2), (1, 1), (2, 2), (1, 2), (2, 1), (1, 0), (2, 0), (0, 0)]
 
 
@@ -224,7 +224,7 @@ def test_against_64_bits(T, C, stream):
         assert all(torch.equal(f[k], f2[k]) for k in f) and all(torch.equal(g[k], g2[k]) for k in g if k != "ws")
 
 
-@pytest.mark.parametrize("T,C,span", [(2500, 256, 7), (2500, 64, 1300), (700, 1152, 197), (4000, 320, 3999), (300, 4160, 2), (149, 4096, 150)])
+@pytest.mark.parametrize("T,C,span", [(2500, 256, 7), (2500, 64, 1300), (700, 1152, 197), (4000, 320, 3999), (300, 4160, 2), (149, 4096, 150), (600, 8192, 64), (200, 9216, 200)])
 def test_many_rows_and_gates_that_serve_spans(T, C, span):
     """More rows than groups of warps: units of several rows, spans that end inside and a last span that is not full."""
     for post, pre in ((0, 2), (1, 1), (2, 0)):
@@ -304,7 +304,7 @@ def test_parts_that_are_absent(stream):
 
 
 @pytest.mark.parametrize("stream", TYPES)
-@pytest.mark.parametrize("T,C", [(50, 320), (9, 4224)])
+@pytest.mark.parametrize("T,C", [(50, 320), (9, 4224), (700, 4128)])
 def test_results_in_the_place_of_inputs(T, C, stream):
     for post, pre in ((1, 1), (2, 2), (0, 2)):
         q = Problem(T, C, post, pre, stream, span=1, p=0.1)

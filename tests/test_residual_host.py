@@ -111,8 +111,8 @@ def test_gradients_against_autograd_and_differences(post, pre, span):
 
 def test_workspace_query(bm):
     q = bm.bimask_residual_norm_workspace_bytes
-    assert q(0, 64, 1) == q(4, 48, 1) == q(4, 8224, 1) == q(4, 64, 0) == q(-1, 64, 1) == 0
-    for C in (32, 384, 1152, 4096, 8192):
+    assert q(0, 64, 1) == q(4, 48, 1) == q(4, 16416, 1) == q(4, 64, 0) == q(-1, 64, 1) == 0
+    for C in (32, 384, 1152, 4096, 4128, 8192, 16384):
         for span in (1, 2, 7, 197, 5000):
             sizes = [q(T, C, span) for T in (*range(1, 400), 1000, 2367, 2368, 2369, 4736, 4737, 12608, 16384, 100000, 1 << 30)]
             assert sizes == sorted(sizes) and sizes[0] >= 16 * C
@@ -167,7 +167,7 @@ def test_refusals_name_the_cause(bm):
         for call in both:
             assert call(args(**kw), None) == inval and word in bm.bimask_last_error(), (kw, bm.bimask_last_error())
     for call in both:
-        assert call(args(C=8224), None) == unsupported and "8192" in bm.bimask_last_error()
+        assert call(args(C=16416), None) == unsupported and "16384" in bm.bimask_last_error()
         assert call(None, None) == inval
     fwd, bwd_ = both
     no_w = ("w_post", "b_post")
