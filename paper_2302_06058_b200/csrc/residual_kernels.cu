@@ -90,8 +90,8 @@ dropout_kernel(const void* x, long long blocks, void* y /* may be x */, const Dr
 }
 
 // ------------------------------------------------------------------------------------------
-// Rows.  A thread owns one block of eight columns for good; `warps` warps of a CTA, and up to four CTAs of a cluster above 4096
-// columns, share a row.  A CTA holds as many such groups as its 16 warps give; they work on rows of their own and never meet (named
+// Rows.  A thread owns two blocks of eight columns for good; `warps` warps of a CTA, and up to four CTAs of a cluster above 4096
+// columns, share a row.  A CTA holds as many such groups as its eight warps give; they work on rows of their own and never meet (named
 // barriers).  A group takes two rows per step: what its threads exchange for both travels together, and the two rows' chains
 // of dependent instructions run side by side.  The rows of the next step are already on their way: every thread copies its own
 // 16-byte pieces into its own places in shared memory (cp.async), so no barrier guards them, no registers wait for them, and
@@ -100,10 +100,10 @@ dropout_kernel(const void* x, long long blocks, void* y /* may be x */, const Dr
 // parts: columns and rows past the end are copied as zeros (from a clamped address, of which cp.async reads nothing) and work like
 // the others, but for their stores.
 // ------------------------------------------------------------------------------------------
-constexpr int ROWS = 2, STAGES = 2;
-constexpr int ROW_THREADS = 512;
-constexpr int MAX_ROW_WARPS = 64;                         // of a cluster of four CTAs
-static_assert(RESIDUAL_MAX_C == 256 * MAX_ROW_WARPS, "eight columns per thread");
+constexpr int ROWS = 2, VECS = 2, STAGES = 2;
+constexpr int ROW_THREADS = 256;
+constexpr int MAX_ROW_WARPS = 32;                         // of a cluster of four CTAs
+static_assert(RESIDUAL_MAX_C == 8 * 32 * VECS * MAX_ROW_WARPS, "eight columns of each of a thread's blocks");
 
 struct ResidualParams {
   uint32_t T, C8;
@@ -189,33 +189,33 @@ __device__ __forceinline__ void fill8(Pair (&v)[4], float x) {
   for (int k = 0; k < 4; ++k) v[k] = act::both(x);
 }
 // (v - mean) rstd, as one multiplication and addition: off by a rounding of (|v| + |mean|) rstd, like the difference first
+template <bool LAYER>
 __device__ __forceinline__ void normalise(Pair (&v)[4], float2 st) {
   const Pair rstd = act::both(st.y), shift = act::both(-st.x * st.y);
 #pragma unroll
-  for (int k = 0; k < 4; ++k) v[k] = act::fma2(v[k], rstd, shift);
+  for (int k = 0; k < 4; ++k) v[k] = LAYER ? act::fma2(v[k], rstd, shift) : act::mul2(v[k], rstd);
 }
 
-// columns that a row's warp w holds
-__device__ __forceinline__ float columns_of(int w, uint32_t C8) { return 8.f * (float)min(max((int)C8 - 32 * w, 0), 32); }
+// columns that a row's warp w holds: blocks 64 w .. 64 w + 63 of the row
+__device__ __forceinline__ float columns_of(int w, uint32_t C8) { return 8.f * (float)min(max((int)C8 - 32 * VECS * w, 0), 32 * VECS); }
 
-// Exchange buffers: a group's two, of four values from each of its row's warps, their number made even (zero where there is no
-// such warp).  Groups of two warps or more: three words for two warps at worst.
-template <bool CLUSTER>
+// Exchange buffers: a group's two, of VALUES values from each of its row's warps (zeros up to a multiple of four warps).  Groups of two
+// warps or more, so that four words for two warps are the worst.
+template <int VALUES, bool CLUSTER>
 struct Exchange {
-  static constexpr int WORDS = CLUSTER ? MAX_ROW_WARPS : ROW_THREADS / 64 * 3;
-  static constexpr int BYTES = 2 * 4 * WORDS * 4;
+  static constexpr int WORDS = CLUSTER ? MAX_ROW_WARPS : ROW_THREADS / 64 * 4;
+  static constexpr int BYTES = 2 * VALUES * WORDS * 4;
 };
-template <bool CLUSTER>
+template <int VALUES, bool CLUSTER>
 struct Group {                                            // a thread's place among those that share its rows
   int lane, group, warps;                                 // warps: of the row in this CTA
   int warp;                                               // the thread's warp, counted through the row
   bool alone;                                             // the row is one warp's
   int cluster;
-  float inv_columns;                                      // 1 / columns that this warp holds
-  float peer_columns;                                     // columns of warp lane % 16 (only without clusters)
-  uint32_t mine, buffer;                                  // address of this warp's first word, and of the buffer in use
-  uint32_t flip;
   int width;                                              // words of a value
+  float inv_columns;                                      // 1 / columns that this warp holds
+  float peer_columns[CLUSTER ? MAX_ROW_WARPS / 16 : 1];   // columns of the warps whose values a lane reads
+  uint32_t buffer, flip;                                  // address of the buffer in use; buffer ^ flip: the other one
 
   __device__ __forceinline__ Group(const ResidualParams& p, uint32_t exchange) {
     const int w = threadIdx.x >> 5;
@@ -225,16 +225,15 @@ struct Group {                                            // a thread's place am
     cluster = p.cluster;
     warp = w - group * warps + (CLUSTER ? (int)ptx::cluster_ctarank() * warps : 0);
     alone = !CLUSTER && warps == 1;
+    width = CLUSTER ? MAX_ROW_WARPS : (warps + 3) & ~3;
     inv_columns = 1.f / fmaxf(columns_of(warp, p.C8), 1.f);
-    peer_columns = columns_of(lane & 15, p.C8);
-    width = CLUSTER ? MAX_ROW_WARPS : warps + (warps & 1);
-    buffer = exchange + (uint32_t)((alone ? 0 : group) * 2 * 4 * width * 4);
-    mine = 4u * (uint32_t)warp;
-    flip = buffer ^ (buffer + 4u * (uint32_t)width * 4u);
+    for (int k = 0; k < (CLUSTER ? MAX_ROW_WARPS / 16 : 1); ++k) peer_columns[k] = columns_of((lane & (CLUSTER ? 15 : 7)) + 16 * k, p.C8);
+    buffer = exchange + (uint32_t)((alone ? 0 : group) * 2 * VALUES * width * 4);
+    flip = buffer ^ (buffer + (uint32_t)(VALUES * width * 4));
   }
   // Value i of this warp, to every CTA that shares the row ...
   __device__ __forceinline__ void publish(int i, float v) const {
-    const uint32_t at = buffer + mine + (uint32_t)(i * width * 4);
+    const uint32_t at = buffer + (uint32_t)((i * width + warp) * 4);
     if (!CLUSTER) asm volatile("st.shared.f32 [%0], %1;" ::"r"(at), "f"(v) : "memory");
     else
       for (int r = 0; r < cluster; ++r) ptx::st_cluster_u32(ptx::mapa(at, (uint32_t)r), __float_as_uint(v));
@@ -249,115 +248,123 @@ struct Group {                                            // a thread's place am
   __device__ __forceinline__ void turn() { buffer ^= flip; }
 };
 
-// Sums over a warp of two or four values at a time: at each step a lane keeps half of its values and hands the others to its
-// partner.  The total of value i ends in the lanes 16 i .. or 8 i ..
-__device__ __forceinline__ float fold2(float a, float b, int lane) {
-  const bool hi = (lane & 16) != 0;
-  float v = (hi ? b : a) + __shfl_xor_sync(0xFFFFFFFFu, hi ? a : b, 16);
+// Sums over a warp of N values at a time: at each step a lane keeps half of its values and hands the others to its partner, until
+// it has one left.  The total of value i ends in the lanes i (32 / N) and on.
+template <int N>
+__device__ __forceinline__ float fold(float (&c)[N], int lane) {
 #pragma unroll
-  for (int d = 8; d >= 1; d >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, d);
-  return v;
-}
-__device__ __forceinline__ float fold4(const float (&c)[4], int lane) {
-  const bool hi = (lane & 16) != 0, mid = (lane & 8) != 0;
-  const float k0 = (hi ? c[2] : c[0]) + __shfl_xor_sync(0xFFFFFFFFu, hi ? c[0] : c[2], 16);
-  const float k1 = (hi ? c[3] : c[1]) + __shfl_xor_sync(0xFFFFFFFFu, hi ? c[1] : c[3], 16);
-  float v = (mid ? k1 : k0) + __shfl_xor_sync(0xFFFFFFFFu, mid ? k0 : k1, 8);
+  for (int n = N / 2, d = 16; n >= 1; n >>= 1, d >>= 1) {
+    const bool hi = (lane & d) != 0;
 #pragma unroll
-  for (int d = 4; d >= 1; d >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, d);
+    for (int i = 0; i < n; ++i) c[i] = (hi ? c[i + n] : c[i]) + __shfl_xor_sync(0xFFFFFFFFu, hi ? c[i] : c[i + n], d);
+  }
+  float v = c[0];
+#pragma unroll
+  for (int d = 16 / N; d >= 1; d >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, d);
   return v;
 }
 
-// Totals over the row of four values; `folded`: fold4 of the thread's.  Split in two, so that other work can be done in between.
-template <bool CLUSTER>
-__device__ __forceinline__ void totals_begin(const Group<CLUSTER>& g, float folded) {
-  if (!g.alone && (g.lane & 7) == 0) g.publish(g.lane >> 3, folded);
-}
-template <bool CLUSTER>
-__device__ __forceinline__ void totals_end(Group<CLUSTER>& g, float folded, float (&c)[4]) {
+// Totals over the row of N values of every thread.
+template <int N, bool CLUSTER>
+__device__ __forceinline__ void row_totals(Group<N, CLUSTER>& g, float (&c)[N]) {
+  constexpr int LANES = 32 / N;                           // that share a value
+  float v = fold<N>(c, g.lane);
   if (!g.alone) {
+    const int i = g.lane / LANES, part = g.lane % LANES;
+    if (part == 0) g.publish(i, v);
     g.meet();
-    folded = 0.f;
+    v = 0.f;
 #pragma unroll
-    for (int k = 0; k < (CLUSTER ? 4 : 1); ++k) {
-      const int w = 2 * (g.lane & 7) + 16 * k;
+    for (int k = 0; k < (CLUSTER ? MAX_ROW_WARPS : ROW_THREADS / 32) / 4; k += LANES) {
+      const int w = 4 * (part + k);
       if (w < g.width) {
-        const float2 v = read_pair(g.published(g.lane >> 3, w));
-        folded += v.x + v.y;
+        float4 x;
+        asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(x.x), "=f"(x.y), "=f"(x.z), "=f"(x.w) : "r"(g.published(i, w)) : "memory");
+        v += (x.x + x.y) + (x.z + x.w);
       }
     }
 #pragma unroll
-    for (int d = 4; d >= 1; d >>= 1) folded += __shfl_xor_sync(0xFFFFFFFFu, folded, d);
+    for (int d = LANES / 2; d >= 1; d >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, d);
     g.turn();
   }
 #pragma unroll
-  for (int i = 0; i < 4; ++i) c[i] = __shfl_sync(0xFFFFFFFFu, folded, 8 * i);
+  for (int i = 0; i < N; ++i) c[i] = __shfl_sync(0xFFFFFFFFu, v, i * LANES);
 }
 
-// Mean and 1 / deviation of two rows.  The squares are taken about each warp's own mean, and the warps are put together by
-// M = sum M_w + sum n_w (m_w - m)^2: one exchange, and no difference of large squares.  rms: all about zero.
-template <bool CLUSTER>
-__device__ __forceinline__ void row_stats(const Pair (&v)[ROWS][4], bool ok, bool layer, float eps, float inv_c, uint32_t C8,
-                                          Group<CLUSTER>& g, float2 (&st)[ROWS]) {
+// 1 / sqrt within 2^-22; of what is below 2^-126 infinity, as of 0
+__device__ __forceinline__ float rsqrt_fast(float x) {
+  float y;
+  asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+// Mean and 1 / deviation of two rows (LAYER: some norm of this kernel subtracts means; `layer`: this one does).  The squares are taken
+// about each warp's own mean, and the warps are put together by M = sum M_w + sum n_w (m_w - m)^2: one exchange, and no difference
+// of large squares.  rms: all about zero.
+template <bool LAYER, bool CLUSTER>
+__device__ __forceinline__ void row_stats(const Pair (&v)[ROWS][VECS][4], const bool (&ok)[VECS], bool layer, float eps, float inv_c,
+                                          Group<4, CLUSTER>& g, float2 (&st)[ROWS]) {
   static_assert(ROWS == 2, "two rows are folded together");
   const int half = g.lane >> 4;                           // the row whose totals this lane holds
   float m = 0.f, q[ROWS];
-  if (layer) {
-    m = fold2(horizontal(sum8(v[0])), horizontal(sum8(v[1])), g.lane) * g.inv_columns;
+  if (LAYER && layer) {
+    float s[ROWS];
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) s[r] = horizontal(act::add2(sum8(v[r][0]), sum8(v[r][1])));
+    m = fold<2>(s, g.lane) * g.inv_columns;
 #pragma unroll
     for (int r = 0; r < ROWS; ++r) {
       const Pair shift = act::both(-__shfl_sync(0xFFFFFFFFu, m, 16 * r));
-      Pair d[4];
+      q[r] = 0.f;
 #pragma unroll
-      for (int k = 0; k < 4; ++k) d[k] = act::add2(v[r][k], shift);
-      q[r] = ok ? horizontal(dot8(d, d)) : 0.f;
+      for (int j = 0; j < VECS; ++j) {
+        Pair d[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) d[k] = act::add2(v[r][j][k], shift);
+        q[r] += ok[j] ? horizontal(dot8(d, d)) : 0.f;
+      }
     }
   } else {
 #pragma unroll
-    for (int r = 0; r < ROWS; ++r) q[r] = horizontal(dot8(v[r], v[r]));
+    for (int r = 0; r < ROWS; ++r) q[r] = horizontal(act::add2(dot8(v[r][0], v[r][0]), dot8(v[r][1], v[r][1])));
   }
-  float sq = fold2(q[0], q[1], g.lane);
+  float sq = fold<2>(q, g.lane);
   if (!g.alone) {
     if ((g.lane & 15) == 0) {
-      if (layer) g.publish(half, m);
+      if (LAYER && layer) g.publish(half, m);
       g.publish(2 + half, sq);
     }
     g.meet();
     sq = 0.f;
-    if (CLUSTER) {
-      if (layer) {
-        m = 0.f;
-        for (int w = g.lane & 15; w < MAX_ROW_WARPS; w += 16) m = fmaf(columns_of(w, C8), read_word(g.published(half, w)), m);
+    constexpr int EACH = CLUSTER ? MAX_ROW_WARPS / 16 : 1, SPREAD = CLUSTER ? 8 : ROW_THREADS / 64;
+    float own[EACH];
 #pragma unroll
-        for (int d = 8; d >= 1; d >>= 1) m += __shfl_xor_sync(0xFFFFFFFFu, m, d);
-        m *= inv_c;
-      }
-      for (int w = g.lane & 15; w < MAX_ROW_WARPS; w += 16) {
+    for (int k = 0; k < EACH; ++k) {
+      const int w = (g.lane & (2 * SPREAD - 1)) + 16 * k;
+      own[k] = 0.f;
+      if (w < g.width) {
         sq += read_word(g.published(2 + half, w));
-        if (layer) {
-          const float d = read_word(g.published(half, w)) - m;
-          sq = fmaf(columns_of(w, C8) * d, d, sq);
-        }
-      }
-    } else {
-      const int w = min(g.lane & 15, g.width - 1);
-      sq = (g.lane & 15) < g.width ? read_word(g.published(2 + half, w)) : 0.f;
-      if (layer) {
-        const float own = read_word(g.published(half, w));
-        m = g.peer_columns * own;
-#pragma unroll
-        for (int d = 8; d >= 1; d >>= 1) m += __shfl_xor_sync(0xFFFFFFFFu, m, d);
-        m *= inv_c;
-        sq = fmaf(g.peer_columns * (own - m), own - m, sq);
+        if (LAYER && layer) own[k] = read_word(g.published(half, w));
       }
     }
+    if (LAYER && layer) {
+      m = 0.f;
 #pragma unroll
-    for (int d = 8; d >= 1; d >>= 1) sq += __shfl_xor_sync(0xFFFFFFFFu, sq, d);
+      for (int k = 0; k < EACH; ++k) m = fmaf(g.peer_columns[k], own[k], m);
+#pragma unroll
+      for (int d = SPREAD; d >= 1; d >>= 1) m += __shfl_xor_sync(0xFFFFFFFFu, m, d);
+      m *= inv_c;
+#pragma unroll
+      for (int k = 0; k < EACH; ++k) sq = fmaf(g.peer_columns[k] * (own[k] - m), own[k] - m, sq);
+    }
+#pragma unroll
+    for (int d = SPREAD; d >= 1; d >>= 1) sq += __shfl_xor_sync(0xFFFFFFFFu, sq, d);
     g.turn();
   }
-  const float rstd = rsqrtf(fmaf(sq, inv_c, eps));        // two units in the last place
+  const float rstd = rsqrt_fast(fmaf(sq, inv_c, eps));
 #pragma unroll
-  for (int r = 0; r < ROWS; ++r) st[r] = make_float2(layer ? __shfl_sync(0xFFFFFFFFu, m, 16 * r) : 0.f, __shfl_sync(0xFFFFFFFFu, rstd, 16 * r));
+  for (int r = 0; r < ROWS; ++r)
+    st[r] = make_float2(LAYER && layer ? __shfl_sync(0xFFFFFFFFu, m, 16 * r) : 0.f, __shfl_sync(0xFFFFFFFFu, rstd, 16 * r));
 }
 
 // A group's walk over its units, ROWS rows at a time.  SPAN: units of many rows that end with their gate row's span; else of one
@@ -397,8 +404,12 @@ constexpr int PITCH = ROW_THREADS * 16;                   // from a thread's pie
 constexpr int STATS_STAGE = 2 * ROWS * 8;                 // bytes of a warp's statistics: before, after
 constexpr int STATS_BYTES = STAGES * (ROW_THREADS / 32) * STATS_STAGE;
 BIMASK_HD constexpr int fwd_slots(bool f32, bool gate) { return (f32 ? 2 : 1) + 1 + (gate ? 1 : 0); }
-BIMASK_HD constexpr int bwd_slots(bool f32, bool gate) { return (f32 ? 4 : 2) + 2 + (gate ? 1 : 0); }
-BIMASK_HD constexpr int ring_bytes(int slots) { return STAGES * ROWS * slots * PITCH; }
+// With an fp32 stream the ring has no room for a gate's pieces: it is read from memory (L2) where it is used.
+BIMASK_HD constexpr bool bwd_gate_in_ring(bool f32, bool gate) { return gate && !f32; }
+BIMASK_HD constexpr int bwd_slots(bool f32, bool gate) { return (f32 ? 4 : 2) + 2 + (bwd_gate_in_ring(f32, gate) ? 1 : 0); }
+BIMASK_HD constexpr int bwd_values(bool post, bool wide) { return !post ? 2 : !wide ? 4 : 8; }
+BIMASK_HD constexpr int ring_bytes(int slots) { return STAGES * ROWS * VECS * slots * PITCH; }
+constexpr int FWD_CTAS = 2;                               // of the forward kernel on an SM
 
 template <bool F32>
 __device__ __forceinline__ void copy_block(uint32_t dst, const void* base, unsigned long long block, bool live) {
@@ -415,25 +426,56 @@ __device__ __forceinline__ void read_block(uint32_t at, Pair (&v)[4]) {
                  : "r"(at + h * PITCH) : "memory");
   unpack8<F32>(raw, v);
 }
-template <bool CLUSTER>
+template <int VALUES, bool CLUSTER>
 __device__ __forceinline__ void clear_exchange(float* exchange) {
-  for (int i = threadIdx.x; i < Exchange<CLUSTER>::BYTES / 4; i += blockDim.x) exchange[i] = 0.f;
+  for (int i = threadIdx.x; i < Exchange<VALUES, CLUSTER>::BYTES / 4; i += blockDim.x) exchange[i] = 0.f;
   if (CLUSTER) ptx::cluster_sync();                       // before a peer writes here, and before this CTA writes to a peer
   else __syncthreads();
 }
 
-template <bool F32, bool GATE, bool CLUSTER>
-__global__ void __launch_bounds__(ROW_THREADS, 2)
+// A thread's blocks of a row: numbers (clamped ones for loads), and whether they exist.
+struct Blocks {
+  uint32_t at[VECS], safe[VECS];
+  bool ok[VECS];
+  __device__ __forceinline__ Blocks(int warp, int lane, uint32_t C8) {
+#pragma unroll
+    for (int j = 0; j < VECS; ++j) {
+      at[j] = 32u * (uint32_t)(VECS * warp + j) + (uint32_t)lane;
+      ok[j] = at[j] < C8;
+      safe[j] = min(at[j], C8 - 1u);
+    }
+  }
+};
+// every row's blocks times (plus) a vector of parameters, if there is one
+template <bool TIMES>
+__device__ __forceinline__ void affine(Pair (&v)[ROWS][VECS][4], const float* base, const Blocks& b) {
+  if (base == nullptr) return;
+#pragma unroll
+  for (int j = 0; j < VECS; ++j) {
+    Pair w[4];
+    param8(base, b.safe[j], w);
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) {
+      if (TIMES) times8(v[r][j], w);
+      else plus8(v[r][j], w);
+    }
+  }
+}
+// address of a thread's piece: slot of block j of row r
+template <int SLOTS>
+__device__ __forceinline__ uint32_t piece(uint32_t stage_at, int r, int j, int slot) { return stage_at + ((r * VECS + j) * SLOTS + slot) * PITCH; }
+
+template <bool F32, bool GATE, bool LAYER, bool CLUSTER>
+__global__ void __launch_bounds__(ROW_THREADS, FWD_CTAS)
 residual_fwd_kernel(const __grid_constant__ ResidualParams p) {
   extern __shared__ float4 smem[];
   constexpr int SLOTS = fwd_slots(F32, GATE), X = 0, Y = F32 ? 2 : 1, G = Y + 1;
-  constexpr uint32_t STAGE = ROWS * SLOTS * PITCH;
+  constexpr uint32_t STAGE = ROWS * VECS * SLOTS * PITCH;
   float* exchange = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(smem) + ring_bytes(SLOTS));
   pdl_launch_dependents();
-  clear_exchange<CLUSTER>(exchange);
-  Group<CLUSTER> g(p, smem_addr(exchange));
-  const uint32_t col = 32u * (uint32_t)g.warp + (uint32_t)g.lane, colc = min(col, p.C8 - 1u);
-  const bool ok = col < p.C8;
+  clear_exchange<4, CLUSTER>(exchange);
+  Group<4, CLUSTER> g(p, smem_addr(exchange));
+  const Blocks b(g.warp, g.lane, p.C8);
   const uint32_t groups = blockDim.x / (32u * (uint32_t)p.warps);
   const uint32_t stride = CLUSTER ? gridDim.x / (uint32_t)p.cluster : gridDim.x * groups;
   const uint32_t ring = smem_addr(smem) + threadIdx.x * 16u;
@@ -444,14 +486,19 @@ residual_fwd_kernel(const __grid_constant__ ResidualParams p) {
   pdl_wait();
   const unsigned long long number = drop_number(p.drop);
   auto fetch = [&](const Walk<false>& w, uint32_t stage) {
+    const uint32_t at = ring + stage * STAGE;
 #pragma unroll
     for (int r = 0; r < ROWS; ++r) {
-      const bool live = ok && w.more(p) && w.t + r < w.end;
-      const uint32_t t = min(w.t + r, p.T - 1u), at = ring + stage * STAGE + r * SLOTS * PITCH;
-      const unsigned long long block = (unsigned long long)t * p.C8 + colc;
-      copy_block<F32>(at + X * PITCH, p.x, block, live);
-      if (p.y != nullptr) copy16(at + Y * PITCH, p.y + block, live);
-      if (GATE) copy16(at + G * PITCH, p.gate + (long long)(p.gate_span == 1u ? t : t / p.gate_span) * p.gate_pitch8 + colc, live);
+      const bool live = w.more(p) && w.t + r < w.end;
+      const uint32_t t = min(w.t + r, p.T - 1u);
+      const unsigned long long row = (unsigned long long)t * p.C8;
+      const uint4* gate = GATE ? p.gate + (long long)(p.gate_span == 1u ? t : t / p.gate_span) * p.gate_pitch8 : nullptr;
+#pragma unroll
+      for (int j = 0; j < VECS; ++j) {
+        copy_block<F32>(piece<SLOTS>(at, r, j, X), p.x, row + b.safe[j], live && b.ok[j]);
+        if (p.y != nullptr) copy16(piece<SLOTS>(at, r, j, Y), p.y + row + b.safe[j], live && b.ok[j]);
+        if (GATE) copy16(piece<SLOTS>(at, r, j, G), gate + b.safe[j], live && b.ok[j]);
+      }
     }
     copies_commit();
   };
@@ -461,95 +508,87 @@ residual_fwd_kernel(const __grid_constant__ ResidualParams p) {
     ahead.next(p, stride);
     fetch(ahead, stage ^ 1u);
     copies_wait<1>();
-    bool live[ROWS];
     const uint32_t at = ring + stage * STAGE;
-    unsigned long long block[ROWS];
-    Pair v[ROWS][4];
+    bool live[ROWS];
+    unsigned long long row[ROWS];
+    Pair v[ROWS][VECS][4];
 #pragma unroll
     for (int r = 0; r < ROWS; ++r) {
-      live[r] = ok && work.t + r < work.end;
-      block[r] = (unsigned long long)(work.t + r) * p.C8 + col;
+      live[r] = work.t + r < work.end;
+      row[r] = (unsigned long long)(work.t + r) * p.C8;
     }
     if (p.y != nullptr) {
 #pragma unroll
-      for (int r = 0; r < ROWS; ++r) read_block<false>(at + (r * SLOTS + Y) * PITCH, v[r]);
+      for (int r = 0; r < ROWS; ++r)
+#pragma unroll
+        for (int j = 0; j < VECS; ++j) read_block<false>(piece<SLOTS>(at, r, j, Y), v[r][j]);
       if (p.post != BIMASK_NORM_NONE) {
         float2 st[ROWS];
-        row_stats(v, ok, p.post == BIMASK_NORM_LAYER, p.eps_post, p.inv_c, p.C8, g, st);
+        row_stats<LAYER>(v, b.ok, p.post == BIMASK_NORM_LAYER, p.eps_post, p.inv_c, g, st);
 #pragma unroll
         for (int r = 0; r < ROWS; ++r) {
-          if (p.stats_post != nullptr && col == 0 && live[r]) p.stats_post[work.t + r] = st[r];
-          normalise(v[r], st[r]);
-        }
-        Pair w[4];
-        if (p.w_post != nullptr) {
-          param8(p.w_post, colc, w);
+          if (p.stats_post != nullptr && b.at[0] == 0 && live[r]) p.stats_post[work.t + r] = st[r];
 #pragma unroll
-          for (int r = 0; r < ROWS; ++r) times8(v[r], w);
+          for (int j = 0; j < VECS; ++j) normalise<LAYER>(v[r][j], st[r]);
         }
-        if (p.b_post != nullptr) {
-          param8(p.b_post, colc, w);
-#pragma unroll
-          for (int r = 0; r < ROWS; ++r) plus8(v[r], w);
-        }
+        affine<true>(v, p.w_post, b);
+        affine<false>(v, p.b_post, b);
       }
       if (p.drop.thr != 0u) {
 #pragma unroll
-        for (int r = 0; r < ROWS; ++r) drop8(v[r], block[r], number, p.drop);
+        for (int r = 0; r < ROWS; ++r)
+#pragma unroll
+          for (int j = 0; j < VECS; ++j) drop8(v[r][j], row[r] + b.at[j], number, p.drop);
       }
       if (GATE) {
 #pragma unroll
-        for (int r = 0; r < ROWS; ++r) {
-          Pair w[4];
-          read_block<false>(at + (r * SLOTS + G) * PITCH, w);
-          times8(v[r], w);
-        }
-      }
-      if (p.scale != nullptr) {
-        Pair w[4];
-        param8(p.scale, colc, w);
+        for (int r = 0; r < ROWS; ++r)
 #pragma unroll
-        for (int r = 0; r < ROWS; ++r) times8(v[r], w);
+          for (int j = 0; j < VECS; ++j) {
+            Pair w[4];
+            read_block<false>(piece<SLOTS>(at, r, j, G), w);
+            times8(v[r][j], w);
+          }
       }
+      affine<true>(v, p.scale, b);
     } else {
 #pragma unroll
-      for (int r = 0; r < ROWS; ++r) fill8(v[r], 0.f);
+      for (int r = 0; r < ROWS; ++r)
+#pragma unroll
+        for (int j = 0; j < VECS; ++j) fill8(v[r][j], 0.f);
     }
     const Pair alpha = act::both(p.alpha);
 #pragma unroll
-    for (int r = 0; r < ROWS; ++r) {
-      Pair x[4];
-      read_block<F32>(at + (r * SLOTS + X) * PITCH, x);
+    for (int r = 0; r < ROWS; ++r)
 #pragma unroll
-      for (int k = 0; k < 4; ++k) v[r][k] = act::fma2(x[k], alpha, v[r][k]);
-      if (p.xo != nullptr && live[r]) store8<F32>(p.xo, (long long)block[r], v[r]);
-    }
+      for (int j = 0; j < VECS; ++j) {
+        Pair x[4];
+        read_block<F32>(piece<SLOTS>(at, r, j, X), x);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[r][j][k] = act::fma2(x[k], alpha, v[r][j][k]);
+        if (p.xo != nullptr && live[r] && b.ok[j]) store8<F32>(p.xo, (long long)(row[r] + b.at[j]), v[r][j]);
+      }
     if (p.pre != BIMASK_NORM_NONE) {
       float2 st[ROWS];
-      if (!ok) {                                          // whatever came of the zeros there (a bias, an infinite statistic) stays out
 #pragma unroll
-        for (int r = 0; r < ROWS; ++r) fill8(v[r], 0.f);
-      }
-      row_stats(v, ok, p.pre == BIMASK_NORM_LAYER, p.eps_pre, p.inv_c, p.C8, g, st);
-      Pair w[4];
+      for (int j = 0; j < VECS; ++j)
+        if (!b.ok[j])                                     // whatever came of the zeros there (a bias, an infinite statistic) stays out
+#pragma unroll
+          for (int r = 0; r < ROWS; ++r) fill8(v[r][j], 0.f);
+      row_stats<LAYER>(v, b.ok, p.pre == BIMASK_NORM_LAYER, p.eps_pre, p.inv_c, g, st);
 #pragma unroll
       for (int r = 0; r < ROWS; ++r) {
-        if (p.stats_pre != nullptr && col == 0 && live[r]) p.stats_pre[work.t + r] = st[r];
-        normalise(v[r], st[r]);
-      }
-      if (p.w_pre != nullptr) {
-        param8(p.w_pre, colc, w);
+        if (p.stats_pre != nullptr && b.at[0] == 0 && live[r]) p.stats_pre[work.t + r] = st[r];
 #pragma unroll
-        for (int r = 0; r < ROWS; ++r) times8(v[r], w);
+        for (int j = 0; j < VECS; ++j) normalise<LAYER>(v[r][j], st[r]);
       }
-      if (p.b_pre != nullptr) {
-        param8(p.b_pre, colc, w);
-#pragma unroll
-        for (int r = 0; r < ROWS; ++r) plus8(v[r], w);
-      }
+      affine<true>(v, p.w_pre, b);
+      affine<false>(v, p.b_pre, b);
 #pragma unroll
       for (int r = 0; r < ROWS; ++r)
-        if (live[r]) store8<false>(p.n, (long long)block[r], v[r]);
+#pragma unroll
+        for (int j = 0; j < VECS; ++j)
+          if (live[r] && b.ok[j]) store8<false>(p.n, (long long)(row[r] + b.at[j]), v[r][j]);
     }
     work.next(p, stride);
     stage ^= 1u;
@@ -559,31 +598,36 @@ residual_fwd_kernel(const __grid_constant__ ResidualParams p) {
 }
 
 // ------------------------------------------------------------------------------------------
-// Gradient.  With m the dropout's multiplier, xh and yh the normalised values and u = yh w_post + b_post:
-//   D  = dx' + rstd (g - mean(g) [layer] - xh mean(g xh)),  g = w_pre dn;        dx = alpha D
-//   e  = m gate D;  dy the same norm formula on scale e w_post;                   dgate = m D scale u
-// and four column sums carry every parameter's gradient: G1 = sum dn xh (w_pre), G2 = sum dn (b_pre), A = sum e yh, B = sum e:
+// Gradient.  With m the dropout's multiplier, xh and yh the normalised values, r and q their 1 / deviation and w = scale w_post:
+//   g = w_pre dn,  E = dx' + r g,  k1 = -r mean(g xh),  k2 = -r mean(g) [layer]
+//   D = E + k1 xh + k2;   dx = alpha D;   e = m gate D;   dgate = m D (w yh + scale b_post)
+//   dy = q (w e - s2 [layer] - yh s1),  s1 = mean(w e yh),  s2 = mean(w e)
+// s1 and s2 seem to need D, and so k1 and k2, first; but D is linear in them: with z = w m gate yh,
+//   C s1 = sum z E + k1 sum z xh + k2 sum z   (s2 likewise, without yh),
+// so that all sums of a row are taken at once and its threads meet once.  The terms are those of the formula, added in another order.
+// Four column sums carry every parameter's gradient: G1 = sum dn xh (w_pre), G2 = sum dn (b_pre), A = sum e yh, B = sum e:
 //   dw_post = scale A,  db_post = scale B,  dscale = w_post A + b_post B.
 // A thread keeps its columns' sums in registers; each cluster (CTA) leaves one row of partial sums.
-// Columns and rows past the end: dx', dn and y are zeros, and so are D (its means are left out there) and every sum.
-// GATE: 0 no gate, 1 a gate whose gradient, if wanted, is a row per token, 2 one whose gradient is summed over spans.
+// Columns and rows past the end: dx', dn, y (and m of columns) are zeros, and so are D (its means are left out there) and every sum.
+// GATE: 0 no gate, 1 a gate whose gradient, if wanted, is a row per token, 2 one whose gradient is summed over spans.  WIDE: some norm
+// subtracts means, or a sum other than A and G1 is wanted; without, a row has three sums to exchange instead of eight.
 // ------------------------------------------------------------------------------------------
 enum { SUM_A = 1, SUM_B = 2, SUM_G1 = 4, SUM_G2 = 8 };
 
-template <bool F32, int GATE, bool CLUSTER>
+template <bool F32, int GATE, bool POST, bool WIDE, bool CLUSTER>
 __global__ void __launch_bounds__(ROW_THREADS, 1)
 residual_bwd_kernel(const __grid_constant__ ResidualParams p) {
   extern __shared__ float4 smem[];
   constexpr int SLOTS = bwd_slots(F32, GATE != 0), XB = F32 ? 2 : 1, X = 0, DX = XB, DN = 2 * XB, Y = DN + 1, G = Y + 1;
-  constexpr uint32_t STAGE = ROWS * SLOTS * PITCH;
+  constexpr bool GATE_RING = bwd_gate_in_ring(F32, GATE != 0);
+  constexpr int NV = bwd_values(POST, WIDE);              // a row's sums: g xh, g, z E, z xh, z, w m gate (E, xh, 1)
+  constexpr uint32_t STAGE = ROWS * VECS * SLOTS * PITCH;
   uint8_t* const after = reinterpret_cast<uint8_t*>(smem) + ring_bytes(SLOTS);
   float* const exchange = reinterpret_cast<float*>(after + STATS_BYTES);
   pdl_launch_dependents();
-  clear_exchange<CLUSTER>(exchange);
-  Group<CLUSTER> g(p, smem_addr(exchange));
-  const uint32_t col = 32u * (uint32_t)g.warp + (uint32_t)g.lane, colc = min(col, p.C8 - 1u);
-  const bool ok = col < p.C8;
-  const float inv_c = ok ? p.inv_c : 0.f;
+  clear_exchange<ROWS * NV, CLUSTER>(exchange);
+  Group<ROWS * NV, CLUSTER> g(p, smem_addr(exchange));
+  const Blocks b(g.warp, g.lane, p.C8);
   const uint32_t groups = blockDim.x / (32u * (uint32_t)p.warps);
   const uint32_t stride = CLUSTER ? gridDim.x / (uint32_t)p.cluster : gridDim.x * groups;
   const uint32_t ring = smem_addr(smem) + threadIdx.x * 16u;
@@ -594,22 +638,29 @@ residual_bwd_kernel(const __grid_constant__ ResidualParams p) {
   ahead = work;
   pdl_wait();
   const unsigned long long number = drop_number(p.drop);
-  const bool pre = p.pre != BIMASK_NORM_NONE, post = p.post != BIMASK_NORM_NONE && p.branch != 0;
-  const bool layer_pre = p.pre == BIMASK_NORM_LAYER, layer_post = p.post == BIMASK_NORM_LAYER;
+  const bool pre = p.pre != BIMASK_NORM_NONE;
+  const bool layer_pre = WIDE && p.pre == BIMASK_NORM_LAYER, layer_post = WIDE && POST && p.post == BIMASK_NORM_LAYER;
+  auto gate_row = [&](uint32_t t) { return p.gate + (long long)(p.gate_span == 1u ? t : t / p.gate_span) * p.gate_pitch8; };
   auto fetch = [&](const Walk<GATE == 2>& w, uint32_t stage) {
     const bool more = w.more(p);
+    const uint32_t at = ring + stage * STAGE;
 #pragma unroll
     for (int r = 0; r < ROWS; ++r) {
-      const bool live = ok && more && w.t + r < w.end;
-      const uint32_t t = min(w.t + r, p.T - 1u), at = ring + stage * STAGE + r * SLOTS * PITCH;
-      const unsigned long long block = (unsigned long long)t * p.C8 + colc;
-      if (pre) {
-        copy_block<F32>(at + X * PITCH, p.xo, block, live);
-        copy16(at + DN * PITCH, p.dn + block, live);
+      const bool live = more && w.t + r < w.end;
+      const uint32_t t = min(w.t + r, p.T - 1u);
+      const unsigned long long row = (unsigned long long)t * p.C8;
+#pragma unroll
+      for (int j = 0; j < VECS; ++j) {
+        const bool there = live && b.ok[j];
+        const unsigned long long block = row + b.safe[j];
+        if (pre) {
+          copy_block<F32>(piece<SLOTS>(at, r, j, X), p.xo, block, there);
+          copy16(piece<SLOTS>(at, r, j, DN), p.dn + block, there);
+        }
+        if (p.dxo != nullptr) copy_block<F32>(piece<SLOTS>(at, r, j, DX), p.dxo, block, there);
+        if (p.y != nullptr) copy16(piece<SLOTS>(at, r, j, Y), p.y + block, there);
+        if (GATE_RING) copy16(piece<SLOTS>(at, r, j, G), gate_row(t) + b.safe[j], there);
       }
-      if (p.dxo != nullptr) copy_block<F32>(at + DX * PITCH, p.dxo, block, live);
-      if (p.y != nullptr) copy16(at + Y * PITCH, p.y + block, live);
-      if (GATE != 0) copy16(at + G * PITCH, p.gate + (long long)(p.gate_span == 1u ? t : t / p.gate_span) * p.gate_pitch8 + colc, live);
     }
     if (g.lane < 2 * ROWS) {                              // lanes 0, 1: the rows' statistics before, 2, 3: after
       const uint32_t t = w.t + (g.lane & 1);
@@ -618,10 +669,15 @@ residual_bwd_kernel(const __grid_constant__ ResidualParams p) {
     }
     copies_commit();
   };
-  Pair sums[4][4], fsum[4];
+  Pair sum_a[VECS][4], sum_g1[VECS][4], sum_b[VECS][4], sum_g2[VECS][4], fsum[VECS][4];
 #pragma unroll
-  for (int a = 0; a < 4; ++a) fill8(sums[a], 0.f);
-  fill8(fsum, 0.f);
+  for (int j = 0; j < VECS; ++j) {
+    fill8(sum_a[j], 0.f);
+    fill8(sum_g1[j], 0.f);
+    fill8(sum_b[j], 0.f);
+    fill8(sum_g2[j], 0.f);
+    fill8(fsum[j], 0.f);
+  }
   fetch(ahead, 0);
   uint32_t stage = 0;
   while (work.more(p)) {
@@ -630,160 +686,202 @@ residual_bwd_kernel(const __grid_constant__ ResidualParams p) {
     fetch(ahead, stage ^ 1u);
     copies_wait<1>();
     __syncwarp();                                         // the statistics are other lanes' copies
-    bool live[ROWS];
     const uint32_t at = ring + stage * STAGE, st_at = stats + stage * STATS_STAGE;
-    unsigned long long block[ROWS];
-    Pair D[ROWS][4];
-    uint4 bits[ROWS];
+    bool live[ROWS];
+    unsigned long long row[ROWS];
+    Pair E[ROWS][VECS][4], xh[ROWS][VECS][4], yh[ROWS][VECS][4], m[ROWS][VECS][4];
+    float c[ROWS * NV], r_pre[ROWS], r_post[ROWS];
+#pragma unroll
+    for (int i = 0; i < ROWS * NV; ++i) c[i] = 0.f;
 #pragma unroll
     for (int r = 0; r < ROWS; ++r) {
-      live[r] = ok && work.t + r < work.end;
-      block[r] = (unsigned long long)(work.t + r) * p.C8 + col;
-      if (p.dxo != nullptr) read_block<F32>(at + (r * SLOTS + DX) * PITCH, D[r]);
-      else fill8(D[r], 0.f);
-    }
-    auto draw = [&]() {
-      if (p.drop.thr != 0u) {
+      live[r] = work.t + r < work.end;
+      row[r] = (unsigned long long)(work.t + r) * p.C8;
+      r_pre[r] = 0.f;
+      r_post[r] = 1.f;
 #pragma unroll
-        for (int r = 0; r < ROWS; ++r) bits[r] = philox(block[r], number, p.drop);
+      for (int j = 0; j < VECS; ++j) {
+        if (p.dxo != nullptr) read_block<F32>(piece<SLOTS>(at, r, j, DX), E[r][j]);
+        else fill8(E[r][j], 0.f);
       }
-    };
+    }
     if (pre) {
-      Pair xh[ROWS][4], gr[ROWS][4];
-      float c[4], rstd[ROWS];
-      Pair w[4];
-      if (p.w_pre != nullptr) param8(p.w_pre, colc, w);
+      Pair w[VECS][4];
+      if (p.w_pre != nullptr)
+#pragma unroll
+        for (int j = 0; j < VECS; ++j) param8(p.w_pre, b.safe[j], w[j]);
 #pragma unroll
       for (int r = 0; r < ROWS; ++r) {
         const float2 st = read_pair(st_at + 8 * r);
-        rstd[r] = st.y;
-        read_block<F32>(at + (r * SLOTS + X) * PITCH, xh[r]);
-        read_block<false>(at + (r * SLOTS + DN) * PITCH, gr[r]);
-        normalise(xh[r], st);
+        r_pre[r] = st.y;
+        const Pair rs = act::both(st.y);
+        Pair s = act::both(0.f), s0 = act::both(0.f);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) sums[2][k] = act::fma2(gr[r][k], xh[r][k], sums[2][k]);
-        if (p.want & SUM_G2) plus8(sums[3], gr[r]);
-        if (p.w_pre != nullptr) times8(gr[r], w);
-        c[2 * r] = horizontal(dot8(gr[r], xh[r]));
-        c[2 * r + 1] = layer_pre ? horizontal(sum8(gr[r])) : 0.f;
-      }
-      const float folded = fold4(c, g.lane);
-      totals_begin(g, folded);
-      draw();                                             // needs nothing of the others: done while they arrive
-      totals_end(g, folded, c);
+        for (int j = 0; j < VECS; ++j) {
+          Pair gr[4];
+          read_block<F32>(piece<SLOTS>(at, r, j, X), xh[r][j]);
+          read_block<false>(piece<SLOTS>(at, r, j, DN), gr);
+          normalise<WIDE>(xh[r][j], st);
 #pragma unroll
-      for (int r = 0; r < ROWS; ++r) {
-        const float scaled = -rstd[r] * inv_c;
-        const Pair c1 = act::both(c[2 * r] * scaled), rs = act::both(rstd[r]);
-        if (layer_pre) {
-          const Pair c2 = act::both(c[2 * r + 1] * scaled);
+          for (int k = 0; k < 4; ++k) sum_g1[j][k] = act::fma2(gr[k], xh[r][j][k], sum_g1[j][k]);
+          if (WIDE) plus8(sum_g2[j], gr);
+          if (p.w_pre != nullptr) times8(gr, w[j]);
 #pragma unroll
-          for (int k = 0; k < 4; ++k) D[r][k] = act::add2(D[r][k], c2);
+          for (int k = 0; k < 4; ++k) s = act::fma2(gr[k], xh[r][j][k], s);
+          if (WIDE) s0 = act::add2(s0, sum8(gr));
+#pragma unroll
+          for (int k = 0; k < 4; ++k) E[r][j][k] = act::fma2(gr[k], rs, E[r][j][k]);
         }
-#pragma unroll
-        for (int k = 0; k < 4; ++k) D[r][k] = act::fma2(gr[r][k], rs, act::fma2(xh[r][k], c1, D[r][k]));
+        c[r * NV] = horizontal(s);
+        if (layer_pre) c[r * NV + 1] = horizontal(s0);
       }
     } else {
-      draw();
+#pragma unroll
+      for (int r = 0; r < ROWS; ++r)
+#pragma unroll
+        for (int j = 0; j < VECS; ++j) fill8(xh[r][j], 0.f);
     }
-    if (p.dx != nullptr) {
-      const Pair alpha = act::both(p.alpha);
+    Pair w[VECS][4];                                      // scale w_post
+    const bool weighted = p.scale != nullptr || (POST && p.w_post != nullptr);
+    if (p.branch) {
+#pragma unroll
+      for (int j = 0; j < VECS; ++j) {
+        if (POST && p.w_post != nullptr) param8(p.w_post, b.safe[j], w[j]);
+        if (p.scale != nullptr) {
+          Pair s[4];
+          param8(p.scale, b.safe[j], s);
+          if (POST && p.w_post != nullptr) times8(w[j], s);
+          else
+#pragma unroll
+            for (int k = 0; k < 4; ++k) w[j][k] = s[k];
+        }
+      }
 #pragma unroll
       for (int r = 0; r < ROWS; ++r) {
-        Pair o[4];
+        float2 st = make_float2(0.f, 1.f);
+        if (POST) st = read_pair(st_at + 8 * (ROWS + r));
+        r_post[r] = st.y;
+        Pair ze = act::both(0.f), zx = ze, z0 = ze, te = ze, tx = ze, t0 = ze;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) o[k] = act::mul2(D[r][k], alpha);
-        if (live[r]) store8<F32>(p.dx, (long long)block[r], o);
+        for (int j = 0; j < VECS; ++j) {
+          fill8(m[r][j], b.ok[j] ? 1.f : 0.f);            // nothing past the end in the sums with z
+          if (p.drop.thr != 0u) drop8(m[r][j], row[r] + b.at[j], number, p.drop);
+          if (p.y != nullptr) read_block<false>(piece<SLOTS>(at, r, j, Y), yh[r][j]);
+          else fill8(yh[r][j], 0.f);
+          if (POST) {
+            normalise<WIDE>(yh[r][j], st);
+            Pair z[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) z[k] = m[r][j][k];
+            if (weighted) times8(z, w[j]);
+            if (GATE != 0) {
+              Pair gt[4];
+              if (GATE_RING) read_block<false>(piece<SLOTS>(at, r, j, G), gt);
+              else unpack8<false>(Vec8<false>{__ldg(gate_row(min(work.t + r, p.T - 1u)) + b.safe[j])}, gt);
+              times8(z, gt);
+            }
+            if (WIDE) {
+#pragma unroll
+              for (int k = 0; k < 4; ++k) te = act::fma2(z[k], E[r][j][k], te), tx = act::fma2(z[k], xh[r][j][k], tx);
+              t0 = act::add2(t0, sum8(z));
+            }
+            times8(z, yh[r][j]);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) ze = act::fma2(z[k], E[r][j][k], ze), zx = act::fma2(z[k], xh[r][j][k], zx);
+            if (WIDE) z0 = act::add2(z0, sum8(z));
+          }
+        }
+        if (POST) {
+          c[r * NV + 2] = horizontal(ze);
+          c[r * NV + 3] = horizontal(zx);
+          if (WIDE) {
+            c[r * NV + 4] = horizontal(z0);
+            if (layer_post) { c[r * NV + 5] = horizontal(te); c[r * NV + 6] = horizontal(tx); c[r * NV + 7] = horizontal(t0); }
+          }
+        }
+      }
+    }
+    if (pre || POST) row_totals(g, c);
+    float s1[ROWS], s2[ROWS];
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) {
+      const float scaled = -r_pre[r] * p.inv_c, f1 = c[r * NV] * scaled, f2 = WIDE ? c[r * NV + 1] * scaled : 0.f;
+      s1[r] = s2[r] = 0.f;
+      if (POST) {
+        s1[r] = c[r * NV + 2] + f1 * c[r * NV + 3];
+        if (WIDE) {
+          s1[r] += f2 * c[r * NV + 4];
+          s2[r] = c[r * NV + 5] + f1 * c[r * NV + 6] + f2 * c[r * NV + 7];
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < VECS; ++j) {
+        const Pair k1 = act::both(f1), k2 = act::both(f2);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) E[r][j][k] = act::fma2(xh[r][j][k], k1, WIDE ? act::add2(E[r][j][k], k2) : E[r][j][k]);      // D
+        if (p.dx != nullptr && live[r] && b.ok[j]) {
+          const Pair alpha = act::both(p.alpha);
+          Pair o[4];
+#pragma unroll
+          for (int k = 0; k < 4; ++k) o[k] = act::mul2(E[r][j][k], alpha);
+          store8<F32>(p.dx, (long long)(row[r] + b.at[j]), o);
+        }
       }
     }
     if (p.branch) {
-      Pair yh[ROWS][4];
-      float c[4], rstd[ROWS];
-      Pair w[4];                                          // scale w_post
-      const bool weighted = p.scale != nullptr || p.w_post != nullptr;
-      if (p.w_post != nullptr) param8(p.w_post, colc, w);
-      if (p.scale != nullptr) {
-        Pair s[4];
-        param8(p.scale, colc, s);
-        if (p.w_post != nullptr) times8(w, s);
-        else
-#pragma unroll
-          for (int k = 0; k < 4; ++k) w[k] = s[k];
-      }
 #pragma unroll
       for (int r = 0; r < ROWS; ++r) {
-        rstd[r] = 1.f;
-        if (p.y != nullptr) read_block<false>(at + (r * SLOTS + Y) * PITCH, yh[r]);
-        else fill8(yh[r], 0.f);
-        if (post) {
-          const float2 st = read_pair(st_at + 8 * (ROWS + r));
-          rstd[r] = st.y;
-          normalise(yh[r], st);
-        }
-        if (p.drop.thr != 0u) {
-          D[r][0] = drop_pair(D[r][0], bits[r].x, p.drop.thr, p.drop.scale);
-          D[r][1] = drop_pair(D[r][1], bits[r].y, p.drop.thr, p.drop.scale);
-          D[r][2] = drop_pair(D[r][2], bits[r].z, p.drop.thr, p.drop.scale);
-          D[r][3] = drop_pair(D[r][3], bits[r].w, p.drop.thr, p.drop.scale);
-        }
-        if (GATE != 0) {
-          if (GATE == 2 || p.dgate != nullptr) {          // scale u
-            Pair u[4];
+        const float scaled = -r_post[r] * p.inv_c;
+        const Pair k1 = act::both(s1[r] * scaled), k2 = act::both(s2[r] * scaled), rs = act::both(r_post[r]);
 #pragma unroll
-            for (int k = 0; k < 4; ++k) u[k] = yh[r][k];
-            if (weighted) times8(u, w);
-            if (p.b_post != nullptr) {
-              Pair b[4];
-              param8(p.b_post, colc, b);
-              if (p.scale != nullptr) {
-                Pair s[4];
-                param8(p.scale, colc, s);
-                times8(b, s);
+        for (int j = 0; j < VECS; ++j) {
+          times8(E[r][j], m[r][j]);
+          if (GATE != 0) {
+            if (GATE == 2 || p.dgate != nullptr) {        // scale u
+              Pair u[4];
+#pragma unroll
+              for (int k = 0; k < 4; ++k) u[k] = yh[r][j][k];
+              if (weighted) times8(u, w[j]);
+              if (POST && p.b_post != nullptr) {
+                Pair bias[4];
+                param8(p.b_post, b.safe[j], bias);
+                if (p.scale != nullptr) {
+                  Pair s[4];
+                  param8(p.scale, b.safe[j], s);
+                  times8(bias, s);
+                }
+                plus8(u, bias);
               }
-              plus8(u, b);
-            }
-            if (GATE == 2) {
+              if (GATE == 2) {
 #pragma unroll
-              for (int k = 0; k < 4; ++k) fsum[k] = act::fma2(D[r][k], u[k], fsum[k]);
-            } else {
-              times8(u, D[r]);
-              if (live[r]) store8<false>(p.dgate, (long long)(work.t + r) * p.gate_pitch8 + col, u);
+                for (int k = 0; k < 4; ++k) fsum[j][k] = act::fma2(E[r][j][k], u[k], fsum[j][k]);
+              } else {
+                times8(u, E[r][j]);
+                if (live[r] && b.ok[j]) store8<false>(p.dgate, (long long)(work.t + r) * p.gate_pitch8 + b.at[j], u);
+              }
             }
+            Pair gt[4];
+            if (GATE_RING) read_block<false>(piece<SLOTS>(at, r, j, G), gt);
+            else unpack8<false>(Vec8<false>{__ldg(gate_row(min(work.t + r, p.T - 1u)) + b.safe[j])}, gt);
+            times8(E[r][j], gt);
           }
-          Pair gt[4];
-          read_block<false>(at + (r * SLOTS + G) * PITCH, gt);
-          times8(D[r], gt);
+#pragma unroll
+          for (int k = 0; k < 4; ++k) sum_a[j][k] = act::fma2(E[r][j][k], yh[r][j][k], sum_a[j][k]);
+          if (POST && WIDE) plus8(sum_b[j], E[r][j]);
+          if (weighted) times8(E[r][j], w[j]);
+          if (POST) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) E[r][j][k] = act::fma2(E[r][j][k], rs, WIDE ? act::fma2(yh[r][j][k], k1, k2) : act::mul2(yh[r][j][k], k1));
+          }
+          if (p.dy != nullptr && live[r] && b.ok[j]) store8<false>(p.dy, (long long)(row[r] + b.at[j]), E[r][j]);
         }
-#pragma unroll
-        for (int k = 0; k < 4; ++k) sums[0][k] = act::fma2(D[r][k], yh[r][k], sums[0][k]);
-        if (p.want & SUM_B) plus8(sums[1], D[r]);
-        if (weighted) times8(D[r], w);
-      }
-      if (post) {
-#pragma unroll
-        for (int r = 0; r < ROWS; ++r) {
-          c[2 * r] = horizontal(dot8(D[r], yh[r]));
-          c[2 * r + 1] = layer_post ? horizontal(sum8(D[r])) : 0.f;
-        }
-        const float folded = fold4(c, g.lane);
-        totals_begin(g, folded);
-        totals_end(g, folded, c);
-#pragma unroll
-        for (int r = 0; r < ROWS; ++r) {
-          const float scaled = -rstd[r] * inv_c;
-          const Pair c1 = act::both(c[2 * r] * scaled), c2 = act::both(layer_post ? c[2 * r + 1] * scaled : 0.f), rs = act::both(rstd[r]);
-#pragma unroll
-          for (int k = 0; k < 4; ++k) D[r][k] = act::fma2(D[r][k], rs, act::fma2(yh[r][k], c1, c2));
-        }
-      }
-      if (p.dy != nullptr) {
-#pragma unroll
-        for (int r = 0; r < ROWS; ++r)
-          if (live[r]) store8<false>(p.dy, (long long)block[r], D[r]);
       }
       if (GATE == 2 && work.last()) {
-        if (ok) store8<true>(p.gate_sums, (long long)work.unit * p.C8 + col, fsum);
-        fill8(fsum, 0.f);
+#pragma unroll
+        for (int j = 0; j < VECS; ++j) {
+          if (b.ok[j]) store8<true>(p.gate_sums, (long long)work.unit * p.C8 + b.at[j], fsum[j]);
+          fill8(fsum[j], 0.f);
+        }
       }
     }
     work.next(p, stride);
@@ -792,32 +890,43 @@ residual_bwd_kernel(const __grid_constant__ ResidualParams p) {
   copies_wait<0>();
   // the groups' sums are added through the ring, in their order
   int slot = 0;
-#pragma unroll
-  for (int a = 0; a < 4; ++a) {
-    if (!(p.want & (1 << a))) continue;                   // the same for every thread
+  auto leave = [&](int which, Pair (&sum)[VECS][4]) {
+    if (!(p.want & which)) return;                        // the same for every thread
+    float* const out = p.sums + ((size_t)(CLUSTER ? blockIdx.x / (uint32_t)p.cluster : blockIdx.x) * __popc(p.want) + slot) * p.C8 * 8;
     if (groups > 1) {
       __syncthreads();
-      const Vec8<true> v = pack8<true>(sums[a]);
       uint4* mine = reinterpret_cast<uint4*>(smem) + threadIdx.x;
-      mine[0] = v.w[0];
-      mine[ROW_THREADS] = v.w[1];
+#pragma unroll
+      for (int j = 0; j < VECS; ++j) {
+        const Vec8<true> v = pack8<true>(sum[j]);
+        mine[2 * j * ROW_THREADS] = v.w[0];
+        mine[(2 * j + 1) * ROW_THREADS] = v.w[1];
+      }
       __syncthreads();
     }
-    if (g.group == 0 && ok) {
-      for (uint32_t o = 1; o < groups; ++o) {
-        Pair q[4];
-        read_block<true>(ring + o * (uint32_t)p.warps * 512u, q);
-        plus8(sums[a], q);
+    if (g.group == 0) {
+#pragma unroll
+      for (int j = 0; j < VECS; ++j) {
+        for (uint32_t o = 1; o < groups; ++o) {
+          Pair q[4];
+          read_block<true>(ring + o * (uint32_t)p.warps * 512u + 2 * j * PITCH, q);
+          plus8(sum[j], q);
+        }
+        if (b.ok[j]) store8<true>(out, b.at[j], sum[j]);
       }
-      store8<true>(p.sums, ((long long)(CLUSTER ? blockIdx.x / (uint32_t)p.cluster : blockIdx.x) * __popc(p.want) + slot) * p.C8 + col, sums[a]);
     }
     ++slot;
-  }
+  };
+  leave(SUM_A, sum_a);
+  if (POST && WIDE) leave(SUM_B, sum_b);
+  leave(SUM_G1, sum_g1);
+  if (WIDE) leave(SUM_G2, sum_g2);
   if (CLUSTER) ptx::cluster_sync();                       // shared memory outlives the peers' writes to it
 }
 
-// The parameters' gradients from the CTAs' partial sums: a CTA covers 8 float4 columns, its 32 row slots take the partial
-// rows in turn and are added through shared memory, in a fixed order.
+// The parameters' gradients from the clusters' partial sums: a CTA covers eight float4 columns of one wanted array (blockIdx.y), its
+// 32 row slots take the partial rows in turn and are added through shared memory, in a fixed order.  A carries dscale with it, and B
+// where dscale has a part from there.
 struct ResidualReduce {
   const float4* sums;
   int slots, want, C4;
@@ -829,49 +938,57 @@ __device__ __forceinline__ float4 mul4(float4 a, float4 b) { return make_float4(
 
 __global__ void __launch_bounds__(256)
 residual_reduce_kernel(const ResidualReduce p) {
+  __shared__ float4 red[2][32][8];
   pdl_launch_dependents();
-  pdl_wait();
-  __shared__ float4 red[32][8];
   const int lane = threadIdx.x & 7, slot = threadIdx.x >> 3;
-  const int e = blockIdx.x * 8 + lane;
-  const int arrays = __popc(p.want);
-  const float4 zero = make_float4(0.f, 0.f, 0.f, 0.f);
-  float4 total[4];
-  int at = 0;
-#pragma unroll
-  for (int a = 0; a < 4; ++a) {
-    total[a] = zero;
-    if (!(p.want & (1 << a))) continue;
-    float4 acc = zero;
-    if (e < p.C4)
-#pragma unroll 8
-      for (int s = slot; s < p.slots; s += 32) acc = add4(acc, p.sums[((size_t)s * arrays + at) * p.C4 + e]);
-    ++at;
-    __syncthreads();
-    red[slot][lane] = acc;
-    __syncthreads();
-#pragma unroll
-    for (int half = 16; half >= 1; half >>= 1) {
-      if (slot < half) {
-        acc = add4(acc, red[slot + half][lane]);
-        red[slot][lane] = acc;
-      }
-      __syncthreads();
+  const int e = blockIdx.x * 8 + lane, arrays = __popc(p.want);
+  int which = p.want;                                     // its bit number blockIdx.y
+  for (unsigned k = 0; k < blockIdx.y; ++k) which &= which - 1;
+  which &= -which;
+  const bool both = which == SUM_A && p.dscale != nullptr && p.b_post != nullptr;        // then B comes next after A
+  pdl_wait();
+  float4 acc[2];
+  acc[0] = acc[1] = make_float4(0.f, 0.f, 0.f, 0.f);
+  if (e < p.C4) {
+    const float4* src = p.sums + (size_t)blockIdx.y * p.C4 + e;
+    const size_t step = (size_t)arrays * p.C4;
+#pragma unroll 5
+    for (int s = slot; s < p.slots; s += 32) {
+      acc[0] = add4(acc[0], src[s * step]);
+      if (both) acc[1] = add4(acc[1], src[s * step + p.C4]);
     }
-    total[a] = acc;
+  }
+#pragma unroll
+  for (int i = 0; i < 2; ++i) red[i][slot][lane] = acc[i];
+  __syncthreads();
+#pragma unroll
+  for (int half = 16; half >= 1; half >>= 1) {
+    if (slot < half) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        acc[i] = add4(acc[i], red[i][slot + half][lane]);
+        red[i][slot][lane] = acc[i];
+      }
+    }
+    __syncthreads();
   }
   if (slot != 0 || e >= p.C4) return;
   const float4 one = make_float4(1.f, 1.f, 1.f, 1.f);
-  const float4 s = p.scale != nullptr ? __ldg(p.scale + e) : one, w = p.w_post != nullptr ? __ldg(p.w_post + e) : one;
-  if (p.dw_post != nullptr) p.dw_post[e] = mul4(s, total[0]);
-  if (p.db_post != nullptr) p.db_post[e] = mul4(s, total[1]);
-  if (p.dscale != nullptr) {
-    float4 d = mul4(w, total[0]);
-    if (p.b_post != nullptr) d = add4(d, mul4(__ldg(p.b_post + e), total[1]));
-    p.dscale[e] = d;
+  const float4 s = p.scale != nullptr ? __ldg(p.scale + e) : one;
+  if (which == SUM_A) {
+    if (p.dw_post != nullptr) p.dw_post[e] = mul4(s, acc[0]);
+    if (p.dscale != nullptr) {
+      float4 d = mul4(p.w_post != nullptr ? __ldg(p.w_post + e) : one, acc[0]);
+      if (both) d = add4(d, mul4(__ldg(p.b_post + e), acc[1]));
+      p.dscale[e] = d;
+    }
+  } else if (which == SUM_B) {
+    if (p.db_post != nullptr) p.db_post[e] = mul4(s, acc[0]);
+  } else if (which == SUM_G1) {
+    p.dw_pre[e] = acc[0];
+  } else {
+    p.db_pre[e] = acc[0];
   }
-  if (p.dw_pre != nullptr) p.dw_pre[e] = total[2];
-  if (p.db_pre != nullptr) p.db_pre[e] = total[3];
 }
 
 // dgate of a row that serves a span of tokens: the sum of its units, in order.
@@ -902,8 +1019,8 @@ struct RowPlan {
 // ctas: how many the card holds.  span > 1: units end where a gate row's span ends, and are as many as the groups of warps.
 RowPlan plan_rows(int T, int C, int span, int ctas) {
   RowPlan b = {};
-  const int all = (C / 8 + 31) / 32;                      // warps of a row
-  b.cluster = all > 32 ? 4 : all > 16 ? 2 : 1;
+  const int all = (C / 8 + 32 * VECS - 1) / (32 * VECS), most = ROW_THREADS / 32;         // warps of a row, of a CTA
+  b.cluster = all > 2 * most ? 4 : all > most ? 2 : 1;
   b.warps = (all + b.cluster - 1) / b.cluster;
   b.groups = ROW_THREADS / 32 / b.warps;
   b.threads = 32 * b.warps * b.groups;
@@ -1028,15 +1145,19 @@ static ResidualParams residual_params(const bimask_residual_args& a) {
 
 int launch_residual_fwd(const bimask_residual_args& a, cudaStream_t s) {
   ResidualParams p = residual_params(a);
-  const RowPlan b = plan_rows(a.T, a.C, 1, 2 * sm_count());
+  const RowPlan b = plan_rows(a.T, a.C, 1, FWD_CTAS * sm_count());
   take_plan(p, b);
-  auto run = [&](auto f32, auto gate, auto cluster) -> int {
-    constexpr bool F = decltype(f32)::value, G = decltype(gate)::value, K = decltype(cluster)::value;
-    return launch_rows(residual_fwd_kernel<F, G, K>, b, ring_bytes(fwd_slots(F, G)) + Exchange<K>::BYTES, s, p);
-  };
   using Yes = std::true_type;
   using No = std::false_type;
-  auto pick = [&](auto f32, auto gate) -> int { return b.cluster > 1 ? run(f32, gate, Yes()) : run(f32, gate, No()); };
+  auto run = [&](auto f32, auto gate, auto layer, auto cluster) -> int {
+    constexpr bool F = decltype(f32)::value, G = decltype(gate)::value, L = decltype(layer)::value, K = decltype(cluster)::value;
+    return launch_rows(residual_fwd_kernel<F, G, L, K>, b, ring_bytes(fwd_slots(F, G)) + Exchange<4, K>::BYTES, s, p);
+  };
+  const bool means = p.post == BIMASK_NORM_LAYER || p.pre == BIMASK_NORM_LAYER;
+  auto pick = [&](auto f32, auto gate) -> int {
+    if (b.cluster > 1) return means ? run(f32, gate, Yes(), Yes()) : run(f32, gate, No(), Yes());
+    return means ? run(f32, gate, Yes(), No()) : run(f32, gate, No(), No());
+  };
   const bool gate = p.gate_span != 0;
   const int rc = a.stream_type == BIMASK_TYPE_F32 ? (gate ? pick(Yes(), Yes()) : pick(Yes(), No())) : (gate ? pick(No(), Yes()) : pick(No(), No()));
   if (rc != BIMASK_OK) return rc;
@@ -1057,13 +1178,22 @@ int launch_residual_bwd(const bimask_residual_args& a, cudaStream_t s) {
   p.want = (a.dw_post || scale ? SUM_A : 0) | (a.db_post || (scale && a.b_post) ? SUM_B : 0) | (a.dw_pre ? SUM_G1 : 0) | (a.db_pre ? SUM_G2 : 0);
   p.sums = reinterpret_cast<float*>(a.ws);
   if (spanned) p.gate_sums = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(a.ws) + column_sums_bytes(a.T, a.C, (int)p.gate_span));
-  auto run = [&](auto f32, auto gate, auto cluster) -> int {
-    constexpr bool F = decltype(f32)::value, K = decltype(cluster)::value;
-    constexpr int G = decltype(gate)::value, bytes = ring_bytes(bwd_slots(F, G != 0)) + STATS_BYTES + Exchange<K>::BYTES;
+  using Yes = std::true_type;
+  using No = std::false_type;
+  auto run = [&](auto f32, auto gate, auto post, auto wide, auto cluster) -> int {
+    constexpr bool F = decltype(f32)::value, P = decltype(post)::value, W = decltype(wide)::value, K = decltype(cluster)::value;
+    constexpr int G = decltype(gate)::value;
+    constexpr int bytes = ring_bytes(bwd_slots(F, G != 0)) + STATS_BYTES + Exchange<bwd_values(P, W) * ROWS, K>::BYTES;
     static_assert(bytes <= 227 * 1024, "shared memory of a CTA");
-    return launch_rows(residual_bwd_kernel<F, G, K>, b, bytes, s, p);
+    return launch_rows(residual_bwd_kernel<F, G, P, W, K>, b, bytes, s, p);
   };
-  auto pick2 = [&](auto f32, auto gate) -> int { return b.cluster > 1 ? run(f32, gate, std::true_type()) : run(f32, gate, std::false_type()); };
+  const bool after = p.post != BIMASK_NORM_NONE && p.branch;
+  const bool wide = (p.post == BIMASK_NORM_LAYER && p.branch) || p.pre == BIMASK_NORM_LAYER || (p.want & (SUM_B | SUM_G2)) != 0;
+  auto pick3 = [&](auto f32, auto gate, auto post) -> int {
+    if (b.cluster > 1) return wide ? run(f32, gate, post, Yes(), Yes()) : run(f32, gate, post, No(), Yes());
+    return wide ? run(f32, gate, post, Yes(), No()) : run(f32, gate, post, No(), No());
+  };
+  auto pick2 = [&](auto f32, auto gate) -> int { return after ? pick3(f32, gate, Yes()) : pick3(f32, gate, No()); };
   auto pick = [&](auto f32) -> int {
     if (spanned) return pick2(f32, std::integral_constant<int, 2>());
     if (p.gate_span != 0) return pick2(f32, std::integral_constant<int, 1>());
@@ -1085,7 +1215,7 @@ int launch_residual_bwd(const bimask_residual_args& a, cudaStream_t s) {
     r.db_post = reinterpret_cast<float4*>(a.db_post);
     r.dw_pre = reinterpret_cast<float4*>(a.dw_pre);
     r.db_pre = reinterpret_cast<float4*>(a.db_pre);
-    BIMASK_CUDA_OK(launch_pdl(residual_reduce_kernel, (unsigned)((r.C4 + 7) / 8), 256, 0, s, r));
+    BIMASK_CUDA_OK(launch_pdl(residual_reduce_kernel, dim3((r.C4 + 7) / 8, __builtin_popcount(p.want)), 256, 0, s, r));
     count_launch();
   }
   if (p.gate_sums != nullptr) {

@@ -213,8 +213,8 @@ FORMS = [(0, 1), (0, 2), (1, 1), (2, 2), (1, 2), (2, 1), (1, 0), (2, 0), (0, 0)]
 @pytest.mark.parametrize("T,C", SIZES)
 @pytest.mark.parametrize("stream", TYPES)
 def test_against_64_bits(T, C, stream):
-    for i, (post, pre) in enumerate(FORMS):
-        span = (0, 1, 2, T, T + 3)[i % 5]
+    for i, ((post, pre), k) in enumerate(itertools.product(FORMS, range(5 if C < 600 else 1))):
+        span = (0, 1, 2, T, T + 3)[k if C < 600 else i % 5]
         q = Problem(T, C, post, pre, stream, span=span, scale=i % 2 == 0, bias=i % 3 != 0, p=(0.0, 0.3)[(i // 2) % 2], alpha=(1.0, 0.8)[i % 2])
         f = q.forward()
         q.check_forward(f)
