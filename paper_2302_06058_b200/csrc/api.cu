@@ -433,7 +433,7 @@ int bimask_act_dropout_bwd(const uint16_t* dY, const int8_t* Zq, const uint8_t* 
   int rc = check_act_bwd("bimask_act_dropout_bwd", dY, Zq, Zs, act, T, C, dZ, dbias, ws, ws_bytes);
   if (rc != BIMASK_OK) return rc;
   if ((rc = check_drop("bimask_act_dropout_bwd", drop)) != BIMASK_OK) return rc;
-  return launch_act_bwd(dY, Zq, Zs, act, T, C, dZ, dbias, reinterpret_cast<float*>(ws), (cudaStream_t)stream, drop);
+  return launch_act_dropout_bwd(dY, Zq, Zs, act, *drop, T, C, dZ, dbias, reinterpret_cast<float*>(ws), (cudaStream_t)stream);
 }
 
 size_t bimask_residual_norm_workspace_bytes(int T, int C, int gate_span) {

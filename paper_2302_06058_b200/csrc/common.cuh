@@ -276,7 +276,9 @@ int launch_ckpt_unpack(const int8_t* q, const uint8_t* s, int act, int T, int C,
                        const bimask_dropout_args* drop = nullptr);
 size_t act_bwd_partial_bytes(int T, int C);
 int launch_act_bwd(const uint16_t* dY, const int8_t* zq, const uint8_t* zs, int act, int T, int C, uint16_t* dZ, float* dbias,
-                   float* partial, cudaStream_t st, const bimask_dropout_args* drop = nullptr);
+                   float* partial, cudaStream_t st);
+int launch_act_dropout_bwd(const uint16_t* dY, const int8_t* zq, const uint8_t* zs, int act, const bimask_dropout_args& drop, int T, int C,
+                           uint16_t* dZ, float* dbias, float* partial, cudaStream_t st);
 // Dropout and the residual junction (residual_kernels.cu).  Kept iff 16 random bits are at least the threshold.
 inline uint32_t drop_threshold(float p) {
   const long t = lrint(65536.0 * (double)p);

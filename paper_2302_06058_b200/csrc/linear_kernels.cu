@@ -50,8 +50,8 @@ ckpt_pack_kernel(const uint4* __restrict__ x, long long halves, uint4* __restric
 // an activation, now 76: 5.3 TB/s); two steps' bytes are loaded at a time.  DROP: dropout of the result; its blocks of eight
 // are the threads'.
 template <int ACT, bool DROP>
-__global__ void __launch_bounds__(STREAM_THREADS)
-ckpt_unpack_kernel(const uint2* __restrict__ q, const uint8_t* __restrict__ s, long long eighths, uint4* __restrict__ x, const DropParams d) {
+__global__ void __launch_bounds__(STREAM_THREADS, 8)
+ckpt_unpack_kernel(const uint2* __restrict__ q, const uint8_t* __restrict__ s, long long eighths, uint4* __restrict__ x, const __grid_constant__ DropParams d) {
   pdl_launch_dependents();
   pdl_wait();
   const unsigned long long number = DROP ? drop_number(d) : 0ull;
@@ -88,18 +88,16 @@ ckpt_unpack_kernel(const uint2* __restrict__ q, const uint8_t* __restrict__ s, l
 // by side are added through shared memory at its end, in a fixed order, and each CTA leaves one row of partial sums for
 // bias_reduce_kernel (no atomics: the result does not depend on timing).  8192 x 16384 in 127 us on the device, 5.3 TB/s
 // (the bias gradient alone 47 us); 12608 x 1536 in 22 + 3 us: there the launches and the uneven end of the CTAs are a
-// third.  CTA (x, y): column tile x of 2 * half groups of eight, row slot y of gridDim.y.  DROP: dY is first dropped; its
-// blocks of eight are the threads' groups.
+// third.  CTA (x, y): column tile x of 2 * half groups of eight, row slot y of gridDim.y.
 // ------------------------------------------------------------------------------------------
 constexpr int ACTBWD_MAX_THREADS = 512;
 
-template <int ACT, bool DROP>
+template <int ACT>
 __global__ void __launch_bounds__(ACTBWD_MAX_THREADS, 1)
 act_bwd_kernel(const uint4* dY, const uint2* __restrict__ zq, const uint8_t* __restrict__ zs, int T, int C8, int half, int rows,
-               uint4* dZ /* may be dY */, float4* __restrict__ partial, const DropParams drop) {
+               uint4* dZ /* may be dY */, float4* __restrict__ partial) {
   pdl_launch_dependents();
   pdl_wait();
-  const unsigned long long number = DROP ? drop_number(drop) : 0ull;
   __shared__ float red[ACTBWD_MAX_THREADS][17];           // 17: neighbouring threads fall into different banks
   const int g = threadIdx.x / half, lc = threadIdx.x - g * half;
   const int ca = blockIdx.x * 2 * half + lc, cb = ca + half;
@@ -142,15 +140,6 @@ act_bwd_kernel(const uint4* dY, const uint2* __restrict__ zq, const uint8_t* __r
           }
         }
         fetch(u, t + U * stride);
-        if constexpr (DROP) {
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            act::Pair w[4] = {v[4 * h], v[4 * h + 1], v[4 * h + 2], v[4 * h + 3]};
-            drop8(w, (unsigned long long)(t * C8 + ca + (h != 0 ? half : 0)), number, drop);
-#pragma unroll
-            for (int k = 0; k < 4; ++k) v[4 * h + k] = w[k];
-          }
-        }
         if constexpr (ACT != BIMASK_ACT_NONE) {
 #pragma unroll
           for (int k = 0; k < 8; ++k) v[k] = act::mul2(v[k], act::slope2<ACT>(a[k]));
@@ -187,6 +176,102 @@ act_bwd_kernel(const uint4* dY, const uint2* __restrict__ zq, const uint8_t* __r
       out[2 * half] = make_float4(s[8], s[9], s[10], s[11]);
       out[2 * half + 1] = make_float4(s[12], s[13], s[14], s[15]);
     }
+  }
+}
+
+// ------------------------------------------------------------------------------------------
+// The same with dY dropped first.  The generator doubles the instructions per element (245 for a block of eight with a GELU, two
+// thirds of what the SMs can issue in the time that HBM needs), so this kernel wants warps rather than registers: 32 of them, a
+// thread with one block of eight columns, and the rows ahead in shared memory, copied by the threads that will use them (cp.async:
+// every thread waits for its own pieces only).  A scale byte comes with the aligned word around it.
+// ------------------------------------------------------------------------------------------
+constexpr int DROPBWD_THREADS = 1024, DROPBWD_STAGES = 4;
+constexpr int DROPBWD_SMEM = DROPBWD_STAGES * DROPBWD_THREADS * (16 + 8 + 4);
+
+template <int ACT>
+__global__ void __launch_bounds__(DROPBWD_THREADS, 1)
+act_dropout_bwd_kernel(const uint4* dY, const uint2* __restrict__ zq, const uint8_t* __restrict__ zs, uint32_t T, uint32_t C8, int cols,
+                       uint32_t rows, uint4* dZ /* may be dY */, float4* __restrict__ partial, const __grid_constant__ DropParams drop) {
+  extern __shared__ uint4 smem[];
+  pdl_launch_dependents();
+  const uint32_t g = threadIdx.x / (uint32_t)cols, lc = threadIdx.x - g * (uint32_t)cols, c = blockIdx.x * (uint32_t)cols + lc;
+  const bool ok = g < rows && c < C8;
+  const uint32_t base = (uint32_t)__cvta_generic_to_shared(smem);
+  const uint32_t ring_d = base + threadIdx.x * 16u, ring_q = base + DROPBWD_STAGES * DROPBWD_THREADS * 16u + threadIdx.x * 8u,
+                 ring_s = base + DROPBWD_STAGES * DROPBWD_THREADS * 24u + threadIdx.x * 4u;
+  pdl_wait();
+  const unsigned long long number = drop_number(drop);
+  act::Pair sum[4];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) sum[k] = act::both(0.f);
+  if (ok) {
+    const uint32_t stride = rows * gridDim.y;
+    uint32_t ahead = blockIdx.y * rows + g;
+    auto fetch = [&](uint32_t stage) {
+      if (ahead < T) {
+        const unsigned long long at = (unsigned long long)ahead * C8 + c;
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(ring_d + stage * (DROPBWD_THREADS * 16)), "l"(dY + at) : "memory");
+        if (ACT != BIMASK_ACT_NONE) {
+          asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(ring_q + stage * (DROPBWD_THREADS * 8)), "l"(zq + at) : "memory");
+          asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(ring_s + stage * (DROPBWD_THREADS * 4)), "l"(zs + ((at >> 2) & ~3ull)) : "memory");
+        }
+      }
+      asm volatile("cp.async.commit_group;" ::: "memory");
+      ahead += stride;
+    };
+#pragma unroll
+    for (int s = 0; s < DROPBWD_STAGES - 1; ++s) fetch(s);
+    uint32_t stage = 0;
+    for (uint32_t t = blockIdx.y * rows + g; t < T; t += stride) {
+      asm volatile("cp.async.wait_group %0;" ::"n"(DROPBWD_STAGES - 2) : "memory");
+      const unsigned long long at = (unsigned long long)t * C8 + c;
+      uint4 d;
+      asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(d.x), "=r"(d.y), "=r"(d.z), "=r"(d.w) : "r"(ring_d + stage * (DROPBWD_THREADS * 16)) : "memory");
+      act::Pair v[4] = {bf16_pair(d.x), bf16_pair(d.y), bf16_pair(d.z), bf16_pair(d.w)};
+      act::Pair a[4];
+      if constexpr (ACT != BIMASK_ACT_NONE) {
+        uint2 z;
+        uint32_t s;
+        asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(z.x), "=r"(z.y) : "r"(ring_q + stage * (DROPBWD_THREADS * 8)) : "memory");
+        asm volatile("ld.shared.u32 %0, [%1];" : "=r"(s) : "r"(ring_s + stage * (DROPBWD_THREADS * 4)) : "memory");
+        const act::Pair scale = act::both(ckpt::scale_value((s >> (8u * ((uint32_t)(at >> 2) & 3u))) & 255u));
+        ckpt::decode4(z.x, scale, a);
+        ckpt::decode4(z.y, scale, a + 2);
+      }
+      fetch((stage + DROPBWD_STAGES - 1) % DROPBWD_STAGES);      // into the pieces that the row before this one left
+      stage = (stage + 1) % DROPBWD_STAGES;
+      drop8(v, at, number, drop);
+      if constexpr (ACT != BIMASK_ACT_NONE) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[k] = act::mul2(v[k], act::slope2<ACT>(a[k]));
+      }
+#pragma unroll
+      for (int k = 0; k < 4; ++k) sum[k] = act::add2(sum[k], v[k]);
+      if (dZ != nullptr) dZ[at] = make_uint4(pack_bf16_p(v[0]), pack_bf16_p(v[1]), pack_bf16_p(v[2]), pack_bf16_p(v[3]));
+    }
+    asm volatile("cp.async.wait_group 0;" ::: "memory");
+  }
+  if (partial == nullptr) return;
+  // the rows that worked side by side are added in their order; each thread's sums lie in the first of its own pieces and the next
+  float s[8];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) act::split(sum[k], s[2 * k], s[2 * k + 1]);
+  float4* fold = reinterpret_cast<float4*>(smem);
+  if (rows > 1) {
+    fold[threadIdx.x] = make_float4(s[0], s[1], s[2], s[3]);
+    fold[DROPBWD_THREADS + threadIdx.x] = make_float4(s[4], s[5], s[6], s[7]);
+    __syncthreads();
+    if (g == 0)
+      for (uint32_t r = 1; r < rows; ++r) {
+        const float4 x = fold[r * (uint32_t)cols + lc], y = fold[DROPBWD_THREADS + r * (uint32_t)cols + lc];
+        s[0] += x.x; s[1] += x.y; s[2] += x.z; s[3] += x.w;
+        s[4] += y.x; s[5] += y.y; s[6] += y.z; s[7] += y.w;
+      }
+  }
+  if (g == 0 && ok) {
+    float4* out = partial + ((size_t)blockIdx.y * C8 + c) * 2;
+    out[0] = make_float4(s[0], s[1], s[2], s[3]);
+    out[1] = make_float4(s[4], s[5], s[6], s[7]);
   }
 }
 
@@ -246,9 +331,29 @@ ActBwdPlan plan_act_bwd(int T, int C) {
   return p;
 }
 
+// The same of the kernel with dropout: `half` is the columns (groups of eight) of a tile, a thread's one.
+ActBwdPlan plan_dropout_bwd(int T, int C) {
+  ActBwdPlan p;
+  const int C8 = C / 8;
+  p.tiles = (C8 + DROPBWD_THREADS / 2 - 1) / (DROPBWD_THREADS / 2);
+  p.half = (C8 + p.tiles - 1) / p.tiles;
+  p.rows = DROPBWD_THREADS / p.half;
+  if (p.rows > T) p.rows = T;
+  p.threads = (p.half * p.rows + 31) / 32 * 32;
+  p.slots = PLAN_SMS / p.tiles;
+  const int most = (T + p.rows - 1) / p.rows;
+  if (p.slots > most) p.slots = most;
+  if (p.slots < 1) p.slots = 1;
+  return p;
+}
+
 }  // namespace
 
-size_t act_bwd_partial_bytes(int T, int C) { return (size_t)plan_act_bwd(T, C).slots * C * sizeof(float); }
+// enough for either kernel
+size_t act_bwd_partial_bytes(int T, int C) {
+  const int a = plan_act_bwd(T, C).slots, b = plan_dropout_bwd(T, C).slots;
+  return (size_t)(a > b ? a : b) * C * sizeof(float);
+}
 
 int launch_ckpt_pack(const uint16_t* x, int T, int C, int8_t* q, uint8_t* s, cudaStream_t st) {
   const long long halves = (long long)T * (C / 16);
@@ -282,32 +387,65 @@ int launch_ckpt_unpack(const int8_t* q, const uint8_t* s, int act, int T, int C,
   return BIMASK_OK;
 }
 
+// db from the partial rows
+static int launch_bias_reduce(const float* partial, int slots, int C, float* dbias, cudaStream_t st) {
+  BIMASK_CUDA_OK(launch_pdl(bias_reduce_kernel, (C / 4 + 7) / 8, 256, 0, st, reinterpret_cast<const float4*>(partial), slots, C / 4,
+                            reinterpret_cast<float4*>(dbias)));
+  count_launch();
+  return BIMASK_OK;
+}
+
 int launch_act_bwd(const uint16_t* dY, const int8_t* zq, const uint8_t* zs, int act, int T, int C, uint16_t* dZ, float* dbias,
-                   float* partial, cudaStream_t st, const bimask_dropout_args* drop) {
+                   float* partial, cudaStream_t st) {
   const ActBwdPlan p = plan_act_bwd(T, C);
-  const DropParams d = drop_params(drop);
   float* part = dbias == nullptr ? nullptr : p.slots == 1 ? dbias : partial;      // one slot: its row is the result
   auto run = [&](auto kern) {
     return launch_pdl(kern, dim3(p.tiles, p.slots), p.threads, 0, st, reinterpret_cast<const uint4*>(dY), reinterpret_cast<const uint2*>(zq),
-                      zs, T, C / 8, p.half, p.rows, reinterpret_cast<uint4*>(dZ), reinterpret_cast<float4*>(part), d);
+                      zs, T, C / 8, p.half, p.rows, reinterpret_cast<uint4*>(dZ), reinterpret_cast<float4*>(part));
   };
   cudaError_t e;
-#define BIMASK_RUN(ACT) (d.thr != 0u ? run(act_bwd_kernel<ACT, true>) : run(act_bwd_kernel<ACT, false>))
   switch (act) {
-    case BIMASK_ACT_RELU: e = BIMASK_RUN(BIMASK_ACT_RELU); break;
-    case BIMASK_ACT_GELU: e = BIMASK_RUN(BIMASK_ACT_GELU); break;
-    case BIMASK_ACT_GELU_TANH: e = BIMASK_RUN(BIMASK_ACT_GELU_TANH); break;
-    case BIMASK_ACT_SILU: e = BIMASK_RUN(BIMASK_ACT_SILU); break;
-    default: e = BIMASK_RUN(BIMASK_ACT_NONE); break;
+    case BIMASK_ACT_RELU: e = run(act_bwd_kernel<BIMASK_ACT_RELU>); break;
+    case BIMASK_ACT_GELU: e = run(act_bwd_kernel<BIMASK_ACT_GELU>); break;
+    case BIMASK_ACT_GELU_TANH: e = run(act_bwd_kernel<BIMASK_ACT_GELU_TANH>); break;
+    case BIMASK_ACT_SILU: e = run(act_bwd_kernel<BIMASK_ACT_SILU>); break;
+    default: e = run(act_bwd_kernel<BIMASK_ACT_NONE>); break;
   }
-#undef BIMASK_RUN
   BIMASK_CUDA_OK(e);
   count_launch();
   if (dbias != nullptr && p.slots > 1) {
-    BIMASK_CUDA_OK(launch_pdl(bias_reduce_kernel, (C / 4 + 7) / 8, 256, 0, st, reinterpret_cast<const float4*>(partial), p.slots, C / 4,
-                              reinterpret_cast<float4*>(dbias)));
-    count_launch();
+    const int rc = launch_bias_reduce(partial, p.slots, C, dbias, st);
+    if (rc != BIMASK_OK) return rc;
   }
+  BIMASK_CUDA_OK(cudaGetLastError());
+  return BIMASK_OK;
+}
+
+int launch_act_dropout_bwd(const uint16_t* dY, const int8_t* zq, const uint8_t* zs, int act, const bimask_dropout_args& drop, int T, int C,
+                           uint16_t* dZ, float* dbias, float* partial, cudaStream_t st) {
+  const DropParams d = drop_params(&drop);
+  if (d.thr == 0u) return launch_act_bwd(dY, zq, zs, act, T, C, dZ, dbias, partial, st);
+  const ActBwdPlan p = plan_dropout_bwd(T, C);
+  float* part = dbias == nullptr ? nullptr : p.slots == 1 ? dbias : partial;      // one slot: its row is the result
+  auto run = [&](auto kern) -> int {
+    const int rc = set_smem_attr(kern, DROPBWD_SMEM);
+    if (rc != BIMASK_OK) return rc;
+    BIMASK_CUDA_OK(launch_pdl(kern, dim3(p.tiles, p.slots), p.threads, DROPBWD_SMEM, st, reinterpret_cast<const uint4*>(dY),
+                              reinterpret_cast<const uint2*>(zq), zs, (uint32_t)T, (uint32_t)C / 8, p.half, (uint32_t)p.rows,
+                              reinterpret_cast<uint4*>(dZ), reinterpret_cast<float4*>(part), d));
+    count_launch();
+    return BIMASK_OK;
+  };
+  int rc;
+  switch (act) {
+    case BIMASK_ACT_RELU: rc = run(act_dropout_bwd_kernel<BIMASK_ACT_RELU>); break;
+    case BIMASK_ACT_GELU: rc = run(act_dropout_bwd_kernel<BIMASK_ACT_GELU>); break;
+    case BIMASK_ACT_GELU_TANH: rc = run(act_dropout_bwd_kernel<BIMASK_ACT_GELU_TANH>); break;
+    case BIMASK_ACT_SILU: rc = run(act_dropout_bwd_kernel<BIMASK_ACT_SILU>); break;
+    default: rc = run(act_dropout_bwd_kernel<BIMASK_ACT_NONE>); break;
+  }
+  if (rc == BIMASK_OK && dbias != nullptr && p.slots > 1) rc = launch_bias_reduce(partial, p.slots, C, dbias, st);
+  if (rc != BIMASK_OK) return rc;
   BIMASK_CUDA_OK(cudaGetLastError());
   return BIMASK_OK;
 }

@@ -64,27 +64,29 @@ __device__ __forceinline__ void store8(void* base, long long block, const Pair (
 }
 
 template <bool F32>
-__global__ void __launch_bounds__(DROP_THREADS)
-dropout_kernel(const void* x, long long blocks, void* y /* may be x */, const DropParams d) {
+__global__ void __launch_bounds__(DROP_THREADS, F32 ? 5 : 6)
+dropout_kernel(const void* x, long long blocks, void* y /* may be x */, const __grid_constant__ DropParams d) {
   pdl_launch_dependents();
   pdl_wait();
   const unsigned long long number = drop_number(d);
   constexpr int U = 2;
   const long long step = (long long)gridDim.x * DROP_THREADS;
-  for (long long i0 = (long long)blockIdx.x * DROP_THREADS + threadIdx.x; i0 < blocks; i0 += U * step) {
-    Vec8<F32> v[U];
+  long long i = (long long)blockIdx.x * DROP_THREADS + threadIdx.x;
+  Vec8<F32> v[U];
+  auto fetch = [&](int u, long long at) {
+    if (at < blocks) v[u] = load8<F32>(x, at);
+  };
 #pragma unroll
-    for (int u = 0; u < U; ++u)
-      if (i0 + u * step < blocks) v[u] = load8<F32>(x, i0 + u * step);
+  for (int u = 0; u < U; ++u) fetch(u, i + u * step);
+  while (i < blocks) {
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const long long i = i0 + u * step;
-      if (i < blocks) {
-        Pair p[4];
-        unpack8<F32>(v[u], p);
-        if (d.thr != 0u) drop8(p, (unsigned long long)i, number, d);
-        store8<F32>(y, i, p);
-      }
+    for (int u = 0; u < U; ++u, i += step) {
+      if (i >= blocks) break;
+      Pair p[4];
+      unpack8<F32>(v[u], p);
+      fetch(u, i + U * step);
+      if (d.thr != 0u) drop8(p, (unsigned long long)i, number, d);
+      store8<F32>(y, i, p);
     }
   }
 }
@@ -1100,7 +1102,7 @@ DropParams drop_params(const bimask_dropout_args* d) {
 
 int launch_dropout(const void* x, int type, int T, int C, const bimask_dropout_args& d, void* y, cudaStream_t s) {
   const long long blocks = (long long)T * (C / 8);
-  const long long ctas = (blocks + DROP_THREADS - 1) / DROP_THREADS, most = 32ll * sm_count();
+  const long long ctas = (blocks + DROP_THREADS - 1) / DROP_THREADS, most = (type == BIMASK_TYPE_F32 ? 5ll : 6ll) * sm_count();
   auto run = [&](auto kern) {
     return launch_pdl(kern, (unsigned)(ctas < most ? ctas : most), DROP_THREADS, 0, s, x, blocks, y, drop_params(&d));
   };
