@@ -45,12 +45,19 @@ __device__ __forceinline__ act::Pair drop_pair(act::Pair v, uint32_t bits, uint3
   act::split(act::mul2(v, act::both(scale)), lo, hi);
   return act::pair((bits << 16) >= thr ? lo : 0.f, bits >= thr ? hi : 0.f);
 }
-__device__ __forceinline__ void drop8(act::Pair (&v)[4], unsigned long long block, unsigned long long number, const DropParams& d) {
-  const uint4 r = philox(block, number, d);
+// The multipliers of two elements: `kept` or 0.
+__device__ __forceinline__ act::Pair drop_choice(uint32_t bits, uint32_t thr, float kept) {
+  return act::pair((bits << 16) >= thr ? kept : 0.f, bits >= thr ? kept : 0.f);
+}
+__device__ __forceinline__ void drop8(act::Pair (&v)[4], const uint4& r, const DropParams& d) {
   v[0] = drop_pair(v[0], r.x, d.thr, d.scale);
   v[1] = drop_pair(v[1], r.y, d.thr, d.scale);
   v[2] = drop_pair(v[2], r.z, d.thr, d.scale);
   v[3] = drop_pair(v[3], r.w, d.thr, d.scale);
+}
+
+__device__ __forceinline__ void drop8(act::Pair (&v)[4], unsigned long long block, unsigned long long number, const DropParams& d) {
+  drop8(v, philox(block, number, d), d);
 }
 
 }  // namespace bimask

@@ -136,7 +136,9 @@ struct ResidualParams {
   float* sums;                       // [clusters][wanted arrays][C]
   float* gate_sums;                  // [units][C]
   int want;                          // bits: SUM_* arrays that are wanted
-  int branch;                        // a gradient of the branch is wanted
+  int has;                           // bits: HAS_* inputs that there are (others: any valid address, of which nothing is read)
+  const float* weight;               // w_post or scale, whichever there is; scale_too: scale if there are both
+  const float* scale_too;
   // Rows are given out in units of consecutive ones.  units_per_span: 0, or the units that a gate row's span is cut into.
   uint32_t units, unit_rows, units_per_span;
 };
@@ -463,6 +465,16 @@ __device__ __forceinline__ void affine(Pair (&v)[ROWS][VECS][4], const float* ba
     }
   }
 }
+// a vector of parameters, or ones
+__device__ __forceinline__ void param_or_one(const float* base, const Blocks& b, Pair (&w)[VECS][4]) {
+  if (base != nullptr) {
+#pragma unroll
+    for (int j = 0; j < VECS; ++j) param8(base, b.safe[j], w[j]);
+  } else {
+#pragma unroll
+    for (int j = 0; j < VECS; ++j) fill8(w[j], 1.f);
+  }
+}
 // address of a thread's piece: slot of block j of row r
 template <int SLOTS>
 __device__ __forceinline__ uint32_t piece(uint32_t stage_at, int r, int j, int slot) { return stage_at + ((r * VECS + j) * SLOTS + slot) * PITCH; }
@@ -536,11 +548,16 @@ residual_fwd_kernel(const __grid_constant__ ResidualParams p) {
         affine<true>(v, p.w_post, b);
         affine<false>(v, p.b_post, b);
       }
-      if (p.drop.thr != 0u) {
+      if (p.drop.thr != 0u) {                             // all blocks of the step together: their chains interleave
+        uint4 bits[ROWS][VECS];
 #pragma unroll
         for (int r = 0; r < ROWS; ++r)
 #pragma unroll
-          for (int j = 0; j < VECS; ++j) drop8(v[r][j], row[r] + b.at[j], number, p.drop);
+          for (int j = 0; j < VECS; ++j) bits[r][j] = philox(row[r] + b.at[j], number, p.drop);
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r)
+#pragma unroll
+          for (int j = 0; j < VECS; ++j) drop8(v[r][j], bits[r][j], p.drop);
       }
       if (GATE) {
 #pragma unroll
@@ -610,11 +627,13 @@ residual_fwd_kernel(const __grid_constant__ ResidualParams p) {
 // Four column sums carry every parameter's gradient: G1 = sum dn xh (w_pre), G2 = sum dn (b_pre), A = sum e yh, B = sum e:
 //   dw_post = scale A,  db_post = scale B,  dscale = w_post A + b_post B.
 // A thread keeps its columns' sums in registers; each cluster (CTA) leaves one row of partial sums.
-// Columns and rows past the end: dx', dn, y (and m of columns) are zeros, and so are D (its means are left out there) and every sum.
+// Columns and rows past the end: dx', dn, y (and m of columns) are zeros, and so is every sum.  What is absent (no norm before, dx' or y)
+// is copied as zeros, too, statistics among them: then all that depends on it is zero as it should be.
 // GATE: 0 no gate, 1 a gate whose gradient, if wanted, is a row per token, 2 one whose gradient is summed over spans.  WIDE: some norm
 // subtracts means, or a sum other than A and G1 is wanted; without, a row has three sums to exchange instead of eight.
 // ------------------------------------------------------------------------------------------
 enum { SUM_A = 1, SUM_B = 2, SUM_G1 = 4, SUM_G2 = 8 };
+enum { HAS_PRE = 1, HAS_DXO = 2, HAS_Y = 4, HAS_POST = 8 };
 
 template <bool F32, int GATE, bool POST, bool WIDE, bool CLUSTER>
 __global__ void __launch_bounds__(ROW_THREADS, 1)
@@ -640,7 +659,6 @@ residual_bwd_kernel(const __grid_constant__ ResidualParams p) {
   ahead = work;
   pdl_wait();
   const unsigned long long number = drop_number(p.drop);
-  const bool pre = p.pre != BIMASK_NORM_NONE;
   const bool layer_pre = WIDE && p.pre == BIMASK_NORM_LAYER, layer_post = WIDE && POST && p.post == BIMASK_NORM_LAYER;
   auto gate_row = [&](uint32_t t) { return p.gate + (long long)(p.gate_span == 1u ? t : t / p.gate_span) * p.gate_pitch8; };
   auto fetch = [&](const Walk<GATE == 2>& w, uint32_t stage) {
@@ -655,19 +673,18 @@ residual_bwd_kernel(const __grid_constant__ ResidualParams p) {
       for (int j = 0; j < VECS; ++j) {
         const bool there = live && b.ok[j];
         const unsigned long long block = row + b.safe[j];
-        if (pre) {
-          copy_block<F32>(piece<SLOTS>(at, r, j, X), p.xo, block, there);
-          copy16(piece<SLOTS>(at, r, j, DN), p.dn + block, there);
-        }
-        if (p.dxo != nullptr) copy_block<F32>(piece<SLOTS>(at, r, j, DX), p.dxo, block, there);
-        if (p.y != nullptr) copy16(piece<SLOTS>(at, r, j, Y), p.y + block, there);
+        copy_block<F32>(piece<SLOTS>(at, r, j, X), p.xo, block, there && (p.has & HAS_PRE));
+        copy16(piece<SLOTS>(at, r, j, DN), p.dn + block, there && (p.has & HAS_PRE));
+        copy_block<F32>(piece<SLOTS>(at, r, j, DX), p.dxo, block, there && (p.has & HAS_DXO));
+        copy16(piece<SLOTS>(at, r, j, Y), p.y + block, there && (p.has & HAS_Y));
         if (GATE_RING) copy16(piece<SLOTS>(at, r, j, G), gate_row(t) + b.safe[j], there);
       }
     }
     if (g.lane < 2 * ROWS) {                              // lanes 0, 1: the rows' statistics before, 2, 3: after
       const uint32_t t = w.t + (g.lane & 1);
-      const float2* src = g.lane < 2 ? p.stats_pre : p.stats_post;
-      if (src != nullptr) copy8(stats + stage * STATS_STAGE + g.lane * 8u, src + min(t, p.T - 1u), more && t < w.end);
+      const bool before = g.lane < 2;
+      copy8(stats + stage * STATS_STAGE + g.lane * 8u, (before ? p.stats_pre : p.stats_post) + min(t, p.T - 1u),
+            more && t < w.end && (p.has & (before ? HAS_PRE : HAS_POST)));
     }
     copies_commit();
   };
@@ -686,6 +703,8 @@ residual_bwd_kernel(const __grid_constant__ ResidualParams p) {
     __syncwarp();                                         // every lane has read the statistics that are overwritten now
     ahead.next(p, stride);
     fetch(ahead, stage ^ 1u);
+    Pair w_pre[VECS][4];
+    param_or_one(p.w_pre, b, w_pre);
     copies_wait<1>();
     __syncwarp();                                         // the statistics are other lanes' copies
     const uint32_t at = ring + stage * STAGE, st_at = stats + stage * STATS_STAGE;
@@ -694,196 +713,177 @@ residual_bwd_kernel(const __grid_constant__ ResidualParams p) {
     Pair E[ROWS][VECS][4], xh[ROWS][VECS][4], yh[ROWS][VECS][4], m[ROWS][VECS][4];
     float c[ROWS * NV], r_pre[ROWS], r_post[ROWS];
 #pragma unroll
-    for (int i = 0; i < ROWS * NV; ++i) c[i] = 0.f;
-#pragma unroll
     for (int r = 0; r < ROWS; ++r) {
       live[r] = work.t + r < work.end;
       row[r] = (unsigned long long)(work.t + r) * p.C8;
-      r_pre[r] = 0.f;
-      r_post[r] = 1.f;
-#pragma unroll
-      for (int j = 0; j < VECS; ++j) {
-        if (p.dxo != nullptr) read_block<F32>(piece<SLOTS>(at, r, j, DX), E[r][j]);
-        else fill8(E[r][j], 0.f);
-      }
     }
-    if (pre) {
-      Pair w[VECS][4];
-      if (p.w_pre != nullptr)
+    if (p.drop.thr != 0u) {                               // all blocks of the step together: their chains interleave
+      uint4 bits[ROWS][VECS];
 #pragma unroll
-        for (int j = 0; j < VECS; ++j) param8(p.w_pre, b.safe[j], w[j]);
+      for (int r = 0; r < ROWS; ++r)
 #pragma unroll
-      for (int r = 0; r < ROWS; ++r) {
-        const float2 st = read_pair(st_at + 8 * r);
-        r_pre[r] = st.y;
-        const Pair rs = act::both(st.y);
-        Pair s = act::both(0.f), s0 = act::both(0.f);
+        for (int j = 0; j < VECS; ++j) bits[r][j] = philox(row[r] + b.at[j], number, p.drop);
+#pragma unroll
+      for (int r = 0; r < ROWS; ++r)
 #pragma unroll
         for (int j = 0; j < VECS; ++j) {
-          Pair gr[4];
-          read_block<F32>(piece<SLOTS>(at, r, j, X), xh[r][j]);
-          read_block<false>(piece<SLOTS>(at, r, j, DN), gr);
-          normalise<WIDE>(xh[r][j], st);
-#pragma unroll
-          for (int k = 0; k < 4; ++k) sum_g1[j][k] = act::fma2(gr[k], xh[r][j][k], sum_g1[j][k]);
-          if (WIDE) plus8(sum_g2[j], gr);
-          if (p.w_pre != nullptr) times8(gr, w[j]);
-#pragma unroll
-          for (int k = 0; k < 4; ++k) s = act::fma2(gr[k], xh[r][j][k], s);
-          if (WIDE) s0 = act::add2(s0, sum8(gr));
-#pragma unroll
-          for (int k = 0; k < 4; ++k) E[r][j][k] = act::fma2(gr[k], rs, E[r][j][k]);
+          const float scale = b.ok[j] ? p.drop.scale : 0.f;       // nothing past the end in the sums with z
+          m[r][j][0] = drop_choice(bits[r][j].x, p.drop.thr, scale);
+          m[r][j][1] = drop_choice(bits[r][j].y, p.drop.thr, scale);
+          m[r][j][2] = drop_choice(bits[r][j].z, p.drop.thr, scale);
+          m[r][j][3] = drop_choice(bits[r][j].w, p.drop.thr, scale);
         }
-        c[r * NV] = horizontal(s);
-        if (layer_pre) c[r * NV + 1] = horizontal(s0);
-      }
     } else {
 #pragma unroll
       for (int r = 0; r < ROWS; ++r)
 #pragma unroll
-        for (int j = 0; j < VECS; ++j) fill8(xh[r][j], 0.f);
+        for (int j = 0; j < VECS; ++j) fill8(m[r][j], b.ok[j] ? 1.f : 0.f);
     }
     Pair w[VECS][4];                                      // scale w_post
-    const bool weighted = p.scale != nullptr || (POST && p.w_post != nullptr);
-    if (p.branch) {
+    param_or_one(p.weight, b, w);
+    if (POST && p.scale_too != nullptr) {
 #pragma unroll
       for (int j = 0; j < VECS; ++j) {
-        if (POST && p.w_post != nullptr) param8(p.w_post, b.safe[j], w[j]);
-        if (p.scale != nullptr) {
-          Pair s[4];
-          param8(p.scale, b.safe[j], s);
-          if (POST && p.w_post != nullptr) times8(w[j], s);
-          else
-#pragma unroll
-            for (int k = 0; k < 4; ++k) w[j][k] = s[k];
-        }
-      }
-#pragma unroll
-      for (int r = 0; r < ROWS; ++r) {
-        float2 st = make_float2(0.f, 1.f);
-        if (POST) st = read_pair(st_at + 8 * (ROWS + r));
-        r_post[r] = st.y;
-        Pair ze = act::both(0.f), zx = ze, z0 = ze, te = ze, tx = ze, t0 = ze;
-#pragma unroll
-        for (int j = 0; j < VECS; ++j) {
-          fill8(m[r][j], b.ok[j] ? 1.f : 0.f);            // nothing past the end in the sums with z
-          if (p.drop.thr != 0u) drop8(m[r][j], row[r] + b.at[j], number, p.drop);
-          if (p.y != nullptr) read_block<false>(piece<SLOTS>(at, r, j, Y), yh[r][j]);
-          else fill8(yh[r][j], 0.f);
-          if (POST) {
-            normalise<WIDE>(yh[r][j], st);
-            Pair z[4];
-#pragma unroll
-            for (int k = 0; k < 4; ++k) z[k] = m[r][j][k];
-            if (weighted) times8(z, w[j]);
-            if (GATE != 0) {
-              Pair gt[4];
-              if (GATE_RING) read_block<false>(piece<SLOTS>(at, r, j, G), gt);
-              else unpack8<false>(Vec8<false>{__ldg(gate_row(min(work.t + r, p.T - 1u)) + b.safe[j])}, gt);
-              times8(z, gt);
-            }
-            if (WIDE) {
-#pragma unroll
-              for (int k = 0; k < 4; ++k) te = act::fma2(z[k], E[r][j][k], te), tx = act::fma2(z[k], xh[r][j][k], tx);
-              t0 = act::add2(t0, sum8(z));
-            }
-            times8(z, yh[r][j]);
-#pragma unroll
-            for (int k = 0; k < 4; ++k) ze = act::fma2(z[k], E[r][j][k], ze), zx = act::fma2(z[k], xh[r][j][k], zx);
-            if (WIDE) z0 = act::add2(z0, sum8(z));
-          }
-        }
-        if (POST) {
-          c[r * NV + 2] = horizontal(ze);
-          c[r * NV + 3] = horizontal(zx);
-          if (WIDE) {
-            c[r * NV + 4] = horizontal(z0);
-            if (layer_post) { c[r * NV + 5] = horizontal(te); c[r * NV + 6] = horizontal(tx); c[r * NV + 7] = horizontal(t0); }
-          }
-        }
+        Pair s[4];
+        param8(p.scale_too, b.safe[j], s);
+        times8(w[j], s);
       }
     }
-    if (pre || POST) row_totals(g, c);
-    float s1[ROWS], s2[ROWS];
 #pragma unroll
     for (int r = 0; r < ROWS; ++r) {
-      const float scaled = -r_pre[r] * p.inv_c, f1 = c[r * NV] * scaled, f2 = WIDE ? c[r * NV + 1] * scaled : 0.f;
-      s1[r] = s2[r] = 0.f;
-      if (POST) {
-        s1[r] = c[r * NV + 2] + f1 * c[r * NV + 3];
-        if (WIDE) {
-          s1[r] += f2 * c[r * NV + 4];
-          s2[r] = c[r * NV + 5] + f1 * c[r * NV + 6] + f2 * c[r * NV + 7];
-        }
-      }
+      const float2 st = read_pair(st_at + 8 * r);
+      r_pre[r] = st.y;
+      const Pair rs = act::both(st.y);
+      Pair s = act::both(0.f), s0 = s;
 #pragma unroll
       for (int j = 0; j < VECS; ++j) {
-        const Pair k1 = act::both(f1), k2 = act::both(f2);
+        Pair gr[4];
+        read_block<F32>(piece<SLOTS>(at, r, j, DX), E[r][j]);
+        read_block<F32>(piece<SLOTS>(at, r, j, X), xh[r][j]);
+        read_block<false>(piece<SLOTS>(at, r, j, DN), gr);
+        normalise<WIDE>(xh[r][j], st);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) E[r][j][k] = act::fma2(xh[r][j][k], k1, WIDE ? act::add2(E[r][j][k], k2) : E[r][j][k]);      // D
-        if (p.dx != nullptr && live[r] && b.ok[j]) {
-          const Pair alpha = act::both(p.alpha);
-          Pair o[4];
+        for (int k = 0; k < 4; ++k) sum_g1[j][k] = act::fma2(gr[k], xh[r][j][k], sum_g1[j][k]);
+        if (WIDE) plus8(sum_g2[j], gr);
+        times8(gr, w_pre[j]);
 #pragma unroll
-          for (int k = 0; k < 4; ++k) o[k] = act::mul2(E[r][j][k], alpha);
-          store8<F32>(p.dx, (long long)(row[r] + b.at[j]), o);
-        }
+        for (int k = 0; k < 4; ++k) s = act::fma2(gr[k], xh[r][j][k], s);
+        if (WIDE) s0 = act::add2(s0, sum8(gr));
+#pragma unroll
+        for (int k = 0; k < 4; ++k) E[r][j][k] = act::fma2(gr[k], rs, E[r][j][k]);
       }
-    }
-    if (p.branch) {
+      c[r * NV] = horizontal(s);
+      c[r * NV + 1] = WIDE && layer_pre ? horizontal(s0) : 0.f;
+      float2 sq = make_float2(0.f, 1.f);
+      if (POST) sq = read_pair(st_at + 8 * (ROWS + r));
+      r_post[r] = sq.y;
+      Pair ze = act::both(0.f), zx = ze, z0 = ze, te = ze, tx = ze, t0 = ze;
 #pragma unroll
-      for (int r = 0; r < ROWS; ++r) {
-        const float scaled = -r_post[r] * p.inv_c;
-        const Pair k1 = act::both(s1[r] * scaled), k2 = act::both(s2[r] * scaled), rs = act::both(r_post[r]);
+      for (int j = 0; j < VECS; ++j) {
+        read_block<false>(piece<SLOTS>(at, r, j, Y), yh[r][j]);
+        if (POST) {
+          normalise<WIDE>(yh[r][j], sq);
+          Pair z[4];
 #pragma unroll
-        for (int j = 0; j < VECS; ++j) {
-          times8(E[r][j], m[r][j]);
+          for (int k = 0; k < 4; ++k) z[k] = act::mul2(m[r][j][k], w[j][k]);
           if (GATE != 0) {
-            if (GATE == 2 || p.dgate != nullptr) {        // scale u
-              Pair u[4];
-#pragma unroll
-              for (int k = 0; k < 4; ++k) u[k] = yh[r][j][k];
-              if (weighted) times8(u, w[j]);
-              if (POST && p.b_post != nullptr) {
-                Pair bias[4];
-                param8(p.b_post, b.safe[j], bias);
-                if (p.scale != nullptr) {
-                  Pair s[4];
-                  param8(p.scale, b.safe[j], s);
-                  times8(bias, s);
-                }
-                plus8(u, bias);
-              }
-              if (GATE == 2) {
-#pragma unroll
-                for (int k = 0; k < 4; ++k) fsum[j][k] = act::fma2(E[r][j][k], u[k], fsum[j][k]);
-              } else {
-                times8(u, E[r][j]);
-                if (live[r] && b.ok[j]) store8<false>(p.dgate, (long long)(work.t + r) * p.gate_pitch8 + b.at[j], u);
-              }
-            }
             Pair gt[4];
             if (GATE_RING) read_block<false>(piece<SLOTS>(at, r, j, G), gt);
             else unpack8<false>(Vec8<false>{__ldg(gate_row(min(work.t + r, p.T - 1u)) + b.safe[j])}, gt);
-            times8(E[r][j], gt);
+            times8(z, gt);
           }
+          if (WIDE) {
 #pragma unroll
-          for (int k = 0; k < 4; ++k) sum_a[j][k] = act::fma2(E[r][j][k], yh[r][j][k], sum_a[j][k]);
-          if (POST && WIDE) plus8(sum_b[j], E[r][j]);
-          if (weighted) times8(E[r][j], w[j]);
-          if (POST) {
-#pragma unroll
-            for (int k = 0; k < 4; ++k) E[r][j][k] = act::fma2(E[r][j][k], rs, WIDE ? act::fma2(yh[r][j][k], k1, k2) : act::mul2(yh[r][j][k], k1));
+            for (int k = 0; k < 4; ++k) te = act::fma2(z[k], E[r][j][k], te), tx = act::fma2(z[k], xh[r][j][k], tx);
+            t0 = act::add2(t0, sum8(z));
           }
-          if (p.dy != nullptr && live[r] && b.ok[j]) store8<false>(p.dy, (long long)(row[r] + b.at[j]), E[r][j]);
+          times8(z, yh[r][j]);
+#pragma unroll
+          for (int k = 0; k < 4; ++k) ze = act::fma2(z[k], E[r][j][k], ze), zx = act::fma2(z[k], xh[r][j][k], zx);
+          if (WIDE) z0 = act::add2(z0, sum8(z));
         }
       }
-      if (GATE == 2 && work.last()) {
-#pragma unroll
-        for (int j = 0; j < VECS; ++j) {
-          if (b.ok[j]) store8<true>(p.gate_sums, (long long)work.unit * p.C8 + b.at[j], fsum[j]);
-          fill8(fsum[j], 0.f);
+      if (POST) {
+        c[r * NV + 2] = horizontal(ze);
+        c[r * NV + 3] = horizontal(zx);
+        if (WIDE) {
+          c[r * NV + 4] = horizontal(z0);
+          c[r * NV + 5] = layer_post ? horizontal(te) : 0.f;
+          c[r * NV + 6] = layer_post ? horizontal(tx) : 0.f;
+          c[r * NV + 7] = layer_post ? horizontal(t0) : 0.f;
         }
+      }
+    }
+    row_totals(g, c);
+    const Pair alpha = act::both(p.alpha);
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) {
+      const float scaled = -r_pre[r] * p.inv_c, f1 = c[r * NV] * scaled, f2 = WIDE ? c[r * NV + 1] * scaled : 0.f;
+      float s1 = 0.f, s2 = 0.f;
+      if (POST) {
+        const float scaled_post = -r_post[r] * p.inv_c;
+        s1 = c[r * NV + 2] + f1 * c[r * NV + 3];
+        if (WIDE) {
+          s1 += f2 * c[r * NV + 4];
+          s2 = (c[r * NV + 5] + f1 * c[r * NV + 6] + f2 * c[r * NV + 7]) * scaled_post;
+        }
+        s1 *= scaled_post;
+      }
+      const Pair k1 = act::both(f1), k2 = act::both(f2), q1 = act::both(s1), q2 = act::both(s2), rs = act::both(r_post[r]);
+#pragma unroll
+      for (int j = 0; j < VECS; ++j) {
+        const bool there = live[r] && b.ok[j];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) E[r][j][k] = act::fma2(xh[r][j][k], k1, WIDE ? act::add2(E[r][j][k], k2) : E[r][j][k]);      // D
+        Pair o[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) o[k] = act::mul2(E[r][j][k], alpha);
+        if (there && p.dx != nullptr) store8<F32>(p.dx, (long long)(row[r] + b.at[j]), o);
+        times8(E[r][j], m[r][j]);
+        if (GATE != 0) {
+          if (GATE == 2 || p.dgate != nullptr) {          // scale u
+            Pair u[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) u[k] = act::mul2(yh[r][j][k], w[j][k]);
+            if (POST && p.b_post != nullptr) {
+              Pair bias[4];
+              param8(p.b_post, b.safe[j], bias);
+              if (p.scale != nullptr) {
+                Pair s[4];
+                param8(p.scale, b.safe[j], s);
+                times8(bias, s);
+              }
+              plus8(u, bias);
+            }
+            if (GATE == 2) {
+#pragma unroll
+              for (int k = 0; k < 4; ++k) fsum[j][k] = act::fma2(E[r][j][k], u[k], fsum[j][k]);
+            } else {
+              times8(u, E[r][j]);
+              if (there) store8<false>(p.dgate, (long long)(work.t + r) * p.gate_pitch8 + b.at[j], u);
+            }
+          }
+          Pair gt[4];
+          if (GATE_RING) read_block<false>(piece<SLOTS>(at, r, j, G), gt);
+          else unpack8<false>(Vec8<false>{__ldg(gate_row(min(work.t + r, p.T - 1u)) + b.safe[j])}, gt);
+          times8(E[r][j], gt);
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) sum_a[j][k] = act::fma2(E[r][j][k], yh[r][j][k], sum_a[j][k]);
+        if (POST && WIDE) plus8(sum_b[j], E[r][j]);
+        times8(E[r][j], w[j]);
+        if (POST) {
+#pragma unroll
+          for (int k = 0; k < 4; ++k) E[r][j][k] = act::fma2(E[r][j][k], rs, WIDE ? act::fma2(yh[r][j][k], q1, q2) : act::mul2(yh[r][j][k], q1));
+        }
+        if (there && p.dy != nullptr) store8<false>(p.dy, (long long)(row[r] + b.at[j]), E[r][j]);
+      }
+    }
+    if (GATE == 2 && work.last()) {
+#pragma unroll
+      for (int j = 0; j < VECS; ++j) {
+        if (b.ok[j]) store8<true>(p.gate_sums, (long long)work.unit * p.C8 + b.at[j], fsum[j]);
+        fill8(fsum[j], 0.f);
       }
     }
     work.next(p, stride);
@@ -1172,10 +1172,16 @@ int launch_residual_bwd(const bimask_residual_args& a, cudaStream_t s) {
   const bool spanned = a.dgate != nullptr && p.gate_span > 1;
   const RowPlan b = plan_rows(a.T, a.C, spanned ? (int)p.gate_span : 1, PLAN_SMS);
   take_plan(p, b);
-  p.branch = a.dy || a.dgate || a.dscale || a.dw_post || a.db_post;
-  if (!p.branch) { p.y = nullptr; p.stats_post = nullptr; }
-  if (p.pre == BIMASK_NORM_NONE) p.stats_pre = nullptr;
-  if (p.post == BIMASK_NORM_NONE) p.stats_post = nullptr;
+  const bool branch = a.dy || a.dgate || a.dscale || a.dw_post || a.db_post, post = branch && a.post != BIMASK_NORM_NONE;
+  p.has = (a.pre != BIMASK_NORM_NONE ? HAS_PRE : 0) | (a.dxo ? HAS_DXO : 0) | (branch && a.y ? HAS_Y : 0) | (post ? HAS_POST : 0);
+  const void* some = p.has & HAS_PRE ? a.xo : a.dxo;       // one of the two is there
+  if (!(p.has & HAS_PRE)) { p.xo = const_cast<void*>(some); p.dn = reinterpret_cast<const uint4*>(some); p.w_pre = nullptr; }
+  if (!(p.has & HAS_DXO)) p.dxo = some;
+  if (!(p.has & HAS_Y)) p.y = reinterpret_cast<const uint4*>(some);
+  if (!(p.has & HAS_PRE)) p.stats_pre = reinterpret_cast<float2*>(const_cast<void*>(some));
+  if (!(p.has & HAS_POST)) p.stats_post = reinterpret_cast<float2*>(const_cast<void*>(some));
+  p.weight = post && a.w_post ? a.w_post : branch ? a.scale : nullptr;
+  p.scale_too = post && a.w_post ? a.scale : nullptr;
   const bool scale = a.dscale != nullptr;
   p.want = (a.dw_post || scale ? SUM_A : 0) | (a.db_post || (scale && a.b_post) ? SUM_B : 0) | (a.dw_pre ? SUM_G1 : 0) | (a.db_pre ? SUM_G2 : 0);
   p.sums = reinterpret_cast<float*>(a.ws);
@@ -1189,13 +1195,12 @@ int launch_residual_bwd(const bimask_residual_args& a, cudaStream_t s) {
     static_assert(bytes <= 227 * 1024, "shared memory of a CTA");
     return launch_rows(residual_bwd_kernel<F, G, P, W, K>, b, bytes, s, p);
   };
-  const bool after = p.post != BIMASK_NORM_NONE && p.branch;
-  const bool wide = (p.post == BIMASK_NORM_LAYER && p.branch) || p.pre == BIMASK_NORM_LAYER || (p.want & (SUM_B | SUM_G2)) != 0;
+  const bool wide = (post && p.post == BIMASK_NORM_LAYER) || p.pre == BIMASK_NORM_LAYER || (p.want & (SUM_B | SUM_G2)) != 0;
   auto pick3 = [&](auto f32, auto gate, auto post) -> int {
     if (b.cluster > 1) return wide ? run(f32, gate, post, Yes(), Yes()) : run(f32, gate, post, No(), Yes());
     return wide ? run(f32, gate, post, Yes(), No()) : run(f32, gate, post, No(), No());
   };
-  auto pick2 = [&](auto f32, auto gate) -> int { return after ? pick3(f32, gate, Yes()) : pick3(f32, gate, No()); };
+  auto pick2 = [&](auto f32, auto gate) -> int { return post ? pick3(f32, gate, Yes()) : pick3(f32, gate, No()); };
   auto pick = [&](auto f32) -> int {
     if (spanned) return pick2(f32, std::integral_constant<int, 2>());
     if (p.gate_span != 0) return pick2(f32, std::integral_constant<int, 1>());
