@@ -411,6 +411,10 @@ BIMASK_HD constexpr int fwd_slots(bool f32, bool gate) { return (f32 ? 2 : 1) + 
 // With an fp32 stream the ring has no room for a gate's pieces: it is read from memory (L2) where it is used.
 BIMASK_HD constexpr bool bwd_gate_in_ring(bool f32, bool gate) { return gate && !f32; }
 BIMASK_HD constexpr int bwd_slots(bool f32, bool gate) { return (f32 ? 4 : 2) + 2 + (bwd_gate_in_ring(f32, gate) ? 1 : 0); }
+// The backward pass keeps two parameters of the threads' columns beside the ring (from memory they cost it a fifth of the time with
+// an fp32 stream, whose ring leaves no first-level cache); only there a cluster's larger exchange buffers leave no room.
+BIMASK_HD constexpr bool bwd_keeps_params(bool f32, bool cluster) { return !(f32 && cluster); }
+constexpr int PARAM_BYTES = 2 * VECS * 2 * PITCH;
 BIMASK_HD constexpr int bwd_values(bool post, bool wide) { return !post ? 2 : !wide ? 4 : 8; }
 BIMASK_HD constexpr int ring_bytes(int slots) { return STAGES * ROWS * VECS * slots * PITCH; }
 constexpr int FWD_CTAS = 2;                               // of the forward kernel on an SM
@@ -643,7 +647,8 @@ residual_bwd_kernel(const __grid_constant__ ResidualParams p) {
   constexpr bool GATE_RING = bwd_gate_in_ring(F32, GATE != 0);
   constexpr int NV = bwd_values(POST, WIDE);              // a row's sums: g xh, g, z E, z xh, z, w m gate (E, xh, 1)
   constexpr uint32_t STAGE = ROWS * VECS * SLOTS * PITCH;
-  uint8_t* const after = reinterpret_cast<uint8_t*>(smem) + ring_bytes(SLOTS);
+  constexpr bool KEPT = bwd_keeps_params(F32, CLUSTER);
+  uint8_t* const after = reinterpret_cast<uint8_t*>(smem) + ring_bytes(SLOTS) + (KEPT ? PARAM_BYTES : 0);
   float* const exchange = reinterpret_cast<float*>(after + STATS_BYTES);
   pdl_launch_dependents();
   clear_exchange<ROWS * NV, CLUSTER>(exchange);
@@ -688,6 +693,44 @@ residual_bwd_kernel(const __grid_constant__ ResidualParams p) {
     }
     copies_commit();
   };
+  // the parameters of this thread's columns, w_pre and scale w_post: from its own pieces after the ring, or from memory
+  const uint32_t kept = ring + ring_bytes(SLOTS);
+  auto weights = [&](Pair (&w)[VECS][4]) {
+    param_or_one(p.weight, b, w);
+    if (POST && p.scale_too != nullptr) {
+#pragma unroll
+      for (int j = 0; j < VECS; ++j) {
+        Pair s[4];
+        param8(p.scale_too, b.safe[j], s);
+        times8(w[j], s);
+      }
+    }
+  };
+  auto params = [&](int which, Pair (&w)[VECS][4]) {
+    if (KEPT) {
+#pragma unroll
+      for (int j = 0; j < VECS; ++j) read_block<true>(kept + (uint32_t)(which * VECS + j) * 2 * PITCH, w[j]);
+    } else if (which == 0) {
+      param_or_one(p.w_pre, b, w);
+    } else {
+      weights(w);
+    }
+  };
+  if (KEPT) {
+    uint4* mine = reinterpret_cast<uint4*>(reinterpret_cast<uint8_t*>(smem) + ring_bytes(SLOTS)) + threadIdx.x;
+#pragma unroll
+    for (int which = 0; which < 2; ++which) {
+      Pair w[VECS][4];
+      if (which == 0) param_or_one(p.w_pre, b, w);
+      else weights(w);
+#pragma unroll
+      for (int j = 0; j < VECS; ++j) {
+        const Vec8<true> v = pack8<true>(w[j]);
+        mine[(which * VECS + j) * 2 * ROW_THREADS] = v.w[0];
+        mine[((which * VECS + j) * 2 + 1) * ROW_THREADS] = v.w[1];
+      }
+    }
+  }
   Pair sum_a[VECS][4], sum_g1[VECS][4], sum_b[VECS][4], sum_g2[VECS][4], fsum[VECS][4];
 #pragma unroll
   for (int j = 0; j < VECS; ++j) {
@@ -703,8 +746,6 @@ residual_bwd_kernel(const __grid_constant__ ResidualParams p) {
     __syncwarp();                                         // every lane has read the statistics that are overwritten now
     ahead.next(p, stride);
     fetch(ahead, stage ^ 1u);
-    Pair w_pre[VECS][4];
-    param_or_one(p.w_pre, b, w_pre);
     copies_wait<1>();
     __syncwarp();                                         // the statistics are other lanes' copies
     const uint32_t at = ring + stage * STAGE, st_at = stats + stage * STATS_STAGE;
@@ -739,16 +780,9 @@ residual_bwd_kernel(const __grid_constant__ ResidualParams p) {
 #pragma unroll
         for (int j = 0; j < VECS; ++j) fill8(m[r][j], b.ok[j] ? 1.f : 0.f);
     }
-    Pair w[VECS][4];                                      // scale w_post
-    param_or_one(p.weight, b, w);
-    if (POST && p.scale_too != nullptr) {
-#pragma unroll
-      for (int j = 0; j < VECS; ++j) {
-        Pair s[4];
-        param8(p.scale_too, b.safe[j], s);
-        times8(w[j], s);
-      }
-    }
+    Pair w_pre[VECS][4], w[VECS][4];
+    params(0, w_pre);
+    params(1, w);
 #pragma unroll
     for (int r = 0; r < ROWS; ++r) {
       const float2 st = read_pair(st_at + 8 * r);
@@ -1191,7 +1225,7 @@ int launch_residual_bwd(const bimask_residual_args& a, cudaStream_t s) {
   auto run = [&](auto f32, auto gate, auto post, auto wide, auto cluster) -> int {
     constexpr bool F = decltype(f32)::value, P = decltype(post)::value, W = decltype(wide)::value, K = decltype(cluster)::value;
     constexpr int G = decltype(gate)::value;
-    constexpr int bytes = ring_bytes(bwd_slots(F, G != 0)) + STATS_BYTES + Exchange<bwd_values(P, W) * ROWS, K>::BYTES;
+    constexpr int bytes = ring_bytes(bwd_slots(F, G != 0)) + (bwd_keeps_params(F, K) ? PARAM_BYTES : 0) + STATS_BYTES + Exchange<bwd_values(P, W) * ROWS, K>::BYTES;
     static_assert(bytes <= 227 * 1024, "shared memory of a CTA");
     return launch_rows(residual_bwd_kernel<F, G, P, W, K>, b, bytes, s, p);
   };
