@@ -6,6 +6,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from ctypes import c_float, c_int, c_int32, c_int64, c_size_t, c_uint64, c_void_p, c_char_p, POINTER, Structure
 
 import torch
@@ -74,6 +75,10 @@ class ResidualArgs(Structure):
                 ("gate_pitch", c_int64), ("eps_post", c_float), ("eps_pre", c_float), ("alpha", c_float), ("drop", Dropout),
                 *((name, c_void_p) for name in _RESIDUAL_POINTERS), ("ws_bytes", c_size_t)]
 
+
+# the same fields for struct.pack, in one call (setting 30 fields one by one takes longer than a short kernel)
+_RESIDUAL_PACK = struct.Struct("@6iq3f4xfQQP23PN").pack
+assert struct.calcsize("@6iq3f4xfQQP23PN") == ctypes.sizeof(ResidualArgs) and len(_RESIDUAL_POINTERS) == 23
 
 CONV_AUTO, CONV_EXPLICIT, CONV_IMPLICIT = 0, 1, 2
 
@@ -317,36 +322,40 @@ def bimask_residual_norm_workspace_bytes(T: int, C: int, gate_span: int = 1) -> 
     return lib().bimask_residual_norm_workspace_bytes(T, C, gate_span)
 
 
-def _row_pitch(t, C):
-    """Elements between the rows of a gate: a tensor of rows that are contiguous in themselves."""
-    if not isinstance(t, torch.Tensor) or t.is_contiguous():
-        return C
+def _row_pitch(t, pitch):
+    """Elements between the rows of a gate that is not contiguous (its rows are, in themselves), or an address."""
+    if not isinstance(t, torch.Tensor):
+        return pitch
     if t.dim() != 2 or t.stride(1) != 1:
         raise ValueError("a gate's rows must be contiguous")
     return t.stride(0)
+
+
+def _row_ptr(name, t):
+    if name in ("gate", "dgate") and isinstance(t, torch.Tensor):
+        return t.data_ptr()                              # its row pitch is checked by itself
+    return _ptr(t)
 
 
 def make_residual_args(T, C, bufs: dict, stream_type=TYPE_BF16, post=NORM_NONE, pre=NORM_NONE, eps_post=1e-5, eps_pre=1e-5, alpha=1.0,
                        gate_span=1, drop: Dropout | None = None) -> ResidualArgs:
     """Fill a bimask_residual_args from a dict of tensors keyed by field name (missing keys -> NULL).  The rows of gate and dgate
     may be slices of a wider matrix, both of the same pitch (bufs["gate_pitch"] gives it where they are addresses)."""
-    a = ResidualArgs(T, C, stream_type, post, pre, gate_span, 0, eps_post, eps_pre, alpha)
-    if drop is not None:
-        a.drop = drop
     get = bufs.get
-    for name in _RESIDUAL_POINTERS:
-        t = get(name)
+    pointers = [0 if t is None else t.data_ptr() if type(t) is _Tensor and t.is_contiguous() else _row_ptr(name, t)
+                for name, t in zip(_RESIDUAL_POINTERS, map(get, _RESIDUAL_POINTERS))]
+    pitch = 0
+    for t in (get("gate"), get("dgate")):
         if t is not None:
-            if name == "gate" or name == "dgate":
-                pitch = _row_pitch(t, get("gate_pitch", C))
-                if a.gate_pitch not in (0, pitch):
-                    raise ValueError("gate and dgate must have the same row pitch")
-                a.gate_pitch = pitch
-                t = t.data_ptr() if isinstance(t, torch.Tensor) else t
-            setattr(a, name, _ptr(t))
+            own = C if type(t) is _Tensor and t.is_contiguous() else _row_pitch(t, get("gate_pitch", C))
+            if pitch not in (0, own):
+                raise ValueError("gate and dgate must have the same row pitch")
+            pitch = own
     ws = get("ws")
-    a.ws_bytes = ws.numel() * ws.element_size() if isinstance(ws, torch.Tensor) else int(get("ws_bytes", 0))
-    return a
+    ws_bytes = ws.numel() * ws.element_size() if type(ws) is _Tensor else int(get("ws_bytes", 0))
+    p, seed, stream_no, counter = (0.0, 0, 0, 0) if drop is None else (drop.p, drop.seed, drop.stream_no, drop.counter or 0)
+    return ResidualArgs.from_buffer_copy(_RESIDUAL_PACK(T, C, stream_type, post, pre, gate_span, pitch, eps_post, eps_pre, alpha, p, seed,
+                                                        stream_no, counter, *pointers, ws_bytes))
 
 
 def bimask_residual_norm_fwd(args: ResidualArgs, stream=None):
