@@ -133,9 +133,14 @@ struct ResidualParams {
   void* dx;
   uint4* dy;
   uint4* dgate;
-  float* sums;                       // [clusters][wanted arrays][C]
-  float* gate_sums;                  // [units][C]
+  float* sums;                       // [clusters][wanted arrays][C]; null: one cluster takes all rows and leaves the gradients themselves
+  float* gate_sums;                  // [units][C]; null: a unit is a whole span, and leaves its row of dgate
   int want;                          // bits: SUM_* arrays that are wanted
+  float* dscale;
+  float* dw_post;
+  float* db_post;
+  float* dw_pre;
+  float* db_pre;
   int has;                           // bits: HAS_* inputs that there are (others: any valid address, of which nothing is read)
   const float* weight;               // w_post or scale, whichever there is; scale_too: scale if there are both
   const float* scale_too;
@@ -916,7 +921,10 @@ residual_bwd_kernel(const __grid_constant__ ResidualParams p) {
     if (GATE == 2 && work.last()) {
 #pragma unroll
       for (int j = 0; j < VECS; ++j) {
-        if (b.ok[j]) store8<true>(p.gate_sums, (long long)work.unit * p.C8 + b.at[j], fsum[j]);
+        if (b.ok[j]) {
+          if (p.gate_sums != nullptr) store8<true>(p.gate_sums, (long long)work.unit * p.C8 + b.at[j], fsum[j]);
+          else store8<false>(p.dgate, (long long)work.unit * p.gate_pitch8 + b.at[j], fsum[j]);
+        }
         fill8(fsum[j], 0.f);
       }
     }
@@ -924,11 +932,10 @@ residual_bwd_kernel(const __grid_constant__ ResidualParams p) {
     stage ^= 1u;
   }
   copies_wait<0>();
-  // the groups' sums are added through the ring, in their order
+  // The groups' sums are added through the ring, in their order.
   int slot = 0;
   auto leave = [&](int which, Pair (&sum)[VECS][4]) {
     if (!(p.want & which)) return;                        // the same for every thread
-    float* const out = p.sums + ((size_t)(CLUSTER ? blockIdx.x / (uint32_t)p.cluster : blockIdx.x) * __popc(p.want) + slot) * p.C8 * 8;
     if (groups > 1) {
       __syncthreads();
       uint4* mine = reinterpret_cast<uint4*>(smem) + threadIdx.x;
@@ -941,6 +948,7 @@ residual_bwd_kernel(const __grid_constant__ ResidualParams p) {
       __syncthreads();
     }
     if (g.group == 0) {
+      float* const out = p.sums + ((size_t)(CLUSTER ? blockIdx.x / (uint32_t)p.cluster : blockIdx.x) * __popc(p.want) + slot) * p.C8 * 8;
 #pragma unroll
       for (int j = 0; j < VECS; ++j) {
         for (uint32_t o = 1; o < groups; ++o) {
@@ -948,7 +956,7 @@ residual_bwd_kernel(const __grid_constant__ ResidualParams p) {
           read_block<true>(ring + o * (uint32_t)p.warps * 512u + 2 * j * PITCH, q);
           plus8(sum[j], q);
         }
-        if (b.ok[j]) store8<true>(out, b.at[j], sum[j]);
+        if (b.ok[j] && p.sums != nullptr) store8<true>(out, b.at[j], sum[j]);
       }
     }
     ++slot;
@@ -957,57 +965,102 @@ residual_bwd_kernel(const __grid_constant__ ResidualParams p) {
   if (POST && WIDE) leave(SUM_B, sum_b);
   leave(SUM_G1, sum_g1);
   if (WIDE) leave(SUM_G2, sum_g2);
+  if (p.sums == nullptr && p.want != 0 && g.group == 0) { // what residual_reduce_kernel makes of the sums
+#pragma unroll
+    for (int j = 0; j < VECS; ++j) {
+      if (!b.ok[j]) continue;
+      const uint32_t at = b.at[j];
+      if (p.dw_pre != nullptr) store8<true>(p.dw_pre, at, sum_g1[j]);
+      if (WIDE && p.db_pre != nullptr) store8<true>(p.db_pre, at, sum_g2[j]);
+      Pair s[4], o[4];
+      fill8(s, 1.f);
+      if (p.scale != nullptr) param8(p.scale, at, s);
+      auto scaled = [&](const Pair (&sum)[4]) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) o[k] = act::mul2(sum[k], s[k]);
+      };
+      if (p.dw_post != nullptr) { scaled(sum_a[j]); store8<true>(p.dw_post, at, o); }
+      if (WIDE && p.db_post != nullptr) { scaled(sum_b[j]); store8<true>(p.db_post, at, o); }
+      if (p.dscale != nullptr) {
+        fill8(s, 1.f);
+        if (POST && p.w_post != nullptr) param8(p.w_post, at, s);
+        scaled(sum_a[j]);
+        if (POST && WIDE && p.b_post != nullptr) {
+          param8(p.b_post, at, s);
+          times8(s, sum_b[j]);
+          plus8(o, s);
+        }
+        store8<true>(p.dscale, at, o);
+      }
+    }
+  }
   if (CLUSTER) ptx::cluster_sync();                       // shared memory outlives the peers' writes to it
 }
 
-// The parameters' gradients from the clusters' partial sums: a CTA covers eight float4 columns of one wanted array (blockIdx.y), its
-// 32 row slots take the partial rows in turn and are added through shared memory, in a fixed order.  A carries dscale with it, and B
-// where dscale has a part from there.
+// What is left to add up, in one launch.  blockIdx.y below the number of wanted arrays: that array's gradients from the clusters'
+// partial sums; a CTA covers eight float4 columns, its 32 row slots take the partial rows in turn and are added through shared memory,
+// in a fixed order (A carries dscale with it, and B where dscale has a part from there).  blockIdx.y above: a row of dgate from its
+// units, the same way.
 struct ResidualReduce {
   const float4* sums;
   int slots, want, C4;
   const float4 *scale, *w_post, *b_post;
   float4 *dscale, *dw_post, *db_post, *dw_pre, *db_pre;
+  const float4* gate_sums;
+  int units_per_span;
+  uint2* dgate;
+  long long gate_pitch4, gates;
 };
 __device__ __forceinline__ float4 add4(float4 a, float4 b) { return make_float4(a.x + b.x, a.y + b.y, a.z + b.z, a.w + b.w); }
 __device__ __forceinline__ float4 mul4(float4 a, float4 b) { return make_float4(a.x * b.x, a.y * b.y, a.z * b.z, a.w * b.w); }
 
 __global__ void __launch_bounds__(256)
-residual_reduce_kernel(const ResidualReduce p) {
+residual_reduce_kernel(const __grid_constant__ ResidualReduce p) {
   __shared__ float4 red[2][32][8];
   pdl_launch_dependents();
   const int lane = threadIdx.x & 7, slot = threadIdx.x >> 3;
   const int e = blockIdx.x * 8 + lane, arrays = __popc(p.want);
+  pdl_wait();
+  const float4 zero = make_float4(0.f, 0.f, 0.f, 0.f);
+  // the sum over `rows` rows of `src`, `step` apart, and over those of its neighbour, in the threads of slot 0
+  auto total = [&](const float4* src, int rows, size_t step, bool both, size_t neighbour, float4 (&acc)[2]) {
+    acc[0] = acc[1] = zero;
+    if (e < p.C4) {
+#pragma unroll 5
+      for (int s = slot; s < rows; s += 32) {
+        acc[0] = add4(acc[0], src[s * step]);
+        if (both) acc[1] = add4(acc[1], src[s * step + neighbour]);
+      }
+    }
+    red[0][slot][lane] = acc[0];
+    red[1][slot][lane] = acc[1];
+    __syncthreads();
+#pragma unroll
+    for (int half = 16; half >= 1; half >>= 1) {
+      if (slot < half) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          acc[i] = add4(acc[i], red[i][slot + half][lane]);
+          red[i][slot][lane] = acc[i];
+        }
+      }
+      __syncthreads();
+    }
+  };
+  float4 acc[2];
+  if ((int)blockIdx.y >= arrays) {
+    const long long stride = gridDim.y - arrays;
+    for (long long row = (int)blockIdx.y - arrays; row < p.gates; row += stride) {
+      total(p.gate_sums + (size_t)row * p.units_per_span * p.C4 + e, p.units_per_span, p.C4, false, 0, acc);
+      if (slot == 0 && e < p.C4) p.dgate[row * p.gate_pitch4 + e] = make_uint2(pack_bf16_f(acc[0].x, acc[0].y), pack_bf16_f(acc[0].z, acc[0].w));
+    }
+    return;
+  }
   int which = p.want;                                     // its bit number blockIdx.y
   for (unsigned k = 0; k < blockIdx.y; ++k) which &= which - 1;
   which &= -which;
   const bool both = which == SUM_A && p.dscale != nullptr && p.b_post != nullptr;        // then B comes next after A
-  pdl_wait();
-  float4 acc[2];
-  acc[0] = acc[1] = make_float4(0.f, 0.f, 0.f, 0.f);
-  if (e < p.C4) {
-    const float4* src = p.sums + (size_t)blockIdx.y * p.C4 + e;
-    const size_t step = (size_t)arrays * p.C4;
-#pragma unroll 5
-    for (int s = slot; s < p.slots; s += 32) {
-      acc[0] = add4(acc[0], src[s * step]);
-      if (both) acc[1] = add4(acc[1], src[s * step + p.C4]);
-    }
-  }
-#pragma unroll
-  for (int i = 0; i < 2; ++i) red[i][slot][lane] = acc[i];
-  __syncthreads();
-#pragma unroll
-  for (int half = 16; half >= 1; half >>= 1) {
-    if (slot < half) {
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        acc[i] = add4(acc[i], red[i][slot + half][lane]);
-        red[i][slot][lane] = acc[i];
-      }
-    }
-    __syncthreads();
-  }
+  total(p.sums + (size_t)blockIdx.y * p.C4 + e, p.slots, (size_t)arrays * p.C4, both, p.C4, acc);
   if (slot != 0 || e >= p.C4) return;
   const float4 one = make_float4(1.f, 1.f, 1.f, 1.f);
   const float4 s = p.scale != nullptr ? __ldg(p.scale + e) : one;
@@ -1027,23 +1080,6 @@ residual_reduce_kernel(const ResidualReduce p) {
   }
 }
 
-// dgate of a row that serves a span of tokens: the sum of its units, in order.
-__global__ void __launch_bounds__(256)
-gate_reduce_kernel(const float4* __restrict__ sums, int units_per_span, long long gates, int C4, uint2* dgate, long long pitch4) {
-  pdl_launch_dependents();
-  pdl_wait();
-  const long long all = gates * C4;
-  for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < all; i += 256ll * gridDim.x) {
-    const long long g = i / C4;
-    const int c = (int)(i - g * C4);
-    const float4* src = sums + g * units_per_span * C4 + c;
-    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 8
-    for (int u = 0; u < units_per_span; ++u) acc = add4(acc, src[(long long)u * C4]);
-    dgate[g * pitch4 + c] = make_uint2(pack_bf16_f(acc.x, acc.y), pack_bf16_f(acc.z, acc.w));
-  }
-}
-
 // ---- plans --------------------------------------------------------------------------------------
 struct RowPlan {
   int cluster, warps, groups, threads;                    // CTAs that share a row, its warps in each, rows side by side
@@ -1052,21 +1088,24 @@ struct RowPlan {
   int unit_rows, units_per_span;
 };
 
+// one_slot: a few rows go to one cluster (two steps cost less than a launch that adds up what several leave).
 // ctas: how many the card holds.  span > 1: units end where a gate row's span ends, and are as many as the groups of warps.
-RowPlan plan_rows(int T, int C, int span, int ctas) {
+RowPlan plan_rows(int T, int C, int span, int ctas, bool one_slot = false) {
   RowPlan b = {};
   const int all = (C / 8 + 32 * VECS - 1) / (32 * VECS), most = ROW_THREADS / 32;         // warps of a row, of a CTA
   b.cluster = all > 2 * most ? 4 : all > most ? 2 : 1;
   b.warps = (all + b.cluster - 1) / b.cluster;
   b.groups = ROW_THREADS / 32 / b.warps;
   b.threads = 32 * b.warps * b.groups;
-  const long long room = (long long)(ctas / b.cluster) * b.groups;
+  const bool few = one_slot && T <= 2 * ROWS * b.groups;
+  const long long room = (long long)(few ? 1 : ctas / b.cluster) * b.groups;
   if (span > 1) {
     const int len = span < T ? span : T;
     b.gates = (T + (long long)span - 1) / span;
     b.unit_rows = (int)((T + room - 1) / room);
     if (b.unit_rows > 1 && b.unit_rows % ROWS != 0) b.unit_rows += ROWS - b.unit_rows % ROWS;
-    if (b.unit_rows > len) b.unit_rows = len;
+    // whole spans where they keep half of the groups busy, or are two steps: nothing is left to add up then
+    if (b.unit_rows > len || 2 * b.gates >= room || len <= 2 * ROWS) b.unit_rows = len;
     b.units_per_span = (len + b.unit_rows - 1) / b.unit_rows;
     b.units = b.gates * b.units_per_span;
   } else {
@@ -1075,6 +1114,7 @@ RowPlan plan_rows(int T, int C, int span, int ctas) {
   }
   const long long slots = (b.units + b.groups - 1) / b.groups;
   b.slots = (int)(slots < ctas / b.cluster ? slots : ctas / b.cluster);
+  if (few) b.slots = 1;
   return b;
 }
 
@@ -1204,7 +1244,7 @@ int launch_residual_fwd(const bimask_residual_args& a, cudaStream_t s) {
 int launch_residual_bwd(const bimask_residual_args& a, cudaStream_t s) {
   ResidualParams p = residual_params(a);
   const bool spanned = a.dgate != nullptr && p.gate_span > 1;
-  const RowPlan b = plan_rows(a.T, a.C, spanned ? (int)p.gate_span : 1, PLAN_SMS);
+  const RowPlan b = plan_rows(a.T, a.C, spanned ? (int)p.gate_span : 1, PLAN_SMS, true);
   take_plan(p, b);
   const bool branch = a.dy || a.dgate || a.dscale || a.dw_post || a.db_post, post = branch && a.post != BIMASK_NORM_NONE;
   p.has = (a.pre != BIMASK_NORM_NONE ? HAS_PRE : 0) | (a.dxo ? HAS_DXO : 0) | (branch && a.y ? HAS_Y : 0) | (post ? HAS_POST : 0);
@@ -1218,8 +1258,13 @@ int launch_residual_bwd(const bimask_residual_args& a, cudaStream_t s) {
   p.scale_too = post && a.w_post ? a.scale : nullptr;
   const bool scale = a.dscale != nullptr;
   p.want = (a.dw_post || scale ? SUM_A : 0) | (a.db_post || (scale && a.b_post) ? SUM_B : 0) | (a.dw_pre ? SUM_G1 : 0) | (a.db_pre ? SUM_G2 : 0);
-  p.sums = reinterpret_cast<float*>(a.ws);
-  if (spanned) p.gate_sums = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(a.ws) + column_sums_bytes(a.T, a.C, (int)p.gate_span));
+  p.dscale = a.dscale;
+  p.dw_post = a.dw_post;
+  p.db_post = a.db_post;
+  p.dw_pre = a.dw_pre;
+  p.db_pre = a.db_pre;
+  if (b.slots > 1) p.sums = reinterpret_cast<float*>(a.ws);
+  if (spanned && b.units_per_span > 1) p.gate_sums = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(a.ws) + column_sums_bytes(a.T, a.C, (int)p.gate_span));
   using Yes = std::true_type;
   using No = std::false_type;
   auto run = [&](auto f32, auto gate, auto post, auto wide, auto cluster) -> int {
@@ -1242,11 +1287,12 @@ int launch_residual_bwd(const bimask_residual_args& a, cudaStream_t s) {
   };
   const int rc = a.stream_type == BIMASK_TYPE_F32 ? pick(std::true_type()) : pick(std::false_type());
   if (rc != BIMASK_OK) return rc;
-  if (p.want != 0) {
+  const int arrays = p.sums != nullptr ? __builtin_popcount(p.want) : 0;
+  if (arrays != 0 || p.gate_sums != nullptr) {
     ResidualReduce r = {};
-    r.sums = reinterpret_cast<const float4*>(a.ws);
+    r.sums = reinterpret_cast<const float4*>(p.sums);
     r.slots = b.slots;
-    r.want = p.want;
+    r.want = arrays != 0 ? p.want : 0;
     r.C4 = a.C / 4;
     r.scale = reinterpret_cast<const float4*>(a.scale);
     r.w_post = reinterpret_cast<const float4*>(a.w_post);
@@ -1256,13 +1302,15 @@ int launch_residual_bwd(const bimask_residual_args& a, cudaStream_t s) {
     r.db_post = reinterpret_cast<float4*>(a.db_post);
     r.dw_pre = reinterpret_cast<float4*>(a.dw_pre);
     r.db_pre = reinterpret_cast<float4*>(a.db_pre);
-    BIMASK_CUDA_OK(launch_pdl(residual_reduce_kernel, dim3((r.C4 + 7) / 8, __builtin_popcount(p.want)), 256, 0, s, r));
-    count_launch();
-  }
-  if (p.gate_sums != nullptr) {
-    const long long ctas = (b.gates * (a.C / 4) + 255) / 256, most = 8ll * sm_count();
-    BIMASK_CUDA_OK(launch_pdl(gate_reduce_kernel, (unsigned)(ctas < most ? ctas : most), 256, 0, s, reinterpret_cast<const float4*>(p.gate_sums),
-                              b.units_per_span, b.gates, a.C / 4, reinterpret_cast<uint2*>(a.dgate), a.gate_pitch / 4));
+    if (p.gate_sums != nullptr) {
+      r.gate_sums = reinterpret_cast<const float4*>(p.gate_sums);
+      r.units_per_span = b.units_per_span;
+      r.dgate = reinterpret_cast<uint2*>(a.dgate);
+      r.gate_pitch4 = a.gate_pitch / 4;
+      r.gates = b.gates;
+    }
+    const long long rows = arrays + (r.gates < 4096 ? r.gates : 4096);
+    BIMASK_CUDA_OK(launch_pdl(residual_reduce_kernel, dim3((r.C4 + 7) / 8, (unsigned)rows), 256, 0, s, r));
     count_launch();
   }
   BIMASK_CUDA_OK(cudaGetLastError());
