@@ -291,9 +291,11 @@ int bimask_act_dropout_bwd(const uint16_t* dY, const int8_t* Zq, const uint8_t* 
  *            norm after, gate, scale, w_*, b_post, drop as in the forward pass; y with a norm after, dgate or dscale.
  *            out, each of them NULL where it is not wanted: dx (may be dxo), dy (may be dn or y), dgate (summed over its span, rounded
  *            once), dscale, dw_post, db_post, dw_pre, db_pre (fp32, added in an order that depends on the sizes alone).
- *            With y absent in the forward pass only dx, dw_pre and db_pre are asked for (xo: alpha x).
+ *            With y absent in the forward pass only dx, dw_pre and db_pre are asked for (xo: alpha x).  Where an element was dropped
+ *            its gradient is 0 times that of x'.
  *            ws: bimask_residual_norm_workspace_bytes(T, C, gate_span, or 1 without a gate) bytes, needed for gradients of vectors
- *            and of a gate with gate_span > 1.  Never fewer for more tokens. */
+ *            and of a gate with gate_span > 1; nothing is expected in it, and calls that may overlap need one each.  Never
+ *            fewer for more tokens. */
 typedef struct {
   int T, C;
   int stream_type, post, pre;  /* BIMASK_TYPE_*, BIMASK_NORM_* */

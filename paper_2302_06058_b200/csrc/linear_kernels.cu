@@ -206,6 +206,8 @@ act_dropout_bwd_kernel(const uint4* dY, const uint2* __restrict__ zq, const uint
   for (int k = 0; k < 4; ++k) sum[k] = act::both(0.f);
   if (ok) {
     const uint32_t stride = rows * gridDim.y;
+    // bytes of zs (their low 32 bits): the last word, which only the last four rows can reach, may have fewer than four
+    const uint32_t scales = (uint32_t)((unsigned long long)T * C8 >> 2), whole = T > 4u ? T - 4u : 0u;
     uint32_t ahead = blockIdx.y * rows + g;
     auto fetch = [&](uint32_t stage) {
       if (ahead < T) {
@@ -213,7 +215,9 @@ act_dropout_bwd_kernel(const uint4* dY, const uint2* __restrict__ zq, const uint
         asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(ring_d + stage * (DROPBWD_THREADS * 16)), "l"(dY + at) : "memory");
         if (ACT != BIMASK_ACT_NONE) {
           asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(ring_q + stage * (DROPBWD_THREADS * 8)), "l"(zq + at) : "memory");
-          asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(ring_s + stage * (DROPBWD_THREADS * 4)), "l"(zs + ((at >> 2) & ~3ull)) : "memory");
+          const unsigned long long word = (at >> 2) & ~3ull;
+          asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(ring_s + stage * (DROPBWD_THREADS * 4)), "l"(zs + word),
+                       "r"(ahead < whole ? 4u : min(4u, scales - (uint32_t)word)) : "memory");
         }
       }
       asm volatile("cp.async.commit_group;" ::: "memory");

@@ -131,9 +131,11 @@ class Problem:
 
     # the statements and their tolerances
     def hat_tolerance(self, v, hat, rstd, extra=0.0):
+        """(of the normalised values, relative of rstd) where v itself is off by up to `extra`."""
+        extra = np.broadcast_to(extra, v.shape)
         mag = (np.abs(v) + np.abs(v).mean(1, keepdims=True)) * rstd
-        rel = 32 * U * (1 + mag.max(1, keepdims=True)) + 2 * np.max(extra * rstd, axis=1, keepdims=True) if np.ndim(extra) else 32 * U * (1 + mag.max(1, keepdims=True))
-        return 32 * U * mag + extra * rstd + (np.mean(extra, axis=1, keepdims=True) * rstd if np.ndim(extra) else 0.0) + np.abs(hat) * rel, rel
+        rel = 32 * U * (1 + mag.max(1, keepdims=True)) + 2 * (extra * rstd).max(1, keepdims=True)
+        return 32 * U * mag + (extra + extra.mean(1, keepdims=True)) * rstd + np.abs(hat) * rel, rel
 
     def check_forward(self, o):
         h, span = self.h, max(self.span, 1)
@@ -293,6 +295,16 @@ def test_parts_that_are_absent(stream):
     q.check_forward(f)
     g = q.backward(f)
     q.check_backward({k: g[k] for k in ("dx", "dy", "dgate")}, f)
+    # gradients of a scale and a weight that are absent in the forward pass, and so 1
+    for post in (0, 2):
+        q = Problem(T, C, post, 1, stream, span=1, p=0.1)
+        for k in ("w_post", "scale"):
+            if k in q.d:
+                del q.d[k]
+                q.h[k] = np.ones(C)
+        f = q.forward()
+        more = q.like(dscale=((C,), torch.float32), **({"dw_post": ((C,), torch.float32)} if post else {}))
+        q.check_backward(q.backward(f, **more), f)
     # every gradient alone is what it is among the others
     q = Problem(T, C, 2, 2, stream, span=9, p=0.1)
     f = q.forward()
