@@ -183,10 +183,10 @@ act_bwd_kernel(const uint4* dY, const uint2* __restrict__ zq, const uint8_t* __r
 // The same with dY dropped first.  The generator doubles the instructions per element (245 for a block of eight with a GELU, two
 // thirds of what the SMs can issue in the time that HBM needs), so this kernel wants warps rather than registers: 32 of them, a
 // thread with one block of eight columns, and the rows ahead in shared memory, copied by the threads that will use them (cp.async:
-// every thread waits for its own pieces only).  A scale byte comes with the aligned word around it.
+// every thread waits for its own pieces only); a row's scale byte, shared by four threads, is loaded a row ahead.
 // ------------------------------------------------------------------------------------------
 constexpr int DROPBWD_THREADS = 1024, DROPBWD_STAGES = 4;
-constexpr int DROPBWD_SMEM = DROPBWD_STAGES * DROPBWD_THREADS * (16 + 8 + 4);
+constexpr int DROPBWD_SMEM = DROPBWD_STAGES * DROPBWD_THREADS * (16 + 8);
 
 template <int ACT>
 __global__ void __launch_bounds__(DROPBWD_THREADS, 1)
@@ -197,52 +197,47 @@ act_dropout_bwd_kernel(const uint4* dY, const uint2* __restrict__ zq, const uint
   const uint32_t g = threadIdx.x / (uint32_t)cols, lc = threadIdx.x - g * (uint32_t)cols, c = blockIdx.x * (uint32_t)cols + lc;
   const bool ok = g < rows && c < C8;
   const uint32_t base = (uint32_t)__cvta_generic_to_shared(smem);
-  const uint32_t ring_d = base + threadIdx.x * 16u, ring_q = base + DROPBWD_STAGES * DROPBWD_THREADS * 16u + threadIdx.x * 8u,
-                 ring_s = base + DROPBWD_STAGES * DROPBWD_THREADS * 24u + threadIdx.x * 4u;
+  const uint32_t ring_d = base + threadIdx.x * 16u, ring_q = base + DROPBWD_STAGES * DROPBWD_THREADS * 16u + threadIdx.x * 8u;
   pdl_wait();
   const unsigned long long number = drop_number(drop);
   act::Pair sum[4];
 #pragma unroll
   for (int k = 0; k < 4; ++k) sum[k] = act::both(0.f);
   if (ok) {
-    const uint32_t stride = rows * gridDim.y;
-    // bytes of zs (their low 32 bits): the last word, which only the last four rows can reach, may have fewer than four
-    const uint32_t scales = (uint32_t)((unsigned long long)T * C8 >> 2), whole = T > 4u ? T - 4u : 0u;
-    uint32_t ahead = blockIdx.y * rows + g;
+    const uint32_t stride = rows * gridDim.y, first = blockIdx.y * rows + g;
+    const unsigned long long hop = (unsigned long long)stride * C8;
+    unsigned long long at = (unsigned long long)first * C8 + c, lead = at;
+    uint32_t ahead = first;
     auto fetch = [&](uint32_t stage) {
       if (ahead < T) {
-        const unsigned long long at = (unsigned long long)ahead * C8 + c;
-        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(ring_d + stage * (DROPBWD_THREADS * 16)), "l"(dY + at) : "memory");
-        if (ACT != BIMASK_ACT_NONE) {
-          asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(ring_q + stage * (DROPBWD_THREADS * 8)), "l"(zq + at) : "memory");
-          const unsigned long long word = (at >> 2) & ~3ull;
-          asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(ring_s + stage * (DROPBWD_THREADS * 4)), "l"(zs + word),
-                       "r"(ahead < whole ? 4u : min(4u, scales - (uint32_t)word)) : "memory");
-        }
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(ring_d + stage * (DROPBWD_THREADS * 16)), "l"(dY + lead) : "memory");
+        if (ACT != BIMASK_ACT_NONE)
+          asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(ring_q + stage * (DROPBWD_THREADS * 8)), "l"(zq + lead) : "memory");
       }
       asm volatile("cp.async.commit_group;" ::: "memory");
       ahead += stride;
+      lead += hop;
     };
 #pragma unroll
     for (int s = 0; s < DROPBWD_STAGES - 1; ++s) fetch(s);
-    uint32_t stage = 0;
-    for (uint32_t t = blockIdx.y * rows + g; t < T; t += stride) {
+    uint32_t stage = 0, next_scale = ACT != BIMASK_ACT_NONE && first < T ? __ldg(zs + (at >> 2)) : 0u;
+    for (uint32_t t = first; t < T; t += stride, at += hop) {
+      const uint32_t scale_byte = next_scale;
+      if (ACT != BIMASK_ACT_NONE && t + stride < T) next_scale = __ldg(zs + ((at + hop) >> 2));
       asm volatile("cp.async.wait_group %0;" ::"n"(DROPBWD_STAGES - 2) : "memory");
-      const unsigned long long at = (unsigned long long)t * C8 + c;
       uint4 d;
       asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(d.x), "=r"(d.y), "=r"(d.z), "=r"(d.w) : "r"(ring_d + stage * (DROPBWD_THREADS * 16)) : "memory");
       act::Pair v[4] = {bf16_pair(d.x), bf16_pair(d.y), bf16_pair(d.z), bf16_pair(d.w)};
       act::Pair a[4];
       if constexpr (ACT != BIMASK_ACT_NONE) {
         uint2 z;
-        uint32_t s;
         asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(z.x), "=r"(z.y) : "r"(ring_q + stage * (DROPBWD_THREADS * 8)) : "memory");
-        asm volatile("ld.shared.u32 %0, [%1];" : "=r"(s) : "r"(ring_s + stage * (DROPBWD_THREADS * 4)) : "memory");
-        const act::Pair scale = act::both(ckpt::scale_value((s >> (8u * ((uint32_t)(at >> 2) & 3u))) & 255u));
+        const act::Pair scale = act::both(ckpt::scale_value(scale_byte));
         ckpt::decode4(z.x, scale, a);
         ckpt::decode4(z.y, scale, a + 2);
       }
-      fetch((stage + DROPBWD_STAGES - 1) % DROPBWD_STAGES);      // into the pieces that the row before this one left
+      // into the pieces that the row before this one left
+      fetch((stage + DROPBWD_STAGES - 1) % DROPBWD_STAGES);
       stage = (stage + 1) % DROPBWD_STAGES;
       drop8(v, at, number, drop);
       if constexpr (ACT != BIMASK_ACT_NONE) {

@@ -698,6 +698,16 @@ residual_bwd_kernel(const __grid_constant__ ResidualParams p) {
     }
     copies_commit();
   };
+  Pair sum_a[VECS][4], sum_g1[VECS][4], sum_b[VECS][4], sum_g2[VECS][4], fsum[VECS][4];
+#pragma unroll
+  for (int j = 0; j < VECS; ++j) {
+    fill8(sum_a[j], 0.f);
+    fill8(sum_g1[j], 0.f);
+    fill8(sum_b[j], 0.f);
+    fill8(sum_g2[j], 0.f);
+    fill8(fsum[j], 0.f);
+  }
+  fetch(ahead, 0);
   // the parameters of this thread's columns, w_pre and scale w_post: from its own pieces after the ring, or from memory
   const uint32_t kept = ring + ring_bytes(SLOTS);
   auto weights = [&](Pair (&w)[VECS][4]) {
@@ -736,16 +746,6 @@ residual_bwd_kernel(const __grid_constant__ ResidualParams p) {
       }
     }
   }
-  Pair sum_a[VECS][4], sum_g1[VECS][4], sum_b[VECS][4], sum_g2[VECS][4], fsum[VECS][4];
-#pragma unroll
-  for (int j = 0; j < VECS; ++j) {
-    fill8(sum_a[j], 0.f);
-    fill8(sum_g1[j], 0.f);
-    fill8(sum_b[j], 0.f);
-    fill8(sum_g2[j], 0.f);
-    fill8(fsum[j], 0.f);
-  }
-  fetch(ahead, 0);
   uint32_t stage = 0;
   while (work.more(p)) {
     __syncwarp();                                         // every lane has read the statistics that are overwritten now
