@@ -92,8 +92,8 @@ dropout_kernel(const void* x, long long blocks, void* y /* may be x */, const __
 }
 
 // ------------------------------------------------------------------------------------------
-// Rows.  A thread owns two blocks of eight columns for good; `warps` warps of a CTA, and up to four CTAs of a cluster above 4096
-// columns, share a row.  A CTA holds as many such groups as its eight warps give; they work on rows of their own and never meet (named
+// Rows.  A thread owns two blocks of eight columns for good; `warps` warps of a CTA, and two or four CTAs of a cluster where a CTA's are
+// not enough, share a row.  A CTA holds as many such groups as its warps give; they work on rows of their own and never meet (named
 // barriers).  A group takes two rows per step: what its threads exchange for both travels together, and the two rows' chains
 // of dependent instructions run side by side.  The rows of the next step are already on their way: every thread copies its own
 // 16-byte pieces into its own places in shared memory (cp.async), so no barrier guards them, no registers wait for them, and
@@ -103,8 +103,9 @@ dropout_kernel(const void* x, long long blocks, void* y /* may be x */, const __
 // the others, but for their stores.
 // ------------------------------------------------------------------------------------------
 constexpr int ROWS = 2, VECS = 2, STAGES = 2;
-constexpr int ROW_THREADS = 256;
-constexpr int MAX_ROW_WARPS = 32;                         // of a cluster of four CTAs
+// Threads of a CTA (one per SM).  The backward pass keeps five to eight arrays of a step in registers and wants 255 of them.
+constexpr int FWD_THREADS = 512, BWD_THREADS = 256;
+constexpr int MAX_ROW_WARPS = 32;                         // of a cluster of two or four CTAs
 static_assert(RESIDUAL_MAX_C == 8 * 32 * VECS * MAX_ROW_WARPS, "eight columns of each of a thread's blocks");
 
 struct ResidualParams {
@@ -210,12 +211,12 @@ __device__ __forceinline__ float columns_of(int w, uint32_t C8) { return 8.f * (
 
 // Exchange buffers: a group's two, of VALUES values from each of its row's warps (zeros up to a multiple of four warps).  Groups of two
 // warps or more, so that four words for two warps are the worst.
-template <int VALUES, bool CLUSTER>
+template <int VALUES, int THREADS, bool CLUSTER>
 struct Exchange {
-  static constexpr int WORDS = CLUSTER ? MAX_ROW_WARPS : ROW_THREADS / 64 * 4;
+  static constexpr int WORDS = CLUSTER ? MAX_ROW_WARPS : THREADS / 64 * 4;
   static constexpr int BYTES = 2 * VALUES * WORDS * 4;
 };
-template <int VALUES, bool CLUSTER>
+template <int VALUES, int THREADS, bool CLUSTER>
 struct Group {                                            // a thread's place among those that share its rows
   int lane, group, warps;                                 // warps: of the row in this CTA
   int warp;                                               // the thread's warp, counted through the row
@@ -236,7 +237,7 @@ struct Group {                                            // a thread's place am
     alone = !CLUSTER && warps == 1;
     width = CLUSTER ? MAX_ROW_WARPS : (warps + 3) & ~3;
     inv_columns = 1.f / fmaxf(columns_of(warp, p.C8), 1.f);
-    for (int k = 0; k < (CLUSTER ? MAX_ROW_WARPS / 16 : 1); ++k) peer_columns[k] = columns_of((lane & (CLUSTER ? 15 : 7)) + 16 * k, p.C8);
+    for (int k = 0; k < (CLUSTER ? MAX_ROW_WARPS / 16 : 1); ++k) peer_columns[k] = columns_of((lane & (CLUSTER ? 15 : THREADS / 32 - 1)) + 16 * k, p.C8);
     buffer = exchange + (uint32_t)((alone ? 0 : group) * 2 * VALUES * width * 4);
     flip = buffer ^ (buffer + (uint32_t)(VALUES * width * 4));
   }
@@ -274,8 +275,8 @@ __device__ __forceinline__ float fold(float (&c)[N], int lane) {
 }
 
 // Totals over the row of N values of every thread.
-template <int N, bool CLUSTER>
-__device__ __forceinline__ void row_totals(Group<N, CLUSTER>& g, float (&c)[N]) {
+template <int N, int THREADS, bool CLUSTER>
+__device__ __forceinline__ void row_totals(Group<N, THREADS, CLUSTER>& g, float (&c)[N]) {
   constexpr int LANES = 32 / N;                           // that share a value
   float v = fold<N>(c, g.lane);
   if (!g.alone) {
@@ -284,7 +285,7 @@ __device__ __forceinline__ void row_totals(Group<N, CLUSTER>& g, float (&c)[N]) 
     g.meet();
     v = 0.f;
 #pragma unroll
-    for (int k = 0; k < (CLUSTER ? MAX_ROW_WARPS : ROW_THREADS / 32) / 4; k += LANES) {
+    for (int k = 0; k < (CLUSTER ? MAX_ROW_WARPS : THREADS / 32) / 4; k += LANES) {
       const int w = 4 * (part + k);
       if (w < g.width) {
         float4 x;
@@ -310,9 +311,9 @@ __device__ __forceinline__ float rsqrt_fast(float x) {
 // Mean and 1 / deviation of two rows (LAYER: some norm of this kernel subtracts means; `layer`: this one does).  The squares are taken
 // about each warp's own mean, and the warps are put together by M = sum M_w + sum n_w (m_w - m)^2: one exchange, and no difference
 // of large squares.  rms: all about zero.
-template <bool LAYER, bool CLUSTER>
+template <bool LAYER, int THREADS, bool CLUSTER>
 __device__ __forceinline__ void row_stats(const Pair (&v)[ROWS][VECS][4], const bool (&ok)[VECS], bool layer, float eps, float inv_c,
-                                          Group<4, CLUSTER>& g, float2 (&st)[ROWS]) {
+                                          Group<4, THREADS, CLUSTER>& g, float2 (&st)[ROWS]) {
   static_assert(ROWS == 2, "two rows are folded together");
   const int half = g.lane >> 4;                           // the row whose totals this lane holds
   float m = 0.f, q[ROWS];
@@ -345,7 +346,7 @@ __device__ __forceinline__ void row_stats(const Pair (&v)[ROWS][VECS][4], const 
     }
     g.meet();
     sq = 0.f;
-    constexpr int EACH = CLUSTER ? MAX_ROW_WARPS / 16 : 1, SPREAD = CLUSTER ? 8 : ROW_THREADS / 64;
+    constexpr int EACH = CLUSTER ? MAX_ROW_WARPS / 16 : 1, SPREAD = CLUSTER ? 8 : THREADS / 64;
     float own[EACH];
 #pragma unroll
     for (int k = 0; k < EACH; ++k) {
@@ -409,28 +410,28 @@ struct Walk {
 };
 
 // Shared memory of a CTA: the ring of the threads' pieces, the statistics of every warp's rows, the exchange buffers.
-constexpr int PITCH = ROW_THREADS * 16;                   // from a thread's piece to its next
+BIMASK_HD constexpr int pitch_of(int threads) { return threads * 16; }      // from a thread's piece to its next
 constexpr int STATS_STAGE = 2 * ROWS * 8;                 // bytes of a warp's statistics: before, after
-constexpr int STATS_BYTES = STAGES * (ROW_THREADS / 32) * STATS_STAGE;
-BIMASK_HD constexpr int fwd_slots(bool f32, bool gate) { return (f32 ? 2 : 1) + 1 + (gate ? 1 : 0); }
+constexpr int STATS_BYTES = STAGES * (BWD_THREADS / 32) * STATS_STAGE;
 // With an fp32 stream the ring has no room for a gate's pieces: it is read from memory (L2) where it is used.
-BIMASK_HD constexpr bool bwd_gate_in_ring(bool f32, bool gate) { return gate && !f32; }
-BIMASK_HD constexpr int bwd_slots(bool f32, bool gate) { return (f32 ? 4 : 2) + 2 + (bwd_gate_in_ring(f32, gate) ? 1 : 0); }
+BIMASK_HD constexpr bool gate_in_ring(bool f32, bool gate) { return gate && !f32; }
+BIMASK_HD constexpr int fwd_slots(bool f32, bool gate) { return (f32 ? 2 : 1) + 1 + (gate_in_ring(f32, gate) ? 1 : 0); }
+BIMASK_HD constexpr int bwd_slots(bool f32, bool gate) { return (f32 ? 4 : 2) + 2 + (gate_in_ring(f32, gate) ? 1 : 0); }
 // The backward pass keeps two parameters of the threads' columns beside the ring (from memory they cost it a fifth of the time with
 // an fp32 stream, whose ring leaves no first-level cache); only there a cluster's larger exchange buffers leave no room.
 BIMASK_HD constexpr bool bwd_keeps_params(bool f32, bool cluster) { return !(f32 && cluster); }
-constexpr int PARAM_BYTES = 2 * VECS * 2 * PITCH;
+constexpr int PARAM_BYTES = 2 * VECS * 2 * pitch_of(BWD_THREADS);
 BIMASK_HD constexpr int bwd_values(bool post, bool wide) { return !post ? 2 : !wide ? 4 : 8; }
-BIMASK_HD constexpr int ring_bytes(int slots) { return STAGES * ROWS * VECS * slots * PITCH; }
-constexpr int FWD_CTAS = 2;                               // of the forward kernel on an SM
+BIMASK_HD constexpr int stage_bytes(int threads, int slots) { return ROWS * VECS * slots * pitch_of(threads); }
+BIMASK_HD constexpr int ring_bytes(int threads, int slots) { return STAGES * stage_bytes(threads, slots); }
 
-template <bool F32>
+template <bool F32, int PITCH>
 __device__ __forceinline__ void copy_block(uint32_t dst, const void* base, unsigned long long block, bool live) {
   const uint4* src = reinterpret_cast<const uint4*>(base) + block * (F32 ? 2 : 1);
   copy16(dst, src, live);
   if (F32) copy16(dst + PITCH, src + 1, live);
 }
-template <bool F32>
+template <bool F32, int PITCH>
 __device__ __forceinline__ void read_block(uint32_t at, Pair (&v)[4]) {
   Vec8<F32> raw;
 #pragma unroll
@@ -439,9 +440,9 @@ __device__ __forceinline__ void read_block(uint32_t at, Pair (&v)[4]) {
                  : "r"(at + h * PITCH) : "memory");
   unpack8<F32>(raw, v);
 }
-template <int VALUES, bool CLUSTER>
+template <int VALUES, int THREADS, bool CLUSTER>
 __device__ __forceinline__ void clear_exchange(float* exchange) {
-  for (int i = threadIdx.x; i < Exchange<VALUES, CLUSTER>::BYTES / 4; i += blockDim.x) exchange[i] = 0.f;
+  for (int i = threadIdx.x; i < Exchange<VALUES, THREADS, CLUSTER>::BYTES / 4; i += blockDim.x) exchange[i] = 0.f;
   if (CLUSTER) ptx::cluster_sync();                       // before a peer writes here, and before this CTA writes to a peer
   else __syncthreads();
 }
@@ -485,19 +486,21 @@ __device__ __forceinline__ void param_or_one(const float* base, const Blocks& b,
   }
 }
 // address of a thread's piece: slot of block j of row r
-template <int SLOTS>
+template <int SLOTS, int PITCH>
 __device__ __forceinline__ uint32_t piece(uint32_t stage_at, int r, int j, int slot) { return stage_at + ((r * VECS + j) * SLOTS + slot) * PITCH; }
 
 template <bool F32, bool GATE, bool LAYER, bool CLUSTER>
-__global__ void __launch_bounds__(ROW_THREADS, FWD_CTAS)
+__global__ void __launch_bounds__(FWD_THREADS, 1)
 residual_fwd_kernel(const __grid_constant__ ResidualParams p) {
   extern __shared__ float4 smem[];
   constexpr int SLOTS = fwd_slots(F32, GATE), X = 0, Y = F32 ? 2 : 1, G = Y + 1;
-  constexpr uint32_t STAGE = ROWS * VECS * SLOTS * PITCH;
-  float* exchange = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(smem) + ring_bytes(SLOTS));
+  constexpr bool GATE_RING = gate_in_ring(F32, GATE);
+  constexpr int PITCH = pitch_of(FWD_THREADS);
+  constexpr uint32_t STAGE = stage_bytes(FWD_THREADS, SLOTS);
+  float* exchange = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(smem) + ring_bytes(FWD_THREADS, SLOTS));
   pdl_launch_dependents();
-  clear_exchange<4, CLUSTER>(exchange);
-  Group<4, CLUSTER> g(p, smem_addr(exchange));
+  clear_exchange<4, FWD_THREADS, CLUSTER>(exchange);
+  Group<4, FWD_THREADS, CLUSTER> g(p, smem_addr(exchange));
   const Blocks b(g.warp, g.lane, p.C8);
   const uint32_t groups = blockDim.x / (32u * (uint32_t)p.warps);
   const uint32_t stride = CLUSTER ? gridDim.x / (uint32_t)p.cluster : gridDim.x * groups;
@@ -508,6 +511,7 @@ residual_fwd_kernel(const __grid_constant__ ResidualParams p) {
   ahead = work;
   pdl_wait();
   const unsigned long long number = drop_number(p.drop);
+  auto gate_row = [&](uint32_t t) { return p.gate + (long long)(p.gate_span == 1u ? t : t / p.gate_span) * p.gate_pitch8; };
   auto fetch = [&](const Walk<false>& w, uint32_t stage) {
     const uint32_t at = ring + stage * STAGE;
 #pragma unroll
@@ -515,12 +519,11 @@ residual_fwd_kernel(const __grid_constant__ ResidualParams p) {
       const bool live = w.more(p) && w.t + r < w.end;
       const uint32_t t = min(w.t + r, p.T - 1u);
       const unsigned long long row = (unsigned long long)t * p.C8;
-      const uint4* gate = GATE ? p.gate + (long long)(p.gate_span == 1u ? t : t / p.gate_span) * p.gate_pitch8 : nullptr;
 #pragma unroll
       for (int j = 0; j < VECS; ++j) {
-        copy_block<F32>(piece<SLOTS>(at, r, j, X), p.x, row + b.safe[j], live && b.ok[j]);
-        if (p.y != nullptr) copy16(piece<SLOTS>(at, r, j, Y), p.y + row + b.safe[j], live && b.ok[j]);
-        if (GATE) copy16(piece<SLOTS>(at, r, j, G), gate + b.safe[j], live && b.ok[j]);
+        copy_block<F32, PITCH>(piece<SLOTS, PITCH>(at, r, j, X), p.x, row + b.safe[j], live && b.ok[j]);
+        if (p.y != nullptr) copy16(piece<SLOTS, PITCH>(at, r, j, Y), p.y + row + b.safe[j], live && b.ok[j]);
+        if (GATE_RING) copy16(piece<SLOTS, PITCH>(at, r, j, G), gate_row(t) + b.safe[j], live && b.ok[j]);
       }
     }
     copies_commit();
@@ -544,7 +547,7 @@ residual_fwd_kernel(const __grid_constant__ ResidualParams p) {
 #pragma unroll
       for (int r = 0; r < ROWS; ++r)
 #pragma unroll
-        for (int j = 0; j < VECS; ++j) read_block<false>(piece<SLOTS>(at, r, j, Y), v[r][j]);
+        for (int j = 0; j < VECS; ++j) read_block<false, PITCH>(piece<SLOTS, PITCH>(at, r, j, Y), v[r][j]);
       if (p.post != BIMASK_NORM_NONE) {
         float2 st[ROWS];
         row_stats<LAYER>(v, b.ok, p.post == BIMASK_NORM_LAYER, p.eps_post, p.inv_c, g, st);
@@ -574,7 +577,8 @@ residual_fwd_kernel(const __grid_constant__ ResidualParams p) {
 #pragma unroll
           for (int j = 0; j < VECS; ++j) {
             Pair w[4];
-            read_block<false>(piece<SLOTS>(at, r, j, G), w);
+            if (GATE_RING) read_block<false, PITCH>(piece<SLOTS, PITCH>(at, r, j, G), w);
+            else unpack8<false>(Vec8<false>{__ldg(gate_row(min(work.t + r, p.T - 1u)) + b.safe[j])}, w);
             times8(v[r][j], w);
           }
       }
@@ -591,7 +595,7 @@ residual_fwd_kernel(const __grid_constant__ ResidualParams p) {
 #pragma unroll
       for (int j = 0; j < VECS; ++j) {
         Pair x[4];
-        read_block<F32>(piece<SLOTS>(at, r, j, X), x);
+        read_block<F32, PITCH>(piece<SLOTS, PITCH>(at, r, j, X), x);
 #pragma unroll
         for (int k = 0; k < 4; ++k) v[r][j][k] = act::fma2(x[k], alpha, v[r][j][k]);
         if (p.xo != nullptr && live[r] && b.ok[j]) store8<F32>(p.xo, (long long)(row[r] + b.at[j]), v[r][j]);
@@ -645,19 +649,20 @@ enum { SUM_A = 1, SUM_B = 2, SUM_G1 = 4, SUM_G2 = 8 };
 enum { HAS_PRE = 1, HAS_DXO = 2, HAS_Y = 4, HAS_POST = 8 };
 
 template <bool F32, int GATE, bool POST, bool WIDE, bool CLUSTER>
-__global__ void __launch_bounds__(ROW_THREADS, 1)
+__global__ void __launch_bounds__(BWD_THREADS, 1)
 residual_bwd_kernel(const __grid_constant__ ResidualParams p) {
   extern __shared__ float4 smem[];
   constexpr int SLOTS = bwd_slots(F32, GATE != 0), XB = F32 ? 2 : 1, X = 0, DX = XB, DN = 2 * XB, Y = DN + 1, G = Y + 1;
-  constexpr bool GATE_RING = bwd_gate_in_ring(F32, GATE != 0);
+  constexpr bool GATE_RING = gate_in_ring(F32, GATE != 0);
   constexpr int NV = bwd_values(POST, WIDE);              // a row's sums: g xh, g, z E, z xh, z, w m gate (E, xh, 1)
-  constexpr uint32_t STAGE = ROWS * VECS * SLOTS * PITCH;
+  constexpr int PITCH = pitch_of(BWD_THREADS);
+  constexpr uint32_t STAGE = stage_bytes(BWD_THREADS, SLOTS);
   constexpr bool KEPT = bwd_keeps_params(F32, CLUSTER);
-  uint8_t* const after = reinterpret_cast<uint8_t*>(smem) + ring_bytes(SLOTS) + (KEPT ? PARAM_BYTES : 0);
+  uint8_t* const after = reinterpret_cast<uint8_t*>(smem) + ring_bytes(BWD_THREADS, SLOTS) + (KEPT ? PARAM_BYTES : 0);
   float* const exchange = reinterpret_cast<float*>(after + STATS_BYTES);
   pdl_launch_dependents();
-  clear_exchange<ROWS * NV, CLUSTER>(exchange);
-  Group<ROWS * NV, CLUSTER> g(p, smem_addr(exchange));
+  clear_exchange<ROWS * NV, BWD_THREADS, CLUSTER>(exchange);
+  Group<ROWS * NV, BWD_THREADS, CLUSTER> g(p, smem_addr(exchange));
   const Blocks b(g.warp, g.lane, p.C8);
   const uint32_t groups = blockDim.x / (32u * (uint32_t)p.warps);
   const uint32_t stride = CLUSTER ? gridDim.x / (uint32_t)p.cluster : gridDim.x * groups;
@@ -683,11 +688,11 @@ residual_bwd_kernel(const __grid_constant__ ResidualParams p) {
       for (int j = 0; j < VECS; ++j) {
         const bool there = live && b.ok[j];
         const unsigned long long block = row + b.safe[j];
-        copy_block<F32>(piece<SLOTS>(at, r, j, X), p.xo, block, there && (p.has & HAS_PRE));
-        copy16(piece<SLOTS>(at, r, j, DN), p.dn + block, there && (p.has & HAS_PRE));
-        copy_block<F32>(piece<SLOTS>(at, r, j, DX), p.dxo, block, there && (p.has & HAS_DXO));
-        copy16(piece<SLOTS>(at, r, j, Y), p.y + block, there && (p.has & HAS_Y));
-        if (GATE_RING) copy16(piece<SLOTS>(at, r, j, G), gate_row(t) + b.safe[j], there);
+        copy_block<F32, PITCH>(piece<SLOTS, PITCH>(at, r, j, X), p.xo, block, there && (p.has & HAS_PRE));
+        copy16(piece<SLOTS, PITCH>(at, r, j, DN), p.dn + block, there && (p.has & HAS_PRE));
+        copy_block<F32, PITCH>(piece<SLOTS, PITCH>(at, r, j, DX), p.dxo, block, there && (p.has & HAS_DXO));
+        copy16(piece<SLOTS, PITCH>(at, r, j, Y), p.y + block, there && (p.has & HAS_Y));
+        if (GATE_RING) copy16(piece<SLOTS, PITCH>(at, r, j, G), gate_row(t) + b.safe[j], there);
       }
     }
     if (g.lane < 2 * ROWS) {                              // lanes 0, 1: the rows' statistics before, 2, 3: after
@@ -709,7 +714,7 @@ residual_bwd_kernel(const __grid_constant__ ResidualParams p) {
   }
   fetch(ahead, 0);
   // the parameters of this thread's columns, w_pre and scale w_post: from its own pieces after the ring, or from memory
-  const uint32_t kept = ring + ring_bytes(SLOTS);
+  const uint32_t kept = ring + ring_bytes(BWD_THREADS, SLOTS);
   auto weights = [&](Pair (&w)[VECS][4]) {
     param_or_one(p.weight, b, w);
     if (POST && p.scale_too != nullptr) {
@@ -724,7 +729,7 @@ residual_bwd_kernel(const __grid_constant__ ResidualParams p) {
   auto params = [&](int which, Pair (&w)[VECS][4]) {
     if (KEPT) {
 #pragma unroll
-      for (int j = 0; j < VECS; ++j) read_block<true>(kept + (uint32_t)(which * VECS + j) * 2 * PITCH, w[j]);
+      for (int j = 0; j < VECS; ++j) read_block<true, PITCH>(kept + (uint32_t)(which * VECS + j) * 2 * PITCH, w[j]);
     } else if (which == 0) {
       param_or_one(p.w_pre, b, w);
     } else {
@@ -732,7 +737,7 @@ residual_bwd_kernel(const __grid_constant__ ResidualParams p) {
     }
   };
   if (KEPT) {
-    uint4* mine = reinterpret_cast<uint4*>(reinterpret_cast<uint8_t*>(smem) + ring_bytes(SLOTS)) + threadIdx.x;
+    uint4* mine = reinterpret_cast<uint4*>(reinterpret_cast<uint8_t*>(smem) + ring_bytes(BWD_THREADS, SLOTS)) + threadIdx.x;
 #pragma unroll
     for (int which = 0; which < 2; ++which) {
       Pair w[VECS][4];
@@ -741,8 +746,8 @@ residual_bwd_kernel(const __grid_constant__ ResidualParams p) {
 #pragma unroll
       for (int j = 0; j < VECS; ++j) {
         const Vec8<true> v = pack8<true>(w[j]);
-        mine[(which * VECS + j) * 2 * ROW_THREADS] = v.w[0];
-        mine[((which * VECS + j) * 2 + 1) * ROW_THREADS] = v.w[1];
+        mine[(which * VECS + j) * 2 * BWD_THREADS] = v.w[0];
+        mine[((which * VECS + j) * 2 + 1) * BWD_THREADS] = v.w[1];
       }
     }
   }
@@ -797,9 +802,9 @@ residual_bwd_kernel(const __grid_constant__ ResidualParams p) {
 #pragma unroll
       for (int j = 0; j < VECS; ++j) {
         Pair gr[4];
-        read_block<F32>(piece<SLOTS>(at, r, j, DX), E[r][j]);
-        read_block<F32>(piece<SLOTS>(at, r, j, X), xh[r][j]);
-        read_block<false>(piece<SLOTS>(at, r, j, DN), gr);
+        read_block<F32, PITCH>(piece<SLOTS, PITCH>(at, r, j, DX), E[r][j]);
+        read_block<F32, PITCH>(piece<SLOTS, PITCH>(at, r, j, X), xh[r][j]);
+        read_block<false, PITCH>(piece<SLOTS, PITCH>(at, r, j, DN), gr);
         normalise<WIDE>(xh[r][j], st);
 #pragma unroll
         for (int k = 0; k < 4; ++k) sum_g1[j][k] = act::fma2(gr[k], xh[r][j][k], sum_g1[j][k]);
@@ -819,7 +824,7 @@ residual_bwd_kernel(const __grid_constant__ ResidualParams p) {
       Pair ze = act::both(0.f), zx = ze, z0 = ze, te = ze, tx = ze, t0 = ze;
 #pragma unroll
       for (int j = 0; j < VECS; ++j) {
-        read_block<false>(piece<SLOTS>(at, r, j, Y), yh[r][j]);
+        read_block<false, PITCH>(piece<SLOTS, PITCH>(at, r, j, Y), yh[r][j]);
         if (POST) {
           normalise<WIDE>(yh[r][j], sq);
           Pair z[4];
@@ -827,7 +832,7 @@ residual_bwd_kernel(const __grid_constant__ ResidualParams p) {
           for (int k = 0; k < 4; ++k) z[k] = act::mul2(m[r][j][k], w[j][k]);
           if (GATE != 0) {
             Pair gt[4];
-            if (GATE_RING) read_block<false>(piece<SLOTS>(at, r, j, G), gt);
+            if (GATE_RING) read_block<false, PITCH>(piece<SLOTS, PITCH>(at, r, j, G), gt);
             else unpack8<false>(Vec8<false>{__ldg(gate_row(min(work.t + r, p.T - 1u)) + b.safe[j])}, gt);
             times8(z, gt);
           }
@@ -903,7 +908,7 @@ residual_bwd_kernel(const __grid_constant__ ResidualParams p) {
             }
           }
           Pair gt[4];
-          if (GATE_RING) read_block<false>(piece<SLOTS>(at, r, j, G), gt);
+          if (GATE_RING) read_block<false, PITCH>(piece<SLOTS, PITCH>(at, r, j, G), gt);
           else unpack8<false>(Vec8<false>{__ldg(gate_row(min(work.t + r, p.T - 1u)) + b.safe[j])}, gt);
           times8(E[r][j], gt);
         }
@@ -942,8 +947,8 @@ residual_bwd_kernel(const __grid_constant__ ResidualParams p) {
 #pragma unroll
       for (int j = 0; j < VECS; ++j) {
         const Vec8<true> v = pack8<true>(sum[j]);
-        mine[2 * j * ROW_THREADS] = v.w[0];
-        mine[(2 * j + 1) * ROW_THREADS] = v.w[1];
+        mine[2 * j * BWD_THREADS] = v.w[0];
+        mine[(2 * j + 1) * BWD_THREADS] = v.w[1];
       }
       __syncthreads();
     }
@@ -953,7 +958,7 @@ residual_bwd_kernel(const __grid_constant__ ResidualParams p) {
       for (int j = 0; j < VECS; ++j) {
         for (uint32_t o = 1; o < groups; ++o) {
           Pair q[4];
-          read_block<true>(ring + o * (uint32_t)p.warps * 512u + 2 * j * PITCH, q);
+          read_block<true, PITCH>(ring + o * (uint32_t)p.warps * 512u + 2 * j * PITCH, q);
           plus8(sum[j], q);
         }
         if (b.ok[j] && p.sums != nullptr) store8<true>(out, b.at[j], sum[j]);
@@ -1090,15 +1095,18 @@ struct RowPlan {
 
 // one_slot: a few rows go to one cluster (two steps cost less than a launch that adds up what several leave).
 // ctas: how many the card holds.  span > 1: units end where a gate row's span ends, and are as many as the groups of warps.
-RowPlan plan_rows(int T, int C, int span, int ctas, bool one_slot = false) {
+RowPlan plan_rows(int threads, int T, int C, int span, int ctas, bool one_slot = false) {
   RowPlan b = {};
-  const int all = (C / 8 + 32 * VECS - 1) / (32 * VECS), most = ROW_THREADS / 32;         // warps of a row, of a CTA
+  const int all = (C / 8 + 32 * VECS - 1) / (32 * VECS), most = threads / 32;             // warps of a row, of a CTA
   b.cluster = all > 2 * most ? 4 : all > most ? 2 : 1;
   b.warps = (all + b.cluster - 1) / b.cluster;
-  b.groups = ROW_THREADS / 32 / b.warps;
+  b.groups = threads / 32 / b.warps;
   b.threads = 32 * b.warps * b.groups;
+  // Clusters that run at once: of four CTAs 33 on a B200, whose parts hold no multiple of four SMs (with 37 the last four ran by
+  // themselves, 2048 x 16384 in 178 us)
+  const int clusters = b.cluster == 4 ? ctas * 32 / 148 : ctas / b.cluster;
   const bool few = one_slot && T <= 2 * ROWS * b.groups;
-  const long long room = (long long)(few ? 1 : ctas / b.cluster) * b.groups;
+  const long long room = (long long)(few ? 1 : clusters) * b.groups;
   if (span > 1) {
     const int len = span < T ? span : T;
     b.gates = (T + (long long)span - 1) / span;
@@ -1113,7 +1121,7 @@ RowPlan plan_rows(int T, int C, int span, int ctas, bool one_slot = false) {
     b.units = ((long long)T + b.unit_rows - 1) / b.unit_rows;
   }
   const long long slots = (b.units + b.groups - 1) / b.groups;
-  b.slots = (int)(slots < ctas / b.cluster ? slots : ctas / b.cluster);
+  b.slots = (int)(slots < clusters ? slots : clusters);
   if (few) b.slots = 1;
   return b;
 }
@@ -1144,14 +1152,14 @@ static size_t up256(size_t v) { return (v + 255) / 256 * 256; }
 // tokens and every smaller number.  With spans there are at most 2 T units (a last span that is not full has its empty ones),
 // and at most two per group of warps and one more per gate row.
 static size_t column_sums_bytes(int T, int C, int span) {
-  const RowPlan b = plan_rows(1, C, 1, PLAN_SMS);
+  const RowPlan b = plan_rows(BWD_THREADS, 1, C, 1, PLAN_SMS);
   const long long most = PLAN_SMS / b.cluster, slots = ((span > 1 ? 2ll : 1ll) * T + b.groups - 1) / b.groups;
   return up256((size_t)(slots < most ? slots : most) * 4 * C * sizeof(float));
 }
 size_t residual_workspace_bytes(int T, int C, int span) {
   size_t bytes = column_sums_bytes(T, C, span);
   if (span > 1) {
-    const RowPlan b = plan_rows(1, C, 1, PLAN_SMS);
+    const RowPlan b = plan_rows(BWD_THREADS, 1, C, 1, PLAN_SMS);
     const long long gates = (T + (long long)span - 1) / span, most = 2ll * (PLAN_SMS / b.cluster) * b.groups + gates;
     bytes += (size_t)(most < 2ll * T ? most : 2ll * T) * C * sizeof(float);
   }
@@ -1221,13 +1229,13 @@ static ResidualParams residual_params(const bimask_residual_args& a) {
 
 int launch_residual_fwd(const bimask_residual_args& a, cudaStream_t s) {
   ResidualParams p = residual_params(a);
-  const RowPlan b = plan_rows(a.T, a.C, 1, FWD_CTAS * sm_count());
+  const RowPlan b = plan_rows(FWD_THREADS, a.T, a.C, 1, sm_count());
   take_plan(p, b);
   using Yes = std::true_type;
   using No = std::false_type;
   auto run = [&](auto f32, auto gate, auto layer, auto cluster) -> int {
     constexpr bool F = decltype(f32)::value, G = decltype(gate)::value, L = decltype(layer)::value, K = decltype(cluster)::value;
-    return launch_rows(residual_fwd_kernel<F, G, L, K>, b, ring_bytes(fwd_slots(F, G)) + Exchange<4, K>::BYTES, s, p);
+    return launch_rows(residual_fwd_kernel<F, G, L, K>, b, ring_bytes(FWD_THREADS, fwd_slots(F, G)) + Exchange<4, FWD_THREADS, K>::BYTES, s, p);
   };
   const bool means = p.post == BIMASK_NORM_LAYER || p.pre == BIMASK_NORM_LAYER;
   auto pick = [&](auto f32, auto gate) -> int {
@@ -1244,7 +1252,7 @@ int launch_residual_fwd(const bimask_residual_args& a, cudaStream_t s) {
 int launch_residual_bwd(const bimask_residual_args& a, cudaStream_t s) {
   ResidualParams p = residual_params(a);
   const bool spanned = a.dgate != nullptr && p.gate_span > 1;
-  const RowPlan b = plan_rows(a.T, a.C, spanned ? (int)p.gate_span : 1, PLAN_SMS, true);
+  const RowPlan b = plan_rows(BWD_THREADS, a.T, a.C, spanned ? (int)p.gate_span : 1, PLAN_SMS, true);
   take_plan(p, b);
   const bool branch = a.dy || a.dgate || a.dscale || a.dw_post || a.db_post, post = branch && a.post != BIMASK_NORM_NONE;
   p.has = (a.pre != BIMASK_NORM_NONE ? HAS_PRE : 0) | (a.dxo ? HAS_DXO : 0) | (branch && a.y ? HAS_Y : 0) | (post ? HAS_POST : 0);
@@ -1270,7 +1278,7 @@ int launch_residual_bwd(const bimask_residual_args& a, cudaStream_t s) {
   auto run = [&](auto f32, auto gate, auto post, auto wide, auto cluster) -> int {
     constexpr bool F = decltype(f32)::value, P = decltype(post)::value, W = decltype(wide)::value, K = decltype(cluster)::value;
     constexpr int G = decltype(gate)::value;
-    constexpr int bytes = ring_bytes(bwd_slots(F, G != 0)) + (bwd_keeps_params(F, K) ? PARAM_BYTES : 0) + STATS_BYTES + Exchange<bwd_values(P, W) * ROWS, K>::BYTES;
+    constexpr int bytes = ring_bytes(BWD_THREADS, bwd_slots(F, G != 0)) + (bwd_keeps_params(F, K) ? PARAM_BYTES : 0) + STATS_BYTES + Exchange<bwd_values(P, W) * ROWS, BWD_THREADS, K>::BYTES;
     static_assert(bytes <= 227 * 1024, "shared memory of a CTA");
     return launch_rows(residual_bwd_kernel<F, G, P, W, K>, b, bytes, s, p);
   };
