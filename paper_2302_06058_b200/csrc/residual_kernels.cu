@@ -425,28 +425,6 @@ BIMASK_HD constexpr int bwd_values(bool post, bool wide) { return !post ? 2 : !w
 BIMASK_HD constexpr int stage_bytes(int threads, int slots) { return ROWS * VECS * slots * pitch_of(threads); }
 BIMASK_HD constexpr int ring_bytes(int threads, int slots) { return STAGES * stage_bytes(threads, slots); }
 
-template <bool F32, int PITCH>
-__device__ __forceinline__ void copy_block(uint32_t dst, const void* base, unsigned long long block, bool live) {
-  const uint4* src = reinterpret_cast<const uint4*>(base) + block * (F32 ? 2 : 1);
-  copy16(dst, src, live);
-  if (F32) copy16(dst + PITCH, src + 1, live);
-}
-template <bool F32, int PITCH>
-__device__ __forceinline__ void read_block(uint32_t at, Pair (&v)[4]) {
-  Vec8<F32> raw;
-#pragma unroll
-  for (int h = 0; h < (F32 ? 2 : 1); ++h)
-    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(raw.w[h].x), "=r"(raw.w[h].y), "=r"(raw.w[h].z), "=r"(raw.w[h].w)
-                 : "r"(at + h * PITCH) : "memory");
-  unpack8<F32>(raw, v);
-}
-template <int VALUES, int THREADS, bool CLUSTER>
-__device__ __forceinline__ void clear_exchange(float* exchange) {
-  for (int i = threadIdx.x; i < Exchange<VALUES, THREADS, CLUSTER>::BYTES / 4; i += blockDim.x) exchange[i] = 0.f;
-  if (CLUSTER) ptx::cluster_sync();                       // before a peer writes here, and before this CTA writes to a peer
-  else __syncthreads();
-}
-
 // A thread's blocks of a row: numbers (clamped ones for loads), and whether they exist.
 struct Blocks {
   uint32_t at[VECS], safe[VECS];
@@ -460,6 +438,55 @@ struct Blocks {
     }
   }
 };
+// 16 bytes at `at`, and for fp32 the next 16 at `second`
+template <bool F32>
+__device__ __forceinline__ void read_block(uint32_t at, uint32_t second, Pair (&v)[4]) {
+  Vec8<F32> raw;
+#pragma unroll
+  for (int h = 0; h < (F32 ? 2 : 1); ++h)
+    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(raw.w[h].x), "=r"(raw.w[h].y), "=r"(raw.w[h].z), "=r"(raw.w[h].w)
+                 : "r"(h == 0 ? at : second) : "memory");
+  unpack8<F32>(raw, v);
+}
+// Blocks of an fp32 stream are 32 bytes.  If every thread copied its own, an instruction would ask for half of each of 32 sectors and the
+// next one for the other halves, and L2 would deliver them twice (8192 x 4096 forward and backward 100 and 150 us).  So a warp copies its
+// blocks' 1024 bytes as two contiguous halves: lane l the half l % 2 of the blocks l / 2 and 16 + l / 2.  In shared memory a block lies
+// in one piece, its halves swapped in every other group of four blocks: eight lanes' reads, or writes, fall into different banks.
+struct StreamPlace {
+  uint32_t first, to, from;                               // first block to copy; offsets within a slot to copy to, to read from
+  __device__ __forceinline__ StreamPlace(int warp, int lane) {
+    const uint32_t b = (uint32_t)lane >> 1, h = (uint32_t)lane & 1u, base = (threadIdx.x >> 5) * 1024u;
+    first = 32u * (uint32_t)(VECS * warp) + b;
+    to = base + b * 32u + ((h ^ ((b >> 2) & 1u)) << 4);
+    from = base + (uint32_t)lane * 32u + ((((uint32_t)lane >> 2) & 1u) << 4);
+  }
+};
+// block j of the stream matrix of a row into a slot (`slot`: address of the slot's first byte, of thread 0)
+template <bool F32>
+__device__ __forceinline__ void copy_stream(uint32_t slot, const void* base, unsigned long long row, int j, bool live, const Blocks& b,
+                                            const StreamPlace& s, uint32_t C8) {
+  if (F32) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const uint32_t block = s.first + 32u * j + 16u * i;
+      copy16(slot + s.to + 512u * i, reinterpret_cast<const uint4*>(base) + (row + min(block, C8 - 1u)) * 2 + (threadIdx.x & 1u), live && block < C8);
+    }
+  } else {
+    copy16(slot + threadIdx.x * 16u, reinterpret_cast<const uint4*>(base) + row + b.safe[j], live && b.ok[j]);
+  }
+}
+template <bool F32>
+__device__ __forceinline__ void read_stream(uint32_t slot, const StreamPlace& s, Pair (&v)[4]) {
+  const uint32_t at = slot + (F32 ? s.from : threadIdx.x * 16u);
+  read_block<F32>(at, at ^ 16u, v);
+}
+template <int VALUES, int THREADS, bool CLUSTER>
+__device__ __forceinline__ void clear_exchange(float* exchange) {
+  for (int i = threadIdx.x; i < Exchange<VALUES, THREADS, CLUSTER>::BYTES / 4; i += blockDim.x) exchange[i] = 0.f;
+  if (CLUSTER) ptx::cluster_sync();                       // before a peer writes here, and before this CTA writes to a peer
+  else __syncthreads();
+}
+
 // every row's blocks times (plus) a vector of parameters, if there is one
 template <bool TIMES>
 __device__ __forceinline__ void affine(Pair (&v)[ROWS][VECS][4], const float* base, const Blocks& b) {
@@ -492,7 +519,7 @@ __device__ __forceinline__ uint32_t piece(uint32_t stage_at, int r, int j, int s
 template <bool F32, bool GATE, bool LAYER, bool CLUSTER>
 __global__ void __launch_bounds__(FWD_THREADS, 1)
 residual_fwd_kernel(const __grid_constant__ ResidualParams p) {
-  extern __shared__ float4 smem[];
+  extern __shared__ __align__(128) float4 smem[];
   constexpr int SLOTS = fwd_slots(F32, GATE), X = 0, Y = F32 ? 2 : 1, G = Y + 1;
   constexpr bool GATE_RING = gate_in_ring(F32, GATE);
   constexpr int PITCH = pitch_of(FWD_THREADS);
@@ -502,6 +529,7 @@ residual_fwd_kernel(const __grid_constant__ ResidualParams p) {
   clear_exchange<4, FWD_THREADS, CLUSTER>(exchange);
   Group<4, FWD_THREADS, CLUSTER> g(p, smem_addr(exchange));
   const Blocks b(g.warp, g.lane, p.C8);
+  const StreamPlace place(g.warp, g.lane);
   const uint32_t groups = blockDim.x / (32u * (uint32_t)p.warps);
   const uint32_t stride = CLUSTER ? gridDim.x / (uint32_t)p.cluster : gridDim.x * groups;
   const uint32_t ring = smem_addr(smem) + threadIdx.x * 16u;
@@ -513,7 +541,7 @@ residual_fwd_kernel(const __grid_constant__ ResidualParams p) {
   const unsigned long long number = drop_number(p.drop);
   auto gate_row = [&](uint32_t t) { return p.gate + (long long)(p.gate_span == 1u ? t : t / p.gate_span) * p.gate_pitch8; };
   auto fetch = [&](const Walk<false>& w, uint32_t stage) {
-    const uint32_t at = ring + stage * STAGE;
+    const uint32_t at = ring + stage * STAGE, slot0 = smem_addr(smem) + stage * STAGE;
 #pragma unroll
     for (int r = 0; r < ROWS; ++r) {
       const bool live = w.more(p) && w.t + r < w.end;
@@ -521,7 +549,7 @@ residual_fwd_kernel(const __grid_constant__ ResidualParams p) {
       const unsigned long long row = (unsigned long long)t * p.C8;
 #pragma unroll
       for (int j = 0; j < VECS; ++j) {
-        copy_block<F32, PITCH>(piece<SLOTS, PITCH>(at, r, j, X), p.x, row + b.safe[j], live && b.ok[j]);
+        copy_stream<F32>(slot0 + piece<SLOTS, PITCH>(0, r, j, X), p.x, row, j, live, b, place, p.C8);
         if (p.y != nullptr) copy16(piece<SLOTS, PITCH>(at, r, j, Y), p.y + row + b.safe[j], live && b.ok[j]);
         if (GATE_RING) copy16(piece<SLOTS, PITCH>(at, r, j, G), gate_row(t) + b.safe[j], live && b.ok[j]);
       }
@@ -531,10 +559,12 @@ residual_fwd_kernel(const __grid_constant__ ResidualParams p) {
   fetch(ahead, 0);
   uint32_t stage = 0;
   while (work.more(p)) {
+    if (F32) __syncwarp();                                // every lane has read the pieces that are overwritten now
     ahead.next(p, stride);
     fetch(ahead, stage ^ 1u);
     copies_wait<1>();
-    const uint32_t at = ring + stage * STAGE;
+    if (F32) __syncwarp();                                // the stream's pieces are other lanes' copies
+    const uint32_t at = ring + stage * STAGE, slot0 = smem_addr(smem) + stage * STAGE;
     bool live[ROWS];
     unsigned long long row[ROWS];
     Pair v[ROWS][VECS][4];
@@ -547,7 +577,7 @@ residual_fwd_kernel(const __grid_constant__ ResidualParams p) {
 #pragma unroll
       for (int r = 0; r < ROWS; ++r)
 #pragma unroll
-        for (int j = 0; j < VECS; ++j) read_block<false, PITCH>(piece<SLOTS, PITCH>(at, r, j, Y), v[r][j]);
+        for (int j = 0; j < VECS; ++j) read_block<false>(piece<SLOTS, PITCH>(at, r, j, Y), 0, v[r][j]);
       if (p.post != BIMASK_NORM_NONE) {
         float2 st[ROWS];
         row_stats<LAYER>(v, b.ok, p.post == BIMASK_NORM_LAYER, p.eps_post, p.inv_c, g, st);
@@ -577,7 +607,7 @@ residual_fwd_kernel(const __grid_constant__ ResidualParams p) {
 #pragma unroll
           for (int j = 0; j < VECS; ++j) {
             Pair w[4];
-            if (GATE_RING) read_block<false, PITCH>(piece<SLOTS, PITCH>(at, r, j, G), w);
+            if (GATE_RING) read_block<false>(piece<SLOTS, PITCH>(at, r, j, G), 0, w);
             else unpack8<false>(Vec8<false>{__ldg(gate_row(min(work.t + r, p.T - 1u)) + b.safe[j])}, w);
             times8(v[r][j], w);
           }
@@ -595,7 +625,7 @@ residual_fwd_kernel(const __grid_constant__ ResidualParams p) {
 #pragma unroll
       for (int j = 0; j < VECS; ++j) {
         Pair x[4];
-        read_block<F32, PITCH>(piece<SLOTS, PITCH>(at, r, j, X), x);
+        read_stream<F32>(slot0 + piece<SLOTS, PITCH>(0, r, j, X), place, x);
 #pragma unroll
         for (int k = 0; k < 4; ++k) v[r][j][k] = act::fma2(x[k], alpha, v[r][j][k]);
         if (p.xo != nullptr && live[r] && b.ok[j]) store8<F32>(p.xo, (long long)(row[r] + b.at[j]), v[r][j]);
@@ -651,7 +681,7 @@ enum { HAS_PRE = 1, HAS_DXO = 2, HAS_Y = 4, HAS_POST = 8 };
 template <bool F32, int GATE, bool POST, bool WIDE, bool CLUSTER>
 __global__ void __launch_bounds__(BWD_THREADS, 1)
 residual_bwd_kernel(const __grid_constant__ ResidualParams p) {
-  extern __shared__ float4 smem[];
+  extern __shared__ __align__(128) float4 smem[];
   constexpr int SLOTS = bwd_slots(F32, GATE != 0), XB = F32 ? 2 : 1, X = 0, DX = XB, DN = 2 * XB, Y = DN + 1, G = Y + 1;
   constexpr bool GATE_RING = gate_in_ring(F32, GATE != 0);
   constexpr int NV = bwd_values(POST, WIDE);              // a row's sums: g xh, g, z E, z xh, z, w m gate (E, xh, 1)
@@ -664,6 +694,7 @@ residual_bwd_kernel(const __grid_constant__ ResidualParams p) {
   clear_exchange<ROWS * NV, BWD_THREADS, CLUSTER>(exchange);
   Group<ROWS * NV, BWD_THREADS, CLUSTER> g(p, smem_addr(exchange));
   const Blocks b(g.warp, g.lane, p.C8);
+  const StreamPlace place(g.warp, g.lane);
   const uint32_t groups = blockDim.x / (32u * (uint32_t)p.warps);
   const uint32_t stride = CLUSTER ? gridDim.x / (uint32_t)p.cluster : gridDim.x * groups;
   const uint32_t ring = smem_addr(smem) + threadIdx.x * 16u;
@@ -678,7 +709,7 @@ residual_bwd_kernel(const __grid_constant__ ResidualParams p) {
   auto gate_row = [&](uint32_t t) { return p.gate + (long long)(p.gate_span == 1u ? t : t / p.gate_span) * p.gate_pitch8; };
   auto fetch = [&](const Walk<GATE == 2>& w, uint32_t stage) {
     const bool more = w.more(p);
-    const uint32_t at = ring + stage * STAGE;
+    const uint32_t at = ring + stage * STAGE, slot0 = smem_addr(smem) + stage * STAGE;
 #pragma unroll
     for (int r = 0; r < ROWS; ++r) {
       const bool live = more && w.t + r < w.end;
@@ -688,9 +719,9 @@ residual_bwd_kernel(const __grid_constant__ ResidualParams p) {
       for (int j = 0; j < VECS; ++j) {
         const bool there = live && b.ok[j];
         const unsigned long long block = row + b.safe[j];
-        copy_block<F32, PITCH>(piece<SLOTS, PITCH>(at, r, j, X), p.xo, block, there && (p.has & HAS_PRE));
+        copy_stream<F32>(slot0 + piece<SLOTS, PITCH>(0, r, j, X), p.xo, row, j, live && (p.has & HAS_PRE), b, place, p.C8);
         copy16(piece<SLOTS, PITCH>(at, r, j, DN), p.dn + block, there && (p.has & HAS_PRE));
-        copy_block<F32, PITCH>(piece<SLOTS, PITCH>(at, r, j, DX), p.dxo, block, there && (p.has & HAS_DXO));
+        copy_stream<F32>(slot0 + piece<SLOTS, PITCH>(0, r, j, DX), p.dxo, row, j, live && (p.has & HAS_DXO), b, place, p.C8);
         copy16(piece<SLOTS, PITCH>(at, r, j, Y), p.y + block, there && (p.has & HAS_Y));
         if (GATE_RING) copy16(piece<SLOTS, PITCH>(at, r, j, G), gate_row(t) + b.safe[j], there);
       }
@@ -729,7 +760,7 @@ residual_bwd_kernel(const __grid_constant__ ResidualParams p) {
   auto params = [&](int which, Pair (&w)[VECS][4]) {
     if (KEPT) {
 #pragma unroll
-      for (int j = 0; j < VECS; ++j) read_block<true, PITCH>(kept + (uint32_t)(which * VECS + j) * 2 * PITCH, w[j]);
+      for (int j = 0; j < VECS; ++j) read_block<true>(kept + (uint32_t)(which * VECS + j) * 2 * PITCH, kept + ((uint32_t)(which * VECS + j) * 2 + 1) * PITCH, w[j]);
     } else if (which == 0) {
       param_or_one(p.w_pre, b, w);
     } else {
@@ -753,12 +784,12 @@ residual_bwd_kernel(const __grid_constant__ ResidualParams p) {
   }
   uint32_t stage = 0;
   while (work.more(p)) {
-    __syncwarp();                                         // every lane has read the statistics that are overwritten now
+    __syncwarp();                                         // every lane has read the statistics and pieces that are overwritten now
     ahead.next(p, stride);
     fetch(ahead, stage ^ 1u);
     copies_wait<1>();
-    __syncwarp();                                         // the statistics are other lanes' copies
-    const uint32_t at = ring + stage * STAGE, st_at = stats + stage * STATS_STAGE;
+    __syncwarp();                                         // the statistics, and pieces of an fp32 stream, are other lanes' copies
+    const uint32_t at = ring + stage * STAGE, slot0 = smem_addr(smem) + stage * STAGE, st_at = stats + stage * STATS_STAGE;
     bool live[ROWS];
     unsigned long long row[ROWS];
     Pair E[ROWS][VECS][4], xh[ROWS][VECS][4], yh[ROWS][VECS][4], m[ROWS][VECS][4];
@@ -802,9 +833,9 @@ residual_bwd_kernel(const __grid_constant__ ResidualParams p) {
 #pragma unroll
       for (int j = 0; j < VECS; ++j) {
         Pair gr[4];
-        read_block<F32, PITCH>(piece<SLOTS, PITCH>(at, r, j, DX), E[r][j]);
-        read_block<F32, PITCH>(piece<SLOTS, PITCH>(at, r, j, X), xh[r][j]);
-        read_block<false, PITCH>(piece<SLOTS, PITCH>(at, r, j, DN), gr);
+        read_stream<F32>(slot0 + piece<SLOTS, PITCH>(0, r, j, DX), place, E[r][j]);
+        read_stream<F32>(slot0 + piece<SLOTS, PITCH>(0, r, j, X), place, xh[r][j]);
+        read_block<false>(piece<SLOTS, PITCH>(at, r, j, DN), 0, gr);
         normalise<WIDE>(xh[r][j], st);
 #pragma unroll
         for (int k = 0; k < 4; ++k) sum_g1[j][k] = act::fma2(gr[k], xh[r][j][k], sum_g1[j][k]);
@@ -824,7 +855,7 @@ residual_bwd_kernel(const __grid_constant__ ResidualParams p) {
       Pair ze = act::both(0.f), zx = ze, z0 = ze, te = ze, tx = ze, t0 = ze;
 #pragma unroll
       for (int j = 0; j < VECS; ++j) {
-        read_block<false, PITCH>(piece<SLOTS, PITCH>(at, r, j, Y), yh[r][j]);
+        read_block<false>(piece<SLOTS, PITCH>(at, r, j, Y), 0, yh[r][j]);
         if (POST) {
           normalise<WIDE>(yh[r][j], sq);
           Pair z[4];
@@ -832,7 +863,7 @@ residual_bwd_kernel(const __grid_constant__ ResidualParams p) {
           for (int k = 0; k < 4; ++k) z[k] = act::mul2(m[r][j][k], w[j][k]);
           if (GATE != 0) {
             Pair gt[4];
-            if (GATE_RING) read_block<false, PITCH>(piece<SLOTS, PITCH>(at, r, j, G), gt);
+            if (GATE_RING) read_block<false>(piece<SLOTS, PITCH>(at, r, j, G), 0, gt);
             else unpack8<false>(Vec8<false>{__ldg(gate_row(min(work.t + r, p.T - 1u)) + b.safe[j])}, gt);
             times8(z, gt);
           }
@@ -908,7 +939,7 @@ residual_bwd_kernel(const __grid_constant__ ResidualParams p) {
             }
           }
           Pair gt[4];
-          if (GATE_RING) read_block<false, PITCH>(piece<SLOTS, PITCH>(at, r, j, G), gt);
+          if (GATE_RING) read_block<false>(piece<SLOTS, PITCH>(at, r, j, G), 0, gt);
           else unpack8<false>(Vec8<false>{__ldg(gate_row(min(work.t + r, p.T - 1u)) + b.safe[j])}, gt);
           times8(E[r][j], gt);
         }
@@ -958,7 +989,7 @@ residual_bwd_kernel(const __grid_constant__ ResidualParams p) {
       for (int j = 0; j < VECS; ++j) {
         for (uint32_t o = 1; o < groups; ++o) {
           Pair q[4];
-          read_block<true, PITCH>(ring + o * (uint32_t)p.warps * 512u + 2 * j * PITCH, q);
+          read_block<true>(ring + o * (uint32_t)p.warps * 512u + 2 * j * PITCH, ring + o * (uint32_t)p.warps * 512u + (2 * j + 1) * PITCH, q);
           plus8(sum[j], q);
         }
         if (b.ok[j] && p.sums != nullptr) store8<true>(out, b.at[j], sum[j]);
