@@ -63,30 +63,44 @@ __device__ __forceinline__ void store8(void* base, long long block, const Pair (
   for (int h = 0; h < (F32 ? 2 : 1); ++h) dst[h] = v.w[h];
 }
 
+// A thread's item is 16 bytes: a block of bf16, half a block of fp32 (both halves draw the block's bits: with whole blocks a warp's
+// instruction would touch half of each sector).
 template <bool F32>
-__global__ void __launch_bounds__(DROP_THREADS, F32 ? 5 : 6)
-dropout_kernel(const void* x, long long blocks, void* y /* may be x */, const __grid_constant__ DropParams d) {
+__global__ void __launch_bounds__(DROP_THREADS, 6)
+dropout_kernel(const uint4* x, long long items, uint4* y /* may be x */, const __grid_constant__ DropParams d) {
   pdl_launch_dependents();
   pdl_wait();
   const unsigned long long number = drop_number(d);
   constexpr int U = 2;
   const long long step = (long long)gridDim.x * DROP_THREADS;
   long long i = (long long)blockIdx.x * DROP_THREADS + threadIdx.x;
-  Vec8<F32> v[U];
+  uint4 v[U];
   auto fetch = [&](int u, long long at) {
-    if (at < blocks) v[u] = load8<F32>(x, at);
+    if (at < items) v[u] = x[at];
   };
 #pragma unroll
   for (int u = 0; u < U; ++u) fetch(u, i + u * step);
-  while (i < blocks) {
+  while (i < items) {
 #pragma unroll
     for (int u = 0; u < U; ++u, i += step) {
-      if (i >= blocks) break;
-      Pair p[4];
-      unpack8<F32>(v[u], p);
+      if (i >= items) break;
+      uint4 w = v[u];
       fetch(u, i + U * step);
-      if (d.thr != 0u) drop8(p, (unsigned long long)i, number, d);
-      store8<F32>(y, i, p);
+      if (d.thr != 0u) {
+        if constexpr (F32) {
+          const uint4 bits = philox((unsigned long long)(i >> 1), number, d);
+          float f[4];
+          act::split(drop_pair(act::pair(__uint_as_float(w.x), __uint_as_float(w.y)), i & 1 ? bits.z : bits.x, d.thr, d.scale), f[0], f[1]);
+          act::split(drop_pair(act::pair(__uint_as_float(w.z), __uint_as_float(w.w)), i & 1 ? bits.w : bits.y, d.thr, d.scale), f[2], f[3]);
+          w = make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
+        } else {
+          Pair p[4];
+          unpack8<false>(Vec8<false>{w}, p);
+          drop8(p, (unsigned long long)i, number, d);
+          w = pack8<false>(p).w[0];
+        }
+      }
+      y[i] = w;
     }
   }
 }
@@ -418,8 +432,8 @@ BIMASK_HD constexpr bool gate_in_ring(bool f32, bool gate) { return gate && !f32
 BIMASK_HD constexpr int fwd_slots(bool f32, bool gate) { return (f32 ? 2 : 1) + 1 + (gate_in_ring(f32, gate) ? 1 : 0); }
 BIMASK_HD constexpr int bwd_slots(bool f32, bool gate) { return (f32 ? 4 : 2) + 2 + (gate_in_ring(f32, gate) ? 1 : 0); }
 // The backward pass keeps two parameters of the threads' columns beside the ring (from memory they cost it a fifth of the time with
-// an fp32 stream, whose ring leaves no first-level cache); only there a cluster's larger exchange buffers leave no room.
-BIMASK_HD constexpr bool bwd_keeps_params(bool f32, bool cluster) { return !(f32 && cluster); }
+// an fp32 stream, whose ring leaves no first-level cache); only there a cluster's largest exchange buffers leave no room.
+BIMASK_HD constexpr bool bwd_keeps_params(bool f32, bool cluster, int values) { return !(f32 && cluster && values == 8); }
 constexpr int PARAM_BYTES = 2 * VECS * 2 * pitch_of(BWD_THREADS);
 BIMASK_HD constexpr int bwd_values(bool post, bool wide) { return !post ? 2 : !wide ? 4 : 8; }
 BIMASK_HD constexpr int stage_bytes(int threads, int slots) { return ROWS * VECS * slots * pitch_of(threads); }
@@ -450,7 +464,7 @@ __device__ __forceinline__ void read_block(uint32_t at, uint32_t second, Pair (&
 }
 // Blocks of an fp32 stream are 32 bytes.  If every thread copied its own, an instruction would ask for half of each of 32 sectors and the
 // next one for the other halves, and L2 would deliver them twice (8192 x 4096 forward and backward 100 and 150 us).  So a warp copies its
-// blocks' 1024 bytes as two contiguous halves: lane l the half l % 2 of the blocks l / 2 and 16 + l / 2.  In shared memory a block lies
+// blocks' 1024 bytes as two contiguous halves (stores need no such thing: exchanged to whole sectors they cost 10 us more): lane l the half l % 2 of the blocks l / 2 and 16 + l / 2.  In shared memory a block lies
 // in one piece, its halves swapped in every other group of four blocks: eight lanes' reads, or writes, fall into different banks.
 struct StreamPlace {
   uint32_t first, to, from;                               // first block to copy; offsets within a slot to copy to, to read from
@@ -687,7 +701,7 @@ residual_bwd_kernel(const __grid_constant__ ResidualParams p) {
   constexpr int NV = bwd_values(POST, WIDE);              // a row's sums: g xh, g, z E, z xh, z, w m gate (E, xh, 1)
   constexpr int PITCH = pitch_of(BWD_THREADS);
   constexpr uint32_t STAGE = stage_bytes(BWD_THREADS, SLOTS);
-  constexpr bool KEPT = bwd_keeps_params(F32, CLUSTER);
+  constexpr bool KEPT = bwd_keeps_params(F32, CLUSTER, NV);
   uint8_t* const after = reinterpret_cast<uint8_t*>(smem) + ring_bytes(BWD_THREADS, SLOTS) + (KEPT ? PARAM_BYTES : 0);
   float* const exchange = reinterpret_cast<float*>(after + STATS_BYTES);
   pdl_launch_dependents();
@@ -913,7 +927,7 @@ residual_bwd_kernel(const __grid_constant__ ResidualParams p) {
         Pair o[4];
 #pragma unroll
         for (int k = 0; k < 4; ++k) o[k] = act::mul2(E[r][j][k], alpha);
-        if (there && p.dx != nullptr) store8<F32>(p.dx, (long long)(row[r] + b.at[j]), o);
+        if (p.dx != nullptr && there) store8<F32>(p.dx, (long long)(row[r] + b.at[j]), o);
         times8(E[r][j], m[r][j]);
         if (GATE != 0) {
           if (GATE == 2 || p.dgate != nullptr) {          // scale u
@@ -1214,10 +1228,11 @@ DropParams drop_params(const bimask_dropout_args* d) {
 }
 
 int launch_dropout(const void* x, int type, int T, int C, const bimask_dropout_args& d, void* y, cudaStream_t s) {
-  const long long blocks = (long long)T * (C / 8);
-  const long long ctas = (blocks + DROP_THREADS - 1) / DROP_THREADS, most = (type == BIMASK_TYPE_F32 ? 5ll : 6ll) * sm_count();
+  const long long items = (long long)T * (C / (type == BIMASK_TYPE_F32 ? 4 : 8));
+  const long long ctas = (items + DROP_THREADS - 1) / DROP_THREADS, most = 6ll * sm_count();
   auto run = [&](auto kern) {
-    return launch_pdl(kern, (unsigned)(ctas < most ? ctas : most), DROP_THREADS, 0, s, x, blocks, y, drop_params(&d));
+    return launch_pdl(kern, (unsigned)(ctas < most ? ctas : most), DROP_THREADS, 0, s, reinterpret_cast<const uint4*>(x), items,
+                      reinterpret_cast<uint4*>(y), drop_params(&d));
   };
   BIMASK_CUDA_OK(type == BIMASK_TYPE_F32 ? run(dropout_kernel<true>) : run(dropout_kernel<false>));
   count_launch();
@@ -1309,7 +1324,7 @@ int launch_residual_bwd(const bimask_residual_args& a, cudaStream_t s) {
   auto run = [&](auto f32, auto gate, auto post, auto wide, auto cluster) -> int {
     constexpr bool F = decltype(f32)::value, P = decltype(post)::value, W = decltype(wide)::value, K = decltype(cluster)::value;
     constexpr int G = decltype(gate)::value;
-    constexpr int bytes = ring_bytes(BWD_THREADS, bwd_slots(F, G != 0)) + (bwd_keeps_params(F, K) ? PARAM_BYTES : 0) + STATS_BYTES + Exchange<bwd_values(P, W) * ROWS, BWD_THREADS, K>::BYTES;
+    constexpr int bytes = ring_bytes(BWD_THREADS, bwd_slots(F, G != 0)) + (bwd_keeps_params(F, K, bwd_values(P, W)) ? PARAM_BYTES : 0) + STATS_BYTES + Exchange<bwd_values(P, W) * ROWS, BWD_THREADS, K>::BYTES;
     static_assert(bytes <= 227 * 1024, "shared memory of a CTA");
     return launch_rows(residual_bwd_kernel<F, G, P, W, K>, b, bytes, s, p);
   };
