@@ -9,7 +9,7 @@ namespace bimask {
 // keyed bijection of 128-bit counters.  Eight consecutive elements of a T x C matrix are one block (C % 8 == 0: a block stays in
 // its row); the block's number and the call's stream number are the counter, the seed is the key, and element k of the block
 // takes 16 of the 128 bits.  Ten rounds are 20 wide multiplications and as many three-way exclusive ors, whose key words come from
-// the kernel's arguments: 5 operations per element, and 3 to compare and to choose.
+// the kernel's arguments: 5 operations per element, and 2.5 to compare and to choose (55 to 65 instructions per block, measured).
 struct DropParams {
   uint32_t thr;                      // kept iff the 16 bits are at least thr / 65536 (thr has them at its upper end); 0: no dropout
   float scale;                       // 65536 / (65536 - the threshold)

@@ -1,6 +1,7 @@
 // The residual junction between two blocks of a network (norm after a block, dropout, gate, residual scale, norm before the
 // next block), its gradient, and dropout alone.  All of them stream: every matrix is read once and written once, a row stays
-// in the registers of the warps that share it, and the statistics are exchanged by shuffles and one barrier per norm.
+// in the registers of the warps that share it, and its sums are exchanged by shuffles and one barrier per norm (forward) or row
+// (backward).
 #include "dropout.cuh"
 #include "sm100_ptx.cuh"
 #include <type_traits>
@@ -12,7 +13,9 @@ namespace {
 using act::Pair;
 
 // ------------------------------------------------------------------------------------------
-// Dropout alone: a flat stream of blocks of eight elements.
+// Dropout alone: a flat stream of blocks of eight elements, the next items of a thread on their way.  Bound by HBM: 8192 x 16384 of
+// bf16 in 93 us on the device (5.8 TB/s), the generator's wide multiplications two thirds of what their pipe can do meanwhile; 8192 x
+// 8192 of fp32 in 99 us (5.4 TB/s).  More items on their way (four) and more CTAs than fit at once were no faster.
 // ------------------------------------------------------------------------------------------
 constexpr int DROP_THREADS = 256;
 
@@ -45,14 +48,6 @@ __device__ __forceinline__ Vec8<F32> pack8(const Pair (&p)[4]) {
   } else {
     v.w[0] = make_uint4(pack_bf16_p(p[0]), pack_bf16_p(p[1]), pack_bf16_p(p[2]), pack_bf16_p(p[3]));
   }
-  return v;
-}
-template <bool F32>
-__device__ __forceinline__ Vec8<F32> load8(const void* base, long long block) {
-  Vec8<F32> v;
-  const uint4* src = reinterpret_cast<const uint4*>(base) + block * (F32 ? 2 : 1);
-#pragma unroll
-  for (int h = 0; h < (F32 ? 2 : 1); ++h) v.w[h] = src[h];
   return v;
 }
 template <bool F32>
@@ -115,6 +110,10 @@ dropout_kernel(const uint4* x, long long items, uint4* y /* may be x */, const _
 // What bounds these kernels next to HBM is the instructions they issue, so the rows' code has no branches but those of absent
 // parts: columns and rows past the end are copied as zeros (from a clamped address, of which cp.async reads nothing) and work like
 // the others, but for their stores.
+// Why two blocks and two rows per thread: what a step costs beside its blocks is shared by four (two RMS norms and dropout, forward: 304
+// instructions per block with one block and two rows per step, 245 with two and two).  8192 x 4096 with two RMS norms and dropout, on the device: forward 56 us (floor 41; without
+// dropout 45), backward 76 (floor 61).  A third stage of the ring, three CTAs per SM and parameters in shared memory (forward)
+// changed nothing or cost time; one row per step with twice the warps does not fit the registers of the backward pass.
 // ------------------------------------------------------------------------------------------
 constexpr int ROWS = 2, VECS = 2, STAGES = 2;
 // Threads of a CTA (one per SM).  The backward pass keeps five to eight arrays of a step in registers and wants 255 of them.
@@ -463,9 +462,10 @@ __device__ __forceinline__ void read_block(uint32_t at, uint32_t second, Pair (&
   unpack8<F32>(raw, v);
 }
 // Blocks of an fp32 stream are 32 bytes.  If every thread copied its own, an instruction would ask for half of each of 32 sectors and the
-// next one for the other halves, and L2 would deliver them twice (8192 x 4096 forward and backward 100 and 150 us).  So a warp copies its
-// blocks' 1024 bytes as two contiguous halves (stores need no such thing: exchanged to whole sectors they cost 10 us more): lane l the half l % 2 of the blocks l / 2 and 16 + l / 2.  In shared memory a block lies
-// in one piece, its halves swapped in every other group of four blocks: eight lanes' reads, or writes, fall into different banks.
+// next one for the other halves, and L2 would deliver them twice (8192 x 4096 forward and backward 100 and 150 us, so 80 and 104).  So a
+// warp copies its blocks' 1024 bytes as two contiguous halves, lane l the half l % 2 of the blocks l / 2 and 16 + l / 2.  In shared
+// memory a block lies in one piece, its halves swapped in every other group of four blocks: eight lanes' reads, or writes, fall into
+// different banks.  Stores need no such thing: exchanged to whole sectors they cost the forward pass 10 us.
 struct StreamPlace {
   uint32_t first, to, from;                               // first block to copy; offsets within a slot to copy to, to read from
   __device__ __forceinline__ StreamPlace(int warp, int lane) {
@@ -684,6 +684,9 @@ residual_fwd_kernel(const __grid_constant__ ResidualParams p) {
 // Four column sums carry every parameter's gradient: G1 = sum dn xh (w_pre), G2 = sum dn (b_pre), A = sum e yh, B = sum e:
 //   dw_post = scale A,  db_post = scale B,  dscale = w_post A + b_post B.
 // A thread keeps its columns' sums in registers; each cluster (CTA) leaves one row of partial sums.
+// Eight warps per SM with all their registers: what bounds the pass beside HBM is the chain of a step (issue slots 45 % used at
+// 8192 x 4096, RMS norms, dropout).  In steps of the build: two exchanges per row 131 us, one 101, absent parts as zeros and the step's
+// random bits drawn together 91, parameters beside the ring 79, rows sent for before those 76.
 // Columns and rows past the end: dx', dn, y (and m of columns) are zeros, and so is every sum.  What is absent (no norm before, dx' or y)
 // is copied as zeros, too, statistics among them: then all that depends on it is zero as it should be.
 // GATE: 0 no gate, 1 a gate whose gradient, if wanted, is a row per token, 2 one whose gradient is summed over spans.  WIDE: some norm
@@ -1157,7 +1160,7 @@ RowPlan plan_rows(int threads, int T, int C, int span, int ctas, bool one_slot =
     b.gates = (T + (long long)span - 1) / span;
     b.unit_rows = (int)((T + room - 1) / room);
     if (b.unit_rows > 1 && b.unit_rows % ROWS != 0) b.unit_rows += ROWS - b.unit_rows % ROWS;
-    // whole spans where they keep half of the groups busy, or are two steps: nothing is left to add up then
+    // whole spans where they keep half of the groups busy, or are two steps: nothing is left to add up then (a launch of 2 us)
     if (b.unit_rows > len || 2 * b.gates >= room || len <= 2 * ROWS) b.unit_rows = len;
     b.units_per_span = (len + b.unit_rows - 1) / b.unit_rows;
     b.units = b.gates * b.units_per_span;
@@ -1324,7 +1327,8 @@ int launch_residual_bwd(const bimask_residual_args& a, cudaStream_t s) {
   auto run = [&](auto f32, auto gate, auto post, auto wide, auto cluster) -> int {
     constexpr bool F = decltype(f32)::value, P = decltype(post)::value, W = decltype(wide)::value, K = decltype(cluster)::value;
     constexpr int G = decltype(gate)::value;
-    constexpr int bytes = ring_bytes(BWD_THREADS, bwd_slots(F, G != 0)) + (bwd_keeps_params(F, K, bwd_values(P, W)) ? PARAM_BYTES : 0) + STATS_BYTES + Exchange<bwd_values(P, W) * ROWS, BWD_THREADS, K>::BYTES;
+    constexpr int values = bwd_values(P, W), kept = bwd_keeps_params(F, K, values) ? PARAM_BYTES : 0;
+    constexpr int bytes = ring_bytes(BWD_THREADS, bwd_slots(F, G != 0)) + kept + STATS_BYTES + Exchange<values * ROWS, BWD_THREADS, K>::BYTES;
     static_assert(bytes <= 227 * 1024, "shared memory of a CTA");
     return launch_rows(residual_bwd_kernel<F, G, P, W, K>, b, bytes, s, p);
   };
