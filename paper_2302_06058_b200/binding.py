@@ -76,6 +76,7 @@ class ResidualArgs(Structure):
                 *((name, c_void_p) for name in _RESIDUAL_POINTERS), ("ws_bytes", c_size_t)]
 
 
+_RESIDUAL_INDEX = {name: i for i, name in enumerate(_RESIDUAL_POINTERS)}
 # the same fields for struct.pack, in one call (setting 30 fields one by one takes longer than a short kernel)
 _RESIDUAL_PACK = struct.Struct("@6iq3f4xfQQP23PN").pack
 assert struct.calcsize("@6iq3f4xfQQP23PN") == ctypes.sizeof(ResidualArgs) and len(_RESIDUAL_POINTERS) == 23
@@ -341,9 +342,11 @@ def make_residual_args(T, C, bufs: dict, stream_type=TYPE_BF16, post=NORM_NONE, 
                        gate_span=1, drop: Dropout | None = None) -> ResidualArgs:
     """Fill a bimask_residual_args from a dict of tensors keyed by field name (missing keys -> NULL).  The rows of gate and dgate
     may be slices of a wider matrix, both of the same pitch (bufs["gate_pitch"] gives it where they are addresses)."""
-    get = bufs.get
-    pointers = [0 if t is None else t.data_ptr() if type(t) is _Tensor and t.is_contiguous() else _row_ptr(name, t)
-                for name, t in zip(_RESIDUAL_POINTERS, map(get, _RESIDUAL_POINTERS))]
+    get, index, pointers = bufs.get, _RESIDUAL_INDEX.get, [0] * len(_RESIDUAL_POINTERS)
+    for name, t in bufs.items():
+        i = index(name)
+        if i is not None and t is not None:
+            pointers[i] = t.data_ptr() if type(t) is _Tensor and t.is_contiguous() else _row_ptr(name, t)
     pitch = 0
     for t in (get("gate"), get("dgate")):
         if t is not None:

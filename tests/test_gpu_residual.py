@@ -207,8 +207,9 @@ class Problem:
         return out
 
 
-# one token, a few, several rows per group; one warp, parts of one, several, the widest rows of one, two and four CTAs
-SIZES = [(1, 32), (3, 64), (2, 256), (37, 288), (5, 512), (70, 544), (301, 384), (33, 1152), (6, 2080), (4, 4096), (3, 4128), (5, 8192), (3, 8224), (9, 16384)]
+# one token, a few, several rows per group; one warp, parts of one, several, the widest rows of one, two and four CTAs; as many rows
+# as one CTA's launch takes in the backward pass, and one more
+SIZES = [(1, 32), (3, 64), (2, 256), (32, 256), (33, 256), (37, 288), (5, 512), (70, 544), (301, 384), (33, 1152), (6, 2080), (4, 4096), (3, 4128), (5, 8192), (3, 8224), (9, 16384)]
 FORMS = [(0, 1), (0, 2), (1, 1), (2, 2), (1, 2), (2, 1), (1, 0), (2, 0), (0, 0)]
 
 
@@ -226,7 +227,7 @@ def test_against_64_bits(T, C, stream):
         assert all(torch.equal(f[k], f2[k]) for k in f) and all(torch.equal(g[k], g2[k]) for k in g if k != "ws")
 
 
-@pytest.mark.parametrize("T,C,span", [(2500, 256, 7), (2500, 64, 1300), (700, 1152, 197), (4000, 320, 3999), (300, 4160, 2), (149, 4096, 150), (600, 8192, 64), (200, 9216, 200)])
+@pytest.mark.parametrize("T,C,span", [(2500, 256, 7), (2500, 64, 1300), (700, 1152, 197), (4000, 320, 3999), (300, 4160, 2), (149, 4096, 150), (9000, 64, 7), (600, 8192, 64), (200, 9216, 200)])
 def test_many_rows_and_gates_that_serve_spans(T, C, span):
     """More rows than groups of warps: units of several rows, spans that end inside and a last span that is not full."""
     for post, pre in ((0, 2), (1, 1), (2, 0)):
@@ -404,6 +405,23 @@ def test_captured_passes_that_share_a_workspace():
             q.m = RO.multiplier(q.T, q.C, q.p, SEED, NUMBER + step)
             q.check_forward(f)
             q.check_backward(g, f)
+
+
+def test_steps_of_a_counter_reach_the_gradient():
+    """Forward and backward passes of one step share a mask, those of two steps do not."""
+    q = Problem(50, 96, 1, 2, p=0.4)
+    counter = torch.zeros(1, dtype=torch.int64, device="cuda")
+    q.drop = bm.make_dropout(q.p, SEED, NUMBER - 3, counter)
+    seen = []
+    for step in (3, 4):
+        counter.fill_(step)
+        q.m = RO.multiplier(q.T, q.C, q.p, SEED, NUMBER - 3 + step)
+        f = q.forward()
+        q.check_forward(f)
+        g = q.backward(f)
+        q.check_backward(g, f)
+        seen.append(g["dy"])
+    assert not torch.equal(*seen)
 
 
 def test_another_stream():
