@@ -576,8 +576,6 @@ residual_fwd_kernel(const __grid_constant__ ResidualParams p) {
     if (F32) __syncwarp();                                // every lane has read the pieces that are overwritten now
     ahead.next(p, stride);
     fetch(ahead, stage ^ 1u);
-    copies_wait<1>();
-    if (F32) __syncwarp();                                // the stream's pieces are other lanes' copies
     const uint32_t at = ring + stage * STAGE, slot0 = smem_addr(smem) + stage * STAGE;
     bool live[ROWS];
     unsigned long long row[ROWS];
@@ -587,6 +585,15 @@ residual_fwd_kernel(const __grid_constant__ ResidualParams p) {
       live[r] = work.t + r < work.end;
       row[r] = (unsigned long long)(work.t + r) * p.C8;
     }
+    uint4 bits[ROWS][VECS];
+    if (p.drop.thr != 0u) {                               // all blocks of the step together, so that their chains interleave, and before its
+#pragma unroll                                            // rows are waited for
+      for (int r = 0; r < ROWS; ++r)
+#pragma unroll
+        for (int j = 0; j < VECS; ++j) bits[r][j] = philox(row[r] + b.at[j], number, p.drop);
+    }
+    copies_wait<1>();
+    if (F32) __syncwarp();                                // the stream's pieces are other lanes' copies
     if (p.y != nullptr) {
 #pragma unroll
       for (int r = 0; r < ROWS; ++r)
@@ -604,12 +611,7 @@ residual_fwd_kernel(const __grid_constant__ ResidualParams p) {
         affine<true>(v, p.w_post, b);
         affine<false>(v, p.b_post, b);
       }
-      if (p.drop.thr != 0u) {                             // all blocks of the step together: their chains interleave
-        uint4 bits[ROWS][VECS];
-#pragma unroll
-        for (int r = 0; r < ROWS; ++r)
-#pragma unroll
-          for (int j = 0; j < VECS; ++j) bits[r][j] = philox(row[r] + b.at[j], number, p.drop);
+      if (p.drop.thr != 0u) {
 #pragma unroll
         for (int r = 0; r < ROWS; ++r)
 #pragma unroll
