@@ -4,6 +4,7 @@
 // (backward).
 #include "dropout.cuh"
 #include "sm100_ptx.cuh"
+#include <algorithm>
 #include <type_traits>
 
 namespace bimask {
@@ -116,8 +117,10 @@ dropout_kernel(const uint4* x, long long items, uint4* y /* may be x */, const _
 // changed nothing or cost time; one row per step with twice the warps does not fit the registers of the backward pass.
 // ------------------------------------------------------------------------------------------
 constexpr int ROWS = 2, VECS = 2, STAGES = 2;
-// Threads of a CTA (one per SM).  The backward pass keeps five to eight arrays of a step in registers and wants 255 of them.
-constexpr int FWD_THREADS = 512, BWD_THREADS = 256;
+// Threads of a CTA (one per SM).  The backward pass keeps five to eight arrays of a step in registers: 255 of them with two rows per step,
+// 168 with one (see bwd_rows).
+constexpr int FWD_THREADS = 512;
+BIMASK_HD constexpr int bwd_threads(int rows) { return rows == 2 ? 256 : 384; }
 constexpr int MAX_ROW_WARPS = 32;                         // of a cluster of two or four CTAs
 static_assert(RESIDUAL_MAX_C == 8 * 32 * VECS * MAX_ROW_WARPS, "eight columns of each of a thread's blocks");
 
@@ -298,7 +301,7 @@ __device__ __forceinline__ void row_totals(Group<N, THREADS, CLUSTER>& g, float 
     g.meet();
     v = 0.f;
 #pragma unroll
-    for (int k = 0; k < (CLUSTER ? MAX_ROW_WARPS : THREADS / 32) / 4; k += LANES) {
+    for (int k = 0; k < ((CLUSTER ? MAX_ROW_WARPS : THREADS / 32) + 3) / 4; k += LANES) {
       const int w = 4 * (part + k);
       if (w < g.width) {
         float4 x;
@@ -392,7 +395,7 @@ __device__ __forceinline__ void row_stats(const Pair (&v)[ROWS][VECS][4], const 
 
 // A group's walk over its units, ROWS rows at a time.  SPAN: units of many rows that end with their gate row's span; else of one
 // row (all others of the step are none) or ROWS.
-template <bool SPAN>
+template <int ROWS, bool SPAN>
 struct Walk {
   uint32_t unit, t, end;
   __device__ __forceinline__ void enter(const ResidualParams& p) {
@@ -424,8 +427,8 @@ struct Walk {
 
 // Shared memory of a CTA: the ring of the threads' pieces, the statistics of every warp's rows, the exchange buffers.
 BIMASK_HD constexpr int pitch_of(int threads) { return threads * 16; }      // from a thread's piece to its next
-constexpr int STATS_STAGE = 2 * ROWS * 8;                 // bytes of a warp's statistics: before, after
-constexpr int STATS_BYTES = STAGES * (BWD_THREADS / 32) * STATS_STAGE;
+BIMASK_HD constexpr int stats_stage(int rows) { return 2 * rows * 8; }                 // bytes of a warp's statistics: before, after
+BIMASK_HD constexpr int stats_bytes(int rows) { return STAGES * (bwd_threads(rows) / 32) * stats_stage(rows); }
 // With an fp32 stream the ring has no room for a gate's pieces: it is read from memory (L2) where it is used.
 BIMASK_HD constexpr bool gate_in_ring(bool f32, bool gate) { return gate && !f32; }
 BIMASK_HD constexpr int fwd_slots(bool f32, bool gate) { return (f32 ? 2 : 1) + 1 + (gate_in_ring(f32, gate) ? 1 : 0); }
@@ -433,10 +436,10 @@ BIMASK_HD constexpr int bwd_slots(bool f32, bool gate) { return (f32 ? 4 : 2) + 
 // The backward pass keeps two parameters of the threads' columns beside the ring (from memory they cost it a fifth of the time with
 // an fp32 stream, whose ring leaves no first-level cache); only there a cluster's largest exchange buffers leave no room.
 BIMASK_HD constexpr bool bwd_keeps_params(bool f32, bool cluster, int values) { return !(f32 && cluster && values == 8); }
-constexpr int PARAM_BYTES = 2 * VECS * 2 * pitch_of(BWD_THREADS);
+BIMASK_HD constexpr int param_bytes(int threads) { return 2 * VECS * 2 * pitch_of(threads); }
 BIMASK_HD constexpr int bwd_values(bool post, bool wide) { return !post ? 2 : !wide ? 4 : 8; }
-BIMASK_HD constexpr int stage_bytes(int threads, int slots) { return ROWS * VECS * slots * pitch_of(threads); }
-BIMASK_HD constexpr int ring_bytes(int threads, int slots) { return STAGES * stage_bytes(threads, slots); }
+BIMASK_HD constexpr int stage_bytes(int rows, int threads, int slots) { return rows * VECS * slots * pitch_of(threads); }
+BIMASK_HD constexpr int ring_bytes(int rows, int threads, int slots) { return STAGES * stage_bytes(rows, threads, slots); }
 
 // A thread's blocks of a row: numbers (clamped ones for loads), and whether they exist.
 struct Blocks {
@@ -537,8 +540,8 @@ residual_fwd_kernel(const __grid_constant__ ResidualParams p) {
   constexpr int SLOTS = fwd_slots(F32, GATE), X = 0, Y = F32 ? 2 : 1, G = Y + 1;
   constexpr bool GATE_RING = gate_in_ring(F32, GATE);
   constexpr int PITCH = pitch_of(FWD_THREADS);
-  constexpr uint32_t STAGE = stage_bytes(FWD_THREADS, SLOTS);
-  float* exchange = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(smem) + ring_bytes(FWD_THREADS, SLOTS));
+  constexpr uint32_t STAGE = stage_bytes(ROWS, FWD_THREADS, SLOTS);
+  float* exchange = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(smem) + ring_bytes(ROWS, FWD_THREADS, SLOTS));
   pdl_launch_dependents();
   clear_exchange<4, FWD_THREADS, CLUSTER>(exchange);
   Group<4, FWD_THREADS, CLUSTER> g(p, smem_addr(exchange));
@@ -547,14 +550,14 @@ residual_fwd_kernel(const __grid_constant__ ResidualParams p) {
   const uint32_t groups = blockDim.x / (32u * (uint32_t)p.warps);
   const uint32_t stride = CLUSTER ? gridDim.x / (uint32_t)p.cluster : gridDim.x * groups;
   const uint32_t ring = smem_addr(smem) + threadIdx.x * 16u;
-  Walk<false> work, ahead;
+  Walk<ROWS, false> work, ahead;
   work.unit = CLUSTER ? blockIdx.x / (uint32_t)p.cluster : blockIdx.x * groups + (uint32_t)g.group;
   work.enter(p);
   ahead = work;
   pdl_wait();
   const unsigned long long number = drop_number(p.drop);
   auto gate_row = [&](uint32_t t) { return p.gate + (long long)(p.gate_span == 1u ? t : t / p.gate_span) * p.gate_pitch8; };
-  auto fetch = [&](const Walk<false>& w, uint32_t stage) {
+  auto fetch = [&](const Walk<ROWS, false>& w, uint32_t stage) {
     const uint32_t at = ring + stage * STAGE, slot0 = smem_addr(smem) + stage * STAGE;
 #pragma unroll
     for (int r = 0; r < ROWS; ++r) {
@@ -697,28 +700,29 @@ residual_fwd_kernel(const __grid_constant__ ResidualParams p) {
 enum { SUM_A = 1, SUM_B = 2, SUM_G1 = 4, SUM_G2 = 8 };
 enum { HAS_PRE = 1, HAS_DXO = 2, HAS_Y = 4, HAS_POST = 8 };
 
-template <bool F32, int GATE, bool POST, bool WIDE, bool CLUSTER>
-__global__ void __launch_bounds__(BWD_THREADS, 1)
+template <int ROWS, bool F32, int GATE, bool POST, bool WIDE, bool CLUSTER>
+__global__ void __launch_bounds__(bwd_threads(ROWS), 1)
 residual_bwd_kernel(const __grid_constant__ ResidualParams p) {
   extern __shared__ __align__(128) float4 smem[];
+  constexpr int THREADS = bwd_threads(ROWS), STATS_STAGE = stats_stage(ROWS);
   constexpr int SLOTS = bwd_slots(F32, GATE != 0), XB = F32 ? 2 : 1, X = 0, DX = XB, DN = 2 * XB, Y = DN + 1, G = Y + 1;
   constexpr bool GATE_RING = gate_in_ring(F32, GATE != 0);
   constexpr int NV = bwd_values(POST, WIDE);              // a row's sums: g xh, g, z E, z xh, z, w m gate (E, xh, 1)
-  constexpr int PITCH = pitch_of(BWD_THREADS);
-  constexpr uint32_t STAGE = stage_bytes(BWD_THREADS, SLOTS);
+  constexpr int PITCH = pitch_of(THREADS);
+  constexpr uint32_t STAGE = stage_bytes(ROWS, THREADS, SLOTS);
   constexpr bool KEPT = bwd_keeps_params(F32, CLUSTER, NV);
-  uint8_t* const after = reinterpret_cast<uint8_t*>(smem) + ring_bytes(BWD_THREADS, SLOTS) + (KEPT ? PARAM_BYTES : 0);
-  float* const exchange = reinterpret_cast<float*>(after + STATS_BYTES);
+  uint8_t* const after = reinterpret_cast<uint8_t*>(smem) + ring_bytes(ROWS, THREADS, SLOTS) + (KEPT ? param_bytes(THREADS) : 0);
+  float* const exchange = reinterpret_cast<float*>(after + stats_bytes(ROWS));
   pdl_launch_dependents();
-  clear_exchange<ROWS * NV, BWD_THREADS, CLUSTER>(exchange);
-  Group<ROWS * NV, BWD_THREADS, CLUSTER> g(p, smem_addr(exchange));
+  clear_exchange<ROWS * NV, THREADS, CLUSTER>(exchange);
+  Group<ROWS * NV, THREADS, CLUSTER> g(p, smem_addr(exchange));
   const Blocks b(g.warp, g.lane, p.C8);
   const StreamPlace place(g.warp, g.lane);
   const uint32_t groups = blockDim.x / (32u * (uint32_t)p.warps);
   const uint32_t stride = CLUSTER ? gridDim.x / (uint32_t)p.cluster : gridDim.x * groups;
   const uint32_t ring = smem_addr(smem) + threadIdx.x * 16u;
   const uint32_t stats = smem_addr(after) + (threadIdx.x >> 5) * (STAGES * STATS_STAGE);
-  Walk<GATE == 2> work, ahead;
+  Walk<ROWS, GATE == 2> work, ahead;
   work.unit = CLUSTER ? blockIdx.x / (uint32_t)p.cluster : blockIdx.x * groups + (uint32_t)g.group;
   work.enter(p);
   ahead = work;
@@ -726,7 +730,7 @@ residual_bwd_kernel(const __grid_constant__ ResidualParams p) {
   const unsigned long long number = drop_number(p.drop);
   const bool layer_pre = WIDE && p.pre == BIMASK_NORM_LAYER, layer_post = WIDE && POST && p.post == BIMASK_NORM_LAYER;
   auto gate_row = [&](uint32_t t) { return p.gate + (long long)(p.gate_span == 1u ? t : t / p.gate_span) * p.gate_pitch8; };
-  auto fetch = [&](const Walk<GATE == 2>& w, uint32_t stage) {
+  auto fetch = [&](const Walk<ROWS, GATE == 2>& w, uint32_t stage) {
     const bool more = w.more(p);
     const uint32_t at = ring + stage * STAGE, slot0 = smem_addr(smem) + stage * STAGE;
 #pragma unroll
@@ -746,8 +750,8 @@ residual_bwd_kernel(const __grid_constant__ ResidualParams p) {
       }
     }
     if (g.lane < 2 * ROWS) {                              // lanes 0, 1: the rows' statistics before, 2, 3: after
-      const uint32_t t = w.t + (g.lane & 1);
-      const bool before = g.lane < 2;
+      const uint32_t t = w.t + (uint32_t)(g.lane % ROWS);
+      const bool before = g.lane < ROWS;
       copy8(stats + stage * STATS_STAGE + g.lane * 8u, (before ? p.stats_pre : p.stats_post) + min(t, p.T - 1u),
             more && t < w.end && (p.has & (before ? HAS_PRE : HAS_POST)));
     }
@@ -764,7 +768,7 @@ residual_bwd_kernel(const __grid_constant__ ResidualParams p) {
   }
   fetch(ahead, 0);
   // the parameters of this thread's columns, w_pre and scale w_post: from its own pieces after the ring, or from memory
-  const uint32_t kept = ring + ring_bytes(BWD_THREADS, SLOTS);
+  const uint32_t kept = ring + ring_bytes(ROWS, THREADS, SLOTS);
   auto weights = [&](Pair (&w)[VECS][4]) {
     param_or_one(p.weight, b, w);
     if (POST && p.scale_too != nullptr) {
@@ -787,7 +791,7 @@ residual_bwd_kernel(const __grid_constant__ ResidualParams p) {
     }
   };
   if (KEPT) {
-    uint4* mine = reinterpret_cast<uint4*>(reinterpret_cast<uint8_t*>(smem) + ring_bytes(BWD_THREADS, SLOTS)) + threadIdx.x;
+    uint4* mine = reinterpret_cast<uint4*>(reinterpret_cast<uint8_t*>(smem) + ring_bytes(ROWS, THREADS, SLOTS)) + threadIdx.x;
 #pragma unroll
     for (int which = 0; which < 2; ++which) {
       Pair w[VECS][4];
@@ -796,8 +800,8 @@ residual_bwd_kernel(const __grid_constant__ ResidualParams p) {
 #pragma unroll
       for (int j = 0; j < VECS; ++j) {
         const Vec8<true> v = pack8<true>(w[j]);
-        mine[(which * VECS + j) * 2 * BWD_THREADS] = v.w[0];
-        mine[((which * VECS + j) * 2 + 1) * BWD_THREADS] = v.w[1];
+        mine[(which * VECS + j) * 2 * THREADS] = v.w[0];
+        mine[((which * VECS + j) * 2 + 1) * THREADS] = v.w[1];
       }
     }
   }
@@ -997,8 +1001,8 @@ residual_bwd_kernel(const __grid_constant__ ResidualParams p) {
 #pragma unroll
       for (int j = 0; j < VECS; ++j) {
         const Vec8<true> v = pack8<true>(sum[j]);
-        mine[2 * j * BWD_THREADS] = v.w[0];
-        mine[(2 * j + 1) * BWD_THREADS] = v.w[1];
+        mine[2 * j * THREADS] = v.w[0];
+        mine[(2 * j + 1) * THREADS] = v.w[1];
       }
       __syncthreads();
     }
@@ -1145,7 +1149,7 @@ struct RowPlan {
 
 // one_slot: a few rows go to one cluster (two steps cost less than a launch that adds up what several leave).
 // ctas: how many the card holds.  span > 1: units end where a gate row's span ends, and are as many as the groups of warps.
-RowPlan plan_rows(int threads, int T, int C, int span, int ctas, bool one_slot = false) {
+RowPlan plan_rows(int rows, int threads, int T, int C, int span, int ctas, bool one_slot = false) {
   RowPlan b = {};
   const int all = (C / 8 + 32 * VECS - 1) / (32 * VECS), most = threads / 32;             // warps of a row, of a CTA
   b.cluster = all > 2 * most ? 4 : all > most ? 2 : 1;
@@ -1155,25 +1159,38 @@ RowPlan plan_rows(int threads, int T, int C, int span, int ctas, bool one_slot =
   // Clusters that run at once: of four CTAs 33 on a B200, whose parts hold no multiple of four SMs (with 37 the last four ran by
   // themselves, 2048 x 16384 in 178 us)
   const int clusters = b.cluster == 4 ? ctas * 32 / 148 : ctas / b.cluster;
-  const bool few = one_slot && T <= 2 * ROWS * b.groups;
+  const bool few = one_slot && T <= 2 * rows * b.groups;
   const long long room = (long long)(few ? 1 : clusters) * b.groups;
   if (span > 1) {
     const int len = span < T ? span : T;
     b.gates = (T + (long long)span - 1) / span;
     b.unit_rows = (int)((T + room - 1) / room);
-    if (b.unit_rows > 1 && b.unit_rows % ROWS != 0) b.unit_rows += ROWS - b.unit_rows % ROWS;
+    if (b.unit_rows > 1 && b.unit_rows % rows != 0) b.unit_rows += rows - b.unit_rows % rows;
     // whole spans where they keep half of the groups busy, or are two steps: nothing is left to add up then (a launch of 2 us)
-    if (b.unit_rows > len || 2 * b.gates >= room || len <= 2 * ROWS) b.unit_rows = len;
+    if (b.unit_rows > len || 2 * b.gates >= room || len <= 2 * rows) b.unit_rows = len;
     b.units_per_span = (len + b.unit_rows - 1) / b.unit_rows;
     b.units = b.gates * b.units_per_span;
   } else {
-    b.unit_rows = T > room ? ROWS : 1;                    // fewer rows than groups: one each
+    b.unit_rows = T > room ? rows : 1;                    // fewer rows than groups: one each
     b.units = ((long long)T + b.unit_rows - 1) / b.unit_rows;
   }
   const long long slots = (b.units + b.groups - 1) / b.groups;
   b.slots = (int)(slots < clusters ? slots : clusters);
   if (few) b.slots = 1;
   return b;
+}
+
+// Rows per step of the backward pass: two with eight warps per SM, or one with twelve.  One hides less latency per warp and pays for an
+// exchange per row, so it is taken where it keeps twice the warps busy or needs no cluster: rows of three, five or six warps (bf16,
+// 2^25 values, RMS norms both sides and dropout: 1152 columns 114 -> 93 us, 1536 91 -> 77, 2560 105 -> 91; but 4096 81 -> 95), and of
+// nine to twelve (5120 columns 122 -> 94, fp32 stream with a layer norm before 196 -> 148).  Not with a norm after and means or
+// biases: eight values per row and 168 registers, of which it spills (5120 columns 130 -> 145); nor for short rows of an fp32 stream with means
+// (1152 columns 118 -> 133).
+int bwd_rows(int C, bool f32, bool post, bool wide) {
+  const int all = (C / 8 + 32 * VECS - 1) / (32 * VECS);
+  if (post && wide) return 2;
+  if (all > bwd_threads(2) / 32) return all <= bwd_threads(1) / 32 ? 1 : 2;
+  return (all == 3 || all == 5 || all == 6) && !(f32 && wide) ? 1 : 2;
 }
 
 template <typename K>
@@ -1201,17 +1218,26 @@ static size_t up256(size_t v) { return (v + 255) / 256 * 256; }
 // Scratch of the backward pass: the clusters' partial sums (four arrays at most), then the units' of a spanned gate, each for T
 // tokens and every smaller number.  With spans there are at most 2 T units (a last span that is not full has its empty ones),
 // and at most two per group of warps and one more per gate row.
+// Either number of rows per step: the query does not know the norms.
 static size_t column_sums_bytes(int T, int C, int span) {
-  const RowPlan b = plan_rows(BWD_THREADS, 1, C, 1, PLAN_SMS);
-  const long long most = PLAN_SMS / b.cluster, slots = ((span > 1 ? 2ll : 1ll) * T + b.groups - 1) / b.groups;
-  return up256((size_t)(slots < most ? slots : most) * 4 * C * sizeof(float));
+  size_t bytes = 0;
+  for (int rows = 1; rows <= 2; ++rows) {
+    const RowPlan b = plan_rows(rows, bwd_threads(rows), 1, C, 1, PLAN_SMS);
+    const long long most = PLAN_SMS / b.cluster, slots = ((span > 1 ? 2ll : 1ll) * T + b.groups - 1) / b.groups;
+    bytes = std::max(bytes, up256((size_t)(slots < most ? slots : most) * 4 * C * sizeof(float)));
+  }
+  return bytes;
 }
 size_t residual_workspace_bytes(int T, int C, int span) {
   size_t bytes = column_sums_bytes(T, C, span);
   if (span > 1) {
-    const RowPlan b = plan_rows(BWD_THREADS, 1, C, 1, PLAN_SMS);
-    const long long gates = (T + (long long)span - 1) / span, most = 2ll * (PLAN_SMS / b.cluster) * b.groups + gates;
-    bytes += (size_t)(most < 2ll * T ? most : 2ll * T) * C * sizeof(float);
+    const long long gates = (T + (long long)span - 1) / span;
+    long long units = 0;
+    for (int rows = 1; rows <= 2; ++rows) {
+      const RowPlan b = plan_rows(rows, bwd_threads(rows), 1, C, 1, PLAN_SMS);
+      units = std::max(units, 2ll * (PLAN_SMS / b.cluster) * b.groups + gates);
+    }
+    bytes += (size_t)(units < 2ll * T ? units : 2ll * T) * C * sizeof(float);
   }
   return bytes;
 }
@@ -1280,13 +1306,13 @@ static ResidualParams residual_params(const bimask_residual_args& a) {
 
 int launch_residual_fwd(const bimask_residual_args& a, cudaStream_t s) {
   ResidualParams p = residual_params(a);
-  const RowPlan b = plan_rows(FWD_THREADS, a.T, a.C, 1, sm_count());
+  const RowPlan b = plan_rows(ROWS, FWD_THREADS, a.T, a.C, 1, sm_count());
   take_plan(p, b);
   using Yes = std::true_type;
   using No = std::false_type;
   auto run = [&](auto f32, auto gate, auto layer, auto cluster) -> int {
     constexpr bool F = decltype(f32)::value, G = decltype(gate)::value, L = decltype(layer)::value, K = decltype(cluster)::value;
-    return launch_rows(residual_fwd_kernel<F, G, L, K>, b, ring_bytes(FWD_THREADS, fwd_slots(F, G)) + Exchange<4, FWD_THREADS, K>::BYTES, s, p);
+    return launch_rows(residual_fwd_kernel<F, G, L, K>, b, ring_bytes(ROWS, FWD_THREADS, fwd_slots(F, G)) + Exchange<4, FWD_THREADS, K>::BYTES, s, p);
   };
   const bool means = p.post == BIMASK_NORM_LAYER || p.pre == BIMASK_NORM_LAYER;
   auto pick = [&](auto f32, auto gate) -> int {
@@ -1303,8 +1329,6 @@ int launch_residual_fwd(const bimask_residual_args& a, cudaStream_t s) {
 int launch_residual_bwd(const bimask_residual_args& a, cudaStream_t s) {
   ResidualParams p = residual_params(a);
   const bool spanned = a.dgate != nullptr && p.gate_span > 1;
-  const RowPlan b = plan_rows(BWD_THREADS, a.T, a.C, spanned ? (int)p.gate_span : 1, PLAN_SMS, true);
-  take_plan(p, b);
   const bool branch = a.dy || a.dgate || a.dscale || a.dw_post || a.db_post, post = branch && a.post != BIMASK_NORM_NONE;
   p.has = (a.pre != BIMASK_NORM_NONE ? HAS_PRE : 0) | (a.dxo ? HAS_DXO : 0) | (branch && a.y ? HAS_Y : 0) | (post ? HAS_POST : 0);
   const void* some = p.has & HAS_PRE ? a.xo : a.dxo;       // one of the two is there
@@ -1322,19 +1346,27 @@ int launch_residual_bwd(const bimask_residual_args& a, cudaStream_t s) {
   p.db_post = a.db_post;
   p.dw_pre = a.dw_pre;
   p.db_pre = a.db_pre;
+  const bool wide = (post && p.post == BIMASK_NORM_LAYER) || p.pre == BIMASK_NORM_LAYER || (p.want & (SUM_B | SUM_G2)) != 0;
+  const int rows = bwd_rows(a.C, a.stream_type == BIMASK_TYPE_F32, post, wide);
+  const RowPlan b = plan_rows(rows, bwd_threads(rows), a.T, a.C, spanned ? (int)p.gate_span : 1, PLAN_SMS, true);
+  take_plan(p, b);
   if (b.slots > 1) p.sums = reinterpret_cast<float*>(a.ws);
   if (spanned && b.units_per_span > 1) p.gate_sums = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(a.ws) + column_sums_bytes(a.T, a.C, (int)p.gate_span));
   using Yes = std::true_type;
   using No = std::false_type;
-  auto run = [&](auto f32, auto gate, auto post, auto wide, auto cluster) -> int {
+  auto run_with = [&](auto step, auto f32, auto gate, auto post, auto wide, auto cluster) -> int {
     constexpr bool F = decltype(f32)::value, P = decltype(post)::value, W = decltype(wide)::value, K = decltype(cluster)::value;
-    constexpr int G = decltype(gate)::value;
-    constexpr int values = bwd_values(P, W), kept = bwd_keeps_params(F, K, values) ? PARAM_BYTES : 0;
-    constexpr int bytes = ring_bytes(BWD_THREADS, bwd_slots(F, G != 0)) + kept + STATS_BYTES + Exchange<values * ROWS, BWD_THREADS, K>::BYTES;
+    constexpr int G = decltype(gate)::value, R = decltype(step)::value, H = bwd_threads(R);
+    constexpr int values = bwd_values(P, W), kept = bwd_keeps_params(F, K, values) ? param_bytes(H) : 0;
+    constexpr int bytes = ring_bytes(R, H, bwd_slots(F, G != 0)) + kept + stats_bytes(R) + Exchange<values * R, H, K>::BYTES;
     static_assert(bytes <= 227 * 1024, "shared memory of a CTA");
-    return launch_rows(residual_bwd_kernel<F, G, P, W, K>, b, bytes, s, p);
+    return launch_rows(residual_bwd_kernel<R, F, G, P, W, K>, b, bytes, s, p);
   };
-  const bool wide = (post && p.post == BIMASK_NORM_LAYER) || p.pre == BIMASK_NORM_LAYER || (p.want & (SUM_B | SUM_G2)) != 0;
+  auto run = [&](auto f32, auto gate, auto post, auto wide, auto cluster) -> int {
+    if constexpr (!decltype(cluster)::value && !(decltype(post)::value && decltype(wide)::value))
+      if (rows == 1) return run_with(std::integral_constant<int, 1>(), f32, gate, post, wide, cluster);
+    return run_with(std::integral_constant<int, 2>(), f32, gate, post, wide, cluster);
+  };
   auto pick3 = [&](auto f32, auto gate, auto post) -> int {
     if (b.cluster > 1) return wide ? run(f32, gate, post, Yes(), Yes()) : run(f32, gate, post, No(), Yes());
     return wide ? run(f32, gate, post, Yes(), No()) : run(f32, gate, post, No(), No());

@@ -227,6 +227,32 @@ def test_against_64_bits(T, C, stream):
         assert all(torch.equal(f[k], f2[k]) for k in f) and all(torch.equal(g[k], g2[k]) for k in g if k != "ws")
 
 
+# widths whose backward pass takes one row per step in some forms: rows of three, five, six, nine and twelve warps, and the first that
+# two CTAs share again; as many rows as one CTA's launch takes and one more, and more than one row per group of warps
+ONE_ROW = [(8, 1152), (9, 1152), (650, 1056), (4, 2080), (5, 2560), (310, 2336), (3, 2816), (2, 4128), (3, 4608), (301, 5120), (160, 6144), (40, 6176)]
+
+
+@pytest.mark.parametrize("T,C", ONE_ROW)
+@pytest.mark.parametrize("stream", TYPES)
+def test_widths_of_one_row_per_step(T, C, stream):
+    for i, (post, pre) in enumerate([(0, 1), (0, 2), (1, 1), (1, 2), (1, 0), (0, 0)]):
+        q = Problem(T, C, post, pre, stream, span=(0, 1, 2, T)[(i + T) % 4], scale=i % 2 == 1, bias=i % 3 == 1, p=(0.3, 0.0)[i // 3], alpha=(0.8, 1.0)[i % 2])
+        f = q.forward()
+        g = q.backward(f)
+        q.check_backward(g, f)
+        g2 = q.backward(f)                                                 # and the same bits again
+        assert all(torch.equal(g[k], g2[k]) for k in g if k != "ws")
+
+
+@pytest.mark.parametrize("T,C,span", [(900, 1152, 5), (700, 1536, 350), (500, 2560, 97), (400, 5120, 6), (300, 6144, 1000), (310, 4608, 2)])
+@pytest.mark.parametrize("stream", TYPES)
+def test_widths_of_one_row_per_step_and_gates_that_serve_spans(T, C, span, stream):
+    for post, pre in ((0, 2), (1, 1), (1, 0)):
+        q = Problem(T, C, post, pre, stream, span=span, bias=post == 0, p=0.1)
+        f = q.forward()
+        q.check_backward(q.backward(f), f)
+
+
 @pytest.mark.parametrize("T,C,span", [(2500, 256, 7), (2500, 64, 1300), (700, 1152, 197), (4000, 320, 3999), (300, 4160, 2), (149, 4096, 150), (9000, 64, 7), (600, 8192, 64), (200, 9216, 200)])
 def test_many_rows_and_gates_that_serve_spans(T, C, span):
     """More rows than groups of warps: units of several rows, spans that end inside and a last span that is not full."""
