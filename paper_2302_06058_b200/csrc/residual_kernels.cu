@@ -1148,7 +1148,7 @@ struct RowPlan {
 };
 
 // one_slot: a few rows go to one cluster (two steps cost less than a launch that adds up what several leave).
-// ctas: how many the card holds.  span > 1: units end where a gate row's span ends, and are as many as the groups of warps.
+// ctas: how many the card holds.  span > 1: units end where a gate row's span ends.
 RowPlan plan_rows(int rows, int threads, int T, int C, int span, int ctas, bool one_slot = false) {
   RowPlan b = {};
   const int all = (C / 8 + 32 * VECS - 1) / (32 * VECS), most = threads / 32;             // warps of a row, of a CTA
@@ -1164,10 +1164,22 @@ RowPlan plan_rows(int rows, int threads, int T, int C, int span, int ctas, bool 
   if (span > 1) {
     const int len = span < T ? span : T;
     b.gates = (T + (long long)span - 1) / span;
-    b.unit_rows = (int)((T + room - 1) / room);
-    if (b.unit_rows > 1 && b.unit_rows % rows != 0) b.unit_rows += rows - b.unit_rows % rows;
-    // whole spans where they keep half of the groups busy, or are two steps: nothing is left to add up then (a launch of 2 us)
-    if (b.unit_rows > len || 2 * b.gates >= room || len <= 2 * rows) b.unit_rows = len;
+    // Fewer rows than groups: one each, but spans of two steps whole (nothing is left to add up then, a launch of 2 us).  Else the units
+    // per span whose rounds over the groups take the fewest steps, among the largest number that makes one round or two, and one to
+    // four; two steps more for any but one.  (43690 x 768 with spans of 197: three units each, of rows / groups, made 1.1 rounds and 187
+    // us; five of 40 rows make two in 118.)
+    long long best = 0;
+    b.unit_rows = len <= 2 * rows ? len : 1;
+    for (int k = 0; k < 6 && T > room; ++k) {
+      const long long most_units = (k - 3) * room / b.gates, want = k < 4 ? k + 1 : most_units < len ? most_units : len;
+      if (want < 1 || want > len || (want > 1 && want * b.gates > 2 * room + b.gates)) continue;
+      const long long unit = ((len + want - 1) / want + rows - 1) / rows * rows, each = (len + unit - 1) / unit;
+      const long long steps = (b.gates * each + room - 1) / room * (unit / rows) + (each > 1 ? 2 : 0);
+      if (best == 0 || steps < best) {
+        best = steps;
+        b.unit_rows = each > 1 ? (int)unit : len;
+      }
+    }
     b.units_per_span = (len + b.unit_rows - 1) / b.unit_rows;
     b.units = b.gates * b.units_per_span;
   } else {
