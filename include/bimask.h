@@ -290,7 +290,8 @@ int bimask_act_dropout_bwd(const uint16_t* dY, const int8_t* Zq, const uint8_t* 
  * Backward.  in: dxo, the gradient of x' from its other uses (NULL: zero), dn; xo, stats_pre with a norm before, stats_post with a
  *            norm after, gate, scale, w_*, b_post, drop as in the forward pass; y with a norm after, dgate or dscale.
  *            out, each of them NULL where it is not wanted: dx (may be dxo), dy (may be dn or y), dgate (summed over its span, rounded
- *            once), dscale, dw_post, db_post, dw_pre, db_pre (fp32, added in an order that depends on the sizes alone).
+ *            once), dscale, dw_post, db_post, dw_pre, db_pre (fp32, added in an order that depends on the sizes, the types, the norms
+ *            and the gate's span, and with gate_span > 1 on whether dgate is wanted).
  *            With y absent in the forward pass only dx, dw_pre and db_pre are asked for (xo: alpha x).  Where an element was dropped
  *            its gradient is 0 times that of x'.
  *            ws: bimask_residual_norm_workspace_bytes(T, C, gate_span, or 1 without a gate) bytes, needed for gradients of vectors

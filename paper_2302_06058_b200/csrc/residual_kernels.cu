@@ -1195,14 +1195,17 @@ RowPlan plan_rows(int rows, int threads, int T, int C, int span, int ctas, bool 
 // Rows per step of the backward pass: two with eight warps per SM, or one with twelve.  One hides less latency per warp and pays for an
 // exchange per row, so it is taken where it keeps twice the warps busy or needs no cluster: rows of three, five or six warps (bf16,
 // 2^25 values, RMS norms both sides and dropout: 1152 columns 114 -> 93 us, 1536 91 -> 77, 2560 105 -> 91; but 4096 81 -> 95), and of
-// nine to twelve (5120 columns 122 -> 94, fp32 stream with a layer norm before 196 -> 148).  Not with a norm after and means or
-// biases: eight values per row and 168 registers, of which it spills (5120 columns 130 -> 145); nor for short rows of an fp32 stream with means
-// (1152 columns 118 -> 133).
-int bwd_rows(int C, bool f32, bool post, bool wide) {
-  const int all = (C / 8 + 32 * VECS - 1) / (32 * VECS);
-  if (post && wide) return 2;
+// nine to twelve (5120 columns 122 -> 94, fp32 stream with a layer norm before 196 -> 148).  A gate per token next to a layer norm leaves
+// two rows too few of 255 registers, one row enough of 168 (1024 columns 116 -> 98, 4096 132 -> 104).  Not with a norm after and means:
+// eight values per row, of which 168 registers spill (5120 columns 130 -> 145); nor for short rows of an fp32 stream with means and no
+// gate (1152 columns 118 -> 133).  Which gradients are wanted plays no part: one alone is added up as it is among the others.
+int bwd_rows(const bimask_residual_args& a) {
+  const int all = (a.C / 8 + 32 * VECS - 1) / (32 * VECS);
+  const bool f32 = a.stream_type == BIMASK_TYPE_F32, means = a.post == BIMASK_NORM_LAYER || a.pre == BIMASK_NORM_LAYER;
+  if (a.post != BIMASK_NORM_NONE && means) return 2;
   if (all > bwd_threads(2) / 32) return all <= bwd_threads(1) / 32 ? 1 : 2;
-  return (all == 3 || all == 5 || all == 6) && !(f32 && wide) ? 1 : 2;
+  if (a.gate != nullptr && a.gate_span == 1 && means && !f32) return 1;
+  return (all == 3 || all == 5 || all == 6) && !(f32 && means && a.gate == nullptr) ? 1 : 2;
 }
 
 template <typename K>
@@ -1359,7 +1362,7 @@ int launch_residual_bwd(const bimask_residual_args& a, cudaStream_t s) {
   p.dw_pre = a.dw_pre;
   p.db_pre = a.db_pre;
   const bool wide = (post && p.post == BIMASK_NORM_LAYER) || p.pre == BIMASK_NORM_LAYER || (p.want & (SUM_B | SUM_G2)) != 0;
-  const int rows = bwd_rows(a.C, a.stream_type == BIMASK_TYPE_F32, post, wide);
+  const int rows = bwd_rows(a);
   const RowPlan b = plan_rows(rows, bwd_threads(rows), a.T, a.C, spanned ? (int)p.gate_span : 1, PLAN_SMS, true);
   take_plan(p, b);
   if (b.slots > 1) p.sums = reinterpret_cast<float*>(a.ws);
@@ -1375,7 +1378,7 @@ int launch_residual_bwd(const bimask_residual_args& a, cudaStream_t s) {
     return launch_rows(residual_bwd_kernel<R, F, G, P, W, K>, b, bytes, s, p);
   };
   auto run = [&](auto f32, auto gate, auto post, auto wide, auto cluster) -> int {
-    if constexpr (!decltype(cluster)::value && !(decltype(post)::value && decltype(wide)::value))
+    if constexpr (!decltype(cluster)::value)
       if (rows == 1) return run_with(std::integral_constant<int, 1>(), f32, gate, post, wide, cluster);
     return run_with(std::integral_constant<int, 2>(), f32, gate, post, wide, cluster);
   };

@@ -244,6 +244,20 @@ def test_widths_of_one_row_per_step(T, C, stream):
         assert all(torch.equal(g[k], g2[k]) for k in g if k != "ws")
 
 
+@pytest.mark.parametrize("T,C", [(1, 32), (24, 256), (25, 256), (1800, 384), (12, 768), (13, 768), (601, 1024), (4, 2048), (155, 3584), (301, 4096)])
+@pytest.mark.parametrize("stream", TYPES)
+def test_a_gate_per_token_with_means_or_biases(T, C, stream):
+    for post, pre in ((0, 2), (0, 1), (2, 1)):
+        q = Problem(T, C, post, pre, stream, span=1, scale=pre == 1, p=0.2)
+        f = q.forward()
+        g = q.backward(f)
+        q.check_backward(g, f)
+        for k in ("dgate", "dscale", "dw_pre", "dy"):                      # every gradient alone is what it is among the others
+            if k in g:
+                alone = q.backward(f, **{o: None for o in g if o not in (k, "ws")})
+                assert torch.equal(alone[k], g[k]), k
+
+
 @pytest.mark.parametrize("T,C,span", [(900, 1152, 5), (700, 1536, 350), (500, 2560, 97), (400, 5120, 6), (300, 6144, 1000), (310, 4608, 2)])
 @pytest.mark.parametrize("stream", TYPES)
 def test_widths_of_one_row_per_step_and_gates_that_serve_spans(T, C, span, stream):
