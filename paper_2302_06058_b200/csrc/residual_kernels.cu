@@ -121,6 +121,7 @@ constexpr int ROWS = 2, VECS = 2, STAGES = 2;
 // 168 with one (see bwd_rows).
 constexpr int FWD_THREADS = 512;
 BIMASK_HD constexpr int bwd_threads(int rows) { return rows == 2 ? 256 : 384; }
+constexpr long long CLUSTER_WAIT = 4000000000ll;          // cycles, some two seconds, that a CTA waits for its peers' values
 constexpr int MAX_ROW_WARPS = 32;                         // of a cluster of two or four CTAs
 static_assert(RESIDUAL_MAX_C == 8 * 32 * VECS * MAX_ROW_WARPS, "eight columns of each of a thread's blocks");
 
@@ -230,7 +231,7 @@ __device__ __forceinline__ float columns_of(int w, uint32_t C8) { return 8.f * (
 template <int VALUES, int THREADS, bool CLUSTER>
 struct Exchange {
   static constexpr int WORDS = CLUSTER ? MAX_ROW_WARPS : THREADS / 64 * 4;
-  static constexpr int BYTES = 2 * VALUES * WORDS * 4;
+  static constexpr int BARRIERS = 2 * VALUES * WORDS * 4, BYTES = BARRIERS + (CLUSTER ? 16 : 0);      // a cluster's: one per buffer
 };
 template <int VALUES, int THREADS, bool CLUSTER>
 struct Group {                                            // a thread's place among those that share its rows
@@ -242,6 +243,7 @@ struct Group {                                            // a thread's place am
   float inv_columns;                                      // 1 / columns that this warp holds
   float peer_columns[CLUSTER ? MAX_ROW_WARPS / 16 : 1];   // columns of the warps whose values a lane reads
   uint32_t buffer, flip;                                  // address of the buffer in use; buffer ^ flip: the other one
+  uint32_t barrier, phase;                                // of a cluster's buffer in use; 8 * its parity, and 1 once a wait ran out
 
   __device__ __forceinline__ Group(const ResidualParams& p, uint32_t exchange) {
     const int w = threadIdx.x >> 5;
@@ -256,22 +258,39 @@ struct Group {                                            // a thread's place am
     for (int k = 0; k < (CLUSTER ? MAX_ROW_WARPS / 16 : 1); ++k) peer_columns[k] = columns_of((lane & (CLUSTER ? 15 : THREADS / 32 - 1)) + 16 * k, p.C8);
     buffer = exchange + (uint32_t)((alone ? 0 : group) * 2 * VALUES * width * 4);
     flip = buffer ^ (buffer + (uint32_t)(VALUES * width * 4));
+    barrier = exchange + Exchange<VALUES, THREADS, CLUSTER>::BARRIERS;
+    phase = 0;
   }
   // Value i of this warp, to every CTA that shares the row ...
   __device__ __forceinline__ void publish(int i, float v) const {
     const uint32_t at = buffer + (uint32_t)((i * width + warp) * 4);
     if (!CLUSTER) asm volatile("st.shared.f32 [%0], %1;" ::"r"(at), "f"(v) : "memory");
     else
-      for (int r = 0; r < cluster; ++r) ptx::st_cluster_u32(ptx::mapa(at, (uint32_t)r), __float_as_uint(v));
+      for (int r = 0; r < cluster; ++r) ptx::st_async_u32(ptx::mapa(at, (uint32_t)r), __float_as_uint(v), ptx::mapa(barrier, (uint32_t)r));
   }
-  __device__ __forceinline__ void meet() const {
-    if (CLUSTER) ptx::cluster_sync();
-    else ptx::named_bar_sync(group + 1, 32 * warps);
+  // values: as many as every warp publishes.  A cluster's CTAs each count the bytes that arrive: the cluster's own barrier also waits for
+  // the rows that were just stored (backward, 2^25 values of 8192 columns: bf16 101 us, so 89, fp32 stream 164 and 113; forward 2048 x
+  // 16384 83 and 68).  Nobody is a phase ahead: a warp's next values leave after it has all of this phase's.  False, and the row's results
+  // NaN, if the peers' values did not come in time.
+  __device__ __forceinline__ bool meet(int values) {
+    if (!CLUSTER) {
+      ptx::named_bar_sync(group + 1, 32 * warps);
+      return true;
+    }
+    if (threadIdx.x == 0) ptx::mbar_expect_tx(barrier, (uint32_t)(values * cluster * warps * 4));
+    if ((phase & 1u) == 0u && !ptx::mbar_wait_cluster(barrier, phase >> 3 & 1u, CLUSTER_WAIT)) phase |= 1u;
+    return (phase & 1u) == 0u;
   }
   // ... and all warps' values, after they have met.  Two buffers in turn: who writes one has met the others over the other one, and
   // by then everybody had read this one.
   __device__ __forceinline__ uint32_t published(int i, int w) const { return buffer + (uint32_t)((i * width + w) * 4); }
-  __device__ __forceinline__ void turn() { buffer ^= flip; }
+  __device__ __forceinline__ void turn() {
+    buffer ^= flip;
+    if (CLUSTER) {
+      phase ^= (barrier & 8u);                            // after the second buffer
+      barrier ^= 8u;
+    }
+  }
 };
 
 // Sums over a warp of N values at a time: at each step a lane keeps half of its values and hands the others to its partner, until
@@ -298,8 +317,7 @@ __device__ __forceinline__ void row_totals(Group<N, THREADS, CLUSTER>& g, float 
   if (!g.alone) {
     const int i = g.lane / LANES, part = g.lane % LANES;
     if (part == 0) g.publish(i, v);
-    g.meet();
-    v = 0.f;
+    v = g.meet(N) ? 0.f : NAN;
 #pragma unroll
     for (int k = 0; k < ((CLUSTER ? MAX_ROW_WARPS : THREADS / 32) + 3) / 4; k += LANES) {
       const int w = 4 * (part + k);
@@ -360,8 +378,7 @@ __device__ __forceinline__ void row_stats(const Pair (&v)[ROWS][VECS][4], const 
       if (LAYER && layer) g.publish(half, m);
       g.publish(2 + half, sq);
     }
-    g.meet();
-    sq = 0.f;
+    sq = g.meet(LAYER && layer ? 2 * ROWS : ROWS) ? 0.f : NAN;
     constexpr int EACH = CLUSTER ? MAX_ROW_WARPS / 16 : 1, SPREAD = CLUSTER ? 8 : THREADS / 64;
     float own[EACH];
 #pragma unroll
@@ -499,9 +516,18 @@ __device__ __forceinline__ void read_stream(uint32_t slot, const StreamPlace& s,
 }
 template <int VALUES, int THREADS, bool CLUSTER>
 __device__ __forceinline__ void clear_exchange(float* exchange) {
-  for (int i = threadIdx.x; i < Exchange<VALUES, THREADS, CLUSTER>::BYTES / 4; i += blockDim.x) exchange[i] = 0.f;
-  if (CLUSTER) ptx::cluster_sync();                       // before a peer writes here, and before this CTA writes to a peer
-  else __syncthreads();
+  constexpr int BARRIERS = Exchange<VALUES, THREADS, CLUSTER>::BARRIERS;
+  for (int i = threadIdx.x; i < BARRIERS / 4; i += blockDim.x) exchange[i] = 0.f;
+  if (CLUSTER) {
+    if (threadIdx.x == 0) {
+      ptx::mbar_init(smem_addr(exchange) + BARRIERS, 1);
+      ptx::mbar_init(smem_addr(exchange) + BARRIERS + 8, 1);
+      ptx::fence_barrier_init();
+    }
+    ptx::cluster_sync();                                  // before a peer writes here, and before this CTA writes to a peer
+  } else {
+    __syncthreads();
+  }
 }
 
 // every row's blocks times (plus) a vector of parameters, if there is one
