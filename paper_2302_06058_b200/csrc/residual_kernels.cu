@@ -15,7 +15,7 @@ using act::Pair;
 
 // ------------------------------------------------------------------------------------------
 // Dropout alone: a flat stream of blocks of eight elements, the next items of a thread on their way.  Bound by HBM: 8192 x 16384 of
-// bf16 in 93 us on the device (5.8 TB/s), the generator's wide multiplications two thirds of what their pipe can do meanwhile; 8192 x
+// bf16 in 90 us on the device (6.0 TB/s), the generator's wide multiplications two thirds of what their pipe can do meanwhile; 8192 x
 // 8192 of fp32 in 99 us (5.4 TB/s).  More items on their way (four) and more CTAs than fit at once were no faster.
 // ------------------------------------------------------------------------------------------
 constexpr int DROP_THREADS = 256;
@@ -112,9 +112,10 @@ dropout_kernel(const uint4* x, long long items, uint4* y /* may be x */, const _
 // parts: columns and rows past the end are copied as zeros (from a clamped address, of which cp.async reads nothing) and work like
 // the others, but for their stores.
 // Why two blocks and two rows per thread: what a step costs beside its blocks is shared by four (two RMS norms and dropout, forward: 304
-// instructions per block with one block and two rows per step, 245 with two and two).  8192 x 4096 with two RMS norms and dropout, on the device: forward 56 us (floor 41; without
-// dropout 45), backward 76 (floor 61).  A third stage of the ring, three CTAs per SM and parameters in shared memory (forward)
-// changed nothing or cost time; one row per step with twice the warps does not fit the registers of the backward pass.
+// instructions per block with one block and two rows per step, 245 with two and two).  8192 x 4096 with two RMS norms and dropout, back
+// to back: forward 50 us (floor 41), backward 74 with the sums (floor 61).  A third stage of the ring, three CTAs per SM and parameters
+// in shared memory (forward) changed nothing or cost time; so did one row per step with 24 warps in the forward pass, but for rows of
+// nine to twelve warps (5120 columns 70 and 66 us).  The backward pass takes it where it pays: bwd_rows.
 // ------------------------------------------------------------------------------------------
 constexpr int ROWS = 2, VECS = 2, STAGES = 2;
 // Threads of a CTA (one per SM).  The backward pass keeps five to eight arrays of a step in registers: 255 of them with two rows per step,
