@@ -130,7 +130,7 @@ struct ResidualParams {
   uint32_t T, C8;
   int warps, cluster;                // warps per row in a CTA, CTAs per row
   int post, pre;
-  float eps_post, eps_pre, alpha, inv_c;
+  float eps_post, eps_pre, alpha, inv_c, minus_zero;
   uint32_t gate_span;                // 0: no gate
   long long gate_pitch8;
   DropParams drop;
@@ -665,7 +665,10 @@ residual_fwd_kernel(const __grid_constant__ ResidualParams p) {
 #pragma unroll
         for (int j = 0; j < VECS; ++j) fill8(v[r][j], 0.f);
     }
-    const Pair alpha = act::both(p.alpha);
+    // alpha x is rounded by itself: that takes off what alpha in fp32 has more or less than its decimal where alpha x has few bits, and ties
+    // go to the even side.  (Fused, the excess decided all ties alike: 350 of 98304 sums of bf16 with alpha = 1.7 were rounded the wrong way.)
+    // The product has an addend of -0 that only the caller knows, because ptxas fuses packed mul.rn and add.rn where it sees both.
+    const Pair alpha = act::both(p.alpha), nothing = act::both(p.minus_zero);
 #pragma unroll
     for (int r = 0; r < ROWS; ++r)
 #pragma unroll
@@ -673,7 +676,7 @@ residual_fwd_kernel(const __grid_constant__ ResidualParams p) {
         Pair x[4];
         read_stream<F32>(slot0 + piece<SLOTS, PITCH>(0, r, j, X), place, x);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) v[r][j][k] = act::fma2(x[k], alpha, v[r][j][k]);
+        for (int k = 0; k < 4; ++k) v[r][j][k] = act::add2(act::fma2(x[k], alpha, nothing), v[r][j][k]);
         if (p.xo != nullptr && live[r] && b.ok[j]) store8<F32>(p.xo, (long long)(row[r] + b.at[j]), v[r][j]);
       }
     if (p.pre != BIMASK_NORM_NONE) {
@@ -1323,6 +1326,7 @@ static ResidualParams residual_params(const bimask_residual_args& a) {
   p.eps_pre = a.eps_pre;
   p.alpha = a.alpha;
   p.inv_c = 1.f / (float)a.C;
+  p.minus_zero = -0.f;
   p.gate_span = a.gate != nullptr ? (uint32_t)a.gate_span : 0u;
   p.gate_pitch8 = a.gate_pitch / 8;
   p.drop = drop_params(&a.drop);
