@@ -130,7 +130,7 @@ struct ResidualParams {
   uint32_t T, C8;
   int warps, cluster;                // warps per row in a CTA, CTAs per row
   int post, pre;
-  float eps_post, eps_pre, alpha, inv_c, minus_zero;
+  float eps_post, eps_pre, alpha, inv_c;
   uint32_t gate_span;                // 0: no gate
   long long gate_pitch8;
   DropParams drop;
@@ -199,6 +199,12 @@ __device__ __forceinline__ Pair dot8(const Pair (&v)[4], const Pair (&w)[4]) {
   return act::add2(act::fma2(v[1], w[1], act::mul2(v[0], w[0])), act::fma2(v[3], w[3], act::mul2(v[2], w[2])));
 }
 
+// both numbers times `a`, never fused with an addition that follows
+__device__ __forceinline__ Pair scalar_product(Pair v, float a) {
+  float lo, hi;
+  act::split(v, lo, hi);
+  return act::pair(__fmul_rn(lo, a), __fmul_rn(hi, a));
+}
 // eight fp32 parameters of block c
 __device__ __forceinline__ void param8(const float* base, uint32_t c, Pair (&p)[4]) {
   const float4 a = __ldg(reinterpret_cast<const float4*>(base) + 2 * c), b = __ldg(reinterpret_cast<const float4*>(base) + 2 * c + 1);
@@ -667,8 +673,9 @@ residual_fwd_kernel(const __grid_constant__ ResidualParams p) {
     }
     // alpha x is rounded by itself: that takes off what alpha in fp32 has more or less than its decimal where alpha x has few bits, and ties
     // go to the even side.  (Fused, the excess decided all ties alike: 350 of 98304 sums of bf16 with alpha = 1.7 were rounded the wrong way.)
-    // The product has an addend of -0 that only the caller knows, because ptxas fuses packed mul.rn and add.rn where it sees both.
-    const Pair alpha = act::both(p.alpha), nothing = act::both(p.minus_zero);
+    // In scalar products, because ptxas fuses packed mul.rn and add.rn where it sees both; for fp32, whose pairs come as such from shared
+    // memory, only where alpha is not 1.
+    const bool scaled = p.alpha != 1.f;
 #pragma unroll
     for (int r = 0; r < ROWS; ++r)
 #pragma unroll
@@ -676,7 +683,10 @@ residual_fwd_kernel(const __grid_constant__ ResidualParams p) {
         Pair x[4];
         read_stream<F32>(slot0 + piece<SLOTS, PITCH>(0, r, j, X), place, x);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) v[r][j][k] = act::add2(act::fma2(x[k], alpha, nothing), v[r][j][k]);
+        for (int k = 0; k < 4; ++k) {
+          if (!F32 || scaled) x[k] = scalar_product(x[k], p.alpha);
+          v[r][j][k] = act::add2(x[k], v[r][j][k]);
+        }
         if (p.xo != nullptr && live[r] && b.ok[j]) store8<F32>(p.xo, (long long)(row[r] + b.at[j]), v[r][j]);
       }
     if (p.pre != BIMASK_NORM_NONE) {
@@ -1326,7 +1336,6 @@ static ResidualParams residual_params(const bimask_residual_args& a) {
   p.eps_pre = a.eps_pre;
   p.alpha = a.alpha;
   p.inv_c = 1.f / (float)a.C;
-  p.minus_zero = -0.f;
   p.gate_span = a.gate != nullptr ? (uint32_t)a.gate_span : 0u;
   p.gate_pitch8 = a.gate_pitch / 8;
   p.drop = drop_params(&a.drop);
