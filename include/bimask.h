@@ -296,7 +296,10 @@ int bimask_act_dropout_bwd(const uint16_t* dY, const int8_t* Zq, const uint8_t* 
  *            its gradient is 0 times that of x'.
  *            ws: bimask_residual_norm_workspace_bytes(T, C, gate_span, or 1 without a gate) bytes, needed for gradients of vectors
  *            and of a gate with gate_span > 1; nothing is expected in it, and calls that may overlap need one each.  Never
- *            fewer for more tokens. */
+ *            fewer for more tokens.
+ * Rows too wide for one CTA (above 8192 columns forward, 4096 to 6144 backward) are shared by two or four, which wait for one another's
+ * sums, about two seconds at most.  If a wait runs out the call ends all the same: *status_word (device int, may be NULL) becomes
+ * BIMASK_ETIMEOUT, and results of that row, of later rows of the same CTAs and of sums over rows are NaN where they are not right. */
 typedef struct {
   int T, C;
   int stream_type, post, pre;  /* BIMASK_TYPE_*, BIMASK_NORM_* */
@@ -317,6 +320,7 @@ typedef struct {
   float *dscale, *dw_post, *db_post, *dw_pre, *db_pre;
   void* ws;
   size_t ws_bytes;
+  int32_t* status_word;
 } bimask_residual_args;
 
 size_t bimask_residual_norm_workspace_bytes(int T, int C, int gate_span);
@@ -500,6 +504,12 @@ size_t bimask_perm_search_static_max_entries(void);
  * wait gives up, *status_word (device int) becomes BIMASK_ETIMEOUT and the kernel returns
  * normally (no trap: the context stays usable). */
 int bimask_debug_wait_probe(int32_t* status_word, void* stream);
+
+/* Debug helper, not on the hot path: bimask_residual_norm_fwd (backward: _bwd) whose CTAs that share a row wait for one another
+ * limit_cycles (at most 4e9) instead of two seconds, and of whose rows warp late_warp (0 .. 31, counted through the row; -1: none) gives up
+ * at once in its CTAs' meeting number late_meeting (0 .. 3): they meet once per norm and step of two rows (backward: once per step). */
+int bimask_debug_residual_give_up(const bimask_residual_args* args, int backward, int64_t limit_cycles, int late_warp, int late_meeting,
+                                  void* stream);
 
 /* Debug helper, host only: how bimask_linear_fwd runs a layer of this size (dense: hw_meta_f == NULL).  HOST array out[4] =
  * {kernel: 0 few tokens, 1 one row tile, 2 CTA pairs, 3 CTA pairs with two row tiles each; CTAs that share a tile's

@@ -27,7 +27,7 @@ EXPORTS = ("bimask_last_error", "bimask_launch_count", "bimask_hw_meta_bytes", "
            "bimask_debug_linear_plan",
            "bimask_linear_workspace_bytes", "bimask_linear_fwd", "bimask_act_bwd", "bimask_ckpt_pack", "bimask_ckpt_unpack",
            "bimask_wgrad_ckpt", "bimask_dropout", "bimask_ckpt_unpack_dropout", "bimask_act_dropout_bwd",
-           "bimask_residual_norm_workspace_bytes", "bimask_residual_norm_fwd", "bimask_residual_norm_bwd")
+           "bimask_residual_norm_workspace_bytes", "bimask_residual_norm_fwd", "bimask_residual_norm_bwd", "bimask_debug_residual_give_up")
 
 
 class BimaskError(RuntimeError):
@@ -73,13 +73,13 @@ class ResidualArgs(Structure):
     """Mirror of bimask_residual_args."""
     _fields_ = [("T", c_int), ("C", c_int), ("stream_type", c_int), ("post", c_int), ("pre", c_int), ("gate_span", c_int),
                 ("gate_pitch", c_int64), ("eps_post", c_float), ("eps_pre", c_float), ("alpha", c_float), ("drop", Dropout),
-                *((name, c_void_p) for name in _RESIDUAL_POINTERS), ("ws_bytes", c_size_t)]
+                *((name, c_void_p) for name in _RESIDUAL_POINTERS), ("ws_bytes", c_size_t), ("status_word", c_void_p)]
 
 
 _RESIDUAL_INDEX = {name: i for i, name in enumerate(_RESIDUAL_POINTERS)}
 # the same fields for struct.pack, in one call (setting 30 fields one by one takes longer than a short kernel)
-_RESIDUAL_PACK = struct.Struct("@6iq3f4xfQQP23PN").pack
-assert struct.calcsize("@6iq3f4xfQQP23PN") == ctypes.sizeof(ResidualArgs) and len(_RESIDUAL_POINTERS) == 23
+_RESIDUAL_PACK = struct.Struct("@6iq3f4xfQQP23PNP").pack
+assert struct.calcsize("@6iq3f4xfQQP23PNP") == ctypes.sizeof(ResidualArgs) and len(_RESIDUAL_POINTERS) == 23
 
 CONV_AUTO, CONV_EXPLICIT, CONV_IMPLICIT = 0, 1, 2
 
@@ -143,6 +143,7 @@ def lib() -> ctypes.CDLL:
         L.bimask_residual_norm_workspace_bytes.argtypes = [c_int, c_int, c_int]
         L.bimask_residual_norm_fwd.argtypes = [POINTER(ResidualArgs), c_void_p]
         L.bimask_residual_norm_bwd.argtypes = [POINTER(ResidualArgs), c_void_p]
+        L.bimask_debug_residual_give_up.argtypes = [POINTER(ResidualArgs), c_int, c_int64, c_int, c_int, c_void_p]
         L.bimask_check_perms.argtypes = [c_void_p, c_int, c_int, c_void_p, c_void_p, c_size_t, c_void_p]
         L.bimask_debug_wait_probe.argtypes = [c_void_p, c_void_p]
         L.bimask_debug_status.argtypes = [c_void_p]
@@ -358,7 +359,7 @@ def make_residual_args(T, C, bufs: dict, stream_type=TYPE_BF16, post=NORM_NONE, 
     ws_bytes = ws.numel() * ws.element_size() if type(ws) is _Tensor else int(get("ws_bytes", 0))
     p, seed, stream_no, counter = (0.0, 0, 0, 0) if drop is None else (drop.p, drop.seed, drop.stream_no, drop.counter or 0)
     return ResidualArgs.from_buffer_copy(_RESIDUAL_PACK(T, C, stream_type, post, pre, gate_span, pitch, eps_post, eps_pre, alpha, p, seed,
-                                                        stream_no, counter, *pointers, ws_bytes))
+                                                        stream_no, counter, *pointers, ws_bytes, _ptr(get("status_word")) or 0))
 
 
 def bimask_residual_norm_fwd(args: ResidualArgs, stream=None):
@@ -367,6 +368,10 @@ def bimask_residual_norm_fwd(args: ResidualArgs, stream=None):
 
 def bimask_residual_norm_bwd(args: ResidualArgs, stream=None):
     return _check(lib().bimask_residual_norm_bwd(args, _stream(stream)))
+
+
+def bimask_debug_residual_give_up(args: ResidualArgs, backward, limit_cycles, late_warp=-1, late_meeting=0, stream=None):
+    return _check(lib().bimask_debug_residual_give_up(args, int(backward), limit_cycles, late_warp, late_meeting, _stream(stream)))
 
 
 def make_layer_args(T, I, J, N, M, P, seed, do_search, bufs: dict, stream=None) -> LayerArgs:

@@ -464,19 +464,21 @@ static int check_residual(const char* who, const bimask_residual_args* a, bool b
   const void* all[] = {a->x, a->y, a->gate, a->scale, a->w_post, a->b_post, a->w_pre, a->b_pre, a->xo, a->n, a->stats_post, a->stats_pre,
                        a->dxo, a->dn, a->dx, a->dy, a->dgate, a->dscale, a->dw_post, a->db_post, a->dw_pre, a->db_pre, a->ws};
   for (const void* p : all) BIMASK_REQUIRE(aligned16(p), BIMASK_EINVAL, "%s: pointers must be 16-byte aligned", who);
+  BIMASK_REQUIRE((uintptr_t)a->status_word % 4 == 0, BIMASK_EINVAL, "%s: status_word must be 4-byte aligned", who);
   return BIMASK_OK;
 }
 
-int bimask_residual_norm_fwd(const bimask_residual_args* a, void* stream) {
+static int residual_fwd(const bimask_residual_args* a, const ResidualGiveUp* give_up, void* stream) {
   BIMASK_REQUIRE(a != nullptr, BIMASK_EINVAL, "bimask_residual_norm_fwd: null argument struct");
   const int rc = check_residual("bimask_residual_norm_fwd", a, a->y != nullptr);
   if (rc != BIMASK_OK) return rc;
   const bool pre = a->pre != BIMASK_NORM_NONE;
   BIMASK_REQUIRE(a->x && (a->xo || pre) && (a->n || !pre), BIMASK_EINVAL, "bimask_residual_norm_fwd: null pointer (x, xo or n)");
-  return launch_residual_fwd(*a, (cudaStream_t)stream);
+  return launch_residual_fwd(*a, (cudaStream_t)stream, give_up);
 }
+int bimask_residual_norm_fwd(const bimask_residual_args* a, void* stream) { return residual_fwd(a, nullptr, stream); }
 
-int bimask_residual_norm_bwd(const bimask_residual_args* a, void* stream) {
+static int residual_bwd(const bimask_residual_args* a, const ResidualGiveUp* give_up, void* stream) {
   BIMASK_REQUIRE(a != nullptr, BIMASK_EINVAL, "bimask_residual_norm_bwd: null argument struct");
   const char* who = "bimask_residual_norm_bwd";
   const bool branch = a->dy || a->dgate || a->dscale || a->dw_post || a->db_post;
@@ -497,7 +499,15 @@ int bimask_residual_norm_bwd(const bimask_residual_args* a, void* stream) {
     const size_t need = residual_workspace_bytes(a->T, a->C, spanned ? a->gate_span : 1);
     BIMASK_REQUIRE(a->ws && a->ws_bytes >= need, BIMASK_EINVAL, "%s: workspace too small (%zu bytes, need %zu)", who, a->ws ? a->ws_bytes : 0, need);
   }
-  return launch_residual_bwd(*a, (cudaStream_t)stream);
+  return launch_residual_bwd(*a, (cudaStream_t)stream, give_up);
+}
+int bimask_residual_norm_bwd(const bimask_residual_args* a, void* stream) { return residual_bwd(a, nullptr, stream); }
+
+int bimask_debug_residual_give_up(const bimask_residual_args* a, int backward, int64_t limit_cycles, int late_warp, int late_meeting, void* stream) {
+  BIMASK_REQUIRE(limit_cycles >= 0 && limit_cycles <= 4000000000ll && late_warp >= -1 && late_warp < 32 && late_meeting >= 0 && late_meeting <= 3, BIMASK_EINVAL,
+                 "bimask_debug_residual_give_up: limit %lld, warp %d, meeting %d out of range", (long long)limit_cycles, late_warp, late_meeting);
+  const ResidualGiveUp g = {limit_cycles, late_warp, late_meeting};
+  return backward ? residual_bwd(a, &g, stream) : residual_fwd(a, &g, stream);
 }
 
 int bimask_wgrad_ckpt(const uint16_t* dY, const int8_t* Xq, const uint8_t* Xs, int T, int I, int J, float* dW, void* ws,

@@ -287,8 +287,12 @@ inline uint32_t drop_threshold(float p) {
 int launch_dropout(const void* x, int type, int T, int C, const bimask_dropout_args& d, void* y, cudaStream_t s);
 constexpr int RESIDUAL_MAX_C = 16384;                     // 16 warps of eight columns per thread, in each of four CTAs
 size_t residual_workspace_bytes(int T, int C, int span);
-int launch_residual_fwd(const bimask_residual_args& a, cudaStream_t s);
-int launch_residual_bwd(const bimask_residual_args& a, cudaStream_t s);
+struct ResidualGiveUp {                                   // of bimask_debug_residual_give_up
+  long long limit_cycles;
+  int late_warp, late_meeting;
+};
+int launch_residual_fwd(const bimask_residual_args& a, cudaStream_t s, const ResidualGiveUp* give_up = nullptr);
+int launch_residual_bwd(const bimask_residual_args& a, cudaStream_t s, const ResidualGiveUp* give_up = nullptr);
 // Weight gradient whose token operand is a checkpoint; ws: wgrad_ckpt_bytes(T, I, J).  wgrad_ckpt_query_bytes: enough for T and
 // every smaller number of tokens; wgrad_most_splits: the same for the partial sums of launch_wgrad_impl.
 size_t wgrad_ckpt_bytes(int T, int I, int J);

@@ -122,7 +122,7 @@ constexpr int ROWS = 2, VECS = 2, STAGES = 2;
 // 168 with one (see bwd_rows).
 constexpr int FWD_THREADS = 512;
 BIMASK_HD constexpr int bwd_threads(int rows) { return rows == 2 ? 256 : 384; }
-constexpr long long CLUSTER_WAIT = 4000000000ll;          // cycles, some two seconds, that a CTA waits for its peers' values
+constexpr long long CLUSTER_WAIT = 4000000000ll;          // cycles, some two seconds, that a warp waits for its row's other warps
 constexpr int MAX_ROW_WARPS = 32;                         // of a cluster of two or four CTAs
 static_assert(RESIDUAL_MAX_C == 8 * 32 * VECS * MAX_ROW_WARPS, "eight columns of each of a thread's blocks");
 
@@ -165,6 +165,10 @@ struct ResidualParams {
   const float* scale_too;
   // Rows are given out in units of consecutive ones.  units_per_span: 0, or the units that a gate row's span is cut into.
   uint32_t units, unit_rows, units_per_span;
+  // Rows shared by a cluster: where a wait that ran out is reported (or null), its limit, and a warp that gives up by itself (tests).
+  int32_t* status;
+  long long wait_cycles;
+  uint32_t late;                     // 32 * warp + 8 * (number of its meeting modulo 4); above all of them: none
 };
 
 __device__ __forceinline__ uint32_t smem_addr(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
@@ -238,21 +242,54 @@ __device__ __forceinline__ float columns_of(int w, uint32_t C8) { return 8.f * (
 template <int VALUES, int THREADS, bool CLUSTER>
 struct Exchange {
   static constexpr int WORDS = CLUSTER ? MAX_ROW_WARPS : THREADS / 64 * 4;
-  static constexpr int BARRIERS = 2 * VALUES * WORDS * 4, BYTES = BARRIERS + (CLUSTER ? 16 : 0);      // a cluster's: one per buffer
+  // a cluster's: one barrier per buffer, and a byte for each of the row's warps that is set once the warp has given up
+  static constexpr int BARRIERS = 2 * VALUES * WORDS * 4, MARKS = BARRIERS + 16, BYTES = BARRIERS + (CLUSTER ? 16 + MAX_ROW_WARPS : 0);
 };
+// The CTAs of a cluster meet through values that are counted where they arrive.  A warp whose wait runs out gives up for good: it makes the
+// row's results and those of its later rows NaN, and publishes nothing any more.  So no later meeting is ever complete, each of the
+// others gives up in the next one at the latest, and no warp is ahead of another by more than one meeting: no value of a later row can
+// reach a place, or count for a meeting, that a slower warp still waits for.
+//
+// Thread 0 of a CTA at the end of a kernel in which some warp of the cluster gave up: values that were sent in the last two meetings may
+// still be on their way here.  Of the last one some warps sent none: their bytes are counted as sent, or not expected, so that its
+// barrier's phase ends when all that were sent have come.  Of all warps' last meetings there are two at most, one after the other, so that
+// their numbers modulo 4 tell which is later; if some warp did not give up, all have been to the very last.  own, last_own: this
+// warp of the row's, and its last meeting, modulo 4.
+__device__ __noinline__ void settle_meetings(uint32_t marks, uint32_t own, uint32_t last_own, uint32_t all, uint32_t even_bytes, uint32_t odd_bytes) {
+  auto last = [&](uint32_t w) {
+    uint32_t v;
+    asm volatile("ld.shared.u8 %0, [%1];" : "=r"(v) : "r"(marks + w) : "memory");
+    return v != 0u ? v - 1u : last_own;
+  };
+  uint32_t late = last(0), behind = 0;                    // the later of the last meetings, the warps that did not publish in it
+  for (uint32_t w = 1; w < all; ++w)
+    if (((last(w) - late) & 3u) == 1u) late = last(w);
+  for (uint32_t w = 0; w < all; ++w) behind += last(w) != late;
+  const uint32_t barriers = marks - 16u, at = barriers + ((late & 1u) << 3), before = (late + 3u) & 3u;
+  if (behind != 0u) {
+    const uint32_t bytes = late & 1u ? odd_bytes : even_bytes;
+    // this thread told the barrier to expect all bytes if its warp got as far
+    if (last(own) == late) ptx::mbar_complete_tx(at, behind * bytes);
+    else ptx::mbar_expect_tx(at, (all - behind) * bytes);
+  }
+  ptx::mbar_wait_cluster(at, late >> 1, CLUSTER_WAIT);
+  ptx::mbar_wait_cluster(barriers + ((before & 1u) << 3), before >> 1, CLUSTER_WAIT);        // over at once if there was none before
+}
+
 template <int VALUES, int THREADS, bool CLUSTER>
 struct Group {                                            // a thread's place among those that share its rows
   int lane, group, warps;                                 // warps: of the row in this CTA
   int warp;                                               // the thread's warp, counted through the row
   bool alone;                                             // the row is one warp's
-  int cluster;
+  int cluster;                                            // CTAs of the row
   int width;                                              // words of a value
   float inv_columns;                                      // 1 / columns that this warp holds
   float peer_columns[CLUSTER ? MAX_ROW_WARPS / 16 : 1];   // columns of the warps whose values a lane reads
   uint32_t buffer, flip;                                  // address of the buffer in use; buffer ^ flip: the other one
-  uint32_t barrier, phase;                                // of a cluster's buffer in use; 8 * its parity, and 1 once a wait ran out
+  uint32_t barrier, phase;                                // of a cluster's buffer in use; 16 * its parity
+  const ResidualParams& p;
 
-  __device__ __forceinline__ Group(const ResidualParams& p, uint32_t exchange) {
+  __device__ __forceinline__ Group(const ResidualParams& params, uint32_t exchange) : p(params) {
     const int w = threadIdx.x >> 5;
     lane = threadIdx.x & 31;
     warps = p.warps;
@@ -277,26 +314,52 @@ struct Group {                                            // a thread's place am
   }
   // values: as many as every warp publishes.  A cluster's CTAs each count the bytes that arrive: the cluster's own barrier also waits for
   // the rows that were just stored (backward, 2^25 values of 8192 columns: bf16 101 us, so 89, fp32 stream 164 and 113; forward 2048 x
-  // 16384 83 and 68).  Nobody is a phase ahead: a warp's next values leave after it has all of this phase's.  False, and the row's results
-  // NaN, if the peers' values did not come in time.
+  // 16384 83 and 68).  Nobody is a meeting ahead: a warp's next values leave after it has all of this one's.  False, for the whole warp,
+  // if they did not come in time: then it does not come here again.
   __device__ __forceinline__ bool meet(int values) {
     if (!CLUSTER) {
       ptx::named_bar_sync(group + 1, 32 * warps);
       return true;
     }
     if (threadIdx.x == 0) ptx::mbar_expect_tx(barrier, (uint32_t)(values * cluster * warps * 4));
-    if ((phase & 1u) == 0u && !ptx::mbar_wait_cluster(barrier, phase >> 3 & 1u, CLUSTER_WAIT)) phase |= 1u;
-    return (phase & 1u) == 0u;
+    const bool came = (uint32_t)(warp << 5) + phase + (barrier & 8u) != p.late && ptx::mbar_wait_cluster(barrier, phase >> 4, p.wait_cycles);
+    return __all_sync(0xFFFFFFFFu, came);
   }
+  // After a meeting without the others: the warp's mark with every CTA, 1 more than that meeting's number modulo 4.
+  __device__ __forceinline__ void give_up() const {
+    if (lane != 0) return;
+    for (int r = 0; r < cluster; ++r)
+      asm volatile("st.shared::cluster.u8 [%0], %1;" ::"r"(ptx::mapa(marks() + (uint32_t)warp, (uint32_t)r)), "r"(((phase + (barrier & 8u)) >> 3) + 1u) : "memory");
+    if (p.status != nullptr) atomicExch(p.status, (int32_t)BIMASK_ETIMEOUT);
+  }
+  __device__ __forceinline__ uint32_t marks() const { return (barrier & ~8u) + 16u; }
   // ... and all warps' values, after they have met.  Two buffers in turn: who writes one has met the others over the other one, and
   // by then everybody had read this one.
   __device__ __forceinline__ uint32_t published(int i, int w) const { return buffer + (uint32_t)((i * width + w) * 4); }
   __device__ __forceinline__ void turn() {
     buffer ^= flip;
     if (CLUSTER) {
-      phase ^= (barrier & 8u);                            // after the second buffer
+      phase ^= (barrier & 8u) << 1;                       // after the second buffer
       barrier ^= 8u;
     }
+  }
+  // The end of a kernel whose rows are shared by a cluster: shared memory outlives the peers' writes to it.  even, odd: values that a warp
+  // publishes in meetings of such a number.
+  __device__ __forceinline__ void finish(bool lost, int even, int odd) const {
+    if (!CLUSTER) return;
+    if (lost) give_up();
+    ptx::cluster_sync();
+    uint32_t any = 0;
+#pragma unroll
+    for (int w = 0; w < MAX_ROW_WARPS / 16; ++w) {
+      uint4 x;
+      asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(x.x), "=r"(x.y), "=r"(x.z), "=r"(x.w) : "r"(marks() + 16u * w) : "memory");
+      any |= x.x | x.y | x.z | x.w;
+    }
+    if (any == 0u) return;                                // the same in every CTA of the cluster
+    const uint32_t meeting = (phase + (barrier & 8u)) >> 3;                               // the one that was lost, or the next
+    if (threadIdx.x == 0) settle_meetings(marks(), (uint32_t)warp, lost ? meeting : (meeting + 3u) & 3u, (uint32_t)(cluster * warps), 4u * even, 4u * odd);
+    ptx::cluster_sync();
   }
 };
 
@@ -316,15 +379,16 @@ __device__ __forceinline__ float fold(float (&c)[N], int lane) {
   return v;
 }
 
-// Totals over the row of N values of every thread.
+// Totals over the row of N values of every thread; false if the row's other CTAs did not come.
 template <int N, int THREADS, bool CLUSTER>
-__device__ __forceinline__ void row_totals(Group<N, THREADS, CLUSTER>& g, float (&c)[N]) {
+__device__ __forceinline__ bool row_totals(Group<N, THREADS, CLUSTER>& g, float (&c)[N]) {
   constexpr int LANES = 32 / N;                           // that share a value
   float v = fold<N>(c, g.lane);
   if (!g.alone) {
     const int i = g.lane / LANES, part = g.lane % LANES;
     if (part == 0) g.publish(i, v);
-    v = g.meet(N) ? 0.f : NAN;
+    if (!g.meet(N)) return false;
+    v = 0.f;
 #pragma unroll
     for (int k = 0; k < ((CLUSTER ? MAX_ROW_WARPS : THREADS / 32) + 3) / 4; k += LANES) {
       const int w = 4 * (part + k);
@@ -340,6 +404,7 @@ __device__ __forceinline__ void row_totals(Group<N, THREADS, CLUSTER>& g, float 
   }
 #pragma unroll
   for (int i = 0; i < N; ++i) c[i] = __shfl_sync(0xFFFFFFFFu, v, i * LANES);
+  return true;
 }
 
 // 1 / sqrt within 2^-22; of what is below 2^-126 infinity, as of 0
@@ -351,9 +416,9 @@ __device__ __forceinline__ float rsqrt_fast(float x) {
 
 // Mean and 1 / deviation of two rows (LAYER: some norm of this kernel subtracts means; `layer`: this one does).  The squares are taken
 // about each warp's own mean, and the warps are put together by M = sum M_w + sum n_w (m_w - m)^2: one exchange, and no difference
-// of large squares.  rms: all about zero.
+// of large squares.  rms: all about zero.  False if the rows' other CTAs did not come.
 template <bool LAYER, int THREADS, bool CLUSTER>
-__device__ __forceinline__ void row_stats(const Pair (&v)[ROWS][VECS][4], const bool (&ok)[VECS], bool layer, float eps, float inv_c,
+__device__ __forceinline__ bool row_stats(const Pair (&v)[ROWS][VECS][4], const bool (&ok)[VECS], bool layer, float eps, float inv_c,
                                           Group<4, THREADS, CLUSTER>& g, float2 (&st)[ROWS]) {
   static_assert(ROWS == 2, "two rows are folded together");
   const int half = g.lane >> 4;                           // the row whose totals this lane holds
@@ -385,7 +450,8 @@ __device__ __forceinline__ void row_stats(const Pair (&v)[ROWS][VECS][4], const 
       if (LAYER && layer) g.publish(half, m);
       g.publish(2 + half, sq);
     }
-    sq = g.meet(LAYER && layer ? 2 * ROWS : ROWS) ? 0.f : NAN;
+    if (!g.meet(LAYER && layer ? 2 * ROWS : ROWS)) return false;
+    sq = 0.f;
     constexpr int EACH = CLUSTER ? MAX_ROW_WARPS / 16 : 1, SPREAD = CLUSTER ? 8 : THREADS / 64;
     float own[EACH];
 #pragma unroll
@@ -415,6 +481,7 @@ __device__ __forceinline__ void row_stats(const Pair (&v)[ROWS][VECS][4], const 
 #pragma unroll
   for (int r = 0; r < ROWS; ++r)
     st[r] = make_float2(LAYER && layer ? __shfl_sync(0xFFFFFFFFu, m, 16 * r) : 0.f, __shfl_sync(0xFFFFFFFFu, rstd, 16 * r));
+  return true;
 }
 
 // A group's walk over its units, ROWS rows at a time.  SPAN: units of many rows that end with their gate row's span; else of one
@@ -523,10 +590,11 @@ __device__ __forceinline__ void read_stream(uint32_t slot, const StreamPlace& s,
 }
 template <int VALUES, int THREADS, bool CLUSTER>
 __device__ __forceinline__ void clear_exchange(float* exchange) {
-  constexpr int BARRIERS = Exchange<VALUES, THREADS, CLUSTER>::BARRIERS;
+  constexpr int BARRIERS = Exchange<VALUES, THREADS, CLUSTER>::BARRIERS, MARKS = Exchange<VALUES, THREADS, CLUSTER>::MARKS;
   for (int i = threadIdx.x; i < BARRIERS / 4; i += blockDim.x) exchange[i] = 0.f;
   if (CLUSTER) {
     if (threadIdx.x == 0) {
+      for (int i = 0; i < MAX_ROW_WARPS / 4; ++i) exchange[MARKS / 4 + i] = 0.f;
       ptx::mbar_init(smem_addr(exchange) + BARRIERS, 1);
       ptx::mbar_init(smem_addr(exchange) + BARRIERS + 8, 1);
       ptx::fence_barrier_init();
@@ -608,6 +676,7 @@ residual_fwd_kernel(const __grid_constant__ ResidualParams p) {
   };
   fetch(ahead, 0);
   uint32_t stage = 0;
+  bool lost = false;                                      // this warp has given up
   while (work.more(p)) {
     if (F32) __syncwarp();                                // every lane has read the pieces that are overwritten now
     ahead.next(p, stride);
@@ -637,7 +706,7 @@ residual_fwd_kernel(const __grid_constant__ ResidualParams p) {
         for (int j = 0; j < VECS; ++j) read_block<false>(piece<SLOTS, PITCH>(at, r, j, Y), 0, v[r][j]);
       if (p.post != BIMASK_NORM_NONE) {
         float2 st[ROWS];
-        row_stats<LAYER>(v, b.ok, p.post == BIMASK_NORM_LAYER, p.eps_post, p.inv_c, g, st);
+        if (lost = !row_stats<LAYER>(v, b.ok, p.post == BIMASK_NORM_LAYER, p.eps_post, p.inv_c, g, st); lost) break;
 #pragma unroll
         for (int r = 0; r < ROWS; ++r) {
           if (p.stats_post != nullptr && b.at[0] == 0 && live[r]) p.stats_post[work.t + r] = st[r];
@@ -696,7 +765,7 @@ residual_fwd_kernel(const __grid_constant__ ResidualParams p) {
         if (!b.ok[j])                                     // whatever came of the zeros there (a bias, an infinite statistic) stays out
 #pragma unroll
           for (int r = 0; r < ROWS; ++r) fill8(v[r][j], 0.f);
-      row_stats<LAYER>(v, b.ok, p.pre == BIMASK_NORM_LAYER, p.eps_pre, p.inv_c, g, st);
+      if (lost = !row_stats<LAYER>(v, b.ok, p.pre == BIMASK_NORM_LAYER, p.eps_pre, p.inv_c, g, st); lost) break;
 #pragma unroll
       for (int r = 0; r < ROWS; ++r) {
         if (p.stats_pre != nullptr && b.at[0] == 0 && live[r]) p.stats_pre[work.t + r] = st[r];
@@ -715,7 +784,23 @@ residual_fwd_kernel(const __grid_constant__ ResidualParams p) {
     stage ^= 1u;
   }
   copies_wait<0>();
-  if (CLUSTER) ptx::cluster_sync();                       // shared memory outlives the peers' writes to it
+  if (CLUSTER && lost) {                                  // the rows that are left
+    Pair nan[4];
+    fill8(nan, NAN);
+    for (; work.more(p); work.next(p, stride))
+      for (int r = 0; r < ROWS && work.t + r < work.end; ++r) {
+        for (int j = 0; j < VECS; ++j) {
+          const long long at = (long long)(work.t + r) * p.C8 + b.at[j];
+          if (b.ok[j] && p.xo != nullptr) store8<F32>(p.xo, at, nan);
+          if (b.ok[j] && p.pre != BIMASK_NORM_NONE) store8<false>(p.n, at, nan);
+        }
+        if (p.stats_post != nullptr && b.at[0] == 0) p.stats_post[work.t + r] = make_float2(NAN, NAN);
+        if (p.stats_pre != nullptr && b.at[0] == 0) p.stats_pre[work.t + r] = make_float2(NAN, NAN);
+      }
+  }
+  const bool both = p.post != BIMASK_NORM_NONE && p.pre != BIMASK_NORM_NONE;
+  auto values = [](int norm) { return LAYER && norm == BIMASK_NORM_LAYER ? 2 * ROWS : ROWS; };
+  g.finish(lost, values(both ? p.post : p.post + p.pre), values(both ? p.pre : p.post + p.pre));        // a row's norms in turn
 }
 
 // ------------------------------------------------------------------------------------------
@@ -806,6 +891,14 @@ residual_bwd_kernel(const __grid_constant__ ResidualParams p) {
     fill8(sum_g2[j], 0.f);
     fill8(fsum[j], 0.f);
   }
+  auto leave_unit = [&]() {
+#pragma unroll
+    for (int j = 0; j < VECS; ++j) {
+      if (!b.ok[j]) continue;
+      if (p.gate_sums != nullptr) store8<true>(p.gate_sums, (long long)work.unit * p.C8 + b.at[j], fsum[j]);
+      else store8<false>(p.dgate, (long long)work.unit * p.gate_pitch8 + b.at[j], fsum[j]);
+    }
+  };
   fetch(ahead, 0);
   // the parameters of this thread's columns, w_pre and scale w_post: from its own pieces after the ring, or from memory
   const uint32_t kept = ring + ring_bytes(ROWS, THREADS, SLOTS);
@@ -846,6 +939,7 @@ residual_bwd_kernel(const __grid_constant__ ResidualParams p) {
     }
   }
   uint32_t stage = 0;
+  bool lost = false;                                      // this warp has given up
   while (work.more(p)) {
     __syncwarp();                                         // every lane has read the statistics and pieces that are overwritten now
     ahead.next(p, stride);
@@ -952,7 +1046,7 @@ residual_bwd_kernel(const __grid_constant__ ResidualParams p) {
         }
       }
     }
-    row_totals(g, c);
+    if (lost = !row_totals(g, c); lost) break;
     const Pair alpha = act::both(p.alpha);
 #pragma unroll
     for (int r = 0; r < ROWS; ++r) {
@@ -1018,19 +1112,35 @@ residual_bwd_kernel(const __grid_constant__ ResidualParams p) {
       }
     }
     if (GATE == 2 && work.last()) {
+      leave_unit();
 #pragma unroll
-      for (int j = 0; j < VECS; ++j) {
-        if (b.ok[j]) {
-          if (p.gate_sums != nullptr) store8<true>(p.gate_sums, (long long)work.unit * p.C8 + b.at[j], fsum[j]);
-          else store8<false>(p.dgate, (long long)work.unit * p.gate_pitch8 + b.at[j], fsum[j]);
-        }
-        fill8(fsum[j], 0.f);
-      }
+      for (int j = 0; j < VECS; ++j) fill8(fsum[j], 0.f);
     }
     work.next(p, stride);
     stage ^= 1u;
   }
   copies_wait<0>();
+  if (CLUSTER && lost) {                                  // the rows that are left
+    Pair nan[4];
+    fill8(nan, NAN);
+    for (int j = 0; j < VECS; ++j) {
+      fill8(sum_a[j], NAN);
+      fill8(sum_g1[j], NAN);
+      fill8(sum_b[j], NAN);
+      fill8(sum_g2[j], NAN);
+      fill8(fsum[j], NAN);
+    }
+    for (; work.more(p); work.next(p, stride)) {
+      for (int r = 0; r < ROWS && work.t + r < work.end; ++r)
+        for (int j = 0; j < VECS; ++j) {
+          const long long at = (long long)(work.t + r) * p.C8 + b.at[j];
+          if (b.ok[j] && p.dx != nullptr) store8<F32>(p.dx, at, nan);
+          if (b.ok[j] && p.dy != nullptr) store8<false>(p.dy, at, nan);
+          if (GATE == 1 && b.ok[j] && p.dgate != nullptr) store8<false>(p.dgate, (long long)(work.t + r) * p.gate_pitch8 + b.at[j], nan);
+        }
+      if (GATE == 2 && work.last()) leave_unit();
+    }
+  }
   // The groups' sums are added through the ring, in their order.
   int slot = 0;
   auto leave = [&](int which, Pair (&sum)[VECS][4]) {
@@ -1093,7 +1203,7 @@ residual_bwd_kernel(const __grid_constant__ ResidualParams p) {
       }
     }
   }
-  if (CLUSTER) ptx::cluster_sync();                       // shared memory outlives the peers' writes to it
+  g.finish(lost, ROWS * NV, ROWS * NV);
 }
 
 // What is left to add up, in one launch.  blockIdx.y below the number of wanted arrays: that array's gradients from the clusters'
@@ -1326,8 +1436,11 @@ int launch_dropout(const void* x, int type, int T, int C, const bimask_dropout_a
   return BIMASK_OK;
 }
 
-static ResidualParams residual_params(const bimask_residual_args& a) {
+static ResidualParams residual_params(const bimask_residual_args& a, const ResidualGiveUp* give_up) {
   ResidualParams p = {};
+  p.status = a.status_word;
+  p.wait_cycles = give_up != nullptr ? give_up->limit_cycles : CLUSTER_WAIT;
+  p.late = give_up != nullptr && give_up->late_warp >= 0 ? 32u * give_up->late_warp + 8u * give_up->late_meeting : 0xFFFFFFFFu;
   p.T = (uint32_t)a.T;
   p.C8 = (uint32_t)a.C / 8;
   p.post = a.post;
@@ -1359,8 +1472,8 @@ static ResidualParams residual_params(const bimask_residual_args& a) {
   return p;
 }
 
-int launch_residual_fwd(const bimask_residual_args& a, cudaStream_t s) {
-  ResidualParams p = residual_params(a);
+int launch_residual_fwd(const bimask_residual_args& a, cudaStream_t s, const ResidualGiveUp* give_up) {
+  ResidualParams p = residual_params(a, give_up);
   const RowPlan b = plan_rows(ROWS, FWD_THREADS, a.T, a.C, 1, sm_count());
   take_plan(p, b);
   using Yes = std::true_type;
@@ -1381,8 +1494,8 @@ int launch_residual_fwd(const bimask_residual_args& a, cudaStream_t s) {
   return BIMASK_OK;
 }
 
-int launch_residual_bwd(const bimask_residual_args& a, cudaStream_t s) {
-  ResidualParams p = residual_params(a);
+int launch_residual_bwd(const bimask_residual_args& a, cudaStream_t s, const ResidualGiveUp* give_up) {
+  ResidualParams p = residual_params(a, give_up);
   const bool spanned = a.dgate != nullptr && p.gate_span > 1;
   const bool branch = a.dy || a.dgate || a.dscale || a.dw_post || a.db_post, post = branch && a.post != BIMASK_NORM_NONE;
   p.has = (a.pre != BIMASK_NORM_NONE ? HAS_PRE : 0) | (a.dxo ? HAS_DXO : 0) | (branch && a.y ? HAS_Y : 0) | (post ? HAS_POST : 0);

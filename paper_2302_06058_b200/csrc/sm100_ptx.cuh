@@ -352,7 +352,6 @@ __device__ __forceinline__ float4 ld_cluster_v4(uint32_t addr) {
 __device__ __forceinline__ void mbar_arrive_cluster(uint32_t bar_cluster_addr) {
   asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar_cluster_addr) : "memory");
 }
-// Named barrier among `nthreads` threads of the CTA (id 1..15; 0 is __syncthreads).
 // A word into a peer's shared memory, counted by the peer's mbarrier when it is there.
 __device__ __forceinline__ void st_async_u32(uint32_t cluster_addr, uint32_t v, uint32_t cluster_bar) {
   asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.u32 [%0], %1, [%2];" ::"r"(cluster_addr), "r"(v), "r"(cluster_bar) : "memory");
@@ -374,6 +373,7 @@ __device__ __forceinline__ bool mbar_wait_cluster(uint32_t bar, uint32_t parity,
     else if ((spins & 63u) == 0u && clock64() - t0 > budget_cycles) return false;
   }
 }
+// Named barrier among `nthreads` threads of the CTA (id 1..15; 0 is __syncthreads).
 __device__ __forceinline__ void named_bar_sync(uint32_t id, uint32_t nthreads) {
   asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(nthreads) : "memory");
 }

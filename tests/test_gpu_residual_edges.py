@@ -23,3 +23,53 @@ def test_the_scaled_stream_is_a_product_of_its_own(T, C, stream, alpha):
     want = (q.d["x"].float() * q.alpha + q.d["y"].float()).to(q.dt)
     assert torch.equal(f["xo"], want)
     q.check_forward(f)
+
+
+@pytest.mark.parametrize("T,C", [(1, 8224), (2, 16384), (150, 12288), (230, 8224), (400, 16384)])
+@pytest.mark.parametrize("stream", TYPES)
+@pytest.mark.parametrize("post,pre,span", [(1, 1, 0), (2, 2, 1), (0, 2, 7), (1, 0, 0)])
+def test_a_wait_of_a_cluster_that_runs_out(T, C, stream, post, pre, span):
+    """A warp of every row gives up, at its first meeting or a later one; the others run out of time (a millisecond) one after the other.
+    The call ends and reports it, every result is NaN or what it is otherwise, and the next call is as if nothing had been."""
+    q = Problem(T, C, post, pre, stream, span=span, p=0.1)
+    f = q.forward()
+    g = q.backward(f)
+    q.check_forward(f)
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+
+    def either(got, want, where):
+        """Whether there are NaN in `got`, where it may not differ from `want` in another way."""
+        lost = False
+        for k in want:
+            if k != "ws":
+                nan = torch.isnan(got[k])
+                assert bool((nan | (got[k] == want[k])).all()), (k, where)
+                lost |= bool(nan.any())
+        return lost
+
+    def run(backward, *limits):
+        """Results of a pass; with limits: of one with a wait that ends early, reported in `status`."""
+        out = q.gradients() if backward else q.outputs()
+        bufs = {**q.d, **out, "status_word": status}
+        if backward:
+            bufs.update({k: f[k] for k in ("xo", "stats_post", "stats_pre") if k in f})
+        else:
+            bufs.pop("dxo"), bufs.pop("dn")
+        a = q.args({k: v for k, v in bufs.items() if backward or k[0] != "d"})
+        status.zero_()
+        if limits:
+            bm.bimask_debug_residual_give_up(a, backward, *limits)
+        else:
+            (bm.bimask_residual_norm_bwd if backward else bm.bimask_residual_norm_fwd)(a)
+        torch.cuda.synchronize()
+        return out
+
+    for backward, want in ((False, f), (True, g)):
+        for limits in ((2000000, 0, 0), (2000000, 9, 0), (1000000, 4, 1), (1000000, 11, 2), (1000000, 0, 1)):
+            lost = either(run(backward, *limits), want, limits)
+            assert lost == (int(status.item()) == bm.binding.BIMASK_ETIMEOUT) and (lost or limits[2] > 0), limits
+        for limits in ((0,), (200,), (1 << 31, -1, 3)):          # whoever is late by itself; nobody
+            lost = either(run(backward, *limits), want, limits)
+            assert int(status.item()) != 0 if lost else limits[0] <= 200 or int(status.item()) == 0, limits
+            assert not (lost and limits[0] > 200), limits
+        assert not either(run(backward), want, None) and int(status.item()) == 0
