@@ -293,7 +293,7 @@ int bimask_act_dropout_bwd(const uint16_t* dY, const int8_t* Zq, const uint8_t* 
  *            once), dscale, dw_post, db_post, dw_pre, db_pre (fp32, added in an order that depends on the sizes, the types, the norms
  *            and the gate's span, and with gate_span > 1 on whether dgate is wanted).
  *            With y absent in the forward pass only dx, dw_pre and db_pre are asked for (xo: alpha x).  Where an element was dropped
- *            its gradient is 0 times that of x'.
+ *            its gradient is 0 times that of x', and it counts as 0 in those of gate and scale, whatever it was.
  *            ws: bimask_residual_norm_workspace_bytes(T, C, gate_span, or 1 without a gate) bytes, needed for gradients of vectors
  *            and of a gate with gate_span > 1; nothing is expected in it, and calls that may overlap need one each.  Never
  *            fewer for more tokens.

@@ -73,3 +73,23 @@ def test_a_wait_of_a_cluster_that_runs_out(T, C, stream, post, pre, span):
             assert int(status.item()) != 0 if lost else limits[0] <= 200 or int(status.item()) == 0, limits
             assert not (lost and limits[0] > 200), limits
         assert not either(run(backward), want, None) and int(status.item()) == 0
+
+
+@pytest.mark.parametrize("T,C,spans", [(45, 288, (0, 1, 9, 45, 50)), (700, 384, (0, 1, 197)), (37, 1152, (0, 1, 5)), (6, 5120, (0, 1, 4)), (5, 16384, (0, 1, 2))])
+@pytest.mark.parametrize("stream", TYPES)
+def test_a_dropped_element_counts_as_zero_in_every_gradient(T, C, spans, stream):
+    """Whatever a dropped element of y was, the gradients are bit for bit those with a zero in its place, as the results are."""
+    for span in spans:
+        for pre in (0, 1, 2):
+            q = Problem(T, C, 0, pre, stream, span=span, p=0.3)
+            dropped = torch.from_numpy(q.m == 0).cuda()
+            zeros = q.d["y"].masked_fill(dropped, 0.0)
+            odd = torch.tensor([float("inf"), float("nan"), -float("inf"), 3e38], device="cuda", dtype=torch.bfloat16).repeat(T * C // 4).view(T, C)
+            seen = []
+            for y in (zeros, torch.where(dropped, odd, zeros)):
+                q.d["y"] = y
+                f = q.forward()
+                seen.append({**f, **q.backward(f)})
+            for k in seen[0]:
+                if k != "ws":
+                    assert bool(torch.isfinite(seen[1][k]).all()) and torch.equal(seen[0][k], seen[1][k]), (k, span, pre)
