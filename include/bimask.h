@@ -289,8 +289,8 @@ int bimask_act_dropout_bwd(const uint16_t* dY, const int8_t* Zq, const uint8_t* 
  *            before; may be y), stats_post, stats_pre (may be NULL).
  * Backward.  in: dxo, the gradient of x' from its other uses (NULL: zero), dn; xo, stats_pre with a norm before, stats_post with a
  *            norm after, gate, scale, w_*, b_post, drop as in the forward pass; y with a norm after, dgate or dscale.
- *            out, each of them NULL where it is not wanted: dx (may be dxo), dy (may be dn or y), dgate (summed over its span, rounded
- *            once), dscale, dw_post, db_post, dw_pre, db_pre (fp32, added in an order that depends on the sizes, the types, the norms
+ *            out, each of them NULL where it is not wanted: dx (may be dxo), dy (may be dn or y), dgate (may be gate; summed over its
+ *            span, rounded once), dscale, dw_post, db_post, dw_pre, db_pre (fp32, added in an order that depends on the sizes, the types, the norms
  *            and the gate's span, and with gate_span > 1 on whether dgate is wanted).
  *            With y absent in the forward pass only dx, dw_pre and db_pre are asked for (xo: alpha x).  Where an element was dropped
  *            its gradient is 0 times that of x', and it counts as 0 in those of gate and scale, whatever it was.

@@ -1044,7 +1044,7 @@ residual_bwd_kernel(const __grid_constant__ ResidualParams p) {
           if (GATE != 0) {
             Pair gt[4];
             if (GATE_RING) read_block<false>(piece<SLOTS, PITCH>(at, r, j, G), 0, gt);
-            else unpack8<false>(Vec8<false>{__ldg(gate_row(min(work.t + r, p.T - 1u)) + b.safe[j])}, gt);
+            else unpack8<false>(Vec8<false>{gate_row(min(work.t + r, p.T - 1u))[b.safe[j]]}, gt);
             times8(z, gt);
           }
           if (WIDE) {
@@ -1107,6 +1107,13 @@ residual_bwd_kernel(const __grid_constant__ ResidualParams p) {
         if (p.dx != nullptr && there) store8<F32>(p.dx, (long long)(row[r] + b.at[j]), o);
         times8(E[r][j], m[r][j]);
         if (GATE != 0) {
+          Pair gt[4];
+          auto read_gate = [&]() {
+            if (GATE_RING) read_block<false>(piece<SLOTS, PITCH>(at, r, j, G), 0, gt);
+            else unpack8<false>(Vec8<false>{gate_row(min(work.t + r, p.T - 1u))[b.safe[j]]}, gt);
+          };
+          constexpr bool EARLY = !GATE_RING && GATE == 1;  // from memory, where its gradient may take its place
+          if (EARLY) read_gate();
           if (GATE == 2 || p.dgate != nullptr) {          // scale u
             Pair u[4];
 #pragma unroll
@@ -1129,9 +1136,7 @@ residual_bwd_kernel(const __grid_constant__ ResidualParams p) {
               if (there) store8<false>(p.dgate, (long long)(work.t + r) * p.gate_pitch8 + b.at[j], u);
             }
           }
-          Pair gt[4];
-          if (GATE_RING) read_block<false>(piece<SLOTS, PITCH>(at, r, j, G), 0, gt);
-          else unpack8<false>(Vec8<false>{__ldg(gate_row(min(work.t + r, p.T - 1u)) + b.safe[j])}, gt);
+          if (!EARLY) read_gate();
           times8(E[r][j], gt);
         }
 #pragma unroll

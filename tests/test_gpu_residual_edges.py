@@ -93,3 +93,17 @@ def test_a_dropped_element_counts_as_zero_in_every_gradient(T, C, spans, stream)
             for k in seen[0]:
                 if k != "ws":
                     assert bool(torch.isfinite(seen[1][k]).all()) and torch.equal(seen[0][k], seen[1][k]), (k, span, pre)
+
+
+@pytest.mark.parametrize("T,C,pitch", [(50, 320, None), (23, 160, 480), (700, 1152, None), (301, 4096, None), (5, 8192, 16384), (9, 16384, None)])
+@pytest.mark.parametrize("stream", TYPES)
+def test_the_gradient_of_a_gate_in_its_place(T, C, pitch, stream):
+    for post, pre, span in ((1, 1, 1), (0, 2, 1), (2, 2, 1), (0, 1, 3), (1, 0, T)):
+        q = Problem(T, C, post, pre, stream, span=span, p=0.1, pitch=pitch)
+        f = q.forward()
+        g = q.backward(f)
+        q.check_backward(g, f)
+        if pitch:
+            q.d["gate"] = q.wide.clone()[:, :C]
+        i = q.backward(f, dgate=q.d["gate"])
+        assert all(torch.equal(i[k], g[k]) for k in g if k != "ws"), (post, pre, span)
