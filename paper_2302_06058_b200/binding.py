@@ -302,9 +302,16 @@ NORM_NONE, NORM_RMS, NORM_LAYER = 0, 1, 2
 
 
 def make_dropout(p, seed, stream_no=0, counter=None) -> Dropout:
-    """Probability, seed and stream number of a dropout; counter: one-element int64 CUDA tensor that is added to the stream
-    number when the kernel runs."""
-    return Dropout(p, seed, stream_no, _ptr(counter))
+    """Probability, seed and stream number of a dropout; counter: one-element int64 CUDA tensor (or an address) that is added to the
+    stream number when the kernel runs.  The result, and the arguments of a junction made with it, keep the tensor alive."""
+    if isinstance(counter, torch.Tensor):
+        if counter.numel() != 1 or counter.dtype not in (torch.int64, torch.uint64):
+            raise ValueError("counter must be one element of int64")
+        if not (counter.is_cuda or counter.is_pinned()):
+            raise ValueError("counter must be on the device")
+    drop = Dropout(p, seed, stream_no, _ptr(counter))
+    drop.held = counter
+    return drop
 
 
 def bimask_dropout(X, type, T, C, drop, Y, stream=None):
@@ -358,8 +365,11 @@ def make_residual_args(T, C, bufs: dict, stream_type=TYPE_BF16, post=NORM_NONE, 
     ws = get("ws")
     ws_bytes = ws.numel() * ws.element_size() if type(ws) is _Tensor else int(get("ws_bytes", 0))
     p, seed, stream_no, counter = (0.0, 0, 0, 0) if drop is None else (drop.p, drop.seed, drop.stream_no, drop.counter or 0)
-    return ResidualArgs.from_buffer_copy(_RESIDUAL_PACK(T, C, stream_type, post, pre, gate_span, pitch, eps_post, eps_pre, alpha, p, seed,
+    args = ResidualArgs.from_buffer_copy(_RESIDUAL_PACK(T, C, stream_type, post, pre, gate_span, pitch, eps_post, eps_pre, alpha, p, seed,
                                                         stream_no, counter, *pointers, ws_bytes, _ptr(get("status_word")) or 0))
+    if counter:
+        args.held = getattr(drop, "held", None)
+    return args
 
 
 def bimask_residual_norm_fwd(args: ResidualArgs, stream=None):

@@ -107,3 +107,19 @@ def test_the_gradient_of_a_gate_in_its_place(T, C, pitch, stream):
             q.d["gate"] = q.wide.clone()[:, :C]
         i = q.backward(f, dgate=q.d["gate"])
         assert all(torch.equal(i[k], g[k]) for k in g if k != "ws"), (post, pre, span)
+
+
+def test_a_counter_lives_as_long_as_what_was_made_with_it():
+    """A counter that nobody else holds, and tensors made after it that would take its place."""
+    x = torch.ones(64, 64, device="cuda", dtype=torch.bfloat16)
+    y, want = torch.empty_like(x), torch.empty_like(x)
+    bm.bimask_dropout(x, bm.TYPE_BF16, 64, 64, bm.make_dropout(0.5, 3, 12), want)
+    drop = bm.make_dropout(0.5, 3, 5, torch.full((1,), 7, dtype=torch.int64, device="cuda"))
+    others = [torch.full((1,), 1000 + i, dtype=torch.int64, device="cuda") for i in range(8)]
+    bm.bimask_dropout(x, bm.TYPE_BF16, 64, 64, drop, y)
+    assert torch.equal(y, want)
+    bufs = {"x": torch.zeros_like(x), "y": x, "xo": y}
+    args = bm.make_residual_args(64, 64, bufs, drop=bm.make_dropout(0.5, 3, 5, torch.full((1,), 7, dtype=torch.int64, device="cuda")))
+    others += [torch.full((1,), 2000 + i, dtype=torch.int64, device="cuda") for i in range(8)]
+    bm.bimask_residual_norm_fwd(args)
+    assert torch.equal(y, want) and len(others) == 16

@@ -27,3 +27,13 @@ def test_status_word_and_limits_of_the_debug_helper(bm):
             assert L.bimask_debug_residual_give_up(good, backward, *limits, None) == inval and "out of range" in bm.bimask_last_error()
     assert L.bimask_debug_residual_give_up(None, 0, 0, -1, 0, None) == inval
     assert bm.bimask_launch_count() == n0
+
+
+def test_a_counter_is_one_64_bit_number_on_the_device(bm):
+    """Another type would be read as eight bytes of something else, host memory faults when the kernel runs."""
+    for bad in (torch.zeros(1, dtype=torch.int32), torch.zeros(1), torch.zeros(2, dtype=torch.int64), torch.zeros(0, dtype=torch.int64)):
+        with pytest.raises(ValueError, match="counter"):
+            bm.make_dropout(0.1, 1, 0, bad)
+    with pytest.raises(ValueError, match="device"):
+        bm.make_dropout(0.1, 1, 0, torch.zeros(1, dtype=torch.int64))
+    assert bm.make_dropout(0.1, 1, 0, 4096).counter == 4096 and bm.make_dropout(0.1, 1).counter is None
