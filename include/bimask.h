@@ -277,7 +277,8 @@ int bimask_act_dropout_bwd(const uint16_t* dY, const int8_t* Zq, const uint8_t* 
  * Every part but x may be absent: y == NULL leaves the norm of alpha x alone (the first block's input), norm NONE leaves its
  * norm out, gate / scale / w / b == NULL stand for 1, 1, 1 and 0, drop.p == 0 for no dropout, alpha is 1 for a plain residual.
  * All arithmetic is fp32 (alpha x a product of its own), results are rounded once; n is taken from x' before its rounding.
- * Squares are fp32: a row with magnitudes above 1e18 may overflow them.
+ * Squares are fp32: a norm's rows may have magnitudes up to 1e18 (above it they may overflow), and with eps == 0 they need a deviation
+ * (RMS: a root mean square) of 1e-18 at least, below which 1 / it may be infinite.
  *
  * Sizes: C % 32 == 0, C <= 16384 (BIMASK_EUNSUPPORTED above), any T.  T x C matrices of the stream (x, xo, dx, dxo) have
  * stream_type; y, n, gate and their gradients are bf16; C-vectors are fp32.  stats: T x 2 fp32 (mean, rstd; mean 0 for RMS),

@@ -430,7 +430,8 @@ __device__ __forceinline__ float rsqrt_fast(float x) {
 
 // Mean and 1 / deviation of two rows (LAYER: some norm of this kernel subtracts means; `layer`: this one does).  The squares are taken
 // about each warp's own mean, and the warps are put together by M = sum M_w + sum n_w (m_w - m)^2: one exchange, and no difference
-// of large squares.  rms: all about zero.  False if the rows' other CTAs did not come.
+// of large squares.  rms: all about zero.  Divided by the columns before they leave a thread, the squares fit fp32 at any width (up to
+// 1e18: 16 squares of a difference are 6e37).  False if the rows' other CTAs did not come.
 template <bool LAYER, int THREADS, bool CLUSTER>
 __device__ __forceinline__ bool row_stats(const Pair (&v)[ROWS][VECS][4], const bool (&ok)[VECS], bool layer, float eps, float inv_c,
                                           Group<4, THREADS, CLUSTER>& g, float2 (&st)[ROWS]) {
@@ -458,6 +459,8 @@ __device__ __forceinline__ bool row_stats(const Pair (&v)[ROWS][VECS][4], const 
 #pragma unroll
     for (int r = 0; r < ROWS; ++r) q[r] = horizontal(act::add2(dot8(v[r][0], v[r][0]), dot8(v[r][1], v[r][1])));
   }
+#pragma unroll
+  for (int r = 0; r < ROWS; ++r) q[r] *= inv_c;
   float sq = fold<2>(q, g.lane);
   if (!g.alone) {
     if ((g.lane & 15) == 0) {
@@ -485,13 +488,13 @@ __device__ __forceinline__ bool row_stats(const Pair (&v)[ROWS][VECS][4], const 
       for (int d = SPREAD; d >= 1; d >>= 1) m += __shfl_xor_sync(0xFFFFFFFFu, m, d);
       m *= inv_c;
 #pragma unroll
-      for (int k = 0; k < EACH; ++k) sq = fmaf(g.peer_columns[k] * (own[k] - m), own[k] - m, sq);
+      for (int k = 0; k < EACH; ++k) sq = fmaf(g.peer_columns[k] * inv_c * (own[k] - m), own[k] - m, sq);
     }
 #pragma unroll
     for (int d = SPREAD; d >= 1; d >>= 1) sq += __shfl_xor_sync(0xFFFFFFFFu, sq, d);
     g.turn();
   }
-  const float rstd = rsqrt_fast(fmaf(sq, inv_c, eps));
+  const float rstd = rsqrt_fast(sq + eps);
 #pragma unroll
   for (int r = 0; r < ROWS; ++r)
     st[r] = make_float2(LAYER && layer ? __shfl_sync(0xFFFFFFFFu, m, 16 * r) : 0.f, __shfl_sync(0xFFFFFFFFu, rstd, 16 * r));

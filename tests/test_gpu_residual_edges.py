@@ -123,3 +123,21 @@ def test_a_counter_lives_as_long_as_what_was_made_with_it():
     others += [torch.full((1,), 2000 + i, dtype=torch.int64, device="cuda") for i in range(8)]
     bm.bimask_residual_norm_fwd(args)
     assert torch.equal(y, want) and len(others) == 16
+
+
+@pytest.mark.parametrize("T,C", [(5, 32), (3, 384), (4, 4096), (3, 5120), (3, 16384)])
+@pytest.mark.parametrize("stream", TYPES)
+@pytest.mark.parametrize("size,eps", [(1e18, 1e-5), (2e-18, 0.0)])
+def test_rows_at_the_ends_of_the_range(T, C, stream, size, eps, monkeypatch):
+    """Rows of which every value is within a factor of two of the largest magnitude that the norms take, and of the smallest with eps 0."""
+    monkeypatch.setattr(R, "EPS", (eps, eps))
+    rng = np.random.default_rng(C)
+    for post, pre in ((0, 1), (0, 2), (1, 1), (2, 2), (1, 0)):
+        q = Problem(T, C, post, pre, stream, scale=False)
+        for k, s in (("x", 0.7 if post == 0 else 1.0), ("y", 0.3 if post == 0 else 1.0)):
+            v = torch.from_numpy(rng.uniform(0.5, 1.0, (T, C)) * rng.choice((-1.0, 1.0), (T, C)) * size * s)
+            t = (v * 0.99).float().to(q.d[k].dtype)                        # 0.99: a rounding up stays in the range
+            q.d[k], q.h[k] = t.cuda(), t.double().numpy()
+        f = q.forward()
+        q.check_forward(f)
+        q.check_backward(q.backward(f), f)
