@@ -512,6 +512,10 @@ int bimask_debug_wait_probe(int32_t* status_word, void* stream);
 int bimask_debug_residual_give_up(const bimask_residual_args* args, int backward, int64_t limit_cycles, int late_warp, int late_meeting,
                                   void* stream);
 
+/* Debug helper, host only: how often the library has set a kernel's shared-memory limit since it was loaded (once per kernel that
+ * needs one, and device). */
+uint64_t bimask_debug_limits_set(void);
+
 /* Debug helper, host only: how bimask_linear_fwd runs a layer of this size (dense: hw_meta_f == NULL).  HOST array out[4] =
  * {kernel: 0 few tokens, 1 one row tile, 2 CTA pairs, 3 CTA pairs with two row tiles each; CTAs that share a tile's
  * reduction; tiles of 128 rows x 128 tokens; clusters of that many CTAs that the device holds at once}. */

@@ -27,7 +27,8 @@ EXPORTS = ("bimask_last_error", "bimask_launch_count", "bimask_hw_meta_bytes", "
            "bimask_debug_linear_plan",
            "bimask_linear_workspace_bytes", "bimask_linear_fwd", "bimask_act_bwd", "bimask_ckpt_pack", "bimask_ckpt_unpack",
            "bimask_wgrad_ckpt", "bimask_dropout", "bimask_ckpt_unpack_dropout", "bimask_act_dropout_bwd",
-           "bimask_residual_norm_workspace_bytes", "bimask_residual_norm_fwd", "bimask_residual_norm_bwd", "bimask_debug_residual_give_up")
+           "bimask_residual_norm_workspace_bytes", "bimask_residual_norm_fwd", "bimask_residual_norm_bwd", "bimask_debug_residual_give_up",
+           "bimask_debug_limits_set")
 
 
 class BimaskError(RuntimeError):
@@ -96,6 +97,7 @@ def lib() -> ctypes.CDLL:
         L = ctypes.CDLL(LIB_PATH)
         L.bimask_last_error.restype = c_char_p
         L.bimask_launch_count.restype = c_uint64
+        L.bimask_debug_limits_set.restype = c_uint64
         L.bimask_hw_meta_bytes.restype = c_size_t
         L.bimask_hw_meta_bytes.argtypes = [c_int, c_int]
         L.bimask_workspace_bytes.restype = c_size_t
@@ -154,7 +156,7 @@ def lib() -> ctypes.CDLL:
                                                 c_void_p, c_void_p, c_void_p, c_void_p]
         L.bimask_perm_search_static_max_entries.restype = c_size_t
         for name in EXPORTS:
-            if name not in ("bimask_last_error", "bimask_launch_count", "bimask_hw_meta_bytes", "bimask_workspace_bytes",
+            if name not in ("bimask_last_error", "bimask_launch_count", "bimask_debug_limits_set", "bimask_hw_meta_bytes", "bimask_workspace_bytes",
                             "bimask_perm_search_static_max_entries", "bimask_conv_workspace_bytes",
                             "bimask_refine_workspace_bytes", "bimask_linear_workspace_bytes",
                             "bimask_residual_norm_workspace_bytes"):
@@ -201,6 +203,10 @@ def _check(rc: int) -> int:
 
 def bimask_last_error() -> str:
     return lib().bimask_last_error().decode()
+
+
+def bimask_debug_limits_set() -> int:
+    return int(lib().bimask_debug_limits_set())
 
 
 def bimask_launch_count() -> int:

@@ -8,8 +8,9 @@
 namespace bimask {
 
 static thread_local char g_err[512] = "";
-static std::atomic<unsigned long long> g_launches{0};
+static std::atomic<unsigned long long> g_launches{0}, g_limits{0};
 
+void count_limit_set() { g_limits.fetch_add(1, std::memory_order_relaxed); }
 void count_launch(int n) { g_launches.fetch_add((unsigned long long)n, std::memory_order_relaxed); }
 
 void set_error(const char* fmt, ...) {
@@ -990,6 +991,8 @@ int bimask_debug_wait_probe(int32_t* status_word, void* stream) {
   BIMASK_REQUIRE(status_word != nullptr, BIMASK_EINVAL, "bimask_debug_wait_probe: null pointer");
   return launch_wait_probe(status_word, (cudaStream_t)stream);
 }
+
+uint64_t bimask_debug_limits_set(void) { return g_limits.load(std::memory_order_relaxed); }
 
 int bimask_debug_linear_plan(int T, int I, int J, int dense, int32_t* out) {
   const int rc = check_gemm(T, I, J);

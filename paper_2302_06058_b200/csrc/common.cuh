@@ -15,6 +15,7 @@ namespace bimask {
 
 void set_error(const char* fmt, ...);       // defined in api.cu
 void count_launch(int n = 1);               // defined in api.cu: kernel launches made so far
+void count_limit_set();                     // defined in api.cu: shared-memory limits set so far
 int cuda_fail(cudaError_t e, const char* what);
 
 #define BIMASK_CUDA_OK(call)                                   \
@@ -113,24 +114,28 @@ namespace bimask {
 
 // The dynamic shared-memory limit of a kernel is set once per (device, kernel): the call costs a microsecond or two
 // on the host, which a layer step of ten short launches would notice.  A kernel is always launched with the same size.
-template <typename K>
+// Kernels of one pointer type share a table, which is entered by a hash of the address (a launch looks at one or two slots):
+// SLOTS, a power of two, has to exceed their number, or the rest would set their limits at every launch.
+template <int SLOTS = 64, typename K>
 inline int set_smem_attr(K kernel, int bytes) {
-  constexpr int SLOTS = 64;
+  static_assert((SLOTS & (SLOTS - 1)) == 0, "a power of two");
   static std::atomic<const void*> done[64][SLOTS];       // [device][slot]; zero-initialised
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) dev = -1;
   const void* key = reinterpret_cast<const void*>(kernel);
+  const unsigned first = (unsigned)((reinterpret_cast<uintptr_t>(key) >> 4) * 0x9E3779B97F4A7C15ull >> 32);
   if (dev >= 0)
-    for (int i = 0; i < SLOTS; ++i) {
-      const void* seen = done[dev][i].load(std::memory_order_acquire);
+    for (unsigned i = 0; i < SLOTS; ++i) {
+      const void* seen = done[dev][(first + i) % SLOTS].load(std::memory_order_acquire);
       if (seen == key) return BIMASK_OK;
       if (seen == nullptr) break;
     }
+  count_limit_set();
   BIMASK_CUDA_OK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes));
   if (dev >= 0)
-    for (int i = 0; i < SLOTS; ++i) {
+    for (unsigned i = 0; i < SLOTS; ++i) {
       const void* expect = nullptr;
-      if (done[dev][i].compare_exchange_strong(expect, key, std::memory_order_acq_rel) || expect == key) break;
+      if (done[dev][(first + i) % SLOTS].compare_exchange_strong(expect, key, std::memory_order_acq_rel) || expect == key) break;
     }
   return BIMASK_OK;
 }

@@ -1402,7 +1402,7 @@ int bwd_rows(const bimask_residual_args& a) {
 
 template <typename K>
 int launch_rows(K kernel, const RowPlan& b, int bytes, cudaStream_t s, const ResidualParams& p) {
-  const int rc = set_smem_attr(kernel, bytes);
+  const int rc = set_smem_attr<256>(kernel, bytes);        // of one type: 16 kernels forward, up to 72 backward
   if (rc != BIMASK_OK) return rc;
   if (b.cluster == 1) BIMASK_CUDA_OK(launch_pdl(kernel, (unsigned)b.slots, b.threads, (size_t)bytes, s, p));
   else BIMASK_CUDA_OK(launch_pdl_cluster(kernel, (unsigned)(b.slots * b.cluster), b.threads, b.cluster, (size_t)bytes, s, p));

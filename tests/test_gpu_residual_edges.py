@@ -141,3 +141,20 @@ def test_rows_at_the_ends_of_the_range(T, C, stream, size, eps, monkeypatch):
         f = q.forward()
         q.check_forward(f)
         q.check_backward(q.backward(f), f)
+
+
+def test_every_form_in_one_process_sets_its_limit_once():
+    """Forward and backward passes in all forms that differ in their kernel: stream, gate, norms with and without means, one row or two
+    per step, clusters.  A second round through them sets no shared-memory limit any more."""
+    def every_form():
+        for stream in TYPES:
+            for T, C in ((9, 256), (9, 1152), (9, 2304), (5, 16384)):
+                for span in (0, 1, 3):
+                    for post, pre, bias in ((0, 1, False), (0, 2, True), (1, 1, False), (2, 2, True), (1, 1, True)):
+                        q = Problem(T, C, post, pre, stream, span=span, bias=bias)
+                        q.backward(q.forward())
+    every_form()
+    n = bm.bimask_debug_limits_set()
+    assert n > 64
+    every_form()
+    assert bm.bimask_debug_limits_set() == n
