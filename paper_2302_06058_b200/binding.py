@@ -364,12 +364,12 @@ def make_residual_args(T, C, bufs: dict, stream_type=TYPE_BF16, post=NORM_NONE, 
     pitch = 0
     for t in (get("gate"), get("dgate")):
         if t is not None:
-            own = C if type(t) is _Tensor and t.is_contiguous() else _row_pitch(t, get("gate_pitch", C))
+            own = C if isinstance(t, _Tensor) and t.is_contiguous() else _row_pitch(t, get("gate_pitch", C))
             if pitch not in (0, own):
                 raise ValueError("gate and dgate must have the same row pitch")
             pitch = own
     ws = get("ws")
-    ws_bytes = ws.numel() * ws.element_size() if type(ws) is _Tensor else int(get("ws_bytes", 0))
+    ws_bytes = ws.numel() * ws.element_size() if isinstance(ws, _Tensor) else int(get("ws_bytes", 0))
     p, seed, stream_no, counter = (0.0, 0, 0, 0) if drop is None else (drop.p, drop.seed, drop.stream_no, drop.counter or 0)
     args = ResidualArgs.from_buffer_copy(_RESIDUAL_PACK(T, C, stream_type, post, pre, gate_span, pitch, eps_post, eps_pre, alpha, p, seed,
                                                         stream_no, counter, *pointers, ws_bytes, _ptr(get("status_word")) or 0))

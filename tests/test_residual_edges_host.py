@@ -37,3 +37,14 @@ def test_a_counter_is_one_64_bit_number_on_the_device(bm):
     with pytest.raises(ValueError, match="device"):
         bm.make_dropout(0.1, 1, 0, torch.zeros(1, dtype=torch.int64))
     assert bm.make_dropout(0.1, 1, 0, 4096).counter == 4096 and bm.make_dropout(0.1, 1).counter is None
+
+
+def test_parameters_are_tensors_like_any_other(bm):
+    """A gate of three dimensions and a workspace that are registered parameters of a module."""
+    def parameter(*shape, dtype=torch.bfloat16):
+        return torch.nn.Parameter(torch.zeros(*shape, dtype=dtype), requires_grad=False)
+
+    gate = parameter(4, 1, 64)
+    a = bm.make_residual_args(4, 64, {"gate": gate, "dgate": gate.detach().clone(), "ws": parameter(1000, dtype=torch.float32)})
+    assert (a.gate_pitch, a.ws_bytes, a.gate) == (64, 4000, gate.data_ptr())
+    assert bm.make_residual_args(4, 64, {"gate": parameter(4, 128).detach()[:, :64]}).gate_pitch == 128
