@@ -310,6 +310,8 @@ NORM_NONE, NORM_RMS, NORM_LAYER = 0, 1, 2
 def make_dropout(p, seed, stream_no=0, counter=None) -> Dropout:
     """Probability, seed and stream number of a dropout; counter: one-element int64 CUDA tensor (or an address) that is added to the
     stream number when the kernel runs.  The result, and the arguments of a junction made with it, keep the tensor alive."""
+    if counter is None:
+        return Dropout(p, seed, stream_no)
     if isinstance(counter, torch.Tensor):
         if counter.numel() != 1 or counter.dtype not in (torch.int64, torch.uint64):
             raise ValueError("counter must be one element of int64")
@@ -368,11 +370,11 @@ def make_residual_args(T, C, bufs: dict, stream_type=TYPE_BF16, post=NORM_NONE, 
             if pitch not in (0, own):
                 raise ValueError("gate and dgate must have the same row pitch")
             pitch = own
-    ws = get("ws")
+    ws, status = get("ws"), get("status_word")
     ws_bytes = ws.numel() * ws.element_size() if isinstance(ws, _Tensor) else int(get("ws_bytes", 0))
     p, seed, stream_no, counter = (0.0, 0, 0, 0) if drop is None else (drop.p, drop.seed, drop.stream_no, drop.counter or 0)
     args = ResidualArgs.from_buffer_copy(_RESIDUAL_PACK(T, C, stream_type, post, pre, gate_span, pitch, eps_post, eps_pre, alpha, p, seed,
-                                                        stream_no, counter, *pointers, ws_bytes, _ptr(get("status_word")) or 0))
+                                                        stream_no, counter, *pointers, ws_bytes, 0 if status is None else _ptr(status)))
     if counter:
         args.held = getattr(drop, "held", None)
     return args
