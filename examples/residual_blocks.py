@@ -73,9 +73,10 @@ class Junction:
         self.xo, self.y = _empty(T, width, dtype=F32), _empty(T, width)
         self.stats_pre, self.stats_post = _empty(T, 2, dtype=F32), _empty(T, 2, dtype=F32)
         self.ws = _empty(bm.bimask_residual_norm_workspace_bytes(T, width), dtype=torch.uint8)
+        self.status_word = torch.zeros(1, dtype=torch.int32, device="cuda")
 
     def _args(self, T, **buffers):
-        b = {**self.params, "stats_pre": self.stats_pre[:T], "xo": self.xo[:T], **buffers}
+        b = {**self.params, "stats_pre": self.stats_pre[:T], "xo": self.xo[:T], "status_word": self.status_word, **buffers}
         if self.join:
             b.update(y=self.y[:T], stats_post=self.stats_post[:T])
         return bm.make_residual_args(T, self.width, b, bm.TYPE_F32, bm.NORM_RMS if self.join else bm.NORM_NONE, bm.NORM_LAYER,
@@ -140,7 +141,8 @@ class Stack:
         self.step.add_(1)
 
     def status(self):
-        return [int(layer.b["status_word"].item()) for block in self.blocks for layer in (block.fc1, block.fc2)]
+        words = [layer.b["status_word"] for block in self.blocks for layer in (block.fc1, block.fc2)]
+        return [int(word.item()) for word in words + [junction.status_word for junction in self.junctions]]
 
 
 def train(tokens=4096, width=1024, hidden=4096, blocks=4, steps=20, dropout=0.1, lr=1.0, search_every=10, seed=0):

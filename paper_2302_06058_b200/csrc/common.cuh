@@ -290,7 +290,7 @@ inline uint32_t drop_threshold(float p) {
   return t > 65535 ? 65535u : (uint32_t)t;
 }
 int launch_dropout(const void* x, int type, int T, int C, const bimask_dropout_args& d, void* y, cudaStream_t s);
-constexpr int RESIDUAL_MAX_C = 16384;                     // 16 warps of eight columns per thread, in each of four CTAs
+constexpr int RESIDUAL_MAX_C = 16384;                     // 32 warps, of a cluster's CTAs together, with 16 columns per thread
 size_t residual_workspace_bytes(int T, int C, int span);
 struct ResidualGiveUp {                                   // of bimask_debug_residual_give_up
   long long limit_cycles;

@@ -1390,7 +1390,10 @@ RowPlan plan_rows(int rows, int threads, int T, int C, int span, int ctas, bool 
 // nine to twelve (5120 columns 122 -> 94, fp32 stream with a layer norm before 196 -> 148).  A gate per token next to a layer norm leaves
 // two rows too few of 255 registers, one row enough of 168 (1024 columns 116 -> 98, 4096 132 -> 104).  Not with a norm after and means:
 // eight values per row, of which 168 registers spill (5120 columns 130 -> 145); nor for short rows of an fp32 stream with means and no
-// gate (1152 columns 118 -> 133).  Which gradients are wanted plays no part: one alone is added up as it is among the others.
+// gate (1152 columns 118 -> 133).  Which gradients are wanted plays no part: one alone is added up as it is among the others.  So RMS norms
+// with biases, whose gradients need the eight values, too, go by their widths like those without.  With a gate that is the faster side
+// (two rows and one, gate per token 2560 columns 221 -> 192, 6144 179 -> 175; per 197 tokens 282 -> 232, 245 -> 207), without one it is up to
+// 2560 columns (144 -> 139; fp32 stream 174 -> 179), not above (5120 136 -> 148, 6144 118 -> 139).
 int bwd_rows(const bimask_residual_args& a) {
   const int all = (a.C / 8 + 32 * VECS - 1) / (32 * VECS);
   const bool f32 = a.stream_type == BIMASK_TYPE_F32, means = a.post == BIMASK_NORM_LAYER || a.pre == BIMASK_NORM_LAYER;

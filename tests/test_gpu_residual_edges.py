@@ -145,7 +145,7 @@ def test_rows_at_the_ends_of_the_range(T, C, stream, size, eps, monkeypatch):
 
 def test_every_form_in_one_process_sets_its_limit_once():
     """Forward and backward passes in all forms that differ in their kernel: stream, gate, norms with and without means, one row or two
-    per step, clusters.  A second round through them sets no shared-memory limit any more."""
+    per step, clusters.  Going through them again sets no shared-memory limit any more."""
     def every_form():
         for stream in TYPES:
             for T, C in ((9, 256), (9, 1152), (9, 2304), (5, 16384)):
