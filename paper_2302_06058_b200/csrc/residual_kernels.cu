@@ -153,7 +153,7 @@ struct ResidualParams {
   uint4* dy;
   uint4* dgate;
   float* sums;                       // [clusters][wanted arrays][C]; null: one cluster takes all rows and leaves the gradients themselves
-  float* gate_sums;                  // [units][C]; null: a unit is a whole span, and leaves its row of dgate
+  float* gate_sums;                  // [units][C]; null: units are whole spans and leave their rows of dgate
   int want;                          // bits: SUM_* arrays that are wanted
   float* dscale;
   float* dw_post;
@@ -873,6 +873,9 @@ residual_bwd_kernel(const __grid_constant__ ResidualParams p) {
   const bool dropped = p.drop.thr != 0u && (p.has & HAS_Y) != 0;
   const bool layer_pre = WIDE && p.pre == BIMASK_NORM_LAYER, layer_post = WIDE && POST && p.post == BIMASK_NORM_LAYER;
   auto gate_row = [&](uint32_t t) { return p.gate + (long long)(p.gate_span == 1u ? t : t / p.gate_span) * p.gate_pitch8; };
+  // A gate's block from memory.  Its gradient may take its place: per token while others still read their rows, with spans not before the
+  // kernel is over (launch_residual_bwd), so that the loads may pass the stores (8192 x 4096, norm before, 124 us, so 116).
+  auto gate_block = [&](uint32_t t, int j) { return GATE == 2 ? __ldg(gate_row(t) + b.safe[j]) : gate_row(t)[b.safe[j]]; };
   auto fetch = [&](const Walk<ROWS, GATE == 2>& w, uint32_t stage) {
     const bool more = w.more(p);
     const uint32_t at = ring + stage * STAGE, slot0 = smem_addr(smem) + stage * STAGE;
@@ -1047,7 +1050,7 @@ residual_bwd_kernel(const __grid_constant__ ResidualParams p) {
           if (GATE != 0) {
             Pair gt[4];
             if (GATE_RING) read_block<false>(piece<SLOTS, PITCH>(at, r, j, G), 0, gt);
-            else unpack8<false>(Vec8<false>{gate_row(min(work.t + r, p.T - 1u))[b.safe[j]]}, gt);
+            else unpack8<false>(Vec8<false>{gate_block(min(work.t + r, p.T - 1u), j)}, gt);
             times8(z, gt);
           }
           if (WIDE) {
@@ -1073,8 +1076,9 @@ residual_bwd_kernel(const __grid_constant__ ResidualParams p) {
       }
     }
     // What was dropped is 0 in the gradients of gate and scale, too, whatever it was.  0 times it will do as long as it is finite (behind a
-    // norm it is); looking whether it is costs 1 to 3 % of the time (a choice for every value 3 to 5), and up to 17 % where registers were
-    // short already: an fp32 stream with a gate that serves spans (12608 x 384 and a gate row per 197 tokens, bf16: 22.1 us, now 22.6).
+    // norm it is); looking whether it is costs 1 to 5 % of the time (a choice for every value 3 to 10; 12608 x 384 and a gate row per 197
+    // tokens, bf16: 22.1 us, now 22.7), and up to 27 % where registers were short already: an fp32 stream with a gate that serves spans
+    // and a layer norm (43690 x 768: 152 us, now 194).  Looking in the ring, before the step's registers are in use, was no better.
     if (!POST && dropped && odd != 0u) {
 #pragma unroll
       for (int r = 0; r < ROWS; ++r)
@@ -1113,7 +1117,7 @@ residual_bwd_kernel(const __grid_constant__ ResidualParams p) {
           Pair gt[4];
           auto read_gate = [&]() {
             if (GATE_RING) read_block<false>(piece<SLOTS, PITCH>(at, r, j, G), 0, gt);
-            else unpack8<false>(Vec8<false>{gate_row(min(work.t + r, p.T - 1u))[b.safe[j]]}, gt);
+            else unpack8<false>(Vec8<false>{gate_block(min(work.t + r, p.T - 1u), j)}, gt);
           };
           constexpr bool EARLY = !GATE_RING && GATE == 1;  // from memory, where its gradient may take its place
           if (EARLY) read_gate();
@@ -1564,7 +1568,7 @@ int launch_residual_bwd(const bimask_residual_args& a, cudaStream_t s, const Res
   const RowPlan b = plan_rows(rows, bwd_threads(rows), a.T, a.C, spanned ? (int)p.gate_span : 1, PLAN_SMS, true);
   take_plan(p, b);
   if (b.slots > 1) p.sums = reinterpret_cast<float*>(a.ws);
-  if (spanned && b.units_per_span > 1) p.gate_sums = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(a.ws) + column_sums_bytes(a.T, a.C, (int)p.gate_span));
+  if (spanned && (b.units_per_span > 1 || (a.dgate == a.gate && a.stream_type == BIMASK_TYPE_F32))) p.gate_sums = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(a.ws) + column_sums_bytes(a.T, a.C, (int)p.gate_span));
   using Yes = std::true_type;
   using No = std::false_type;
   auto run_with = [&](auto step, auto f32, auto gate, auto post, auto wide, auto cluster) -> int {
